@@ -2,10 +2,11 @@
 
     python -m paper_2407_04480_b200.build [--force] [--verbose]
 
-Produces paper_2407_04480_b200/libloco_b200.so next to this file.  nvcc cross-compiles
-without a GPU, so this runs anywhere the CUDA toolkit is installed.  The kernel templates are
-instantiated in several object files (see csrc/loco_dispatch.h) that are compiled in parallel
-and linked into the one shared library; the objects live in a temporary directory.
+Produces paper_2407_04480_b200/libloco_b200.so and libloco_layer_b200.so (the operators of a
+decoder layer, include/loco_layer.h) next to this file.  nvcc cross-compiles without a GPU, so
+this runs anywhere the CUDA toolkit is installed.  The kernel templates are instantiated in
+several object files (see csrc/loco_dispatch.h) that are compiled in parallel and linked into
+one shared library each; the objects live in a temporary directory.
 """
 from __future__ import annotations
 
@@ -21,6 +22,10 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libloco_b200.so")
 DEPS = [os.path.join(CSRC, f) for f in ("loco_api.cu", "loco_send_tu.cu", "loco_reduce_tu.cu", "loco_kernels.cuh",
                                         "loco_dispatch.h")] + [os.path.join(os.path.dirname(HERE), "include", "loco.h")]
+LAYER_LIB = os.path.join(HERE, "libloco_layer_b200.so")
+LAYER_SOURCES = ("layer_rotary.cu", "layer_router.cu", "layer_attention.cu", "layer_attention_api.cu")
+LAYER_DEPS = [os.path.join(CSRC, f) for f in LAYER_SOURCES + ("layer_common.h", "layer_attention.h")] + [
+    os.path.join(os.path.dirname(HERE), "include", f) for f in ("loco.h", "loco_layer.h")]
 
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC"]
@@ -45,15 +50,21 @@ def nvcc_path() -> str:
     return p
 
 
-def stale() -> bool:
-    if not os.path.exists(LIB):
+def stale(lib: str = LIB, deps=DEPS) -> bool:
+    if not os.path.exists(lib):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(d) > t for d in DEPS)
+    t = os.path.getmtime(lib)
+    return any(os.path.getmtime(d) > t for d in deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not stale():
+    """Build what is out of date (everything with `force`); returns the path of libloco_b200.so."""
+    wanted = []                                          # (library, its units)
+    if force or stale():
+        wanted.append((LIB, units()))
+    if force or stale(LAYER_LIB, LAYER_DEPS):
+        wanted.append((LAYER_LIB, [(s[:-3], s, []) for s in LAYER_SOURCES]))
+    if not wanted:
         return LIB
     nvcc = nvcc_path()
     extra = ["-Xptxas", "-v"] if verbose else []
@@ -65,11 +76,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
             return obj
 
         with ThreadPoolExecutor(max_workers=max(1, os.cpu_count() or 1)) as ex:
-            objs = list(ex.map(compile_one, units()))
-        tmp = LIB + ".tmp.%d" % os.getpid()
-        subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static",
-                               "-Xcompiler", "-fPIC", "-o", tmp, *objs])
-        os.replace(tmp, LIB)
+            jobs = [(lib, [ex.submit(compile_one, u) for u in us]) for lib, us in wanted]
+            for lib, futures in jobs:
+                objs = [f.result() for f in futures]
+                tmp = lib + ".tmp.%d" % os.getpid()
+                subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static",
+                                       "-Xcompiler", "-fPIC", "-o", tmp, *objs])
+                os.replace(tmp, lib)
     return LIB
 
 
