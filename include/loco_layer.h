@@ -161,6 +161,14 @@ int loco_router_backward(const loco_router_t *cfg, int64_t tokens, const void *d
                          const uint8_t *d_mask, const int32_t *d_index, const int32_t *d_counts, const float *d_dlosses,
                          const float *d_dweight, void *d_dlogits, int64_t drow_stride, void *stream);
 
+/*
+ * Flags raised on the current device since the library was loaded; SYNCHRONISES `stream`.  The attention kernels wait on
+ * their own copies and products, never on another block; a wait that exceeds two seconds gives up, the block leaves its
+ * outputs unwritten and the flag is raised.
+ */
+#define LOCO_LAYER_FLAG_TIMEOUT 1u
+int loco_layer_status(uint32_t *flags, void *stream);
+
 /* Number of kernels launched by the functions of this header in the calling process. */
 uint64_t loco_layer_launch_count(void);
 

@@ -24,7 +24,7 @@ DEPS = [os.path.join(CSRC, f) for f in ("loco_api.cu", "loco_send_tu.cu", "loco_
                                         "loco_dispatch.h")] + [os.path.join(os.path.dirname(HERE), "include", "loco.h")]
 LAYER_LIB = os.path.join(HERE, "libloco_layer_b200.so")
 LAYER_SOURCES = ("layer_rotary.cu", "layer_router.cu", "layer_attention.cu", "layer_attention_api.cu")
-LAYER_DEPS = [os.path.join(CSRC, f) for f in LAYER_SOURCES + ("layer_common.h", "layer_attention.h")] + [
+LAYER_DEPS = [os.path.join(CSRC, f) for f in LAYER_SOURCES + ("layer_common.h", "layer_attention.h", "layer_tc.cuh")] + [
     os.path.join(os.path.dirname(HERE), "include", f) for f in ("loco.h", "loco_layer.h")]
 
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",

@@ -1,156 +1,885 @@
-// Attention, one warp per row: every sum in fp32, four dimensions of the head per lane.
+// Attention on the tensor cores: tiles of 128 queries and 128 keys, products accumulated in tensor memory (TMEM).
+//
+// All three kernels have the same parts.  One warp copies tiles to shared memory (TMA, 128-byte swizzle), one thread issues
+// the products, two groups of four warps turn scores into probabilities (a thread per TMEM lane, i.e. per row), and one warp
+// zeroes what a copy brought in from past the end of a sample, so that whatever lies there (NaN included) meets a zero
+// probability as a zero.  Probabilities go back to TMEM as bfloat16 over the scores they came from and are the first operand
+// of the second product from there: they never pass through shared memory.
+//
+//   forward           two tiles of 128 queries stay, keys and values stream; one warp group per query tile, so that one
+//                     group's exponentials run under the other tile's products.  The running maximum is moved (and o
+//                     rescaled) only when it grows by more than 2^8: until then exp2 stays inside the range of fp32 and
+//                     bfloat16, and the final division by the sum takes the common factor out exactly.
+//   backward queries  128 queries stay, keys and values stream: S, dP, then dq += dS K.  It also leaves D = do . o.
+//   backward keys     128 keys and values stay, the queries of all heads that share them stream: the transposed scores,
+//                     so that P^T and dS^T have the keys as rows: dv += P^T dO, dk += dS^T Q.  A shared head's gradient is
+//                     summed in its accumulator, and no output needs an atomic: the price is seven products instead
+//                     of the five that a single kernel with atomic dq would need.
+#include <cuda.h>
+
+#include <cstring>
+#include <mutex>
+
 #include "layer_attention.h"
+#include "layer_tc.cuh"
 
 namespace loco_layer {
 
-constexpr int kAttnWarps = 8;
+using namespace tc;
 
-__device__ __forceinline__ float warp_total(float x) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
+constexpr int kTile = 128;                       // queries and keys of a tile
+constexpr int kGroupWarps = 4;                   // warps of a softmax group: the 128 lanes of TMEM
+constexpr int kThreads = (2 * kGroupWarps + 3) * 32;
+constexpr int kLoadWarp = 2 * kGroupWarps, kProductWarp = kLoadWarp + 1, kHelpWarp = kLoadWarp + 2;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ unsigned g_status;                    // LOCO_LAYER_FLAG_*
+
+struct Maps { CUtensorMap q, k, v, d_o; };
+
+// Shared memory: two tiles that stay, the ring of tiles that stream, then Shared.  Either head size fills the SM, so that no
+// two blocks compete for its tensor memory.
+template <int kDim> __host__ __device__ constexpr int tile_bytes() { return kTile * kDim * 2; }
+template <int kDim> __host__ __device__ constexpr int stream_slots() { return kDim == 128 ? 4 : 8; }
+constexpr int kMaxSlots = 8;
+struct Shared {
+    uint64_t full[kMaxSlots], empty[kMaxSlots];  // streaming tiles: copied, no longer read
+    uint64_t stay;                               // the tiles that stay are copied
+    uint64_t score[2], second[2];                // products ready: S per tile or buffer; o (forward) or dP (backward)
+    uint64_t prob[2], grad;                      // P, dS written to TMEM
+    uint64_t last, clean;                        // a tile with rows past the end is copied; those rows are zero
+    uint64_t stats[2], stats_free[2];            // backward keys: row statistics of a query tile
+    uint64_t done, drain;
+    uint32_t tmem, failed;
+    alignas(16) float row[2][2][kTile];          // backward keys: lse * log2(e), D of the query tile; backward queries: D
+};
+template <int kDim> constexpr int shared_bytes() {
+    return (2 + stream_slots<kDim>()) * tile_bytes<kDim>() + static_cast<int>(sizeof(Shared)) + 1024;
 }
 
-struct Four { float v[4]; };
-__device__ __forceinline__ Four load4(const __nv_bfloat16 *row, int lane, int d) {
-    Four f{{0.0f, 0.0f, 0.0f, 0.0f}};
-    if (lane * 4 < d) {
-        const Pack<__nv_bfloat16, 4> p = *reinterpret_cast<const Pack<__nv_bfloat16, 4> *>(row + lane * 4);
+template <int kDim> __device__ __forceinline__ void load_tile(uint32_t to, const CUtensorMap *map, int row, int head, int batch, uint32_t bar) {
+    bar_expect(bar, tile_bytes<kDim>());
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f.v[i] = __bfloat162float(p.v[i]);
+    for (int x = 0; x < kDim; x += 64) load_box(to + x / 64 * (kTile * 128), map, x, row, head, batch, bar);
+}
+
+// Zero the rows from `first` on of a tile, by one warp.
+template <int kDim> __device__ __forceinline__ void clean_tile(uint8_t *tile, int first, int lane) {
+    for (int x = 0; x < kDim; x += 64)
+        for (int i = first * 8 + lane; i < kTile * 8; i += 32)
+            reinterpret_cast<uint4 *>(tile + x / 64 * (kTile * 128))[i] = make_uint4(0, 0, 0, 0);
+}
+
+// S (128 x 128) = A B^T over kDim columns, both tiles in shared memory.
+template <int kDim> __device__ __forceinline__ void product_scores(uint32_t d, uint32_t a, uint32_t b, uint32_t word) {
+#pragma unroll
+    for (int x = 0; x < kDim; x += 16) {
+        const uint32_t off = x / 64 * (kTile * 128) + x % 64 * 2;
+        mma_ss(d, desc_along_columns(a + off), desc_along_columns(b + off), word, x > 0);
+    }
+}
+// d (128 x kDim) += A B: A (128 x 128) in TMEM, its columns at `a0` (first 64) and `a1`; B's rows are the tile's.
+template <int kDim> __device__ __forceinline__ void product_apply(uint32_t d, uint32_t a0, uint32_t a1, uint32_t b, uint32_t accumulate) {
+    constexpr uint32_t word = product(kDim, true);
+#pragma unroll
+    for (int r = 0; r < kTile; r += 16)
+        mma_ts(d, (r < 64 ? a0 : a1) + r % 64 / 2, desc_along_rows(b + r * 128, kTile * 128), word, accumulate | (r > 0));
+}
+
+// Sets up barriers and TMEM; returns the TMEM base.
+template <int kColumns> __device__ __forceinline__ uint32_t begin_block(Shared &S, int slots, int last_arrivals, int prob_arrivals) {
+    const int warp = threadIdx.x / 32;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < slots; ++i) {
+            bar_init(smem_addr(&S.full[i]), 1);
+            bar_init(smem_addr(&S.empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_addr(&S.score[i]), 1);
+            bar_init(smem_addr(&S.second[i]), 1);
+            bar_init(smem_addr(&S.prob[i]), prob_arrivals);
+            bar_init(smem_addr(&S.stats[i]), 1);
+            bar_init(smem_addr(&S.stats_free[i]), 2 * kGroupWarps);
+        }
+        bar_init(smem_addr(&S.grad), 2 * kGroupWarps);
+        bar_init(smem_addr(&S.stay), 1);
+        bar_init(smem_addr(&S.last), last_arrivals);
+        bar_init(smem_addr(&S.clean), 1);
+        bar_init(smem_addr(&S.done), 1);
+        bar_init(smem_addr(&S.drain), 1);
+        S.failed = 0;
+        fence_bar_init();
+        fence_async_shared();
+    }
+    if (warp == kProductWarp) tmem_alloc<kColumns>(smem_addr(&S.tmem));
+    fence_before();
+    __syncthreads();
+    fence_after();
+    return S.tmem;
+}
+template <int kColumns> __device__ __forceinline__ void end_block(Shared &S, uint32_t tmem) {
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (threadIdx.x / 32 == kProductWarp) tmem_free<kColumns>(tmem);
+    if (threadIdx.x == 0 && S.failed) atomicOr(&g_status, LOCO_LAYER_FLAG_TIMEOUT);
+}
+
+// A role that gave up still waits for the copies it started before the block's shared memory goes away.
+__device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
+    const uint64_t begin = now_ns();
+    while (!bar_test(bar, parity) && now_ns() - begin < kWaitLimitNs) {}
+}
+
+// Ring of streaming tiles, seen by the thread that fills it and the one that empties it.
+struct Ring {
+    uint32_t slot = 0, phase = 0;
+    template <int kSlots> __device__ __forceinline__ void next() {
+        if (++slot == kSlots) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+template <int kDim> __device__ __forceinline__ void store_row(__nv_bfloat16 *to, const uint32_t (&r)[32], int first, int dim, float by) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+        if (first + i < dim) {                   // dim is a multiple of 8
+            uint4 w;
+            w.x = pack_bf16(__uint_as_float(r[i]) * by, __uint_as_float(r[i + 1]) * by);
+            w.y = pack_bf16(__uint_as_float(r[i + 2]) * by, __uint_as_float(r[i + 3]) * by);
+            w.z = pack_bf16(__uint_as_float(r[i + 4]) * by, __uint_as_float(r[i + 5]) * by);
+            w.w = pack_bf16(__uint_as_float(r[i + 6]) * by, __uint_as_float(r[i + 7]) * by);
+            *reinterpret_cast<uint4 *>(to + first + i) = w;
+        }
+    }
+}
+__device__ __forceinline__ void zero_row(__nv_bfloat16 *to, int from, int until) {
+    for (int i = from; i < until; i += 8) *reinterpret_cast<uint4 *>(to + i) = make_uint4(0, 0, 0, 0);
+}
+
+// Whether a streamed tile that holds the last of n rows also holds rows past them that are not the copy's zero fill.
+__device__ __forceinline__ bool ends_inside(const Rows &r, int packed, int seq) { return r.n % kTile != 0 && (packed || r.n != seq); }
+
+// The block's place: tiles are the slow index, so that blocks of one wave share keys; `reverse` starts with the last tile,
+// which under a causal mask is the longest for queries.
+struct BlockPlace { int tile, head, batch; };
+__device__ __forceinline__ BlockPlace block_place(int heads, int batch, int tiles, bool reverse) {
+    const int hb = heads * batch;
+    const int t = static_cast<int>(blockIdx.x) / hb, r = static_cast<int>(blockIdx.x) - t * hb;
+    return BlockPlace{reverse ? tiles - 1 - t : t, r % heads, r / heads};
+}
+
+// Keys that query i sees: [0, limit).
+__device__ __forceinline__ int key_limit(const Rows &Q, const Rows &K, int causal, int i) {
+    if (i >= Q.n) return 0;
+    return causal ? max(0, min(K.n, i + K.n - Q.n + 1)) : K.n;
+}
+// Key tiles that the queries [first, first + 128) need.
+__device__ __forceinline__ int key_tiles(const Rows &Q, const Rows &K, int causal, int first) {
+    if (first >= Q.n) return 0;
+    return (key_limit(Q, K, causal, min(first + kTile, Q.n) - 1) + kTile - 1) / kTile;
+}
+
+// ------------------------------------------------------------------------------------------------ forward
+
+template <int kDim>
+__global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
+    constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
+    extern __shared__ uint8_t raw[];
+    uint8_t *const tiles = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+    Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
+    const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.causal);
+    const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
+    const int first = at.tile * 2 * kTile, head_kv = at.head / P.group;
+    if (P.packed && first >= Q.n) return;
+    const int n0 = key_tiles(Q, K, P.causal, first), n1 = key_tiles(Q, K, P.causal, first + kTile), n = max(n0, n1);
+    const bool ragged = ends_inside(K, P.packed, P.seq_k) && n == K.n / kTile + 1;
+    const uint32_t tmem = begin_block<512>(S, kSlots, 1, kGroupWarps);
+    volatile uint32_t *const failed = &S.failed;
+
+    if (warp == kLoadWarp && lane == 0 && n > 0) {
+        Ring r;
+        bar_expect(smem_addr(&S.stay), (n0 > 0 ? kBytes : 0) + (n1 > 0 ? kBytes : 0));
+        for (int t = 0; t < 2; ++t)
+            if ((t ? n1 : n0) > 0)
+#pragma unroll
+                for (int x = 0; x < kDim; x += 64)
+                    load_box(base + t * kBytes + x / 64 * (kTile * 128), &M.q, x, Q.first + first + t * kTile, at.head, Q.at, smem_addr(&S.stay));
+        int sent = 0;
+        for (int j = 0; j < 2 * n; ++j) {
+            if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+            load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
+                            smem_addr(ragged && j >= 2 * n - 1 ? &S.last : &S.full[r.slot]));
+            ++sent;
+            r.next<kSlots>();
+        }
+        if (*failed) {
+            settle(smem_addr(&S.stay), 0);
+            for (int j = max(0, sent - kSlots); j < sent; ++j)
+                if (ragged && j >= 2 * n - 1) settle(smem_addr(&S.last), 0);
+                else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
+        }
+    } else if (warp == kProductWarp && lane == 0 && n > 0) {
+        const uint32_t scores = product(kTile, false, P.scale < 0.0f);
+        bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && bar_wait(smem_addr(&S.full[0]), 0, failed);
+        if (ok) {
+            for (int t = 0; t < 2; ++t)
+                if ((t ? n1 : n0) > 0) {
+                    product_scores<kDim>(tmem + t * kTile, base + t * kBytes, ring, scores);
+                    commit(smem_addr(&S.score[t]));
+                }
+            commit(smem_addr(&S.empty[0]));
+        }
+        Ring v, k;                               // value tiles at odd places of the ring, key tiles at even ones
+        v.next<kSlots>();
+        k.next<kSlots>();
+        k.next<kSlots>();
+        for (int j = 0; ok && j < n; ++j) {
+            ok = (ragged && j == n - 1 ? bar_wait(smem_addr(&S.clean), 0, failed) : bar_wait(smem_addr(&S.full[v.slot]), v.phase, failed)) &&
+                 (j + 1 == n || bar_wait(smem_addr(&S.full[k.slot]), k.phase, failed));
+            for (int t = 0; ok && t < 2; ++t) {
+                const int nt = t ? n1 : n0;
+                if (j >= nt) continue;
+                ok = bar_wait(smem_addr(&S.prob[t]), j & 1, failed);
+                if (!ok) break;
+                fence_after();
+                const uint32_t p = tmem + t * kTile;
+                product_apply<kDim>(tmem + 2 * kTile + t * kTile, p, p + 32, ring + v.slot * kBytes, j > 0);
+                commit(smem_addr(&S.second[t]));
+                if (j + 1 < nt) {
+                    product_scores<kDim>(p, base + t * kBytes, ring + k.slot * kBytes, scores);
+                    commit(smem_addr(&S.score[t]));
+                }
+            }
+            if (!ok) break;
+            commit(smem_addr(&S.empty[v.slot]));
+            if (j + 1 < n) commit(smem_addr(&S.empty[k.slot]));
+            for (int i = 0; i < 2; ++i) {
+                v.next<kSlots>();
+                k.next<kSlots>();
+            }
+        }
+        commit(smem_addr(&S.drain));
+        settle(smem_addr(&S.drain), 0);
+    } else if (warp == kHelpWarp && ragged) {
+        const int load = 2 * n - 1;              // the last value tile
+        if (bar_wait(smem_addr(&S.last), 0, failed)) {
+            clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.clean));
+        }
+    } else if (warp < 2 * kGroupWarps) {
+        const int t = warp / kGroupWarps, i = first + t * kTile + threadIdx.x % kTile;
+        const int nt = t ? n1 : n0, limit = key_limit(Q, K, P.causal, i);
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % kGroupWarps * 32) << 16);
+        const uint32_t s_at = lanes + t * kTile, o_at = lanes + 2 * kTile + t * kTile;
+        const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
+        const float room = 8.0f / scale;         // how far the maximum may grow before o is rescaled
+        float top = -INFINITY, total = 0.0f;
+        bool ok = true;
+        for (int j = 0; ok && j < nt; ++j) {
+            ok = bar_wait(smem_addr(&S.score[t]), j & 1, failed);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            fence_after();
+            uint32_t s[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) load_columns(s_at + c * 32, s[c]);
+            wait_loads();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) pin(s[c]);
+            const int left = limit - j * kTile;  // columns from here on are not seen
+            if (__any_sync(0xffffffffu, left < kTile)) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int x = 0; x < 32; ++x)
+                        if (c * 32 + x >= left) s[c][x] = 0xff800000u;
+            }
+            float m[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                m[c] = __uint_as_float(s[c][0]);
+#pragma unroll
+                for (int x = 1; x < 32; ++x) m[c] = fmaxf(m[c], __uint_as_float(s[c][x]));
+            }
+            const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            if (j == 0) {
+                top = most;
+            } else if (__any_sync(0xffffffffu, most - top > room)) {
+                const float next = fmaxf(top, most);
+                const float fade = next == -INFINITY ? 1.0f : exp2_fast((top - next) * scale);
+                ok = bar_wait(smem_addr(&S.second[t]), (j - 1) & 1, failed);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                fence_after();
+#pragma unroll
+                for (int c = 0; c < kDim / 32; ++c) {
+                    uint32_t o[32];
+                    load_columns(o_at + c * 32, o);
+                    wait_loads();
+                    pin(o);
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * fade);
+                    store_columns(o_at + c * 32, o);
+                }
+                total *= fade;
+                top = next;
+            }
+            const float shift = top == -INFINITY ? 0.0f : top * scale;
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t p[16];
+#pragma unroll
+                for (int x = 0; x < 32; x += 2) {
+                    const float a = exp2_fast(fmaf(__uint_as_float(s[c][x]), scale, -shift));
+                    const float b = exp2_fast(fmaf(__uint_as_float(s[c][x + 1]), scale, -shift));
+                    sum[x / 2 % 4] += a + b;
+                    p[x / 2] = pack_bf16(a, b);
+                }
+                store_columns(s_at + c * 16, p);
+            }
+            total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            wait_stores();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.prob[t]));
+        }
+        if (ok && nt > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&S.second[t]), (nt - 1) & 1, failed));
+        if (ok) {
+            const bool wanted = i < (P.packed ? Q.n : P.seq_q);
+            const float by = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+            __nv_bfloat16 *o = row_of(P.o, Q, i, at.head);
+            if (nt > 0) {
+                fence_after();
+#pragma unroll
+                for (int c = 0; c < kDim / 32; ++c) {
+                    uint32_t r[32];
+                    load_columns(o_at + c * 32, r);
+                    wait_loads();
+                    pin(r);
+                    if (wanted && limit > 0) store_row<kDim>(o, r, c * 32, P.head_dim, by);
+                }
+            }
+            if (wanted) {
+                if (limit == 0) zero_row(o, 0, P.head_dim);
+                P.lse[stat_at(P, Q, i, at.head)] = limit > 0 ? (top * scale + log2f(total)) * kLn2 : -INFINITY;
+            }
+        }
+    }
+    __syncwarp();
+    end_block<512>(S, tmem);
+}
+
+// ------------------------------------------------------------------------------------------------ backward: queries
+
+// TMEM: S (two buffers), dP, dq.  dS goes over its S: columns 0-31 from the first warp group, 64-95 from the second.
+template <int kDim>
+__global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
+    constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
+    extern __shared__ uint8_t raw[];
+    uint8_t *const tiles = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+    Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
+    const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + kTile - 1) / kTile, P.causal);
+    const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
+    const int first = at.tile * kTile, head_kv = at.head / P.group;
+    if (P.packed && first >= Q.n) return;
+    const int n = key_tiles(Q, K, P.causal, first);
+    const bool ragged = ends_inside(K, P.packed, P.seq_k) && n == K.n / kTile + 1;
+    const uint32_t tmem = begin_block<512>(S, kSlots, 2, 2 * kGroupWarps);
+    const uint32_t dp_at = tmem + 2 * kTile, dq_at = tmem + 3 * kTile;
+    volatile uint32_t *const failed = &S.failed;
+
+    if (warp == kLoadWarp && lane == 0 && n > 0) {
+        Ring r;
+        bar_expect(smem_addr(&S.stay), 2 * kBytes);
+#pragma unroll
+        for (int x = 0; x < kDim; x += 64) {
+            load_box(base + x / 64 * (kTile * 128), &M.q, x, Q.first + first, at.head, Q.at, smem_addr(&S.stay));
+            load_box(base + kBytes + x / 64 * (kTile * 128), &M.d_o, x, Q.first + first, at.head, Q.at, smem_addr(&S.stay));
+        }
+        int sent = 0;
+        for (int j = 0; j < 2 * n; ++j) {
+            if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+            load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
+                            smem_addr(ragged && j >= 2 * n - 2 ? &S.last : &S.full[r.slot]));
+            ++sent;
+            r.next<kSlots>();
+        }
+        if (*failed) {
+            settle(smem_addr(&S.stay), 0);
+            for (int j = max(0, sent - kSlots); j < sent; ++j)
+                if (ragged && j >= 2 * n - 2) settle(smem_addr(&S.last), 0);
+                else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
+        }
+    } else if (warp == kProductWarp && lane == 0 && n > 0) {
+        const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
+        // tile j: keys at place 2j of the ring, values at 2j + 1
+        const auto slot = [](int load) { return load % kSlots; };
+        const auto ready = [&](int load) {
+            return ragged && load >= 2 * n - 2 ? bar_wait(smem_addr(&S.clean), 0, failed)
+                                               : bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
+        };
+        bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && ready(0) && ready(1);
+        if (ok) {
+            product_scores<kDim>(tmem, base, ring, scores);
+            commit(smem_addr(&S.score[0]));
+            product_scores<kDim>(dp_at, base + kBytes, ring + kBytes, plain);
+            commit(smem_addr(&S.second[0]));
+            commit(smem_addr(&S.empty[1]));
+        }
+        for (int j = 0; ok && j < n; ++j) {
+            if (j + 1 < n) {
+                ok = ready(2 * j + 2);
+                if (!ok) break;
+                product_scores<kDim>(tmem + (j + 1) % 2 * kTile, base, ring + slot(2 * j + 2) * kBytes, scores);
+                commit(smem_addr(&S.score[(j + 1) % 2]));
+            }
+            ok = bar_wait(smem_addr(&S.grad), j & 1, failed) && (j + 1 == n || ready(2 * j + 3));
+            if (!ok) break;
+            fence_after();
+            if (j + 1 < n) {
+                product_scores<kDim>(dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+                commit(smem_addr(&S.second[0]));
+                commit(smem_addr(&S.empty[slot(2 * j + 3)]));
+            }
+            const uint32_t ds = tmem + j % 2 * kTile;
+            product_apply<kDim>(dq_at, ds, ds + 64, ring + slot(2 * j) * kBytes, j > 0);
+            commit(smem_addr(&S.empty[slot(2 * j)]));
+        }
+        if (ok) commit(smem_addr(&S.done));
+        commit(smem_addr(&S.drain));
+        settle(smem_addr(&S.drain), 0);
+    } else if (warp == kHelpWarp && ragged) {
+        if (bar_wait(smem_addr(&S.last), 0, failed)) {
+            for (int load = 2 * n - 2; load < 2 * n; ++load) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.clean));
+        }
+    } else if (warp < 2 * kGroupWarps) {
+        const int t = warp / kGroupWarps, row = threadIdx.x % kTile, i = first + row;
+        const int limit = key_limit(Q, K, P.causal, i);
+        const uint32_t lanes = static_cast<uint32_t>(warp % kGroupWarps * 32) << 16;
+        const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
+        const bool wanted = i < (P.packed ? Q.n : P.seq_q);
+        // D: each group takes half of the row
+        float dot = 0.0f;
+        if (limit > 0) {
+            const __nv_bfloat16 *o = row_of(P.o, Q, i, at.head), *g = row_of(P.d_o, Q, i, at.head);
+            for (int x = t * (kDim / 2); x < min((t + 1) * (kDim / 2), P.head_dim); x += 8) {
+                const Pack<__nv_bfloat16, 8> a = *reinterpret_cast<const Pack<__nv_bfloat16, 8> *>(o + x);
+                const Pack<__nv_bfloat16, 8> b = *reinterpret_cast<const Pack<__nv_bfloat16, 8> *>(g + x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dot = fmaf(__bfloat162float(a.v[e]), __bfloat162float(b.v[e]), dot);
+            }
+        }
+        S.row[t][0][row] = dot;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        dot = S.row[0][0][row] + S.row[1][0][row];
+        float shift = INFINITY;                  // a row that sees nothing has p = exp2(-inf) = 0
+        if (limit > 0) {
+            shift = P.lse[stat_at(P, Q, i, at.head)] * kLog2e;
+            if (shift == -INFINITY) shift = INFINITY;
+        }
+        if (t == 0 && wanted) P.row_dot[stat_at(P, Q, i, at.head)] = dot;
+        bool ok = true;
+        for (int j = 0; ok && j < n; ++j) {
+            const uint32_t s_at = tmem + lanes + j % 2 * kTile + t * 64;
+            ok = bar_wait(smem_addr(&S.score[j % 2]), j / 2 & 1, failed);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            fence_after();
+            uint32_t s[2][32], d[2][32];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) load_columns(s_at + c * 32, s[c]);
+            wait_loads();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) pin(s[c]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int x = 0; x < 32; ++x) s[c][x] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x]), scale, -shift)));
+            const int left = limit - j * kTile - t * 64;
+            if (__any_sync(0xffffffffu, left < 64)) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int x = 0; x < 32; ++x)
+                        if (c * 32 + x >= left) s[c][x] = 0;
+            }
+            ok = bar_wait(smem_addr(&S.second[0]), j & 1, failed);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            fence_after();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) load_columns(dp_at + lanes + t * 64 + c * 32, d[c]);
+            wait_loads();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) pin(d[c]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t w[16];
+#pragma unroll
+                for (int x = 0; x < 32; x += 2)
+                    w[x / 2] = pack_bf16(__uint_as_float(s[c][x]) * (__uint_as_float(d[c][x]) - dot),
+                                         __uint_as_float(s[c][x + 1]) * (__uint_as_float(d[c][x + 1]) - dot));
+                store_columns(s_at + c * 16, w);
+            }
+            wait_stores();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.grad));
+        }
+        if (ok && n > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&S.done), 0, failed));
+        if (ok) {
+            __nv_bfloat16 *dq = row_of(P.dq, Q, i, at.head);
+            if (n > 0) {
+                fence_after();
+#pragma unroll
+                for (int c = t * (kDim / 64); c < (t + 1) * (kDim / 64); ++c) {
+                    uint32_t r[32];
+                    load_columns(dq_at + lanes + c * 32, r);
+                    wait_loads();
+                    pin(r);
+                    if (wanted && limit > 0) store_row<kDim>(dq, r, c * 32, P.head_dim, P.scale);
+                }
+            }
+            if (wanted && limit == 0) zero_row(dq, t * (kDim / 2), min((t + 1) * (kDim / 2), P.head_dim));
+        }
+    }
+    __syncwarp();
+    end_block<512>(S, tmem);
+}
+
+// ------------------------------------------------------------------------------------------------ backward: keys
+
+// TMEM: S^T, dP^T, dv, dk; P^T goes over S^T and dS^T over dP^T.
+template <int kDim>
+__global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
+    constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
+    extern __shared__ uint8_t raw[];
+    uint8_t *const tiles = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+    Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
+    const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const BlockPlace at = block_place(P.heads_kv, P.batch, (P.max_k + kTile - 1) / kTile, false);
+    const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
+    const int first = at.tile * kTile;
+    if (P.packed && first >= K.n) return;
+    // query tiles [from, until) see this tile; the heads of the group one after the other
+    const int off = K.n - Q.n;
+    const int until = (Q.n + kTile - 1) / kTile, from = P.causal ? min(until, max(0, first - off) / kTile) : 0;
+    const int per = first < K.n ? until - from : 0, n = per * P.group;
+    const bool ragged = ends_inside(Q, P.packed, P.seq_q);
+    const uint32_t tmem = begin_block<512>(S, kSlots, 1, 2 * kGroupWarps);
+    const uint32_t s_at = tmem, dp_at = tmem + kTile, dv_at = tmem + 2 * kTile, dk_at = tmem + 3 * kTile;
+    volatile uint32_t *const failed = &S.failed;
+
+    if (warp == kLoadWarp && lane == 0 && n > 0) {
+        Ring r;
+        bar_expect(smem_addr(&S.stay), 2 * kBytes);
+#pragma unroll
+        for (int x = 0; x < kDim; x += 64) {
+            load_box(base + x / 64 * (kTile * 128), &M.k, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
+            load_box(base + kBytes + x / 64 * (kTile * 128), &M.v, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
+        }
+        int sent = 0;
+        for (int j = 0; j < 2 * n; ++j) {
+            if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+            const int g = j / 2 / per, tile = from + j / 2 - g * per;
+            load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.d_o : &M.q, Q.first + tile * kTile, at.head * P.group + g, Q.at, smem_addr(&S.full[r.slot]));
+            ++sent;
+            r.next<kSlots>();
+        }
+        if (*failed) {
+            settle(smem_addr(&S.stay), 0);
+            for (int j = max(0, sent - kSlots); j < sent; ++j) settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
+        }
+    } else if (warp == kProductWarp && lane == 0 && n > 0) {
+        const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
+        const auto slot = [](int load) { return load % kSlots; };
+        const auto ready = [&](int load) { return bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed); };
+        const auto whole = [&](int j) { return bar_wait(smem_addr(&S.stats[j % 2]), j / 2 & 1, failed); };
+        bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && ready(0) && ready(1) && whole(0);
+        if (ok) {
+            product_scores<kDim>(s_at, base, ring, scores);
+            commit(smem_addr(&S.score[0]));
+            product_scores<kDim>(dp_at, base + kBytes, ring + kBytes, plain);
+            commit(smem_addr(&S.second[0]));
+        }
+        for (int j = 0; ok && j < n; ++j) {
+            ok = bar_wait(smem_addr(&S.prob[0]), j & 1, failed) && (j + 1 == n || (ready(2 * j + 2) && whole(j + 1)));
+            if (!ok) break;
+            fence_after();
+            product_apply<kDim>(dv_at, s_at, s_at + 64, ring + slot(2 * j + 1) * kBytes, j > 0);
+            commit(smem_addr(&S.empty[slot(2 * j + 1)]));
+            if (j + 1 < n) {
+                product_scores<kDim>(s_at, base, ring + slot(2 * j + 2) * kBytes, scores);
+                commit(smem_addr(&S.score[0]));
+            }
+            ok = bar_wait(smem_addr(&S.grad), j & 1, failed) && (j + 1 == n || ready(2 * j + 3));
+            if (!ok) break;
+            fence_after();
+            product_apply<kDim>(dk_at, dp_at, dp_at + 64, ring + slot(2 * j) * kBytes, j > 0);
+            commit(smem_addr(&S.empty[slot(2 * j)]));
+            if (j + 1 < n) {
+                product_scores<kDim>(dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+                commit(smem_addr(&S.second[0]));
+            }
+        }
+        if (ok) commit(smem_addr(&S.done));
+        commit(smem_addr(&S.drain));
+        settle(smem_addr(&S.drain), 0);
+    } else if (warp == kHelpWarp) {
+        // row statistics of each query tile, and zeros past the sample's end in the tile that holds it
+        for (int j = 0; j < n; ++j) {
+            const int g = j / per, tile = from + j - g * per, b = j % 2;
+            float l[4], d[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int i = tile * kTile + x * 32 + lane;
+                l[x] = INFINITY;                 // no such query, or one that sees nothing: p = exp2(-inf) = 0
+                d[x] = 0.0f;
+                if (i < Q.n) {
+                    const int64_t s = stat_at(P, Q, i, at.head * P.group + g);
+                    l[x] = P.lse[s] * kLog2e;
+                    d[x] = P.row_dot[s];
+                    if (l[x] == -INFINITY) l[x] = INFINITY;
+                }
+            }
+            bool ok = bar_wait(smem_addr(&S.stats_free[b]), (j / 2 & 1) ^ 1, failed);
+            if (ragged && tile == until - 1)
+                for (int load = 2 * j; ok && load < 2 * j + 2; ++load) {
+                    ok = bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
+                    if (ok) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, Q.n % kTile, lane);
+                }
+            if (!__all_sync(0xffffffffu, ok)) break;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                S.row[b][0][x * 32 + lane] = l[x];
+                S.row[b][1][x * 32 + lane] = d[x];
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.stats[b]));
+        }
+    } else if (warp < 2 * kGroupWarps) {
+        const int t = warp / kGroupWarps, key = first + threadIdx.x % kTile;
+        const uint32_t lanes = static_cast<uint32_t>(warp % kGroupWarps * 32) << 16;
+        const uint32_t my_s = s_at + lanes + t * 64, my_dp = dp_at + lanes + t * 64;
+        const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
+        bool ok = true;
+        for (int j = 0; ok && j < n; ++j) {
+            const int tile = from + j % per, b = j % 2;
+            const float4 *lse = reinterpret_cast<const float4 *>(S.row[b][0] + t * 64), *dot = reinterpret_cast<const float4 *>(S.row[b][1] + t * 64);
+            ok = bar_wait(smem_addr(&S.stats[b]), j / 2 & 1, failed) && bar_wait(smem_addr(&S.score[0]), j & 1, failed);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            fence_after();
+            uint32_t s[2][32], d[2][32];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) load_columns(my_s + c * 32, s[c]);
+            wait_loads();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) pin(s[c]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int x = 0; x < 32; x += 4) {
+                    const float4 l = lse[c * 8 + x / 4];
+                    s[c][x] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x]), scale, -l.x)));
+                    s[c][x + 1] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x + 1]), scale, -l.y)));
+                    s[c][x + 2] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x + 2]), scale, -l.z)));
+                    s[c][x + 3] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x + 3]), scale, -l.w)));
+                }
+            // under the causal mask the queries from key - off on see this key
+            const int begin = P.causal ? key - off - tile * kTile - t * 64 : 0;
+            if (__any_sync(0xffffffffu, begin > 0)) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int x = 0; x < 32; ++x)
+                        if (c * 32 + x < begin) s[c][x] = 0;
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t w[16];
+#pragma unroll
+                for (int x = 0; x < 32; x += 2) w[x / 2] = pack_bf16(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1]));
+                store_columns(my_s + c * 16, w);
+            }
+            wait_stores();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.prob[0]));
+            ok = bar_wait(smem_addr(&S.second[0]), j & 1, failed);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            fence_after();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) load_columns(my_dp + c * 32, d[c]);
+            wait_loads();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) pin(d[c]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t w[16];
+#pragma unroll
+                for (int x = 0; x < 32; x += 4) {
+                    const float4 e = dot[c * 8 + x / 4];
+                    w[x / 2] = pack_bf16(__uint_as_float(s[c][x]) * (__uint_as_float(d[c][x]) - e.x),
+                                         __uint_as_float(s[c][x + 1]) * (__uint_as_float(d[c][x + 1]) - e.y));
+                    w[x / 2 + 1] = pack_bf16(__uint_as_float(s[c][x + 2]) * (__uint_as_float(d[c][x + 2]) - e.z),
+                                             __uint_as_float(s[c][x + 3]) * (__uint_as_float(d[c][x + 3]) - e.w));
+                }
+                store_columns(my_dp + c * 16, w);
+            }
+            wait_stores();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                bar_arrive(smem_addr(&S.grad));
+                bar_arrive(smem_addr(&S.stats_free[b]));
+            }
+        }
+        if (ok && n > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&S.done), 0, failed));
+        if (ok) {
+            // the first group writes dv, the second dk
+            const bool wanted = key < (P.packed ? K.n : P.seq_k);
+            __nv_bfloat16 *out = t ? row_of(P.dk, K, key, at.head) : row_of(P.dv, K, key, at.head);
+            if (n > 0) {
+                fence_after();
+#pragma unroll
+                for (int c = 0; c < kDim / 32; ++c) {
+                    uint32_t r[32];
+                    load_columns((t ? dk_at : dv_at) + lanes + c * 32, r);
+                    wait_loads();
+                    pin(r);
+                    if (wanted && key < K.n) store_row<kDim>(out, r, c * 32, P.head_dim, t ? P.scale : 1.0f);
+                }
+            }
+            if (wanted && (key >= K.n || n == 0)) zero_row(out, 0, P.head_dim);
+        }
+    }
+    __syncwarp();
+    end_block<512>(S, tmem);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+namespace {
+
+using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn() {
+    static std::atomic<EncodeFn> known{nullptr};
+    EncodeFn f = known.load();
+    if (!f) {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult how;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &how) != cudaSuccess || how != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return nullptr;
+        }
+        f = reinterpret_cast<EncodeFn>(p);
+        known.store(f);
     }
     return f;
 }
-__device__ __forceinline__ void store4(__nv_bfloat16 *row, int lane, int d, const Four &f) {
-    if (lane * 4 < d) {
-        Pack<__nv_bfloat16, 4> p;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p.v[i] = __float2bfloat16_rn(f.v[i]);
-        *reinterpret_cast<Pack<__nv_bfloat16, 4> *>(row + lane * 4) = p;
+
+// Heads as [batch, head, row, dim] in boxes of 128 rows by 64 dimensions; what lies past the tensor reads as zero.
+bool make_map(CUtensorMap &map, const Heads &t, int batch, int heads, int rows, int dim, const void *stand_in) {
+    const EncodeFn encode = encode_fn();
+    if (!encode) return false;
+    const bool none = rows == 0 || batch == 0;             // never read
+    void *at = none ? const_cast<void *>(stand_in) : static_cast<void *>(t.ptr);
+    const cuuint64_t size[4] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(none ? 1 : rows), static_cast<cuuint64_t>(heads),
+                                static_cast<cuuint64_t>(none ? 1 : batch)};
+    // the stride of a single row, head or sample means nothing, but has to be a valid one
+    const auto stride = [&](int64_t s, cuuint64_t n) { return static_cast<cuuint64_t>(n == 1 ? 256 : s * 2); };
+    const cuuint64_t strides[3] = {stride(t.row_stride, size[1]), stride(t.head_stride, size[2]), stride(t.batch_stride, size[3])};
+    const cuuint32_t box[4] = {64, kTile, 1, 1}, step[4] = {1, 1, 1, 1};
+    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, at, size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+using Kernel = void (*)(const AttentionParams, const Maps);
+
+// Shared-memory limit of a kernel, set once per device.
+bool allow(Kernel fn, int which, int bytes) {
+    static std::atomic<bool> set[64][6];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return false;
     }
-}
-__device__ __forceinline__ float dot4(const Four &a, const Four &b) {
-    return warp_total(a.v[0] * b.v[0] + a.v[1] * b.v[1] + a.v[2] * b.v[2] + a.v[3] * b.v[3]);
-}
-__device__ __forceinline__ void add4(Four &a, float w, const Four &b) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a.v[i] = fmaf(w, b.v[i], a.v[i]);
-}
-
-struct Place { int b, h, i; };
-__device__ __forceinline__ Place place(int rows, int heads) {
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * kAttnWarps + threadIdx.x / 32;
-    const int64_t bh = r / rows;
-    return Place{static_cast<int>(bh / heads), static_cast<int>(bh % heads), static_cast<int>(r - bh * rows)};
-}
-
-__global__ void __launch_bounds__(kAttnWarps * 32) attention_forward_rows(const __grid_constant__ AttentionParams P) {
-    const Place at = place(P.max_q, P.heads_q);
-    if (at.b >= P.batch) return;
-    const int lane = threadIdx.x % 32, d = P.head_dim;
-    const Rows Q = query_rows(P, at.b), K = key_rows(P, at.b);
-    if (at.i >= Q.n && P.packed) return;
-    const int see = at.i >= Q.n ? 0 : (P.causal ? min(K.n, at.i + K.n - Q.n + 1) : K.n);
-    Four o{{0.0f, 0.0f, 0.0f, 0.0f}};
-    float top = -INFINITY, total = 0.0f;
-    if (see > 0) {
-        const Four q = load4(row_of(P.q, Q, at.i, at.h), lane, d);
-        for (int j = 0; j < see; ++j) {
-            const float s = dot4(q, load4(row_of(P.k, K, j, at.h / P.group), lane, d)) * P.scale;
-            const float next = fmaxf(top, s), fade = top == -INFINITY ? 0.0f : expf(top - next), p = expf(s - next);
-            total = fmaf(total, fade, p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o.v[i] *= fade;
-            add4(o, p, load4(row_of(P.v, K, j, at.h / P.group), lane, d));
-            top = next;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o.v[i] /= total;
+    if (set[dev][which].load(std::memory_order_acquire)) return true;
+    if (cudaFuncSetAttribute(reinterpret_cast<const void *>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
     }
-    store4(row_of(P.o, Q, at.i, at.h), lane, d, o);
-    if (lane == 0) P.lse[stat_at(P, Q, at.i, at.h)] = see > 0 ? logf(total) + top : -INFINITY;
+    set[dev][which].store(true, std::memory_order_release);
+    return true;
 }
 
-__global__ void __launch_bounds__(kAttnWarps * 32) attention_backward_queries(const __grid_constant__ AttentionParams P) {
-    const Place at = place(P.max_q, P.heads_q);
-    if (at.b >= P.batch) return;
-    const int lane = threadIdx.x % 32, d = P.head_dim;
-    const Rows Q = query_rows(P, at.b), K = key_rows(P, at.b);
-    if (at.i >= Q.n && P.packed) return;
-    const int see = at.i >= Q.n ? 0 : (P.causal ? min(K.n, at.i + K.n - Q.n + 1) : K.n);
-    Four dq{{0.0f, 0.0f, 0.0f, 0.0f}};
-    float dot = 0.0f;
-    if (see > 0) {
-        const Four q = load4(row_of(P.q, Q, at.i, at.h), lane, d), go = load4(row_of(P.d_o, Q, at.i, at.h), lane, d);
-        dot = dot4(go, load4(row_of(P.o, Q, at.i, at.h), lane, d));
-        const float lse = P.lse[stat_at(P, Q, at.i, at.h)];
-        for (int j = 0; j < see; ++j) {
-            const Four k = load4(row_of(P.k, K, j, at.h / P.group), lane, d);
-            const float p = expf(dot4(q, k) * P.scale - lse);
-            add4(dq, p * (dot4(go, load4(row_of(P.v, K, j, at.h / P.group), lane, d)) - dot), k);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dq.v[i] *= P.scale;
-    }
-    store4(row_of(P.dq, Q, at.i, at.h), lane, d, dq);
-    if (lane == 0) P.row_dot[stat_at(P, Q, at.i, at.h)] = dot;
-}
-
-__global__ void __launch_bounds__(kAttnWarps * 32) attention_backward_keys(const __grid_constant__ AttentionParams P) {
-    const Place at = place(P.max_k, P.heads_kv);
-    if (at.b >= P.batch) return;
-    const int lane = threadIdx.x % 32, d = P.head_dim;
-    const Rows Q = query_rows(P, at.b), K = key_rows(P, at.b);
-    if (at.i >= K.n && P.packed) return;
-    Four dk{{0.0f, 0.0f, 0.0f, 0.0f}}, dv = dk;
-    if (at.i < K.n) {
-        const Four k = load4(row_of(P.k, K, at.i, at.h), lane, d), v = load4(row_of(P.v, K, at.i, at.h), lane, d);
-        const int from = P.causal ? max(0, at.i - (K.n - Q.n)) : 0;
-        for (int g = 0; g < P.group; ++g) {
-            const int h = at.h * P.group + g;
-            for (int i = from; i < Q.n; ++i) {
-                const Four q = load4(row_of(P.q, Q, i, h), lane, d), go = load4(row_of(P.d_o, Q, i, h), lane, d);
-                const int64_t s = stat_at(P, Q, i, h);
-                const float p = expf(dot4(q, k) * P.scale - P.lse[s]);
-                add4(dv, p, go);
-                add4(dk, p * (dot4(go, v) - P.row_dot[s]), q);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dk.v[i] *= P.scale;
-    }
-    store4(row_of(P.dk, K, at.i, at.h), lane, d, dk);
-    store4(row_of(P.dv, K, at.i, at.h), lane, d, dv);
-}
-
-static unsigned row_blocks(int64_t batch, int64_t heads, int64_t rows) {
-    const int64_t n = (batch * heads * rows + kAttnWarps - 1) / kAttnWarps;
-    return n > 0x7fffffff ? 0u : static_cast<unsigned>(n);
-}
-
-int launch_attention_forward(const AttentionParams &P, cudaStream_t stream) {
-    if (P.max_q == 0) return LOCO_OK;
-    const unsigned n = row_blocks(P.batch, P.heads_q, P.max_q);
-    if (!n) return LOCO_ERR_UNSUPPORTED;
-    attention_forward_rows<<<n, kAttnWarps * 32, 0, stream>>>(P);
+int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const AttentionParams &P, const Maps &M, cudaStream_t stream) {
+    const int64_t blocks = tiles * heads * P.batch;
+    if (blocks == 0) return LOCO_OK;
+    if (blocks > 0x7fffffff) return LOCO_ERR_UNSUPPORTED;
+    if (!allow(fn, which, bytes)) return LOCO_ERR_CUDA;
+    fn<<<static_cast<unsigned>(blocks), kThreads, static_cast<size_t>(bytes), stream>>>(P, M);
     return launched();
 }
 
+bool make_maps(const AttentionParams &P, Maps &M, bool gradient) {
+    const int b = P.packed ? 1 : P.batch;
+    const void *any = P.seq_q > 0 ? P.q.ptr : P.k.ptr;
+    return make_map(M.q, P.q, b, P.heads_q, P.seq_q, P.head_dim, any) && make_map(M.k, P.k, b, P.heads_kv, P.seq_k, P.head_dim, any) &&
+           make_map(M.v, P.v, b, P.heads_kv, P.seq_k, P.head_dim, any) &&
+           (!gradient || make_map(M.d_o, P.d_o, b, P.heads_q, P.seq_q, P.head_dim, any));
+}
+
+template <int kDim> int forward(const AttentionParams &P, const Maps &M, cudaStream_t stream) {
+    constexpr int bytes = shared_bytes<kDim>();
+    return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, bytes, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, P, M, stream);
+}
+template <int kDim> int backward(const AttentionParams &P, const Maps &M, cudaStream_t stream) {
+    constexpr int bytes = shared_bytes<kDim>();
+    const int rc = launch(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, bytes, (P.max_q + kTile - 1) / kTile, P.heads_q, P, M, stream);
+    if (rc != LOCO_OK) return rc;
+    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, bytes, (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream);
+}
+
+}  // namespace
+
+int launch_attention_forward(const AttentionParams &P, cudaStream_t stream) {
+    Maps M;
+    if (!make_maps(P, M, false)) return LOCO_ERR_CUDA;
+    return P.head_dim <= 64 ? forward<64>(P, M, stream) : forward<128>(P, M, stream);
+}
+
 int launch_attention_backward(const AttentionParams &P, cudaStream_t stream) {
-    if (P.max_q > 0) {
-        const unsigned n = row_blocks(P.batch, P.heads_q, P.max_q);
-        if (!n) return LOCO_ERR_UNSUPPORTED;
-        attention_backward_queries<<<n, kAttnWarps * 32, 0, stream>>>(P);
-        const int rc = launched();
-        if (rc != LOCO_OK) return rc;
-    }
-    if (P.max_k > 0) {
-        const unsigned n = row_blocks(P.batch, P.heads_kv, P.max_k);
-        if (!n) return LOCO_ERR_UNSUPPORTED;
-        attention_backward_keys<<<n, kAttnWarps * 32, 0, stream>>>(P);
-        return launched();
-    }
-    return LOCO_OK;
+    Maps M;
+    if (!make_maps(P, M, true)) return LOCO_ERR_CUDA;
+    return P.head_dim <= 64 ? backward<64>(P, M, stream) : backward<128>(P, M, stream);
 }
 
 }  // namespace loco_layer
+
+extern "C" int loco_layer_status(uint32_t *flags, void *stream) {
+    if (!flags) return LOCO_ERR_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    unsigned host = 0;
+    if (cudaMemcpyFromSymbolAsync(&host, loco_layer::g_status, sizeof(host), 0, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+        cudaStreamSynchronize(s) != cudaSuccess) {
+        cudaGetLastError();
+        return LOCO_ERR_CUDA;
+    }
+    *flags = host;
+    return LOCO_OK;
+}

@@ -28,7 +28,8 @@ SCALINGS = {"plain": ROTARY_PLAIN, "linear": ROTARY_LINEAR, "parts": ROTARY_PART
 
 EXPORTS = ("loco_rotary_table", "loco_rotary_apply", "loco_attention_forward", "loco_attention_backward",
            "loco_attention_backward_workspace_bytes", "loco_router_workspace_bytes", "loco_router_forward",
-           "loco_router_backward", "loco_layer_launch_count")
+           "loco_router_backward", "loco_layer_status", "loco_layer_launch_count")
+FLAG_TIMEOUT = 1
 
 # the C structures, packed in one go: a call marshals a few dozen scalars and has to cost microseconds
 _HEADS = struct.Struct("@Pqqq")                       # loco_heads_t
@@ -59,6 +60,7 @@ def lib() -> C.CDLL:
         L.loco_router_workspace_bytes.argtypes = [st]
         L.loco_router_forward.argtypes = [st, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, u64, vp]
         L.loco_router_backward.argtypes = [st, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.loco_layer_status.argtypes = [C.POINTER(C.c_uint32), vp]
         L.loco_layer_launch_count.argtypes = []
         for name in EXPORTS:
             getattr(L, name).restype = u64 if name.endswith(("_bytes", "_count")) else C.c_int
@@ -110,6 +112,14 @@ def _flat(t: Optional[torch.Tensor], shape, dtype, device, what: str) -> Optiona
 
 def loco_layer_launch_count() -> int:
     return int(lib().loco_layer_launch_count())
+
+
+def loco_layer_status(stream=None) -> int:
+    """Flags raised on the current device since the library was loaded; synchronises the stream."""
+    flags = C.c_uint32(0)
+    _check(lib().loco_layer_status(C.byref(flags), (torch.cuda.current_stream() if stream is None else stream).cuda_stream),
+           "loco_layer_status")
+    return int(flags.value)
 
 
 # ---- rotary positions ------------------------------------------------------------------------
