@@ -29,7 +29,7 @@ using namespace tc;
 
 constexpr int kTile = 128;                       // queries and keys of a tile
 constexpr int kGroupWarps = 4;                   // warps of a softmax group: the 128 lanes of TMEM
-constexpr int kThreads = (2 * kGroupWarps + 3) * 32;
+constexpr int kThreads = 3 * kGroupWarps * 32;   // two softmax groups and one of single warps, the last of which idles
 constexpr int kLoadWarp = 2 * kGroupWarps, kProductWarp = kLoadWarp + 1, kHelpWarp = kLoadWarp + 2;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -52,7 +52,7 @@ struct Shared {
     uint64_t stats[2], stats_free[2];            // backward keys: row statistics of a query tile
     uint64_t done, drain;
     uint32_t tmem, failed;
-    alignas(16) float row[2][2][kTile];          // backward keys: lse * log2(e), D of the query tile; backward queries: D
+    alignas(16) float row[2][2][kTile];          // backward keys: -lse * log2(e), -D of the query tile; backward queries: D
 };
 template <int kDim> constexpr int shared_bytes() {
     return (2 + stream_slots<kDim>()) * tile_bytes<kDim>() + static_cast<int>(sizeof(Shared)) + 1024;
@@ -126,6 +126,12 @@ template <int kColumns> __device__ __forceinline__ void end_block(Shared &S, uin
     if (threadIdx.x == 0 && S.failed) atomicOr(&g_status, LOCO_LAYER_FLAG_TIMEOUT);
 }
 
+// Registers: the block starts with 168 a thread (3 x 128 x 168 of the SM's 65536); the softmax groups, which hold rows of
+// scores, take 208 each and the third group keeps 88: 2 x 208 + 88 = 3 x 168.
+// Set at the head of each side's own code.
+__device__ __forceinline__ void registers_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+__device__ __forceinline__ void registers_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+
 // A role that gave up still waits for the copies it started before the block's shared memory goes away.
 __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
     const uint64_t begin = now_ns();
@@ -183,6 +189,22 @@ __device__ __forceinline__ int key_tiles(const Rows &Q, const Rows &K, int causa
     return (key_limit(Q, K, causal, min(first + kTile, Q.n) - 1) + kTile - 1) / kTile;
 }
 
+__device__ __forceinline__ void mask_from(uint32_t (&s)[32], int left) {
+#pragma unroll
+    for (int x = 0; x < 32; ++x)
+        if (x >= left) s[x] = 0xff800000u;       // -inf
+}
+__device__ __forceinline__ float row_max(const uint32_t (&s)[32]) {
+    float m[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) m[x] = fmaxf(__uint_as_float(s[x]), __uint_as_float(s[x + 4]));
+#pragma unroll
+    for (int x = 8; x < 32; x += 8)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) m[y] = max3(m[y], __uint_as_float(s[x + y]), __uint_as_float(s[x + y + 4]));
+    return fmaxf(max3(m[0], m[1], m[2]), m[3]);
+}
+
 // ------------------------------------------------------------------------------------------------ forward
 
 template <int kDim>
@@ -202,79 +224,83 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
     const uint32_t tmem = begin_block<512>(S, kSlots, 1, kGroupWarps);
     volatile uint32_t *const failed = &S.failed;
 
-    if (warp == kLoadWarp && lane == 0 && n > 0) {
-        Ring r;
-        bar_expect(smem_addr(&S.stay), (n0 > 0 ? kBytes : 0) + (n1 > 0 ? kBytes : 0));
-        for (int t = 0; t < 2; ++t)
-            if ((t ? n1 : n0) > 0)
-#pragma unroll
-                for (int x = 0; x < kDim; x += 64)
-                    load_box(base + t * kBytes + x / 64 * (kTile * 128), &M.q, x, Q.first + first + t * kTile, at.head, Q.at, smem_addr(&S.stay));
-        int sent = 0;
-        for (int j = 0; j < 2 * n; ++j) {
-            if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
-            load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
-                            smem_addr(ragged && j >= 2 * n - 1 ? &S.last : &S.full[r.slot]));
-            ++sent;
-            r.next<kSlots>();
-        }
-        if (*failed) {
-            settle(smem_addr(&S.stay), 0);
-            for (int j = max(0, sent - kSlots); j < sent; ++j)
-                if (ragged && j >= 2 * n - 1) settle(smem_addr(&S.last), 0);
-                else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
-        }
-    } else if (warp == kProductWarp && lane == 0 && n > 0) {
-        const uint32_t scores = product(kTile, false, P.scale < 0.0f);
-        bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && bar_wait(smem_addr(&S.full[0]), 0, failed);
-        if (ok) {
+    if (warp >= 2 * kGroupWarps) {
+        registers_few();
+        if (warp == kLoadWarp && lane == 0 && n > 0) {
+            Ring r;
+            bar_expect(smem_addr(&S.stay), (n0 > 0 ? kBytes : 0) + (n1 > 0 ? kBytes : 0));
             for (int t = 0; t < 2; ++t)
-                if ((t ? n1 : n0) > 0) {
-                    product_scores<kDim>(tmem + t * kTile, base + t * kBytes, ring, scores);
-                    commit(smem_addr(&S.score[t]));
+                if ((t ? n1 : n0) > 0)
+    #pragma unroll
+                    for (int x = 0; x < kDim; x += 64)
+                        load_box(base + t * kBytes + x / 64 * (kTile * 128), &M.q, x, Q.first + first + t * kTile, at.head, Q.at, smem_addr(&S.stay));
+            int sent = 0;
+            for (int j = 0; j < 2 * n; ++j) {
+                if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+                load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
+                                smem_addr(ragged && j >= 2 * n - 1 ? &S.last : &S.full[r.slot]));
+                ++sent;
+                r.next<kSlots>();
+            }
+            if (*failed) {
+                settle(smem_addr(&S.stay), 0);
+                for (int j = max(0, sent - kSlots); j < sent; ++j)
+                    if (ragged && j >= 2 * n - 1) settle(smem_addr(&S.last), 0);
+                    else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
+            }
+        } else if (warp == kProductWarp && lane == 0 && n > 0) {
+            const uint32_t scores = product(kTile, false, P.scale < 0.0f);
+            bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && bar_wait(smem_addr(&S.full[0]), 0, failed);
+            if (ok) {
+                for (int t = 0; t < 2; ++t)
+                    if ((t ? n1 : n0) > 0) {
+                        product_scores<kDim>(tmem + t * kTile, base + t * kBytes, ring, scores);
+                        commit(smem_addr(&S.score[t]));
+                    }
+                commit(smem_addr(&S.empty[0]));
+            }
+            Ring v, k;                               // value tiles at odd places of the ring, key tiles at even ones
+            v.next<kSlots>();
+            k.next<kSlots>();
+            k.next<kSlots>();
+            for (int j = 0; ok && j < n; ++j) {
+                ok = (ragged && j == n - 1 ? bar_wait(smem_addr(&S.clean), 0, failed) : bar_wait(smem_addr(&S.full[v.slot]), v.phase, failed)) &&
+                     (j + 1 == n || bar_wait(smem_addr(&S.full[k.slot]), k.phase, failed));
+                for (int t = 0; ok && t < 2; ++t) {
+                    const int nt = t ? n1 : n0;
+                    if (j >= nt) continue;
+                    ok = bar_wait(smem_addr(&S.prob[t]), j & 1, failed);
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t p = tmem + t * kTile;
+                    product_apply<kDim>(tmem + 2 * kTile + t * kTile, p, p + 32, ring + v.slot * kBytes, j > 0);
+                    commit(smem_addr(&S.second[t]));
+                    if (j + 1 < nt) {
+                        product_scores<kDim>(p, base + t * kBytes, ring + k.slot * kBytes, scores);
+                        commit(smem_addr(&S.score[t]));
+                    }
                 }
-            commit(smem_addr(&S.empty[0]));
-        }
-        Ring v, k;                               // value tiles at odd places of the ring, key tiles at even ones
-        v.next<kSlots>();
-        k.next<kSlots>();
-        k.next<kSlots>();
-        for (int j = 0; ok && j < n; ++j) {
-            ok = (ragged && j == n - 1 ? bar_wait(smem_addr(&S.clean), 0, failed) : bar_wait(smem_addr(&S.full[v.slot]), v.phase, failed)) &&
-                 (j + 1 == n || bar_wait(smem_addr(&S.full[k.slot]), k.phase, failed));
-            for (int t = 0; ok && t < 2; ++t) {
-                const int nt = t ? n1 : n0;
-                if (j >= nt) continue;
-                ok = bar_wait(smem_addr(&S.prob[t]), j & 1, failed);
                 if (!ok) break;
-                fence_after();
-                const uint32_t p = tmem + t * kTile;
-                product_apply<kDim>(tmem + 2 * kTile + t * kTile, p, p + 32, ring + v.slot * kBytes, j > 0);
-                commit(smem_addr(&S.second[t]));
-                if (j + 1 < nt) {
-                    product_scores<kDim>(p, base + t * kBytes, ring + k.slot * kBytes, scores);
-                    commit(smem_addr(&S.score[t]));
+                commit(smem_addr(&S.empty[v.slot]));
+                if (j + 1 < n) commit(smem_addr(&S.empty[k.slot]));
+                for (int i = 0; i < 2; ++i) {
+                    v.next<kSlots>();
+                    k.next<kSlots>();
                 }
             }
-            if (!ok) break;
-            commit(smem_addr(&S.empty[v.slot]));
-            if (j + 1 < n) commit(smem_addr(&S.empty[k.slot]));
-            for (int i = 0; i < 2; ++i) {
-                v.next<kSlots>();
-                k.next<kSlots>();
+            commit(smem_addr(&S.drain));
+            settle(smem_addr(&S.drain), 0);
+        } else if (warp == kHelpWarp && ragged) {
+            const int load = 2 * n - 1;              // the last value tile
+            if (bar_wait(smem_addr(&S.last), 0, failed)) {
+                clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&S.clean));
             }
         }
-        commit(smem_addr(&S.drain));
-        settle(smem_addr(&S.drain), 0);
-    } else if (warp == kHelpWarp && ragged) {
-        const int load = 2 * n - 1;              // the last value tile
-        if (bar_wait(smem_addr(&S.last), 0, failed)) {
-            clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&S.clean));
-        }
-    } else if (warp < 2 * kGroupWarps) {
+    } else {
+        registers_many();
         const int t = warp / kGroupWarps, i = first + t * kTile + threadIdx.x % kTile;
         const int nt = t ? n1 : n0, limit = key_limit(Q, K, P.causal, i);
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % kGroupWarps * 32) << 16);
@@ -288,27 +314,28 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
             if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
             fence_after();
             uint32_t s[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) load_columns(s_at + c * 32, s[c]);
+            load_columns(s_at, s[0]);
+            load_columns(s_at + 32, s[1]);
             wait_loads();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) pin(s[c]);
+            pin(s[0]);
+            pin(s[1]);
+            load_columns(s_at + 64, s[2]);
+            load_columns(s_at + 96, s[3]);
             const int left = limit - j * kTile;  // columns from here on are not seen
-            if (__any_sync(0xffffffffu, left < kTile)) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int x = 0; x < 32; ++x)
-                        if (c * 32 + x >= left) s[c][x] = 0xff800000u;
+            const bool edge = __any_sync(0xffffffffu, left < kTile);
+            if (edge) {
+                mask_from(s[0], left);
+                mask_from(s[1], left - 32);
             }
-            float m[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                m[c] = __uint_as_float(s[c][0]);
-#pragma unroll
-                for (int x = 1; x < 32; ++x) m[c] = fmaxf(m[c], __uint_as_float(s[c][x]));
+            float most = fmaxf(row_max(s[0]), row_max(s[1]));
+            wait_loads();
+            pin(s[2]);
+            pin(s[3]);
+            if (edge) {
+                mask_from(s[2], left - 64);
+                mask_from(s[3], left - 96);
             }
-            const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            most = max3(most, row_max(s[2]), row_max(s[3]));
             if (j == 0) {
                 top = most;
             } else if (__any_sync(0xffffffffu, most - top > room)) {
@@ -331,20 +358,23 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
                 top = next;
             }
             const float shift = top == -INFINITY ? 0.0f : top * scale;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            float2 sum[2] = {make_float2(total, 0.0f), make_float2(0.0f, 0.0f)};
+            const float2 by = make_float2(scale, scale), minus = make_float2(-shift, -shift);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t p[16];
 #pragma unroll
                 for (int x = 0; x < 32; x += 2) {
-                    const float a = exp2_fast(fmaf(__uint_as_float(s[c][x]), scale, -shift));
-                    const float b = exp2_fast(fmaf(__uint_as_float(s[c][x + 1]), scale, -shift));
-                    sum[x / 2 % 4] += a + b;
-                    p[x / 2] = pack_bf16(a, b);
+                    float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, minus);
+                    e.x = exp2_fast(e.x);
+                    e.y = exp2_fast(e.y);
+                    sum[x / 2 % 2] = add2(sum[x / 2 % 2], e);
+                    p[x / 2] = pack_bf16(e.x, e.y);
                 }
                 store_columns(s_at + c * 16, p);
             }
-            total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            sum[0] = add2(sum[0], sum[1]);
+            total = sum[0].x + sum[0].y;
             wait_stores();
             fence_before();
             __syncwarp();
@@ -397,74 +427,78 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
     const uint32_t dp_at = tmem + 2 * kTile, dq_at = tmem + 3 * kTile;
     volatile uint32_t *const failed = &S.failed;
 
-    if (warp == kLoadWarp && lane == 0 && n > 0) {
-        Ring r;
-        bar_expect(smem_addr(&S.stay), 2 * kBytes);
-#pragma unroll
-        for (int x = 0; x < kDim; x += 64) {
-            load_box(base + x / 64 * (kTile * 128), &M.q, x, Q.first + first, at.head, Q.at, smem_addr(&S.stay));
-            load_box(base + kBytes + x / 64 * (kTile * 128), &M.d_o, x, Q.first + first, at.head, Q.at, smem_addr(&S.stay));
-        }
-        int sent = 0;
-        for (int j = 0; j < 2 * n; ++j) {
-            if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
-            load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
-                            smem_addr(ragged && j >= 2 * n - 2 ? &S.last : &S.full[r.slot]));
-            ++sent;
-            r.next<kSlots>();
-        }
-        if (*failed) {
-            settle(smem_addr(&S.stay), 0);
-            for (int j = max(0, sent - kSlots); j < sent; ++j)
-                if (ragged && j >= 2 * n - 2) settle(smem_addr(&S.last), 0);
-                else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
-        }
-    } else if (warp == kProductWarp && lane == 0 && n > 0) {
-        const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
-        // tile j: keys at place 2j of the ring, values at 2j + 1
-        const auto slot = [](int load) { return load % kSlots; };
-        const auto ready = [&](int load) {
-            return ragged && load >= 2 * n - 2 ? bar_wait(smem_addr(&S.clean), 0, failed)
-                                               : bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
-        };
-        bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && ready(0) && ready(1);
-        if (ok) {
-            product_scores<kDim>(tmem, base, ring, scores);
-            commit(smem_addr(&S.score[0]));
-            product_scores<kDim>(dp_at, base + kBytes, ring + kBytes, plain);
-            commit(smem_addr(&S.second[0]));
-            commit(smem_addr(&S.empty[1]));
-        }
-        for (int j = 0; ok && j < n; ++j) {
-            if (j + 1 < n) {
-                ok = ready(2 * j + 2);
-                if (!ok) break;
-                product_scores<kDim>(tmem + (j + 1) % 2 * kTile, base, ring + slot(2 * j + 2) * kBytes, scores);
-                commit(smem_addr(&S.score[(j + 1) % 2]));
+    if (warp >= 2 * kGroupWarps) {
+        registers_few();
+        if (warp == kLoadWarp && lane == 0 && n > 0) {
+            Ring r;
+            bar_expect(smem_addr(&S.stay), 2 * kBytes);
+    #pragma unroll
+            for (int x = 0; x < kDim; x += 64) {
+                load_box(base + x / 64 * (kTile * 128), &M.q, x, Q.first + first, at.head, Q.at, smem_addr(&S.stay));
+                load_box(base + kBytes + x / 64 * (kTile * 128), &M.d_o, x, Q.first + first, at.head, Q.at, smem_addr(&S.stay));
             }
-            ok = bar_wait(smem_addr(&S.grad), j & 1, failed) && (j + 1 == n || ready(2 * j + 3));
-            if (!ok) break;
-            fence_after();
-            if (j + 1 < n) {
-                product_scores<kDim>(dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+            int sent = 0;
+            for (int j = 0; j < 2 * n; ++j) {
+                if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+                load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
+                                smem_addr(ragged && j >= 2 * n - 2 ? &S.last : &S.full[r.slot]));
+                ++sent;
+                r.next<kSlots>();
+            }
+            if (*failed) {
+                settle(smem_addr(&S.stay), 0);
+                for (int j = max(0, sent - kSlots); j < sent; ++j)
+                    if (ragged && j >= 2 * n - 2) settle(smem_addr(&S.last), 0);
+                    else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
+            }
+        } else if (warp == kProductWarp && lane == 0 && n > 0) {
+            const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
+            // tile j: keys at place 2j of the ring, values at 2j + 1
+            const auto slot = [](int load) { return load % kSlots; };
+            const auto ready = [&](int load) {
+                return ragged && load >= 2 * n - 2 ? bar_wait(smem_addr(&S.clean), 0, failed)
+                                                   : bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
+            };
+            bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && ready(0) && ready(1);
+            if (ok) {
+                product_scores<kDim>(tmem, base, ring, scores);
+                commit(smem_addr(&S.score[0]));
+                product_scores<kDim>(dp_at, base + kBytes, ring + kBytes, plain);
                 commit(smem_addr(&S.second[0]));
-                commit(smem_addr(&S.empty[slot(2 * j + 3)]));
+                commit(smem_addr(&S.empty[1]));
             }
-            const uint32_t ds = tmem + j % 2 * kTile;
-            product_apply<kDim>(dq_at, ds, ds + 64, ring + slot(2 * j) * kBytes, j > 0);
-            commit(smem_addr(&S.empty[slot(2 * j)]));
+            for (int j = 0; ok && j < n; ++j) {
+                if (j + 1 < n) {
+                    ok = ready(2 * j + 2);
+                    if (!ok) break;
+                    product_scores<kDim>(tmem + (j + 1) % 2 * kTile, base, ring + slot(2 * j + 2) * kBytes, scores);
+                    commit(smem_addr(&S.score[(j + 1) % 2]));
+                }
+                ok = bar_wait(smem_addr(&S.grad), j & 1, failed) && (j + 1 == n || ready(2 * j + 3));
+                if (!ok) break;
+                fence_after();
+                if (j + 1 < n) {
+                    product_scores<kDim>(dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+                    commit(smem_addr(&S.second[0]));
+                    commit(smem_addr(&S.empty[slot(2 * j + 3)]));
+                }
+                const uint32_t ds = tmem + j % 2 * kTile;
+                product_apply<kDim>(dq_at, ds, ds + 64, ring + slot(2 * j) * kBytes, j > 0);
+                commit(smem_addr(&S.empty[slot(2 * j)]));
+            }
+            if (ok) commit(smem_addr(&S.done));
+            commit(smem_addr(&S.drain));
+            settle(smem_addr(&S.drain), 0);
+        } else if (warp == kHelpWarp && ragged) {
+            if (bar_wait(smem_addr(&S.last), 0, failed)) {
+                for (int load = 2 * n - 2; load < 2 * n; ++load) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&S.clean));
+            }
         }
-        if (ok) commit(smem_addr(&S.done));
-        commit(smem_addr(&S.drain));
-        settle(smem_addr(&S.drain), 0);
-    } else if (warp == kHelpWarp && ragged) {
-        if (bar_wait(smem_addr(&S.last), 0, failed)) {
-            for (int load = 2 * n - 2; load < 2 * n; ++load) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&S.clean));
-        }
-    } else if (warp < 2 * kGroupWarps) {
+    } else {
+        registers_many();
         const int t = warp / kGroupWarps, row = threadIdx.x % kTile, i = first + row;
         const int limit = key_limit(Q, K, P.causal, i);
         const uint32_t lanes = static_cast<uint32_t>(warp % kGroupWarps * 32) << 16;
@@ -490,6 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
             if (shift == -INFINITY) shift = INFINITY;
         }
         if (t == 0 && wanted) P.row_dot[stat_at(P, Q, i, at.head)] = dot;
+        const float2 by = make_float2(scale, scale), minus = make_float2(-shift, -shift), less = make_float2(-dot, -dot);
         bool ok = true;
         for (int j = 0; ok && j < n; ++j) {
             const uint32_t s_at = tmem + lanes + j % 2 * kTile + t * 64;
@@ -505,7 +540,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int x = 0; x < 32; ++x) s[c][x] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x]), scale, -shift)));
+                for (int x = 0; x < 32; x += 2) {
+                    const float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, minus);
+                    s[c][x] = __float_as_uint(exp2_fast(e.x));
+                    s[c][x + 1] = __float_as_uint(exp2_fast(e.y));
+                }
             const int left = limit - j * kTile - t * 64;
             if (__any_sync(0xffffffffu, left < 64)) {
 #pragma unroll
@@ -526,9 +565,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
             for (int c = 0; c < 2; ++c) {
                 uint32_t w[16];
 #pragma unroll
-                for (int x = 0; x < 32; x += 2)
-                    w[x / 2] = pack_bf16(__uint_as_float(s[c][x]) * (__uint_as_float(d[c][x]) - dot),
-                                         __uint_as_float(s[c][x + 1]) * (__uint_as_float(d[c][x + 1]) - dot));
+                for (int x = 0; x < 32; x += 2) {
+                    const float2 e = mul2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])),
+                                          add2(make_float2(__uint_as_float(d[c][x]), __uint_as_float(d[c][x + 1])), less));
+                    w[x / 2] = pack_bf16(e.x, e.y);
+                }
                 store_columns(s_at + c * 16, w);
             }
             wait_stores();
@@ -581,99 +622,104 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
     const uint32_t s_at = tmem, dp_at = tmem + kTile, dv_at = tmem + 2 * kTile, dk_at = tmem + 3 * kTile;
     volatile uint32_t *const failed = &S.failed;
 
-    if (warp == kLoadWarp && lane == 0 && n > 0) {
-        Ring r;
-        bar_expect(smem_addr(&S.stay), 2 * kBytes);
-#pragma unroll
-        for (int x = 0; x < kDim; x += 64) {
-            load_box(base + x / 64 * (kTile * 128), &M.k, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
-            load_box(base + kBytes + x / 64 * (kTile * 128), &M.v, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
-        }
-        int sent = 0;
-        for (int j = 0; j < 2 * n; ++j) {
-            if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
-            const int g = j / 2 / per, tile = from + j / 2 - g * per;
-            load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.d_o : &M.q, Q.first + tile * kTile, at.head * P.group + g, Q.at, smem_addr(&S.full[r.slot]));
-            ++sent;
-            r.next<kSlots>();
-        }
-        if (*failed) {
-            settle(smem_addr(&S.stay), 0);
-            for (int j = max(0, sent - kSlots); j < sent; ++j) settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
-        }
-    } else if (warp == kProductWarp && lane == 0 && n > 0) {
-        const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
-        const auto slot = [](int load) { return load % kSlots; };
-        const auto ready = [&](int load) { return bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed); };
-        const auto whole = [&](int j) { return bar_wait(smem_addr(&S.stats[j % 2]), j / 2 & 1, failed); };
-        bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && ready(0) && ready(1) && whole(0);
-        if (ok) {
-            product_scores<kDim>(s_at, base, ring, scores);
-            commit(smem_addr(&S.score[0]));
-            product_scores<kDim>(dp_at, base + kBytes, ring + kBytes, plain);
-            commit(smem_addr(&S.second[0]));
-        }
-        for (int j = 0; ok && j < n; ++j) {
-            ok = bar_wait(smem_addr(&S.prob[0]), j & 1, failed) && (j + 1 == n || (ready(2 * j + 2) && whole(j + 1)));
-            if (!ok) break;
-            fence_after();
-            product_apply<kDim>(dv_at, s_at, s_at + 64, ring + slot(2 * j + 1) * kBytes, j > 0);
-            commit(smem_addr(&S.empty[slot(2 * j + 1)]));
-            if (j + 1 < n) {
-                product_scores<kDim>(s_at, base, ring + slot(2 * j + 2) * kBytes, scores);
-                commit(smem_addr(&S.score[0]));
+    if (warp >= 2 * kGroupWarps) {
+        registers_few();
+        if (warp == kLoadWarp && lane == 0 && n > 0) {
+            Ring r;
+            bar_expect(smem_addr(&S.stay), 2 * kBytes);
+    #pragma unroll
+            for (int x = 0; x < kDim; x += 64) {
+                load_box(base + x / 64 * (kTile * 128), &M.k, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
+                load_box(base + kBytes + x / 64 * (kTile * 128), &M.v, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
             }
-            ok = bar_wait(smem_addr(&S.grad), j & 1, failed) && (j + 1 == n || ready(2 * j + 3));
-            if (!ok) break;
-            fence_after();
-            product_apply<kDim>(dk_at, dp_at, dp_at + 64, ring + slot(2 * j) * kBytes, j > 0);
-            commit(smem_addr(&S.empty[slot(2 * j)]));
-            if (j + 1 < n) {
-                product_scores<kDim>(dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+            int sent = 0;
+            for (int j = 0; j < 2 * n; ++j) {
+                if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+                const int g = j / 2 / per, tile = from + j / 2 - g * per;
+                load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.d_o : &M.q, Q.first + tile * kTile, at.head * P.group + g, Q.at, smem_addr(&S.full[r.slot]));
+                ++sent;
+                r.next<kSlots>();
+            }
+            if (*failed) {
+                settle(smem_addr(&S.stay), 0);
+                for (int j = max(0, sent - kSlots); j < sent; ++j) settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
+            }
+        } else if (warp == kProductWarp && lane == 0 && n > 0) {
+            const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
+            const auto slot = [](int load) { return load % kSlots; };
+            const auto ready = [&](int load) { return bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed); };
+            const auto whole = [&](int j) { return bar_wait(smem_addr(&S.stats[j % 2]), j / 2 & 1, failed); };
+            bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && ready(0) && ready(1) && whole(0);
+            if (ok) {
+                product_scores<kDim>(s_at, base, ring, scores);
+                commit(smem_addr(&S.score[0]));
+                product_scores<kDim>(dp_at, base + kBytes, ring + kBytes, plain);
                 commit(smem_addr(&S.second[0]));
             }
-        }
-        if (ok) commit(smem_addr(&S.done));
-        commit(smem_addr(&S.drain));
-        settle(smem_addr(&S.drain), 0);
-    } else if (warp == kHelpWarp) {
-        // row statistics of each query tile, and zeros past the sample's end in the tile that holds it
-        for (int j = 0; j < n; ++j) {
-            const int g = j / per, tile = from + j - g * per, b = j % 2;
-            float l[4], d[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int i = tile * kTile + x * 32 + lane;
-                l[x] = INFINITY;                 // no such query, or one that sees nothing: p = exp2(-inf) = 0
-                d[x] = 0.0f;
-                if (i < Q.n) {
-                    const int64_t s = stat_at(P, Q, i, at.head * P.group + g);
-                    l[x] = P.lse[s] * kLog2e;
-                    d[x] = P.row_dot[s];
-                    if (l[x] == -INFINITY) l[x] = INFINITY;
+            for (int j = 0; ok && j < n; ++j) {
+                ok = bar_wait(smem_addr(&S.prob[0]), j & 1, failed) && (j + 1 == n || (ready(2 * j + 2) && whole(j + 1)));
+                if (!ok) break;
+                fence_after();
+                product_apply<kDim>(dv_at, s_at, s_at + 64, ring + slot(2 * j + 1) * kBytes, j > 0);
+                commit(smem_addr(&S.empty[slot(2 * j + 1)]));
+                if (j + 1 < n) {
+                    product_scores<kDim>(s_at, base, ring + slot(2 * j + 2) * kBytes, scores);
+                    commit(smem_addr(&S.score[0]));
+                }
+                ok = bar_wait(smem_addr(&S.grad), j & 1, failed) && (j + 1 == n || ready(2 * j + 3));
+                if (!ok) break;
+                fence_after();
+                product_apply<kDim>(dk_at, dp_at, dp_at + 64, ring + slot(2 * j) * kBytes, j > 0);
+                commit(smem_addr(&S.empty[slot(2 * j)]));
+                if (j + 1 < n) {
+                    product_scores<kDim>(dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+                    commit(smem_addr(&S.second[0]));
                 }
             }
-            bool ok = bar_wait(smem_addr(&S.stats_free[b]), (j / 2 & 1) ^ 1, failed);
-            if (ragged && tile == until - 1)
-                for (int load = 2 * j; ok && load < 2 * j + 2; ++load) {
-                    ok = bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
-                    if (ok) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, Q.n % kTile, lane);
+            if (ok) commit(smem_addr(&S.done));
+            commit(smem_addr(&S.drain));
+            settle(smem_addr(&S.drain), 0);
+        } else if (warp == kHelpWarp) {
+            // row statistics of each query tile, and zeros past the sample's end in the tile that holds it
+            for (int j = 0; j < n; ++j) {
+                const int g = j / per, tile = from + j - g * per, b = j % 2;
+                float l[4], d[4];
+    #pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int i = tile * kTile + x * 32 + lane;
+                    l[x] = INFINITY;                 // no such query, or one that sees nothing: p = exp2(-inf) = 0
+                    d[x] = 0.0f;
+                    if (i < Q.n) {
+                        const int64_t s = stat_at(P, Q, i, at.head * P.group + g);
+                        l[x] = P.lse[s] * kLog2e;
+                        d[x] = P.row_dot[s];
+                        if (l[x] == -INFINITY) l[x] = INFINITY;
+                    }
                 }
-            if (!__all_sync(0xffffffffu, ok)) break;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                S.row[b][0][x * 32 + lane] = l[x];
-                S.row[b][1][x * 32 + lane] = d[x];
+                bool ok = bar_wait(smem_addr(&S.stats_free[b]), (j / 2 & 1) ^ 1, failed);
+                if (ragged && tile == until - 1)
+                    for (int load = 2 * j; ok && load < 2 * j + 2; ++load) {
+                        ok = bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
+                        if (ok) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, Q.n % kTile, lane);
+                    }
+                if (!__all_sync(0xffffffffu, ok)) break;
+    #pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    S.row[b][0][x * 32 + lane] = -l[x];
+                    S.row[b][1][x * 32 + lane] = -d[x];
+                }
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&S.stats[b]));
             }
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&S.stats[b]));
         }
-    } else if (warp < 2 * kGroupWarps) {
+    } else {
+        registers_many();
         const int t = warp / kGroupWarps, key = first + threadIdx.x % kTile;
         const uint32_t lanes = static_cast<uint32_t>(warp % kGroupWarps * 32) << 16;
         const uint32_t my_s = s_at + lanes + t * 64, my_dp = dp_at + lanes + t * 64;
         const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
+        const float2 by = make_float2(scale, scale);
         bool ok = true;
         for (int j = 0; ok && j < n; ++j) {
             const int tile = from + j % per, b = j % 2;
@@ -692,10 +738,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
 #pragma unroll
                 for (int x = 0; x < 32; x += 4) {
                     const float4 l = lse[c * 8 + x / 4];
-                    s[c][x] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x]), scale, -l.x)));
-                    s[c][x + 1] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x + 1]), scale, -l.y)));
-                    s[c][x + 2] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x + 2]), scale, -l.z)));
-                    s[c][x + 3] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c][x + 3]), scale, -l.w)));
+                    const float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, make_float2(l.x, l.y));
+                    const float2 f = fma2(make_float2(__uint_as_float(s[c][x + 2]), __uint_as_float(s[c][x + 3])), by, make_float2(l.z, l.w));
+                    s[c][x] = __float_as_uint(exp2_fast(e.x));
+                    s[c][x + 1] = __float_as_uint(exp2_fast(e.y));
+                    s[c][x + 2] = __float_as_uint(exp2_fast(f.x));
+                    s[c][x + 3] = __float_as_uint(exp2_fast(f.y));
                 }
             // under the causal mask the queries from key - off on see this key
             const int begin = P.causal ? key - off - tile * kTile - t * 64 : 0;
@@ -731,10 +779,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
 #pragma unroll
                 for (int x = 0; x < 32; x += 4) {
                     const float4 e = dot[c * 8 + x / 4];
-                    w[x / 2] = pack_bf16(__uint_as_float(s[c][x]) * (__uint_as_float(d[c][x]) - e.x),
-                                         __uint_as_float(s[c][x + 1]) * (__uint_as_float(d[c][x + 1]) - e.y));
-                    w[x / 2 + 1] = pack_bf16(__uint_as_float(s[c][x + 2]) * (__uint_as_float(d[c][x + 2]) - e.z),
-                                             __uint_as_float(s[c][x + 3]) * (__uint_as_float(d[c][x + 3]) - e.w));
+                    const float2 f = mul2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])),
+                                          add2(make_float2(__uint_as_float(d[c][x]), __uint_as_float(d[c][x + 1])), make_float2(e.x, e.y)));
+                    const float2 h = mul2(make_float2(__uint_as_float(s[c][x + 2]), __uint_as_float(s[c][x + 3])),
+                                          add2(make_float2(__uint_as_float(d[c][x + 2]), __uint_as_float(d[c][x + 3])), make_float2(e.z, e.w)));
+                    w[x / 2] = pack_bf16(f.x, f.y);
+                    w[x / 2 + 1] = pack_bf16(h.x, h.y);
                 }
                 store_columns(my_dp + c * 16, w);
             }
