@@ -163,8 +163,8 @@ int loco_router_backward(const loco_router_t *cfg, int64_t tokens, const void *d
 
 /*
  * Flags raised on the current device since the library was loaded; SYNCHRONISES `stream`.  The attention kernels wait on
- * their own copies and products, never on another block; a wait that exceeds two seconds gives up, the block leaves its
- * outputs unwritten and the flag is raised.
+ * their own copies and products, never on another block; a wait that exceeds two seconds gives up, the outputs of its
+ * block are meaningless and the flag is raised.
  */
 #define LOCO_LAYER_FLAG_TIMEOUT 1u
 int loco_layer_status(uint32_t *flags, void *stream);

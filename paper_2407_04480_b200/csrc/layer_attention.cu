@@ -41,8 +41,8 @@ struct Maps { CUtensorMap q, k, v, d_o; };
 // Shared memory: two tiles that stay, the ring of tiles that stream, then Shared.  Either head size fills the SM, so that no
 // two blocks compete for its tensor memory.
 template <int kDim> __host__ __device__ constexpr int tile_bytes() { return kTile * kDim * 2; }
-template <int kDim> __host__ __device__ constexpr int stream_slots() { return kDim == 128 ? 4 : 8; }
-constexpr int kMaxSlots = 8;
+template <int kDim> __host__ __device__ constexpr int stream_slots() { return kDim == 128 ? 5 : 10; }
+constexpr int kMaxSlots = 10;
 struct Shared {
     uint64_t full[kMaxSlots], empty[kMaxSlots];  // streaming tiles: copied, no longer read
     uint64_t stay;                               // the tiles that stay are copied
@@ -55,8 +55,9 @@ struct Shared {
     alignas(16) float row[2][2][kTile];          // backward keys: -lse * log2(e), -D of the query tile; backward queries: D
 };
 template <int kDim> constexpr int shared_bytes() {
-    return (2 + stream_slots<kDim>()) * tile_bytes<kDim>() + static_cast<int>(sizeof(Shared)) + 1024;
+    return (2 + stream_slots<kDim>()) * tile_bytes<kDim>() + static_cast<int>(sizeof(Shared));
 }
+static_assert(shared_bytes<128>() <= 227 * 1024 && shared_bytes<64>() <= 227 * 1024, "shared memory of a block");
 
 template <int kDim> __device__ __forceinline__ void load_tile(uint32_t to, const CUtensorMap *map, int row, int head, int batch, uint32_t bar) {
     bar_expect(bar, tile_bytes<kDim>());
@@ -72,19 +73,21 @@ template <int kDim> __device__ __forceinline__ void clean_tile(uint8_t *tile, in
 }
 
 // S (128 x 128) = A B^T over kDim columns, both tiles in shared memory.
-template <int kDim> __device__ __forceinline__ void product_scores(uint32_t d, uint32_t a, uint32_t b, uint32_t word) {
+template <int kDim> __device__ __forceinline__ void product_scores(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t word) {
+    const uint32_t da = desc_along_columns(a), db = desc_along_columns(b);
 #pragma unroll
     for (int x = 0; x < kDim; x += 16) {
-        const uint32_t off = x / 64 * (kTile * 128) + x % 64 * 2;
-        mma_ss(d, desc_along_columns(a + off), desc_along_columns(b + off), word, x > 0);
+        const uint32_t off = (x / 64 * (kTile * 128) + x % 64 * 2) >> 4;
+        mma_ss(lead, d, da + off, db + off, word, x > 0);
     }
 }
 // d (128 x kDim) += A B: A (128 x 128) in TMEM, its columns at `a0` (first 64) and `a1`; B's rows are the tile's.
-template <int kDim> __device__ __forceinline__ void product_apply(uint32_t d, uint32_t a0, uint32_t a1, uint32_t b, uint32_t accumulate) {
+template <int kDim> __device__ __forceinline__ void product_apply(uint32_t lead, uint32_t d, uint32_t a0, uint32_t a1, uint32_t b, uint32_t accumulate) {
     constexpr uint32_t word = product(kDim, true);
+    const uint32_t db = desc_along_rows(b, kTile * 128);
 #pragma unroll
     for (int r = 0; r < kTile; r += 16)
-        mma_ts(d, (r < 64 ? a0 : a1) + r % 64 / 2, desc_along_rows(b + r * 128, kTile * 128), word, accumulate | (r > 0));
+        mma_ts(lead, d, (r < 64 ? a0 : a1) + r % 64 / 2, db + (r * 128 >> 4), word, accumulate | (r > 0));
 }
 
 // Sets up barriers and TMEM; returns the TMEM base.
@@ -135,7 +138,7 @@ __device__ __forceinline__ void registers_few() { asm volatile("setmaxnreg.dec.s
 // A role that gave up still waits for the copies it started before the block's shared memory goes away.
 __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
     const uint64_t begin = now_ns();
-    while (!bar_test(bar, parity) && now_ns() - begin < kWaitLimitNs) {}
+    while (!bar_test(bar, parity) && now_ns() - begin < kWaitLimitNs / 20) {}
 }
 
 // Ring of streaming tiles, seen by the thread that fills it and the one that empties it.
@@ -210,11 +213,10 @@ __device__ __forceinline__ float row_max(const uint32_t (&s)[32]) {
 template <int kDim>
 __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
     constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
-    extern __shared__ uint8_t raw[];
-    uint8_t *const tiles = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+    extern __shared__ __align__(1024) uint8_t tiles[];
     Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.causal);
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * 2 * kTile, head_kv = at.head / P.group;
@@ -236,7 +238,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
                         load_box(base + t * kBytes + x / 64 * (kTile * 128), &M.q, x, Q.first + first + t * kTile, at.head, Q.at, smem_addr(&S.stay));
             int sent = 0;
             for (int j = 0; j < 2 * n; ++j) {
-                if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+                bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed);
+                if (*failed) break;
                 load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
                                 smem_addr(ragged && j >= 2 * n - 1 ? &S.last : &S.full[r.slot]));
                 ++sent;
@@ -248,56 +251,55 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
                     if (ragged && j >= 2 * n - 1) settle(smem_addr(&S.last), 0);
                     else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
             }
-        } else if (warp == kProductWarp && lane == 0 && n > 0) {
+        } else if (warp == kProductWarp && n > 0) {
+            const uint32_t lead = elect_lane();
             const uint32_t scores = product(kTile, false, P.scale < 0.0f);
-            bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && bar_wait(smem_addr(&S.full[0]), 0, failed);
-            if (ok) {
-                for (int t = 0; t < 2; ++t)
-                    if ((t ? n1 : n0) > 0) {
-                        product_scores<kDim>(tmem + t * kTile, base + t * kBytes, ring, scores);
-                        commit(smem_addr(&S.score[t]));
-                    }
-                commit(smem_addr(&S.empty[0]));
-            }
-            Ring v, k;                               // value tiles at odd places of the ring, key tiles at even ones
+            bar_wait(smem_addr(&S.stay), 0, failed);
+            bar_wait(smem_addr(&S.full[0]), 0, failed);
+            for (int t = 0; t < 2; ++t)
+                if ((t ? n1 : n0) > 0) {
+                    product_scores<kDim>(lead, tmem + t * kTile, base + t * kBytes, ring, scores);
+                    commit(lead, smem_addr(&S.score[t]));
+                }
+            commit(lead, smem_addr(&S.empty[0]));
+            Ring v, k;                               // value tiles at odd places of the stream, key tiles at even ones
             v.next<kSlots>();
             k.next<kSlots>();
             k.next<kSlots>();
-            for (int j = 0; ok && j < n; ++j) {
-                ok = (ragged && j == n - 1 ? bar_wait(smem_addr(&S.clean), 0, failed) : bar_wait(smem_addr(&S.full[v.slot]), v.phase, failed)) &&
-                     (j + 1 == n || bar_wait(smem_addr(&S.full[k.slot]), k.phase, failed));
-                for (int t = 0; ok && t < 2; ++t) {
+            for (int j = 0; j < n; ++j) {
+                if (ragged && j == n - 1) bar_wait(smem_addr(&S.clean), 0, failed);
+                else bar_wait(smem_addr(&S.full[v.slot]), v.phase, failed);
+                if (j + 1 < n) bar_wait(smem_addr(&S.full[k.slot]), k.phase, failed);
+                for (int t = 0; t < 2; ++t) {
                     const int nt = t ? n1 : n0;
                     if (j >= nt) continue;
-                    ok = bar_wait(smem_addr(&S.prob[t]), j & 1, failed);
-                    if (!ok) break;
+                    bar_wait(smem_addr(&S.prob[t]), j & 1, failed);
                     fence_after();
                     const uint32_t p = tmem + t * kTile;
-                    product_apply<kDim>(tmem + 2 * kTile + t * kTile, p, p + 32, ring + v.slot * kBytes, j > 0);
-                    commit(smem_addr(&S.second[t]));
+                    product_apply<kDim>(lead, tmem + 2 * kTile + t * kTile, p, p + 32, ring + v.slot * kBytes, j > 0);
+                    commit(lead, smem_addr(&S.second[t]));
                     if (j + 1 < nt) {
-                        product_scores<kDim>(p, base + t * kBytes, ring + k.slot * kBytes, scores);
-                        commit(smem_addr(&S.score[t]));
+                        product_scores<kDim>(lead, p, base + t * kBytes, ring + k.slot * kBytes, scores);
+                        commit(lead, smem_addr(&S.score[t]));
                     }
                 }
-                if (!ok) break;
-                commit(smem_addr(&S.empty[v.slot]));
-                if (j + 1 < n) commit(smem_addr(&S.empty[k.slot]));
+                commit(lead, smem_addr(&S.empty[v.slot]));
+                if (j + 1 < n) commit(lead, smem_addr(&S.empty[k.slot]));
                 for (int i = 0; i < 2; ++i) {
                     v.next<kSlots>();
                     k.next<kSlots>();
                 }
             }
-            commit(smem_addr(&S.drain));
-            settle(smem_addr(&S.drain), 0);
+            commit(lead, smem_addr(&S.drain));
+            bar_wait(smem_addr(&S.drain), 0, failed);
+            if (*failed) settle(smem_addr(&S.drain), 0);
         } else if (warp == kHelpWarp && ragged) {
             const int load = 2 * n - 1;              // the last value tile
-            if (bar_wait(smem_addr(&S.last), 0, failed)) {
-                clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
-                fence_async_shared();
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_addr(&S.clean));
-            }
+            bar_wait(smem_addr(&S.last), 0, failed);
+            clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.clean));
         }
     } else {
         registers_many();
@@ -308,10 +310,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
         const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
         const float room = 8.0f / scale;         // how far the maximum may grow before o is rescaled
         float top = -INFINITY, total = 0.0f;
-        bool ok = true;
-        for (int j = 0; ok && j < nt; ++j) {
-            ok = bar_wait(smem_addr(&S.score[t]), j & 1, failed);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        for (int j = 0; j < nt; ++j) {
+            bar_wait(smem_addr(&S.score[t]), j & 1, failed);
+            __syncwarp();
             fence_after();
             uint32_t s[4][32];
             load_columns(s_at, s[0]);
@@ -341,8 +342,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
             } else if (__any_sync(0xffffffffu, most - top > room)) {
                 const float next = fmaxf(top, most);
                 const float fade = next == -INFINITY ? 1.0f : exp2_fast((top - next) * scale);
-                ok = bar_wait(smem_addr(&S.second[t]), (j - 1) & 1, failed);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                bar_wait(smem_addr(&S.second[t]), (j - 1) & 1, failed);
+                __syncwarp();
                 fence_after();
 #pragma unroll
                 for (int c = 0; c < kDim / 32; ++c) {
@@ -380,8 +381,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
             __syncwarp();
             if (lane == 0) bar_arrive(smem_addr(&S.prob[t]));
         }
-        if (ok && nt > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&S.second[t]), (nt - 1) & 1, failed));
-        if (ok) {
+        if (nt > 0) bar_wait(smem_addr(&S.second[t]), (nt - 1) & 1, failed);
+        __syncwarp();
+        {
             const bool wanted = i < (P.packed ? Q.n : P.seq_q);
             const float by = total > 0.0f || total != total ? 1.0f / total : 0.0f;
             __nv_bfloat16 *o = row_of(P.o, Q, i, at.head);
@@ -412,11 +414,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
 template <int kDim>
 __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
     constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
-    extern __shared__ uint8_t raw[];
-    uint8_t *const tiles = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+    extern __shared__ __align__(1024) uint8_t tiles[];
     Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + kTile - 1) / kTile, P.causal);
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * kTile, head_kv = at.head / P.group;
@@ -439,7 +440,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
             }
             int sent = 0;
             for (int j = 0; j < 2 * n; ++j) {
-                if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+                bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed);
+                if (*failed) break;
                 load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
                                 smem_addr(ragged && j >= 2 * n - 2 ? &S.last : &S.full[r.slot]));
                 ++sent;
@@ -451,51 +453,51 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
                     if (ragged && j >= 2 * n - 2) settle(smem_addr(&S.last), 0);
                     else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
             }
-        } else if (warp == kProductWarp && lane == 0 && n > 0) {
+        } else if (warp == kProductWarp && n > 0) {
+            const uint32_t lead = elect_lane();
             const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
             // tile j: keys at place 2j of the ring, values at 2j + 1
             const auto slot = [](int load) { return load % kSlots; };
             const auto ready = [&](int load) {
-                return ragged && load >= 2 * n - 2 ? bar_wait(smem_addr(&S.clean), 0, failed)
-                                                   : bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
+                if (ragged && load >= 2 * n - 2) bar_wait(smem_addr(&S.clean), 0, failed);
+                else bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
             };
-            bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && ready(0) && ready(1);
-            if (ok) {
-                product_scores<kDim>(tmem, base, ring, scores);
-                commit(smem_addr(&S.score[0]));
-                product_scores<kDim>(dp_at, base + kBytes, ring + kBytes, plain);
-                commit(smem_addr(&S.second[0]));
-                commit(smem_addr(&S.empty[1]));
-            }
-            for (int j = 0; ok && j < n; ++j) {
+            bar_wait(smem_addr(&S.stay), 0, failed);
+            ready(0);
+            product_scores<kDim>(lead, tmem, base, ring, scores);
+            commit(lead, smem_addr(&S.score[0]));
+            ready(1);
+            product_scores<kDim>(lead, dp_at, base + kBytes, ring + kBytes, plain);
+            commit(lead, smem_addr(&S.second[0]));
+            commit(lead, smem_addr(&S.empty[1]));
+            for (int j = 0; j < n; ++j) {
                 if (j + 1 < n) {
-                    ok = ready(2 * j + 2);
-                    if (!ok) break;
-                    product_scores<kDim>(tmem + (j + 1) % 2 * kTile, base, ring + slot(2 * j + 2) * kBytes, scores);
-                    commit(smem_addr(&S.score[(j + 1) % 2]));
+                    ready(2 * j + 2);
+                    product_scores<kDim>(lead, tmem + (j + 1) % 2 * kTile, base, ring + slot(2 * j + 2) * kBytes, scores);
+                    commit(lead, smem_addr(&S.score[(j + 1) % 2]));
                 }
-                ok = bar_wait(smem_addr(&S.grad), j & 1, failed) && (j + 1 == n || ready(2 * j + 3));
-                if (!ok) break;
+                bar_wait(smem_addr(&S.grad), j & 1, failed);
+                if (j + 1 < n) ready(2 * j + 3);
                 fence_after();
                 if (j + 1 < n) {
-                    product_scores<kDim>(dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
-                    commit(smem_addr(&S.second[0]));
-                    commit(smem_addr(&S.empty[slot(2 * j + 3)]));
+                    product_scores<kDim>(lead, dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+                    commit(lead, smem_addr(&S.second[0]));
+                    commit(lead, smem_addr(&S.empty[slot(2 * j + 3)]));
                 }
                 const uint32_t ds = tmem + j % 2 * kTile;
-                product_apply<kDim>(dq_at, ds, ds + 64, ring + slot(2 * j) * kBytes, j > 0);
-                commit(smem_addr(&S.empty[slot(2 * j)]));
+                product_apply<kDim>(lead, dq_at, ds, ds + 64, ring + slot(2 * j) * kBytes, j > 0);
+                commit(lead, smem_addr(&S.empty[slot(2 * j)]));
             }
-            if (ok) commit(smem_addr(&S.done));
-            commit(smem_addr(&S.drain));
-            settle(smem_addr(&S.drain), 0);
+            commit(lead, smem_addr(&S.done));
+            commit(lead, smem_addr(&S.drain));
+            bar_wait(smem_addr(&S.drain), 0, failed);
+            if (*failed) settle(smem_addr(&S.drain), 0);
         } else if (warp == kHelpWarp && ragged) {
-            if (bar_wait(smem_addr(&S.last), 0, failed)) {
-                for (int load = 2 * n - 2; load < 2 * n; ++load) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
-                fence_async_shared();
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_addr(&S.clean));
-            }
+            bar_wait(smem_addr(&S.last), 0, failed);
+            for (int load = 2 * n - 2; load < 2 * n; ++load) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.clean));
         }
     } else {
         registers_many();
@@ -525,11 +527,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
         }
         if (t == 0 && wanted) P.row_dot[stat_at(P, Q, i, at.head)] = dot;
         const float2 by = make_float2(scale, scale), minus = make_float2(-shift, -shift), less = make_float2(-dot, -dot);
-        bool ok = true;
-        for (int j = 0; ok && j < n; ++j) {
+        for (int j = 0; j < n; ++j) {
             const uint32_t s_at = tmem + lanes + j % 2 * kTile + t * 64;
-            ok = bar_wait(smem_addr(&S.score[j % 2]), j / 2 & 1, failed);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            bar_wait(smem_addr(&S.score[j % 2]), j / 2 & 1, failed);
+            __syncwarp();
             fence_after();
             uint32_t s[2][32], d[2][32];
 #pragma unroll
@@ -553,8 +554,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
                     for (int x = 0; x < 32; ++x)
                         if (c * 32 + x >= left) s[c][x] = 0;
             }
-            ok = bar_wait(smem_addr(&S.second[0]), j & 1, failed);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            bar_wait(smem_addr(&S.second[0]), j & 1, failed);
+            __syncwarp();
             fence_after();
 #pragma unroll
             for (int c = 0; c < 2; ++c) load_columns(dp_at + lanes + t * 64 + c * 32, d[c]);
@@ -577,8 +578,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
             __syncwarp();
             if (lane == 0) bar_arrive(smem_addr(&S.grad));
         }
-        if (ok && n > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&S.done), 0, failed));
-        if (ok) {
+        if (n > 0) bar_wait(smem_addr(&S.done), 0, failed);
+        __syncwarp();
+        {
             __nv_bfloat16 *dq = row_of(P.dq, Q, i, at.head);
             if (n > 0) {
                 fence_after();
@@ -604,11 +606,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
 template <int kDim>
 __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
     constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
-    extern __shared__ uint8_t raw[];
-    uint8_t *const tiles = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+    extern __shared__ __align__(1024) uint8_t tiles[];
     Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P.heads_kv, P.batch, (P.max_k + kTile - 1) / kTile, false);
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * kTile;
@@ -634,7 +635,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             }
             int sent = 0;
             for (int j = 0; j < 2 * n; ++j) {
-                if (!bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed)) break;
+                bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed);
+                if (*failed) break;
                 const int g = j / 2 / per, tile = from + j / 2 - g * per;
                 load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.d_o : &M.q, Q.first + tile * kTile, at.head * P.group + g, Q.at, smem_addr(&S.full[r.slot]));
                 ++sent;
@@ -644,41 +646,45 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
                 settle(smem_addr(&S.stay), 0);
                 for (int j = max(0, sent - kSlots); j < sent; ++j) settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
             }
-        } else if (warp == kProductWarp && lane == 0 && n > 0) {
+        } else if (warp == kProductWarp && n > 0) {
+            const uint32_t lead = elect_lane();
             const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
             const auto slot = [](int load) { return load % kSlots; };
-            const auto ready = [&](int load) { return bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed); };
-            const auto whole = [&](int j) { return bar_wait(smem_addr(&S.stats[j % 2]), j / 2 & 1, failed); };
-            bool ok = bar_wait(smem_addr(&S.stay), 0, failed) && ready(0) && ready(1) && whole(0);
-            if (ok) {
-                product_scores<kDim>(s_at, base, ring, scores);
-                commit(smem_addr(&S.score[0]));
-                product_scores<kDim>(dp_at, base + kBytes, ring + kBytes, plain);
-                commit(smem_addr(&S.second[0]));
-            }
-            for (int j = 0; ok && j < n; ++j) {
-                ok = bar_wait(smem_addr(&S.prob[0]), j & 1, failed) && (j + 1 == n || (ready(2 * j + 2) && whole(j + 1)));
-                if (!ok) break;
+            const auto ready = [&](int load) { bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed); };
+            const auto whole = [&](int j) { bar_wait(smem_addr(&S.stats[j % 2]), j / 2 & 1, failed); };
+            bar_wait(smem_addr(&S.stay), 0, failed);
+            whole(0);
+            ready(0);
+            product_scores<kDim>(lead, s_at, base, ring, scores);
+            commit(lead, smem_addr(&S.score[0]));
+            ready(1);
+            product_scores<kDim>(lead, dp_at, base + kBytes, ring + kBytes, plain);
+            commit(lead, smem_addr(&S.second[0]));
+            for (int j = 0; j < n; ++j) {
+                bar_wait(smem_addr(&S.prob[0]), j & 1, failed);
                 fence_after();
-                product_apply<kDim>(dv_at, s_at, s_at + 64, ring + slot(2 * j + 1) * kBytes, j > 0);
-                commit(smem_addr(&S.empty[slot(2 * j + 1)]));
+                product_apply<kDim>(lead, dv_at, s_at, s_at + 64, ring + slot(2 * j + 1) * kBytes, j > 0);
+                commit(lead, smem_addr(&S.empty[slot(2 * j + 1)]));
                 if (j + 1 < n) {
-                    product_scores<kDim>(s_at, base, ring + slot(2 * j + 2) * kBytes, scores);
-                    commit(smem_addr(&S.score[0]));
+                    whole(j + 1);
+                    ready(2 * j + 2);
+                    product_scores<kDim>(lead, s_at, base, ring + slot(2 * j + 2) * kBytes, scores);
+                    commit(lead, smem_addr(&S.score[0]));
                 }
-                ok = bar_wait(smem_addr(&S.grad), j & 1, failed) && (j + 1 == n || ready(2 * j + 3));
-                if (!ok) break;
+                bar_wait(smem_addr(&S.grad), j & 1, failed);
                 fence_after();
-                product_apply<kDim>(dk_at, dp_at, dp_at + 64, ring + slot(2 * j) * kBytes, j > 0);
-                commit(smem_addr(&S.empty[slot(2 * j)]));
+                product_apply<kDim>(lead, dk_at, dp_at, dp_at + 64, ring + slot(2 * j) * kBytes, j > 0);
+                commit(lead, smem_addr(&S.empty[slot(2 * j)]));
                 if (j + 1 < n) {
-                    product_scores<kDim>(dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
-                    commit(smem_addr(&S.second[0]));
+                    ready(2 * j + 3);
+                    product_scores<kDim>(lead, dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+                    commit(lead, smem_addr(&S.second[0]));
                 }
             }
-            if (ok) commit(smem_addr(&S.done));
-            commit(smem_addr(&S.drain));
-            settle(smem_addr(&S.drain), 0);
+            commit(lead, smem_addr(&S.done));
+            commit(lead, smem_addr(&S.drain));
+            bar_wait(smem_addr(&S.drain), 0, failed);
+            if (*failed) settle(smem_addr(&S.drain), 0);
         } else if (warp == kHelpWarp) {
             // row statistics of each query tile, and zeros past the sample's end in the tile that holds it
             for (int j = 0; j < n; ++j) {
@@ -696,13 +702,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
                         if (l[x] == -INFINITY) l[x] = INFINITY;
                     }
                 }
-                bool ok = bar_wait(smem_addr(&S.stats_free[b]), (j / 2 & 1) ^ 1, failed);
+                bar_wait(smem_addr(&S.stats_free[b]), (j / 2 & 1) ^ 1, failed);
                 if (ragged && tile == until - 1)
-                    for (int load = 2 * j; ok && load < 2 * j + 2; ++load) {
-                        ok = bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
-                        if (ok) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, Q.n % kTile, lane);
+                    for (int load = 2 * j; load < 2 * j + 2; ++load) {
+                        bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
+                        clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, Q.n % kTile, lane);
                     }
-                if (!__all_sync(0xffffffffu, ok)) break;
     #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     S.row[b][0][x * 32 + lane] = -l[x];
@@ -720,12 +725,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
         const uint32_t my_s = s_at + lanes + t * 64, my_dp = dp_at + lanes + t * 64;
         const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
         const float2 by = make_float2(scale, scale);
-        bool ok = true;
-        for (int j = 0; ok && j < n; ++j) {
+        for (int j = 0; j < n; ++j) {
             const int tile = from + j % per, b = j % 2;
             const float4 *lse = reinterpret_cast<const float4 *>(S.row[b][0] + t * 64), *dot = reinterpret_cast<const float4 *>(S.row[b][1] + t * 64);
-            ok = bar_wait(smem_addr(&S.stats[b]), j / 2 & 1, failed) && bar_wait(smem_addr(&S.score[0]), j & 1, failed);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            bar_wait(smem_addr(&S.stats[b]), j / 2 & 1, failed);
+            bar_wait(smem_addr(&S.score[0]), j & 1, failed);
+            __syncwarp();
             fence_after();
             uint32_t s[2][32], d[2][32];
 #pragma unroll
@@ -765,8 +770,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(smem_addr(&S.prob[0]));
-            ok = bar_wait(smem_addr(&S.second[0]), j & 1, failed);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            bar_wait(smem_addr(&S.second[0]), j & 1, failed);
+            __syncwarp();
             fence_after();
 #pragma unroll
             for (int c = 0; c < 2; ++c) load_columns(my_dp + c * 32, d[c]);
@@ -796,8 +801,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
                 bar_arrive(smem_addr(&S.stats_free[b]));
             }
         }
-        if (ok && n > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&S.done), 0, failed));
-        if (ok) {
+        if (n > 0) bar_wait(smem_addr(&S.done), 0, failed);
+        __syncwarp();
+        {
             // the first group writes dv, the second dk
             const bool wanted = key < (P.packed ? K.n : P.seq_k);
             __nv_bfloat16 *out = t ? row_of(P.dk, K, key, at.head) : row_of(P.dv, K, key, at.head);

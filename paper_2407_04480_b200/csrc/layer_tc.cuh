@@ -36,22 +36,17 @@ __device__ __forceinline__ uint64_t now_ns() {
 
 constexpr uint64_t kWaitLimitNs = 2000000000ull;      // a wait longer than this gives up
 
-// Waits for the phase; false once the limit is reached or another role of the block has given up.
-__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
+// Waits for the phase.  Past the limit it raises `failed` and returns; from then on every wait of the block returns at
+// once, so that all its roles run to their ends (on meaningless values) and nothing hangs.
+__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
+    if (bar_test(bar, parity)) return;
     const uint64_t begin = now_ns();
     for (;;) {
         for (int i = 0; i < 64; ++i)
-            if (bar_test(bar, parity)) return true;
-        if (*failed) return false;
-        if (now_ns() - begin > kWaitLimitNs) {
-            *failed = 1;
-            return false;
-        }
+            if (bar_test(bar, parity)) return;
+        if (*failed) return;
+        if (now_ns() - begin > kWaitLimitNs) *failed = 1;
     }
-}
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
-    if (bar_test(bar, parity)) return true;
-    return bar_wait_slow(bar, parity, failed);
 }
 
 // Order generic writes to shared memory before reads of the tensor core and the copy engine.
@@ -117,16 +112,12 @@ __device__ __forceinline__ void wait_stores() { asm volatile("tcgen05.wait::st.s
 
 // Operand tiles are [columns / 64][rows][64] bfloat16 with the copy engine's 128-byte swizzle: rows of 128 bytes, groups of
 // 8 rows of 1024.  Descriptor fields in 16-byte units: address 0-13, leading offset 16-29, stride 32-45, version 1 at 46,
-// swizzle 128 B = 2 at 61.
-constexpr uint64_t kDescBase = (1ull << 46) | (2ull << 61);
+// swizzle 128 B = 2 at 61.  Only the low word depends on the tile.
+constexpr uint32_t kDescHigh = (1024 >> 4) | (1u << 14) | (2u << 29);
 // contraction along the columns: 8-row groups 1024 bytes apart
-__device__ __forceinline__ uint64_t desc_along_columns(uint32_t addr) {
-    return kDescBase | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 16) | ((addr & 0x3ffff) >> 4);
-}
+__device__ __forceinline__ uint32_t desc_along_columns(uint32_t addr) { return (1u << 16) | (addr >> 4); }
 // contraction along the rows: 8-row groups 1024 bytes apart, 64-column blocks `block` bytes apart
-__device__ __forceinline__ uint64_t desc_along_rows(uint32_t addr, uint32_t block) {
-    return kDescBase | (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(block >> 4) << 16) | ((addr & 0x3ffff) >> 4);
-}
+__device__ __forceinline__ uint32_t desc_along_rows(uint32_t addr, uint32_t block) { return ((block >> 4) << 16) | (addr >> 4); }
 
 // Instruction word: fp32 accumulators, bfloat16 operands, 128 x n.
 __host__ __device__ constexpr uint32_t product(int n, bool b_along_rows, bool negate = false) {
@@ -134,18 +125,29 @@ __host__ __device__ constexpr uint32_t product(int n, bool b_along_rows, bool ne
            (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
 }
 
-// One 128 x n x 16 step, by one thread; both operands in shared memory, or A in tensor memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t word, uint32_t accumulate) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                 ::"r"(d), "l"(a), "l"(b), "r"(word), "r"(accumulate) : "memory");
+// One lane of the warp.  The products' operands live in uniform registers: the whole warp runs the issuing code and the
+// instruction itself is predicated, since in code that only one lane runs every operand would have to be moved there first.
+__device__ __forceinline__ uint32_t elect_lane() {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r;
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t word, uint32_t accumulate) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-                 ::"r"(d), "r"(a), "l"(b), "r"(word), "r"(accumulate) : "memory");
+
+// One 128 x n x 16 step, by the elected lane; both operands in shared memory, or A in tensor memory.
+__device__ __forceinline__ void mma_ss(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t word, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p, q;\n .reg .b64 a, b;\n mov.b64 a, {%1, %6};\n mov.b64 b, {%2, %6};\n setp.ne.u32 p, %4, 0;\n setp.ne.u32 q, %5, 0;\n"
+                 " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "r"(b), "r"(word), "r"(accumulate), "r"(lead), "r"(kDescHigh) : "memory");
 }
-// Arrives on the barrier when every product this thread has issued is complete.
-__device__ __forceinline__ void commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t word, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p, q;\n .reg .b64 b;\n mov.b64 b, {%2, %6};\n setp.ne.u32 p, %4, 0;\n setp.ne.u32 q, %5, 0;\n"
+                 " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "r"(b), "r"(word), "r"(accumulate), "r"(lead), "r"(kDescHigh) : "memory");
+}
+// Arrives on the barrier when every product the elected lane has issued is complete.
+__device__ __forceinline__ void commit(uint32_t lead, uint32_t bar) {
+    asm volatile("{\n .reg .pred q;\n setp.ne.u32 q, %1, 0;\n @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n"
+                 ::"r"(bar), "r"(lead) : "memory");
 }
 
 // ---- small arithmetic ------------------------------------------------------------------------
