@@ -42,12 +42,12 @@ struct Maps { CUtensorMap q, k, v, d_o; };
 // two blocks compete for its tensor memory.
 template <int kDim> __host__ __device__ constexpr int tile_bytes() { return kTile * kDim * 2; }
 template <int kDim> __host__ __device__ constexpr int stream_slots() { return kDim == 128 ? 5 : 10; }
-constexpr int kMaxSlots = 10;
+constexpr int kMaxSlots = 12;
 struct Shared {
     uint64_t full[kMaxSlots], empty[kMaxSlots];  // streaming tiles: copied, no longer read
-    uint64_t stay;                               // the tiles that stay are copied
+    uint64_t stay, rows_in;                      // the tiles that stay are in shared memory, in TMEM
     uint64_t score[2], second[2];                // products ready: S per tile or buffer; o (forward) or dP (backward)
-    uint64_t prob[2], grad;                      // P, dS written to TMEM
+    uint64_t prob[2], grad;                      // P written to TMEM (backward queries: S read), dS written
     uint64_t last, clean;                        // a tile with rows past the end is copied; those rows are zero
     uint64_t stats[2], stats_free[2];            // backward keys: row statistics of a query tile
     uint64_t done, drain;
@@ -81,6 +81,12 @@ template <int kDim> __device__ __forceinline__ void product_scores(uint32_t lead
         mma_ss(lead, d, da + off, db + off, word, x > 0);
     }
 }
+// The same with A in TMEM, two dimensions to a column.
+template <int kDim> __device__ __forceinline__ void product_scores_tmem(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t word) {
+    const uint32_t db = desc_along_columns(b);
+#pragma unroll
+    for (int x = 0; x < kDim; x += 16) mma_ts(lead, d, a + x / 2, db + ((x / 64 * (kTile * 128) + x % 64 * 2) >> 4), word, x > 0);
+}
 // d (128 x kDim) += A B: A (128 x 128) in TMEM, its columns at `a0` (first 64) and `a1`; B's rows are the tile's.
 template <int kDim> __device__ __forceinline__ void product_apply(uint32_t lead, uint32_t d, uint32_t a0, uint32_t a1, uint32_t b, uint32_t accumulate) {
     constexpr uint32_t word = product(kDim, true);
@@ -107,6 +113,7 @@ template <int kColumns> __device__ __forceinline__ uint32_t begin_block(Shared &
         }
         bar_init(smem_addr(&S.grad), 2 * kGroupWarps);
         bar_init(smem_addr(&S.stay), 1);
+        bar_init(smem_addr(&S.rows_in), 2 * kGroupWarps);
         bar_init(smem_addr(&S.last), last_arrivals);
         bar_init(smem_addr(&S.clean), 1);
         bar_init(smem_addr(&S.done), 1);
@@ -164,6 +171,11 @@ template <int kDim> __device__ __forceinline__ void store_row(__nv_bfloat16 *to,
             *reinterpret_cast<uint4 *>(to + first + i) = w;
         }
     }
+}
+// c + the product of two pairs of bfloat16
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
+    c = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), c);
+    return fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), c);
 }
 __device__ __forceinline__ void zero_row(__nv_bfloat16 *to, int from, int until) {
     for (int i = from; i < until; i += 8) *reinterpret_cast<uint4 *>(to + i) = make_uint4(0, 0, 0, 0);
@@ -233,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
             bar_expect(smem_addr(&S.stay), (n0 > 0 ? kBytes : 0) + (n1 > 0 ? kBytes : 0));
             for (int t = 0; t < 2; ++t)
                 if ((t ? n1 : n0) > 0)
-    #pragma unroll
+#pragma unroll
                     for (int x = 0; x < kDim; x += 64)
                         load_box(base + t * kBytes + x / 64 * (kTile * 128), &M.q, x, Q.first + first + t * kTile, at.head, Q.at, smem_addr(&S.stay));
             int sent = 0;
@@ -410,13 +422,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
 
 // ------------------------------------------------------------------------------------------------ backward: queries
 
-// TMEM: S (two buffers), dP, dq.  dS goes over its S: columns 0-31 from the first warp group, 64-95 from the second.
+// TMEM: S, dP, dq, and as bfloat16 the q and do that stay: read from there they leave shared memory to the stream (seven
+// tiles of keys and values instead of five: with five the copies' latency showed) and halve what the score products read
+// from it.  S is free again once the softmax groups have it in registers; dS goes over dP: columns 0-31 from the first
+// group, 64-95 from the second.
 template <int kDim>
 __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
-    constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
+    constexpr int kSlots = stream_slots<kDim>() + 2, kBytes = tile_bytes<kDim>();
     extern __shared__ __align__(1024) uint8_t tiles[];
-    Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
-    const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
+    Shared &S = *reinterpret_cast<Shared *>(tiles + kSlots * kBytes);
+    const uint32_t ring = smem_addr(tiles);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + kTile - 1) / kTile, P.causal);
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
@@ -425,19 +440,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
     const int n = key_tiles(Q, K, P.causal, first);
     const bool ragged = ends_inside(K, P.packed, P.seq_k) && n == K.n / kTile + 1;
     const uint32_t tmem = begin_block<512>(S, kSlots, 2, 2 * kGroupWarps);
-    const uint32_t dp_at = tmem + 2 * kTile, dq_at = tmem + 3 * kTile;
+    const uint32_t s_at = tmem, dp_at = tmem + kTile, dq_at = tmem + 2 * kTile, q_at = tmem + 3 * kTile, do_at = q_at + kDim / 2;
     volatile uint32_t *const failed = &S.failed;
 
     if (warp >= 2 * kGroupWarps) {
         registers_few();
         if (warp == kLoadWarp && lane == 0 && n > 0) {
             Ring r;
-            bar_expect(smem_addr(&S.stay), 2 * kBytes);
-    #pragma unroll
-            for (int x = 0; x < kDim; x += 64) {
-                load_box(base + x / 64 * (kTile * 128), &M.q, x, Q.first + first, at.head, Q.at, smem_addr(&S.stay));
-                load_box(base + kBytes + x / 64 * (kTile * 128), &M.d_o, x, Q.first + first, at.head, Q.at, smem_addr(&S.stay));
-            }
             int sent = 0;
             for (int j = 0; j < 2 * n; ++j) {
                 bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed);
@@ -448,7 +457,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
                 r.next<kSlots>();
             }
             if (*failed) {
-                settle(smem_addr(&S.stay), 0);
                 for (int j = max(0, sent - kSlots); j < sent; ++j)
                     if (ragged && j >= 2 * n - 2) settle(smem_addr(&S.last), 0);
                     else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
@@ -462,31 +470,33 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
                 if (ragged && load >= 2 * n - 2) bar_wait(smem_addr(&S.clean), 0, failed);
                 else bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
             };
-            bar_wait(smem_addr(&S.stay), 0, failed);
+            bar_wait(smem_addr(&S.rows_in), 0, failed);
             ready(0);
-            product_scores<kDim>(lead, tmem, base, ring, scores);
+            fence_after();
+            product_scores_tmem<kDim>(lead, s_at, q_at, ring, scores);
             commit(lead, smem_addr(&S.score[0]));
             ready(1);
-            product_scores<kDim>(lead, dp_at, base + kBytes, ring + kBytes, plain);
+            product_scores_tmem<kDim>(lead, dp_at, do_at, ring + kBytes, plain);
             commit(lead, smem_addr(&S.second[0]));
             commit(lead, smem_addr(&S.empty[1]));
             for (int j = 0; j < n; ++j) {
                 if (j + 1 < n) {
+                    bar_wait(smem_addr(&S.prob[0]), j & 1, failed);
                     ready(2 * j + 2);
-                    product_scores<kDim>(lead, tmem + (j + 1) % 2 * kTile, base, ring + slot(2 * j + 2) * kBytes, scores);
-                    commit(lead, smem_addr(&S.score[(j + 1) % 2]));
+                    fence_after();
+                    product_scores_tmem<kDim>(lead, s_at, q_at, ring + slot(2 * j + 2) * kBytes, scores);
+                    commit(lead, smem_addr(&S.score[0]));
                 }
                 bar_wait(smem_addr(&S.grad), j & 1, failed);
-                if (j + 1 < n) ready(2 * j + 3);
                 fence_after();
+                product_apply<kDim>(lead, dq_at, dp_at, dp_at + 64, ring + slot(2 * j) * kBytes, j > 0);
+                commit(lead, smem_addr(&S.empty[slot(2 * j)]));
                 if (j + 1 < n) {
-                    product_scores<kDim>(lead, dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+                    ready(2 * j + 3);
+                    product_scores_tmem<kDim>(lead, dp_at, do_at, ring + slot(2 * j + 3) * kBytes, plain);
                     commit(lead, smem_addr(&S.second[0]));
                     commit(lead, smem_addr(&S.empty[slot(2 * j + 3)]));
                 }
-                const uint32_t ds = tmem + j % 2 * kTile;
-                product_apply<kDim>(lead, dq_at, ds, ds + 64, ring + slot(2 * j) * kBytes, j > 0);
-                commit(lead, smem_addr(&S.empty[slot(2 * j)]));
             }
             commit(lead, smem_addr(&S.done));
             commit(lead, smem_addr(&S.drain));
@@ -494,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
             if (*failed) settle(smem_addr(&S.drain), 0);
         } else if (warp == kHelpWarp && ragged) {
             bar_wait(smem_addr(&S.last), 0, failed);
-            for (int load = 2 * n - 2; load < 2 * n; ++load) clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
+            for (int load = 2 * n - 2; load < 2 * n; ++load) clean_tile<kDim>(tiles + load % kSlots * kBytes, K.n % kTile, lane);
             fence_async_shared();
             __syncwarp();
             if (lane == 0) bar_arrive(smem_addr(&S.clean));
@@ -506,20 +516,33 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
         const uint32_t lanes = static_cast<uint32_t>(warp % kGroupWarps * 32) << 16;
         const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
         const bool wanted = i < (P.packed ? Q.n : P.seq_q);
-        // D: each group takes half of the row
+        // the first group brings in the rows of q, the second those of do, and D with them
         float dot = 0.0f;
-        if (limit > 0) {
-            const __nv_bfloat16 *o = row_of(P.o, Q, i, at.head), *g = row_of(P.d_o, Q, i, at.head);
-            for (int x = t * (kDim / 2); x < min((t + 1) * (kDim / 2), P.head_dim); x += 8) {
-                const Pack<__nv_bfloat16, 8> a = *reinterpret_cast<const Pack<__nv_bfloat16, 8> *>(o + x);
-                const Pack<__nv_bfloat16, 8> b = *reinterpret_cast<const Pack<__nv_bfloat16, 8> *>(g + x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dot = fmaf(__bfloat162float(a.v[e]), __bfloat162float(b.v[e]), dot);
+        for (int c = 0; c < kDim / 64; ++c) {
+            const __nv_bfloat16 *from = row_of(t ? P.d_o : P.q, Q, i, at.head) + c * 64, *o = row_of(P.o, Q, i, at.head) + c * 64;
+            uint32_t r[32];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                uint4 w = make_uint4(0, 0, 0, 0);
+                if (limit > 0 && c * 64 + x * 8 < P.head_dim) {
+                    w = *reinterpret_cast<const uint4 *>(from + x * 8);
+                    if (t) {
+                        const uint4 u = *reinterpret_cast<const uint4 *>(o + x * 8);
+                        dot = dot2(w.x, u.x, dot2(w.y, u.y, dot2(w.z, u.z, dot2(w.w, u.w, dot))));
+                    }
+                }
+                r[4 * x] = w.x; r[4 * x + 1] = w.y; r[4 * x + 2] = w.z; r[4 * x + 3] = w.w;
             }
+            store_columns((t ? do_at : q_at) + lanes + c * 32, r);
         }
-        S.row[t][0][row] = dot;
+        wait_stores();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_addr(&S.rows_in));
+        if (t) S.row[0][0][row] = dot;
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        dot = S.row[0][0][row] + S.row[1][0][row];
+        dot = S.row[0][0][row];
         float shift = INFINITY;                  // a row that sees nothing has p = exp2(-inf) = 0
         if (limit > 0) {
             shift = P.lse[stat_at(P, Q, i, at.head)] * kLog2e;
@@ -528,16 +551,18 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
         if (t == 0 && wanted) P.row_dot[stat_at(P, Q, i, at.head)] = dot;
         const float2 by = make_float2(scale, scale), minus = make_float2(-shift, -shift), less = make_float2(-dot, -dot);
         for (int j = 0; j < n; ++j) {
-            const uint32_t s_at = tmem + lanes + j % 2 * kTile + t * 64;
-            bar_wait(smem_addr(&S.score[j % 2]), j / 2 & 1, failed);
+            bar_wait(smem_addr(&S.score[0]), j & 1, failed);
             __syncwarp();
             fence_after();
             uint32_t s[2][32], d[2][32];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) load_columns(s_at + c * 32, s[c]);
+            for (int c = 0; c < 2; ++c) load_columns(s_at + lanes + t * 64 + c * 32, s[c]);
             wait_loads();
 #pragma unroll
             for (int c = 0; c < 2; ++c) pin(s[c]);
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.prob[0]));
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -571,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
                                           add2(make_float2(__uint_as_float(d[c][x]), __uint_as_float(d[c][x + 1])), less));
                     w[x / 2] = pack_bf16(e.x, e.y);
                 }
-                store_columns(s_at + c * 16, w);
+                store_columns(dp_at + lanes + t * 64 + c * 16, w);
             }
             wait_stores();
             fence_before();
@@ -628,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
         if (warp == kLoadWarp && lane == 0 && n > 0) {
             Ring r;
             bar_expect(smem_addr(&S.stay), 2 * kBytes);
-    #pragma unroll
+#pragma unroll
             for (int x = 0; x < kDim; x += 64) {
                 load_box(base + x / 64 * (kTile * 128), &M.k, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
                 load_box(base + kBytes + x / 64 * (kTile * 128), &M.v, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
@@ -690,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             for (int j = 0; j < n; ++j) {
                 const int g = j / per, tile = from + j - g * per, b = j % 2;
                 float l[4], d[4];
-    #pragma unroll
+#pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int i = tile * kTile + x * 32 + lane;
                     l[x] = INFINITY;                 // no such query, or one that sees nothing: p = exp2(-inf) = 0
@@ -708,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
                         bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
                         clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, Q.n % kTile, lane);
                     }
-    #pragma unroll
+#pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     S.row[b][0][x * 32 + lane] = -l[x];
                     S.row[b][1][x * 32 + lane] = -d[x];
