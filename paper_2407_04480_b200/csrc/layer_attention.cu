@@ -46,8 +46,8 @@ constexpr int kMaxSlots = 12;
 struct Shared {
     uint64_t full[kMaxSlots], empty[kMaxSlots];  // streaming tiles: copied, no longer read
     uint64_t stay, rows_in;                      // the tiles that stay are in shared memory, in TMEM
-    uint64_t score[2], second[2];                // products ready: S per tile or buffer; o (forward) or dP (backward)
-    uint64_t prob[2], grad;                      // P written to TMEM (backward queries: S read), dS written
+    uint64_t score[2], second[2];                // products ready: S per query tile; o per query tile (forward), dP and dv (backward)
+    uint64_t prob[2], grad;                      // P written to TMEM (forward: per query tile), S read (backward); dS written
     uint64_t last, clean;                        // a tile with rows past the end is copied; those rows are zero
     uint64_t stats[2], stats_free[2];            // backward keys: row statistics of a query tile
     uint64_t done, drain;
@@ -59,27 +59,26 @@ template <int kDim> constexpr int shared_bytes() {
 }
 static_assert(shared_bytes<128>() <= 227 * 1024 && shared_bytes<64>() <= 227 * 1024, "shared memory of a block");
 
-template <int kDim> __device__ __forceinline__ void load_tile(uint32_t to, const CUtensorMap *map, int row, int head, int batch, uint32_t bar) {
-    bar_expect(bar, tile_bytes<kDim>());
+template <int kDim, int kRows = kTile>
+__device__ __forceinline__ void load_tile(uint32_t to, const CUtensorMap *map, int row, int head, int batch, uint32_t bar) {
+    bar_expect(bar, kRows * kDim * 2);
 #pragma unroll
-    for (int x = 0; x < kDim; x += 64) load_box(to + x / 64 * (kTile * 128), map, x, row, head, batch, bar);
+    for (int x = 0; x < kDim; x += 64) load_box(to + x / 64 * (kRows * 128), map, x, row, head, batch, bar);
 }
 
 // Zero the rows from `first` on of a tile, by one warp.
-template <int kDim> __device__ __forceinline__ void clean_tile(uint8_t *tile, int first, int lane) {
+template <int kDim, int kRows = kTile> __device__ __forceinline__ void clean_tile(uint8_t *tile, int first, int lane) {
     for (int x = 0; x < kDim; x += 64)
-        for (int i = first * 8 + lane; i < kTile * 8; i += 32)
-            reinterpret_cast<uint4 *>(tile + x / 64 * (kTile * 128))[i] = make_uint4(0, 0, 0, 0);
+        for (int i = first * 8 + lane; i < kRows * 8; i += 32)
+            reinterpret_cast<uint4 *>(tile + x / 64 * (kRows * 128))[i] = make_uint4(0, 0, 0, 0);
 }
 
-// S (128 x 128) = A B^T over kDim columns, both tiles in shared memory.
-template <int kDim> __device__ __forceinline__ void product_scores(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t word) {
+// S (128 x kRows) = A B^T over kDim columns, both tiles in shared memory.
+template <int kDim, int kRows = kTile> __device__ __forceinline__ void product_scores(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t word) {
     const uint32_t da = desc_along_columns(a), db = desc_along_columns(b);
 #pragma unroll
-    for (int x = 0; x < kDim; x += 16) {
-        const uint32_t off = (x / 64 * (kTile * 128) + x % 64 * 2) >> 4;
-        mma_ss(lead, d, da + off, db + off, word, x > 0);
-    }
+    for (int x = 0; x < kDim; x += 16)
+        mma_ss(lead, d, da + ((x / 64 * (kTile * 128) + x % 64 * 2) >> 4), db + ((x / 64 * (kRows * 128) + x % 64 * 2) >> 4), word, x > 0);
 }
 // The same with A in TMEM, two dimensions to a column.
 template <int kDim> __device__ __forceinline__ void product_scores_tmem(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t word) {
@@ -87,13 +86,14 @@ template <int kDim> __device__ __forceinline__ void product_scores_tmem(uint32_t
 #pragma unroll
     for (int x = 0; x < kDim; x += 16) mma_ts(lead, d, a + x / 2, db + ((x / 64 * (kTile * 128) + x % 64 * 2) >> 4), word, x > 0);
 }
-// d (128 x kDim) += A B: A (128 x 128) in TMEM, its columns at `a0` (first 64) and `a1`; B's rows are the tile's.
-template <int kDim> __device__ __forceinline__ void product_apply(uint32_t lead, uint32_t d, uint32_t a0, uint32_t a1, uint32_t b, uint32_t accumulate) {
+// d (128 x kDim) += A B: A (128 x kRows) in TMEM, its columns at `a0` (first half) and `a1`; B's rows are the tile's.
+template <int kDim, int kRows = kTile>
+__device__ __forceinline__ void product_apply(uint32_t lead, uint32_t d, uint32_t a0, uint32_t a1, uint32_t b, uint32_t accumulate) {
     constexpr uint32_t word = product(kDim, true);
-    const uint32_t db = desc_along_rows(b, kTile * 128);
+    const uint32_t db = desc_along_rows(b, kRows * 128);
 #pragma unroll
-    for (int r = 0; r < kTile; r += 16)
-        mma_ts(lead, d, (r < 64 ? a0 : a1) + r % 64 / 2, db + (r * 128 >> 4), word, accumulate | (r > 0));
+    for (int r = 0; r < kRows; r += 16)
+        mma_ts(lead, d, r < kRows / 2 ? a0 + r / 2 : a1 + (r - kRows / 2) / 2, db + (r * 128 >> 4), word, accumulate | (r > 0));
 }
 
 // Sets up barriers and TMEM; returns the TMEM base.
@@ -182,7 +182,7 @@ __device__ __forceinline__ void zero_row(__nv_bfloat16 *to, int from, int until)
 }
 
 // Whether a streamed tile that holds the last of n rows also holds rows past them that are not the copy's zero fill.
-__device__ __forceinline__ bool ends_inside(const Rows &r, int packed, int seq) { return r.n % kTile != 0 && (packed || r.n != seq); }
+__device__ __forceinline__ bool ends_inside(const Rows &r, int packed, int seq, int tile = kTile) { return r.n % tile != 0 && (packed || r.n != seq); }
 
 // The block's place: tiles are the slow index, so that blocks of one wave share keys; `reverse` starts with the last tile,
 // which under a causal mask is the longest for queries.
@@ -627,12 +627,23 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
 
 // ------------------------------------------------------------------------------------------------ backward: keys
 
-// TMEM: S^T, dP^T, dv, dk; P^T goes over S^T and dS^T over dP^T.
+// TMEM: dv, dk, S^T, dP^T and P^T; dS^T goes over dP^T.  S^T is free again once the softmax groups have it in registers, so
+// that the next scores are computed under this tile's exponentials.  With heads of 128 that takes query tiles of 96: 128 of
+// them would fill TMEM without a place of its own for P^T, and the next scores would wait for dv (measured at 4096, 32
+// heads: 472 us).  A group has half of the tile's queries, a thread one key's half row.
+template <int kDim> __host__ __device__ constexpr int query_tile() { return kDim == 128 ? 96 : 128; }
+template <int kDim> __host__ __device__ constexpr int query_slots() { return kDim == 128 ? 6 : 10; }
+template <int kDim> constexpr int shared_bytes_keys() {
+    return 2 * tile_bytes<kDim>() + query_slots<kDim>() * query_tile<kDim>() * kDim * 2 + static_cast<int>(sizeof(Shared));
+}
+static_assert(shared_bytes_keys<128>() <= 227 * 1024 && shared_bytes_keys<64>() <= 227 * 1024, "shared memory of a block");
+
 template <int kDim>
 __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
-    constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
+    constexpr int kSlots = query_slots<kDim>(), kRows = query_tile<kDim>(), kBytes = tile_bytes<kDim>(), kStep = kRows * kDim * 2;
+    constexpr int kHalf = kRows / 2;
     extern __shared__ __align__(1024) uint8_t tiles[];
-    Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
+    Shared &S = *reinterpret_cast<Shared *>(tiles + 2 * kBytes + kSlots * kStep);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P.heads_kv, P.batch, (P.max_k + kTile - 1) / kTile, false);
@@ -641,11 +652,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
     if (P.packed && first >= K.n) return;
     // query tiles [from, until) see this tile; the heads of the group one after the other
     const int off = K.n - Q.n;
-    const int until = (Q.n + kTile - 1) / kTile, from = P.causal ? min(until, max(0, first - off) / kTile) : 0;
+    const int until = (Q.n + kRows - 1) / kRows, from = P.causal ? min(until, max(0, first - off) / kRows) : 0;
     const int per = first < K.n ? until - from : 0, n = per * P.group;
-    const bool ragged = ends_inside(Q, P.packed, P.seq_q);
+    const bool ragged = ends_inside(Q, P.packed, P.seq_q, kRows);
     const uint32_t tmem = begin_block<512>(S, kSlots, 1, 2 * kGroupWarps);
-    const uint32_t s_at = tmem, dp_at = tmem + kTile, dv_at = tmem + 2 * kTile, dk_at = tmem + 3 * kTile;
+    const uint32_t dv_at = tmem, dk_at = tmem + kDim, s_at = tmem + 2 * kDim, dp_at = s_at + kRows, p_at = dp_at + kRows;
     volatile uint32_t *const failed = &S.failed;
 
     if (warp >= 2 * kGroupWarps) {
@@ -658,14 +669,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
                 load_box(base + x / 64 * (kTile * 128), &M.k, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
                 load_box(base + kBytes + x / 64 * (kTile * 128), &M.v, x, K.first + first, at.head, K.at, smem_addr(&S.stay));
             }
-            int sent = 0;
-            for (int j = 0; j < 2 * n; ++j) {
-                bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed);
+            int sent = 0, g = 0, tile = from;
+            for (int j = 0; j < n; ++j) {
+                for (int x = 0; x < 2; ++x) {
+                    bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed);
+                    if (*failed) break;
+                    load_tile<kDim, kRows>(ring + r.slot * kStep, x ? &M.d_o : &M.q, Q.first + tile * kRows, at.head * P.group + g, Q.at, smem_addr(&S.full[r.slot]));
+                    ++sent;
+                    r.next<kSlots>();
+                }
                 if (*failed) break;
-                const int g = j / 2 / per, tile = from + j / 2 - g * per;
-                load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.d_o : &M.q, Q.first + tile * kTile, at.head * P.group + g, Q.at, smem_addr(&S.full[r.slot]));
-                ++sent;
-                r.next<kSlots>();
+                if (++tile == until) {
+                    tile = from;
+                    ++g;
+                }
             }
             if (*failed) {
                 settle(smem_addr(&S.stay), 0);
@@ -673,36 +690,39 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             }
         } else if (warp == kProductWarp && n > 0) {
             const uint32_t lead = elect_lane();
-            const uint32_t scores = product(kTile, false, P.scale < 0.0f), plain = product(kTile, false);
+            const uint32_t scores = product(kRows, false, P.scale < 0.0f), plain = product(kRows, false);
             const auto slot = [](int load) { return load % kSlots; };
             const auto ready = [&](int load) { bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed); };
             const auto whole = [&](int j) { bar_wait(smem_addr(&S.stats[j % 2]), j / 2 & 1, failed); };
             bar_wait(smem_addr(&S.stay), 0, failed);
             whole(0);
             ready(0);
-            product_scores<kDim>(lead, s_at, base, ring, scores);
+            product_scores<kDim, kRows>(lead, s_at, base, ring, scores);
             commit(lead, smem_addr(&S.score[0]));
             ready(1);
-            product_scores<kDim>(lead, dp_at, base + kBytes, ring + kBytes, plain);
+            product_scores<kDim, kRows>(lead, dp_at, base + kBytes, ring + kStep, plain);
             commit(lead, smem_addr(&S.second[0]));
             for (int j = 0; j < n; ++j) {
-                bar_wait(smem_addr(&S.prob[0]), j & 1, failed);
-                fence_after();
-                product_apply<kDim>(lead, dv_at, s_at, s_at + 64, ring + slot(2 * j + 1) * kBytes, j > 0);
-                commit(lead, smem_addr(&S.empty[slot(2 * j + 1)]));
                 if (j + 1 < n) {
                     whole(j + 1);
                     ready(2 * j + 2);
-                    product_scores<kDim>(lead, s_at, base, ring + slot(2 * j + 2) * kBytes, scores);
+                    bar_wait(smem_addr(&S.prob[1]), j & 1, failed);
+                    fence_after();
+                    product_scores<kDim, kRows>(lead, s_at, base, ring + slot(2 * j + 2) * kStep, scores);
                     commit(lead, smem_addr(&S.score[0]));
                 }
+                bar_wait(smem_addr(&S.prob[0]), j & 1, failed);
+                fence_after();
+                product_apply<kDim, kRows>(lead, dv_at, p_at, p_at + kHalf / 2, ring + slot(2 * j + 1) * kStep, j > 0);
+                commit(lead, smem_addr(&S.second[1]));
+                commit(lead, smem_addr(&S.empty[slot(2 * j + 1)]));
                 bar_wait(smem_addr(&S.grad), j & 1, failed);
                 fence_after();
-                product_apply<kDim>(lead, dk_at, dp_at, dp_at + 64, ring + slot(2 * j) * kBytes, j > 0);
+                product_apply<kDim, kRows>(lead, dk_at, dp_at, dp_at + kHalf, ring + slot(2 * j) * kStep, j > 0);
                 commit(lead, smem_addr(&S.empty[slot(2 * j)]));
                 if (j + 1 < n) {
                     ready(2 * j + 3);
-                    product_scores<kDim>(lead, dp_at, base + kBytes, ring + slot(2 * j + 3) * kBytes, plain);
+                    product_scores<kDim, kRows>(lead, dp_at, base + kBytes, ring + slot(2 * j + 3) * kStep, plain);
                     commit(lead, smem_addr(&S.second[0]));
                 }
             }
@@ -711,34 +731,45 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             bar_wait(smem_addr(&S.drain), 0, failed);
             if (*failed) settle(smem_addr(&S.drain), 0);
         } else if (warp == kHelpWarp) {
-            // row statistics of each query tile, and zeros past the sample's end in the tile that holds it
-            for (int j = 0; j < n; ++j) {
-                const int g = j / per, tile = from + j - g * per, b = j % 2;
-                float l[4], d[4];
+            // row statistics of each query tile, read one tile ahead, and zeros past the sample's end in the tile that holds it
+            constexpr int kMine = kRows / 32;
+            float l[kMine], d[kMine];
+            int g = 0, tile = from;
+            const auto read = [&]() {
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int i = tile * kTile + x * 32 + lane;
-                    l[x] = INFINITY;                 // no such query, or one that sees nothing: p = exp2(-inf) = 0
+                for (int x = 0; x < kMine; ++x) {
+                    const int i = tile * kRows + x * 32 + lane;
+                    l[x] = INFINITY;             // no such query, or one that sees nothing: p = exp2(-inf) = 0
                     d[x] = 0.0f;
                     if (i < Q.n) {
                         const int64_t s = stat_at(P, Q, i, at.head * P.group + g);
-                        l[x] = P.lse[s] * kLog2e;
+                        l[x] = P.lse[s];
                         d[x] = P.row_dot[s];
-                        if (l[x] == -INFINITY) l[x] = INFINITY;
                     }
                 }
+            };
+            if (n > 0) read();
+            for (int j = 0; j < n; ++j) {
+                const int b = j % 2;
+                const bool clean = ragged && tile == until - 1;
                 bar_wait(smem_addr(&S.stats_free[b]), (j / 2 & 1) ^ 1, failed);
-                if (ragged && tile == until - 1)
-                    for (int load = 2 * j; load < 2 * j + 2; ++load) {
-                        bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
-                        clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, Q.n % kTile, lane);
-                    }
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    S.row[b][0][x * 32 + lane] = -l[x];
+                for (int x = 0; x < kMine; ++x) {
+                    S.row[b][0][x * 32 + lane] = l[x] == -INFINITY ? -INFINITY : -l[x] * kLog2e;
                     S.row[b][1][x * 32 + lane] = -d[x];
                 }
-                fence_async_shared();
+                if (++tile == until) {
+                    tile = from;
+                    ++g;
+                }
+                if (j + 1 < n) read();
+                if (clean) {
+                    for (int load = 2 * j; load < 2 * j + 2; ++load) {
+                        bar_wait(smem_addr(&S.full[load % kSlots]), load / kSlots & 1, failed);
+                        clean_tile<kDim, kRows>(tiles + 2 * kBytes + load % kSlots * kStep, Q.n % kRows, lane);
+                    }
+                    fence_async_shared();
+                }
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_addr(&S.stats[b]));
             }
@@ -747,27 +778,31 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
         registers_many();
         const int t = warp / kGroupWarps, key = first + threadIdx.x % kTile;
         const uint32_t lanes = static_cast<uint32_t>(warp % kGroupWarps * 32) << 16;
-        const uint32_t my_s = s_at + lanes + t * 64, my_dp = dp_at + lanes + t * 64;
+        const uint32_t my_s = s_at + lanes + t * kHalf, my_dp = dp_at + lanes + t * kHalf, my_p = p_at + lanes + t * (kHalf / 2);
         const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
         const float2 by = make_float2(scale, scale);
+        int tile = from;
         for (int j = 0; j < n; ++j) {
-            const int tile = from + j % per, b = j % 2;
-            const float4 *lse = reinterpret_cast<const float4 *>(S.row[b][0] + t * 64), *dot = reinterpret_cast<const float4 *>(S.row[b][1] + t * 64);
+            const int b = j % 2;
+            const float4 *lse = reinterpret_cast<const float4 *>(S.row[b][0] + t * kHalf), *dot = reinterpret_cast<const float4 *>(S.row[b][1] + t * kHalf);
             bar_wait(smem_addr(&S.stats[b]), j / 2 & 1, failed);
             bar_wait(smem_addr(&S.score[0]), j & 1, failed);
             __syncwarp();
             fence_after();
-            uint32_t s[2][32], d[2][32];
+            uint32_t s[kHalf / 16][16], d[kHalf / 16][16];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) load_columns(my_s + c * 32, s[c]);
+            for (int c = 0; c < kHalf / 16; ++c) load_columns(my_s + c * 16, s[c]);
             wait_loads();
 #pragma unroll
-            for (int c = 0; c < 2; ++c) pin(s[c]);
+            for (int c = 0; c < kHalf / 16; ++c) pin(s[c]);
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.prob[1]));
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int c = 0; c < kHalf / 16; ++c)
 #pragma unroll
-                for (int x = 0; x < 32; x += 4) {
-                    const float4 l = lse[c * 8 + x / 4];
+                for (int x = 0; x < 16; x += 4) {
+                    const float4 l = lse[c * 4 + x / 4];
                     const float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, make_float2(l.x, l.y));
                     const float2 f = fma2(make_float2(__uint_as_float(s[c][x + 2]), __uint_as_float(s[c][x + 3])), by, make_float2(l.z, l.w));
                     s[c][x] = __float_as_uint(exp2_fast(e.x));
@@ -776,20 +811,26 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
                     s[c][x + 3] = __float_as_uint(exp2_fast(f.y));
                 }
             // under the causal mask the queries from key - off on see this key
-            const int begin = P.causal ? key - off - tile * kTile - t * 64 : 0;
+            const int begin = P.causal ? key - off - tile * kRows - t * kHalf : 0;
             if (__any_sync(0xffffffffu, begin > 0)) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < kHalf / 16; ++c)
 #pragma unroll
-                    for (int x = 0; x < 32; ++x)
-                        if (c * 32 + x < begin) s[c][x] = 0;
+                    for (int x = 0; x < 16; ++x)
+                        if (c * 16 + x < begin) s[c][x] = 0;
+            }
+            if (++tile == until) tile = from;
+            if (j > 0) {                         // dv has read the previous P^T
+                bar_wait(smem_addr(&S.second[1]), (j - 1) & 1, failed);
+                __syncwarp();
+                fence_after();
             }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t w[16];
+            for (int c = 0; c < kHalf / 16; ++c) {
+                uint32_t w[8];
 #pragma unroll
-                for (int x = 0; x < 32; x += 2) w[x / 2] = pack_bf16(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1]));
-                store_columns(my_s + c * 16, w);
+                for (int x = 0; x < 16; x += 2) w[x / 2] = pack_bf16(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1]));
+                store_columns(my_p + c * 8, w);
             }
             wait_stores();
             fence_before();
@@ -799,16 +840,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             __syncwarp();
             fence_after();
 #pragma unroll
-            for (int c = 0; c < 2; ++c) load_columns(my_dp + c * 32, d[c]);
+            for (int c = 0; c < kHalf / 16; ++c) load_columns(my_dp + c * 16, d[c]);
             wait_loads();
 #pragma unroll
-            for (int c = 0; c < 2; ++c) pin(d[c]);
+            for (int c = 0; c < kHalf / 16; ++c) pin(d[c]);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t w[16];
+            for (int c = 0; c < kHalf / 16; ++c) {
+                uint32_t w[8];
 #pragma unroll
-                for (int x = 0; x < 32; x += 4) {
-                    const float4 e = dot[c * 8 + x / 4];
+                for (int x = 0; x < 16; x += 4) {
+                    const float4 e = dot[c * 4 + x / 4];
                     const float2 f = mul2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])),
                                           add2(make_float2(__uint_as_float(d[c][x]), __uint_as_float(d[c][x + 1])), make_float2(e.x, e.y)));
                     const float2 h = mul2(make_float2(__uint_as_float(s[c][x + 2]), __uint_as_float(s[c][x + 3])),
@@ -816,7 +857,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
                     w[x / 2] = pack_bf16(f.x, f.y);
                     w[x / 2 + 1] = pack_bf16(h.x, h.y);
                 }
-                store_columns(my_dp + c * 16, w);
+                store_columns(my_dp + c * 8, w);
             }
             wait_stores();
             fence_before();
@@ -828,23 +869,21 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
         }
         if (n > 0) bar_wait(smem_addr(&S.done), 0, failed);
         __syncwarp();
-        {
-            // the first group writes dv, the second dk
-            const bool wanted = key < (P.packed ? K.n : P.seq_k);
-            __nv_bfloat16 *out = t ? row_of(P.dk, K, key, at.head) : row_of(P.dv, K, key, at.head);
-            if (n > 0) {
-                fence_after();
+        // the first group writes dv, the second dk
+        const bool wanted = key < (P.packed ? K.n : P.seq_k);
+        __nv_bfloat16 *out = t ? row_of(P.dk, K, key, at.head) : row_of(P.dv, K, key, at.head);
+        if (n > 0) {
+            fence_after();
 #pragma unroll
-                for (int c = 0; c < kDim / 32; ++c) {
-                    uint32_t r[32];
-                    load_columns((t ? dk_at : dv_at) + lanes + c * 32, r);
-                    wait_loads();
-                    pin(r);
-                    if (wanted && key < K.n) store_row<kDim>(out, r, c * 32, P.head_dim, t ? P.scale : 1.0f);
-                }
+            for (int c = 0; c < kDim / 32; ++c) {
+                uint32_t r[32];
+                load_columns((t ? dk_at : dv_at) + lanes + c * 32, r);
+                wait_loads();
+                pin(r);
+                if (wanted && key < K.n) store_row<kDim>(out, r, c * 32, P.head_dim, t ? P.scale : 1.0f);
             }
-            if (wanted && (key >= K.n || n == 0)) zero_row(out, 0, P.head_dim);
         }
+        if (wanted && (key >= K.n || n == 0)) zero_row(out, 0, P.head_dim);
     }
     __syncwarp();
     end_block<512>(S, tmem);
@@ -873,8 +912,8 @@ EncodeFn encode_fn() {
     return f;
 }
 
-// Heads as [batch, head, row, dim] in boxes of 128 rows by 64 dimensions; what lies past the tensor reads as zero.
-bool make_map(CUtensorMap &map, const Heads &t, int batch, int heads, int rows, int dim, const void *stand_in) {
+// Heads as [batch, head, row, dim] in boxes of `box_rows` rows by 64 dimensions; what lies past the tensor reads as zero.
+bool make_map(CUtensorMap &map, const Heads &t, int batch, int heads, int rows, int dim, int box_rows, const void *stand_in) {
     const EncodeFn encode = encode_fn();
     if (!encode) return false;
     const bool none = rows == 0 || batch == 0;             // never read
@@ -884,7 +923,7 @@ bool make_map(CUtensorMap &map, const Heads &t, int batch, int heads, int rows, 
     // the stride of a single row, head or sample means nothing, but has to be a valid one
     const auto stride = [&](int64_t s, cuuint64_t n) { return static_cast<cuuint64_t>(n == 1 ? 256 : s * 2); };
     const cuuint64_t strides[3] = {stride(t.row_stride, size[1]), stride(t.head_stride, size[2]), stride(t.batch_stride, size[3])};
-    const cuuint32_t box[4] = {64, kTile, 1, 1}, step[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1}, step[4] = {1, 1, 1, 1};
     return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, at, size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -917,37 +956,35 @@ int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const 
     return launched();
 }
 
-bool make_maps(const AttentionParams &P, Maps &M, bool gradient) {
+bool make_maps(const AttentionParams &P, Maps &M, int query_box, bool gradient) {
     const int b = P.packed ? 1 : P.batch;
     const void *any = P.seq_q > 0 ? P.q.ptr : P.k.ptr;
-    return make_map(M.q, P.q, b, P.heads_q, P.seq_q, P.head_dim, any) && make_map(M.k, P.k, b, P.heads_kv, P.seq_k, P.head_dim, any) &&
-           make_map(M.v, P.v, b, P.heads_kv, P.seq_k, P.head_dim, any) &&
-           (!gradient || make_map(M.d_o, P.d_o, b, P.heads_q, P.seq_q, P.head_dim, any));
+    return make_map(M.q, P.q, b, P.heads_q, P.seq_q, P.head_dim, query_box, any) && make_map(M.k, P.k, b, P.heads_kv, P.seq_k, P.head_dim, kTile, any) &&
+           make_map(M.v, P.v, b, P.heads_kv, P.seq_k, P.head_dim, kTile, any) &&
+           (!gradient || make_map(M.d_o, P.d_o, b, P.heads_q, P.seq_q, P.head_dim, query_box, any));
 }
 
-template <int kDim> int forward(const AttentionParams &P, const Maps &M, cudaStream_t stream) {
-    constexpr int bytes = shared_bytes<kDim>();
-    return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, bytes, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, P, M, stream);
+template <int kDim> int forward(const AttentionParams &P, cudaStream_t stream) {
+    Maps M;
+    if (!make_maps(P, M, kTile, false)) return LOCO_ERR_CUDA;
+    return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, P, M, stream);
 }
-template <int kDim> int backward(const AttentionParams &P, const Maps &M, cudaStream_t stream) {
-    constexpr int bytes = shared_bytes<kDim>();
-    const int rc = launch(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, bytes, (P.max_q + kTile - 1) / kTile, P.heads_q, P, M, stream);
+template <int kDim> int backward(const AttentionParams &P, cudaStream_t stream) {
+    Maps M;                                      // the first kernel reads k and v through it only
+    if (!make_maps(P, M, query_tile<kDim>(), true)) return LOCO_ERR_CUDA;
+    const int rc = launch(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + kTile - 1) / kTile, P.heads_q, P, M, stream);
     if (rc != LOCO_OK) return rc;
-    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, bytes, (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream);
+    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream);
 }
 
 }  // namespace
 
 int launch_attention_forward(const AttentionParams &P, cudaStream_t stream) {
-    Maps M;
-    if (!make_maps(P, M, false)) return LOCO_ERR_CUDA;
-    return P.head_dim <= 64 ? forward<64>(P, M, stream) : forward<128>(P, M, stream);
+    return P.head_dim <= 64 ? forward<64>(P, stream) : forward<128>(P, stream);
 }
 
 int launch_attention_backward(const AttentionParams &P, cudaStream_t stream) {
-    Maps M;
-    if (!make_maps(P, M, true)) return LOCO_ERR_CUDA;
-    return P.head_dim <= 64 ? backward<64>(P, M, stream) : backward<128>(P, M, stream);
+    return P.head_dim <= 64 ? backward<64>(P, stream) : backward<128>(P, stream);
 }
 
 }  // namespace loco_layer
