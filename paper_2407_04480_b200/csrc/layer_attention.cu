@@ -36,7 +36,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ unsigned g_status;                    // LOCO_LAYER_FLAG_*
 
-struct Maps { CUtensorMap q, k, v, d_o; };
+struct Maps { CUtensorMap q, k, v, d_o, o; };
 
 // Shared memory: two tiles that stay, the ring of tiles that stream, then Shared.  Either head size fills the SM, so that no
 // two blocks compete for its tensor memory.
@@ -159,28 +159,56 @@ struct Ring {
     }
 };
 
-template <int kDim> __device__ __forceinline__ void store_row(__nv_bfloat16 *to, const uint32_t (&r)[32], int first, int dim, float by) {
+// A warp's 32 rows of an accumulator leave through shared memory, so that its stores cover whole rows: a thread's own row
+// of 16-byte pieces would touch 32 lines an instruction (measured: 2000 clocks a block more).  kCols columns a row; the
+// pieces are permuted so that neither side meets a bank twice.
+template <int kCols> __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
+    constexpr int kPieces = kCols / 8;
+    return row * (kCols * 2) + ((piece ^ (kPieces >= 8 ? row & 7 : row >> 1 & 3)) << 4);
+}
+template <int kCols> __device__ __forceinline__ void stage_columns(uint8_t *stage, int row, const uint32_t (&r)[32], int first, float by, bool some) {
 #pragma unroll
     for (int i = 0; i < 32; i += 8) {
-        if (first + i < dim) {                   // dim is a multiple of 8
-            uint4 w;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (some) {
             w.x = pack_bf16(__uint_as_float(r[i]) * by, __uint_as_float(r[i + 1]) * by);
             w.y = pack_bf16(__uint_as_float(r[i + 2]) * by, __uint_as_float(r[i + 3]) * by);
             w.z = pack_bf16(__uint_as_float(r[i + 4]) * by, __uint_as_float(r[i + 5]) * by);
             w.w = pack_bf16(__uint_as_float(r[i + 6]) * by, __uint_as_float(r[i + 7]) * by);
-            *reinterpret_cast<uint4 *>(to + first + i) = w;
         }
+        *reinterpret_cast<uint4 *>(stage + piece_at<kCols>(row, (first + i) / 8)) = w;
     }
+}
+// kCols accumulator columns at `tmem` times `by` (zeros where not `some`), rows [i, i + 32) below `end` of a head, from
+// dimension `x` on.  `filled` is false where the accumulator holds nothing.
+template <int kCols>
+__device__ __forceinline__ void store_rows(uint8_t *stage, uint32_t tmem, bool filled, float by, bool some, const Heads &t, const Rows &rows, int i, int end,
+                                           int head, int x, int dim) {
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int c = 0; c < kCols; c += 32) {
+        uint32_t r[32];
+        if (filled) {
+            load_columns(tmem + c, r);
+            wait_loads();
+            pin(r);
+        }
+        stage_columns<kCols>(stage, lane, r, c, by, some && filled);
+    }
+    __syncwarp();
+    constexpr int kPieces = kCols / 8;
+    const int piece = lane % kPieces;
+    if (x + piece * 8 < dim)                     // dim is a multiple of 8
+#pragma unroll 4
+        for (int row = lane / kPieces; row < 32; row += 32 / kPieces)
+            if (i + row < end)
+                *reinterpret_cast<uint4 *>(row_of(t, rows, i + row, head) + x + piece * 8) = *reinterpret_cast<const uint4 *>(stage + piece_at<kCols>(row, piece));
 }
 // c + the product of two pairs of bfloat16
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
     c = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), c);
     return fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), c);
 }
-__device__ __forceinline__ void zero_row(__nv_bfloat16 *to, int from, int until) {
-    for (int i = from; i < until; i += 8) *reinterpret_cast<uint4 *>(to + i) = make_uint4(0, 0, 0, 0);
-}
-
 // Whether a streamed tile that holds the last of n rows also holds rows past them that are not the copy's zero fill.
 __device__ __forceinline__ bool ends_inside(const Rows &r, int packed, int seq, int tile = kTile) { return r.n % tile != 0 && (packed || r.n != seq); }
 
@@ -395,26 +423,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
         }
         if (nt > 0) bar_wait(smem_addr(&S.second[t]), (nt - 1) & 1, failed);
         __syncwarp();
-        {
-            const bool wanted = i < (P.packed ? Q.n : P.seq_q);
-            const float by = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-            __nv_bfloat16 *o = row_of(P.o, Q, i, at.head);
-            if (nt > 0) {
-                fence_after();
-#pragma unroll
-                for (int c = 0; c < kDim / 32; ++c) {
-                    uint32_t r[32];
-                    load_columns(o_at + c * 32, r);
-                    wait_loads();
-                    pin(r);
-                    if (wanted && limit > 0) store_row<kDim>(o, r, c * 32, P.head_dim, by);
-                }
-            }
-            if (wanted) {
-                if (limit == 0) zero_row(o, 0, P.head_dim);
-                P.lse[stat_at(P, Q, i, at.head)] = limit > 0 ? (top * scale + log2f(total)) * kLn2 : -INFINITY;
-            }
-        }
+        fence_after();
+        const int end = P.packed ? Q.n : P.seq_q;
+        // through this tile's queries, which no product reads any more
+        store_rows<kDim>(tiles + t * kBytes + warp % kGroupWarps * (32 * kDim * 2), o_at, nt > 0, 1.0f / total, limit > 0, P.o, Q, i - lane, end,
+                         at.head, 0, P.head_dim);
+        if (i < end) P.lse[stat_at(P, Q, i, at.head)] = limit > 0 ? (top * scale + log2f(total)) * kLn2 : -INFINITY;
     }
     __syncwarp();
     end_block<512>(S, tmem);
@@ -447,8 +461,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
         registers_few();
         if (warp == kLoadWarp && lane == 0 && n > 0) {
             Ring r;
+            // the last three places of the ring hold q, do and o until the softmax groups have read them
+            bar_expect(smem_addr(&S.stay), 3 * kBytes);
+            for (int x = 0; x < 3; ++x)
+#pragma unroll
+                for (int y = 0; y < kDim; y += 64)
+                    load_box(ring + (kSlots - 3 + x) * kBytes + y / 64 * (kTile * 128), x == 0 ? &M.q : x == 1 ? &M.d_o : &M.o, y, Q.first + first, at.head, Q.at,
+                             smem_addr(&S.stay));
             int sent = 0;
             for (int j = 0; j < 2 * n; ++j) {
+                if (j == kSlots - 3) bar_wait(smem_addr(&S.rows_in), 0, failed);
                 bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed);
                 if (*failed) break;
                 load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
@@ -457,6 +479,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
                 r.next<kSlots>();
             }
             if (*failed) {
+                settle(smem_addr(&S.stay), 0);
                 for (int j = max(0, sent - kSlots); j < sent; ++j)
                     if (ragged && j >= 2 * n - 2) settle(smem_addr(&S.last), 0);
                     else settle(smem_addr(&S.full[j % kSlots]), j / kSlots & 1);
@@ -515,26 +538,28 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
         const int limit = key_limit(Q, K, P.causal, i);
         const uint32_t lanes = static_cast<uint32_t>(warp % kGroupWarps * 32) << 16;
         const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
-        const bool wanted = i < (P.packed ? Q.n : P.seq_q);
-        // the first group brings in the rows of q, the second those of do, and D with them
+        const int end = P.packed ? Q.n : P.seq_q;
+        // the first group moves its rows of q to TMEM, the second those of do, and forms D on the way
         float dot = 0.0f;
+        if (n > 0) {
+            bar_wait(smem_addr(&S.stay), 0, failed);
+            __syncwarp();
 #pragma unroll
-        for (int c = 0; c < kDim / 64; ++c) {
-            const __nv_bfloat16 *from = row_of(t ? P.d_o : P.q, Q, i, at.head) + c * 64, *o = row_of(P.o, Q, i, at.head) + c * 64;
-            uint32_t r[32];
+            for (int c = 0; c < kDim / 64; ++c) {
+                const uint8_t *from = tiles + (kSlots - 3 + t) * kBytes + c * (kTile * 128) + row * 128;
+                uint32_t r[32];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                uint4 w = make_uint4(0, 0, 0, 0);
-                if (limit > 0 && c * 64 + x * 8 < P.head_dim) {
-                    w = *reinterpret_cast<const uint4 *>(from + x * 8);
+                for (int x = 0; x < 8; ++x) {
+                    const int at_piece = (x ^ (row & 7)) * 16;           // the copy's swizzle
+                    const uint4 w = *reinterpret_cast<const uint4 *>(from + at_piece);
+                    r[4 * x] = w.x; r[4 * x + 1] = w.y; r[4 * x + 2] = w.z; r[4 * x + 3] = w.w;
                     if (t) {
-                        const uint4 u = *reinterpret_cast<const uint4 *>(o + x * 8);
+                        const uint4 u = *reinterpret_cast<const uint4 *>(from + kBytes + at_piece);
                         dot = dot2(w.x, u.x, dot2(w.y, u.y, dot2(w.z, u.z, dot2(w.w, u.w, dot))));
                     }
                 }
-                r[4 * x] = w.x; r[4 * x + 1] = w.y; r[4 * x + 2] = w.z; r[4 * x + 3] = w.w;
+                store_columns((t ? do_at : q_at) + lanes + c * 32, r);
             }
-            store_columns((t ? do_at : q_at) + lanes + c * 32, r);
         }
         wait_stores();
         fence_before();
@@ -542,13 +567,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
         if (lane == 0) bar_arrive(smem_addr(&S.rows_in));
         if (t) S.row[0][0][row] = dot;
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        dot = S.row[0][0][row];
+        dot = limit > 0 ? S.row[0][0][row] : 0.0f;
         float shift = INFINITY;                  // a row that sees nothing has p = exp2(-inf) = 0
         if (limit > 0) {
             shift = P.lse[stat_at(P, Q, i, at.head)] * kLog2e;
             if (shift == -INFINITY) shift = INFINITY;
         }
-        if (t == 0 && wanted) P.row_dot[stat_at(P, Q, i, at.head)] = dot;
+        if (t == 0 && i < end) P.row_dot[stat_at(P, Q, i, at.head)] = dot;
         const float2 by = make_float2(scale, scale), minus = make_float2(-shift, -shift), less = make_float2(-dot, -dot);
         for (int j = 0; j < n; ++j) {
             bar_wait(smem_addr(&S.score[0]), j & 1, failed);
@@ -605,21 +630,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
         }
         if (n > 0) bar_wait(smem_addr(&S.done), 0, failed);
         __syncwarp();
-        {
-            __nv_bfloat16 *dq = row_of(P.dq, Q, i, at.head);
-            if (n > 0) {
-                fence_after();
-#pragma unroll
-                for (int c = t * (kDim / 64); c < (t + 1) * (kDim / 64); ++c) {
-                    uint32_t r[32];
-                    load_columns(dq_at + lanes + c * 32, r);
-                    wait_loads();
-                    pin(r);
-                    if (wanted && limit > 0) store_row<kDim>(dq, r, c * 32, P.head_dim, P.scale);
-                }
-            }
-            if (wanted && limit == 0) zero_row(dq, t * (kDim / 2), min((t + 1) * (kDim / 2), P.head_dim));
-        }
+        fence_after();
+        store_rows<kDim / 2>(tiles + warp * (32 * kDim), dq_at + lanes + t * (kDim / 2), n > 0, P.scale, limit > 0, P.dq, Q, i - lane, end, at.head,
+                             t * (kDim / 2), P.head_dim);
     }
     __syncwarp();
     end_block<512>(S, tmem);
@@ -869,21 +882,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
         }
         if (n > 0) bar_wait(smem_addr(&S.done), 0, failed);
         __syncwarp();
-        // the first group writes dv, the second dk
-        const bool wanted = key < (P.packed ? K.n : P.seq_k);
-        __nv_bfloat16 *out = t ? row_of(P.dk, K, key, at.head) : row_of(P.dv, K, key, at.head);
-        if (n > 0) {
-            fence_after();
-#pragma unroll
-            for (int c = 0; c < kDim / 32; ++c) {
-                uint32_t r[32];
-                load_columns((t ? dk_at : dv_at) + lanes + c * 32, r);
-                wait_loads();
-                pin(r);
-                if (wanted && key < K.n) store_row<kDim>(out, r, c * 32, P.head_dim, t ? P.scale : 1.0f);
-            }
-        }
-        if (wanted && (key >= K.n || n == 0)) zero_row(out, 0, P.head_dim);
+        fence_after();
+        // the first group writes dv, the second dk, each through one of the tiles that stayed
+        store_rows<kDim>(tiles + t * kBytes + warp % kGroupWarps * (32 * kDim * 2), (t ? dk_at : dv_at) + lanes, n > 0, t ? P.scale : 1.0f, key < K.n,
+                         t ? P.dk : P.dv, K, key - lane, P.packed ? K.n : P.seq_k, at.head, 0, P.head_dim);
     }
     __syncwarp();
     end_block<512>(S, tmem);
@@ -956,24 +958,27 @@ int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const 
     return launched();
 }
 
-bool make_maps(const AttentionParams &P, Maps &M, int query_box, bool gradient) {
-    const int b = P.packed ? 1 : P.batch;
-    const void *any = P.seq_q > 0 ? P.q.ptr : P.k.ptr;
-    return make_map(M.q, P.q, b, P.heads_q, P.seq_q, P.head_dim, query_box, any) && make_map(M.k, P.k, b, P.heads_kv, P.seq_k, P.head_dim, kTile, any) &&
-           make_map(M.v, P.v, b, P.heads_kv, P.seq_k, P.head_dim, kTile, any) &&
-           (!gradient || make_map(M.d_o, P.d_o, b, P.heads_q, P.seq_q, P.head_dim, query_box, any));
+// What each kernel reads, in boxes of its own tiles.
+bool make_query_map(const AttentionParams &P, CUtensorMap &map, const Heads &t, int box_rows) {
+    return make_map(map, t, P.packed ? 1 : P.batch, P.heads_q, P.seq_q, P.head_dim, box_rows, P.seq_q > 0 ? P.q.ptr : P.k.ptr);
+}
+bool make_key_map(const AttentionParams &P, CUtensorMap &map, const Heads &t) {
+    return make_map(map, t, P.packed ? 1 : P.batch, P.heads_kv, P.seq_k, P.head_dim, kTile, P.seq_q > 0 ? P.q.ptr : P.k.ptr);
 }
 
 template <int kDim> int forward(const AttentionParams &P, cudaStream_t stream) {
     Maps M;
-    if (!make_maps(P, M, kTile, false)) return LOCO_ERR_CUDA;
+    if (!make_query_map(P, M.q, P.q, kTile) || !make_key_map(P, M.k, P.k) || !make_key_map(P, M.v, P.v)) return LOCO_ERR_CUDA;
     return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, P, M, stream);
 }
 template <int kDim> int backward(const AttentionParams &P, cudaStream_t stream) {
-    Maps M;                                      // the first kernel reads k and v through it only
-    if (!make_maps(P, M, query_tile<kDim>(), true)) return LOCO_ERR_CUDA;
+    Maps M;
+    if (!make_query_map(P, M.q, P.q, kTile) || !make_query_map(P, M.d_o, P.d_o, kTile) || !make_query_map(P, M.o, P.o, kTile) ||
+        !make_key_map(P, M.k, P.k) || !make_key_map(P, M.v, P.v)) return LOCO_ERR_CUDA;
     const int rc = launch(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + kTile - 1) / kTile, P.heads_q, P, M, stream);
     if (rc != LOCO_OK) return rc;
+    if (query_tile<kDim>() != kTile && (!make_query_map(P, M.q, P.q, query_tile<kDim>()) || !make_query_map(P, M.d_o, P.d_o, query_tile<kDim>())))
+        return LOCO_ERR_CUDA;
     return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream);
 }
 
