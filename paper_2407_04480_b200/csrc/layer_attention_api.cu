@@ -16,14 +16,15 @@ int check_attention(const loco_attention_t *c) {
     return LOCO_OK;
 }
 
-// An operand with rows: present, on 16-byte boundaries, strides of whole 16-byte units and none negative.
-int take(const loco_heads_t *t, int64_t rows, Heads &out) {
+// An operand with rows: present, on 16-byte boundaries, strides of whole 16-byte units and none negative.  The stride of a
+// dimension of extent one means nothing.
+int take(const loco_attention_t *c, const loco_heads_t *t, int32_t heads, int32_t rows, Heads &out) {
     if (!t) return LOCO_ERR_ARG;
-    out = Heads{static_cast<__nv_bfloat16 *>(t->ptr), t->batch_stride, t->row_stride, t->head_stride};
-    if (rows == 0) return LOCO_OK;
-    if (!t->ptr) return LOCO_ERR_ARG;
-    if (t->batch_stride < 0 || t->row_stride < 0 || t->head_stride < 0) return LOCO_ERR_ARG;
-    if (!aligned(t->ptr, 16) || t->batch_stride % 8 || t->row_stride % 8 || t->head_stride % 8) return LOCO_ERR_ALIGN;
+    const int64_t b = c->packed || c->batch <= 1 ? 0 : t->batch_stride, r = rows <= 1 ? 0 : t->row_stride, h = heads <= 1 ? 0 : t->head_stride;
+    out = Heads{static_cast<__nv_bfloat16 *>(t->ptr), b, r, h};
+    if (rows == 0 || c->batch == 0) return LOCO_OK;
+    if (!t->ptr || b < 0 || r < 0 || h < 0) return LOCO_ERR_ARG;
+    if (!aligned(t->ptr, 16) || b % 8 || r % 8 || h % 8) return LOCO_ERR_ALIGN;
     return LOCO_OK;
 }
 
@@ -58,10 +59,10 @@ int loco_attention_forward(const loco_attention_t *c, const loco_heads_t *q, con
     AttentionParams P{};
     int rc = fill(c, P);
     const int64_t nq = rc == LOCO_OK ? rows_of(c, c->seq_q) : 0, nk = rc == LOCO_OK ? rows_of(c, c->seq_k) : 0;
-    if (rc == LOCO_OK) rc = take(q, nq, P.q);
-    if (rc == LOCO_OK) rc = take(k, nk, P.k);
-    if (rc == LOCO_OK) rc = take(v, nk, P.v);
-    if (rc == LOCO_OK) rc = take(o, nq, P.o);
+    if (rc == LOCO_OK) rc = take(c, q, c->heads_q, c->seq_q, P.q);
+    if (rc == LOCO_OK) rc = take(c, k, c->heads_kv, c->seq_k, P.k);
+    if (rc == LOCO_OK) rc = take(c, v, c->heads_kv, c->seq_k, P.v);
+    if (rc == LOCO_OK) rc = take(c, o, c->heads_q, c->seq_q, P.o);
     if (rc != LOCO_OK) return rc;
     if (nq == 0) return LOCO_OK;
     if (!d_lse) return LOCO_ERR_ARG;
@@ -81,14 +82,14 @@ int loco_attention_backward(const loco_attention_t *c, const loco_heads_t *q, co
     AttentionParams P{};
     int rc = fill(c, P);
     const int64_t nq = rc == LOCO_OK ? rows_of(c, c->seq_q) : 0, nk = rc == LOCO_OK ? rows_of(c, c->seq_k) : 0;
-    if (rc == LOCO_OK) rc = take(q, nq, P.q);
-    if (rc == LOCO_OK) rc = take(k, nk, P.k);
-    if (rc == LOCO_OK) rc = take(v, nk, P.v);
-    if (rc == LOCO_OK) rc = take(o, nq, P.o);
-    if (rc == LOCO_OK) rc = take(d_o, nq, P.d_o);
-    if (rc == LOCO_OK) rc = take(dq, nq, P.dq);
-    if (rc == LOCO_OK) rc = take(dk, nk, P.dk);
-    if (rc == LOCO_OK) rc = take(dv, nk, P.dv);
+    if (rc == LOCO_OK) rc = take(c, q, c->heads_q, c->seq_q, P.q);
+    if (rc == LOCO_OK) rc = take(c, k, c->heads_kv, c->seq_k, P.k);
+    if (rc == LOCO_OK) rc = take(c, v, c->heads_kv, c->seq_k, P.v);
+    if (rc == LOCO_OK) rc = take(c, o, c->heads_q, c->seq_q, P.o);
+    if (rc == LOCO_OK) rc = take(c, d_o, c->heads_q, c->seq_q, P.d_o);
+    if (rc == LOCO_OK) rc = take(c, dq, c->heads_q, c->seq_q, P.dq);
+    if (rc == LOCO_OK) rc = take(c, dk, c->heads_kv, c->seq_k, P.dk);
+    if (rc == LOCO_OK) rc = take(c, dv, c->heads_kv, c->seq_k, P.dv);
     if (rc != LOCO_OK) return rc;
     if (nq == 0 && nk == 0) return LOCO_OK;
     if (!d_work || (nq > 0 && !d_lse)) return LOCO_ERR_ARG;

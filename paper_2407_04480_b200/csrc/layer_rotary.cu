@@ -230,11 +230,14 @@ int loco_rotary_apply(const loco_rotary_t *c, const float *d_table, const void *
         if (heads[i] == 0) continue;
         if (!x[i].ptr || !y[i].ptr) return LOCO_ERR_ARG;
         if (!aligned(x[i].ptr, static_cast<uintptr_t>(size)) || !aligned(y[i].ptr, static_cast<uintptr_t>(size))) return LOCO_ERR_ALIGN;
-        P.t[i] = RotaryTensor{x[i].ptr, y[i].ptr, x[i].batch_stride, x[i].row_stride, x[i].head_stride,
-                              y[i].batch_stride, y[i].row_stride, y[i].head_stride, static_cast<uint32_t>(heads[i]), 0};
-        wide = wide && aligned(x[i].ptr, 16) && aligned(y[i].ptr, 16);
-        for (int64_t s : {x[i].batch_stride, x[i].row_stride, x[i].head_stride, y[i].batch_stride, y[i].row_stride, y[i].head_stride})
-            wide = wide && s % vec == 0;
+        RotaryTensor &t = P.t[i];
+        t = RotaryTensor{x[i].ptr, y[i].ptr, x[i].batch_stride, x[i].row_stride, x[i].head_stride,
+                         y[i].batch_stride, y[i].row_stride, y[i].head_stride, static_cast<uint32_t>(heads[i]), 0};
+        if (c->batch == 1) t.xb = t.yb = 0;              // the stride of a dimension of extent one means nothing
+        if (c->seq == 1) t.xr = t.yr = 0;
+        if (heads[i] == 1) t.xh = t.yh = 0;
+        wide = wide && aligned(t.x, 16) && aligned(t.y, 16);
+        for (int64_t s : {t.xb, t.xr, t.xh, t.yb, t.yr, t.yh}) wide = wide && s % vec == 0;
     }
     P.table = d_table;
     P.positions = d_positions;

@@ -73,40 +73,43 @@ def _check(code: int, where: str) -> None:
         raise LocoError(code, where)
 
 
-def _stream(stream: Optional[torch.cuda.Stream], device: torch.device) -> int:
+# torch's accessor of the current stream's address; torch.cuda.current_stream() builds an object around it, which takes as
+# long as a launch
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
     """The raw stream; the current device must be the operands' own, as for every call of the library."""
-    if torch.cuda.current_device() != device.index:
-        raise ValueError("the operands live on %s, which is not the current device" % device)
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    if torch.cuda.current_device() != device:
+        raise ValueError("the operands live on cuda:%d, which is not the current device" % device)
+    return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
 def _dtype(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return F32
     raise ValueError("expected bfloat16 or float32, got %s" % t.dtype)
 
 
-def _heads(t: torch.Tensor, shape, dtype, device) -> Tuple[int, int, int, int]:
+def _heads(t: torch.Tensor, shape, dtype, device: int) -> Tuple[int, int, int, int]:
     """(address, batch, row, head stride) of a [batch, row, head, dim] or [row, head, dim] tensor."""
-    if t.dtype != dtype or t.device != device:
-        raise ValueError("all heads must be %s on %s" % (dtype, device))
+    if t.dtype is not dtype or t.get_device() != device:
+        raise ValueError("all heads must be %s on cuda:%d" % (dtype, device))
     if t.shape != shape:
         raise ValueError("expected heads of shape %s, got %s" % (tuple(shape), tuple(t.shape)))
     s = t.stride()
     if s[-1] != 1 and shape[-1] != 1:
         raise ValueError("the dimensions of a head must be contiguous")
-    if 1 in shape[:-1]:                                # the stride of a single row means nothing
-        s = tuple(0 if n == 1 else x for n, x in zip(shape, s))
     return (t.data_ptr(), s[0], s[1], s[2]) if len(s) == 4 else (t.data_ptr(), 0, s[0], s[1])
 
 
-def _flat(t: Optional[torch.Tensor], shape, dtype, device, what: str) -> Optional[int]:
+def _flat(t: Optional[torch.Tensor], shape, dtype, device: int, what: str) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d" % (what, dtype, tuple(shape), device))
     return t.data_ptr()
 
 
@@ -133,7 +136,7 @@ def loco_rotary_table(table: torch.Tensor, base: float = 10000.0, scaling: str =
     if scaling not in SCALINGS:
         raise ValueError("scaling must be one of %s" % (tuple(SCALINGS),))
     cfg = _TABLE.pack(table.shape[1], table.shape[0], SCALINGS[scaling], base, factor, trained, slow, fast, magnitude)
-    _check(lib().loco_rotary_table(cfg, table.data_ptr(), _stream(stream, table.device)), "loco_rotary_table")
+    _check(lib().loco_rotary_table(cfg, table.data_ptr(), _stream(stream, table.get_device())), "loco_rotary_table")
 
 
 def loco_rotary_apply(table: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor], q_out: torch.Tensor,
@@ -142,33 +145,36 @@ def loco_rotary_apply(table: torch.Tensor, q: torch.Tensor, k: Optional[torch.Te
     """Rotate q [batch, seq, heads, dim] into q_out and k (or None) into k_out; an output may be its input.
 
     table: from loco_rotary_table; positions: int32 or int64 [batch, seq], None for 0, 1, 2, ... in every sample."""
-    if layout not in LAYOUTS:
+    kind = LAYOUTS.get(layout)
+    if kind is None:
         raise ValueError("layout must be one of %s" % (tuple(LAYOUTS),))
-    device, shape = q.device, q.shape
-    if not q.is_cuda or len(shape) != 4:
+    device, shape, dtype, tshape = q.get_device(), q.shape, q.dtype, table.shape
+    if device < 0 or len(shape) != 4:
         raise ValueError("expected CUDA heads [batch, seq, heads, dim]")
-    if table.dim() != 2 or table.dtype != torch.float32 or table.device != device or not table.is_contiguous():
-        raise ValueError("the table must be a contiguous fp32 tensor [positions, rotary_dim] on %s" % device)
-    x = _heads(q, shape, q.dtype, device)
-    y = _heads(q_out, shape, q.dtype, device)
+    if table.dtype is not torch.float32 or len(tshape) != 2 or table.get_device() != device or not table.is_contiguous():
+        raise ValueError("the table must be a contiguous fp32 tensor [positions, rotary_dim] on cuda:%d" % device)
+    b, n, hq, d = shape
     hk = 0
     if k is None:
-        xs, ys = _HEADS.pack(*x), _HEADS.pack(*y)
+        xs, ys = _HEADS.pack(*_heads(q, shape, dtype, device)), _HEADS.pack(*_heads(q_out, shape, dtype, device))
     else:
-        if len(k.shape) != 4 or k.shape[:2] != shape[:2] or k.shape[3] != shape[3] or k_out is None:
+        kshape = k.shape
+        if len(kshape) != 4 or kshape[0] != b or kshape[1] != n or kshape[3] != d or k_out is None:
             raise ValueError("k must have q's batch, rows and head size, and an output")
-        hk = k.shape[2]
-        xs = _TWO_HEADS.pack(*x, *_heads(k, k.shape, q.dtype, device))
-        ys = _TWO_HEADS.pack(*y, *_heads(k_out, k.shape, q.dtype, device))
+        hk = kshape[2]
+        xs = _TWO_HEADS.pack(*_heads(q, shape, dtype, device), *_heads(k, kshape, dtype, device))
+        ys = _TWO_HEADS.pack(*_heads(q_out, shape, dtype, device), *_heads(k_out, kshape, dtype, device))
     at, wide = None, 0
     if positions is not None:
-        wide = positions.element_size()
-        if positions.dtype not in (torch.int32, torch.int64):
+        if positions.dtype is torch.int32:
+            wide = 4
+        elif positions.dtype is torch.int64:
+            wide = 8
+        else:
             raise ValueError("positions must be int32 or int64")
-        at = _flat(positions, shape[:2], positions.dtype, device, "positions")
-    rows, r = table.shape
-    cfg = _ROTARY.pack(_dtype(q), LAYOUTS[layout], shape[3], r, shape[0], shape[1], rows, wide, 1 if inverse else 0)
-    _check(lib().loco_rotary_apply(cfg, table.data_ptr(), at, xs, ys, _TWO_INTS.pack(shape[2], hk), 1 if k is None else 2,
+        at = _flat(positions, (b, n), positions.dtype, device, "positions")
+    cfg = _ROTARY.pack(_dtype(q), kind, d, tshape[1], b, n, tshape[0], wide, 1 if inverse else 0)
+    _check(lib().loco_rotary_apply(cfg, table.data_ptr(), at, xs, ys, _TWO_INTS.pack(hq, hk), 1 if k is None else 2,
                                    _stream(stream, device)), "loco_rotary_apply")
 
 
@@ -176,10 +182,10 @@ def loco_rotary_apply(table: torch.Tensor, q: torch.Tensor, k: Optional[torch.Te
 
 def _attention_config(q, k, causal, scale, len_q, len_k, cu_q, cu_k, max_q, max_k) -> Tuple[bytes, tuple]:
     """loco_attention_t and the shape of the log-sum-exp."""
-    if not q.is_cuda or q.dtype != torch.bfloat16:
+    if not q.is_cuda or q.dtype is not torch.bfloat16:
         raise ValueError("attention takes bfloat16 CUDA tensors")
     packed = cu_q is not None or cu_k is not None
-    device, qs, ks = q.device, q.shape, k.shape
+    device, qs, ks = q.get_device(), q.shape, k.shape
     if len(qs) != (3 if packed else 4) or len(ks) != len(qs) or ks[-1] != qs[-1]:
         raise ValueError("expected heads [batch, row, head, dim], or [row, head, dim] with cu_q and cu_k")
     if packed:
@@ -210,7 +216,7 @@ def loco_attention_forward(q, k, v, o, lse, causal: bool = False, scale: Optiona
     len_q, len_k int32 [batch] (None: seq).  Packed: q, o [rows_q, heads, dim], k, v [rows_k, heads_kv, dim], lse
     [heads, rows_q], offsets cu_q, cu_k int32 [batch + 1], max_q, max_k the longest sample.  scale: None = 1/sqrt(dim)."""
     cfg, stats = _attention_config(q, k, causal, scale, len_q, len_k, cu_q, cu_k, max_q, max_k)
-    dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
+    dev, dt, qs, ks = q.get_device(), q.dtype, q.shape, k.shape
     _check(lib().loco_attention_forward(cfg, _HEADS.pack(*_heads(q, qs, dt, dev)), _HEADS.pack(*_heads(k, ks, dt, dev)),
                                         _HEADS.pack(*_heads(v, ks, dt, dev)), _HEADS.pack(*_heads(o, qs, dt, dev)),
                                         _flat(lse, stats, torch.float32, dev, "lse"), _stream(stream, dev)),
@@ -229,9 +235,9 @@ def loco_attention_backward(q, k, v, o, lse, do, dq, dk, dv, work, causal: bool 
 
     work: a contiguous CUDA tensor of loco_attention_backward_workspace_bytes() bytes or more."""
     cfg, stats = _attention_config(q, k, causal, scale, len_q, len_k, cu_q, cu_k, max_q, max_k)
-    dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
-    if work.device != dev or not work.is_contiguous():
-        raise ValueError("the workspace must be a contiguous tensor on %s" % dev)
+    dev, dt, qs, ks = q.get_device(), q.dtype, q.shape, k.shape
+    if work.get_device() != dev or not work.is_contiguous():
+        raise ValueError("the workspace must be a contiguous tensor on cuda:%d" % dev)
     _check(lib().loco_attention_backward(cfg, _HEADS.pack(*_heads(q, qs, dt, dev)), _HEADS.pack(*_heads(k, ks, dt, dev)),
                                          _HEADS.pack(*_heads(v, ks, dt, dev)), _HEADS.pack(*_heads(o, qs, dt, dev)),
                                          _flat(lse, stats, torch.float32, dev, "lse"), _HEADS.pack(*_heads(do, qs, dt, dev)),
@@ -272,9 +278,9 @@ def loco_router_forward(cfg: Router, logits, index, weight, counts, mean, losses
 
     work: a CUDA tensor of loco_router_workspace_bytes() bytes, zero before its first use."""
     n, at, stride = _rows(logits, cfg, "logits")
-    dev, k = logits.device, cfg.top_k
-    if work.device != dev or not work.is_contiguous():
-        raise ValueError("the workspace must be a contiguous tensor on %s" % dev)
+    dev, k = logits.get_device(), cfg.top_k
+    if work.get_device() != dev or not work.is_contiguous():
+        raise ValueError("the workspace must be a contiguous tensor on cuda:%d" % dev)
     _check(lib().loco_router_forward(cfg.c(_dtype(logits)), n, at, stride, _flat(mask, (n,), torch.uint8, dev, "mask"),
                                      _flat(index, (n, k), torch.int32, dev, "index"),
                                      _flat(weight, (n, k), torch.float32, dev, "weight"),
@@ -288,7 +294,7 @@ def loco_router_backward(cfg: Router, logits, index, counts, dlogits, mask=None,
                          stream=None) -> None:
     """Gradient of the logits from those of the two losses (fp32 [2]) and of the weights (fp32 [tokens, top_k])."""
     n, at, stride = _rows(logits, cfg, "logits")
-    dev, k = logits.device, cfg.top_k
+    dev, k = logits.get_device(), cfg.top_k
     n2, dat, dstride = _rows(dlogits, cfg, "dlogits")
     if n2 != n or dlogits.dtype != logits.dtype:
         raise ValueError("dlogits must have the logits' shape and type")

@@ -85,7 +85,7 @@ def test_attention_refuses_bad_operands():
     assert forward(cfg, v=heads(r=-128)) == loco.ERR_ARG
     assert forward(cfg, k=heads(ptr=PTR + 8)) == loco.ERR_ALIGN
     assert forward(cfg, k=heads(h=124)) == loco.ERR_ALIGN
-    assert forward(cfg, o=heads(b=4)) == loco.ERR_ALIGN
+    assert forward(attention_cfg(batch=2), o=heads(b=4)) == loco.ERR_ALIGN
     assert forward(cfg, lse=None) == loco.ERR_ARG
     assert forward(cfg, lse=PTR + 2) == loco.ERR_ALIGN
     need = L.loco_attention_backward_workspace_bytes(cfg)
