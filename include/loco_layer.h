@@ -126,7 +126,7 @@ int loco_attention_backward(const loco_attention_t *cfg, const loco_heads_t *q, 
  *   weight: p / (sum of the chosen p) with normalize, else p
  *   n_e = tokens that chose e;  P_e = (1/N) sum_t p_te
  *   balance loss = balance_coef * E * sum_e n_e / (N top_k) * P_e        z loss = z_coef / N * sum_t lse_t^2
- * The counts are constants of the gradient.  A NaN logit counts as the largest and makes both losses NaN.
+ * The counts are constants of the gradient.  A NaN logit counts as +infinity in the choice and makes both losses NaN.
  */
 typedef struct {
     int32_t dtype;           /* loco_dtype_t of the logits and of their gradient          */

@@ -1,22 +1,24 @@
 // Top-k router with balance and z loss: one pass over the logits forward, one backward.
 //
+// A token belongs to a group of kGroup lanes, each with kMine of its logits in registers (eight experts or fewer: one
+// thread; 256 or more: a warp), read as 16-byte vectors where rows allow it, the next token's while this one is worked on.
+// The passes are bound by instructions, not by HBM: the k rounds of the choice cost a few dozen each.
+//
 // Forward: softmax, choice and weights are local to a token; the losses need the sums over tokens of p_te, of lse^2 and
-// the counts.  Every thread (up to 32 experts) or lane (more) keeps the sums of its own experts in registers over all
-// its tokens, the block adds them up in a fixed order and leaves one partial row in the workspace, and the block that
-// finishes last adds the rows, again in a fixed order.  One launch, and no floating-point atomics.
+// the counts.  Every lane keeps the sums of its own experts in registers over all its tokens, the block adds them up in a
+// fixed order and leaves one partial row in the workspace, and the block that finishes last adds the rows, again in a fixed
+// order.  One launch, and no floating-point atomics.
 // Backward: with the counts known the gradient of a token's logits is local to the token again; it is recomputed from
 // the logits, which are the only thing both passes have to read.
 #include "layer_common.h"
 
 namespace loco_layer {
 
-constexpr int kRouterThreads = 256;
-constexpr int kRouterWarps = kRouterThreads / 32;
 constexpr int kMaxExperts = 512;
 constexpr int kMaxChoice = 16;
-constexpr int kBlocksPerSm = 2;
-constexpr int kMaxBlocks = 512;                     // partial rows the workspace holds
+constexpr int kMaxBlocks = 256;                     // partial rows the workspace holds
 constexpr unsigned kAll = 0xffffffffu;
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct RouterParams {
     const void *logits;
@@ -49,68 +51,107 @@ __device__ __forceinline__ double warp_sum(double x) {
     return x;
 }
 
-// Order of the choice as unsigned integers: larger logit first, NaN before all.  -inf maps to 0x007fffff; 0 is free.
-__device__ __forceinline__ unsigned order_key(float z) {
-    const unsigned u = __float_as_uint(z);
-    const unsigned k = u & 0x80000000u ? ~u : u | 0x80000000u;
-    return z != z ? 0xffffffffu : (z == 0.0f ? 0x80000000u : k);
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-constexpr unsigned kKeyMinusInf = 0x007fffffu;
 
-// A row of up to N logits, -inf where there is none.
-template <typename T, int N, bool kWide> __device__ __forceinline__ void load_row(const T *row, int experts, float *z) {
-    constexpr int kV = 16 / sizeof(T);
-    if constexpr (kWide) {
+// Which expert the lane's i-th value belongs to: vectors of 16 bytes go round the group, single values otherwise.
+template <typename T, int kGroup, bool kWide> __device__ __forceinline__ int expert_of(int lane, int i) {
+    constexpr int kV = kWide ? 16 / static_cast<int>(sizeof(T)) : 1;
+    return (i / kV * kGroup + lane) * kV + i % kV;
+}
+
+// The lane's part of a row as it lies in memory; what is past the last expert reads as -inf.
+template <typename T, int kGroup, int kMine, bool kWide> struct Row {
+    static constexpr int kV = kWide ? 16 / static_cast<int>(sizeof(T)) : 1;
+    Pack<T, kV> v[kMine / kV];
+    __device__ __forceinline__ void load(const T *row, int lane, int experts) {
 #pragma unroll
-        for (int i = 0; i < N / kV; ++i) {
-            if (i * kV < experts) {
-                const Pack<T, kV> p = *reinterpret_cast<const Pack<T, kV> *>(row + i * kV);
-#pragma unroll
-                for (int j = 0; j < kV; ++j) z[i * kV + j] = to_f32(p.v[j]);
+        for (int i = 0; i < kMine / kV; ++i) {
+            const int e = (i * kGroup + lane) * kV;
+            if (e < experts) {
+                v[i] = *reinterpret_cast<const Pack<T, kV> *>(row + e);
             } else {
 #pragma unroll
-                for (int j = 0; j < kV; ++j) z[i * kV + j] = -INFINITY;
+                for (int x = 0; x < kV; ++x) v[i].v[x] = from_f32<T>(-INFINITY);
             }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = i < experts ? to_f32(row[i]) : -INFINITY;
     }
+    __device__ __forceinline__ float operator[](int i) const { return to_f32(v[i / kV].v[i % kV]); }
+};
+
+template <int kGroup> __device__ __forceinline__ float group_sum(float x) {
+#pragma unroll
+    for (int o = kGroup / 2; o; o >>= 1) x += __shfl_xor_sync(kAll, x, o);
+    return x;
+}
+template <int kGroup> __device__ __forceinline__ float group_max(float x) {
+#pragma unroll
+    for (int o = kGroup / 2; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kAll, x, o));
+    return x;
+}
+
+// p[i] = exp(z[i] - top), their sum and log-sum-exp over the group; false where no expert is available.
+template <int kGroup, int kMine> __device__ __forceinline__ bool softmax(const float *z, float *p, float &top, float &total, float &lse) {
+    top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) top = fmaxf(top, z[i]);
+    top = group_max<kGroup>(top);
+    const bool some = top != -INFINITY;
+    const float from = some ? top : 0.0f;
+    total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        p[i] = exp2_fast((z[i] - from) * kLog2e);   // -inf gives 0
+        total += p[i];
+    }
+    total = group_sum<kGroup>(total);
+    lse = logf(total) + from;
+    return some || total != total;
 }
 
 // Adds the blocks' partial rows once all of them are written; called by every thread with the block's own row in shared
 // memory: sums[E], tally[E], extra = {sum of lse^2, active tokens}.
 __device__ void finish(const RouterParams &P, const float *sums, const int *tally, float zsq, int active) {
     __shared__ bool last;
-    __shared__ double fold[kRouterThreads];
-    __shared__ int ifold[kRouterThreads];
+    __shared__ double fold[1024];
+    __shared__ int ifold[1024];
     __shared__ float mean[kMaxExperts];
     __shared__ int count[kMaxExperts];
-    const int E = P.experts, width = 2 * E + 2, tid = threadIdx.x;
+    const int E = P.experts, width = 2 * E + 2, tid = threadIdx.x, threads = blockDim.x;
     const int blocks = static_cast<int>(gridDim.x);
-    float *mine = P.part + static_cast<int64_t>(blockIdx.x) * width;
-    for (int e = tid; e < E; e += kRouterThreads) {
-        mine[e] = sums[e];
-        mine[E + e] = __int_as_float(tally[e]);
+    if (blocks > 1) {
+        float *mine = P.part + static_cast<int64_t>(blockIdx.x) * width;
+        for (int e = tid; e < E; e += threads) {
+            mine[e] = sums[e];
+            mine[E + e] = __int_as_float(tally[e]);
+        }
+        if (tid == 0) {
+            mine[2 * E] = zsq;
+            mine[2 * E + 1] = __int_as_float(active);
+        }
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) last = atomicAdd(P.ticket, 1u) == gridDim.x - 1;
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+        if (tid == 0) *P.ticket = 0;
     }
-    if (tid == 0) {
-        mine[2 * E] = zsq;
-        mine[2 * E + 1] = __int_as_float(active);
-    }
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) last = atomicAdd(P.ticket, 1u) == gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    if (tid == 0) *P.ticket = 0;
     // slices of blocks per column, so that few experts still use all threads
     int slices = 1;
-    while (slices * 2 * (E + 1) <= kRouterThreads && slices < blocks) slices *= 2;
-    double zz = 0.0;
-    int n = 0;
+    while (slices * 2 * (E + 1) <= threads && slices < blocks && slices < 32) slices *= 2;
+    double zz = zsq;
+    int n = active;
+    if (blocks == 1)
+        for (int e = tid; e < E; e += threads) {
+            mean[e] = sums[e];
+            count[e] = tally[e];
+        }
     const int columns = E + 1;                        // the last one: lse^2 and active tokens
-    for (int c0 = 0; c0 < columns; c0 += kRouterThreads / slices) {
+    for (int c0 = blocks == 1 ? columns : 0; c0 < columns; c0 += threads / slices) {
         const int c = c0 + tid / slices, s = tid % slices;
         double a = 0.0;
         int k = 0;
@@ -140,7 +181,7 @@ __device__ void finish(const RouterParams &P, const float *sums, const int *tall
             }
         }
         __syncthreads();
-        if (c0 + kRouterThreads / slices >= columns) {
+        if (c0 + threads / slices >= columns) {
             zz = fold[(columns - 1 - c0) * slices];
             n = ifold[(columns - 1 - c0) * slices];
         }
@@ -148,7 +189,7 @@ __device__ void finish(const RouterParams &P, const float *sums, const int *tall
     }
     const double per = n > 0 ? 1.0 / n : 0.0;
     double load = 0.0;
-    for (int e = tid; e < E; e += kRouterThreads) {
+    for (int e = tid; e < E; e += threads) {
         const float m = static_cast<float>(mean[e] * per);
         P.mean[e] = m;
         P.counts[e] = count[e];
@@ -159,385 +200,286 @@ __device__ void finish(const RouterParams &P, const float *sums, const int *tall
     __syncthreads();
     if (tid == 0) {
         double all = 0.0;
-        for (int w = 0; w < kRouterWarps; ++w) all += fold[w];
+        for (int w = 0; w < threads / 32; ++w) all += fold[w];
         P.counts[E] = n;
         P.losses[0] = static_cast<float>(static_cast<double>(P.balance_coef) * E * all * per / P.top_k);
         P.losses[1] = static_cast<float>(static_cast<double>(P.z_coef) * zz * per);
     }
 }
 
-// Softmax of a row kept by one thread: z becomes exp(z - max); false where no expert is available.
-template <int N> __device__ __forceinline__ bool row_softmax(float *z, float &total, float &lse) {
-    float top = -INFINITY;
-    bool nan = false;
+// The choice among a token's logits: next() gives the group's largest one left, lowest expert first, and takes it out.
+// fp32: the largest value, then the lowest expert that has it, one reduction over the group each.  NaN counts as +inf.
+template <typename T, int kGroup, int kMine, bool kWide> struct Chooser {
+    float z[kMine];
+    __device__ __forceinline__ Chooser(const float *from, int) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        top = fmaxf(top, z[i]);
-        nan |= z[i] != z[i];
+        for (int i = 0; i < kMine; ++i) z[i] = from[i] != from[i] ? INFINITY : from[i];
     }
-    if (top == -INFINITY && !nan) return false;
-    total = 0.0f;
+    __device__ __forceinline__ int next(int lane, float &value) {
+        float best = z[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        z[i] = z[i] == -INFINITY ? 0.0f : expf(z[i] - top);
-        total += z[i];
+        for (int i = 1; i < kMine; ++i) best = fmaxf(best, z[i]);
+        best = group_max<kGroup>(best);
+        value = best;
+        int mine = kMine;
+#pragma unroll
+        for (int i = kMine - 1; i >= 0; --i) mine = z[i] == best ? i : mine;
+        // the lane's first place with it, as an expert
+        constexpr int kV = kWide ? 16 / static_cast<int>(sizeof(T)) : 1;
+        const int own = mine < kMine ? (mine / kV * kGroup + lane) * kV + mine % kV : 0x7fffffff;
+        int at = own;
+#pragma unroll
+        for (int o = kGroup / 2; o; o >>= 1) at = min(at, __shfl_xor_sync(kAll, at, o));
+        mine = own == at ? mine : kMine;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) z[i] = i == mine ? -INFINITY : z[i];
+        return best == -INFINITY ? -1 : at;
     }
-    lse = logf(total) + top;
-    return true;
-}
+};
+// bfloat16: value and expert fit one integer whose order is the choice's (order of the value in the upper half, 0xffff -
+// expert in the lower), so that one reduction finds both.  Adding 0 makes -0 and NaN plain.
+template <int kGroup, int kMine, bool kWide> struct Chooser<__nv_bfloat16, kGroup, kMine, kWide> {
+    unsigned key[kMine];
+    __device__ __forceinline__ Chooser(const float *from, int lane) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int u = __float_as_int(from[i] + 0.0f);
+            key[i] = ((u ^ (u >> 31 | 0x80000000u)) & 0xffff0000u) | (0xffffu - expert_of<__nv_bfloat16, kGroup, kWide>(lane, i));
+        }
+    }
+    __device__ __forceinline__ int next(int, float &value) {
+        unsigned best = key[0];
+#pragma unroll
+        for (int i = 1; i < kMine; ++i) best = max(best, key[i]);
+        if constexpr (kGroup == 32) {
+            best = __reduce_max_sync(kAll, best);
+        } else {
+#pragma unroll
+            for (int o = kGroup / 2; o; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
+        }
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) key[i] = key[i] == best ? 0u : key[i];
+        const unsigned v = best & 0xffff0000u;
+        value = __uint_as_float(v & 0x80000000u ? v ^ 0x80000000u : ~v & 0xffff0000u);
+        return v <= 0x007f0000u ? -1 : static_cast<int>(0xffffu - (best & 0xffffu));
+    }
+};
 
-// Up to 32 experts: a thread per token.
-template <typename T, int N, bool kWide>
-__global__ void __launch_bounds__(kRouterThreads) router_forward_thread(const __grid_constant__ RouterParams P) {
-    __shared__ float sums[kRouterWarps][N];
-    __shared__ int tally[kRouterWarps][N];
-    __shared__ float extra[kRouterWarps];
-    __shared__ int active[kRouterWarps];
-    const int E = P.experts, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    float sum[N], zsq = 0.0f;
-    int cnt[N], act = 0;
+// Where a lane keeps the group's choices: choice j in lane j % kGroup, place j / kGroup.
+template <int kGroup, int kMine> __host__ __device__ constexpr int choice_places() {
+    return ((kGroup * kMine < kMaxChoice ? kGroup * kMine : kMaxChoice) + kGroup - 1) / kGroup;
+}
+template <int kMine> __host__ __device__ constexpr int forward_threads() { return kMine > 12 ? 512 : 1024; }
+
+template <typename T, int kGroup, int kMine, bool kWide>
+__global__ void __launch_bounds__(forward_threads<kMine>()) router_forward(const __grid_constant__ RouterParams P) {
+    extern __shared__ float sums[];                  // [warp][experts of all places]
+    __shared__ int tally[kMaxExperts];
+    __shared__ float extra[32];
+    __shared__ int active[32];
+    constexpr int kPlaces = choice_places<kGroup, kMine>(), kRow = kGroup * kMine;
+    const int E = P.experts, tid = threadIdx.x, warp = tid / 32, lane = tid % kGroup, warps = blockDim.x / 32, k = P.top_k;
+    for (int e = tid; e < E; e += blockDim.x) tally[e] = 0;
+    __syncthreads();
+    float sum[kMine], zsq = 0.0f;
+    int act = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) { sum[i] = 0.0f; cnt[i] = 0; }
-    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRouterThreads + tid; t < P.tokens; t += static_cast<int64_t>(gridDim.x) * kRouterThreads) {
-        float z[N];
-        load_row<T, N, kWide>(static_cast<const T *>(P.logits) + t * P.row_stride, E, z);
-        if (P.mask && P.mask[t] == 0) {
+    for (int i = 0; i < kMine; ++i) sum[i] = 0.0f;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * blockDim.x / kGroup;
+    int64_t t = (static_cast<int64_t>(blockIdx.x) * blockDim.x + tid) / kGroup;
+    const T *logits = static_cast<const T *>(P.logits);
+    Row<T, kGroup, kMine, kWide> next;
+    const auto fetch = [&](int64_t at) { next.load(logits + at * P.row_stride, lane, at < P.tokens && (!P.mask || P.mask[at] != 0) ? E : 0); };
+    fetch(t);
+    // every lane of a warp goes round as often as the warp's first group
+    for (int64_t lead = t - (tid % 32) / kGroup; lead < P.tokens; lead += step, t += step) {
+        float z[kMine], p[kMine];
 #pragma unroll
-            for (int i = 0; i < N; ++i) z[i] = -INFINITY;
-        }
-        unsigned key[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) key[i] = order_key(z[i]);
-        float total = 1.0f, lse = 0.0f;
-        const bool some = row_softmax<N>(z, total, lse);
+        for (int i = 0; i < kMine; ++i) z[i] = next[i];
+        if (lead + step < P.tokens) fetch(t + step);
+        float top, total, lse;
+        const bool some = softmax<kGroup, kMine>(z, p, top, total, lse);
         const float inv = some ? 1.0f / total : 0.0f;
-        float share = 0.0f;
-        int pick[kMaxChoice];
-        float w[kMaxChoice];
+        if (some) {
+            act += lane == 0;
+            zsq = lane == 0 ? fmaf(lse, lse, zsq) : zsq;
 #pragma unroll
-        for (int j = 0; j < kMaxChoice; ++j) {
-            if (j < P.top_k) {
-                unsigned best = kKeyMinusInf;
-                int at = -1;
-                float p = 0.0f;
+            for (int i = 0; i < kMine; ++i) sum[i] = fmaf(p[i], inv, sum[i]);
+        }
+        const float from = top != -INFINITY ? top : 0.0f;
+        float share = 0.0f, w[kPlaces];
+        int pick[kPlaces];
+        Chooser<T, kGroup, kMine, kWide> choose(z, lane);
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (key[i] > best) { best = key[i]; at = i; p = z[i]; }
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (i == at) { key[i] = 0; ++cnt[i]; }
-                pick[j] = some ? at : -1;
-                w[j] = some && at >= 0 ? p * inv : 0.0f;
-                share += w[j];
+        for (int place = 0; place < kPlaces; ++place) {
+            pick[place] = -1;
+            w[place] = 0.0f;
+#pragma unroll 1
+            for (int j = place * kGroup; j < k && j < (place + 1) * kGroup; ++j) {
+                float value;
+                const int at = choose.next(lane, value);
+                const float pe = at < 0 ? 0.0f : exp2_fast((value - from) * kLog2e);
+                share += pe;
+                if (lane == j % kGroup) {
+                    pick[place] = at;
+                    w[place] = pe;
+                }
             }
         }
-        const float norm = P.normalize ? (share != 0.0f ? share : 1.0f) : 1.0f;
+        const float by = P.normalize ? (share != 0.0f ? 1.0f / share : 1.0f) : inv;
+        if (t < P.tokens) {
 #pragma unroll
-        for (int j = 0; j < kMaxChoice; ++j)
-            if (j < P.top_k) {
-                P.index[t * P.top_k + j] = pick[j];
-                P.weight[t * P.top_k + j] = w[j] / norm;
+            for (int place = 0; place < kPlaces; ++place) {
+                const int j = place * kGroup + lane;
+                if (j < k) {
+                    P.index[t * k + j] = pick[place];
+                    P.weight[t * k + j] = w[place] * by;
+                    if (pick[place] >= 0) atomicAdd(&tally[pick[place]], 1);
+                }
             }
-        if (some) {
-            ++act;
-            zsq = fmaf(lse, lse, zsq);
-#pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] = fmaf(z[i], inv, sum[i]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float s = warp_sum(sum[i]);
-        const int c = __reduce_add_sync(kAll, cnt[i]);
-        if (lane == 0) { sums[warp][i] = s; tally[warp][i] = c; }
+    for (int i = 0; i < kMine; ++i) {                // over the groups of the warp
+#pragma unroll
+        for (int o = 16; o >= kGroup; o >>= 1) sum[i] += __shfl_xor_sync(kAll, sum[i], o);
+        if (tid % 32 < kGroup) sums[warp * kRow + expert_of<T, kGroup, kWide>(lane, i)] = sum[i];
     }
     zsq = warp_sum(zsq);
     act = __reduce_add_sync(kAll, act);
-    if (lane == 0) { extra[warp] = zsq; active[warp] = act; }
+    if (tid % 32 == 0) { extra[warp] = zsq; active[warp] = act; }
     __syncthreads();
-    if (tid < N) {
-        for (int w = 1; w < kRouterWarps; ++w) { sums[0][tid] += sums[w][tid]; tally[0][tid] += tally[w][tid]; }
-    }
+    for (int e = tid; e < E; e += blockDim.x)
+        for (int v = 1; v < warps; ++v) sums[e] += sums[v * kRow + e];
     zsq = 0.0f;
     act = 0;
-    for (int w = 0; w < kRouterWarps; ++w) { zsq += extra[w]; act += active[w]; }
+    for (int v = 0; v < warps; ++v) { zsq += extra[v]; act += active[v]; }
     __syncthreads();
-    finish(P, sums[0], tally[0], zsq, act);
+    finish(P, sums, tally, zsq, act);
 }
 
-// More experts: a warp per token, expert i * 32 + lane in the lane's i-th place.
-template <int N> struct WarpRow {
-    float z[N];              // logits, then exp(z - max)
-    float total, lse, top;
-    bool some;
+constexpr int kBackwardThreads = 256;
+
+// dz_e = p_e (g_e - sum_j p_j g_j) + 2 b lse p_e / N + the chosen weights' part, g_e = d balance / d p_e.  All experts are
+// written as if unchosen, then the lanes that hold the choices write theirs.
+template <typename T, int kGroup, int kMine, bool kWide>
+__global__ void __launch_bounds__(kBackwardThreads) router_backward(const __grid_constant__ RouterParams P) {
+    __shared__ float slope[kMaxExperts];
+    constexpr int kPlaces = choice_places<kGroup, kMine>();
+    constexpr int kV = kWide ? 16 / static_cast<int>(sizeof(T)) : 1;
+    const int E = P.experts, tid = threadIdx.x, lane = tid % kGroup, k = P.top_k;
+    const int n = P.in_counts[E];
+    const float per = n > 0 ? 1.0f / static_cast<float>(n) : 0.0f;
+    const float scale = P.dlosses ? P.dlosses[0] * P.balance_coef * static_cast<float>(E) / static_cast<float>(k) * per * per : 0.0f;
+    const float zc = P.dlosses ? P.dlosses[1] * P.z_coef * 2.0f * per : 0.0f;
+    for (int e = tid; e < E; e += kBackwardThreads) slope[e] = scale * static_cast<float>(P.in_counts[e]);
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kBackwardThreads / kGroup;
+    int64_t t = (static_cast<int64_t>(blockIdx.x) * kBackwardThreads + tid) / kGroup;
+    const T *logits = static_cast<const T *>(P.logits);
+    Row<T, kGroup, kMine, kWide> next;
+    const auto fetch = [&](int64_t at) { next.load(logits + at * P.row_stride, lane, at < P.tokens && (!P.mask || P.mask[at] != 0) ? E : 0); };
+    fetch(t);
+    __syncthreads();
+    float g[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int e = expert_of<T, kGroup, kWide>(lane, i);
+        g[i] = e < E ? slope[e] : 0.0f;
+    }
+    for (int64_t lead = t - (tid % 32) / kGroup; lead < P.tokens; lead += step, t += step) {
+        float z[kMine], p[kMine];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) z[i] = next[i];
+        int e[kPlaces];
+        float x[kPlaces], pe[kPlaces];
+#pragma unroll
+        for (int place = 0; place < kPlaces; ++place) {
+            const int j = place * kGroup + lane;
+            e[place] = P.dweight && j < k && t < P.tokens ? P.in_index[t * k + j] : -1;
+            x[place] = e[place] >= 0 ? P.dweight[t * k + j] : 0.0f;
+            pe[place] = e[place] >= 0 ? to_f32(logits[t * P.row_stride + e[place]]) : -INFINITY;      // the logit for now
+        }
+        if (lead + step < P.tokens) fetch(t + step);
+        float top, total, lse;
+        const bool some = softmax<kGroup, kMine>(z, p, top, total, lse);
+        const float inv = some ? 1.0f / total : 0.0f, from = top != -INFINITY ? top : 0.0f;
+        float dot = 0.0f, wd = 0.0f, share = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            p[i] *= inv;
+            dot = fmaf(p[i], g[i], dot);
+        }
+        dot = group_sum<kGroup>(dot);
+        if (P.dweight) {
+#pragma unroll
+            for (int place = 0; place < kPlaces; ++place) {
+                pe[place] = exp2_fast((pe[place] - from) * kLog2e) * inv;
+                share += pe[place];
+                wd = fmaf(pe[place], x[place], wd);
+            }
+            share = group_sum<kGroup>(share);
+            wd = group_sum<kGroup>(wd);
+        }
+        const float common = (some ? zc * lse - dot : 0.0f), all = P.normalize ? common : common - wd;
+        const float norm = share != 0.0f ? 1.0f / share : 1.0f;
+        if (t < P.tokens) {
+            T *out = static_cast<T *>(P.dlogits) + t * P.drow_stride;
+#pragma unroll
+            for (int i = 0; i < kMine / kV; ++i) {
+                const int first = (i * kGroup + lane) * kV;
+                if (first < E) {
+                    Pack<T, kV> v;
+#pragma unroll
+                    for (int y = 0; y < kV; ++y) v.v[y] = from_f32<T>(p[i * kV + y] * (g[i * kV + y] + all));
+                    *reinterpret_cast<Pack<T, kV> *>(out + first) = v;
+                }
+            }
+        }
+        if (P.dweight) {
+            __syncwarp();                            // the choices' values come after the row's
+            if (t < P.tokens) {
+                T *out = static_cast<T *>(P.dlogits) + t * P.drow_stride;
+#pragma unroll
+                for (int place = 0; place < kPlaces; ++place)
+                    if (e[place] >= 0)
+                        out[e[place]] = from_f32<T>(pe[place] * (slope[e[place]] + all) +
+                                                    (P.normalize ? pe[place] * norm * (x[place] - wd * norm) : pe[place] * x[place]));
+            }
+        }
+    }
+}
+
+// Lanes and values a lane by the number of experts: eight values a lane, twelve (three vectors) from 129 to 192 in fp32,
+// sixteen above 256.
+using RouterKernel = void (*)(const RouterParams);
+struct RouterShape {
+    RouterKernel forward, backward;
+    int group, row, threads;
 };
-
-template <typename T, int N> __device__ __forceinline__ void load_warp_row(const RouterParams &P, int64_t t, int lane, float *z) {
-    const T *row = static_cast<const T *>(P.logits) + t * P.row_stride;
-    const bool on = !P.mask || P.mask[t] != 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int e = i * 32 + lane;
-        z[i] = on && e < P.experts ? to_f32(row[e]) : -INFINITY;
-    }
+template <typename T, int kGroup, int kMine, bool kWide> RouterShape shape_of() {
+    return RouterShape{router_forward<T, kGroup, kMine, kWide>, router_backward<T, kGroup, kMine, kWide>, kGroup, kGroup * kMine, forward_threads<kMine>()};
+}
+template <typename T, bool kWide> RouterShape router_shape(int E) {
+    if (E <= 8) return shape_of<T, 1, 8, kWide>();
+    if (E <= 16) return shape_of<T, 2, 8, kWide>();
+    if (E <= 32) return shape_of<T, 4, 8, kWide>();
+    if (E <= 64) return shape_of<T, 8, 8, kWide>();
+    if (E <= 128) return shape_of<T, 16, 8, kWide>();
+    if constexpr (sizeof(T) == 4)
+        if (E <= 192) return shape_of<T, 16, 12, kWide>();
+    if (E <= 256) return shape_of<T, 32, 8, kWide>();
+    return shape_of<T, 32, 16, kWide>();
+}
+RouterShape pick_router(const loco_router_t *c, bool wide) {
+    if (c->dtype == LOCO_BF16) return wide ? router_shape<__nv_bfloat16, true>(c->experts) : router_shape<__nv_bfloat16, false>(c->experts);
+    return wide ? router_shape<float, true>(c->experts) : router_shape<float, false>(c->experts);
 }
 
-template <int N> __device__ __forceinline__ void warp_softmax(WarpRow<N> &r) {
-    float top = -INFINITY;
-    bool nan = false;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        top = fmaxf(top, r.z[i]);
-        nan |= r.z[i] != r.z[i];
-    }
-    const unsigned k = __reduce_max_sync(kAll, order_key(top));
-    r.some = k > kKeyMinusInf || __any_sync(kAll, nan);
-    // back from the ordered integer to the float
-    r.top = k <= kKeyMinusInf ? 0.0f : __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
-    float total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        r.z[i] = r.z[i] == -INFINITY ? 0.0f : expf(r.z[i] - r.top);
-        total += r.z[i];
-    }
-    r.total = warp_sum(total);
-    r.lse = logf(r.total) + r.top;
-}
-
-template <typename T, int N>
-__global__ void __launch_bounds__(kRouterThreads) router_forward_warp(const __grid_constant__ RouterParams P) {
-    __shared__ float sums[kRouterWarps][N * 32];
-    __shared__ int tally[kRouterWarps][N * 32];
-    __shared__ float extra[kRouterWarps];
-    __shared__ int active[kRouterWarps];
-    const int E = P.experts, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    float sum[N], zsq = 0.0f;
-    int cnt[N], act = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) { sum[i] = 0.0f; cnt[i] = 0; }
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kRouterWarps;
-    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRouterWarps + warp; t < P.tokens; t += step) {
-        WarpRow<N> r;
-        load_warp_row<T, N>(P, t, lane, r.z);
-        unsigned key[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) key[i] = order_key(r.z[i]);
-        warp_softmax<N>(r);
-        const float inv = r.some ? 1.0f / r.total : 0.0f;
-        float share = 0.0f, w = 0.0f;
-        int pick = -1;
-        for (int j = 0; j < P.top_k; ++j) {
-            unsigned best = 0;
-            int at = N;
-            float p = 0.0f;
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (key[i] > best) { best = key[i]; at = i; p = r.z[i]; }
-            const unsigned all = __reduce_max_sync(kAll, best);
-            if (all <= kKeyMinusInf) break;
-            const int e = static_cast<int>(__reduce_min_sync(kAll, best == all ? static_cast<unsigned>(at * 32 + lane) : 0xffffffffu));
-            const float pe = __shfl_sync(kAll, p, e % 32) * inv;
-            share += pe;
-            if (lane == e % 32) {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (i == at) { key[i] = 0; ++cnt[i]; }
-            }
-            if (lane == j) { pick = e; w = pe; }
-        }
-        const float norm = P.normalize ? (share != 0.0f ? share : 1.0f) : 1.0f;
-        if (lane < P.top_k) {
-            P.index[t * P.top_k + lane] = pick;
-            P.weight[t * P.top_k + lane] = w / norm;
-        }
-        if (r.some) {
-            ++act;
-            zsq = fmaf(r.lse, r.lse, zsq);
-#pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] = fmaf(r.z[i], inv, sum[i]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) { sums[warp][i * 32 + lane] = sum[i]; tally[warp][i * 32 + lane] = cnt[i]; }
-    if (lane == 0) { extra[warp] = zsq; active[warp] = act; }
-    __syncthreads();
-    for (int e = tid; e < E; e += kRouterThreads)
-        for (int w = 1; w < kRouterWarps; ++w) { sums[0][e] += sums[w][e]; tally[0][e] += tally[w][e]; }
-    zsq = 0.0f;
-    act = 0;
-    for (int w = 0; w < kRouterWarps; ++w) { zsq += extra[w]; act += active[w]; }
-    __syncthreads();
-    finish(P, sums[0], tally[0], zsq, act);
-}
-
-// dz_e = p_e (g_e - sum_j p_j g_j) + zc lse p_e + [chosen] weight gradient, g_e = d balance / d p_e
-
-__device__ __forceinline__ float expert_gradient(const RouterParams &P, int e) {
-    const int n = P.in_counts[P.experts];
-    if (n <= 0 || !P.dlosses) return 0.0f;
-    const float load = static_cast<float>(P.in_counts[e]) / (static_cast<float>(n) * static_cast<float>(P.top_k));
-    return P.dlosses[0] * P.balance_coef * static_cast<float>(P.experts) * load / static_cast<float>(n);
-}
-
-template <typename T, int N, bool kWide>
-__global__ void __launch_bounds__(kRouterThreads) router_backward_thread(const __grid_constant__ RouterParams P) {
-    const int E = P.experts;
-    float g[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) g[i] = i < E ? expert_gradient(P, i) : 0.0f;
-    const int n = P.in_counts[E];
-    const float zc = P.dlosses && n > 0 ? P.dlosses[1] * P.z_coef * 2.0f / static_cast<float>(n) : 0.0f;
-    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRouterThreads + threadIdx.x; t < P.tokens; t += static_cast<int64_t>(gridDim.x) * kRouterThreads) {
-        float z[N], d[N];
-        load_row<T, N, kWide>(static_cast<const T *>(P.logits) + t * P.row_stride, E, z);
-        float total = 1.0f, lse = 0.0f;
-        const bool some = row_softmax<N>(z, total, lse) && (!P.mask || P.mask[t] != 0);
-        if (some) {
-            const float inv = 1.0f / total;
-            float dot = 0.0f;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                z[i] *= inv;
-                dot = fmaf(z[i], g[i], dot);
-            }
-            if (P.dweight) {
-                float share = 0.0f, wd = 0.0f;                    // sum of the chosen p, and of p * dweight
-                float dw[N];
-                unsigned chosen = 0;
-#pragma unroll
-                for (int i = 0; i < N; ++i) dw[i] = 0.0f;
-                for (int j = 0; j < P.top_k; ++j) {
-                    const int e = P.in_index[t * P.top_k + j];
-                    const float x = P.dweight[t * P.top_k + j];
-#pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (i == e) {
-                            dw[i] = x;
-                            share += z[i];
-                            wd = fmaf(z[i], x, wd);
-                            chosen |= 1u << i;
-                        }
-                }
-                const float norm = share != 0.0f ? 1.0f / share : 1.0f;
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float own = P.normalize ? ((chosen >> i) & 1 ? z[i] * norm * (dw[i] - wd * norm) : 0.0f) : z[i] * (dw[i] - wd);
-                    d[i] = z[i] * (g[i] - dot + zc * lse) + own;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) d[i] = z[i] * (g[i] - dot + zc * lse);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) d[i] = 0.0f;
-        }
-        T *out = static_cast<T *>(P.dlogits) + t * P.drow_stride;
-        if constexpr (kWide) {
-            constexpr int kV = 16 / sizeof(T);
-#pragma unroll
-            for (int i = 0; i < N / kV; ++i)
-                if (i * kV < E) {
-                    Pack<T, kV> p;
-#pragma unroll
-                    for (int j = 0; j < kV; ++j) p.v[j] = from_f32<T>(d[i * kV + j]);
-                    *reinterpret_cast<Pack<T, kV> *>(out + i * kV) = p;
-                }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (i < E) out[i] = from_f32<T>(d[i]);
-        }
-    }
-}
-
-template <typename T, int N>
-__global__ void __launch_bounds__(kRouterThreads) router_backward_warp(const __grid_constant__ RouterParams P) {
-    const int E = P.experts, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    float g[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) g[i] = i * 32 + lane < E ? expert_gradient(P, i * 32 + lane) : 0.0f;
-    const int n = P.in_counts[E];
-    const float zc = P.dlosses && n > 0 ? P.dlosses[1] * P.z_coef * 2.0f / static_cast<float>(n) : 0.0f;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kRouterWarps;
-    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRouterWarps + warp; t < P.tokens; t += step) {
-        WarpRow<N> r;
-        load_warp_row<T, N>(P, t, lane, r.z);
-        warp_softmax<N>(r);
-        const float inv = r.some ? 1.0f / r.total : 0.0f;
-        float dot = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            r.z[i] *= inv;
-            dot = fmaf(r.z[i], g[i], dot);
-        }
-        dot = warp_sum(dot);
-        const float common = r.some ? zc * r.lse - dot : 0.0f;
-        float add[N], wd = 0.0f, share = 1.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) add[i] = 0.0f;
-        if (P.dweight && r.some) {
-            // the lane's own choice, for the two sums
-            const int e = lane < P.top_k ? P.in_index[t * P.top_k + lane] : -1;
-            const float x = e >= 0 ? P.dweight[t * P.top_k + lane] : 0.0f;
-            share = 0.0f;
-            for (int j = 0; j < P.top_k; ++j) {
-                const int ej = __shfl_sync(kAll, e, j);
-                const float xj = __shfl_sync(kAll, x, j);
-                if (ej >= 0 && lane == ej % 32) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (i == ej / 32) {
-                            add[i] = xj;
-                            share += r.z[i];
-                            wd = fmaf(r.z[i], xj, wd);
-                        }
-                }
-            }
-            share = warp_sum(share);
-            wd = warp_sum(wd);
-            const float norm = share != 0.0f ? 1.0f / share : 1.0f;
-            if (P.normalize) {
-                for (int j = 0; j < P.top_k; ++j) {
-                    const int ej = __shfl_sync(kAll, e, j);
-                    if (ej >= 0 && lane == ej % 32) {
-#pragma unroll
-                        for (int i = 0; i < N; ++i)
-                            if (i == ej / 32) add[i] = r.z[i] * norm * (add[i] - wd * norm);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) add[i] = r.z[i] * (add[i] - wd);
-            }
-        }
-        T *out = static_cast<T *>(P.dlogits) + t * P.drow_stride;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i * 32 + lane < E) out[i * 32 + lane] = from_f32<T>(r.z[i] * (g[i] + common) + add[i]);
-    }
-}
-
-template <typename T> void launch_forward(const RouterParams &P, unsigned blocks, bool wide, cudaStream_t s) {
-    const int E = P.experts;
-    if (E <= 8) wide ? router_forward_thread<T, 8, true><<<blocks, kRouterThreads, 0, s>>>(P) : router_forward_thread<T, 8, false><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 16) wide ? router_forward_thread<T, 16, true><<<blocks, kRouterThreads, 0, s>>>(P) : router_forward_thread<T, 16, false><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 64) router_forward_warp<T, 2><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 128) router_forward_warp<T, 4><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 192) router_forward_warp<T, 6><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 256) router_forward_warp<T, 8><<<blocks, kRouterThreads, 0, s>>>(P);
-    else router_forward_warp<T, 16><<<blocks, kRouterThreads, 0, s>>>(P);
-}
-
-template <typename T> void launch_backward(const RouterParams &P, unsigned blocks, bool wide, cudaStream_t s) {
-    const int E = P.experts;
-    if (E <= 8) wide ? router_backward_thread<T, 8, true><<<blocks, kRouterThreads, 0, s>>>(P) : router_backward_thread<T, 8, false><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 16) wide ? router_backward_thread<T, 16, true><<<blocks, kRouterThreads, 0, s>>>(P) : router_backward_thread<T, 16, false><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 64) router_backward_warp<T, 2><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 128) router_backward_warp<T, 4><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 192) router_backward_warp<T, 6><<<blocks, kRouterThreads, 0, s>>>(P);
-    else if (E <= 256) router_backward_warp<T, 8><<<blocks, kRouterThreads, 0, s>>>(P);
-    else router_backward_warp<T, 16><<<blocks, kRouterThreads, 0, s>>>(P);
+// Dynamic shared memory above the default limit (32 KB beside the 19 KB of static arrays).
+bool allow_shared(RouterKernel fn) {
+    if (cudaFuncSetAttribute(reinterpret_cast<const void *>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, 65536) == cudaSuccess) return true;
+    cudaGetLastError();
+    return false;
 }
 
 int check_router(const loco_router_t *c) {
@@ -547,13 +489,6 @@ int check_router(const loco_router_t *c) {
     if (c->top_k < 1 || c->top_k > kMaxChoice || c->top_k > c->experts) return LOCO_ERR_ARG;
     if (!std::isfinite(c->balance_coef) || !std::isfinite(c->z_coef)) return LOCO_ERR_ARG;
     return LOCO_OK;
-}
-
-// Blocks of a launch: tokens per block of the kernel the number of experts selects, at most what the machine holds.
-int64_t router_blocks(const loco_router_t *c, int64_t tokens, int most) {
-    const int64_t per = c->experts <= 16 ? kRouterThreads : kRouterWarps;
-    const int64_t need = (tokens + per - 1) / per;
-    return need < most ? (need < 1 ? 1 : need) : most;
 }
 
 }  // namespace loco_layer
@@ -597,13 +532,20 @@ int loco_router_forward(const loco_router_t *c, int64_t tokens, const void *d_lo
     P.normalize = c->normalize;
     P.balance_coef = c->balance_coef;
     P.z_coef = c->z_coef;
-    const int most = sms * kBlocksPerSm < kMaxBlocks ? sms * kBlocksPerSm : kMaxBlocks;
-    const unsigned blocks = static_cast<unsigned>(router_blocks(c, tokens, most));
     // rows that are whole 16-byte vectors on 16-byte boundaries are read as such
     const int vec = 16 / static_cast<int>(size);
     const bool wide = aligned(d_logits, 16) && row_stride % vec == 0 && c->experts % vec == 0;
-    if (c->dtype == LOCO_BF16) launch_forward<__nv_bfloat16>(P, blocks, wide, static_cast<cudaStream_t>(stream));
-    else launch_forward<float>(P, blocks, wide, static_cast<cudaStream_t>(stream));
+    const RouterShape R = pick_router(c, wide);
+    // one block to an SM (every block leaves a partial row to be added), as wide as the tokens need
+    const int64_t warps = (tokens * R.group + 31) / 32;
+    const int most = sms < kMaxBlocks ? sms : kMaxBlocks;
+    int64_t per = (warps + most - 1) / most;
+    per = per < 4 ? 4 : (per > R.threads / 32 ? R.threads / 32 : per);
+    int64_t blocks = (warps + per - 1) / per;
+    blocks = blocks < 1 ? 1 : (blocks > most ? most : blocks);
+    const size_t shared = static_cast<size_t>(per) * R.row * sizeof(float);
+    if (shared > 28672 && !allow_shared(R.forward)) return LOCO_ERR_CUDA;
+    R.forward<<<static_cast<unsigned>(blocks), static_cast<unsigned>(per * 32), shared, static_cast<cudaStream_t>(stream)>>>(P);
     return launched();
 }
 
@@ -638,9 +580,10 @@ int loco_router_backward(const loco_router_t *c, int64_t tokens, const void *d_l
     P.z_coef = c->z_coef;
     const int vec = 16 / static_cast<int>(size);
     const bool wide = aligned(d_logits, 16) && aligned(d_dlogits, 16) && row_stride % vec == 0 && drow_stride % vec == 0 && c->experts % vec == 0;
-    const unsigned blocks = static_cast<unsigned>(router_blocks(c, tokens, sms * 8));
-    if (c->dtype == LOCO_BF16) launch_backward<__nv_bfloat16>(P, blocks, wide, static_cast<cudaStream_t>(stream));
-    else launch_backward<float>(P, blocks, wide, static_cast<cudaStream_t>(stream));
+    const RouterShape R = pick_router(c, wide);
+    int64_t blocks = (tokens * R.group + kBackwardThreads - 1) / kBackwardThreads;
+    if (blocks > sms * 8) blocks = sms * 8;
+    R.backward<<<static_cast<unsigned>(blocks), kBackwardThreads, 0, static_cast<cudaStream_t>(stream)>>>(P);
     return launched();
 }
 
