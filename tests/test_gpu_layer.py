@@ -257,6 +257,15 @@ def test_attention_packed_samples(causal, d):
     check_attention(3, 0, 0, 2, 2, d, causal, nq=[5, 128, 60], nk=[200, 1, 0], packed=True)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_more_work_than_blocks_at_a_time(d):
+    """Several hundred tiles of very different lengths, empty ones among them: a block takes up other blocks' work."""
+    n = [300, 1, 0, 517, 128, 64, 0, 0, 255, 700, 3, 129, 400]
+    check_attention(13, 0, 0, 24, 6, d, True, nq=n, nk=n, packed=True)
+    check_attention(13, 700, 700, 16, 16, d, False, nq=n, nk=n)
+    check_attention(3, 900, 500, 40, 8, d, True)
+
+
 def test_attention_strided_operands():
     def fused(g):
         x = normal(g, 2, 150, 8, 64)
