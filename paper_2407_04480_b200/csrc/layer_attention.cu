@@ -50,7 +50,7 @@ struct Shared {
     uint64_t full[kMaxSlots], empty[kMaxSlots];  // streaming tiles: copied, no longer read
     uint64_t stay, rows_in;                      // the tiles that stay are in shared memory, in TMEM
     uint64_t score[2], second[2];                // products ready: S per query tile; o per query tile (forward), dP and dv (backward)
-    uint64_t prob_rest[2];                       // forward: P of the tile's second 64 keys
+    uint64_t read[2];                            // forward: S in registers
     uint64_t prob[2], grad;                      // P written to TMEM (forward: per query tile), S read (backward); dS written
     uint64_t last, clean;                        // a tile with rows past the end is copied; those rows are zero
     uint64_t stats[2], stats_free[2];            // backward keys: row statistics of a query tile
@@ -90,14 +90,13 @@ template <int kDim> __device__ __forceinline__ void product_scores_tmem(uint32_t
 #pragma unroll
     for (int x = 0; x < kDim; x += 16) mma_ts(lead, d, a + x / 2, db + ((x / 64 * (kTile * 128) + x % 64 * 2) >> 4), word, x > 0);
 }
-// d (128 x kDim) += A B over the rows [kFrom, kUntil) of B's tile: A (128 x kRows) in TMEM, its columns at `a0` (first half)
-// and `a1`.
-template <int kDim, int kRows = kTile, int kFrom = 0, int kUntil = kRows>
+// d (128 x kDim) += A B: A (128 x kRows) in TMEM, its columns at `a0` (first half) and `a1`; B's rows are the tile's.
+template <int kDim, int kRows = kTile>
 __device__ __forceinline__ void product_apply(uint32_t lead, uint32_t d, uint32_t a0, uint32_t a1, uint32_t b, uint32_t accumulate) {
     constexpr uint32_t word = product(kDim, true);
     const uint32_t db = desc_along_rows(b, kRows * 128);
 #pragma unroll
-    for (int r = kFrom; r < kUntil; r += 16)
+    for (int r = 0; r < kRows; r += 16)
         mma_ts(lead, d, r < kRows / 2 ? a0 + r / 2 : a1 + (r - kRows / 2) / 2, db + (r * 128 >> 4), word, accumulate | (r > 0));
 }
 
@@ -113,7 +112,7 @@ template <int kColumns> __device__ __forceinline__ uint32_t begin_block(Shared &
             bar_init(smem_addr(&S.score[i]), 1);
             bar_init(smem_addr(&S.second[i]), 1);
             bar_init(smem_addr(&S.prob[i]), prob_arrivals);
-            bar_init(smem_addr(&S.prob_rest[i]), prob_arrivals);
+            bar_init(smem_addr(&S.read[i]), prob_arrivals);
             bar_init(smem_addr(&S.stats[i]), 1);
             bar_init(smem_addr(&S.stats_free[i]), 2 * kGroupWarps);
         }
@@ -233,42 +232,54 @@ __device__ __forceinline__ int key_limit(const Rows &Q, const Rows &K, int causa
     return causal ? max(0, min(K.n, i + K.n - Q.n + 1)) : K.n;
 }
 // Key tiles that the queries [first, first + 128) need.
-__device__ __forceinline__ int key_tiles(const Rows &Q, const Rows &K, int causal, int first) {
+__device__ __forceinline__ int key_tiles(const Rows &Q, const Rows &K, int causal, int first, int tile = kTile) {
     if (first >= Q.n) return 0;
-    return (key_limit(Q, K, causal, min(first + kTile, Q.n) - 1) + kTile - 1) / kTile;
+    return (key_limit(Q, K, causal, min(first + kTile, Q.n) - 1) + tile - 1) / tile;
 }
 
-__device__ __forceinline__ void mask_from(uint32_t (&s)[32], int left) {
+__device__ __forceinline__ void mask_from(uint32_t (&s)[16], int left) {
 #pragma unroll
-    for (int x = 0; x < 32; ++x)
+    for (int x = 0; x < 16; ++x)
         if (x >= left) s[x] = 0xff800000u;       // -inf
 }
-__device__ __forceinline__ float row_max(const uint32_t (&s)[32]) {
-    float m[4];
+__device__ __forceinline__ float row_max(const uint32_t (&s)[16]) {
+    float m[2];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) m[x] = max2(__uint_as_float(s[x]), __uint_as_float(s[x + 4]));
-#pragma unroll
-    for (int x = 8; x < 32; x += 8)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) m[y] = max3(m[y], __uint_as_float(s[x + y]), __uint_as_float(s[x + y + 4]));
-    return max2(max3(m[0], m[1], m[2]), m[3]);
+    for (int y = 0; y < 2; ++y) {
+        const uint32_t *x = s + 8 * y;
+        m[y] = max3(max3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2])),
+                    max3(__uint_as_float(x[3]), __uint_as_float(x[4]), __uint_as_float(x[5])),
+                    max2(__uint_as_float(x[6]), __uint_as_float(x[7])));
+    }
+    return max2(m[0], m[1]);
 }
 
 // ------------------------------------------------------------------------------------------------ forward
 
+// TMEM: o, S and P of both query tiles.  S is free again once its softmax group has it in registers, so that the next scores
+// are computed under this tile's exponentials; with heads of 128 that takes key tiles of 80, as two tiles of 128 would fill
+// TMEM without a place of its own for P, and the next scores would wait for the product with the values (measured at 4096,
+// 32 heads: 252 us).
+template <int kDim> __host__ __device__ constexpr int key_tile() { return kDim == 128 ? 80 : 128; }
+template <int kDim> __host__ __device__ constexpr int forward_slots() { return 8; }
+template <int kDim> constexpr int forward_bytes() {
+    return 2 * tile_bytes<kDim>() + forward_slots<kDim>() * key_tile<kDim>() * kDim * 2 + static_cast<int>(sizeof(Shared));
+}
+static_assert(forward_bytes<128>() <= 227 * 1024 && forward_bytes<64>() <= 227 * 1024, "shared memory of a block");
+
 template <int kDim>
 __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
-    constexpr int kSlots = stream_slots<kDim>(), kBytes = tile_bytes<kDim>();
+    constexpr int kSlots = forward_slots<kDim>(), kBytes = tile_bytes<kDim>(), kKeys = key_tile<kDim>(), kStep = kKeys * kDim * 2;
     extern __shared__ __align__(1024) uint8_t tiles[];
-    Shared &S = *reinterpret_cast<Shared *>(tiles + (2 + kSlots) * kBytes);
+    Shared &S = *reinterpret_cast<Shared *>(tiles + 2 * kBytes + kSlots * kStep);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.causal);
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * 2 * kTile, head_kv = at.head / P.group;
     if (P.packed && first >= Q.n) return;
-    const int n0 = key_tiles(Q, K, P.causal, first), n1 = key_tiles(Q, K, P.causal, first + kTile), n = max(n0, n1);
-    const bool ragged = ends_inside(K, P.packed, P.seq_k) && n == K.n / kTile + 1;
+    const int n0 = key_tiles(Q, K, P.causal, first, kKeys), n1 = key_tiles(Q, K, P.causal, first + kTile, kKeys), n = max(n0, n1);
+    const bool ragged = ends_inside(K, P.packed, P.seq_k, kKeys) && n == K.n / kKeys + 1;
     const uint32_t tmem = begin_block<512>(S, kSlots, 1, kGroupWarps);
     volatile uint32_t *const failed = &S.failed;
 
@@ -286,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
             for (int j = 0; j < 2 * n; ++j) {
                 bar_wait(smem_addr(&S.empty[r.slot]), r.phase ^ 1, failed);
                 if (*failed) break;
-                load_tile<kDim>(ring + r.slot * kBytes, j % 2 ? &M.v : &M.k, K.first + j / 2 * kTile, head_kv, K.at,
-                                smem_addr(ragged && j >= 2 * n - 1 ? &S.last : &S.full[r.slot]));
+                load_tile<kDim, kKeys>(ring + r.slot * kStep, j % 2 ? &M.v : &M.k, K.first + j / 2 * kKeys, head_kv, K.at,
+                                       smem_addr(ragged && j >= 2 * n - 1 ? &S.last : &S.full[r.slot]));
                 ++sent;
                 r.next<kSlots>();
             }
@@ -299,12 +310,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
             }
         } else if (warp == kProductWarp && n > 0) {
             const uint32_t lead = elect_lane();
-            const uint32_t scores = product(kTile, false, P.scale < 0.0f);
+            const uint32_t scores = product(kKeys, false, P.scale < 0.0f);
+            const uint32_t s_at = tmem + 2 * kDim, p_at = s_at + 2 * kKeys;
             bar_wait(smem_addr(&S.stay), 0, failed);
             bar_wait(smem_addr(&S.full[0]), 0, failed);
             for (int t = 0; t < 2; ++t)
                 if ((t ? n1 : n0) > 0) {
-                    product_scores<kDim>(lead, tmem + t * kTile, base + t * kBytes, ring, scores);
+                    product_scores<kDim, kKeys>(lead, s_at + t * kKeys, base + t * kBytes, ring, scores);
                     commit(lead, smem_addr(&S.score[t]));
                 }
             commit(lead, smem_addr(&S.empty[0]));
@@ -313,23 +325,23 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
             k.next<kSlots>();
             k.next<kSlots>();
             for (int j = 0; j < n; ++j) {
-                if (ragged && j == n - 1) bar_wait(smem_addr(&S.clean), 0, failed);
-                else bar_wait(smem_addr(&S.full[v.slot]), v.phase, failed);
                 if (j + 1 < n) bar_wait(smem_addr(&S.full[k.slot]), k.phase, failed);
                 for (int t = 0; t < 2; ++t) {
                     const int nt = t ? n1 : n0;
-                    if (j >= nt) continue;
-                    bar_wait(smem_addr(&S.prob[t]), j & 1, failed);
-                    fence_after();
-                    const uint32_t p = tmem + t * kTile;
-                    product_apply<kDim, kTile, 0, 64>(lead, tmem + 2 * kTile + t * kTile, p, p + 32, ring + v.slot * kBytes, j > 0);
-                    bar_wait(smem_addr(&S.prob_rest[t]), j & 1, failed);
-                    fence_after();
-                    product_apply<kDim, kTile, 64, 128>(lead, tmem + 2 * kTile + t * kTile, p, p + 32, ring + v.slot * kBytes, 1);
-                    commit(lead, smem_addr(&S.second[t]));
                     if (j + 1 < nt) {
-                        product_scores<kDim>(lead, p, base + t * kBytes, ring + k.slot * kBytes, scores);
+                        bar_wait(smem_addr(&S.read[t]), j & 1, failed);
+                        fence_after();
+                        product_scores<kDim, kKeys>(lead, s_at + t * kKeys, base + t * kBytes, ring + k.slot * kStep, scores);
                         commit(lead, smem_addr(&S.score[t]));
+                    }
+                    if (j < nt) {
+                        if (ragged && j == n - 1) bar_wait(smem_addr(&S.clean), 0, failed);
+                        else bar_wait(smem_addr(&S.full[v.slot]), v.phase, failed);
+                        bar_wait(smem_addr(&S.prob[t]), j & 1, failed);
+                        fence_after();
+                        const uint32_t p = p_at + t * (kKeys / 2);
+                        product_apply<kDim, kKeys>(lead, tmem + t * kDim, p, p + kKeys / 4, ring + v.slot * kStep, j > 0);
+                        commit(lead, smem_addr(&S.second[t]));
                     }
                 }
                 commit(lead, smem_addr(&S.empty[v.slot]));
@@ -345,17 +357,18 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
         } else if (warp == kHelpWarp && ragged) {
             const int load = 2 * n - 1;              // the last value tile
             bar_wait(smem_addr(&S.last), 0, failed);
-            clean_tile<kDim>(tiles + (2 + load % kSlots) * kBytes, K.n % kTile, lane);
+            clean_tile<kDim, kKeys>(tiles + 2 * kBytes + load % kSlots * kStep, K.n % kKeys, lane);
             fence_async_shared();
             __syncwarp();
             if (lane == 0) bar_arrive(smem_addr(&S.clean));
         }
     } else {
         registers_many();
+        constexpr int kParts = kKeys / 16;
         const int t = warp / kGroupWarps, i = first + t * kTile + threadIdx.x % kTile;
         const int nt = t ? n1 : n0, limit = key_limit(Q, K, P.causal, i);
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % kGroupWarps * 32) << 16);
-        const uint32_t s_at = lanes + t * kTile, o_at = lanes + 2 * kTile + t * kTile;
+        const uint32_t o_at = lanes + t * kDim, s_at = lanes + 2 * kDim + t * kKeys, p_at = lanes + 2 * kDim + 2 * kKeys + t * (kKeys / 2);
         const float scale = fmaxf(fabsf(P.scale), 1e-30f) * kLog2e;
         const float room = 8.0f / scale;         // how far the maximum may grow before o is rescaled
         float top = -INFINITY, total = 0.0f;
@@ -363,57 +376,53 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
             bar_wait(smem_addr(&S.score[t]), j & 1, failed);
             __syncwarp();
             fence_after();
-            uint32_t s[4][32];
-            load_columns(s_at, s[0]);
-            load_columns(s_at + 32, s[1]);
+            uint32_t s[kParts][16];
+#pragma unroll
+            for (int c = 0; c < kParts; ++c) load_columns(s_at + c * 16, s[c]);
             wait_loads();
-            pin(s[0]);
-            pin(s[1]);
-            load_columns(s_at + 64, s[2]);
-            load_columns(s_at + 96, s[3]);
-            const int left = limit - j * kTile;  // columns from here on are not seen
-            const bool edge = __any_sync(0xffffffffu, left < kTile);
-            if (edge) {
-                mask_from(s[0], left);
-                mask_from(s[1], left - 32);
+#pragma unroll
+            for (int c = 0; c < kParts; ++c) pin(s[c]);
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&S.read[t]));
+            const int left = limit - j * kKeys;  // columns from here on are not seen
+            if (__any_sync(0xffffffffu, left < kKeys)) {
+#pragma unroll
+                for (int c = 0; c < kParts; ++c) mask_from(s[c], left - c * 16);
             }
-            float most = max2(row_max(s[0]), row_max(s[1]));
-            wait_loads();
-            pin(s[2]);
-            pin(s[3]);
-            if (edge) {
-                mask_from(s[2], left - 64);
-                mask_from(s[3], left - 96);
-            }
-            most = max3(most, row_max(s[2]), row_max(s[3]));
+            float most = row_max(s[0]);
+#pragma unroll
+            for (int c = 1; c < kParts; c += 2) most = c + 1 < kParts ? max3(most, row_max(s[c]), row_max(s[c + 1 < kParts ? c + 1 : c])) : max2(most, row_max(s[c]));
             if (j == 0) {
                 top = most;
-            } else if (__any_sync(0xffffffffu, !(most - top <= room))) {
-                const float next = max2(top, most);
-                const float fade = next == -INFINITY ? 1.0f : exp2_fast((top - next) * scale);
-                bar_wait(smem_addr(&S.second[t]), (j - 1) & 1, failed);
+            } else {
+                bar_wait(smem_addr(&S.second[t]), (j - 1) & 1, failed);      // o is complete so far, and P free
                 __syncwarp();
                 fence_after();
+                if (__any_sync(0xffffffffu, !(most - top <= room))) {
+                    const float next = max2(top, most);
+                    const float fade = next == -INFINITY ? 1.0f : exp2_fast((top - next) * scale);
 #pragma unroll
-                for (int c = 0; c < kDim / 32; ++c) {
-                    uint32_t o[32];
-                    load_columns(o_at + c * 32, o);
-                    wait_loads();
-                    pin(o);
+                    for (int c = 0; c < kDim / 16; ++c) {
+                        uint32_t o[16];
+                        load_columns(o_at + c * 16, o);
+                        wait_loads();
+                        pin(o);
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * fade);
-                    store_columns(o_at + c * 32, o);
+                        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * fade);
+                        store_columns(o_at + c * 16, o);
+                    }
+                    total *= fade;
+                    top = next;
                 }
-                total *= fade;
-                top = next;
             }
             const float shift = top == -INFINITY ? 0.0f : top * scale;
             const float2 by = make_float2(scale, scale), minus = make_float2(-shift, -shift);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t p[16];
+            for (int c = 0; c < kParts; ++c) {
+                uint32_t p[8];
 #pragma unroll
-                for (int x = 0; x < 32; x += 2) {
+                for (int x = 0; x < 16; x += 2) {
                     float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, minus);
                     if (x / 2 % kPolyEvery == kPolyEvery - 1) {
                         e = exp2_poly(e);
@@ -425,28 +434,24 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
                     s[c][x + 1] = __float_as_uint(e.y);
                     p[x / 2] = pack_bf16(e.x, e.y);
                 }
-                if (c == 2) {                  // the first 64 keys have arrived meanwhile: their product can start
-                    wait_stores();
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(smem_addr(&S.prob[t]));
-                }
-                store_columns(s_at + c * 16, p);
+                store_columns(p_at + c * 8, p);
             }
             wait_stores();
             fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&S.prob_rest[t]));
+            if (lane == 0) bar_arrive(smem_addr(&S.prob[t]));
             // the sum is nobody's wait: it is formed under the products
-            float2 sum[4];
+            float2 sum[2];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < kParts; ++c) {
                 pin(s[c]);
-                sum[c] = make_float2(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]));
 #pragma unroll
-                for (int x = 2; x < 32; x += 2) sum[c] = add2(sum[c], make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])));
+                for (int x = 0; x < 16; x += 2) {
+                    const float2 e = make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1]));
+                    sum[x / 2 % 2] = c == 0 && x < 4 ? e : add2(sum[x / 2 % 2], e);
+                }
             }
-            sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+            sum[0] = add2(sum[0], sum[1]);
             total += sum[0].x + sum[0].y;
         }
         if (nt > 0) bar_wait(smem_addr(&S.second[t]), (nt - 1) & 1, failed);
@@ -990,19 +995,20 @@ int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const 
 bool make_query_map(const AttentionParams &P, CUtensorMap &map, const Heads &t, int box_rows) {
     return make_map(map, t, P.packed ? 1 : P.batch, P.heads_q, P.seq_q, P.head_dim, box_rows, P.seq_q > 0 ? P.q.ptr : P.k.ptr);
 }
-bool make_key_map(const AttentionParams &P, CUtensorMap &map, const Heads &t) {
-    return make_map(map, t, P.packed ? 1 : P.batch, P.heads_kv, P.seq_k, P.head_dim, kTile, P.seq_q > 0 ? P.q.ptr : P.k.ptr);
+bool make_key_map(const AttentionParams &P, CUtensorMap &map, const Heads &t, int box_rows) {
+    return make_map(map, t, P.packed ? 1 : P.batch, P.heads_kv, P.seq_k, P.head_dim, box_rows, P.seq_q > 0 ? P.q.ptr : P.k.ptr);
 }
 
 template <int kDim> int forward(const AttentionParams &P, cudaStream_t stream) {
     Maps M;
-    if (!make_query_map(P, M.q, P.q, kTile) || !make_key_map(P, M.k, P.k) || !make_key_map(P, M.v, P.v)) return LOCO_ERR_CUDA;
-    return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, P, M, stream);
+    if (!make_query_map(P, M.q, P.q, kTile) || !make_key_map(P, M.k, P.k, key_tile<kDim>()) || !make_key_map(P, M.v, P.v, key_tile<kDim>()))
+        return LOCO_ERR_CUDA;
+    return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, forward_bytes<kDim>(), (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, P, M, stream);
 }
 template <int kDim> int backward(const AttentionParams &P, cudaStream_t stream) {
     Maps M;
     if (!make_query_map(P, M.q, P.q, kTile) || !make_query_map(P, M.d_o, P.d_o, kTile) || !make_query_map(P, M.o, P.o, kTile) ||
-        !make_key_map(P, M.k, P.k) || !make_key_map(P, M.v, P.v)) return LOCO_ERR_CUDA;
+        !make_key_map(P, M.k, P.k, kTile) || !make_key_map(P, M.v, P.v, kTile)) return LOCO_ERR_CUDA;
     const int rc = launch(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + kTile - 1) / kTile, P.heads_q, P, M, stream);
     if (rc != LOCO_OK) return rc;
     if (query_tile<kDim>() != kTile && (!make_query_map(P, M.q, P.q, query_tile<kDim>()) || !make_query_map(P, M.d_o, P.d_o, query_tile<kDim>())))
