@@ -31,9 +31,10 @@ constexpr int kTile = 128;                       // queries and keys of a tile
 constexpr int kGroupWarps = 4;                   // warps of a softmax group: the 128 lanes of TMEM
 constexpr int kThreads = 3 * kGroupWarps * 32;   // two softmax groups and one of single warps, the last of which idles
 constexpr int kLoadWarp = 2 * kGroupWarps, kProductWarp = kLoadWarp + 1, kHelpWarp = kLoadWarp + 2;
-// Of so many pairs of scores the forward kernel takes one through exp2_poly.  4096, 32 heads: none 258 us, one in eight 254,
-// in four 252, in three 253, in two 276.
-constexpr int kPolyEvery = 4;
+// Of so many pairs of scores one goes through exp2_poly.  Forward, 4096, 32 heads: none 258 us, one in eight 254, in four 252,
+// in three 253, in two 276.  Backward over keys 435, 416, 419 with none, one in eight, in four; over queries (causal) 359,
+// 347, 350.
+constexpr int kPolyForward = 4, kPolyBackward = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -424,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
 #pragma unroll
                 for (int x = 0; x < 16; x += 2) {
                     float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, minus);
-                    if (x / 2 % kPolyEvery == kPolyEvery - 1) {
+                    if (x / 2 % kPolyForward == kPolyForward - 1) {
                         e = exp2_poly(e);
                     } else {
                         e.x = exp2_fast(e.x);
@@ -625,9 +626,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int x = 0; x < 32; x += 2) {
-                    const float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, minus);
-                    s[c][x] = __float_as_uint(exp2_fast(e.x));
-                    s[c][x + 1] = __float_as_uint(exp2_fast(e.y));
+                    float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, minus);
+                    e = x / 2 % kPolyBackward == kPolyBackward - 1 ? exp2_poly(e) : make_float2(exp2_fast(e.x), exp2_fast(e.y));
+                    s[c][x] = __float_as_uint(e.x);
+                    s[c][x + 1] = __float_as_uint(e.y);
                 }
             const int left = limit - j * kTile - t * 64;
             if (__any_sync(0xffffffffu, left < 64)) {
@@ -849,12 +851,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
 #pragma unroll
                 for (int x = 0; x < 16; x += 4) {
                     const float4 l = lse[c * 4 + x / 4];
-                    const float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, make_float2(l.x, l.y));
-                    const float2 f = fma2(make_float2(__uint_as_float(s[c][x + 2]), __uint_as_float(s[c][x + 3])), by, make_float2(l.z, l.w));
-                    s[c][x] = __float_as_uint(exp2_fast(e.x));
-                    s[c][x + 1] = __float_as_uint(exp2_fast(e.y));
-                    s[c][x + 2] = __float_as_uint(exp2_fast(f.x));
-                    s[c][x + 3] = __float_as_uint(exp2_fast(f.y));
+                    float2 e = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), by, make_float2(l.x, l.y));
+                    float2 f = fma2(make_float2(__uint_as_float(s[c][x + 2]), __uint_as_float(s[c][x + 3])), by, make_float2(l.z, l.w));
+                    e = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+                    f = x / 2 % kPolyBackward == kPolyBackward - 2 ? exp2_poly(f) : make_float2(exp2_fast(f.x), exp2_fast(f.y));
+                    s[c][x] = __float_as_uint(e.x);
+                    s[c][x + 1] = __float_as_uint(e.y);
+                    s[c][x + 2] = __float_as_uint(f.x);
+                    s[c][x + 3] = __float_as_uint(f.y);
                 }
             // under the causal mask the queries from key - off on see this key
             const int begin = P.causal ? key - off - tile * kRows - t * kHalf : 0;
