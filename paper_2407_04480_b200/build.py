@@ -2,8 +2,9 @@
 
     python -m paper_2407_04480_b200.build [--force] [--verbose]
 
-Produces paper_2407_04480_b200/libloco_b200.so and libloco_layer_b200.so (the operators of a
-decoder layer, include/loco_layer.h) next to this file.  nvcc cross-compiles without a GPU, so
+Produces paper_2407_04480_b200/libloco_b200.so, libloco_layer_b200.so (the operators of a
+decoder layer, include/loco_layer.h) and _layer_binding.so (the native half of layer.py, the only
+part that needs torch's headers) next to this file.  nvcc cross-compiles without a GPU, so
 this runs anywhere the CUDA toolkit is installed.  The kernel templates are instantiated in
 several object files (see csrc/loco_dispatch.h) that are compiled in parallel and linked into
 one shared library each; the objects live in a temporary directory.
@@ -14,6 +15,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -26,6 +28,8 @@ LAYER_LIB = os.path.join(HERE, "libloco_layer_b200.so")
 LAYER_SOURCES = ("layer_rotary.cu", "layer_router.cu", "layer_attention.cu", "layer_attention_api.cu")
 LAYER_DEPS = [os.path.join(CSRC, f) for f in LAYER_SOURCES + ("layer_common.h", "layer_attention.h", "layer_tc.cuh")] + [
     os.path.join(os.path.dirname(HERE), "include", f) for f in ("loco.h", "loco_layer.h")]
+BINDING = os.path.join(HERE, "_layer_binding.so")
+BINDING_DEPS = [os.path.join(CSRC, "layer_binding.cpp")] + [os.path.join(os.path.dirname(HERE), "include", f) for f in ("loco.h", "loco_layer.h")]
 
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC"]
@@ -57,6 +61,18 @@ def stale(lib: str = LIB, deps=DEPS) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_binding() -> None:
+    """The Python module that marshals layer.py's calls, linked against the layer library and torch."""
+    import torch
+    home, cuda = os.path.dirname(torch.__file__), os.path.dirname(os.path.dirname(nvcc_path()))
+    tmp = BINDING + ".tmp.%d" % os.getpid()
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-I" + os.path.join(home, "include"),
+                           "-I" + os.path.join(home, "include", "torch", "csrc", "api", "include"), "-I" + os.path.join(cuda, "include"),
+                           "-I" + sysconfig.get_paths()["include"], BINDING_DEPS[0], "-o", tmp, "-L" + HERE, "-lloco_layer_b200",
+                           "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, BINDING)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Build what is out of date (everything with `force`); returns the path of libloco_b200.so."""
     wanted = []                                          # (library, its units)
@@ -64,7 +80,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         wanted.append((LIB, units()))
     if force or stale(LAYER_LIB, LAYER_DEPS):
         wanted.append((LAYER_LIB, [(s[:-3], s, []) for s in LAYER_SOURCES]))
+    binding = force or stale(BINDING, BINDING_DEPS)
     if not wanted:
+        if binding:
+            build_binding()
         return LIB
     nvcc = nvcc_path()
     extra = ["-Xptxas", "-v"] if verbose else []
@@ -83,6 +102,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
                 subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static",
                                        "-Xcompiler", "-fPIC", "-o", tmp, *objs])
                 os.replace(tmp, lib)
+    if binding:
+        build_binding()
     return LIB
 
 
