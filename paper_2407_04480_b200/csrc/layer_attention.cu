@@ -490,6 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
     const uint32_t tmem = begin_block<512>(S, kSlots, 2, 2 * kGroupWarps);
     const uint32_t s_at = tmem, dp_at = tmem + kTile, dq_at = tmem + 2 * kTile, q_at = tmem + 3 * kTile, do_at = q_at + kDim / 2;
     volatile uint32_t *const failed = &S.failed;
+    let_next_start();
 
     if (warp >= 2 * kGroupWarps) {
         registers_few();
@@ -697,7 +698,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
     const BlockPlace at = block_place(P.heads_kv, P.batch, (P.max_k + kTile - 1) / kTile, false);
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * kTile;
-    if (P.packed && first >= K.n) return;
+    if (P.packed && first >= K.n) {
+        if (blockIdx.x == 0) wait_for_previous();    // the grid must not end before the one it was started under
+        return;
+    }
     // query tiles [from, until) see this tile; the heads of the group one after the other
     const int off = K.n - Q.n;
     const int until = (Q.n + kRows - 1) / kRows, from = P.causal ? min(until, max(0, first - off) / kRows) : 0;
@@ -779,7 +783,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             bar_wait(smem_addr(&S.drain), 0, failed);
             if (*failed) settle(smem_addr(&S.drain), 0);
         } else if (warp == kHelpWarp) {
-            // row statistics of each query tile, read one tile ahead, and zeros past the sample's end in the tile that holds it
+            // row statistics of each query tile, read one tile ahead, and zeros past the sample's end in the tile that holds it;
+            // D is the only thing this kernel takes from the one before it
+            wait_for_previous();
             constexpr int kMine = kRows / 32;
             float l[kMine], d[kMine];
             int g = 0, tile = from;
@@ -986,12 +992,26 @@ bool allow(Kernel fn, int which, int bytes) {
     return true;
 }
 
-int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const AttentionParams &P, const Maps &M, cudaStream_t stream) {
+// `under_previous`: the blocks may start while the last ones of the launch before are at work.
+int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const AttentionParams &P, const Maps &M, cudaStream_t stream, bool under_previous = false) {
     const int64_t blocks = tiles * heads * P.batch;
     if (blocks == 0) return LOCO_OK;
     if (blocks > 0x7fffffff) return LOCO_ERR_UNSUPPORTED;
     if (!allow(fn, which, bytes)) return LOCO_ERR_CUDA;
-    fn<<<static_cast<unsigned>(blocks), kThreads, static_cast<size_t>(bytes), stream>>>(P, M);
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3(static_cast<unsigned>(blocks));
+    how.blockDim = dim3(kThreads);
+    how.dynamicSmemBytes = static_cast<size_t>(bytes);
+    how.stream = stream;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    how.attrs = &early;
+    how.numAttrs = under_previous ? 1 : 0;
+    if (cudaLaunchKernelEx(&how, fn, P, M) != cudaSuccess) {
+        cudaGetLastError();
+        return LOCO_ERR_CUDA;
+    }
     return launched();
 }
 
@@ -1017,7 +1037,7 @@ template <int kDim> int backward(const AttentionParams &P, cudaStream_t stream) 
     if (rc != LOCO_OK) return rc;
     if (query_tile<kDim>() != kTile && (!make_query_map(P, M.q, P.q, query_tile<kDim>()) || !make_query_map(P, M.d_o, P.d_o, query_tile<kDim>())))
         return LOCO_ERR_CUDA;
-    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream);
+    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream, P.max_q > 0);
 }
 
 }  // namespace
