@@ -227,6 +227,12 @@ __device__ __forceinline__ BlockPlace block_place(int heads, int batch, int tile
     return BlockPlace{reverse ? tiles - 1 - t : t, r % heads, r / heads};
 }
 
+// Whether a packed sample ends before query `first`: most blocks of short samples, so it is asked before a block is set up.
+__device__ __forceinline__ bool no_such_rows(const AttentionParams &P, int batch, int first) {
+    wait_for_previous();
+    return first >= query_rows(P, batch).n;
+}
+
 // Keys that query i sees: [0, limit).
 __device__ __forceinline__ int key_limit(const Rows &Q, const Rows &K, int causal, int i) {
     if (i >= Q.n) return 0;
@@ -276,12 +282,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.causal);
+    if (P.packed && no_such_rows(P, at.batch, at.tile * 2 * kTile)) return;
+    const uint32_t tmem = begin_block<512>(S, kSlots, 1, kGroupWarps);
+    wait_for_previous();
+    let_next_start();
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * 2 * kTile, head_kv = at.head / P.group;
-    if (P.packed && first >= Q.n) return;
     const int n0 = key_tiles(Q, K, P.causal, first, kKeys), n1 = key_tiles(Q, K, P.causal, first + kTile, kKeys), n = max(n0, n1);
     const bool ragged = ends_inside(K, P.packed, P.seq_k, kKeys) && n == K.n / kKeys + 1;
-    const uint32_t tmem = begin_block<512>(S, kSlots, 1, kGroupWarps);
     volatile uint32_t *const failed = &S.failed;
 
     if (warp >= 2 * kGroupWarps) {
@@ -482,15 +490,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
     const uint32_t ring = smem_addr(tiles);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + kTile - 1) / kTile, P.causal);
+    if (P.packed && no_such_rows(P, at.batch, at.tile * kTile)) return;
+    const uint32_t tmem = begin_block<512>(S, kSlots, 2, 2 * kGroupWarps);
+    wait_for_previous();
+    let_next_start();
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * kTile, head_kv = at.head / P.group;
-    if (P.packed && first >= Q.n) return;
     const int n = key_tiles(Q, K, P.causal, first);
     const bool ragged = ends_inside(K, P.packed, P.seq_k) && n == K.n / kTile + 1;
-    const uint32_t tmem = begin_block<512>(S, kSlots, 2, 2 * kGroupWarps);
     const uint32_t s_at = tmem, dp_at = tmem + kTile, dq_at = tmem + 2 * kTile, q_at = tmem + 3 * kTile, do_at = q_at + kDim / 2;
     volatile uint32_t *const failed = &S.failed;
-    let_next_start();
 
     if (warp >= 2 * kGroupWarps) {
         registers_few();
@@ -695,6 +704,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
     Shared &S = *reinterpret_cast<Shared *>(tiles + 2 * kBytes + kSlots * kStep);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
+    // Started under the kernel over queries, which waited for everything before it, this one may read the operands at once;
+    // with no queries it is the first of the call.
+    if (P.max_q == 0) wait_for_previous();
     const BlockPlace at = block_place(P.heads_kv, P.batch, (P.max_k + kTile - 1) / kTile, false);
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * kTile;
@@ -786,6 +798,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             // row statistics of each query tile, read one tile ahead, and zeros past the sample's end in the tile that holds it;
             // D is the only thing this kernel takes from the one before it
             wait_for_previous();
+            let_next_start();
             constexpr int kMine = kRows / 32;
             float l[kMine], d[kMine];
             int g = 0, tile = from;
@@ -992,27 +1005,12 @@ bool allow(Kernel fn, int which, int bytes) {
     return true;
 }
 
-// `under_previous`: the blocks may start while the last ones of the launch before are at work.
-int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const AttentionParams &P, const Maps &M, cudaStream_t stream, bool under_previous = false) {
+int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const AttentionParams &P, const Maps &M, cudaStream_t stream) {
     const int64_t blocks = tiles * heads * P.batch;
     if (blocks == 0) return LOCO_OK;
     if (blocks > 0x7fffffff) return LOCO_ERR_UNSUPPORTED;
     if (!allow(fn, which, bytes)) return LOCO_ERR_CUDA;
-    cudaLaunchConfig_t how{};
-    how.gridDim = dim3(static_cast<unsigned>(blocks));
-    how.blockDim = dim3(kThreads);
-    how.dynamicSmemBytes = static_cast<size_t>(bytes);
-    how.stream = stream;
-    cudaLaunchAttribute early{};
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    how.attrs = &early;
-    how.numAttrs = under_previous ? 1 : 0;
-    if (cudaLaunchKernelEx(&how, fn, P, M) != cudaSuccess) {
-        cudaGetLastError();
-        return LOCO_ERR_CUDA;
-    }
-    return launched();
+    return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), kThreads, static_cast<size_t>(bytes), stream, P, M);
 }
 
 // What each kernel reads, in boxes of its own tiles.
@@ -1037,7 +1035,7 @@ template <int kDim> int backward(const AttentionParams &P, cudaStream_t stream) 
     if (rc != LOCO_OK) return rc;
     if (query_tile<kDim>() != kTile && (!make_query_map(P, M.q, P.q, query_tile<kDim>()) || !make_query_map(P, M.d_o, P.d_o, query_tile<kDim>())))
         return LOCO_ERR_CUDA;
-    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream, P.max_q > 0);
+    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream);
 }
 
 }  // namespace

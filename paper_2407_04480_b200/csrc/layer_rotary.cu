@@ -63,6 +63,8 @@ template <int N> __device__ __forceinline__ void load_floats(const float *p, flo
 // kVec elements of T per access (1: no alignment needed), kHeads heads per thread.
 template <typename T, bool kHalf, int kVec, int kHeads>
 __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_constant__ RotaryParams P) {
+    wait_for_previous();
+    let_next_start();
     const int64_t item64 = static_cast<int64_t>(blockIdx.x) * kRotaryThreads + threadIdx.x;
     if (item64 >= P.items) return;
     const uint32_t per_token = P.vecs * P.groups;
@@ -137,6 +139,8 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
 
 // cos and sin of p w_j in 64 bits; a row per p.
 __global__ void rotary_table_kernel(float *table, const loco_rotary_table_t c) {
+    wait_for_previous();
+    let_next_start();
     const int half = c.rotary_dim / 2;
     const int64_t n = static_cast<int64_t>(c.positions) * half;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
@@ -173,9 +177,7 @@ int launch_rotary(RotaryParams &P, int64_t tokens, void *stream) {
     const int64_t blocks = (P.items + kRotaryThreads - 1) / kRotaryThreads;
     if (blocks > 0x7fffffff) return LOCO_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned>(blocks));
-    if (many) rotary_kernel<T, kHalf, kVec, 4><<<grid, kRotaryThreads, 0, static_cast<cudaStream_t>(stream)>>>(P);
-    else rotary_kernel<T, kHalf, kVec, 1><<<grid, kRotaryThreads, 0, static_cast<cudaStream_t>(stream)>>>(P);
-    return launched();
+    return launch_kernel(many ? rotary_kernel<T, kHalf, kVec, 4> : rotary_kernel<T, kHalf, kVec, 1>, grid, kRotaryThreads, 0, stream, P);
 }
 
 }  // namespace loco_layer
@@ -199,8 +201,7 @@ int loco_rotary_table(const loco_rotary_table_t *c, float *d_table, void *stream
     if (sms == 0) return LOCO_ERR_CUDA;
     const int64_t n = static_cast<int64_t>(c->positions) * (c->rotary_dim / 2);
     const int64_t blocks = (n + 255) / 256;
-    rotary_table_kernel<<<static_cast<unsigned>(blocks < sms * 8 ? blocks : sms * 8), 256, 0, static_cast<cudaStream_t>(stream)>>>(d_table, *c);
-    return launched();
+    return launch_kernel(rotary_table_kernel, dim3(static_cast<unsigned>(blocks < sms * 8 ? blocks : sms * 8)), 256, 0, stream, d_table, *c);
 }
 
 int loco_rotary_apply(const loco_rotary_t *c, const float *d_table, const void *d_positions, const loco_heads_t *x,

@@ -280,6 +280,8 @@ __global__ void __launch_bounds__(forward_threads<kMine>()) router_forward(const
     constexpr int kPlaces = choice_places<kGroup, kMine>(), kRow = kGroup * kMine;
     const int E = P.experts, tid = threadIdx.x, warp = tid / 32, lane = tid % kGroup, warps = blockDim.x / 32, k = P.top_k;
     for (int e = tid; e < E; e += blockDim.x) tally[e] = 0;
+    wait_for_previous();
+    let_next_start();
     __syncthreads();
     float sum[kMine], zsq = 0.0f;
     int act = 0;
@@ -368,6 +370,8 @@ __global__ void __launch_bounds__(kBackwardThreads) router_backward(const __grid
     constexpr int kPlaces = choice_places<kGroup, kMine>();
     constexpr int kV = kWide ? 16 / static_cast<int>(sizeof(T)) : 1;
     const int E = P.experts, tid = threadIdx.x, lane = tid % kGroup, k = P.top_k;
+    wait_for_previous();
+    let_next_start();
     const int n = P.in_counts[E];
     const float per = n > 0 ? 1.0f / static_cast<float>(n) : 0.0f;
     const float scale = P.dlosses ? P.dlosses[0] * P.balance_coef * static_cast<float>(E) / static_cast<float>(k) * per * per : 0.0f;
@@ -545,8 +549,7 @@ int loco_router_forward(const loco_router_t *c, int64_t tokens, const void *d_lo
     blocks = blocks < 1 ? 1 : (blocks > most ? most : blocks);
     const size_t shared = static_cast<size_t>(per) * R.row * sizeof(float);
     if (shared > 28672 && !allow_shared(R.forward)) return LOCO_ERR_CUDA;
-    R.forward<<<static_cast<unsigned>(blocks), static_cast<unsigned>(per * 32), shared, static_cast<cudaStream_t>(stream)>>>(P);
-    return launched();
+    return launch_kernel(R.forward, dim3(static_cast<unsigned>(blocks)), static_cast<unsigned>(per * 32), shared, stream, P);
 }
 
 int loco_router_backward(const loco_router_t *c, int64_t tokens, const void *d_logits, int64_t row_stride, const uint8_t *d_mask,
@@ -583,8 +586,7 @@ int loco_router_backward(const loco_router_t *c, int64_t tokens, const void *d_l
     const RouterShape R = pick_router(c, wide);
     int64_t blocks = (tokens * R.group + kBackwardThreads - 1) / kBackwardThreads;
     if (blocks > sms * 8) blocks = sms * 8;
-    R.backward<<<static_cast<unsigned>(blocks), kBackwardThreads, 0, static_cast<cudaStream_t>(stream)>>>(P);
-    return launched();
+    return launch_kernel(R.backward, dim3(static_cast<unsigned>(blocks)), kBackwardThreads, 0, stream, P);
 }
 
 }  // extern "C"

@@ -53,13 +53,6 @@ __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void fence_bar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 
-// ---- the launch after this one ------------------------------------------------------------------
-
-// Once every block has said so, the next launch's blocks may start as places become free; there wait_for_previous() returns
-// when this grid is complete and its results are visible.
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // ---- tensor copies ---------------------------------------------------------------------------
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {

@@ -497,6 +497,80 @@ def test_router_gradient_against_differences():
         assert abs(slope - float(grad.norm())) <= 2e-3 * abs(slope) + 1e-6 * 300 / step
 
 
+def test_calls_in_a_row_keep_the_streams_order():
+    """Each call's kernels may be set up under the call before; every result has to be what calls with pauses give."""
+    g = gen(31)
+    b, s, h, hk, d = 2, 190, 4, 2, 64
+    table = torch.empty(s, d, device="cuda")
+    cfg = layer.Router(8, 2, z_coef=0.1)
+    x = [normal(g, b, s, h, d), normal(g, b, s, hk, d), normal(g, b, s, hk, d)]
+    proj = torch.randn(h * d, 8, generator=g, device="cuda").to(BF)
+
+    def chain(pause):
+        layer.loco_rotary_table(table, magnitude=1.1)
+        pause()
+        q, k = torch.zeros_like(x[0]), torch.zeros_like(x[1])
+        layer.loco_rotary_apply(table, x[0], x[1], q, k)
+        pause()
+        o, lse = torch.zeros_like(q), torch.zeros(b, h, s, device="cuda")
+        layer.loco_attention_forward(q, k, x[2], o, lse, causal=True)
+        pause()
+        z = o.reshape(b * s, h * d) @ proj
+        i, w = torch.zeros(b * s, 2, dtype=torch.int32, device="cuda"), torch.zeros(b * s, 2, device="cuda")
+        c, m, l = torch.zeros(9, dtype=torch.int32, device="cuda"), torch.zeros(8, device="cuda"), torch.zeros(2, device="cuda")
+        work = torch.zeros(layer.loco_router_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        layer.loco_router_forward(cfg, z, i, w, c, m, l, work)
+        pause()
+        dz = torch.zeros_like(z)
+        layer.loco_router_backward(cfg, z, i, c, dz, dlosses=l, dweights=w)
+        pause()
+        do = (dz @ proj.T).view_as(o)
+        dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(k)
+        scratch = torch.zeros(layer.loco_attention_backward_workspace_bytes(q, k), dtype=torch.uint8, device="cuda")
+        layer.loco_attention_backward(q, k, x[2], o, lse, do, dq, dk, dv, scratch, causal=True)
+        pause()
+        layer.loco_rotary_apply(table, dq, dk, dq, dk, inverse=True)
+        layer.loco_rotary_apply(table, dq, dk, dq, dk)
+        layer.loco_rotary_apply(table, dq, dk, dq, dk, inverse=True)
+        return q, k, o, lse, z, i, w, c, m, l, dz, dq, dk, dv
+    want = chain(torch.cuda.synchronize)
+    for _ in range(20):
+        got = chain(lambda: None)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, r) for p, r in zip(want, got))
+
+
+def test_calls_are_captured_into_a_graph():
+    g = gen(32)
+    q, k, v, do = normal(g, 1, 300, 4, 64), normal(g, 1, 300, 2, 64), normal(g, 1, 300, 2, 64), normal(g, 1, 300, 4, 64)
+    z, cfg = torch.randn(300, 8, generator=g, device="cuda"), layer.Router(8, 2)
+    table = torch.empty(300, 64, device="cuda")
+    layer.loco_rotary_table(table)
+    o, lse = torch.empty_like(q), torch.empty(1, 4, 300, device="cuda")
+    grads = [torch.empty_like(t) for t in (q, k, v)]
+    scratch = torch.zeros(layer.loco_attention_backward_workspace_bytes(q, k), dtype=torch.uint8, device="cuda")
+    i, w = torch.empty(300, 2, dtype=torch.int32, device="cuda"), torch.empty(300, 2, device="cuda")
+    c, m, l = torch.empty(9, dtype=torch.int32, device="cuda"), torch.empty(8, device="cuda"), torch.empty(2, device="cuda")
+    work = torch.zeros(layer.loco_router_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        layer.loco_attention_forward(q, k, v, o, lse, causal=True)
+        layer.loco_attention_backward(q, k, v, o, lse, do, *grads, scratch, causal=True)
+        layer.loco_rotary_apply(table, grads[0], grads[1], grads[0], grads[1], inverse=True)
+        layer.loco_router_forward(cfg, z, i, w, c, m, l, work)
+    calls()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (o, lse, *grads, i, w, c, m, l)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for t in (o, lse, *grads, w, m, l):
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, (o, lse, *grads, i, w, c, m, l)))
+
+
 def test_launches_are_counted():
     before = layer.loco_layer_launch_count()
     t = torch.empty(4, 8, device="cuda")
