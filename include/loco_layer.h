@@ -144,7 +144,7 @@ uint64_t loco_router_workspace_bytes(const loco_router_t *cfg);
  *   d_index       int32 [tokens, top_k]                         d_weight fp32 [tokens, top_k]
  *   d_counts      int32 [E + 1]: n_e, then N                    d_mean   fp32 [E]: P_e (0 where N = 0)
  *   d_losses      fp32 [2]: balance, z (0 where N = 0)
- *   d_work        16-byte aligned; its first 16 bytes must be zero before the first call, and every call leaves them
+ *   d_work        16-byte aligned; its first 256 bytes must be zero before the first call, and every call leaves them
  *                 zero.  Calls that may run at the same time need workspaces of their own.
  * tokens * top_k < 2^31.  No floating-point atomics: the same inputs give the same bits.  One launch.
  * Errors: ARG, ALIGN, SIZE, CUDA.
