@@ -218,13 +218,13 @@ __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
 // Whether a streamed tile that holds the last of n rows also holds rows past them that are not the copy's zero fill.
 __device__ __forceinline__ bool ends_inside(const Rows &r, int packed, int seq, int tile = kTile) { return r.n % tile != 0 && (packed || r.n != seq); }
 
-// The block's place: tiles are the slow index, so that blocks of one wave share keys; `reverse` starts with the last tile,
+// The block's place.  Heads come in spans; within a span the tiles are the slow index and `reverse` starts with the last one,
 // which under a causal mask is the longest for queries.
 struct BlockPlace { int tile, head, batch; };
-__device__ __forceinline__ BlockPlace block_place(int heads, int batch, int tiles, bool reverse) {
-    const int hb = heads * batch;
-    const int t = static_cast<int>(blockIdx.x) / hb, r = static_cast<int>(blockIdx.x) - t * hb;
-    return BlockPlace{reverse ? tiles - 1 - t : t, r % heads, r / heads};
+__device__ __forceinline__ BlockPlace block_place(const AttentionParams &P, int heads, int tiles, bool reverse) {
+    const int first = static_cast<int>(blockIdx.x) / (P.span * tiles) * P.span, size = min(P.span, heads * P.batch - first);
+    const int r = static_cast<int>(blockIdx.x) - first * tiles, t = r / size, hb = first + r - t * size;
+    return BlockPlace{reverse ? tiles - 1 - t : t, hb % heads, hb / heads};
 }
 
 // Whether a packed sample ends before query `first`: most blocks of short samples, so it is asked before a block is set up.
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
     Shared &S = *reinterpret_cast<Shared *>(tiles + 2 * kBytes + kSlots * kStep);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
-    const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.causal);
+    const BlockPlace at = block_place(P, P.heads_q, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.causal);
     if (P.packed && no_such_rows(P, at.batch, at.tile * 2 * kTile)) return;
     const uint32_t tmem = begin_block<512>(S, kSlots, 1, kGroupWarps);
     wait_for_previous();
@@ -489,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
     Shared &S = *reinterpret_cast<Shared *>(tiles + kSlots * kBytes);
     const uint32_t ring = smem_addr(tiles);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
-    const BlockPlace at = block_place(P.heads_q, P.batch, (P.max_q + kTile - 1) / kTile, P.causal);
+    const BlockPlace at = block_place(P, P.heads_q, (P.max_q + kTile - 1) / kTile, P.causal);
     if (P.packed && no_such_rows(P, at.batch, at.tile * kTile)) return;
     const uint32_t tmem = begin_block<512>(S, kSlots, 2, 2 * kGroupWarps);
     wait_for_previous();
@@ -707,7 +707,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
     // Started under the kernel over queries, which waited for everything before it, this one may read the operands at once;
     // with no queries it is the first of the call.
     if (P.max_q == 0) wait_for_previous();
-    const BlockPlace at = block_place(P.heads_kv, P.batch, (P.max_k + kTile - 1) / kTile, false);
+    const BlockPlace at = block_place(P, P.heads_kv, (P.max_k + kTile - 1) / kTile, false);
     const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * kTile;
     if (P.packed && first >= K.n) {
@@ -1005,12 +1005,22 @@ bool allow(Kernel fn, int which, int bytes) {
     return true;
 }
 
-int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, const AttentionParams &P, const Maps &M, cudaStream_t stream) {
+// Without a causal mask blocks are alike, and heads come in spans whose streams stay in L2 (126 MB, whose halves may hold the
+// same lines): with all heads at once 4096 rows of 32 heads were read from HBM three times over (backward 725 us; in spans of
+// 20 MB 695, of 40 MB 700, of 70 MB 727).  Under a causal mask the longest blocks of all heads have to come first: one span
+// (1 x 8192, 32 heads, backward 1467 us; in spans of 20 MB 1565, the grid ending in long blocks).
+constexpr int64_t kSpanBytes = 20ll << 20;
+
+// `stream_bytes`: what the blocks of one head and sample read again and again.
+int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, int64_t stream_bytes, const AttentionParams &P, const Maps &M, cudaStream_t stream) {
     const int64_t blocks = tiles * heads * P.batch;
     if (blocks == 0) return LOCO_OK;
     if (blocks > 0x7fffffff) return LOCO_ERR_UNSUPPORTED;
     if (!allow(fn, which, bytes)) return LOCO_ERR_CUDA;
-    return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), kThreads, static_cast<size_t>(bytes), stream, P, M);
+    AttentionParams Q = P;
+    const int64_t span = kSpanBytes / (stream_bytes > 0 ? stream_bytes : 1), all = heads * P.batch;
+    Q.span = static_cast<int32_t>(P.causal || span > all ? all : span < 1 ? 1 : span);
+    return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), kThreads, static_cast<size_t>(bytes), stream, Q, M);
 }
 
 // What each kernel reads, in boxes of its own tiles.
@@ -1021,21 +1031,25 @@ bool make_key_map(const AttentionParams &P, CUtensorMap &map, const Heads &t, in
     return make_map(map, t, P.packed ? 1 : P.batch, P.heads_kv, P.seq_k, P.head_dim, box_rows, P.seq_q > 0 ? P.q.ptr : P.k.ptr);
 }
 
+// Keys and values per query head, queries and their gradients per key head, of one sample on average.
+int64_t key_bytes(const AttentionParams &P) { return 4ll * P.head_dim * P.seq_k / P.group / (P.packed ? P.batch : 1); }
+int64_t query_bytes(const AttentionParams &P) { return 4ll * P.head_dim * P.seq_q * P.group / (P.packed ? P.batch : 1); }
+
 template <int kDim> int forward(const AttentionParams &P, cudaStream_t stream) {
     Maps M;
     if (!make_query_map(P, M.q, P.q, kTile) || !make_key_map(P, M.k, P.k, key_tile<kDim>()) || !make_key_map(P, M.v, P.v, key_tile<kDim>()))
         return LOCO_ERR_CUDA;
-    return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, forward_bytes<kDim>(), (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, P, M, stream);
+    return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, forward_bytes<kDim>(), (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, key_bytes(P), P, M, stream);
 }
 template <int kDim> int backward(const AttentionParams &P, cudaStream_t stream) {
     Maps M;
     if (!make_query_map(P, M.q, P.q, kTile) || !make_query_map(P, M.d_o, P.d_o, kTile) || !make_query_map(P, M.o, P.o, kTile) ||
         !make_key_map(P, M.k, P.k, kTile) || !make_key_map(P, M.v, P.v, kTile)) return LOCO_ERR_CUDA;
-    const int rc = launch(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + kTile - 1) / kTile, P.heads_q, P, M, stream);
+    const int rc = launch(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + kTile - 1) / kTile, P.heads_q, key_bytes(P), P, M, stream);
     if (rc != LOCO_OK) return rc;
     if (query_tile<kDim>() != kTile && (!make_query_map(P, M.q, P.q, query_tile<kDim>()) || !make_query_map(P, M.d_o, P.d_o, query_tile<kDim>())))
         return LOCO_ERR_CUDA;
-    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, P, M, stream);
+    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, query_bytes(P), P, M, stream);
 }
 
 }  // namespace

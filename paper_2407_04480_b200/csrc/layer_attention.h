@@ -15,6 +15,7 @@ struct AttentionParams {
     float *row_dot;                   // D_i, laid out as lse
     const int32_t *len_q, *len_k;
     int32_t batch, heads_q, heads_kv, group, head_dim, packed, seq_q, seq_k, max_q, max_k, causal;
+    int32_t span;                     // heads (of samples) whose blocks come together
     float scale;
 };
 
