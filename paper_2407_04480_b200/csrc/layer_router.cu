@@ -2,14 +2,17 @@
 //
 // A token belongs to a group of kGroup lanes, each with kMine of its logits in registers (eight experts or fewer: one
 // thread; 256 or more: a warp), read as 16-byte vectors where rows allow it, the next token's while this one is worked on.
-// The passes are bound by instructions, not by HBM: the k rounds of the choice cost a few dozen each.
+// The passes are bound by instructions, not by HBM: a round of the choice costs a few dozen, and with many experts in fp32
+// the k rounds give way to one count.
 //
 // Forward: softmax, choice and weights are local to a token; the losses need the sums over tokens of p_te, of lse^2 and
 // the counts.  Every lane keeps the sums of its own experts in registers over all its tokens, the block adds them up in a
-// fixed order and leaves one partial row in the workspace, and the block that finishes last adds the rows, again in a fixed
+// fixed order and leaves one partial row in the workspace, and the blocks that finish last add the rows, again in a fixed
 // order.  One launch, and no floating-point atomics.
 // Backward: with the counts known the gradient of a token's logits is local to the token again; it is recomputed from
 // the logits, which are the only thing both passes have to read.
+#include <cfloat>
+
 #include "layer_common.h"
 
 namespace loco_layer {
@@ -263,6 +266,97 @@ template <int kGroup, int kMine, bool kWide> struct Chooser<__nv_bfloat16, kGrou
     }
 };
 
+// The choice in one go, for fp32 and 16 or 32 lanes (65 experts and more).  `bar` is the k-th largest of the lanes' largest
+// values: k values at least reach it, so the choice is among those that do.  They are few (to meet k of G lanes takes G (1/G +
+// ... + 1/(G-k+1)) draws of a random order: 7.2 for 6 of 16, 9.0 for 8 of 32); they are laid side by side, and each lane counts
+// those before its own.  False, for the whole warp, where more than G reach `bar` for one of its tokens (equal logits): the
+// rounds of Chooser make the same choice.  Choice j comes back in lane j.
+// Forward, 50021 tokens, fp32, by rounds and so: 160 experts, k = 2: 26.5, 28.9 us; 3: 30.4, 28.9; 6: 41.5, 29.0; 8: 49.4, 31.5;
+// 256 experts, k = 2: 32.9, 34.3; 3: 38.3, 35.0; 8: 65.7, 38.7; 16: 110.0, 47.3; 512 experts, k = 8: 116.4, 56.1.  8 lanes gain 0.7 us
+// at most.  From k = 3, then; with 16 lanes to 8, beyond which more than 16 values often reach `bar` (9 would take 12.7 draws,
+// 10 take 14.9).
+constexpr int kRankFrom = 3;
+template <int kGroup> __host__ __device__ constexpr int rank_most() { return kGroup == 16 ? 8 : 16; }
+template <int kGroup> struct alignas(16) Candidates {
+    float value[kGroup];
+    int expert[kGroup];
+};
+template <int kGroup, int kMine, bool kWide>
+__device__ __forceinline__ bool rank_choice(const float *from, int lane, int k, Candidates<kGroup> &C, float &value, int &pick) {
+    float z[kMine], most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        z[i] = from[i] != from[i] ? INFINITY : from[i];
+        most = fmaxf(most, z[i]);
+    }
+    float bar;
+    if constexpr (kGroup == 32) {                    // one at a time, as integers of the same order
+        const int u = __float_as_int(most + 0.0f);
+        unsigned left = u ^ (u >> 31 | 0x80000000u), best = 0;
+#pragma unroll 1
+        for (int j = 0; j < k; ++j) {
+            best = __reduce_max_sync(kAll, left);
+            left = left == best ? 0u : left;
+        }
+        bar = __uint_as_float(best & 0x80000000u ? best ^ 0x80000000u : ~best);      // 0, none left: NaN
+    } else {
+        int before = 0;
+#pragma unroll
+        for (int o = 1; o < kGroup; ++o) before += __shfl_xor_sync(kAll, most, o) > most;
+        bar = before < k ? most : INFINITY;
+#pragma unroll
+        for (int o = kGroup / 2; o; o >>= 1) bar = fminf(bar, __shfl_xor_sync(kAll, bar, o));
+    }
+    bar = fmaxf(bar, -FLT_MAX);                      // what is not available is never chosen
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) at += z[i] >= bar;
+    const int own = at;
+#pragma unroll
+    for (int o = 1; o < kGroup; o <<= 1) {
+        const int x = __shfl_up_sync(kAll, at, o, kGroup);
+        at += lane >= o ? x : 0;
+    }
+    const int n = __shfl_sync(kAll, at, kGroup - 1, kGroup);
+    if (__any_sync(kAll, n > kGroup)) return false;
+    at -= own;
+    __syncwarp();                                    // the token before has been read
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        if (z[i] >= bar) {
+            C.value[at] = z[i];             // at < n <= kGroup
+            C.expert[at] = expert_of<float, kGroup, kWide>(lane, i);
+            ++at;
+        }
+    }
+    if (lane >= n) {
+        C.value[lane] = -INFINITY;
+        C.expert[lane] = -1;
+    }
+    __syncwarp();
+    const float mine = C.value[lane];
+    const int expert = C.expert[lane];
+    int rank = 0;
+    const int to = kGroup == 32 ? n : kGroup;
+#pragma unroll kGroup == 32 ? 1 : kGroup / 4
+    for (int j = 0; j < to; j += 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(C.value + j);
+        rank += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+    }
+    // equal values share a rank: lowest expert first
+    const unsigned taken = __reduce_or_sync(kAll, lane < n ? 1u << (rank + threadIdx.x % 32 / kGroup * kGroup) : 0u);
+    if (__popc(taken) != __popc(__ballot_sync(kAll, lane < n)))
+        for (int j = 0; j < kGroup; ++j) rank += C.value[j] == mine && C.expert[j] < expert;
+    if (lane >= n) rank = lane;
+    __syncwarp();
+    C.value[rank] = mine;
+    C.expert[rank] = expert;
+    __syncwarp();
+    value = C.value[lane];
+    pick = C.expert[lane];
+    return true;
+}
+
 // Where a lane keeps the group's choices: choice j in lane j % kGroup, place j / kGroup.
 template <int kGroup, int kMine> __host__ __device__ constexpr int choice_places() {
     return ((kGroup * kMine < kMaxChoice ? kGroup * kMine : kMaxChoice) + kGroup - 1) / kGroup;
@@ -276,7 +370,10 @@ __global__ void __launch_bounds__(forward_threads<kMine>()) router_forward(const
     __shared__ float extra[32];
     __shared__ int active[32];
     constexpr int kPlaces = choice_places<kGroup, kMine>(), kRow = kGroup * kMine;
+    constexpr bool kRank = kGroup >= 16 && sizeof(T) == 4;
+    __shared__ Candidates<kGroup> candidates[kRank ? forward_threads<kMine>() / kGroup : 1];
     const int E = P.experts, tid = threadIdx.x, warp = tid / 32, lane = tid % kGroup, warps = blockDim.x / 32, k = P.top_k;
+    const bool rank = k >= kRankFrom && k <= rank_most<kGroup>();
     for (int e = tid; e < E; e += blockDim.x) tally[e] = 0;
     wait_for_previous();
     let_next_start();
@@ -309,23 +406,32 @@ __global__ void __launch_bounds__(forward_threads<kMine>()) router_forward(const
         const float from = top != -INFINITY ? top : 0.0f;
         float share = 0.0f, w[kPlaces];
         int pick[kPlaces];
-        Chooser<T, kGroup, kMine, kWide> choose(z, lane);
+        bool chosen = false;
+        if constexpr (kRank)
+            if (rank) chosen = rank_choice<kGroup, kMine, kWide>(z, lane, k, candidates[tid / kGroup], w[0], pick[0]);
+        if (!chosen) {
+            Chooser<T, kGroup, kMine, kWide> choose(z, lane);
 #pragma unroll
-        for (int place = 0; place < kPlaces; ++place) {
-            pick[place] = -1;
-            w[place] = 0.0f;
+            for (int place = 0; place < kPlaces; ++place) {
+                pick[place] = -1;
+                w[place] = 0.0f;
 #pragma unroll 1
-            for (int j = place * kGroup; j < k && j < (place + 1) * kGroup; ++j) {
-                float value;
-                const int at = choose.next(lane, value);
-                const float pe = at < 0 ? 0.0f : exp2_fast((value - from) * kLog2e);
-                share += pe;
-                if (lane == j % kGroup) {
-                    pick[place] = at;
-                    w[place] = pe;
+                for (int j = place * kGroup; j < k && j < (place + 1) * kGroup; ++j) {
+                    float value;
+                    const int at = choose.next(lane, value);
+                    if (lane == j % kGroup) {
+                        pick[place] = at;
+                        w[place] = value;
+                    }
                 }
             }
         }
+#pragma unroll
+        for (int place = 0; place < kPlaces; ++place) {
+            w[place] = place * kGroup + lane < k && pick[place] >= 0 ? exp2_fast((w[place] - from) * kLog2e) : 0.0f;
+            share += w[place];
+        }
+        share = group_sum<kGroup>(share);
         const float by = P.normalize ? (share != 0.0f ? 1.0f / share : 1.0f) : inv;
         if (t < P.tokens) {
 #pragma unroll

@@ -465,6 +465,54 @@ def test_router_nan_is_loud():
         assert int(i.min()) >= 0 and int(i.max()) < e
 
 
+@pytest.mark.parametrize("e", [65, 128, 160, 190, 193, 256, 301, 512])
+@pytest.mark.parametrize("k", [2, 3, 6, 8, 9, 16])
+def test_router_choice_among_many_experts(e, k):
+    """Rows on which the choice can go wrong, a kind to a token: most warps hold two kinds."""
+    g, n = gen(e * 17 + k), 1500
+    z = torch.randn(n, e, generator=g, device="cuda")
+    kind = torch.arange(n, device="cuda") % 11
+    z = torch.where((kind == 1)[:, None], 0.25, z)                                     # all equal
+    z = torch.where((kind == 2)[:, None], (z * 2).round() / 2, z)                      # few values, both zeros among them
+    free = torch.rand(n, e, generator=g, device="cuda") < k * 1.2 / e
+    z = torch.where((kind == 3)[:, None] & ~free, -math.inf, z)                        # about as many available as are chosen
+    z = torch.where((kind == 4)[:, None], -math.inf, z)                                # none
+    near = torch.arange(e, device="cuda") % 64 < 4
+    z = torch.where((kind == 5)[:, None] & near, z + 9, z)                             # the largest ones are one lane's
+    z = torch.where((kind == 6)[:, None] & (torch.arange(e, device="cuda") > 0), torch.finfo(torch.float32).min, z)
+    z = torch.where((kind == 7)[:, None], torch.arange(e, device="cuda") * 1e-3, z)    # in order
+    z = torch.where((kind == 8)[:, None], torch.arange(e, device="cuda") * -1e-3, z)
+    z = torch.where((kind == 9)[:, None] & (torch.arange(e, device="cuda") != e - 1), -math.inf, z)
+    cfg = layer.Router(e, k)
+    i, w, c, _, _ = layer.router(z, cfg)
+    host = z.double().cpu()
+    value, want = torch.sort(host, dim=1, descending=True, stable=True)
+    value, want = value[:, :k], torch.where(value[:, :k] == -math.inf, -1, want[:, :k])
+    assert torch.equal(i.cpu().long(), want)
+    assert torch.equal(c[:e].cpu().long(), torch.bincount(want[want >= 0], minlength=e))
+    p = torch.where(want >= 0, torch.exp(value - value[:, :1].clamp(min=-1e300)), 0.0)
+    share = p.sum(1, keepdim=True)
+    # exponents' arguments of size up to 2 |z| below the largest; what is further down than fp32 reaches is zero
+    close(w, p / torch.where(share == 0, 1.0, share), V * (k + 16 + 64) * p + 1e-37, "weight")
+    # a token's answer does not depend on its neighbours
+    alone = z.clone()
+    alone[kind != 0] = 0.25
+    j, x, _, _, _ = layer.router(alone, cfg)
+    assert torch.equal(j[kind == 0], i[kind == 0]) and torch.equal(x[kind == 0], w[kind == 0])
+
+
+@pytest.mark.parametrize("e,k", [(160, 6), (512, 8)])
+def test_router_nan_among_many_experts(e, k):
+    z = torch.randn(40, e, generator=gen(3), device="cuda")
+    z[4, e - 2] = float("nan")
+    z[5, :] = float("nan")
+    z[6, 3], z[6, e - 3] = math.inf, float("nan")
+    i, _, _, _, l = layer.router(z, layer.Router(e, k, z_coef=1.0))
+    assert torch.isnan(l).all() and int(i[4, 0]) == e - 2 and i[5].tolist() == list(range(k)) and i[6, :2].tolist() == [3, e - 3]
+    rest = [t for t in range(40) if t not in (4, 5, 6)]
+    assert torch.equal(i[rest].cpu().long(), torch.sort(z[rest].cpu(), dim=1, descending=True, stable=True)[1][:, :k])
+
+
 def test_router_many_tokens_same_bits_twice():
     z = torch.randn(70001, 24, generator=gen(2), device="cuda") * 2
     cfg = layer.Router(24, 4, z_coef=0.1)
