@@ -1,4 +1,6 @@
-// Attention on the tensor cores: tiles of 128 queries and 128 keys, products accumulated in tensor memory (TMEM).
+// Attention on the tensor cores: tiles of 128 rows that stay, tiles of 80, 96 or 128 that stream, products accumulated in
+// tensor memory (TMEM).  4096 tokens, 32 heads of 128, not causal: forward 236 us (1166 TFLOP/s), backward 714 us (the
+// seven products it executes: 1347 TFLOP/s); the tensor pipe, 68 to 73% busy while an SM is active, bounds each.
 //
 // All three kernels have the same parts.  One warp copies tiles to shared memory (TMA, 128-byte swizzle), one thread issues
 // the products, two groups of four warps turn scores into probabilities (a thread per TMEM lane, i.e. per row), and one warp
