@@ -229,10 +229,11 @@ __device__ __forceinline__ BlockPlace block_place(const AttentionParams &P, int 
     return BlockPlace{reverse ? tiles - 1 - t : t, hb % heads, hb / heads};
 }
 
-// Whether a packed sample ends before query `first`: most blocks of short samples, so it is asked before a block is set up.
-__device__ __forceinline__ bool no_such_rows(const AttentionParams &P, int batch, int first) {
+// Whether a packed sample ends before row `first` of its queries or keys: most blocks of short samples, so it is asked
+// before a block is set up.
+template <typename RowsOf> __device__ __forceinline__ bool no_such_rows(const AttentionParams &P, const RowsOf &rows_of, int batch, int first) {
     wait_for_previous();
-    return first >= query_rows(P, batch).n;
+    return first >= rows_of(P, batch).n;
 }
 
 // Keys that query i sees: [0, limit).
@@ -284,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P, P.heads_q, (P.max_q + 2 * kTile - 1) / (2 * kTile), P.causal);
-    if (P.packed && no_such_rows(P, at.batch, at.tile * 2 * kTile)) return;
+    if (P.packed && no_such_rows(P, query_rows, at.batch, at.tile * 2 * kTile)) return;
     const uint32_t tmem = begin_block<512>(S, kSlots, 1, kGroupWarps);
     wait_for_previous();
     let_next_start();
@@ -492,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_queries_kernel
     const uint32_t ring = smem_addr(tiles);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
     const BlockPlace at = block_place(P, P.heads_q, (P.max_q + kTile - 1) / kTile, P.causal);
-    if (P.packed && no_such_rows(P, at.batch, at.tile * kTile)) return;
+    if (P.packed && no_such_rows(P, query_rows, at.batch, at.tile * kTile)) return;
     const uint32_t tmem = begin_block<512>(S, kSlots, 2, 2 * kGroupWarps);
     wait_for_previous();
     let_next_start();
@@ -706,22 +707,19 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
     Shared &S = *reinterpret_cast<Shared *>(tiles + 2 * kBytes + kSlots * kStep);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
-    // Started under the kernel over queries, which waited for everything before it, this one may read the operands at once;
-    // with no queries it is the first of the call.
-    if (P.max_q == 0) wait_for_previous();
     const BlockPlace at = block_place(P, P.heads_kv, (P.max_k + kTile - 1) / kTile, false);
-    const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     const int first = at.tile * kTile;
-    if (P.packed && first >= K.n) {
-        if (blockIdx.x == 0) wait_for_previous();    // the grid must not end before the one it was started under
-        return;
-    }
+    // only the block's set-up runs under the kernel over queries: what that one waited for is visible to it, not to this one
+    if (P.packed && no_such_rows(P, key_rows, at.batch, first)) return;
+    const uint32_t tmem = begin_block<512>(S, kSlots, 1, 2 * kGroupWarps);
+    wait_for_previous();
+    let_next_start();
+    const Rows Q = query_rows(P, at.batch), K = key_rows(P, at.batch);
     // query tiles [from, until) see this tile; the heads of the group one after the other
     const int off = K.n - Q.n;
     const int until = (Q.n + kRows - 1) / kRows, from = P.causal ? min(until, max(0, first - off) / kRows) : 0;
     const int per = first < K.n ? until - from : 0, n = per * P.group;
     const bool ragged = ends_inside(Q, P.packed, P.seq_q, kRows);
-    const uint32_t tmem = begin_block<512>(S, kSlots, 1, 2 * kGroupWarps);
     const uint32_t dv_at = tmem, dk_at = tmem + kDim, s_at = tmem + 2 * kDim, dp_at = s_at + kRows, p_at = dp_at + kRows;
     volatile uint32_t *const failed = &S.failed;
 
@@ -797,10 +795,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
             bar_wait(smem_addr(&S.drain), 0, failed);
             if (*failed) settle(smem_addr(&S.drain), 0);
         } else if (warp == kHelpWarp) {
-            // row statistics of each query tile, read one tile ahead, and zeros past the sample's end in the tile that holds it;
-            // D is the only thing this kernel takes from the one before it
-            wait_for_previous();
-            let_next_start();
+            // row statistics of each query tile, read one tile ahead, and zeros past the sample's end in the tile that holds it
             constexpr int kMine = kRows / 32;
             float l[kMine], d[kMine];
             int g = 0, tile = from;

@@ -1,0 +1,61 @@
+"""The decoder-layer operators on the GPU where they meet other work: launches in a row, values that are not finite, refusals."""
+import math
+
+import pytest
+import torch
+
+from paper_2407_04480_b200 import layer, loco
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, *shape, dtype=BF):
+    return torch.randn(shape, generator=g, device="cuda").to(dtype)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("h,hk,d", [(4, 2, 128), (6, 6, 64)])
+def test_attention_calls_in_a_row_read_what_the_launch_before_wrote(h, hk, d, packed):
+    """Operands, lengths and statistics come from the launches right before; every result has to be what calls with pauses give."""
+    g, n = gen(41), [310, 0, 7, 128, 259, 1]
+    lead = (sum(n),) if packed else (len(n), max(n))
+    src = [normal(g, *lead, x, d) for x in (h, hk, hk, h)]
+    lens = torch.tensor(n, device="cuda", dtype=torch.int32)
+    cu = torch.tensor([0] + n, device="cuda").cumsum(0).to(torch.int32)
+
+    def chain(pause):
+        if packed:
+            at = torch.zeros_like(cu)
+            at.copy_(cu)
+            kw = dict(cu_q=at, cu_k=at, max_q=max(n), max_k=max(n))
+        else:
+            at = torch.zeros_like(lens)
+            at.copy_(lens)
+            kw = dict(len_q=at, len_k=at)
+        pause()
+        q, k, v, do = (torch.empty_like(t).copy_(t) for t in src)
+        pause()
+        o, lse = torch.zeros_like(q), torch.zeros((h, lead[0]) if packed else (lead[0], h, lead[1]), device="cuda")
+        dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+        work = torch.full((layer.loco_attention_backward_workspace_bytes(q, k, **{x: y for x, y in kw.items() if packed}),), 255, dtype=torch.uint8, device="cuda")
+        for _ in range(3):                           # each pass takes its operands from the one before
+            layer.loco_attention_forward(q, k, v, o, lse, causal=True, **kw)
+            pause()
+            layer.loco_attention_backward(q, k, v, o, lse, do, dq, dk, dv, work, causal=True, **kw)
+            pause()
+            q, dq, k, dk, v, dv = dq, q, dk, k, dv, v
+        return q, k, v, o, lse
+    want = chain(torch.cuda.synchronize)
+    for _ in range(10):
+        got = chain(lambda: None)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+    assert layer.loco_layer_status() == 0
