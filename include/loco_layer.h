@@ -155,8 +155,9 @@ int loco_router_forward(const loco_router_t *cfg, int64_t tokens, const void *d_
 
 /*
  * Gradient with respect to the logits of  d_dlosses[0] * balance + d_dlosses[1] * z + sum d_dweight * weight, from the
- * forward call's d_index and d_counts.  d_dlosses (fp32 [2]) or d_dweight (fp32 [tokens, top_k]) may be NULL (zero).
- * d_dlogits: element (t, e) at t*drow_stride + e; rows of inactive tokens get zeros.  One launch.  Errors: ARG, ALIGN, CUDA.
+ * forward call's d_index and d_counts (an index outside 0 .. E - 1 is no choice).  d_dlosses (fp32 [2]) or d_dweight (fp32
+ * [tokens, top_k]) may be NULL (zero).  d_dlogits: element (t, e) at t*drow_stride + e; rows of inactive tokens get zeros.
+ * One launch.  Errors: ARG, ALIGN, CUDA.
  */
 int loco_router_backward(const loco_router_t *cfg, int64_t tokens, const void *d_logits, int64_t row_stride,
                          const uint8_t *d_mask, const int32_t *d_index, const int32_t *d_counts, const float *d_dlosses,

@@ -507,6 +507,7 @@ __global__ void __launch_bounds__(kBackwardThreads, backward_blocks<kMine>()) ro
         for (int place = 0; place < kPlaces; ++place) {
             const int j = place * kGroup + lane;
             e[place] = P.dweight && j < k && t < P.tokens ? P.in_index[t * k + j] : -1;
+            if (e[place] >= E) e[place] = -1;        // whatever the caller's indices hold, accesses stay in the row
             x[place] = e[place] >= 0 ? P.dweight[t * k + j] : 0.0f;
             pe[place] = e[place] >= 0 ? to_f32(logits[t * P.row_stride + e[place]]) : -INFINITY;      // the logit for now
         }

@@ -59,3 +59,20 @@ def test_attention_calls_in_a_row_read_what_the_launch_before_wrote(h, hk, d, pa
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, got))
     assert layer.loco_layer_status() == 0
+
+
+@pytest.mark.parametrize("e,k", [(8, 2), (40, 3), (160, 6), (512, 16)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_router_backward_takes_an_index_out_of_range_as_no_choice(e, k, dtype):
+    g = gen(43)
+    z = normal(g, 70, e, dtype=dtype)
+    cfg = layer.Router(e, k, normalize=False, balance_coef=0.3, z_coef=0.02)
+    index, _, counts, _, _ = layer.router(z, cfg)
+    dw, dl = torch.randn(70, k, generator=g, device="cuda"), torch.ones(2, device="cuda")
+    none, wild = index.clone(), index.clone()
+    none[::3, 0] = -1
+    wild[::3, 0] = torch.tensor([e, e + 1, 1 << 30, -2, -(1 << 31), 600], device="cuda", dtype=torch.int32).repeat(4)
+    want, got = torch.zeros(72, e, device="cuda", dtype=dtype), torch.zeros(72, e, device="cuda", dtype=dtype)
+    layer.loco_router_backward(cfg, z, none, counts, want[1:71], dlosses=dl, dweights=dw)
+    layer.loco_router_backward(cfg, z, wild, counts, got[1:71], dlosses=dl, dweights=dw)
+    assert torch.equal(got, want) and not got[0].any() and not got[71].any() and bool(got[1:71].isfinite().all())
