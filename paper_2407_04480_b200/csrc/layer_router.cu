@@ -620,7 +620,7 @@ int loco_router_forward(const loco_router_t *c, int64_t tokens, const void *d_lo
                         uint64_t d_work_bytes, void *stream) {
     const int rc = check_router(c);
     if (rc != LOCO_OK) return rc;
-    if (tokens < 0 || tokens * c->top_k > 0x7fffffff) return LOCO_ERR_ARG;
+    if (tokens < 0 || tokens > 0x7fffffff / c->top_k) return LOCO_ERR_ARG;
     if (!d_counts || !d_mean || !d_losses || !d_work || (tokens > 0 && (!d_logits || !d_index || !d_weight))) return LOCO_ERR_ARG;
     const uintptr_t size = c->dtype == LOCO_BF16 ? 2 : 4;
     if (!aligned(d_logits, size) || !aligned(d_index, 4) || !aligned(d_weight, 4) || !aligned(d_counts, 4) || !aligned(d_mean, 4) ||
@@ -667,7 +667,7 @@ int loco_router_backward(const loco_router_t *c, int64_t tokens, const void *d_l
                          void *d_dlogits, int64_t drow_stride, void *stream) {
     const int rc = check_router(c);
     if (rc != LOCO_OK) return rc;
-    if (tokens < 0 || tokens * c->top_k > 0x7fffffff) return LOCO_ERR_ARG;
+    if (tokens < 0 || tokens > 0x7fffffff / c->top_k) return LOCO_ERR_ARG;
     if (tokens == 0) return LOCO_OK;
     if (!d_logits || !d_index || !d_counts || !d_dlogits) return LOCO_ERR_ARG;
     const uintptr_t size = c->dtype == LOCO_BF16 ? 2 : 4;
