@@ -92,7 +92,7 @@ int loco_rotary_apply(const loco_rotary_t *cfg, const float *d_table, const void
  * are summed over its query heads.  A query that sees no key has o = 0, lse = -inf and no gradient.
  */
 typedef struct {
-    int32_t batch, heads_q, heads_kv;   /* heads_kv divides heads_q                                             */
+    int32_t batch, heads_q, heads_kv;   /* heads_kv divides heads_q, batch * heads_q < 2^31                     */
     int32_t head_dim;                   /* a multiple of 8, 8 .. 128                                            */
     int32_t packed;                     /* 0: padded samples, 1: samples one after the other                    */
     int32_t seq_q, seq_k;               /* rows: of every sample (padded), of all samples together (packed)     */

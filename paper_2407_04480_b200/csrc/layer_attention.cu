@@ -1008,16 +1008,26 @@ bool allow(Kernel fn, int which, int bytes) {
 // (1 x 8192, 32 heads, backward 1467 us; in spans of 20 MB 1565, the grid ending in long blocks).
 constexpr int64_t kSpanBytes = 20ll << 20;
 
-// `stream_bytes`: what the blocks of one head and sample read again and again.
-int launch(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, int64_t stream_bytes, const AttentionParams &P, const Maps &M, cudaStream_t stream) {
-    const int64_t blocks = tiles * heads * P.batch;
-    if (blocks == 0) return LOCO_OK;
-    if (blocks > 0x7fffffff) return LOCO_ERR_UNSUPPORTED;
-    if (!allow(fn, which, bytes)) return LOCO_ERR_CUDA;
-    AttentionParams Q = P;
+// A launch, checked as far as the host can: nothing of a call is launched before all of it is.  `stream_bytes`: what the blocks
+// of one head and sample read again and again.
+struct Launch {
+    Kernel fn;
+    int which, bytes;                // place in allow(), shared memory
+    int64_t blocks;
+    int32_t span;
+    Maps maps;
+    bool ready() const { return blocks == 0 || allow(fn, which, bytes); }
+    int go(const AttentionParams &P, cudaStream_t stream) const {
+        if (blocks == 0) return LOCO_OK;
+        AttentionParams Q = P;
+        Q.span = span;
+        return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), kThreads, static_cast<size_t>(bytes), stream, Q, maps);
+    }
+};
+constexpr int64_t kMostBlocks = 0x7fffffff;
+Launch plan(Kernel fn, int which, int bytes, int64_t tiles, int64_t heads, int64_t stream_bytes, const AttentionParams &P) {
     const int64_t span = kSpanBytes / (stream_bytes > 0 ? stream_bytes : 1), all = heads * P.batch;
-    Q.span = static_cast<int32_t>(P.causal || span > all ? all : span < 1 ? 1 : span);
-    return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), kThreads, static_cast<size_t>(bytes), stream, Q, M);
+    return Launch{fn, which, bytes, tiles * all, static_cast<int32_t>(P.causal || span > all ? all : span < 1 ? 1 : span), {}};
 }
 
 // What each kernel reads, in boxes of its own tiles.
@@ -1033,20 +1043,24 @@ int64_t key_bytes(const AttentionParams &P) { return 4ll * P.head_dim * P.seq_k 
 int64_t query_bytes(const AttentionParams &P) { return 4ll * P.head_dim * P.seq_q * P.group / (P.packed ? P.batch : 1); }
 
 template <int kDim> int forward(const AttentionParams &P, cudaStream_t stream) {
-    Maps M;
-    if (!make_query_map(P, M.q, P.q, kTile) || !make_key_map(P, M.k, P.k, key_tile<kDim>()) || !make_key_map(P, M.v, P.v, key_tile<kDim>()))
-        return LOCO_ERR_CUDA;
-    return launch(attention_forward_kernel<kDim>, kDim / 64 - 1, forward_bytes<kDim>(), (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, key_bytes(P), P, M, stream);
+    Launch f = plan(attention_forward_kernel<kDim>, kDim / 64 - 1, forward_bytes<kDim>(), (P.max_q + 2 * kTile - 1) / (2 * kTile), P.heads_q, key_bytes(P), P);
+    if (f.blocks > kMostBlocks) return LOCO_ERR_UNSUPPORTED;
+    if (!make_query_map(P, f.maps.q, P.q, kTile) || !make_key_map(P, f.maps.k, P.k, key_tile<kDim>()) || !make_key_map(P, f.maps.v, P.v, key_tile<kDim>()) ||
+        !f.ready()) return LOCO_ERR_CUDA;
+    return f.go(P, stream);
 }
 template <int kDim> int backward(const AttentionParams &P, cudaStream_t stream) {
-    Maps M;
-    if (!make_query_map(P, M.q, P.q, kTile) || !make_query_map(P, M.d_o, P.d_o, kTile) || !make_query_map(P, M.o, P.o, kTile) ||
-        !make_key_map(P, M.k, P.k, kTile) || !make_key_map(P, M.v, P.v, kTile)) return LOCO_ERR_CUDA;
-    const int rc = launch(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + kTile - 1) / kTile, P.heads_q, key_bytes(P), P, M, stream);
-    if (rc != LOCO_OK) return rc;
-    if (query_tile<kDim>() != kTile && (!make_query_map(P, M.q, P.q, query_tile<kDim>()) || !make_query_map(P, M.d_o, P.d_o, query_tile<kDim>())))
+    Launch q = plan(attention_backward_queries_kernel<kDim>, 2 + kDim / 64 - 1, shared_bytes<kDim>(), (P.max_q + kTile - 1) / kTile, P.heads_q, key_bytes(P), P);
+    Launch k = plan(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, query_bytes(P), P);
+    if (q.blocks > kMostBlocks || k.blocks > kMostBlocks) return LOCO_ERR_UNSUPPORTED;
+    if (!make_query_map(P, q.maps.q, P.q, kTile) || !make_query_map(P, q.maps.d_o, P.d_o, kTile) || !make_query_map(P, q.maps.o, P.o, kTile) ||
+        !make_key_map(P, q.maps.k, P.k, kTile) || !make_key_map(P, q.maps.v, P.v, kTile)) return LOCO_ERR_CUDA;
+    k.maps = q.maps;
+    if (query_tile<kDim>() != kTile && (!make_query_map(P, k.maps.q, P.q, query_tile<kDim>()) || !make_query_map(P, k.maps.d_o, P.d_o, query_tile<kDim>())))
         return LOCO_ERR_CUDA;
-    return launch(attention_backward_keys_kernel<kDim>, 4 + kDim / 64 - 1, shared_bytes_keys<kDim>(), (P.max_k + kTile - 1) / kTile, P.heads_kv, query_bytes(P), P, M, stream);
+    if (!q.ready() || !k.ready()) return LOCO_ERR_CUDA;
+    const int rc = q.go(P, stream);
+    return rc == LOCO_OK ? k.go(P, stream) : rc;
 }
 
 }  // namespace

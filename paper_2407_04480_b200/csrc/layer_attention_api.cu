@@ -12,6 +12,7 @@ int check_attention(const loco_attention_t *c) {
     if (c->packed && (c->max_q < 0 || c->max_k < 0 || c->max_q > c->seq_q || c->max_k > c->seq_k || !c->d_len_q || !c->d_len_k))
         return LOCO_ERR_ARG;
     if (c->head_dim > 128 || c->head_dim % 8) return LOCO_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(c->batch) * c->heads_q > 0x7fffffff) return LOCO_ERR_UNSUPPORTED;      // blocks and rows stay within 64 bits
     if (!aligned(c->d_len_q, 4) || !aligned(c->d_len_k, 4)) return LOCO_ERR_ALIGN;
     return LOCO_OK;
 }
