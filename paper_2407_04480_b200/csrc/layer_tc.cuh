@@ -36,16 +36,20 @@ __device__ __forceinline__ uint64_t now_ns() {
 
 constexpr uint64_t kWaitLimitNs = 2000000000ull;      // a wait longer than this gives up
 
-// Waits for the phase.  Past the limit it raises `failed` and returns; from then on every wait of the block returns at
-// once, so that all its roles run to their ends (on meaningless values) and nothing hangs.
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
-    if (bar_test(bar, parity)) return;
+// Waits for the phase.  Past the limit it raises `failed` and returns; from then on every wait of the block returns after one
+// look at its barrier (0.14 us, measured), so that all roles walk to their ends (on meaningless values) in about the time
+// that the block would have taken anyway.  Leaving their loops instead takes a vote of the warp a tile: 5 to 20% slower.
+template <uint64_t kLimitNs = kWaitLimitNs> __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
+    if (bar_test(bar, parity) || *failed) return;
     const uint64_t begin = now_ns();
     for (;;) {
         for (int i = 0; i < 64; ++i)
             if (bar_test(bar, parity)) return;
         if (*failed) return;
-        if (now_ns() - begin > kWaitLimitNs) *failed = 1;
+        if (now_ns() - begin > kLimitNs) {
+            *failed = 1;
+            return;
+        }
     }
 }
 

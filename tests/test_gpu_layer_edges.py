@@ -1,9 +1,13 @@
 """The decoder-layer operators on the GPU where they meet other work: launches in a row, values that are not finite, refusals."""
+import ctypes
 import math
+import os
+import subprocess
 
 import pytest
 import torch
 
+from paper_2407_04480_b200 import build as loco_build
 from paper_2407_04480_b200 import layer, loco
 
 pytestmark = pytest.mark.gpu
@@ -76,3 +80,22 @@ def test_router_backward_takes_an_index_out_of_range_as_no_choice(e, k, dtype):
     layer.loco_router_backward(cfg, z, none, counts, want[1:71], dlosses=dl, dweights=dw)
     layer.loco_router_backward(cfg, z, wild, counts, got[1:71], dlosses=dl, dweights=dw)
     assert torch.equal(got, want) and not got[0].any() and not got[71].any() and bool(got[1:71].isfinite().all())
+
+
+def test_a_wait_that_runs_out_ends_the_block_and_raises_the_flag(tmp_path):
+    """Built into a library of its own, so that the flag of the one in use stays as it is."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    lib = str(tmp_path / "wait.so")
+    subprocess.check_call([loco_build.nvcc_path(), *loco_build.NVCC_FLAGS, "-shared", "-cudart", "static", "-o", lib, os.path.join(here, "attention_wait.cu")])
+    L = ctypes.CDLL(lib)
+    L.run_wait.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p]
+    L.loco_layer_status.argtypes = [ctypes.POINTER(ctypes.c_uint32), ctypes.c_void_p]
+    ns, flags, stream = torch.zeros(3, dtype=torch.int64, device="cuda"), ctypes.c_uint32(7), torch.cuda.current_stream().cuda_stream
+    assert L.loco_layer_status(ctypes.byref(flags), stream) == 0 and flags.value == 0
+    assert L.run_wait(ns.data_ptr(), 100, stream) == 0
+    torch.cuda.synchronize()
+    out, after, word = ns.tolist()
+    assert 20_000_000 <= out < 1_000_000_000 and word == 1
+    assert after < 2_000_000_000, "a hundred waits after it take less together than the limit of one"
+    assert L.loco_layer_status(ctypes.byref(flags), stream) == 0 and flags.value == layer.FLAG_TIMEOUT
+    assert layer.loco_layer_status() == 0
