@@ -470,10 +470,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __
         __syncwarp();
         fence_after();
         const int end = P.packed ? Q.n : P.seq_q;
+        const bool some = limit > 0 && top != -INFINITY;           // a score above -infinity, or NaN
         // through this tile's queries, which no product reads any more
-        store_rows<kDim>(tiles + t * kBytes + warp % kGroupWarps * (32 * kDim * 2), o_at, nt > 0, 1.0f / total, limit > 0, P.o, Q, i - lane, end,
-                         at.head, 0, P.head_dim);
-        if (i < end) P.lse[stat_at(P, Q, i, at.head)] = limit > 0 ? (top * scale + log2f(total)) * kLn2 : -INFINITY;
+        store_rows<kDim>(tiles + t * kBytes + warp % kGroupWarps * (32 * kDim * 2), o_at, nt > 0, 1.0f / total, some, P.o, Q, i - lane, end, at.head, 0,
+                         P.head_dim);
+        if (i < end) P.lse[stat_at(P, Q, i, at.head)] = some ? (top == INFINITY ? INFINITY : (top * scale + log2f(total)) * kLn2) : -INFINITY;
     }
     __syncwarp();
     end_block<512>(S, tmem);
@@ -876,14 +877,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
                     s[c][x + 2] = __float_as_uint(f.x);
                     s[c][x + 3] = __float_as_uint(f.y);
                 }
-            // under the causal mask the queries from key - off on see this key
-            const int begin = P.causal ? key - off - tile * kRows - t * kHalf : 0;
-            if (__any_sync(0xffffffffu, begin > 0)) {
+            // under the causal mask the queries before key - off do not see this key; nor do those past the sample's end, whose zeros
+            // times an infinite key are NaN
+            const int begin = P.causal ? key - off - tile * kRows - t * kHalf : 0, stop = Q.n - tile * kRows - t * kHalf;
+            if (__any_sync(0xffffffffu, begin > 0 || stop < kHalf)) {
+                const unsigned live = static_cast<unsigned>(max(stop - begin, 0));
 #pragma unroll
                 for (int c = 0; c < kHalf / 16; ++c)
 #pragma unroll
                     for (int x = 0; x < 16; ++x)
-                        if (c * 16 + x < begin) s[c][x] = 0;
+                        if (static_cast<unsigned>(c * 16 + x - begin) >= live) s[c][x] = 0;
             }
             if (++tile == until) tile = from;
             if (j > 0) {                         // dv has read the previous P^T

@@ -208,21 +208,21 @@ __device__ __forceinline__ float max2(float a, float b) {
     return d;
 }
 // 2^x without the special-function unit, whose 16 results a clock bound the softmax: x = n + f with |f| <= 1/2, 2^f by the
-// polynomial of degree 4 with the least largest relative error there (2.7e-6; fitted by weighted least squares), n into the
-// exponent.  x below -126 counts as -126; x above 127 is not for this function.
+// polynomial of degree 4 with the least largest relative error there (2.7e-6; fitted by weighted least squares), times 2^n
+// put together as its bits.  Below -127 and at -infinity the answer is 0 (as n + 127 is), for NaN it is NaN; x above 127 is
+// not for this function.
 __device__ __forceinline__ float2 exp2_poly(float2 x) {
     constexpr float kRound = 12582912.0f;          // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
-    x.x = fmaxf(x.x, -126.0f);
-    x.y = fmaxf(x.y, -126.0f);
+    x.x = max2(x.x, -127.0f);
+    x.y = max2(x.y, -127.0f);
     const float2 t = add2(x, make_float2(kRound, kRound));
     const float2 f = fma2(add2(t, make_float2(-kRound, -kRound)), make_float2(-1.0f, -1.0f), x);
     float2 p = fma2(f, make_float2(0.00957007986f, 0.00957007986f), make_float2(0.0559178367f, 0.0559178367f));
     p = fma2(p, f, make_float2(0.240247443f, 0.240247443f));
     p = fma2(p, f, make_float2(0.693121791f, 0.693121791f));
     p = fma2(p, f, make_float2(0.999999285f, 0.999999285f));
-    p.x = __int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23));
-    p.y = __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23));
-    return p;
+    const auto power = [](float t) { return __uint_as_float((__float_as_uint(t) << 23) + 0x3f800000u); };
+    return mul2(p, make_float2(power(t.x), power(t.y)));
 }
 
 }  // namespace tc

@@ -9,9 +9,11 @@ import torch
 
 from paper_2407_04480_b200 import build as loco_build
 from paper_2407_04480_b200 import layer, loco
+from tests import layer_reference as ref
 
 pytestmark = pytest.mark.gpu
 
+U = ref.U                        # of a rounding to bfloat16, relative
 BF, F32 = torch.bfloat16, torch.float32
 
 
@@ -99,3 +101,100 @@ def test_a_wait_that_runs_out_ends_the_block_and_raises_the_flag(tmp_path):
     assert after < 2_000_000_000, "a hundred waits after it take less together than the limit of one"
     assert L.loco_layer_status(ctypes.byref(flags), stream) == 0 and flags.value == layer.FLAG_TIMEOUT
     assert layer.loco_layer_status() == 0
+
+
+def run_attention(q, k, v, do, causal):
+    b, s, h, _ = q.shape
+    o, lse = torch.full_like(q, 7.0), torch.full((b, h, s), 7.0, device="cuda")
+    layer.loco_attention_forward(q, k, v, o, lse, causal=causal)
+    grads = [torch.full_like(t, 7.0) for t in (q, k, v)]
+    work = torch.full((layer.loco_attention_backward_workspace_bytes(q, k),), 255, dtype=torch.uint8, device="cuda")
+    layer.loco_attention_backward(q, k, v, o, lse, do, *grads, work, causal=causal)
+    return (o, lse, *grads)
+
+
+def positive_first(g, b, s, d):
+    """Operands [b, s, 1, d] whose queries are positive, and at least 1/4, in the first dimension."""
+    q, k, v, do = (normal(g, b, s, 1, d) for _ in range(4))
+    q[..., 0] = q[..., 0].abs() + 0.25
+    return q, k, v, do
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_with_an_infinite_score_is_nan_wherever_its_key_lies(d, causal):
+    """Sample j has a score of +infinity at key j: o is NaN and lse +infinity for the queries that see it, and for no others."""
+    n = 250
+    q, k, v, do = positive_first(gen(51), n, n, d)
+    plain = run_attention(q, k, v, do, causal)
+    j = torch.arange(n, device="cuda")
+    k[j, j, 0, 0] = math.inf
+    o, lse, dq, dk, dv = run_attention(q, k, v, do, causal)
+    sees = (j[None, :] >= j[:, None]) if causal else torch.ones(n, n, dtype=torch.bool, device="cuda")      # [sample, query]
+    assert torch.equal(torch.isnan(o).all(-1).all(-1), sees) and torch.equal(torch.isnan(o).any(-1).any(-1), sees)
+    assert torch.equal(lse[:, 0] == math.inf, sees) and torch.isfinite(lse[:, 0][~sees]).all()
+    assert torch.isnan(dq[..., 1:])[sees].all() and torch.isnan(dv[j, j]).all()
+    if causal:                       # two roundings of p and of o each
+        off = (o.float() - plain[0].float()).abs().amax(-1)[..., 0][~sees]
+        assert float(off.max()) <= 4 * U * float(v.float().abs().max())
+        assert torch.isfinite(dq[~sees][..., 1:]).all()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_key_with_a_score_of_minus_infinity_takes_no_part(d, causal):
+    """Sample j has scores of -infinity at key j: p is zero there, as the 64-bit formulas have it."""
+    n = 131
+    q, k, v, do = positive_first(gen(52), n, n, d)
+    j = torch.arange(n, device="cuda")
+    k[j, j, 0, 0] = -math.inf
+    o, lse, dq, dk, dv = run_attention(q, k, v, do, causal)
+    for b in range(n):
+        x, l, a = ref.attention(q[b, :, 0], k[b, :, 0], v[b, :, 0], causal, d ** -0.5)
+        x = torch.nan_to_num(x)
+        empty = l == -math.inf       # causal: the first query of sample 0 sees that key alone
+        assert torch.equal(lse[b, 0][empty].double(), l[empty]) and int(empty.sum()) == (1 if causal and b == 0 else 0)
+        assert float((lse[b, 0] - l)[~empty].abs().max()) <= 1e-4
+        assert bool(((o[b, :, 0] - x).abs() <= U * x.abs() + (U + 1e-4) * a + 1e-30).all())
+        want = ref.attention_gradient(q[b, :, 0], k[b, :, 0], v[b, :, 0], o[b, :, 0], lse[b, 0], do[b, :, 0], causal, d ** -0.5)
+        for got, w, bound, dims in ((dq, want[0], want[3], slice(1, d)), (dk, want[1], want[4], slice(0, d)), (dv, want[2], want[5], slice(0, d))):
+            w, bound = w[:, dims], bound[:, dims]
+            assert bool(((got[b, :, 0, dims] - w).abs() <= U * w.abs() + (U + 1e-4) * bound + 2e-4 * (1 + float(bound.max()))).all())
+        assert not dv[b, b].any() and not dk[b, b].any()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_scores_that_are_all_minus_infinity_is_zero(d):
+    q, k, v, do = positive_first(gen(53), 3, 200, d)
+    k[1, :, 0, 0] = -math.inf
+    o, lse, dq, dk, dv = run_attention(q, k, v, do, False)
+    assert not o[1].any() and (lse[1] == -math.inf).all() and not dv[1].any() and not dk[1].any()
+    for b in (0, 2):
+        x, _, a = ref.attention(q[b, :, 0], k[b, :, 0], v[b, :, 0], False, d ** -0.5)
+        assert bool(((o[b, :, 0] - x).abs() <= U * x.abs() + (U + 1e-4) * a + 1e-30).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_query_that_is_nan_reaches_every_gradient_it_takes_part_in(d):
+    """Sample i has a query i of NaN: its o, lse and dq are NaN, other queries' are not, and every key's dk and dv are."""
+    n = 210
+    q, k, v, do = positive_first(gen(54), n, n, d)
+    i = torch.arange(n, device="cuda")
+    q[i, i] = float("nan")
+    o, lse, dq, dk, dv = run_attention(q, k, v, do, False)
+    own = torch.eye(n, dtype=torch.bool, device="cuda")
+    for t in (o, dq):
+        bad = torch.isnan(t)[:, :, 0]
+        assert torch.equal(bad.all(-1), own) and torch.equal(bad.any(-1), own)
+    assert torch.equal(torch.isnan(lse[:, 0]), own)
+    assert torch.isnan(dk).all() and torch.isnan(dv).all()
+
+
+@pytest.mark.parametrize("n", [150, 128])
+def test_attention_gradient_of_an_infinite_key_does_not_depend_on_where_the_queries_end(n):
+    """All scores of key 3 are -infinity: no query takes it, whether or not a tile has rows past the last query."""
+    for d in (64, 128):
+        q, k, v, do = positive_first(gen(55), 1, n, d)
+        k[0, 3, 0, 0] = -math.inf
+        _, _, _, dk, dv = run_attention(q, k, v, do, False)
+        assert not dk[0, 3].any() and not dv[0, 3].any() and bool(dk.isfinite().all()) and bool(dv.isfinite().all())
