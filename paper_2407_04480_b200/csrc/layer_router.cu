@@ -238,13 +238,14 @@ template <typename T, int kGroup, int kMine, bool kWide> struct Chooser {
     }
 };
 // bfloat16: value and expert fit one integer whose order is the choice's (order of the value in the upper half, 0xffff -
-// expert in the lower), so that one reduction finds both.  Adding 0 makes -0 and NaN plain.
+// expert in the lower), so that one reduction finds both.  Adding 0 makes -0 plain and NaN the largest integer, which then
+// counts as +infinity's.
 template <int kGroup, int kMine, bool kWide> struct Chooser<__nv_bfloat16, kGroup, kMine, kWide> {
     unsigned key[kMine];
     __device__ __forceinline__ Chooser(const float *from, int lane) {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-            const int u = __float_as_int(from[i] + 0.0f);
+            const int u = min(__float_as_int(from[i] + 0.0f), 0x7f800000);
             key[i] = ((u ^ (u >> 31 | 0x80000000u)) & 0xffff0000u) | (0xffffu - expert_of<__nv_bfloat16, kGroup, kWide>(lane, i));
         }
     }

@@ -198,3 +198,48 @@ def test_attention_gradient_of_an_infinite_key_does_not_depend_on_where_the_quer
         k[0, 3, 0, 0] = -math.inf
         _, _, _, dk, dv = run_attention(q, k, v, do, False)
         assert not dk[0, 3].any() and not dv[0, 3].any() and bool(dk.isfinite().all()) and bool(dv.isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("e,k", [(8, 2), (16, 4), (40, 3), (65, 6), (160, 6), (256, 8), (512, 16)])
+def test_router_counts_nan_as_infinity_in_the_choice(e, k, dtype):
+    """Ties between the two go to the lowest expert; the losses are NaN."""
+    z = normal(gen(61), 48, e, dtype=dtype)
+    kind = torch.arange(48, device="cuda") % 6
+    z[kind == 1, e - 2] = float("nan")
+    z[kind == 2] = float("nan")
+    z[kind == 3, 3], z[kind == 3, e - 3] = math.inf, float("nan")
+    z[kind == 4, 1], z[kind == 4, e - 1] = float("nan"), math.inf
+    z[kind == 5, ::2], z[kind == 5, 1::2] = math.inf, float("nan")
+    # a NaN with its sign bit set and another payload
+    bits = z.view(torch.int16 if dtype == BF else torch.int32)
+    bits[1, e - 2] = -1
+    index, _, counts, _, losses = layer.router(z, layer.Router(e, k, z_coef=1.0))
+    order = torch.where(torch.isnan(z), math.inf, z.double()).cpu()
+    want = torch.sort(order, dim=1, descending=True, stable=True)[1][:, :k]
+    assert torch.equal(index.cpu().long(), want)
+    assert torch.isnan(losses).all() and int(counts[e]) == 48
+    assert torch.equal(counts[:e].cpu().long(), torch.bincount(want.flatten(), minlength=e))
+
+
+@pytest.mark.parametrize("e", [9, 64, 65, 128, 160, 193, 256, 301, 512])
+@pytest.mark.parametrize("k", [1, 3, 8, 9])
+def test_router_choice_in_bfloat16(e, k):
+    """Rows on which the choice can go wrong, a kind to a token; the order is that of the rounded logits."""
+    g, n = gen(e * 17 + k), 700
+    z = torch.randn(n, e, generator=g, device="cuda")
+    kind, column = torch.arange(n, device="cuda") % 9, torch.arange(e, device="cuda")
+    z = torch.where((kind == 1)[:, None], 0.25, z)                                     # all equal
+    z = torch.where((kind == 2)[:, None], (z * 2).round() / 2, z)                      # few values, both zeros among them
+    free = torch.rand(n, e, generator=g, device="cuda") < k * 1.2 / e
+    z = torch.where((kind == 3)[:, None] & ~free, -math.inf, z)                        # about as many available as are chosen
+    z = torch.where((kind == 4)[:, None], -math.inf, z)                                # none
+    z = torch.where((kind == 5)[:, None] & (column > 0), torch.finfo(BF).min, z)
+    z = torch.where((kind == 6)[:, None], column * 1e-3, z)                            # in order, ties by rounding
+    z = torch.where((kind == 7)[:, None], column * -1e-3, z)
+    z = torch.where((kind == 8)[:, None] & (column != e - 1), -math.inf, z).to(BF)
+    index, _, counts, _, _ = layer.router(z, layer.Router(e, k))
+    value, want = torch.sort(z.double().cpu(), dim=1, descending=True, stable=True)
+    want = torch.where(value[:, :k] == -math.inf, -1, want[:, :k])
+    assert torch.equal(index.cpu().long(), want)
+    assert torch.equal(counts[:e].cpu().long(), torch.bincount(want[want >= 0], minlength=e))
