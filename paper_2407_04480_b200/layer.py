@@ -198,27 +198,40 @@ def loco_router_backward(cfg: Router, logits, index, counts, dlogits, mask=None,
 
 # ---- differentiable forms --------------------------------------------------------------------
 
-class _Rotary(torch.autograd.Function):
+class _Gradient(torch.autograd.Function):
+    """A backward pass as a node of its own, over everything that it depends on.  Its kernels write memory that autograd does
+    not see into: what differentiates the gradient again has to pass here, and raises."""
     @staticmethod
-    def forward(ctx, q, k, table, positions, layout):
+    def forward(ctx, name, compute, *tensors):
+        ctx.name = name
+        return compute(*tensors)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("layer.%s can be differentiated once: its gradient has no gradient" % ctx.name)
+
+
+class _Rotary(torch.autograd.Function):
+    """Linear in q and k: the gradient is the transposed rotation, which is differentiable in turn."""
+    @staticmethod
+    def forward(ctx, q, k, table, positions, layout, inverse):
         ctx.save_for_backward(table, positions)
-        ctx.layout = layout
+        ctx.how = (layout, inverse)
         qo, ko = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
-        loco_rotary_apply(table, q, k, qo, ko, positions=positions, layout=layout)
+        loco_rotary_apply(table, q, k, qo, ko, positions=positions, layout=layout, inverse=inverse)
         return qo, ko
 
     @staticmethod
     def backward(ctx, dq, dk):
         table, positions = ctx.saved_tensors
-        dq, dk = dq.contiguous(), dk.contiguous()        # also a broadcast gradient gets memory of its own
-        gq, gk = torch.empty_like(dq), torch.empty_like(dk)
-        loco_rotary_apply(table, dq, dk, gq, gk, positions=positions, layout=ctx.layout, inverse=True)
-        return gq, gk, None, None, None
+        layout, inverse = ctx.how
+        # contiguous: also a broadcast gradient gets memory of its own
+        return (*_Rotary.apply(dq.contiguous(), dk.contiguous(), table, positions, layout, not inverse), None, None, None, None)
 
 
 def rotary(q, k, table, positions=None, layout: str = "half"):
     """Rotated queries and keys [batch, seq, heads, dim]."""
-    return _Rotary.apply(q, k, table, positions, layout)
+    return _Rotary.apply(q, k, table, positions, layout, False)
 
 
 class _Attention(torch.autograd.Function):
@@ -235,18 +248,20 @@ class _Attention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, do):
-        q, k, v, o, lse = ctx.saved_tensors
         causal, scale, lens = ctx.how
-        do = do.contiguous()
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        packed = {x: lens.get(x) for x in ("cu_q", "cu_k", "max_q", "max_k")}
-        work = torch.empty(loco_attention_backward_workspace_bytes(q, k, **packed), dtype=torch.uint8, device=q.device)
-        loco_attention_backward(q, k, v, o, lse, do, dq, dk, dv, work, causal=causal, scale=scale, **lens)
-        return dq, dk, dv, None, None, None
+
+        def compute(q, k, v, o, lse, do):
+            do = do.contiguous()
+            dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+            packed = {x: lens.get(x) for x in ("cu_q", "cu_k", "max_q", "max_k")}
+            work = torch.empty(loco_attention_backward_workspace_bytes(q, k, **packed), dtype=torch.uint8, device=q.device)
+            loco_attention_backward(q, k, v, o, lse, do, dq, dk, dv, work, causal=causal, scale=scale, **lens)
+            return dq, dk, dv
+        return (*_Gradient.apply("attention", compute, *ctx.saved_tensors, do), None, None, None)
 
 
 def attention(q, k, v, causal: bool = False, scale: Optional[float] = None, **lens):
-    """softmax(scale q k^T) v; shapes and lengths as loco_attention_forward."""
+    """softmax(scale q k^T) v; shapes and lengths as loco_attention_forward.  Differentiable once."""
     return _Attention.apply(q, k, v, causal, scale, lens)
 
 
@@ -266,15 +281,16 @@ class _Router(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, _index, dweight, _counts, _mean, dlosses):
-        logits, index, counts, mask = ctx.saved_tensors
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        loco_router_backward(ctx.cfg, logits, index, counts, dlogits, mask=mask, dlosses=dlosses.contiguous(),
-                             dweights=dweight.contiguous())
-        return dlogits, None, None, None
+        def compute(logits, index, counts, mask, dweight, dlosses):
+            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+            loco_router_backward(ctx.cfg, logits, index, counts, dlogits, mask=mask, dlosses=dlosses.contiguous(),
+                                 dweights=dweight.contiguous())
+            return dlogits
+        return _Gradient.apply("router", compute, *ctx.saved_tensors, dweight, dlosses), None, None, None
 
 
 def router(logits, cfg: Router, mask=None, work: Optional[torch.Tensor] = None):
-    """(index, weight, counts, mean, losses) of logits [tokens, experts]; weight and losses are differentiable.
+    """(index, weight, counts, mean, losses) of logits [tokens, experts]; weight and losses are differentiable, once.
 
     work: a workspace to keep between calls (loco_router_workspace_bytes() bytes, zeroed once); None allocates one."""
     if work is None:

@@ -243,3 +243,27 @@ def test_router_choice_in_bfloat16(e, k):
     want = torch.where(value[:, :k] == -math.inf, -1, want[:, :k])
     assert torch.equal(index.cpu().long(), want)
     assert torch.equal(counts[:e].cpu().long(), torch.bincount(want[want >= 0], minlength=e))
+
+
+def test_second_derivatives():
+    """Rotary has them (against differentiation of its formula in 64 bits), attention and the router refuse them."""
+    g = gen(71)
+    table = torch.empty(30, 16, device="cuda")
+    layer.loco_rotary_table(table, magnitude=1.2)
+    q, k = normal(g, 2, 30, 3, 16, dtype=F32).requires_grad_(), normal(g, 2, 30, 1, 16, dtype=F32).requires_grad_()
+
+    def second(y, x):
+        grad, = torch.autograd.grad((y ** 3).sum() + (x ** 3).sum(), x, create_graph=True)
+        return grad, torch.autograd.grad((grad ** 2).sum(), x)[0]
+    x = q.detach().double().requires_grad_()
+    c, s = table[:, None, :8].double(), table[:, None, 8:].double()
+    plain = torch.cat([x[..., :8] * c - x[..., 8:] * s, x[..., 8:] * c + x[..., :8] * s], -1)
+    for got, want in zip(second(layer.rotary(q, k, table)[0], q), second(plain, x)):
+        # some twenty roundings in fp32 of terms that cancel to a tenth of their size at the least, in norm
+        assert float((got.double() - want).detach().norm()) <= 200 * 2.0 ** -24 * float(want.detach().norm())
+    heads = [normal(g, 1, 40, 2, 64).requires_grad_() for _ in range(3)]
+    z = normal(g, 40, 8, dtype=F32).requires_grad_()
+    for x, y in ((heads[0], layer.attention(*heads)), (z, layer.router(z, layer.Router(8, 2))[1])):
+        grad, = torch.autograd.grad((y.float() ** 3).sum() + (x.float() ** 3).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="differentiated once"):
+            torch.autograd.grad((grad.float() ** 2).sum(), x)

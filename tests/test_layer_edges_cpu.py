@@ -46,3 +46,86 @@ def test_attention_refuses_more_blocks_than_a_launch_holds_before_it_launches_an
     if tiles * size["batch"] * size["hq"] >= 1 << 31:
         assert L.loco_attention_forward(cfg, x, x, x, x, PTR, None) == loco.ERR_UNSUPPORTED
     assert layer.loco_layer_launch_count() == before
+
+
+# ---- differentiable forms, with plain torch in the place of the kernels
+
+@pytest.fixture
+def kernels(monkeypatch):
+    """Stand-ins that fill the outputs as the kernels do, out of autograd's sight; calls are noted as (name, arguments)."""
+    calls = []
+
+    def stand_in(name):
+        def place(fn):
+            def call(*a, **kw):
+                calls.append((name, a, kw))
+                with torch.no_grad():
+                    fn(*a, **kw)
+            monkeypatch.setattr(layer, name, call)
+            return fn
+        return place
+
+    @stand_in("loco_rotary_apply")
+    def _(table, q, k, qo, ko, positions=None, layout="half", inverse=False):
+        for x, y in ((q, qo), (k, ko)):
+            if x is not None:
+                y.copy_(x * 2)                   # its own transpose
+
+    @stand_in("loco_attention_forward")
+    def _(q, k, v, o, lse, **kw):
+        o.copy_(q * 3)
+        lse.zero_()
+
+    @stand_in("loco_attention_backward")
+    def _(q, k, v, o, lse, do, dq, dk, dv, work, **kw):
+        dq.copy_(do * 3)
+        dk.zero_()
+        dv.zero_()
+
+    @stand_in("loco_router_forward")
+    def _(cfg, logits, index, weight, counts, mean, losses, work, mask=None):
+        weight.copy_(logits[:, :cfg.top_k])
+        for t in (index, counts, mean, losses):
+            t.zero_()
+
+    @stand_in("loco_router_backward")
+    def _(cfg, logits, index, counts, dlogits, mask=None, dlosses=None, dweights=None):
+        dlogits.zero_()
+        dlogits[:, :cfg.top_k] = dweights
+    return calls
+
+
+def forms():
+    """(operands that require a gradient, a differentiable output) of each form."""
+    heads = [torch.randn(1, 4, 2, 8, requires_grad=True) for _ in range(3)]
+    z = torch.randn(5, 8, requires_grad=True)
+    return {"rotary": (heads[0], lambda: layer.rotary(heads[0], heads[1], torch.zeros(4, 8))[0]),
+            "attention": (heads[0], lambda: layer.attention(*heads)),
+            "router": (z, lambda: layer.router(z, layer.Router(8, 2), work=torch.zeros(1))[1])}
+
+
+@pytest.mark.parametrize("form", ["attention", "router"])
+def test_a_second_derivative_is_refused(kernels, form):
+    """The gradient of a gradient would lose the terms that go through the backward kernel."""
+    x, value = forms()[form]
+    for loss in (lambda: (value() ** 3).sum(), lambda: (value() ** 3).sum() + (x ** 3).sum()):
+        grad, = torch.autograd.grad(loss(), x, create_graph=True)
+        assert torch.isfinite(grad).all()
+        with pytest.raises(RuntimeError, match="differentiated once"):
+            torch.autograd.grad((grad ** 2).sum(), x)
+        with pytest.raises(RuntimeError, match="differentiated once"):
+            torch.autograd.grad(loss(), x, create_graph=True)[0].square().sum().backward()
+        # the first one stays as it is, and frees its graph
+        torch.autograd.grad(loss(), x)[0].square().sum()
+
+
+def test_rotary_has_every_derivative(kernels):
+    """Its gradient is a rotation again; the stand-in is a product with 2."""
+    x, value = forms()["rotary"]
+
+    def second(y):
+        grad, = torch.autograd.grad((y() ** 3 + x ** 3).sum(), x, create_graph=True)
+        return grad, torch.autograd.grad((grad ** 2).sum(), x)[0]
+    for got, want in zip(second(value), second(lambda: 2 * x)):
+        assert torch.allclose(got, want)
+    assert [c[2]["inverse"] for c in kernels] == [False, True, False, True]
