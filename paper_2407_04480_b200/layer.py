@@ -236,33 +236,32 @@ def rotary(q, k, table, positions=None, layout: str = "half"):
 
 class _Attention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, causal, scale, lens):
-        lens = dict(lens)
+    def forward(ctx, q, k, v, causal, scale, lens, longest):
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((q.shape[1], q.shape[0]) if lens.get("cu_q") is not None else (q.shape[0], q.shape[2], q.shape[1]),
+        lse = torch.empty((q.shape[1], q.shape[0]) if lens["cu_q"] is not None else (q.shape[0], q.shape[2], q.shape[1]),
                           dtype=torch.float32, device=q.device)
-        loco_attention_forward(q, k, v, o, lse, causal=causal, scale=scale, **lens)
-        ctx.save_for_backward(q, k, v, o, lse)
-        ctx.how = (causal, scale, lens)
+        loco_attention_forward(q, k, v, o, lse, causal=causal, scale=scale, **lens, **longest)
+        ctx.save_for_backward(q, k, v, o, lse, *lens.values())
+        ctx.how = (causal, scale, tuple(lens), longest)
         return o
 
     @staticmethod
     def backward(ctx, do):
-        causal, scale, lens = ctx.how
+        causal, scale, names, longest = ctx.how
 
-        def compute(q, k, v, o, lse, do):
-            do = do.contiguous()
+        def compute(q, k, v, o, lse, *rest):
+            lens, do = dict(zip(names, rest)), rest[-1].contiguous()
             dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-            packed = {x: lens.get(x) for x in ("cu_q", "cu_k", "max_q", "max_k")}
-            work = torch.empty(loco_attention_backward_workspace_bytes(q, k, **packed), dtype=torch.uint8, device=q.device)
-            loco_attention_backward(q, k, v, o, lse, do, dq, dk, dv, work, causal=causal, scale=scale, **lens)
+            work = torch.empty(loco_attention_backward_workspace_bytes(q, k, lens["cu_q"], lens["cu_k"], **longest), dtype=torch.uint8, device=q.device)
+            loco_attention_backward(q, k, v, o, lse, do, dq, dk, dv, work, causal=causal, scale=scale, **lens, **longest)
             return dq, dk, dv
-        return (*_Gradient.apply("attention", compute, *ctx.saved_tensors, do), None, None, None)
+        return (*_Gradient.apply("attention", compute, *ctx.saved_tensors, do), None, None, None, None)
 
 
 def attention(q, k, v, causal: bool = False, scale: Optional[float] = None, **lens):
     """softmax(scale q k^T) v; shapes and lengths as loco_attention_forward.  Differentiable once."""
-    return _Attention.apply(q, k, v, causal, scale, lens)
+    tensors = {x: lens.pop(x, None) for x in ("len_q", "len_k", "cu_q", "cu_k")}
+    return _Attention.apply(q, k, v, causal, scale, tensors, lens)
 
 
 class _Router(torch.autograd.Function):

@@ -267,3 +267,29 @@ def test_second_derivatives():
         grad, = torch.autograd.grad((y.float() ** 3).sum() + (x.float() ** 3).sum(), x, create_graph=True)
         with pytest.raises(RuntimeError, match="differentiated once"):
             torch.autograd.grad((grad.float() ** 2).sum(), x)
+
+
+@pytest.mark.parametrize("how", ["plain", "lengths", "packed"])
+def test_differentiable_attention_is_the_two_calls(how):
+    """The same bits as loco_attention_forward and loco_attention_backward, with lengths and packed samples."""
+    g, n = gen(72), [90, 0, 131]
+    packed = how == "packed"
+    lead = (sum(n),) if packed else (3, 131)
+    q, k, v = (normal(g, *lead, h, 64).requires_grad_() for h in (4, 2, 2))
+    w = normal(g, *lead, 4, 64)
+    lens = {}
+    if how == "lengths":
+        lens = dict(len_q=torch.tensor(n, device="cuda", dtype=torch.int32), len_k=torch.tensor([131, 5, 64], device="cuda", dtype=torch.int32))
+    elif packed:
+        cu = torch.tensor([0] + n, device="cuda").cumsum(0).to(torch.int32)
+        lens = dict(cu_q=cu, cu_k=cu, max_q=131, max_k=131)
+    o = layer.attention(q, k, v, causal=True, scale=0.2, **lens)
+    got = torch.autograd.grad((o * w).sum(), (q, k, v))
+    q, k, v = (t.detach() for t in (q, k, v))
+    want, lse = torch.empty_like(q), torch.empty((4, lead[0]) if packed else (3, 4, 131), device="cuda")
+    layer.loco_attention_forward(q, k, v, want, lse, causal=True, scale=0.2, **lens)
+    grads = [torch.empty_like(t) for t in (q, k, v)]
+    work = torch.empty(layer.loco_attention_backward_workspace_bytes(q, k, **{x: y for x, y in lens.items() if packed}), dtype=torch.uint8, device="cuda")
+    layer.loco_attention_backward(q, k, v, want, lse, w, *grads, work, causal=True, scale=0.2, **lens)
+    assert torch.equal(o, want) and all(torch.equal(a, b) for a, b in zip(got, grads))
+    assert any(bool(t.any()) for t in got)

@@ -129,3 +129,31 @@ def test_rotary_has_every_derivative(kernels):
     for got, want in zip(second(value), second(lambda: 2 * x)):
         assert torch.allclose(got, want)
     assert [c[2]["inverse"] for c in kernels] == [False, True, False, True]
+
+
+def lengths(packed):
+    if packed:
+        cu = torch.tensor([0, 3, 4], dtype=torch.int32)
+        return (4, 2, 8), dict(cu_q=cu, cu_k=cu.clone(), max_q=3, max_k=3)
+    return (2, 4, 2, 8), dict(len_q=torch.tensor([4, 2], dtype=torch.int32), len_k=torch.tensor([1, 4], dtype=torch.int32))
+
+
+@pytest.mark.parametrize("changed", ["len_q", "len_k", "cu_q", "cu_k"])
+def test_attention_notices_lengths_that_change_before_the_backward_pass(kernels, changed):
+    shape, lens = lengths(changed.startswith("cu"))
+    q, k, v = (torch.randn(shape, requires_grad=True) for _ in range(3))
+    o = layer.attention(q, k, v, causal=True, **lens)
+    lens[changed] += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        o.sum().backward()
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_attention_hands_the_same_lengths_to_both_passes(kernels, packed):
+    shape, lens = lengths(packed)
+    q, k, v = (torch.randn(shape, requires_grad=True) for _ in range(3))
+    layer.attention(q, k, v, causal=True, scale=0.3, **lens).sum().backward()
+    (_, _, there), (_, _, back) = kernels
+    assert there.keys() == back.keys() and there["causal"] is True and there["scale"] == 0.3
+    for name, value in lens.items():
+        assert there[name] is value and (back[name] == value if isinstance(value, int) else torch.equal(back[name], value))
