@@ -271,7 +271,7 @@ class _Router(torch.autograd.Function):
         index = torch.empty((n, cfg.top_k), dtype=torch.int32, device=dev)
         weight = torch.empty((n, cfg.top_k), dtype=torch.float32, device=dev)
         counts = torch.empty(cfg.experts + 1, dtype=torch.int32, device=dev)
-        mean, losses = torch.empty(cfg.experts, device=dev), torch.empty(2, device=dev)
+        mean, losses = (torch.empty(size, dtype=torch.float32, device=dev) for size in (cfg.experts, 2))
         loco_router_forward(cfg, logits, index, weight, counts, mean, losses, work, mask=mask)
         ctx.save_for_backward(logits, index, counts, mask)
         ctx.cfg = cfg

@@ -157,3 +157,15 @@ def test_attention_hands_the_same_lengths_to_both_passes(kernels, packed):
     assert there.keys() == back.keys() and there["causal"] is True and there["scale"] == 0.3
     for name, value in lens.items():
         assert there[name] is value and (back[name] == value if isinstance(value, int) else torch.equal(back[name], value))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float64])
+def test_router_results_do_not_take_the_default_type(kernels, dtype):
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(dtype)
+    try:
+        layer.router(torch.randn(5, 8, dtype=torch.float32), layer.Router(8, 2), work=torch.zeros(1))
+    finally:
+        torch.set_default_dtype(was)
+    (_, (_, _, index, weight, counts, mean, losses, _), _), = kernels
+    assert [t.dtype for t in (index, weight, counts, mean, losses)] == [torch.int32, torch.float32, torch.int32, torch.float32, torch.float32]
