@@ -251,6 +251,8 @@ class _Attention(torch.autograd.Function):
 
         def compute(q, k, v, o, lse, *rest):
             lens, do = dict(zip(names, rest)), rest[-1].contiguous()
+            if do.data_ptr() % 16:                   # a contiguous view, off the boundaries that the kernels need
+                do = do.clone()
             dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
             work = torch.empty(loco_attention_backward_workspace_bytes(q, k, lens["cu_q"], lens["cu_k"], **longest), dtype=torch.uint8, device=q.device)
             loco_attention_backward(q, k, v, o, lse, do, dq, dk, dv, work, causal=causal, scale=scale, **lens, **longest)

@@ -169,3 +169,15 @@ def test_router_results_do_not_take_the_default_type(kernels, dtype):
         torch.set_default_dtype(was)
     (_, (_, _, index, weight, counts, mean, losses, _), _), = kernels
     assert [t.dtype for t in (index, weight, counts, mean, losses)] == [torch.int32, torch.float32, torch.int32, torch.float32, torch.float32]
+
+
+def test_attention_takes_a_gradient_that_is_a_view_off_every_boundary(kernels):
+    """torch.cat hands on a contiguous view at an odd offset; the kernels need 16-byte boundaries."""
+    q, k, v = (torch.randn(1, 4, 2, 8, dtype=torch.bfloat16).requires_grad_() for _ in range(3))
+    o = layer.attention(q, k, v)
+    joined = torch.cat([torch.zeros(3, dtype=torch.bfloat16), o.flatten()])
+    w = torch.randn(joined.shape).to(torch.bfloat16)
+    got, = torch.autograd.grad(joined, q, w)
+    _, args, _ = kernels[-1]
+    assert args[5].is_contiguous() and args[5].data_ptr() % 16 == 0
+    assert torch.equal(got, w[3:].view_as(q) * 3)
