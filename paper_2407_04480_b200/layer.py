@@ -260,10 +260,11 @@ class _Attention(torch.autograd.Function):
         return (*_Gradient.apply("attention", compute, *ctx.saved_tensors, do), None, None, None, None)
 
 
-def attention(q, k, v, causal: bool = False, scale: Optional[float] = None, **lens):
-    """softmax(scale q k^T) v; shapes and lengths as loco_attention_forward.  Differentiable once."""
-    tensors = {x: lens.pop(x, None) for x in ("len_q", "len_k", "cu_q", "cu_k")}
-    return _Attention.apply(q, k, v, causal, scale, tensors, lens)
+def attention(q, k, v, causal: bool = False, scale: Optional[float] = None, len_q=None, len_k=None, cu_q=None, cu_k=None,
+              max_q: Optional[int] = None, max_k: Optional[int] = None):
+    """softmax(scale q k^T) v; shapes and lengths as loco_attention_forward, on the current stream.  Differentiable once."""
+    lens = dict(len_q=len_q, len_k=len_k, cu_q=cu_q, cu_k=cu_k)
+    return _Attention.apply(q, k, v, causal, scale, lens, dict(max_q=max_q, max_k=max_k))
 
 
 class _Router(torch.autograd.Function):

@@ -181,3 +181,12 @@ def test_attention_takes_a_gradient_that_is_a_view_off_every_boundary(kernels):
     _, args, _ = kernels[-1]
     assert args[5].is_contiguous() and args[5].data_ptr() % 16 == 0
     assert torch.equal(got, w[3:].view_as(q) * 3)
+
+
+@pytest.mark.parametrize("name", ["stream", "len", "out"])
+def test_differentiable_attention_takes_no_other_argument(kernels, name):
+    """Its results belong to the current stream: work sent to another one would outlive them."""
+    q, k, v = (torch.randn(1, 4, 2, 8) for _ in range(3))
+    with pytest.raises(TypeError):
+        layer.attention(q, k, v, **{name: None})
+    assert not kernels
