@@ -43,7 +43,12 @@ int device_of(const at::Tensor &t) {
 }
 void *stream_of(PyObject *stream, int device) {
     if (stream == Py_None) return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream();
-    return reinterpret_cast<void *>(PyLong_AsUnsignedLongLong(stream));
+    const unsigned long long raw = PyLong_AsUnsignedLongLong(stream);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse("the stream must be a raw stream's address");
+    }
+    return reinterpret_cast<void *>(raw);
 }
 
 int32_t dtype_of(const at::Tensor &t) {
@@ -83,6 +88,14 @@ int64_t integer(PyObject *o, const char *what) {
     }
     return x;
 }
+bool truth(PyObject *o, const char *what) {
+    const int x = PyObject_IsTrue(o);
+    if (x < 0) {
+        PyErr_Clear();
+        refuse(std::string(what) + " must be true or false");
+    }
+    return x != 0;
+}
 float number(PyObject *o, const char *what) {
     const double x = PyFloat_AsDouble(o);
     if (x == -1.0 && PyErr_Occurred()) {
@@ -118,7 +131,7 @@ int rotary_apply(PyObject *const *a) {
     }
     const void *at = positions ? flat(a[5], shape.slice(0, 2), positions->scalar_type(), device, "positions") : nullptr;
     const loco_rotary_t cfg{dtype_of(q), static_cast<int32_t>(integer(a[6], "layout")), small(shape[3], "dim"), small(table.size(1), "rotary_dim"),
-                            small(shape[0], "batch"), small(shape[1], "seq"), small(table.size(0), "positions"), wide, PyObject_IsTrue(a[7])};
+                            small(shape[0], "batch"), small(shape[1], "seq"), small(table.size(0), "positions"), wide, truth(a[7], "inverse")};
     return loco_rotary_apply(&cfg, table.const_data_ptr<float>(), at, x, y, count, k ? 2 : 1, stream_of(a[8], device));
 }
 
@@ -171,7 +184,7 @@ Attention attention(const at::Tensor &q, const at::Tensor &k, PyObject *const *a
     t.packed = packed;
     t.seq_q = small(c.qs[n - 3], "rows");
     t.seq_k = small(c.ks[n - 3], "rows");
-    t.causal = PyObject_IsTrue(a[0]);
+    t.causal = truth(a[0], "causal");
     t.scale = a[1] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(t.head_dim))) : number(a[1], "scale");
     return c;
 }
@@ -211,7 +224,7 @@ struct Rows {
 Rows rows(const at::Tensor &t, PyObject *const *a, const char *what) {
     Rows r{};
     r.device = device_of(t);
-    r.cfg = loco_router_t{dtype_of(t), small(integer(a[0], "experts"), "experts"), small(integer(a[1], "top_k"), "top_k"), PyObject_IsTrue(a[2]),
+    r.cfg = loco_router_t{dtype_of(t), small(integer(a[0], "experts"), "experts"), small(integer(a[1], "top_k"), "top_k"), truth(a[2], "normalize"),
                           number(a[3], "balance_coef"), number(a[4], "z_coef")};
     if (t.dim() != 2 || t.size(1) != r.cfg.experts || (t.stride(1) != 1 && t.size(1) > 1)) refuse(std::string(what) + " must be [tokens, experts] with contiguous rows");
     r.tokens = t.size(0);

@@ -293,3 +293,19 @@ def test_differentiable_attention_is_the_two_calls(how):
     layer.loco_attention_backward(q, k, v, want, lse, w, *grads, work, causal=True, scale=0.2, **lens)
     assert torch.equal(o, want) and all(torch.equal(a, b) for a, b in zip(got, grads))
     assert any(bool(t.any()) for t in got)
+
+
+def test_arguments_that_are_neither_true_nor_false_are_refused_before_a_launch():
+    g, many = gen(73), torch.zeros(2)
+    q, o, lse = normal(g, 1, 4, 2, 64), torch.zeros(1, 4, 2, 64, device="cuda", dtype=BF), torch.zeros(1, 2, 4, device="cuda")
+    table = torch.empty(4, 64, device="cuda")
+    layer.loco_rotary_table(table)
+    z = normal(g, 4, 8)
+    before = layer.loco_layer_launch_count()
+    for call in (lambda: layer.loco_attention_forward(q, q, q, o, lse, causal=many),
+                 lambda: layer.loco_rotary_apply(table, q, None, o, None, inverse=many),
+                 lambda: layer.router(z, layer.Router(8, 2, normalize=many), work=torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")),
+                 lambda: layer._binding().rotary_apply(table, q, None, o, None, None, 0, False, "a stream")):
+        with pytest.raises(ValueError):
+            call()
+    assert layer.loco_layer_launch_count() == before and not o.any()
