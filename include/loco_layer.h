@@ -27,7 +27,7 @@ extern "C" {
 
 /* Heads of a [batch, row, head, dim] tensor: element (b, t, h, i) lies at ptr + b*batch_stride + t*row_stride +
  * h*head_stride + i, strides in elements, so that heads may be cut out of one projection's output.  The stride of a
- * dimension of extent one is ignored. */
+ * dimension of extent one is ignored; a zero stride repeats an input over its dimension and is refused (ARG) in an output. */
 typedef struct {
     void   *ptr;
     int64_t batch_stride, row_stride, head_stride;

@@ -18,13 +18,14 @@ int check_attention(const loco_attention_t *c) {
 }
 
 // An operand with rows: present, on 16-byte boundaries, strides of whole 16-byte units and none negative.  The stride of a
-// dimension of extent one means nothing.
-int take(const loco_attention_t *c, const loco_heads_t *t, int32_t heads, int32_t rows, Heads &out) {
+// dimension of extent one means nothing.  Zero strides repeat what is read; nothing that is written may be repeated.
+int take(const loco_attention_t *c, const loco_heads_t *t, int32_t heads, int32_t rows, Heads &out, bool written = false) {
     if (!t) return LOCO_ERR_ARG;
     const int64_t b = c->packed || c->batch <= 1 ? 0 : t->batch_stride, r = rows <= 1 ? 0 : t->row_stride, h = heads <= 1 ? 0 : t->head_stride;
     out = Heads{static_cast<__nv_bfloat16 *>(t->ptr), b, r, h};
     if (rows == 0 || c->batch == 0) return LOCO_OK;
     if (!t->ptr || b < 0 || r < 0 || h < 0) return LOCO_ERR_ARG;
+    if (written && ((!c->packed && c->batch > 1 && b == 0) || (rows > 1 && r == 0) || (heads > 1 && h == 0))) return LOCO_ERR_ARG;
     if (!aligned(t->ptr, 16) || b % 8 || r % 8 || h % 8) return LOCO_ERR_ALIGN;
     return LOCO_OK;
 }
@@ -63,7 +64,7 @@ int loco_attention_forward(const loco_attention_t *c, const loco_heads_t *q, con
     if (rc == LOCO_OK) rc = take(c, q, c->heads_q, c->seq_q, P.q);
     if (rc == LOCO_OK) rc = take(c, k, c->heads_kv, c->seq_k, P.k);
     if (rc == LOCO_OK) rc = take(c, v, c->heads_kv, c->seq_k, P.v);
-    if (rc == LOCO_OK) rc = take(c, o, c->heads_q, c->seq_q, P.o);
+    if (rc == LOCO_OK) rc = take(c, o, c->heads_q, c->seq_q, P.o, true);
     if (rc != LOCO_OK) return rc;
     if (nq == 0) return LOCO_OK;
     if (!d_lse) return LOCO_ERR_ARG;
@@ -88,9 +89,9 @@ int loco_attention_backward(const loco_attention_t *c, const loco_heads_t *q, co
     if (rc == LOCO_OK) rc = take(c, v, c->heads_kv, c->seq_k, P.v);
     if (rc == LOCO_OK) rc = take(c, o, c->heads_q, c->seq_q, P.o);
     if (rc == LOCO_OK) rc = take(c, d_o, c->heads_q, c->seq_q, P.d_o);
-    if (rc == LOCO_OK) rc = take(c, dq, c->heads_q, c->seq_q, P.dq);
-    if (rc == LOCO_OK) rc = take(c, dk, c->heads_kv, c->seq_k, P.dk);
-    if (rc == LOCO_OK) rc = take(c, dv, c->heads_kv, c->seq_k, P.dv);
+    if (rc == LOCO_OK) rc = take(c, dq, c->heads_q, c->seq_q, P.dq, true);
+    if (rc == LOCO_OK) rc = take(c, dk, c->heads_kv, c->seq_k, P.dk, true);
+    if (rc == LOCO_OK) rc = take(c, dv, c->heads_kv, c->seq_k, P.dv, true);
     if (rc != LOCO_OK) return rc;
     if (nq == 0 && nk == 0) return LOCO_OK;
     if (!d_work || (nq > 0 && !d_lse)) return LOCO_ERR_ARG;

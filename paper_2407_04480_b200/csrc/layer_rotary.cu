@@ -237,6 +237,8 @@ int loco_rotary_apply(const loco_rotary_t *c, const float *d_table, const void *
         if (c->batch == 1) t.xb = t.yb = 0;              // the stride of a dimension of extent one means nothing
         if (c->seq == 1) t.xr = t.yr = 0;
         if (heads[i] == 1) t.xh = t.yh = 0;
+        // zero strides repeat what is read; nothing that is written may be repeated
+        if ((c->batch > 1 && t.yb == 0) || (c->seq > 1 && t.yr == 0) || (heads[i] > 1 && t.yh == 0)) return LOCO_ERR_ARG;
         wide = wide && aligned(t.x, 16) && aligned(t.y, 16);
         for (int64_t s : {t.xb, t.xr, t.xh, t.yb, t.yr, t.yh}) wide = wide && s % vec == 0;
     }

@@ -670,7 +670,7 @@ int loco_router_backward(const loco_router_t *c, int64_t tokens, const void *d_l
     if (rc != LOCO_OK) return rc;
     if (tokens < 0 || tokens > 0x7fffffff / c->top_k) return LOCO_ERR_ARG;
     if (tokens == 0) return LOCO_OK;
-    if (!d_logits || !d_index || !d_counts || !d_dlogits) return LOCO_ERR_ARG;
+    if (!d_logits || !d_index || !d_counts || !d_dlogits || (tokens > 1 && drow_stride == 0)) return LOCO_ERR_ARG;
     const uintptr_t size = c->dtype == LOCO_BF16 ? 2 : 4;
     if (!aligned(d_logits, size) || !aligned(d_dlogits, size) || !aligned(d_index, 4) || !aligned(d_counts, 4) ||
         !aligned(d_dlosses, 4) || !aligned(d_dweight, 4)) return LOCO_ERR_ALIGN;

@@ -309,3 +309,36 @@ def test_arguments_that_are_neither_true_nor_false_are_refused_before_a_launch()
         with pytest.raises(ValueError):
             call()
     assert layer.loco_layer_launch_count() == before and not o.any()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_expanded_operands(d, causal):
+    """Keys and values shared by the batch or by the heads, queries by the batch: the same bits as of copies; an expanded
+    operand's gradient, summed by autograd, is the sum of the copies'."""
+    g, b, s, h = gen(81), 3, 150, 4
+    src = dict(q=normal(g, 1, s, h, d), k=normal(g, 1, s, h, d), v=normal(g, b, s, 1, d), one=normal(g, 1, s, 1, d), row=normal(g, b, 1, h, d))
+    shape = (b, s, h, d)
+    for names in (("q", "k", "v"), ("q", "one", "k"), ("row", "v", "row")):
+        ops = [src[x].clone().requires_grad_() for x in names]
+        seen = [t.expand(shape) for t in ops]
+        copies = [t.detach().contiguous().requires_grad_() for t in seen]
+        assert any(0 in t.stride() for t in seen)
+        w = normal(g, *shape)
+        o, want = layer.attention(*seen, causal=causal), layer.attention(*copies, causal=causal)
+        assert torch.equal(o, want)
+        spread = torch.autograd.grad(want, copies, w)
+        for got, each, t in zip(torch.autograd.grad(o, ops, w), spread, ops):
+            assert torch.equal(got, each.sum_to_size(t.shape))
+
+
+def test_rotary_and_router_of_expanded_operands():
+    g = gen(82)
+    table = torch.empty(40, 64, device="cuda")
+    layer.loco_rotary_table(table)
+    q, k = normal(g, 1, 40, 1, 64).expand(2, 40, 6, 64), normal(g, 2, 1, 2, 64).expand(2, 40, 2, 64)
+    for a, b in zip(layer.rotary(q, k, table), layer.rotary(q.contiguous(), k.contiguous(), table)):
+        assert torch.equal(a, b)
+    z, cfg = normal(g, 1, 40).expand(33, 40), layer.Router(40, 3, z_coef=0.1)
+    for a, b in zip(layer.router(z, cfg), layer.router(z.contiguous(), cfg)):
+        assert torch.equal(a, b)

@@ -48,6 +48,21 @@ def test_attention_refuses_more_blocks_than_a_launch_holds_before_it_launches_an
     assert layer.loco_layer_launch_count() == before
 
 
+@pytest.mark.parametrize("zero", ["batch", "row", "head"])
+def test_outputs_that_repeat_memory_are_refused(zero):
+    """Inputs may (expanded tensors); of an output several threads would write the same place."""
+    L, good = layer.lib(), dict(batch=2048, row=256, head=64)
+    x, bad = heads(*good.values()), heads(*{**good, zero: 0}.values())
+    cfg = attention_cfg(batch=2, hq=4, hk=4, sq=8, sk=8)
+    size = L.loco_attention_backward_workspace_bytes(cfg)
+    assert L.loco_attention_forward(cfg, x, x, x, bad, PTR, None) == loco.ERR_ARG
+    for outs in ((bad, x, x), (x, bad, x), (x, x, bad)):
+        assert L.loco_attention_backward(cfg, x, x, x, x, PTR, x, *outs, PTR, size, None) == loco.ERR_ARG
+    cfg = layer._ROTARY.pack(loco.BF16, 0, 64, 64, 2, 8, 8, 0, 0)
+    assert L.loco_rotary_apply(cfg, PTR, None, x, bad, struct.pack("@i", 4), 1, None) == loco.ERR_ARG
+    assert L.loco_router_backward(layer.Router(8, 2).c(), 4, PTR, 8, None, PTR, PTR, None, None, PTR, 0, None) == loco.ERR_ARG
+
+
 # ---- differentiable forms, with plain torch in the place of the kernels
 
 @pytest.fixture
