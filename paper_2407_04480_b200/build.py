@@ -61,6 +61,19 @@ def stale(lib: str = LIB, deps=DEPS) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def binding_for() -> str:
+    """What the binding is built for: it loads with this torch and interpreter only."""
+    from importlib.metadata import version
+    return "built for torch %s, python %d.%d" % (version("torch"), *sys.version_info[:2])
+
+
+def stale_binding() -> bool:
+    if stale(BINDING, BINDING_DEPS):
+        return True
+    with open(BINDING, "rb") as f:                       # its docstring
+        return binding_for().encode() not in f.read()
+
+
 def build_binding() -> None:
     """The Python module that marshals layer.py's calls, linked against the layer library and torch."""
     import torch
@@ -68,7 +81,7 @@ def build_binding() -> None:
     tmp = BINDING + ".tmp.%d" % os.getpid()
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-I" + os.path.join(home, "include"),
                            "-I" + os.path.join(home, "include", "torch", "csrc", "api", "include"), "-I" + os.path.join(cuda, "include"),
-                           "-I" + sysconfig.get_paths()["include"], BINDING_DEPS[0], "-o", tmp, "-L" + HERE, "-lloco_layer_b200",
+                           "-I" + sysconfig.get_paths()["include"], '-DLOCO_BUILT_FOR="%s"' % binding_for(), BINDING_DEPS[0], "-o", tmp, "-L" + HERE, "-lloco_layer_b200",
                            "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, BINDING)
 
@@ -80,7 +93,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         wanted.append((LIB, units()))
     if force or stale(LAYER_LIB, LAYER_DEPS):
         wanted.append((LAYER_LIB, [(s[:-3], s, []) for s in LAYER_SOURCES]))
-    binding = force or stale(BINDING, BINDING_DEPS)
+    binding = force or stale_binding()
     if not wanted:
         if binding:
             build_binding()

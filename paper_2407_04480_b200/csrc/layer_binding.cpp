@@ -280,7 +280,7 @@ template <int (*kCall)(PyObject *const *), int kArgs> PyObject *entry(PyObject *
 #define LOCO_ENTRY(name, args) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(entry<name, args>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LOCO_ENTRY(rotary_apply, 9), LOCO_ENTRY(attention_forward, 14), LOCO_ENTRY(attention_backward, 19),
                          LOCO_ENTRY(router_forward, 14), LOCO_ENTRY(router_backward, 13), {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layer_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layer_binding", LOCO_BUILT_FOR, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

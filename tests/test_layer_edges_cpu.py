@@ -63,6 +63,15 @@ def test_outputs_that_repeat_memory_are_refused(zero):
     assert L.loco_router_backward(layer.Router(8, 2).c(), 4, PTR, 8, None, PTR, PTR, None, None, PTR, 0, None) == loco.ERR_ARG
 
 
+def test_a_binding_of_another_torch_is_out_of_date(monkeypatch):
+    """It needs that torch's libraries; the sources alone would not show it."""
+    import importlib.metadata as metadata
+    assert not loco_build.stale_binding()
+    real = metadata.version
+    monkeypatch.setattr(metadata, "version", lambda name: "99.0" if name == "torch" else real(name))
+    assert loco_build.stale_binding()
+
+
 # ---- differentiable forms, with plain torch in the place of the kernels
 
 @pytest.fixture
