@@ -217,7 +217,7 @@ class _Rotary(torch.autograd.Function):
     def forward(ctx, q, k, table, positions, layout, inverse):
         ctx.save_for_backward(table, positions)
         ctx.how = (layout, inverse)
-        qo, ko = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
+        qo, ko = (None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k))
         loco_rotary_apply(table, q, k, qo, ko, positions=positions, layout=layout, inverse=inverse)
         return qo, ko
 
@@ -226,11 +226,12 @@ class _Rotary(torch.autograd.Function):
         table, positions = ctx.saved_tensors
         layout, inverse = ctx.how
         # contiguous: also a broadcast gradient gets memory of its own
-        return (*_Rotary.apply(dq.contiguous(), dk.contiguous(), table, positions, layout, not inverse), None, None, None, None)
+        dq, dk = (None if t is None else t.contiguous() for t in (dq, dk))
+        return (*_Rotary.apply(dq, dk, table, positions, layout, not inverse), None, None, None, None)
 
 
 def rotary(q, k, table, positions=None, layout: str = "half"):
-    """Rotated queries and keys [batch, seq, heads, dim]."""
+    """Rotated queries and keys [batch, seq, heads, dim]; k may be None, and is then None in the result."""
     return _Rotary.apply(q, k, table, positions, layout, False)
 
 

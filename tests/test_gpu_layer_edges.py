@@ -342,3 +342,22 @@ def test_rotary_and_router_of_expanded_operands():
     z, cfg = normal(g, 1, 40).expand(33, 40), layer.Router(40, 3, z_coef=0.1)
     for a, b in zip(layer.router(z, cfg), layer.router(z.contiguous(), cfg)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("where", [torch.int32, torch.int64])
+def test_differentiable_rotary_with_positions_and_without_keys(layout, where):
+    g = gen(91)
+    table = torch.empty(70, 24, device="cuda")
+    layer.loco_rotary_table(table, magnitude=1.1)
+    q, k = normal(g, 2, 30, 3, 32).requires_grad_(), normal(g, 2, 30, 1, 32).requires_grad_()
+    at = torch.randint(0, 70, (2, 30), generator=g, device="cuda", dtype=where)
+    y, z = layer.rotary(q, k, table, positions=at, layout=layout)
+    w = normal(g, 2, 30, 3, 32)
+    got, zero = torch.autograd.grad(y, (q, k), w, allow_unused=True)
+    want_y, want = torch.empty_like(w), torch.empty_like(w)
+    layer.loco_rotary_apply(table, q.detach(), None, want_y, None, positions=at, layout=layout)
+    layer.loco_rotary_apply(table, w, None, want, None, positions=at, layout=layout, inverse=True)
+    assert torch.equal(y, want_y) and torch.equal(got, want) and (zero is None or not zero.any())
+    alone, none = layer.rotary(q, None, table, positions=at, layout=layout)
+    assert none is None and torch.equal(alone, y) and torch.equal(torch.autograd.grad(alone, q, w)[0], want)

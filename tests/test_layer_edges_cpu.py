@@ -214,3 +214,11 @@ def test_differentiable_attention_takes_no_other_argument(kernels, name):
     with pytest.raises(TypeError):
         layer.attention(q, k, v, **{name: None})
     assert not kernels
+
+
+def test_rotary_takes_queries_alone(kernels):
+    q = torch.randn(1, 4, 2, 8, requires_grad=True)
+    y, none = layer.rotary(q, None, torch.zeros(4, 8))
+    assert none is None and torch.equal(y, 2 * q)
+    grad, = torch.autograd.grad(y, q, torch.ones_like(y))
+    assert torch.equal(grad, torch.full_like(q, 2.0)) and [c[1][2] for c in kernels] == [None, None]
