@@ -76,6 +76,12 @@ void *flat(PyObject *o, at::IntArrayRef shape, ScalarType type, int device, cons
     return t->data_ptr();
 }
 
+// The tokens that take part: a byte each, of truth values or of numbers.
+uint8_t *mask_of(PyObject *o, int64_t tokens, int device) {
+    const at::Tensor *t = tensor(o, "mask");
+    return static_cast<uint8_t *>(flat(o, {tokens}, t && t->scalar_type() == ScalarType::Bool ? ScalarType::Bool : ScalarType::Byte, device, "mask"));
+}
+
 int32_t small(int64_t x, const char *what) {
     if (x < 0 || x > 0x7fffffff) refuse(std::string("too large: ") + what);
     return static_cast<int32_t>(x);
@@ -239,7 +245,7 @@ int router_forward(PyObject *const *a) {
     const at::Tensor &work = need(a[11], "work");
     if (!work.is_cuda() || work.get_device() != r.device || !work.is_contiguous()) refuse("the workspace must be a contiguous tensor on the operands' device");
     const int64_t n = r.tokens, k = r.cfg.top_k, e = r.cfg.experts;
-    return loco_router_forward(&r.cfg, n, r.at, r.stride, static_cast<uint8_t *>(flat(a[12], {n}, ScalarType::Byte, r.device, "mask")),
+    return loco_router_forward(&r.cfg, n, r.at, r.stride, mask_of(a[12], n, r.device),
                                static_cast<int32_t *>(flat(a[6], {n, k}, ScalarType::Int, r.device, "index")),
                                static_cast<float *>(flat(a[7], {n, k}, ScalarType::Float, r.device, "weight")),
                                static_cast<int32_t *>(flat(a[8], {e + 1}, ScalarType::Int, r.device, "counts")),
@@ -254,7 +260,7 @@ int router_backward(PyObject *const *a) {
     const Rows r = rows(logits, a, "logits"), d = rows(dlogits, a, "dlogits");
     if (d.tokens != r.tokens || dlogits.scalar_type() != logits.scalar_type()) refuse("dlogits must have the logits' shape and type");
     const int64_t n = r.tokens, k = r.cfg.top_k, e = r.cfg.experts;
-    return loco_router_backward(&r.cfg, n, r.at, r.stride, static_cast<uint8_t *>(flat(a[9], {n}, ScalarType::Byte, r.device, "mask")),
+    return loco_router_backward(&r.cfg, n, r.at, r.stride, mask_of(a[9], n, r.device),
                                 static_cast<int32_t *>(flat(a[6], {n, k}, ScalarType::Int, r.device, "index")),
                                 static_cast<int32_t *>(flat(a[7], {e + 1}, ScalarType::Int, r.device, "counts")),
                                 static_cast<float *>(flat(a[10], {2}, ScalarType::Float, r.device, "dlosses")),

@@ -184,7 +184,7 @@ def loco_router_workspace_bytes(cfg: Router) -> int:
 def loco_router_forward(cfg: Router, logits, index, weight, counts, mean, losses, work, mask=None, stream=None) -> None:
     """Choice, weights, counts and losses of logits [tokens, experts]; see include/loco_layer.h for the outputs.
 
-    work: a CUDA tensor of loco_router_workspace_bytes() bytes, zero before its first use."""
+    mask: uint8 or bool [tokens]; work: a CUDA tensor of loco_router_workspace_bytes() bytes, zero before its first use."""
     _check(_binding().router_forward(cfg.experts, cfg.top_k, cfg.normalize, cfg.balance_coef, cfg.z_coef, logits, index, weight,
                                      counts, mean, losses, work, mask, _raw(stream)), "loco_router_forward")
 

@@ -361,3 +361,24 @@ def test_differentiable_rotary_with_positions_and_without_keys(layout, where):
     assert torch.equal(y, want_y) and torch.equal(got, want) and (zero is None or not zero.any())
     alone, none = layer.rotary(q, None, table, positions=at, layout=layout)
     assert none is None and torch.equal(alone, y) and torch.equal(torch.autograd.grad(alone, q, w)[0], want)
+
+
+@pytest.mark.parametrize("e,dtype", [(8, BF), (160, F32)])
+def test_router_mask_of_truth_values_is_one_of_bytes(e, dtype):
+    """Both directions, in the differentiable form; the masked tokens' logits may hold anything."""
+    g = gen(92)
+    z = normal(g, 90, e, dtype=dtype)
+    mask = torch.rand(90, generator=g, device="cuda") < 0.6
+    z[~mask] = float("nan")
+    cfg, results = layer.Router(e, 2, balance_coef=0.3, z_coef=0.1), []
+    for m in (mask, mask.to(torch.uint8) * 5):
+        x = z.clone().requires_grad_()
+        index, weight, counts, mean, losses = layer.router(x, cfg, mask=m)
+        grad, = torch.autograd.grad(losses.sum() + (weight * torch.arange(2, device="cuda")).sum(), x)
+        results.append((index, weight, counts, mean, losses, grad))
+        assert int(counts[e]) == int(mask.sum()) and (index[~mask] == -1).all() and not weight[~mask].any()
+        assert bool(losses.isfinite().all()) and not grad[~mask].any() and bool(grad[mask].any(1).all())
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    for bad in (mask[:89], mask.float(), torch.ones(180, dtype=torch.bool, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            layer.router(z, cfg, mask=bad)
