@@ -110,6 +110,8 @@ def run(shape: Shape = Shape(), steps: int = 8, workers: int = 2, batch: int = 2
         loco.loco_unpack_dequant_reduce_adam(cfg, comms, n, *moments, theta, lr=lr, beta1=0.1, beta2=0.01, delta=1e-12)
         history.append(total)
         report("step %d: loss %.4f, idle experts over all workers %d" % (k, total, idle))
+    if layer.loco_layer_status() & layer.FLAG_TIMEOUT:                # an attention kernel gave up: its outputs mean nothing
+        raise RuntimeError("a wait of an attention kernel ran out: the steps' results are meaningless")
     return history
 
 

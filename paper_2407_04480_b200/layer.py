@@ -94,7 +94,10 @@ def loco_layer_launch_count() -> int:
 
 
 def loco_layer_status(stream=None) -> int:
-    """Flags raised on the current device since the library was loaded; synchronises the stream."""
+    """Flags raised on the current device since the library was loaded; synchronises the stream.
+
+    FLAG_TIMEOUT: a wait in an attention kernel ran out and that call's outputs are meaningless.  Nothing else reads the
+    flag: a program asks where it synchronises anyway, once a step or a checkpoint."""
     flags = C.c_uint32(0)
     _check(lib().loco_layer_status(C.byref(flags), (torch.cuda.current_stream() if stream is None else stream).cuda_stream),
            "loco_layer_status")

@@ -382,3 +382,15 @@ def test_router_mask_of_truth_values_is_one_of_bytes(e, dtype):
     for bad in (mask[:89], mask.float(), torch.ones(180, dtype=torch.bool, device="cuda")[::2]):
         with pytest.raises(ValueError):
             layer.router(z, cfg, mask=bad)
+
+
+def test_training_stops_where_a_wait_has_run_out(monkeypatch):
+    import sys
+    monkeypatch.syspath_prepend(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    sys.modules.pop("decoder_layer_step", None)
+    import decoder_layer_step
+    how = dict(steps=1, workers=1, batch=1, seq=40, report=lambda *_: None)
+    assert len(decoder_layer_step.run(**how)) == 1 and layer.loco_layer_status() == 0
+    monkeypatch.setattr(layer, "loco_layer_status", lambda: layer.FLAG_TIMEOUT)
+    with pytest.raises(RuntimeError, match="ran out"):
+        decoder_layer_step.run(**how)
