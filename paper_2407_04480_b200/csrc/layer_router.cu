@@ -204,7 +204,8 @@ __device__ void finish(const RouterParams &P, const float *sums, const int *tall
         for (int w = 0; w < threads / 32; ++w) all += fold[w];
         P.counts[E] = n;
         P.losses[0] = static_cast<float>(static_cast<double>(P.balance_coef) * E * all * per / P.top_k);
-        P.losses[1] = static_cast<float>(static_cast<double>(P.z_coef) * zz * per);
+        // logits of the type's lowest value have squares past fp32: infinite in the sum, and nothing without a coefficient
+        P.losses[1] = P.z_coef == 0.0f && zz == INFINITY ? 0.0f : static_cast<float>(static_cast<double>(P.z_coef) * zz * per);
     }
 }
 

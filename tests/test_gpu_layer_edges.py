@@ -394,3 +394,31 @@ def test_training_stops_where_a_wait_has_run_out(monkeypatch):
     monkeypatch.setattr(layer, "loco_layer_status", lambda: layer.FLAG_TIMEOUT)
     with pytest.raises(RuntimeError, match="ran out"):
         decoder_layer_step.run(**how)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("e", [8, 40, 160, 512])
+def test_router_token_whose_logits_are_all_the_lowest_value(e, dtype):
+    """It takes part with equal probabilities; without a coefficient its z loss is zero, not zero times an overflow."""
+    z = normal(gen(95), 12, e, dtype=dtype)
+    z[5] = torch.finfo(dtype).min
+    for coef, want in ((0.0, 0.0), (1e-3, math.inf)):            # lse^2 is 1e77 for that token
+        x = z.clone().requires_grad_()
+        index, weight, counts, mean, losses = layer.router(x, layer.Router(e, 2, balance_coef=0.3, z_coef=coef))
+        assert index[5].tolist() == [0, 1] and weight[5].tolist() == [0.5, 0.5] and int(counts[e]) == 12
+        assert math.isfinite(float(losses.detach()[0])) and float(losses.detach()[1]) == want
+        grad, = torch.autograd.grad(losses[0] + weight[:, 0].sum(), x)
+        assert bool(grad.isfinite().all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("packed", [False, True])
+def test_attention_without_queries_or_without_keys(d, packed):
+    g, lead = gen(96), (lambda n: (n,) if packed else (1, n))
+    for nq, nk in ((0, 30), (30, 0), (0, 0)):
+        q, k, v = (normal(g, *lead(n), 2, d).requires_grad_() for n in (nq, nk, nk))
+        cu = lambda n: torch.tensor([0, n], device="cuda", dtype=torch.int32)
+        o = layer.attention(q, k, v, causal=True, **(dict(cu_q=cu(nq), cu_k=cu(nk), max_q=nq, max_k=nk) if packed else {}))
+        assert o.shape == q.shape and not o.any()
+        for t, grad in zip((q, k, v), torch.autograd.grad(o, (q, k, v), torch.ones_like(o))):
+            assert grad.shape == t.shape and not grad.any()
