@@ -982,8 +982,16 @@ bool make_map(CUtensorMap &map, const Heads &t, int batch, int heads, int rows, 
     const auto stride = [&](int64_t s, cuuint64_t n) { return static_cast<cuuint64_t>(n == 1 ? 256 : s * 2); };
     const cuuint64_t strides[3] = {stride(t.row_stride, size[1]), stride(t.head_stride, size[2]), stride(t.batch_stride, size[3])};
     const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1}, step[4] = {1, 1, 1, 1};
-    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, at, size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const auto made = [&] {
+        return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, at, size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    if (made()) return true;
+    // Unlike a launch the encoding binds no context to the calling thread, and needs one: a thread's first call binds it.
+    int dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess) return made();
+    cudaGetLastError();
+    return false;
 }
 
 using Kernel = void (*)(const AttentionParams, const Maps);

@@ -422,3 +422,40 @@ def test_attention_without_queries_or_without_keys(d, packed):
         assert o.shape == q.shape and not o.any()
         for t, grad in zip((q, k, v), torch.autograd.grad(o, (q, k, v), torch.ones_like(o))):
             assert grad.shape == t.shape and not grad.any()
+
+
+def test_attention_from_a_thread_that_has_not_touched_the_device():
+    """Autograd's own thread is one where the backward call is the first of a program: no context is bound to it yet."""
+    import threading
+    g = gen(97)
+    q, k, v, do = (normal(g, 1, 40, 2, 64) for _ in range(4))
+    o, lse, grads = torch.zeros_like(q), torch.zeros(1, 2, 40, device="cuda"), [torch.zeros_like(q) for _ in range(3)]
+    work = torch.zeros(layer.loco_attention_backward_workspace_bytes(q, k), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    calls = (lambda: layer.loco_attention_forward(q, k, v, o, lse),
+             lambda: layer.loco_attention_backward(q, k, v, o, lse, do, *grads, work))
+    for call in calls:
+        failed = []
+
+        def run():
+            try:
+                call()
+            except Exception as e:
+                failed.append(e)
+        t = threading.Thread(target=run)
+        t.start()
+        t.join()
+        assert not failed, failed
+    want = run_attention(q, k, v, do, False)
+    assert all(torch.equal(a, b) for a, b in zip((o, lse, *grads), want))
+
+
+def test_attention_gradient_as_the_first_backward_pass_of_a_program():
+    import subprocess
+    import sys
+    code = ("import torch; from paper_2407_04480_b200 import layer; "
+            "q = torch.ones(1, 16, 2, 64, device='cuda', dtype=torch.bfloat16).requires_grad_(); g = torch.ones_like(q); "
+            "print(float(torch.autograd.grad(layer.attention(q, q.detach(), q.detach()), q, g)[0].abs().max()))")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
+    assert out.returncode == 0 and float(out.stdout) == 0.0, out.stderr[-500:]          # all keys alike
