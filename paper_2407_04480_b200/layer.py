@@ -214,15 +214,24 @@ class _Gradient(torch.autograd.Function):
         raise RuntimeError("layer.%s can be differentiated once: its gradient has no gradient" % ctx.name)
 
 
+def _gradient(name, compute, *tensors):
+    """compute(*tensors), as a node only where a graph of the backward pass is wanted: a node costs some 10 us on the host."""
+    return _Gradient.apply(name, compute, *tensors) if torch.is_grad_enabled() else compute(*tensors)
+
+
+def _rotate(q, k, table, positions, layout, inverse):
+    qo, ko = (None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k))
+    loco_rotary_apply(table, q, k, qo, ko, positions=positions, layout=layout, inverse=inverse)
+    return qo, ko
+
+
 class _Rotary(torch.autograd.Function):
     """Linear in q and k: the gradient is the transposed rotation, which is differentiable in turn."""
     @staticmethod
     def forward(ctx, q, k, table, positions, layout, inverse):
         ctx.save_for_backward(table, positions)
         ctx.how = (layout, inverse)
-        qo, ko = (None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k))
-        loco_rotary_apply(table, q, k, qo, ko, positions=positions, layout=layout, inverse=inverse)
-        return qo, ko
+        return _rotate(q, k, table, positions, layout, inverse)
 
     @staticmethod
     def backward(ctx, dq, dk):
@@ -230,7 +239,8 @@ class _Rotary(torch.autograd.Function):
         layout, inverse = ctx.how
         # contiguous: also a broadcast gradient gets memory of its own
         dq, dk = (None if t is None else t.contiguous() for t in (dq, dk))
-        return (*_Rotary.apply(dq, dk, table, positions, layout, not inverse), None, None, None, None)
+        turn = _Rotary.apply if torch.is_grad_enabled() else _rotate
+        return (*turn(dq, dk, table, positions, layout, not inverse), None, None, None, None)
 
 
 def rotary(q, k, table, positions=None, layout: str = "half"):
@@ -261,7 +271,7 @@ class _Attention(torch.autograd.Function):
             work = torch.empty(loco_attention_backward_workspace_bytes(q, k, lens["cu_q"], lens["cu_k"], **longest), dtype=torch.uint8, device=q.device)
             loco_attention_backward(q, k, v, o, lse, do, dq, dk, dv, work, causal=causal, scale=scale, **lens, **longest)
             return dq, dk, dv
-        return (*_Gradient.apply("attention", compute, *ctx.saved_tensors, do), None, None, None, None)
+        return (*_gradient("attention", compute, *ctx.saved_tensors, do), None, None, None, None)
 
 
 def attention(q, k, v, causal: bool = False, scale: Optional[float] = None, len_q=None, len_k=None, cu_q=None, cu_k=None,
@@ -292,7 +302,7 @@ class _Router(torch.autograd.Function):
             loco_router_backward(ctx.cfg, logits, index, counts, dlogits, mask=mask, dlosses=dlosses.contiguous(),
                                  dweights=dweight.contiguous())
             return dlogits
-        return _Gradient.apply("router", compute, *ctx.saved_tensors, dweight, dlosses), None, None, None
+        return _gradient("router", compute, *ctx.saved_tensors, dweight, dlosses), None, None, None
 
 
 def router(logits, cfg: Router, mask=None, work: Optional[torch.Tensor] = None):
