@@ -459,3 +459,33 @@ def test_attention_gradient_as_the_first_backward_pass_of_a_program():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
     assert out.returncode == 0 and float(out.stdout) == 0.0, out.stderr[-500:]          # all keys alike
+
+
+def test_differentiable_forms_are_captured_into_a_graph():
+    """Forward and backward of the three forms in one graph, replayed on other inputs."""
+    g = gen(98)
+    table = torch.empty(200, 64, device="cuda")
+    layer.loco_rotary_table(table)
+    cfg = layer.Router(8, 2, balance_coef=0.1, z_coef=0.01)
+    work = torch.zeros(layer.loco_router_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    q, k, v = (normal(g, 2, 200, h, 64).requires_grad_() for h in (4, 2, 2))
+    w = normal(g, 256, 8, dtype=F32)
+
+    def step():
+        o = layer.attention(*layer.rotary(q, k, table), v, causal=True)
+        _, weight, _, _, losses = layer.router(o.flatten(2).flatten(0, 1).float() @ w, cfg, work=work)
+        return torch.autograd.grad(losses.sum() + (weight[:, 0] * o.float().mean((2, 3)).flatten()).sum(), (q, k, v))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(2):
+        with torch.no_grad():
+            for t in (q, k, v):
+                t.copy_(normal(g, *t.shape))
+        graph.replay()
+        assert all(torch.equal(a, b) and bool(a.any()) for a, b in zip(got, step()))
