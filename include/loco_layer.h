@@ -90,7 +90,8 @@ int loco_rotary_apply(const loco_rotary_t *cfg, const float *d_table, const void
  *              dq_i = scale * sum_j ds_ij k_j,  dk_j = scale * sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i
  * bf16 heads, fp32 statistics.  Query head h reads key head h / (heads_q / heads_kv); the gradients of a shared key head
  * are summed over its query heads.  A query that sees no key has o = 0, lse = -inf and no gradient; one whose scores are all
- * -inf has o = 0 and lse = -inf.  A score of +inf or NaN makes its query's o NaN (lse: +inf or NaN).
+ * -inf has o = 0 and lse = -inf.  A score of +inf or NaN makes its query's o NaN (lse: +inf or NaN).  Keys and values that
+ * only the causal mask hides have to be finite: zero times what they hold is added where they share a tile.
  */
 typedef struct {
     int32_t batch, heads_q, heads_kv;   /* heads_kv divides heads_q, batch * heads_q < 2^31                     */

@@ -1,12 +1,13 @@
 // Attention on the tensor cores: tiles of 128 rows that stay, tiles of 80, 96 or 128 that stream, products accumulated in
-// tensor memory (TMEM).  4096 tokens, 32 heads of 128, not causal: forward 236 us (1166 TFLOP/s), backward 714 us (the
-// seven products it executes: 1347 TFLOP/s); the tensor pipe, 68 to 73% busy while an SM is active, bounds each.
+// tensor memory (TMEM).  1 x 4096 tokens, 32 heads of 128, not causal, calls in a row: forward 233 us (1180 TFLOP/s),
+// backward 713 us (the seven products it executes: 1350 TFLOP/s); the tensor pipe, 68 to 72% busy while an SM is active,
+// bounds each.
 //
 // All three kernels have the same parts.  One warp copies tiles to shared memory (TMA, 128-byte swizzle), one thread issues
 // the products, two groups of four warps turn scores into probabilities (a thread per TMEM lane, i.e. per row), and one warp
 // zeroes what a copy brought in from past the end of a sample, so that whatever lies there (NaN included) meets a zero
-// probability as a zero.  Probabilities go back to TMEM as bfloat16 over the scores they came from and are the first operand
-// of the second product from there: they never pass through shared memory.
+// probability as a zero.  Probabilities and their gradients go back to TMEM as bfloat16 (P to a place of its own, dS over dP)
+// and are the first operand of the second product from there: they never pass through shared memory.
 //
 //   forward           two tiles of 128 queries stay, keys and values stream; one warp group per query tile, so that one
 //                     group's exponentials run under the other tile's products.  The running maximum is moved (and o
@@ -19,9 +20,6 @@
 //                     of the five that a single kernel with atomic dq would need.
 #include <cuda.h>
 
-#include <cstring>
-#include <mutex>
-
 #include "layer_attention.h"
 #include "layer_tc.cuh"
 
@@ -33,9 +31,9 @@ constexpr int kTile = 128;                       // queries and keys of a tile
 constexpr int kGroupWarps = 4;                   // warps of a softmax group: the 128 lanes of TMEM
 constexpr int kThreads = 3 * kGroupWarps * 32;   // two softmax groups and one of single warps, the last of which idles
 constexpr int kLoadWarp = 2 * kGroupWarps, kProductWarp = kLoadWarp + 1, kHelpWarp = kLoadWarp + 2;
-// Of so many pairs of scores one goes through exp2_poly.  Forward, 4096, 32 heads: none 258 us, one in eight 254, in four 252,
-// in three 253, in two 276.  Backward over keys 435, 416, 419 with none, one in eight, in four; over queries (causal) 359,
-// 347, 350.
+// Of so many pairs of scores one goes through exp2_poly.  Forward with none, one in eight, in four, in three: 4 x 2048, 16
+// heads of 64: 138, 139, 132, 143 us; 1 x 4096, 32 heads of 128: 231, 232, 233, 235.  Backward with none, one in eight, in
+// four: 404, 392, 400 and 716, 713, 720 us.
 constexpr int kPolyForward = 4, kPolyBackward = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -271,15 +269,15 @@ __device__ __forceinline__ float row_max(const uint32_t (&s)[16]) {
 // TMEM without a place of its own for P, and the next scores would wait for the product with the values (measured at 4096,
 // 32 heads: 252 us).
 template <int kDim> __host__ __device__ constexpr int key_tile() { return kDim == 128 ? 80 : 128; }
-template <int kDim> __host__ __device__ constexpr int forward_slots() { return 8; }
+constexpr int kForwardSlots = 8;
 template <int kDim> constexpr int forward_bytes() {
-    return 2 * tile_bytes<kDim>() + forward_slots<kDim>() * key_tile<kDim>() * kDim * 2 + static_cast<int>(sizeof(Shared));
+    return 2 * tile_bytes<kDim>() + kForwardSlots * key_tile<kDim>() * kDim * 2 + static_cast<int>(sizeof(Shared));
 }
 static_assert(forward_bytes<128>() <= 227 * 1024 && forward_bytes<64>() <= 227 * 1024, "shared memory of a block");
 
 template <int kDim>
 __global__ void __launch_bounds__(kThreads, 1) attention_forward_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ Maps M) {
-    constexpr int kSlots = forward_slots<kDim>(), kBytes = tile_bytes<kDim>(), kKeys = key_tile<kDim>(), kStep = kKeys * kDim * 2;
+    constexpr int kSlots = kForwardSlots, kBytes = tile_bytes<kDim>(), kKeys = key_tile<kDim>(), kStep = kKeys * kDim * 2;
     extern __shared__ __align__(1024) uint8_t tiles[];
     Shared &S = *reinterpret_cast<Shared *>(tiles + 2 * kBytes + kSlots * kStep);
     const uint32_t base = smem_addr(tiles), ring = base + 2 * kBytes;
@@ -1014,9 +1012,11 @@ bool allow(Kernel fn, int which, int bytes) {
 }
 
 // Without a causal mask blocks are alike, and heads come in spans whose streams stay in L2 (126 MB, whose halves may hold the
-// same lines): with all heads at once 4096 rows of 32 heads were read from HBM three times over (backward 725 us; in spans of
-// 20 MB 695, of 40 MB 700, of 70 MB 727).  Under a causal mask the longest blocks of all heads have to come first: one span
-// (1 x 8192, 32 heads, backward 1467 us; in spans of 20 MB 1565, the grid ending in long blocks).
+// same lines): with all heads at once 4096 rows of 32 heads were read from HBM three times over.  Backward in spans of 20 MB,
+// of 40 MB, all at once: 1 x 4096, 32 heads of 128: 706, 712, 747 us; 2 x 4096, 32 over 8 of 128: 1489, 1506, 1540; 8 x 2048,
+// 16 of 64: 711, 702, 722; 1 x 16384, 16 of 64: 4008, 4010, 4090; 4 x 1536, 64 over 8 of 128: 922, 917, 940; spans of 5 MB
+// stay within 2% of 20.  Under a causal mask the longest blocks of all heads have to come first: one span (1 x 8192, 32 heads,
+// backward 1467 us; in spans of 20 MB 1565, the grid ending in long blocks).
 constexpr int64_t kSpanBytes = 20ll << 20;
 
 // A launch, checked as far as the host can: nothing of a call is launched before all of it is.  `stream_bytes`: what the blocks

@@ -59,9 +59,6 @@ __device__ __forceinline__ void fence_bar_init() { asm volatile("fence.mbarrier_
 
 // ---- tensor copies ---------------------------------------------------------------------------
 
-__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-}
 // A box of `map` at (x, row, head, batch) to shared memory; completes on `bar`.
 __device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap *map, int x, int row, int head, int batch, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"

@@ -141,7 +141,8 @@ def loco_attention_forward(q, k, v, o, lse, causal: bool = False, scale: Optiona
 
     Padded: q, o [batch, seq_q, heads, dim], k, v [batch, seq_k, heads_kv, dim], lse fp32 [batch, heads, seq_q], lengths
     len_q, len_k int32 [batch] (None: seq).  Packed: q, o [rows_q, heads, dim], k, v [rows_k, heads_kv, dim], lse
-    [heads, rows_q], offsets cu_q, cu_k int32 [batch + 1], max_q, max_k the longest sample.  scale: None = 1/sqrt(dim)."""
+    [heads, rows_q], offsets cu_q, cu_k int32 [batch + 1] that ascend from 0 to rows_q and rows_k (rows outside every sample are
+    not written), max_q, max_k the longest sample.  scale: None = 1/sqrt(dim)."""
     _check(_binding().attention_forward(q, k, v, o, lse, causal, scale, len_q, len_k, cu_q, cu_k, max_q, max_k, _raw(stream)),
            "loco_attention_forward")
 
