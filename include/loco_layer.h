@@ -9,7 +9,12 @@
  *   attention   softmax attention forward (o and the log-sum-exp of every row) and backward, which recomputes the
  *               probabilities; grouped heads, causal, padded or packed samples;
  *   router      the top-k router of a mixture of experts: chosen experts and weights, per-expert counts, balance and
- *               z loss, and their gradient.  An expert whose count is zero has an all-zero gradient segment.
+ *               z loss, and their gradient.  An expert whose count is zero has an all-zero gradient segment;
+ *   norm        root-mean-square norm with the residual's addition, its output in the type of the heads or in 8 bits
+ *               with scales, and its gradient;
+ *   experts     the router's choices sorted by expert, tokens laid out in that order and summed back with their weights,
+ *               the product of every expert's rows with its matrix, and all their gradients;
+ *   gradient    the sum of squares of a list of gradients, and the list scaled down to a largest norm.
  *
  * The conventions are those of loco.h: d_* are DEVICE pointers owned by the caller, `stream` is a cudaStream_t, work
  * is asynchronous, nothing allocates or synchronises unless stated, every call returns a loco_status_t and launches
@@ -165,10 +170,142 @@ int loco_router_backward(const loco_router_t *cfg, int64_t tokens, const void *d
                          const uint8_t *d_mask, const int32_t *d_index, const int32_t *d_counts, const float *d_dlosses,
                          const float *d_dweight, void *d_dlogits, int64_t drow_stride, void *stream);
 
+/* ---- norm ----------------------------------------------------------------------------------
+ *   h = x + residual, rounded to the type of x (no residual: h = x)
+ *   r = 1 / sqrt(mean_i h_i^2 + eps)         y_i = h_i r w_i   (no weight: w = 1)
+ *   8 bits: per row, or per run of `block` columns of a row,  scale = max(max_i |y_i| / 448, 2^-126),  y_i / scale as e4m3
+ *   backward, from h:  g = dy w,  n = h r:   dx = r (g - n mean(g n)) + dtotal,   dw = sum over rows of dy n
+ * dx is the gradient of x and of the residual alike; dtotal is the one that reaches h past the norm.  Through the 8-bit
+ * output it is passed as if nothing had been rounded.  The norm is that of h as it is kept, so that y of a kept h has the
+ * same bits.  Squares are summed in fp32.  A row with NaN or an infinity has NaN in y there; its 8-bit scale is NaN.
+ */
+typedef struct {
+    void   *ptr;             /* element (t, i) of a [rows, dim] tensor lies at ptr + t*row_stride + i             */
+    int64_t row_stride;      /* in elements; ignored with one row, zero repeats an input, >= dim in an output     */
+} loco_rows_t;
+
+typedef struct {
+    int32_t dtype;           /* loco_dtype_t of x, residual, h, weight, y and their gradients                     */
+    int32_t dim;             /* 1 .. 16384                                                                        */
+    int32_t bits8;           /* forward: y is e4m3 with scales                                                    */
+    int32_t block;           /* with bits8: columns that share a scale, 0 (the whole row) or 128                  */
+    float   eps;             /* >= 0                                                                              */
+} loco_norm_t;
+
 /*
- * Flags raised on the current device since the library was loaded; SYNCHRONISES `stream`.  The attention kernels wait on
- * their own copies and products, never on another block; a wait that exceeds two seconds gives up, the outputs of its
- * block are meaningless and the flag is raised.
+ *   residual, weight    NULL: none                    total   h; needed with a residual, NULL without: it would be x
+ *   d_scale             with bits8: fp32 [rows, ceil(dim / block)], one a row with block = 0
+ * total may be x or the residual itself, with its stride; y may too, without bits8 and where total is not there as well.
+ * One launch.  Errors: ARG, ALIGN, CUDA.
+ */
+int loco_norm_forward(const loco_norm_t *cfg, int64_t rows, const loco_rows_t *x, const loco_rows_t *residual, const void *d_weight,
+                      const loco_rows_t *total, const loco_rows_t *y, float *d_scale, void *stream);
+
+/* Bytes of device memory loco_norm_backward needs for the gradient of the weight. */
+uint64_t loco_norm_backward_workspace_bytes(const loco_norm_t *cfg);
+
+/*
+ *   h        what the norm was taken of               dtotal    NULL: none
+ *   d_dweight  NULL: not wanted (d_work may be NULL then); else [dim], the type of x.  d_work: 16-byte aligned, contents
+ *              irrelevant before and after.
+ * dx may be dy or dtotal itself, with its stride.  No atomics on values: the same inputs give the same bits.  One launch, two
+ * with d_dweight.  Errors: ARG, ALIGN, SIZE, CUDA.
+ */
+int loco_norm_backward(const loco_norm_t *cfg, int64_t rows, const loco_rows_t *h, const loco_rows_t *dy, const void *d_weight,
+                       const loco_rows_t *dtotal, const loco_rows_t *dx, void *d_dweight, void *d_work, uint64_t d_work_bytes, void *stream);
+
+/* ---- experts -------------------------------------------------------------------------------
+ * Choices index [tokens, top_k] (the router's; outside 0 .. experts - 1: none) are sorted by expert, then token, then slot:
+ *   offsets[e]  first row of expert e, offsets[experts] the number of rows in use       place[t, j]  row of a choice, or -1
+ *   dispatch    rows[place[t, j]] = x[t]
+ *   combine     y[t] = sum_j weight[t, j] rows[place[t, j]]     (no weight: 1; no choice: nothing)
+ * Dispatch's gradient is combine without weights, combine's without weights is dispatch.  With weights:
+ *   drows[place[t, j]] = weight[t, j] dy[t]      dweight[t, j] = dy[t] . rows[place[t, j]]   (0 where there is no choice)
+ * Rows that no choice has are not written; a place outside the rows is none.  Sums in fp32, in the order of the slots.
+ */
+
+/* Device workspace of loco_experts_sort for any number of tokens (0 for a bad number of experts). */
+uint64_t loco_experts_sort_workspace_bytes(int32_t experts);
+
+/* d_index, d_place: int32 [tokens, top_k]; d_offsets: int32 [experts + 1]; experts 1 .. 512, tokens * top_k < 2^31.  d_work:
+ * 16-byte aligned, contents irrelevant before and after; calls that may run at the same time need workspaces of their own.
+ * One or two launches.  Errors: ARG, ALIGN, SIZE, CUDA. */
+int loco_experts_sort(int32_t experts, int64_t tokens, int32_t top_k, const int32_t *d_index, int32_t *d_offsets, int32_t *d_place,
+                      void *d_work, uint64_t d_work_bytes, void *stream);
+
+typedef struct {
+    int32_t dtype;           /* loco_dtype_t of the tokens and rows                       */
+    int32_t dim;             /* >= 1                                                      */
+    int32_t top_k;           /* 1 .. 16                                                   */
+    int64_t tokens;          /* tokens * top_k < 2^31                                     */
+    int64_t rows;            /* rows of the sorted tensors: places are below, < 2^31      */
+} loco_experts_t;
+
+/* x [tokens, dim], rows [rows, dim]; d_place, d_weight (fp32), d_dweight (fp32): [tokens, top_k].  No place may come twice in
+ * dispatch and combine_backward, which write it.  One launch each.  Errors: ARG, ALIGN, CUDA. */
+int loco_experts_dispatch(const loco_experts_t *cfg, const loco_rows_t *x, const int32_t *d_place, const loco_rows_t *rows, void *stream);
+int loco_experts_combine(const loco_experts_t *cfg, const loco_rows_t *rows, const int32_t *d_place, const float *d_weight,
+                         const loco_rows_t *y, void *stream);
+int loco_experts_combine_backward(const loco_experts_t *cfg, const loco_rows_t *dy, const loco_rows_t *rows, const int32_t *d_place,
+                                  const float *d_weight, const loco_rows_t *drows, float *d_dweight, void *stream);
+
+/* The experts' matrices, [experts, first, second]: element (e, i, j) at ptr + e*expert_stride + i*row_stride + j. */
+typedef struct {
+    void   *ptr;
+    int64_t expert_stride, row_stride;
+} loco_matrices_t;
+
+typedef struct {
+    int32_t experts;         /* 1 .. 512                                                                          */
+    int64_t rows;            /* of x and y, < 2^31; expert e has rows offsets[e] .. offsets[e + 1] - 1            */
+    int32_t d_in, d_out;     /* multiples of 8                                                                    */
+    int32_t transposed;      /* product: the matrices are [experts, d_out, d_in]; else [experts, d_in, d_out]     */
+} loco_product_t;
+
+/*
+ * y_t = x_t W_e, transposed: x_t W_e^T, for the rows t of every expert e; x [rows, d_in], y [rows, d_out]; bfloat16, fp32
+ * sums.  The gradient of x is the same call on dy with `transposed` the other way round (d_in and d_out change places).
+ * d_offsets: int32 [experts + 1], ascending; they are read on the device and clamped to the rows.  Rows outside every expert
+ * are neither read as numbers nor written.  A NaN or infinity in a row or matrix reaches that row's or expert's outputs only.
+ * One launch.  Errors: ARG, ALIGN (a pointer not 16-byte aligned or a stride not a multiple of 8 elements), UNSUPPORTED, CUDA.
+ */
+int loco_experts_product(const loco_product_t *cfg, const loco_rows_t *x, const loco_matrices_t *w, const int32_t *d_offsets,
+                         const loco_rows_t *y, void *stream);
+
+/* dw_e = sum over the rows t of expert e of a_t^T b_t; a [rows, d_in], b [rows, d_out], dw [experts, d_in, d_out]; an expert
+ * without rows gets zeros.  The gradient of the matrices: a = x, b = dy, or, where they are transposed, a = dy, b = x.
+ * `transposed` is ignored.  No atomics: the same inputs give the same bits.  One launch.  Errors: as loco_experts_product. */
+int loco_experts_product_weights(const loco_product_t *cfg, const loco_rows_t *a, const loco_rows_t *b, const int32_t *d_offsets,
+                                 const loco_matrices_t *dw, void *stream);
+
+/* ---- gradient ------------------------------------------------------------------------------
+ * Of a list of gradients g:   squares = sum over all elements of g^2 (64 bits),   norm = sqrt(squares),
+ *   out = c g  with  c = max_norm / norm where norm > max_norm, else 1   (a norm that is infinite: c = 0; NaN: c = NaN)
+ * Between the two calls the squares of the ranks that hold the other shards can be added.
+ */
+typedef struct {
+    const void *x;           /* n elements, any alignment to their own size                                       */
+    void       *y;           /* the same, or x itself; ignored by loco_gradient_squares                           */
+    uint64_t    n;
+    int32_t     dtype;       /* loco_dtype_t                                                                      */
+} loco_span_t;
+
+/* Device workspace of loco_gradient_squares for any list. */
+uint64_t loco_gradient_squares_workspace_bytes(void);
+
+/* d_squares: one double.  d_work: 16-byte aligned; its first 256 bytes must be zero before the first call, and every call
+ * leaves them zero; calls that may run at the same time need workspaces of their own.  The same list gives the same bits.
+ * One launch for every 768 spans.  Errors: ARG, ALIGN, SIZE, CUDA. */
+int loco_gradient_squares(const loco_span_t *spans, int32_t count, double *d_squares, void *d_work, uint64_t d_work_bytes, void *stream);
+
+/* d_norm: one fp32, or NULL.  max_norm >= 0.  Where c is 1 nothing is written to a y that is x.  One launch for every 768
+ * spans.  Errors: ARG, ALIGN, CUDA. */
+int loco_gradient_clip(const loco_span_t *spans, int32_t count, const double *d_squares, double max_norm, float *d_norm, void *stream);
+
+/*
+ * Flags raised on the current device since the library was loaded; SYNCHRONISES `stream`.  The attention and product kernels
+ * wait on their own copies and products, never on another launch; a wait that exceeds two seconds gives up, the outputs of
+ * its block are meaningless and the flag is raised.
  */
 #define LOCO_LAYER_FLAG_TIMEOUT 1u
 int loco_layer_status(uint32_t *flags, void *stream);

@@ -25,8 +25,9 @@ LIB = os.path.join(HERE, "libloco_b200.so")
 DEPS = [os.path.join(CSRC, f) for f in ("loco_api.cu", "loco_send_tu.cu", "loco_reduce_tu.cu", "loco_kernels.cuh",
                                         "loco_dispatch.h")] + [os.path.join(os.path.dirname(HERE), "include", "loco.h")]
 LAYER_LIB = os.path.join(HERE, "libloco_layer_b200.so")
-LAYER_SOURCES = ("layer_rotary.cu", "layer_router.cu", "layer_attention.cu", "layer_attention_api.cu")
-LAYER_DEPS = [os.path.join(CSRC, f) for f in LAYER_SOURCES + ("layer_common.h", "layer_attention.h", "layer_tc.cuh")] + [
+LAYER_SOURCES = ("layer_rotary.cu", "layer_router.cu", "layer_attention.cu", "layer_attention_api.cu", "layer_norm.cu", "layer_experts.cu",
+                 "layer_product.cu", "layer_gradient.cu")
+LAYER_DEPS = [os.path.join(CSRC, f) for f in LAYER_SOURCES + ("layer_common.h", "layer_attention.h", "layer_maps.h", "layer_tc.cuh")] + [
     os.path.join(os.path.dirname(HERE), "include", f) for f in ("loco.h", "loco_layer.h")]
 BINDING = os.path.join(HERE, "_layer_binding.so")
 BINDING_DEPS = [os.path.join(CSRC, "layer_binding.cpp")] + [os.path.join(os.path.dirname(HERE), "include", f) for f in ("loco.h", "loco_layer.h")]

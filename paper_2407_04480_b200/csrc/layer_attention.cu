@@ -21,6 +21,7 @@
 #include <cuda.h>
 
 #include "layer_attention.h"
+#include "layer_maps.h"
 #include "layer_tc.cuh"
 
 namespace loco_layer {
@@ -949,29 +950,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_backward_keys_kernel(co
 
 namespace {
 
-using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn encode_fn() {
-    static std::atomic<EncodeFn> known{nullptr};
-    EncodeFn f = known.load();
-    if (!f) {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult how;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &how) != cudaSuccess || how != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            return nullptr;
-        }
-        f = reinterpret_cast<EncodeFn>(p);
-        known.store(f);
-    }
-    return f;
-}
-
 // Heads as [batch, head, row, dim] in boxes of `box_rows` rows by 64 dimensions; what lies past the tensor reads as zero.
 bool make_map(CUtensorMap &map, const Heads &t, int batch, int heads, int rows, int dim, int box_rows, const void *stand_in) {
-    const EncodeFn encode = encode_fn();
-    if (!encode) return false;
     const bool none = rows == 0 || batch == 0;             // never read
     void *at = none ? const_cast<void *>(stand_in) : static_cast<void *>(t.ptr);
     const cuuint64_t size[4] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(none ? 1 : rows), static_cast<cuuint64_t>(heads),
@@ -979,17 +959,8 @@ bool make_map(CUtensorMap &map, const Heads &t, int batch, int heads, int rows, 
     // the stride of a single row, head or sample means nothing, but has to be a valid one
     const auto stride = [&](int64_t s, cuuint64_t n) { return static_cast<cuuint64_t>(n == 1 ? 256 : s * 2); };
     const cuuint64_t strides[3] = {stride(t.row_stride, size[1]), stride(t.head_stride, size[2]), stride(t.batch_stride, size[3])};
-    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1}, step[4] = {1, 1, 1, 1};
-    const auto made = [&] {
-        return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, at, size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-    };
-    if (made()) return true;
-    // Unlike a launch the encoding binds no context to the calling thread, and needs one: a thread's first call binds it.
-    int dev = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess) return made();
-    cudaGetLastError();
-    return false;
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1};
+    return encode_map(map, 4, at, size, strides, box);
 }
 
 using Kernel = void (*)(const AttentionParams, const Maps);
@@ -1086,15 +1057,20 @@ int launch_attention_backward(const AttentionParams &P, cudaStream_t stream) {
 
 }  // namespace loco_layer
 
+namespace loco_layer {
+// The flags of the product kernels; not there where this file is built alone.
+int __attribute__((weak)) more_status(unsigned *flags, cudaStream_t stream);
+}  // namespace loco_layer
+
 extern "C" int loco_layer_status(uint32_t *flags, void *stream) {
     if (!flags) return LOCO_ERR_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    unsigned host = 0;
+    unsigned host = 0, more = 0;
     if (cudaMemcpyFromSymbolAsync(&host, loco_layer::g_status, sizeof(host), 0, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
-        cudaStreamSynchronize(s) != cudaSuccess) {
+        (loco_layer::more_status && loco_layer::more_status(&more, s) != 0) || cudaStreamSynchronize(s) != cudaSuccess) {
         cudaGetLastError();
         return LOCO_ERR_CUDA;
     }
-    *flags = host;
+    *flags = host | more;
     return LOCO_OK;
 }

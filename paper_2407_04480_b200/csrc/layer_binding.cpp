@@ -11,6 +11,7 @@
 #include <cmath>
 #include <cstdio>
 #include <string>
+#include <vector>
 
 #include "../../include/loco_layer.h"
 
@@ -268,6 +269,206 @@ int router_backward(PyObject *const *a) {
                                 stream_of(a[12], r.device));
 }
 
+// ---- norm, experts, gradient -----------------------------------------------------------------
+
+// [rows, dim] of a type, the columns contiguous.
+loco_rows_t matrix(const at::Tensor &t, int64_t rows, int64_t dim, ScalarType type, int device, const char *what) {
+    if (!t.is_cuda() || t.get_device() != device || t.scalar_type() != type) refuse(std::string("unexpected type or device: ") + what);
+    if (t.dim() != 2 || t.size(0) != rows || t.size(1) != dim) refuse(std::string("unexpected shape of ") + what);
+    if (dim > 1 && rows > 0 && t.stride(1) != 1) refuse(std::string("rows must be contiguous: ") + what);
+    return loco_rows_t{t.data_ptr(), rows > 1 ? t.stride(0) : 0};
+}
+const at::Tensor &rows_of(PyObject *o, const char *what) {
+    const at::Tensor &t = need(o, what);
+    if (t.dim() != 2) refuse(std::string("expected [rows, dim]: ") + what);
+    return t;
+}
+struct Work {
+    void *at;
+    uint64_t bytes;
+};
+Work work_of(PyObject *o, int device) {
+    const at::Tensor *t = tensor(o, "work");
+    if (!t) return Work{nullptr, 0};
+    if (!t->is_cuda() || t->get_device() != device || !t->is_contiguous()) refuse("the workspace must be a contiguous tensor on the operands' device");
+    return Work{t->data_ptr(), t->nbytes()};
+}
+
+// x, y, weight, residual, total, scale, block, eps, stream
+int norm_forward(PyObject *const *a) {
+    const at::Tensor &x = rows_of(a[0], "x"), &y = rows_of(a[1], "y");
+    const at::Tensor *residual = tensor(a[3], "residual"), *total = tensor(a[4], "total");
+    const int device = device_of(x);
+    const int64_t n = x.size(0), d = x.size(1), block = integer(a[6], "block");
+    const ScalarType type = x.scalar_type();
+    const bool bits8 = y.scalar_type() == ScalarType::Float8_e4m3fn;
+    if (!bits8 && (a[5] != Py_None || block != 0)) refuse("scales and a block belong to an output in float8_e4m3fn");
+    const loco_norm_t cfg{dtype_of(x), small(d, "dim"), bits8, small(block, "block"), number(a[7], "eps")};
+    const loco_rows_t rx = matrix(x, n, d, type, device, "x"), ry = matrix(y, n, d, bits8 ? ScalarType::Float8_e4m3fn : type, device, "y");
+    const loco_rows_t rr = residual ? matrix(*residual, n, d, type, device, "residual") : loco_rows_t{}, rt = total ? matrix(*total, n, d, type, device, "total") : loco_rows_t{};
+    if (bits8 && block != 0 && block != 128) refuse("block must be 0 or 128");
+    float *scale = static_cast<float *>(flat(a[5], {n, block ? (d + block - 1) / block : 1}, ScalarType::Float, device, "scale"));
+    return loco_norm_forward(&cfg, n, &rx, residual ? &rr : nullptr, flat(a[2], {d}, type, device, "weight"), total ? &rt : nullptr, &ry, scale, stream_of(a[8], device));
+}
+
+// h, dy, dx, work, weight, dweight, dtotal, eps, stream
+int norm_backward(PyObject *const *a) {
+    const at::Tensor &h = rows_of(a[0], "h");
+    const at::Tensor *dtotal = tensor(a[6], "dtotal");
+    const int device = device_of(h);
+    const int64_t n = h.size(0), d = h.size(1);
+    const ScalarType type = h.scalar_type();
+    const loco_norm_t cfg{dtype_of(h), small(d, "dim"), 0, 0, number(a[7], "eps")};
+    const loco_rows_t rh = matrix(h, n, d, type, device, "h"), rd = matrix(need(a[1], "dy"), n, d, type, device, "dy"), rx = matrix(need(a[2], "dx"), n, d, type, device, "dx");
+    const loco_rows_t rt = dtotal ? matrix(*dtotal, n, d, type, device, "dtotal") : loco_rows_t{};
+    const Work work = work_of(a[3], device);
+    return loco_norm_backward(&cfg, n, &rh, &rd, flat(a[4], {d}, type, device, "weight"), dtotal ? &rt : nullptr, &rx, flat(a[5], {d}, type, device, "dweight"),
+                              work.at, work.bytes, stream_of(a[8], device));
+}
+
+// index, offsets, place, work, stream
+int experts_sort(PyObject *const *a) {
+    const at::Tensor &index = rows_of(a[0], "index"), &offsets = need(a[1], "offsets");
+    const int device = device_of(index);
+    const int64_t n = index.size(0), k = index.size(1), e = offsets.numel() - 1;
+    const Work work = work_of(a[3], device);
+    return loco_experts_sort(small(e, "experts"), n, small(k, "top_k"), static_cast<const int32_t *>(flat(a[0], {n, k}, ScalarType::Int, device, "index")),
+                             static_cast<int32_t *>(flat(a[1], {e + 1}, ScalarType::Int, device, "offsets")),
+                             static_cast<int32_t *>(flat(a[2], {n, k}, ScalarType::Int, device, "place")), work.at, work.bytes, stream_of(a[4], device));
+}
+
+struct Moved {
+    loco_experts_t cfg;
+    int device;
+    ScalarType type;
+    int64_t tokens, choices, dim, rows;
+    const int32_t *place;
+};
+// the tokens' tensor, place, the sorted rows' tensor
+Moved moved(const at::Tensor &tokens, PyObject *place, const at::Tensor &rows) {
+    Moved m{};
+    m.device = device_of(tokens);
+    m.type = tokens.scalar_type();
+    m.tokens = tokens.size(0);
+    m.dim = tokens.size(1);
+    m.rows = rows.size(0);
+    const at::Tensor &p = rows_of(place, "place");
+    m.choices = p.size(1);
+    m.place = static_cast<const int32_t *>(flat(place, {m.tokens, m.choices}, ScalarType::Int, m.device, "place"));
+    m.cfg = loco_experts_t{dtype_of(tokens), small(m.dim, "dim"), small(m.choices, "top_k"), m.tokens, m.rows};
+    return m;
+}
+
+// x, place, rows, stream
+int experts_dispatch(PyObject *const *a) {
+    const at::Tensor &x = rows_of(a[0], "x"), &rows = rows_of(a[2], "rows");
+    const Moved m = moved(x, a[1], rows);
+    const loco_rows_t rx = matrix(x, m.tokens, m.dim, m.type, m.device, "x"), rr = matrix(rows, m.rows, m.dim, m.type, m.device, "rows");
+    return loco_experts_dispatch(&m.cfg, &rx, m.place, &rr, stream_of(a[3], m.device));
+}
+
+// rows, place, y, weight, stream
+int experts_combine(PyObject *const *a) {
+    const at::Tensor &rows = rows_of(a[0], "rows"), &y = rows_of(a[2], "y");
+    const Moved m = moved(y, a[1], rows);
+    const loco_rows_t rr = matrix(rows, m.rows, m.dim, m.type, m.device, "rows"), ry = matrix(y, m.tokens, m.dim, m.type, m.device, "y");
+    return loco_experts_combine(&m.cfg, &rr, m.place, static_cast<const float *>(flat(a[3], {m.tokens, m.choices}, ScalarType::Float, m.device, "weight")), &ry,
+                                stream_of(a[4], m.device));
+}
+
+// dy, rows, place, weight, drows, dweight, stream
+int experts_combine_backward(PyObject *const *a) {
+    const at::Tensor &dy = rows_of(a[0], "dy"), &rows = rows_of(a[1], "rows");
+    const Moved m = moved(dy, a[2], rows);
+    const loco_rows_t rd = matrix(dy, m.tokens, m.dim, m.type, m.device, "dy"), rr = matrix(rows, m.rows, m.dim, m.type, m.device, "rows"),
+                      ro = matrix(need(a[4], "drows"), m.rows, m.dim, m.type, m.device, "drows");
+    return loco_experts_combine_backward(&m.cfg, &rd, &rr, m.place, static_cast<const float *>(flat(a[3], {m.tokens, m.choices}, ScalarType::Float, m.device, "weight")),
+                                         &ro, static_cast<float *>(flat(a[5], {m.tokens, m.choices}, ScalarType::Float, m.device, "dweight")), stream_of(a[6], m.device));
+}
+
+// [experts, rows, columns] bfloat16, the columns contiguous.
+loco_matrices_t matrices(const at::Tensor &t, at::IntArrayRef shape, int device, const char *what) {
+    if (!t.is_cuda() || t.get_device() != device || t.scalar_type() != ScalarType::BFloat16 || t.sizes() != shape)
+        refuse(std::string("expected bfloat16 matrices [experts, first, second] of the rows' sizes on their device: ") + what);
+    if (shape[2] > 1 && t.stride(2) != 1) refuse(std::string("rows must be contiguous: ") + what);
+    return loco_matrices_t{t.data_ptr(), t.stride(0), t.stride(1)};
+}
+const int32_t *offsets_of(PyObject *o, int64_t experts, int device) {
+    return static_cast<const int32_t *>(flat(o, {experts + 1}, ScalarType::Int, device, "offsets"));
+}
+
+// x, w, offsets, y, transposed, stream
+int experts_product(PyObject *const *a) {
+    const at::Tensor &x = rows_of(a[0], "x"), &w = need(a[1], "w"), &y = rows_of(a[3], "y");
+    const int device = device_of(x);
+    const bool turned = truth(a[4], "transposed");
+    const int64_t n = x.size(0), in = x.size(1), out = y.size(1), e = need(a[2], "offsets").numel() - 1;
+    const loco_product_t cfg{small(e, "experts"), n, small(in, "columns"), small(out, "columns"), turned};
+    const loco_rows_t rx = matrix(x, n, in, ScalarType::BFloat16, device, "x"), ry = matrix(y, n, out, ScalarType::BFloat16, device, "y");
+    const loco_matrices_t m = matrices(w, {e, turned ? out : in, turned ? in : out}, device, "w");
+    return loco_experts_product(&cfg, &rx, &m, offsets_of(a[2], e, device), &ry, stream_of(a[5], device));
+}
+
+// a, b, offsets, dw, stream
+int experts_product_weights(PyObject *const *a) {
+    const at::Tensor &x = rows_of(a[0], "a"), &y = rows_of(a[1], "b");
+    const int device = device_of(x);
+    const int64_t n = x.size(0), in = x.size(1), out = y.size(1), e = need(a[2], "offsets").numel() - 1;
+    const loco_product_t cfg{small(e, "experts"), n, small(in, "columns"), small(out, "columns"), 0};
+    const loco_rows_t rx = matrix(x, n, in, ScalarType::BFloat16, device, "a"), ry = matrix(y, n, out, ScalarType::BFloat16, device, "b");
+    const loco_matrices_t m = matrices(need(a[3], "dw"), {e, in, out}, device, "dw");
+    return loco_experts_product_weights(&cfg, &rx, &ry, offsets_of(a[2], e, device), &m, stream_of(a[4], device));
+}
+
+// A list or tuple of tensors, each contiguous, and of as many outputs of the same sizes and types.
+struct List {
+    std::vector<loco_span_t> spans;
+    int device;
+};
+List list_of(PyObject *xs, PyObject *ys, PyObject *beside) {
+    if (!PyList_Check(xs) && !PyTuple_Check(xs)) refuse("expected a list or tuple of gradients");
+    if (ys && !PyList_Check(ys) && !PyTuple_Check(ys)) refuse("expected a list or tuple of outputs");
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(xs);
+    if (ys && PySequence_Fast_GET_SIZE(ys) != n) refuse("there must be an output for every gradient");
+    List l;
+    l.device = device_of(need(beside, "squares"));
+    l.spans.reserve(static_cast<size_t>(n));
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor &x = need(PySequence_Fast_GET_ITEM(xs, i), "a gradient");
+        if (!x.is_cuda() || x.get_device() != l.device || !x.is_contiguous()) refuse("the gradients must be contiguous and on one device");
+        loco_span_t s{x.data_ptr(), nullptr, static_cast<uint64_t>(x.numel()), dtype_of(x)};
+        if (ys) {
+            const at::Tensor &y = need(PySequence_Fast_GET_ITEM(ys, i), "an output");
+            if (!y.is_cuda() || y.get_device() != l.device || !y.is_contiguous() || y.scalar_type() != x.scalar_type() || y.numel() != x.numel())
+                refuse("an output must be contiguous and have its gradient's size, type and device");
+            s.y = y.data_ptr();
+        }
+        l.spans.push_back(s);
+    }
+    return l;
+}
+
+// gradients, squares, work, stream
+int gradient_squares(PyObject *const *a) {
+    const List l = list_of(a[0], nullptr, a[1]);
+    const Work work = work_of(a[2], l.device);
+    return loco_gradient_squares(l.spans.data(), small(static_cast<int64_t>(l.spans.size()), "list"), static_cast<double *>(flat(a[1], {1}, ScalarType::Double, l.device, "squares")),
+                                 work.at, work.bytes, stream_of(a[3], l.device));
+}
+
+// gradients, outputs, squares, norm, max_norm, stream
+int gradient_clip(PyObject *const *a) {
+    const List l = list_of(a[0], a[1], a[2]);
+    const double most = PyFloat_AsDouble(a[4]);
+    if (most == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse("max_norm must be a number");
+    }
+    return loco_gradient_clip(l.spans.data(), small(static_cast<int64_t>(l.spans.size()), "list"),
+                              static_cast<const double *>(flat(a[2], {1}, ScalarType::Double, l.device, "squares")), most,
+                              static_cast<float *>(flat(a[3], {1}, ScalarType::Float, l.device, "norm")), stream_of(a[5], l.device));
+}
+
 template <int (*kCall)(PyObject *const *), int kArgs> PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n != kArgs) {
         PyErr_Format(PyExc_TypeError, "expected %d arguments, got %zd", kArgs, n);
@@ -285,7 +486,9 @@ template <int (*kCall)(PyObject *const *), int kArgs> PyObject *entry(PyObject *
 
 #define LOCO_ENTRY(name, args) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(entry<name, args>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LOCO_ENTRY(rotary_apply, 9), LOCO_ENTRY(attention_forward, 14), LOCO_ENTRY(attention_backward, 19),
-                         LOCO_ENTRY(router_forward, 14), LOCO_ENTRY(router_backward, 13), {nullptr, nullptr, 0, nullptr}};
+                         LOCO_ENTRY(router_forward, 14), LOCO_ENTRY(router_backward, 13), LOCO_ENTRY(norm_forward, 9), LOCO_ENTRY(norm_backward, 9),
+                         LOCO_ENTRY(experts_sort, 5), LOCO_ENTRY(experts_dispatch, 4), LOCO_ENTRY(experts_combine, 5), LOCO_ENTRY(experts_combine_backward, 7),
+                         LOCO_ENTRY(experts_product, 6), LOCO_ENTRY(experts_product_weights, 5), LOCO_ENTRY(gradient_squares, 4), LOCO_ENTRY(gradient_clip, 6), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layer_binding", LOCO_BUILT_FOR, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,402 @@
+// Choices sorted by expert, tokens laid out in that order and summed back with their weights, and the gradients.
+//
+// Sorting is a counting sort: every warp counts the experts of its own run of choices, the counts before it (of the block's
+// warps, and of the blocks before) give the warp's first row of every expert, and the lanes that hold the same expert take
+// rows in their order.  So the order is that of expert, token, slot, and no atomic decides it.
+// The other passes move rows: a team of threads has a token, reads its row once and writes it to all of its places, or
+// reads them all and writes the sum.  One or two operations an element, so HBM bounds them.
+#include "layer_common.h"
+
+namespace loco_layer {
+
+constexpr int kMostExperts = 512;
+constexpr int kMostChoices = 16;
+constexpr int kSortThreads = 512;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortBlocks = 148;                 // most blocks, each leaves its counts to the others
+constexpr int kSortEach = 2048;                  // choices a block is worth starting for
+constexpr int kMoveThreads = 256;
+constexpr unsigned kAll = 0xffffffffu;
+
+struct SortParams {
+    const int32_t *index;
+    int32_t *offsets, *place, *counts;           // counts: [block][expert]
+    int64_t choices, each;                       // choices of a block, a multiple of kSortThreads
+    int32_t experts;
+};
+
+// Counts of each warp's own run of choices, in shared memory.
+__device__ __forceinline__ void count_run(const SortParams &P, int *mine, int64_t from, int64_t until, int lane) {
+    for (int64_t i = from + lane; i < until; i += 32) {
+        const int e = P.index[i];
+        if (static_cast<unsigned>(e) < static_cast<unsigned>(P.experts)) atomicAdd(&mine[e], 1);
+    }
+}
+// The warp's run: choices are dealt to blocks, then warps, in runs.
+__device__ __forceinline__ void run_of(const SortParams &P, int warp, int64_t &from, int64_t &until) {
+    const int64_t each = P.each / kSortWarps;
+    from = static_cast<int64_t>(blockIdx.x) * P.each + warp * each;
+    until = min(from + each, P.choices);
+}
+
+__global__ void __launch_bounds__(kSortThreads) experts_count_kernel(const SortParams P) {
+    wait_for_previous();
+    let_next_start();
+    __shared__ int count[kMostExperts];
+    for (int e = threadIdx.x; e < P.experts; e += kSortThreads) count[e] = 0;
+    __syncthreads();
+    int64_t from, until;
+    run_of(P, threadIdx.x / 32, from, until);
+    count_run(P, count, from, until, threadIdx.x % 32);
+    __syncthreads();
+    for (int e = threadIdx.x; e < P.experts; e += kSortThreads) P.counts[static_cast<int64_t>(blockIdx.x) * P.experts + e] = count[e];
+}
+
+// Sum of the values of the threads before, over the block; `total` is the sum of all.
+__device__ __forceinline__ int before_in_block(int x, int *fold, int &total) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    int s = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(kAll, s, o);
+        s += lane >= o ? y : 0;
+    }
+    if (lane == 31) fold[warp] = s;
+    __syncthreads();
+    int sum = 0;
+    total = 0;
+    for (int w = 0; w < kSortWarps; ++w) {
+        sum += w < warp ? fold[w] : 0;
+        total += fold[w];
+    }
+    return sum + s - x;
+}
+
+__global__ void __launch_bounds__(kSortThreads) experts_place_kernel(const SortParams P) {
+    wait_for_previous();
+    let_next_start();
+    extern __shared__ int next[];                // [warp][expert]: counts, then the warp's next row of the expert
+    __shared__ int fold[kSortWarps];
+    static_assert(kMostExperts <= kSortThreads, "one expert a thread");
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, E = P.experts, blocks = static_cast<int>(gridDim.x);
+    for (int i = threadIdx.x; i < kSortWarps * E; i += kSortThreads) next[i] = 0;
+    __syncthreads();
+    int64_t from, until;
+    run_of(P, warp, from, until);
+    count_run(P, next + warp * E, from, until, lane);
+    __syncthreads();
+    const int e = threadIdx.x;
+    int all = 0, before = 0;                     // of the expert: choices of all blocks, of the blocks before this one
+    if (e < E) {
+        if (blocks == 1) {
+            for (int w = 0; w < kSortWarps; ++w) all += next[w * E + e];
+        } else {
+#pragma unroll 8
+            for (int b = 0; b < blocks; ++b) {
+                const int n = __ldcg(P.counts + static_cast<int64_t>(b) * E + e);
+                all += n;
+                before += b < static_cast<int>(blockIdx.x) ? n : 0;
+            }
+        }
+    }
+    int total;
+    const int first = before_in_block(all, fold, total);
+    if (e < E) {
+        if (blockIdx.x == 0) {
+            P.offsets[e] = first;
+            if (e == 0) P.offsets[E] = total;
+        }
+        int row = first + before;
+        for (int w = 0; w < kSortWarps; ++w) {
+            const int n = next[w * E + e];
+            next[w * E + e] = row;
+            row += n;
+        }
+    }
+    __syncthreads();
+    int *const mine = next + warp * E;
+    for (int64_t i = from; i < until; i += 32) {
+        const int64_t at = i + lane;
+        const int chosen = at < until ? P.index[at] : -1;
+        const bool some = static_cast<unsigned>(chosen) < static_cast<unsigned>(E);
+        const unsigned same = __match_any_sync(kAll, some ? chosen : -1);
+        const int row = some ? mine[chosen] : 0;
+        __syncwarp();
+        if (some && lane == __ffs(same) - 1) mine[chosen] = row + __popc(same);
+        __syncwarp();
+        if (at < until) P.place[at] = some ? row + __popc(same & ((1u << lane) - 1)) : -1;
+    }
+}
+
+struct MoveParams {
+    const void *in, *rows;                       // tokens read (x, dy), sorted rows read
+    void *out, *rows_out;                        // tokens written, sorted rows written
+    const int32_t *place;
+    const float *weight;
+    float *dweight;
+    int64_t in_stride, out_stride, rows_stride, rows_out_stride, tokens, row_count;
+    int32_t dim, top_k, team;
+};
+
+// Token and lane of a thread: a team of threads to a token, several teams to a block.
+struct Seat {
+    int64_t token;
+    int lane;
+};
+__device__ __forceinline__ Seat seat(int team) {
+    return Seat{static_cast<int64_t>(blockIdx.x) * (kMoveThreads / team) + static_cast<int>(threadIdx.x) / team, static_cast<int>(threadIdx.x) % team};
+}
+
+template <typename T, int V> __global__ void __launch_bounds__(kMoveThreads) experts_dispatch_kernel(const __grid_constant__ MoveParams P) {
+    wait_for_previous();
+    let_next_start();
+    using Vec = Pack<T, V>;
+    const Seat s = seat(P.team);
+    if (s.token >= P.tokens) return;
+    const T *x = static_cast<const T *>(P.in) + s.token * P.in_stride;
+    const int32_t *place = P.place + s.token * P.top_k;
+    for (int c = s.lane * V; c < P.dim; c += P.team * V) {
+        const Vec v = *reinterpret_cast<const Vec *>(x + c);
+        for (int j = 0; j < P.top_k; ++j) {
+            const int p = __ldg(place + j);
+            if (p >= 0 && p < P.row_count) *reinterpret_cast<Vec *>(static_cast<T *>(P.rows_out) + p * P.rows_out_stride + c) = v;
+        }
+    }
+}
+
+template <typename T, int V> __global__ void __launch_bounds__(kMoveThreads) experts_combine_kernel(const __grid_constant__ MoveParams P) {
+    wait_for_previous();
+    let_next_start();
+    using Vec = Pack<T, V>;
+    const Seat s = seat(P.team);
+    if (s.token >= P.tokens) return;
+    const int32_t *place = P.place + s.token * P.top_k;
+    const float *weight = P.weight + s.token * P.top_k;
+    T *y = static_cast<T *>(P.out) + s.token * P.out_stride;
+    for (int c = s.lane * V; c < P.dim; c += P.team * V) {
+        float sum[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+#pragma unroll 4
+        for (int j = 0; j < P.top_k; ++j) {
+            const int p = __ldg(place + j);
+            if (p >= 0 && p < P.row_count) {
+                const Vec v = *reinterpret_cast<const Vec *>(static_cast<const T *>(P.rows) + p * P.rows_stride + c);
+                const float w = P.weight ? __ldg(weight + j) : 1.0f;
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] = fmaf(w, to_f32(v.v[i]), sum[i]);
+            }
+        }
+        Vec out;
+#pragma unroll
+        for (int i = 0; i < V; ++i) out.v[i] = from_f32<T>(sum[i]);
+        *reinterpret_cast<Vec *>(y + c) = out;
+    }
+}
+
+// kMost: choices of a token at most.
+template <typename T, int V, int kMost> __global__ void __launch_bounds__(kMoveThreads) experts_backward_kernel(const __grid_constant__ MoveParams P) {
+    wait_for_previous();
+    let_next_start();
+    using Vec = Pack<T, V>;
+    __shared__ float fold[kMoveThreads / 32][kMost];
+    const Seat s = seat(P.team);
+    const bool there = s.token < P.tokens;
+    const T *dy = static_cast<const T *>(P.in) + s.token * P.in_stride;
+    float dot[kMost], w[kMost];
+    int p[kMost];
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+        dot[j] = 0.0f;
+        w[j] = 0.0f;
+        p[j] = -1;
+        if (there && j < P.top_k) {
+            const int at = __ldg(P.place + s.token * P.top_k + j);
+            p[j] = at < P.row_count ? at : -1;
+            w[j] = __ldg(P.weight + s.token * P.top_k + j);
+        }
+    }
+    if (there)
+        for (int c = s.lane * V; c < P.dim; c += P.team * V) {
+            const Vec d = *reinterpret_cast<const Vec *>(dy + c);
+#pragma unroll
+            for (int j = 0; j < kMost; ++j)
+                if (p[j] >= 0) {
+                    const Vec r = *reinterpret_cast<const Vec *>(static_cast<const T *>(P.rows) + p[j] * P.rows_stride + c);
+                    Vec out;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        dot[j] = fmaf(to_f32(d.v[i]), to_f32(r.v[i]), dot[j]);
+                        out.v[i] = from_f32<T>(w[j] * to_f32(d.v[i]));
+                    }
+                    *reinterpret_cast<Vec *>(static_cast<T *>(P.rows_out) + p[j] * P.rows_out_stride + c) = out;
+                }
+        }
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+#pragma unroll
+    for (int j = 0; j < kMost; ++j)
+        for (int o = (P.team < 32 ? P.team : 32) / 2; o; o >>= 1) dot[j] += __shfl_xor_sync(kAll, dot[j], o);
+    float *const dw = P.dweight + s.token * P.top_k;
+    if (P.team <= 32) {
+        if (there && s.lane == 0)
+#pragma unroll
+            for (int j = 0; j < kMost; ++j)
+                if (j < P.top_k) dw[j] = dot[j];
+        return;
+    }
+    if (lane == 0)
+#pragma unroll
+        for (int j = 0; j < kMost; ++j) fold[warp][j] = dot[j];
+    __syncthreads();
+    if (there && s.lane < P.top_k) {
+        float sum = 0.0f;
+        for (int i = 0; i < P.team / 32; ++i) sum += fold[warp + i][s.lane];
+        dw[s.lane] = sum;
+    }
+}
+
+namespace {
+
+using MoveKernel = void (*)(const MoveParams);
+template <typename T, int V> MoveKernel pick_backward(int k) {
+    return k <= 2 ? experts_backward_kernel<T, V, 2> : k <= 4 ? experts_backward_kernel<T, V, 4> : k <= 8 ? experts_backward_kernel<T, V, 8> : experts_backward_kernel<T, V, 16>;
+}
+enum Move { kDispatch, kCombine, kBackward };
+template <typename T, int V> MoveKernel pick_move(Move m, int k) {
+    return m == kDispatch ? experts_dispatch_kernel<T, V> : m == kCombine ? experts_combine_kernel<T, V> : pick_backward<T, V>(k);
+}
+
+int check_experts(const loco_experts_t *c) {
+    if (!c) return LOCO_ERR_ARG;
+    if (c->dtype != LOCO_F32 && c->dtype != LOCO_BF16) return LOCO_ERR_ARG;
+    if (c->dim < 1 || c->top_k < 1 || c->top_k > kMostChoices) return LOCO_ERR_ARG;
+    if (c->tokens < 0 || c->tokens > 0x7fffffff / c->top_k || c->rows < 0 || c->rows > 0x7fffffff) return LOCO_ERR_ARG;
+    return LOCO_OK;
+}
+
+// A tensor of rows: present, aligned to its elements; an output's rows do not overlap.  Narrows `vec` to what its rows allow.
+int take_rows(const loco_experts_t *c, const loco_rows_t *t, int64_t rows, bool written, int &vec, int64_t &stride) {
+    if (!t) return LOCO_ERR_ARG;
+    stride = rows > 1 ? t->row_stride : 0;
+    if (rows == 0) return LOCO_OK;
+    const int size = c->dtype == LOCO_BF16 ? 2 : 4;
+    if (!t->ptr || stride < 0 || (written && rows > 1 && stride < c->dim)) return LOCO_ERR_ARG;
+    if (!aligned(t->ptr, static_cast<uintptr_t>(size))) return LOCO_ERR_ALIGN;
+    while (vec > 1 && (!aligned(t->ptr, static_cast<uintptr_t>(vec * size)) || stride % vec != 0 || c->dim % vec != 0)) vec /= 2;
+    return LOCO_OK;
+}
+
+int launch_move(Move m, MoveParams &P, const loco_experts_t *c, int vec, void *stream) {
+    P.tokens = c->tokens;
+    P.row_count = c->rows;
+    P.dim = c->dim;
+    P.top_k = c->top_k;
+    MoveKernel fn;
+    int v;
+    if (c->dtype == LOCO_BF16) {
+        v = vec >= 8 ? 8 : vec >= 2 ? 2 : 1;
+        fn = v == 8 ? pick_move<__nv_bfloat16, 8>(m, c->top_k) : v == 2 ? pick_move<__nv_bfloat16, 2>(m, c->top_k) : pick_move<__nv_bfloat16, 1>(m, c->top_k);
+    } else {
+        v = vec >= 4 ? 4 : 1;
+        fn = v == 4 ? pick_move<float, 4>(m, c->top_k) : pick_move<float, 1>(m, c->top_k);
+    }
+    int team = 4;
+    while (team < kMoveThreads && team * v < c->dim) team *= 2;
+    P.team = team;
+    const int64_t blocks = (c->tokens + kMoveThreads / team - 1) / (kMoveThreads / team);
+    return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), kMoveThreads, 0, stream, P);
+}
+
+int start(const loco_experts_t *c, const int32_t *place, const float *weight) {
+    const int rc = check_experts(c);
+    if (rc != LOCO_OK || c->tokens == 0) return rc;
+    if (!place) return LOCO_ERR_ARG;
+    return aligned(place, 4) && aligned(weight, 4) ? LOCO_OK : LOCO_ERR_ALIGN;
+}
+
+}  // namespace
+
+}  // namespace loco_layer
+
+using namespace loco_layer;
+
+extern "C" {
+
+uint64_t loco_experts_sort_workspace_bytes(int32_t experts) {
+    return experts < 1 || experts > kMostExperts ? 0 : static_cast<uint64_t>(kSortBlocks) * experts * sizeof(int32_t);
+}
+
+int loco_experts_sort(int32_t experts, int64_t tokens, int32_t top_k, const int32_t *d_index, int32_t *d_offsets, int32_t *d_place,
+                      void *d_work, uint64_t d_work_bytes, void *stream) {
+    if (experts < 1 || experts > kMostExperts || top_k < 1 || top_k > kMostChoices || tokens < 0 || tokens > 0x7fffffff / top_k) return LOCO_ERR_ARG;
+    if (!d_offsets || !d_work || (tokens > 0 && (!d_index || !d_place))) return LOCO_ERR_ARG;
+    if (!aligned(d_index, 4) || !aligned(d_offsets, 4) || !aligned(d_place, 4) || !aligned(d_work, 16)) return LOCO_ERR_ALIGN;
+    if (d_work_bytes < loco_experts_sort_workspace_bytes(experts)) return LOCO_ERR_SIZE;
+    SortParams P{};
+    P.index = d_index;
+    P.offsets = d_offsets;
+    P.place = d_place;
+    P.counts = static_cast<int32_t *>(d_work);
+    P.choices = tokens * top_k;
+    P.experts = experts;
+    int64_t blocks = (P.choices + kSortEach - 1) / kSortEach;
+    blocks = blocks < 1 ? 1 : blocks > kSortBlocks ? kSortBlocks : blocks;
+    P.each = ((P.choices + blocks - 1) / blocks + kSortThreads - 1) / kSortThreads * kSortThreads;
+    const dim3 grid(static_cast<unsigned>(blocks));
+    if (blocks > 1) {
+        const int rc = launch_kernel(experts_count_kernel, grid, kSortThreads, 0, stream, P);
+        if (rc != LOCO_OK) return rc;
+    }
+    return launch_kernel(experts_place_kernel, grid, kSortThreads, static_cast<size_t>(kSortWarps) * experts * sizeof(int), stream, P);
+}
+
+int loco_experts_dispatch(const loco_experts_t *c, const loco_rows_t *x, const int32_t *d_place, const loco_rows_t *rows, void *stream) {
+    int rc = start(c, d_place, nullptr);
+    if (rc != LOCO_OK || c->tokens == 0) return rc;
+    MoveParams P{};
+    int vec = c->dtype == LOCO_BF16 ? 8 : 4;
+    if ((rc = take_rows(c, x, c->tokens, false, vec, P.in_stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(c, rows, c->rows, true, vec, P.rows_out_stride)) != LOCO_OK) return rc;
+    if (c->rows == 0) return LOCO_OK;
+    P.in = x->ptr;
+    P.rows_out = rows->ptr;
+    P.place = d_place;
+    return launch_move(kDispatch, P, c, vec, stream);
+}
+
+int loco_experts_combine(const loco_experts_t *c, const loco_rows_t *rows, const int32_t *d_place, const float *d_weight,
+                         const loco_rows_t *y, void *stream) {
+    int rc = start(c, d_place, d_weight);
+    if (rc != LOCO_OK || c->tokens == 0) return rc;
+    MoveParams P{};
+    int vec = c->dtype == LOCO_BF16 ? 8 : 4;
+    if ((rc = take_rows(c, rows, c->rows, false, vec, P.rows_stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(c, y, c->tokens, true, vec, P.out_stride)) != LOCO_OK) return rc;
+    P.rows = rows->ptr;
+    P.out = y->ptr;
+    P.place = d_place;
+    P.weight = d_weight;
+    return launch_move(kCombine, P, c, vec, stream);
+}
+
+int loco_experts_combine_backward(const loco_experts_t *c, const loco_rows_t *dy, const loco_rows_t *rows, const int32_t *d_place,
+                                  const float *d_weight, const loco_rows_t *drows, float *d_dweight, void *stream) {
+    int rc = start(c, d_place, d_weight);
+    if (rc != LOCO_OK || c->tokens == 0) return rc;
+    if (!d_weight || !d_dweight) return LOCO_ERR_ARG;
+    if (!aligned(d_dweight, 4)) return LOCO_ERR_ALIGN;
+    MoveParams P{};
+    int vec = c->dtype == LOCO_BF16 ? 8 : 4;
+    if ((rc = take_rows(c, dy, c->tokens, false, vec, P.in_stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(c, rows, c->rows, false, vec, P.rows_stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(c, drows, c->rows, true, vec, P.rows_out_stride)) != LOCO_OK) return rc;
+    P.in = dy->ptr;
+    P.rows = rows->ptr;
+    P.rows_out = drows->ptr;
+    P.place = d_place;
+    P.weight = d_weight;
+    P.dweight = d_dweight;
+    return launch_move(kBackward, P, c, vec, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,408 @@
+// The products of every expert's rows with its matrix, and the gradient of the matrices, on the tensor cores.
+//
+// One block to an SM takes tiles of 128 x kCols outputs, one after the other, expert by expert; where an expert's rows begin is
+// known on the device only.  One warp copies 64 of the contraction at a time to a ring in shared memory (TMA, 128-byte
+// swizzle), one issues the products, four write the accumulator out while the next tile's products run into the other half of
+// TMEM.
+//   product   A is 128 rows of x, B is of the expert's matrix, either way round.  Rows of a tile past the expert's last belong to
+//             the next expert (or are the copy's zero fill): what they give is in accumulator rows that are not written.
+//   weights   A and B are rows of a and b, contracted along the rows.  Rows past the expert's last are zeroed in shared memory
+//             in both, so that whatever lies there (NaN included) adds nothing.
+#include <cuda.h>
+
+#include "layer_maps.h"
+#include "layer_tc.cuh"
+
+namespace loco_layer {
+
+using namespace tc;
+
+constexpr int kMostExperts = 512;
+constexpr int kTileRows = 128;                   // of the accumulator
+constexpr int kStep = 64;                        // of the contraction: a swizzled row of 128 bytes
+constexpr int kProductThreads = 256;
+constexpr int kLoadWarp = 0, kIssueWarp = 1, kWriteWarps = 4;      // the last four write; lanes of TMEM go by the warp's number modulo 4
+
+__device__ unsigned g_product_status;            // LOCO_LAYER_FLAG_*
+
+struct ProductMaps { CUtensorMap a, b; };
+struct ProductParams {
+    const int32_t *offsets;
+    __nv_bfloat16 *out;
+    int64_t out_expert, out_row, rows;
+    int32_t experts, deep, high, wide;           // contraction (product), rows of an output matrix (weights), columns of the output
+};
+
+constexpr int kMostStages = 8;
+struct ProductShared {
+    uint64_t full[kMostStages], empty[kMostStages], ready[2], written[2], drain;
+    uint32_t tmem, failed;
+    int32_t begin[kMostExperts], count[kMostExperts], first[kMostExperts + 1];      // rows of an expert, its tiles before
+};
+constexpr int kStageOut = 32 * 128;              // bytes a writing warp puts 32 rows of 64 columns in
+template <int kCols> __host__ __device__ constexpr int stage_bytes() { return (kTileRows + kCols) * 128; }
+template <int kCols> __host__ __device__ constexpr int stages() {
+    constexpr int n = (227 * 1024 - 1024 - kWriteWarps * kStageOut - static_cast<int>(sizeof(ProductShared))) / stage_bytes<kCols>();
+    return n < kMostStages ? n : kMostStages;
+}
+template <int kCols> constexpr int product_bytes() {
+    return 1024 + stages<kCols>() * stage_bytes<kCols>() + kWriteWarps * kStageOut + static_cast<int>(sizeof(ProductShared));
+}
+static_assert(product_bytes<256>() <= 227 * 1024 && product_bytes<64>() <= 227 * 1024, "shared memory of a block");
+
+__device__ __forceinline__ void load_box3(uint32_t to, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
+// Where the tiles are.  `walk` goes on to the tile's expert; tiles only grow.
+struct Tile {
+    int expert, row, col, rows, steps;           // first row within the expert (product) or the matrix (weights), columns; rows of the expert, steps of the contraction
+};
+template <bool kWeights, int kCols> struct Walk {
+    int expert = 0;
+    __device__ __forceinline__ Tile at(const ProductShared &S, const ProductParams &P, int tile) {
+        const int across = (P.wide + kCols - 1) / kCols;
+        if constexpr (kWeights) {
+            const int down = (P.high + kTileRows - 1) / kTileRows, each = down * across;
+            expert = tile / each;
+            const int r = tile - expert * each, n = S.count[expert];
+            return Tile{expert, r % down * kTileRows, r / down * kCols, n, (n + kStep - 1) / kStep};
+        } else {
+            while (tile >= S.first[expert + 1] * across) ++expert;
+            const int down = S.first[expert + 1] - S.first[expert], r = tile - S.first[expert] * across;
+            // bands of eight tiles of rows, column by column, so that the blocks at work share rows and columns in L2
+            const int band = r / (8 * across), high = min(8, down - band * 8), q = r - band * 8 * across;
+            return Tile{expert, (band * 8 + q % high) * kTileRows, q / high * kCols, S.count[expert], (P.deep + kStep - 1) / kStep};
+        }
+    }
+};
+
+__device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
+    const uint64_t begin = now_ns();
+    while (!bar_test(bar, parity) && now_ns() - begin < kWaitLimitNs / 20) {}
+}
+
+// kDown: B's rows are the contraction (matrices [in, out], and weights), else its columns.
+template <bool kWeights, bool kDown, int kCols>
+__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
+    constexpr int kStages = stages<kCols>(), kBytes = stage_bytes<kCols>();
+    constexpr uint32_t kTmem = 2 * kCols < 32 ? 32 : 2 * kCols;
+    extern __shared__ uint8_t raw[];
+    uint8_t *const ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint8_t *const staging = ring + kStages * kBytes;
+    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * kStageOut);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    volatile uint32_t *const failed = &S.failed;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            bar_init(smem_addr(&S.full[i]), 1);
+            bar_init(smem_addr(&S.empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_addr(&S.ready[i]), 1);
+            bar_init(smem_addr(&S.written[i]), kWriteWarps);
+        }
+        bar_init(smem_addr(&S.drain), 1);
+        S.failed = 0;
+        fence_bar_init();
+        fence_async_shared();
+    }
+    if (warp == kIssueWarp) tmem_alloc<kTmem>(smem_addr(&S.tmem));
+    wait_for_previous();
+    let_next_start();
+    for (int e = threadIdx.x; e < P.experts; e += kProductThreads) {       // offsets are clamped to the tensor, whatever they hold
+        const int64_t lo = min(max(static_cast<int64_t>(P.offsets[e]), static_cast<int64_t>(0)), P.rows);
+        const int64_t hi = min(max(static_cast<int64_t>(P.offsets[e + 1]), lo), P.rows);
+        S.begin[e] = static_cast<int>(lo);
+        S.count[e] = static_cast<int>(hi - lo);
+    }
+    __syncthreads();
+    if (warp == 0) {                             // tiles of rows before each expert
+        int before = 0;
+        for (int e0 = 0; e0 < P.experts; e0 += 32) {
+            const int e = e0 + lane;
+            int n = e < P.experts ? (S.count[e] + kTileRows - 1) / kTileRows : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, n, o);
+                n += lane >= o ? y : 0;
+            }
+            if (e < P.experts) S.first[e + 1] = before + n;
+            before += __shfl_sync(0xffffffffu, n, 31);
+        }
+        if (lane == 0) S.first[0] = 0;
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = S.tmem;
+    const int across = (P.wide + kCols - 1) / kCols;
+    const int tiles = kWeights ? P.experts * ((P.high + kTileRows - 1) / kTileRows) * across : S.first[P.experts] * across;
+    const int stride = static_cast<int>(gridDim.x);
+    const uint32_t base = smem_addr(ring);
+    Walk<kWeights, kCols> walk;
+
+    if (warp == kLoadWarp) {
+        if (lane == 0) {
+            int slot = 0, phase = 0, issued = 0;
+            for (int tile = blockIdx.x; tile < tiles && !*failed; tile += stride) {
+                const Tile t = walk.at(S, P, tile);
+                const int begin = S.begin[t.expert];
+                for (int k = 0; k < t.steps; ++k) {
+                    bar_wait(smem_addr(&S.empty[slot]), phase ^ 1, failed);
+                    if (*failed) break;
+                    const uint32_t a = base + slot * kBytes, b = a + kTileRows * 128, bar = smem_addr(&S.full[slot]);
+                    bar_expect(bar, kBytes);
+                    if constexpr (kWeights) {
+#pragma unroll
+                        for (int x = 0; x < kTileRows; x += 64) load_box3(a + x * 128, &M.a, t.row + x, begin + k * kStep, 0, bar);
+#pragma unroll
+                        for (int x = 0; x < kCols; x += 64) load_box3(b + x * 128, &M.b, t.col + x, begin + k * kStep, 0, bar);
+                    } else {
+                        load_box3(a, &M.a, k * kStep, begin + t.row, 0, bar);
+                        if constexpr (kDown) {
+#pragma unroll
+                            for (int x = 0; x < kCols; x += 64) load_box3(b + x * 128, &M.b, t.col + x, k * kStep, t.expert, bar);
+                        } else {
+                            load_box3(b, &M.b, k * kStep, t.col, t.expert, bar);
+                        }
+                    }
+                    ++issued;
+                    if (++slot == kStages) {
+                        slot = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            if (*failed)                         // copies in flight end before the block's shared memory goes away
+                for (int i = 0; i < kStages && i < issued; ++i) {
+                    slot = slot ? slot - 1 : kStages - 1;
+                    if (slot == kStages - 1) phase ^= 1;
+                    settle(smem_addr(&S.full[slot]), phase);
+                }
+        }
+    } else if (warp == kIssueWarp) {
+        const uint32_t lead = elect_lane();
+        constexpr uint32_t word = product(kCols, kDown || kWeights) | (kWeights ? 1u << 15 : 0u);
+        int slot = 0, phase = 0, buffer = 0, turn = 0;
+        for (int tile = blockIdx.x; tile < tiles; tile += stride) {
+            const Tile t = walk.at(S, P, tile);
+            if (t.steps == 0) continue;
+            bar_wait(smem_addr(&S.written[buffer]), turn ^ 1, failed);
+            fence_after();
+            for (int k = 0; k < t.steps; ++k) {
+                bar_wait(smem_addr(&S.full[slot]), phase, failed);
+                __syncwarp();
+                const int left = t.rows - k * kStep;
+                if (kWeights && left < kStep) {  // rows past the expert's last
+                    uint4 *const at = reinterpret_cast<uint4 *>(ring + slot * kBytes);
+                    for (int x = 0; x < (kTileRows + kCols) / 64; ++x)
+                        for (int i = left * 8 + lane; i < kStep * 8; i += 32) at[x * (kStep * 8) + i] = make_uint4(0, 0, 0, 0);
+                    fence_async_shared();
+                    __syncwarp();
+                }
+                fence_after();
+                const uint32_t a = base + slot * kBytes, b = a + kTileRows * 128;
+                const uint32_t da = kWeights ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
+                const uint32_t db = kWeights || kDown ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
+#pragma unroll
+                for (int x = 0; x < kStep; x += 16)
+                    mma_ss(lead, tmem + buffer * kCols, da + (kWeights ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights || kDown ? x * 128 >> 4 : x * 2 >> 4), word,
+                           k > 0 || x > 0);
+                commit(lead, smem_addr(&S.empty[slot]));
+                if (++slot == kStages) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+            }
+            commit(lead, smem_addr(&S.ready[buffer]));
+            buffer ^= 1;
+            if (buffer == 0) turn ^= 1;
+        }
+        commit(lead, smem_addr(&S.drain));
+        bar_wait(smem_addr(&S.drain), 0, failed);
+        if (*failed) settle(smem_addr(&S.drain), 0);
+    } else if (warp >= kWriteWarps) {
+        const int part = warp % 4;
+        uint8_t *const stage = staging + part * kStageOut;
+        int buffer = 0, turn = 0;
+        for (int tile = blockIdx.x; tile < tiles; tile += stride) {
+            const Tile t = walk.at(S, P, tile);
+            const int limit = kWeights ? P.high : t.rows;
+            const int live = min(limit - t.row - part * 32, 32);         // rows of this warp that are written
+            __nv_bfloat16 *const out = P.out + (kWeights ? t.expert * P.out_expert : S.begin[t.expert] * P.out_row) + (t.row + part * 32ll) * P.out_row;
+            if (t.steps > 0) {
+                bar_wait(smem_addr(&S.ready[buffer]), turn, failed);
+                __syncwarp();
+                fence_after();
+            }
+            const int cols = min(kCols, P.wide - t.col);
+            for (int c = 0; c < kCols; c += 64) {
+                if (t.steps > 0) {
+                    uint32_t r[2][32];
+                    const uint32_t at = tmem + buffer * kCols + c + (static_cast<uint32_t>(part * 32) << 16);
+                    load_columns(at, r[0]);
+                    load_columns(at + 32, r[1]);
+                    wait_loads();
+                    pin(r[0]);
+                    pin(r[1]);
+                    if (c + 64 >= kCols) {
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_addr(&S.written[buffer]));
+                    }
+#pragma unroll
+                    for (int i = 0; i < 64; i += 8) {
+                        uint4 w;
+                        const uint32_t *f = &r[i / 32][i % 32];
+                        w.x = pack_bf16(__uint_as_float(f[0]), __uint_as_float(f[1]));
+                        w.y = pack_bf16(__uint_as_float(f[2]), __uint_as_float(f[3]));
+                        w.z = pack_bf16(__uint_as_float(f[4]), __uint_as_float(f[5]));
+                        w.w = pack_bf16(__uint_as_float(f[6]), __uint_as_float(f[7]));
+                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i / 8 ^ lane % 8) << 4)) = w;
+                    }
+                    __syncwarp();
+                }
+                const int piece = lane % 8, col = c + piece * 8;
+                if (col < cols)
+                    for (int row = lane / 8; row < live; row += 4)
+                        *reinterpret_cast<uint4 *>(out + row * P.out_row + t.col + col) =
+                            t.steps > 0 ? *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ row % 8) << 4)) : make_uint4(0, 0, 0, 0);
+                __syncwarp();
+            }
+            if (t.steps > 0) {
+                buffer ^= 1;
+                if (buffer == 0) turn ^= 1;
+            }
+        }
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == kIssueWarp) tmem_free<kTmem>(tmem);
+    if (threadIdx.x == 0 && S.failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
+}
+
+namespace {
+
+using ProductKernel = void (*)(const ProductParams, const ProductMaps);
+
+// Shared-memory limit of a kernel, set once per device.
+bool allow(ProductKernel fn, int which, int bytes) {
+    static std::atomic<bool> set[64][8];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return false;
+    }
+    if (set[dev][which].load(std::memory_order_acquire)) return true;
+    if (cudaFuncSetAttribute(reinterpret_cast<const void *>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    set[dev][which].store(true, std::memory_order_release);
+    return true;
+}
+
+// [slabs, rows, columns] in boxes of `box_rows` rows by 64 columns.
+bool make_map(CUtensorMap &map, void *at, int64_t columns, int64_t rows, int64_t slabs, int64_t row_stride, int64_t slab_stride, int box_rows) {
+    const cuuint64_t size[3] = {static_cast<cuuint64_t>(columns), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(slabs)};
+    // the stride of a single row or matrix means nothing, but has to be a valid one
+    const cuuint64_t strides[2] = {rows > 1 ? static_cast<cuuint64_t>(row_stride) * 2 : 256, slabs > 1 ? static_cast<cuuint64_t>(slab_stride) * 2 : 256};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1};
+    return encode_map(map, 3, at, size, strides, box);
+}
+
+int check_product(const loco_product_t *c, const int32_t *offsets) {
+    if (!c) return LOCO_ERR_ARG;
+    if (c->experts < 1 || c->experts > kMostExperts || c->rows < 0 || c->rows > 0x7fffffff || c->d_in < 1 || c->d_out < 1) return LOCO_ERR_ARG;
+    if (c->d_in % 8 || c->d_out % 8) return LOCO_ERR_UNSUPPORTED;
+    if (!offsets) return LOCO_ERR_ARG;
+    return aligned(offsets, 4) ? LOCO_OK : LOCO_ERR_ALIGN;
+}
+
+// Rows or matrices: present, on 16-byte boundaries, strides of whole 16-byte units below the copies' limit; an output's do not overlap.
+constexpr int64_t kMostStride = 1ll << 38;
+int check_rows(const loco_rows_t *t, int64_t rows, int64_t dim, bool written) {
+    if (!t || !t->ptr) return LOCO_ERR_ARG;
+    if (!aligned(t->ptr, 16)) return LOCO_ERR_ALIGN;
+    if (rows <= 1) return LOCO_OK;
+    if (t->row_stride < 0 || t->row_stride > kMostStride || (written && t->row_stride < dim)) return LOCO_ERR_ARG;
+    return t->row_stride % 8 ? LOCO_ERR_ALIGN : LOCO_OK;
+}
+int check_matrices(const loco_matrices_t *t, int64_t experts, int64_t rows, int64_t columns, bool written) {
+    if (!t || !t->ptr) return LOCO_ERR_ARG;
+    if (!aligned(t->ptr, 16)) return LOCO_ERR_ALIGN;
+    if (rows > 1) {
+        if (t->row_stride < 0 || t->row_stride > kMostStride || (written && t->row_stride < columns)) return LOCO_ERR_ARG;
+        if (t->row_stride % 8) return LOCO_ERR_ALIGN;
+    }
+    if (experts > 1) {
+        const int64_t span = (rows > 1 ? (rows - 1) * t->row_stride : 0) + columns;
+        if (t->expert_stride < 0 || t->expert_stride > kMostStride || (written && t->expert_stride < span)) return LOCO_ERR_ARG;
+        if (t->expert_stride % 8) return LOCO_ERR_ALIGN;
+    }
+    return LOCO_OK;
+}
+
+template <bool kWeights, bool kDown, int kCols> int launch_product(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
+    const int sms = sm_count();
+    if (sms == 0) return LOCO_ERR_CUDA;
+    if (tiles > 0x7fffffff - sms) return LOCO_ERR_UNSUPPORTED;
+    constexpr ProductKernel fn = product_kernel<kWeights, kDown, kCols>;
+    if (!allow(fn, which, product_bytes<kCols>())) return LOCO_ERR_CUDA;
+    return launch_kernel(fn, dim3(static_cast<unsigned>(tiles < sms ? tiles : sms)), kProductThreads, product_bytes<kCols>(), stream, P, M);
+}
+
+int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace
+
+// Read by loco_layer_status, which is also built without this file.
+int more_status(unsigned *flags, cudaStream_t stream) {
+    return cudaMemcpyFromSymbolAsync(flags, g_product_status, sizeof(*flags), 0, cudaMemcpyDeviceToHost, stream) == cudaSuccess ? 0 : 1;
+}
+
+}  // namespace loco_layer
+
+using namespace loco_layer;
+
+extern "C" {
+
+int loco_experts_product(const loco_product_t *c, const loco_rows_t *x, const loco_matrices_t *w, const int32_t *d_offsets, const loco_rows_t *y, void *stream) {
+    int rc = check_product(c, d_offsets);
+    if (rc != LOCO_OK || c->rows == 0) return rc;
+    const bool turned = c->transposed != 0;
+    const int64_t rows = turned ? c->d_out : c->d_in, columns = turned ? c->d_in : c->d_out;
+    if ((rc = check_rows(x, c->rows, c->d_in, false)) != LOCO_OK || (rc = check_rows(y, c->rows, c->d_out, true)) != LOCO_OK ||
+        (rc = check_matrices(w, c->experts, rows, columns, false)) != LOCO_OK) return rc;
+    ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(y->ptr), 0, c->rows > 1 ? y->row_stride : 0, c->rows, c->experts, c->d_in, 0, c->d_out};
+    ProductMaps M;
+    constexpr int kCols = 256;
+    if (!make_map(M.a, x->ptr, c->d_in, c->rows, 1, x->row_stride, 0, kTileRows) ||
+        !make_map(M.b, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? kCols : kStep)) return LOCO_ERR_CUDA;
+    // every expert may end in a tile of its own
+    const int64_t tiles = (c->rows / kTileRows + (c->rows < c->experts ? c->rows : c->experts)) * over(c->d_out, kCols);
+    return turned ? launch_product<false, false, kCols>(P, M, tiles, 0, stream) : launch_product<false, true, kCols>(P, M, tiles, 1, stream);
+}
+
+int loco_experts_product_weights(const loco_product_t *c, const loco_rows_t *a, const loco_rows_t *b, const int32_t *d_offsets, const loco_matrices_t *dw,
+                                 void *stream) {
+    int rc = check_product(c, d_offsets);
+    if (rc != LOCO_OK) return rc;
+    if ((rc = check_matrices(dw, c->experts, c->d_in, c->d_out, true)) != LOCO_OK) return rc;
+    if (c->rows > 0 && ((rc = check_rows(a, c->rows, c->d_in, false)) != LOCO_OK || (rc = check_rows(b, c->rows, c->d_out, false)) != LOCO_OK)) return rc;
+    ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(dw->ptr), c->experts > 1 ? dw->expert_stride : 0, c->d_in > 1 ? dw->row_stride : 0, c->rows, c->experts,
+                    0, c->d_in, c->d_out};
+    ProductMaps M;
+    constexpr int kCols = 256;
+    // without rows nothing is read: the maps need a valid address all the same
+    const bool none = c->rows == 0;
+    if (!make_map(M.a, none ? dw->ptr : a->ptr, c->d_in, none ? 1 : c->rows, 1, none ? 0 : a->row_stride, 0, kStep) ||
+        !make_map(M.b, none ? dw->ptr : b->ptr, c->d_out, none ? 1 : c->rows, 1, none ? 0 : b->row_stride, 0, kStep)) return LOCO_ERR_CUDA;
+    return launch_product<true, true, kCols>(P, M, c->experts * over(c->d_in, kTileRows) * over(c->d_out, kCols), 2, stream);
+}
+
+}  // extern "C"

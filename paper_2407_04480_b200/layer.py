@@ -28,7 +28,10 @@ SCALINGS = {"plain": ROTARY_PLAIN, "linear": ROTARY_LINEAR, "parts": ROTARY_PART
 
 EXPORTS = ("loco_rotary_table", "loco_rotary_apply", "loco_attention_forward", "loco_attention_backward",
            "loco_attention_backward_workspace_bytes", "loco_router_workspace_bytes", "loco_router_forward",
-           "loco_router_backward", "loco_layer_status", "loco_layer_launch_count")
+           "loco_router_backward", "loco_norm_forward", "loco_norm_backward", "loco_norm_backward_workspace_bytes",
+           "loco_experts_sort", "loco_experts_sort_workspace_bytes", "loco_experts_dispatch", "loco_experts_combine",
+           "loco_experts_combine_backward", "loco_experts_product", "loco_experts_product_weights", "loco_gradient_squares",
+           "loco_gradient_squares_workspace_bytes", "loco_gradient_clip", "loco_layer_status", "loco_layer_launch_count")
 FLAG_TIMEOUT = 1
 
 # the C structures, packed in one go
@@ -37,6 +40,12 @@ _TABLE = struct.Struct("@iiiffffff")                  # loco_rotary_table_t
 _ROTARY = struct.Struct("@iiiiiiiii")                 # loco_rotary_t
 _ATTENTION = struct.Struct("@iiiiiiiiiif4xPP")        # loco_attention_t
 _ROUTER = struct.Struct("@iiiiff")                    # loco_router_t
+_ROWS = struct.Struct("@Pq")                          # loco_rows_t
+_NORM = struct.Struct("@iiiif")                       # loco_norm_t
+_EXPERTS = struct.Struct("@iii4xqq")                  # loco_experts_t
+_MATRICES = struct.Struct("@Pqq")                     # loco_matrices_t
+_PRODUCT = struct.Struct("@i4xqiii4x")                # loco_product_t
+_SPAN = struct.Struct("@PPQi4x")                      # loco_span_t
 
 _lib = None
 
@@ -58,6 +67,19 @@ def lib() -> C.CDLL:
         L.loco_router_workspace_bytes.argtypes = [st]
         L.loco_router_forward.argtypes = [st, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, u64, vp]
         L.loco_router_backward.argtypes = [st, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.loco_norm_forward.argtypes = [st, i64, st, st, vp, st, st, vp, vp]
+        L.loco_norm_backward.argtypes = [st, i64, st, st, vp, st, st, vp, vp, u64, vp]
+        L.loco_norm_backward_workspace_bytes.argtypes = [st]
+        L.loco_experts_sort.argtypes = [i32, i64, i32, vp, vp, vp, vp, u64, vp]
+        L.loco_experts_sort_workspace_bytes.argtypes = [i32]
+        L.loco_experts_dispatch.argtypes = [st, st, vp, st, vp]
+        L.loco_experts_combine.argtypes = [st, st, vp, vp, st, vp]
+        L.loco_experts_combine_backward.argtypes = [st, st, st, vp, vp, st, vp, vp]
+        L.loco_experts_product.argtypes = [st, st, st, vp, st, vp]
+        L.loco_experts_product_weights.argtypes = [st, st, st, vp, st, vp]
+        L.loco_gradient_squares.argtypes = [st, i32, vp, vp, u64, vp]
+        L.loco_gradient_squares_workspace_bytes.argtypes = []
+        L.loco_gradient_clip.argtypes = [st, i32, vp, C.c_double, vp, vp]
         L.loco_layer_status.argtypes = [C.POINTER(C.c_uint32), vp]
         L.loco_layer_launch_count.argtypes = []
         for name in EXPORTS:
@@ -198,6 +220,91 @@ def loco_router_backward(cfg: Router, logits, index, counts, dlogits, mask=None,
     """Gradient of the logits from those of the two losses (fp32 [2]) and of the weights (fp32 [tokens, top_k])."""
     _check(_binding().router_backward(cfg.experts, cfg.top_k, cfg.normalize, cfg.balance_coef, cfg.z_coef, logits, index, counts,
                                       dlogits, mask, dlosses, dweights, _raw(stream)), "loco_router_backward")
+
+
+# ---- norm ------------------------------------------------------------------------------------
+
+def loco_norm_forward(x, y, weight=None, residual=None, total=None, scale=None, block: int = 0, eps: float = 1e-5, stream=None) -> None:
+    """y = the root-mean-square norm of x + residual, times weight; total = x + residual as it is kept, in the type of x.
+
+    x, residual, total, y: [rows, dim]; weight [dim].  y in float8_e4m3fn: with scale fp32 [rows, ceil(dim / block)], a scale
+    for every 128 columns (block=128) or [rows, 1] (block=0); y * scale is the norm's output."""
+    _check(_binding().norm_forward(x, y, weight, residual, total, scale, block, eps, _raw(stream)), "loco_norm_forward")
+
+
+def loco_norm_backward_workspace_bytes(dim: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    """Bytes of loco_norm_backward's workspace for rows of `dim` elements."""
+    return int(lib().loco_norm_backward_workspace_bytes(_NORM.pack(BF16 if dtype == torch.bfloat16 else 0, dim, 0, 0, 0.0)))
+
+
+def loco_norm_backward(h, dy, dx, work=None, weight=None, dweight=None, dtotal=None, eps: float = 1e-5, stream=None) -> None:
+    """Gradient of x (and of the residual alike) and of the weight, from h, what the norm was taken of (x + residual, or x).
+
+    dtotal: the gradient that reaches h past the norm.  work: a CUDA tensor of loco_norm_backward_workspace_bytes() bytes,
+    needed with dweight."""
+    _check(_binding().norm_backward(h, dy, dx, work, weight, dweight, dtotal, eps, _raw(stream)), "loco_norm_backward")
+
+
+# ---- experts ---------------------------------------------------------------------------------
+
+def loco_experts_sort_workspace_bytes(experts: int) -> int:
+    return int(lib().loco_experts_sort_workspace_bytes(experts))
+
+
+def loco_experts_sort(index, offsets, place, work, stream=None) -> None:
+    """Sort the router's choices index (int32 [tokens, top_k]) by expert, then token, then slot.
+
+    offsets: int32 [experts + 1], the first row of every expert, then the number of rows; place: int32 [tokens, top_k], the
+    row of a choice or -1; work: a CUDA tensor of loco_experts_sort_workspace_bytes() bytes."""
+    _check(_binding().experts_sort(index, offsets, place, work, _raw(stream)), "loco_experts_sort")
+
+
+def loco_experts_dispatch(x, place, rows, stream=None) -> None:
+    """rows[place[t, j]] = x[t]; x [tokens, dim], rows [rows, dim].  Rows that no choice has are left as they are."""
+    _check(_binding().experts_dispatch(x, place, rows, _raw(stream)), "loco_experts_dispatch")
+
+
+def loco_experts_combine(rows, place, y, weight=None, stream=None) -> None:
+    """y[t] = sum over j of weight[t, j] * rows[place[t, j]]; weight: fp32 [tokens, top_k], None for ones."""
+    _check(_binding().experts_combine(rows, place, y, weight, _raw(stream)), "loco_experts_combine")
+
+
+def loco_experts_combine_backward(dy, rows, place, weight, drows, dweight, stream=None) -> None:
+    """drows[place[t, j]] = weight[t, j] * dy[t] and dweight[t, j] = dy[t] . rows[place[t, j]] (fp32)."""
+    _check(_binding().experts_combine_backward(dy, rows, place, weight, drows, dweight, _raw(stream)), "loco_experts_combine_backward")
+
+
+def loco_experts_product(x, w, offsets, y, transposed: bool = False, stream=None) -> None:
+    """y[t] = x[t] @ w[e] for the rows t of every expert e, offsets[e] to offsets[e + 1]; bfloat16.
+
+    x [rows, d_in], y [rows, d_out], w [experts, d_in, d_out], or [experts, d_out, d_in] and transposed.  The gradient of x is
+    the same call on dy the other way round.  Rows outside every expert are left as they are."""
+    _check(_binding().experts_product(x, w, offsets, y, transposed, _raw(stream)), "loco_experts_product")
+
+
+def loco_experts_product_weights(a, b, offsets, dw, stream=None) -> None:
+    """dw[e] = a[rows of e]^T @ b[rows of e], [experts, a's columns, b's columns]; zeros for an expert without rows."""
+    _check(_binding().experts_product_weights(a, b, offsets, dw, _raw(stream)), "loco_experts_product_weights")
+
+
+# ---- gradient --------------------------------------------------------------------------------
+
+def loco_gradient_squares_workspace_bytes() -> int:
+    return int(lib().loco_gradient_squares_workspace_bytes())
+
+
+def loco_gradient_squares(gradients, squares, work, stream=None) -> None:
+    """squares (fp64 [1]) = the sum of squares over a list of contiguous gradients (bfloat16 or fp32, of any shapes).
+
+    work: a CUDA tensor of loco_gradient_squares_workspace_bytes() bytes, zero before its first use."""
+    _check(_binding().gradient_squares(gradients, squares, work, _raw(stream)), "loco_gradient_squares")
+
+
+def loco_gradient_clip(gradients, outputs, squares, norm, max_norm: float, stream=None) -> None:
+    """outputs = gradients times max_norm / sqrt(squares) where that is below one; norm (fp32 [1], or None) = sqrt(squares).
+
+    An output may be its gradient itself; where nothing is to be scaled nothing is written to it then."""
+    _check(_binding().gradient_clip(gradients, outputs, squares, norm, max_norm, _raw(stream)), "loco_gradient_clip")
 
 
 # ---- differentiable forms --------------------------------------------------------------------
