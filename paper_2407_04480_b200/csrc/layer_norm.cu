@@ -1,19 +1,26 @@
 // Root-mean-square norm with the residual's addition, and its gradient: a row is read once into registers by a team of
 // threads, summed over the team and written.
 //
-// Some ten operations per element read, so the bound is HBM.  A team is 4 to 32 lanes for rows of up to 512 elements, several
-// teams to a block, and a whole block above; the weight stays in registers from row to row.
+// Some ten operations per element read, so the bound is HBM.  A team is 4 to 32 lanes for short rows and up to a block's 1024
+// threads for long ones; a block holds as many teams as fit, its blocks go round the rows, and the weight stays in registers
+// from row to row.  The next row is on its way while one is worked on: every thread copies its own part of it to shared
+// memory (cp.async) and reads nobody else's, so the copies need no barrier.  With the next row in registers instead the
+// backward kernel spilled what it waited for: 8192 rows of 4096, bfloat16, 99 us.
 #include <cuda_fp8.h>
 
+#include <cstring>
+
 #include "layer_common.h"
+#include "layer_tc.cuh"
 
 namespace loco_layer {
 
 constexpr int kMaxDim = 16384;
-constexpr int kNormThreads = 512;                // most threads of a block
-constexpr int kSmallBlock = 256;                 // threads of a block of several teams
+constexpr int kNormThreads = 1024;               // most threads of a block, and threads of an SM
+constexpr int kBlockThreads = 512;               // of a block of several teams
 constexpr int kPartials = 444;                   // most blocks of the backward kernel, each leaves a partial row of dw
 constexpr int kScaleBlock = 128;
+constexpr int kRingBytes = 200 * 1024;           // shared memory of an SM for rows on their way
 constexpr float kLargestE4m3 = 448.0f, kLeastScale = 1.17549435e-38f;
 constexpr unsigned kAll = 0xffffffffu;
 
@@ -22,44 +29,67 @@ struct NormParams {
     void *h, *y, *dx;
     float *scale, *part;
     int64_t xs, rs, hs, ys, dys, dts, dxs, rows;
-    int32_t dim, team, block, groups, wanted;
+    int32_t dim, team, block, groups, wanted, depth;
     float eps, over_dim;
 };
 
-template <typename T, int V> __device__ __forceinline__ void unpack(const Pack<T, V> &p, float *out) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) out[i] = to_f32(p.v[i]);
-}
+// The threads that share a row: a part of a warp, or several warps, which then have a barrier of their own.
+struct Team {
+    int size, lane, mine, all;                   // threads, this one's place; the team's place in the block, teams
+    int shift;                                   // elements between the 16-byte boundary before a row and the row, the same for all of the team's
+    __device__ __forceinline__ Team(const NormParams &P, int vec)
+        : size(P.team), lane(static_cast<int>(threadIdx.x) % P.team), mine(static_cast<int>(threadIdx.x) / P.team), all(static_cast<int>(blockDim.x) / P.team),
+          shift(static_cast<int>((static_cast<int64_t>(blockIdx.x) * all + mine) * P.xs % vec)) {}
+    __device__ __forceinline__ void sync() const {
+        if (size > 32) asm volatile("bar.sync %0, %1;" ::"r"(mine + 1), "r"(size) : "memory");
+        else __syncwarp();
+    }
+};
 
-// Sum over the team, the same in every lane of it; a team above a warp is the block, whose every thread calls.
-__device__ __forceinline__ float2 team_sum(float2 s, int team, float2 *fold) {
-    for (int o = (team < 32 ? team : 32) / 2; o; o >>= 1) {
+// Sums over the team, the same in every lane of it.  `fold` has a place for every warp of the block.
+__device__ __forceinline__ float2 team_sum(float2 s, const Team &t, float2 *fold) {
+    for (int o = (t.size < 32 ? t.size : 32) / 2; o; o >>= 1) {
         s.x += __shfl_xor_sync(kAll, s.x, o);
         s.y += __shfl_xor_sync(kAll, s.y, o);
     }
-    if (team > 32) {
-        const int warps = team / 32;
-        __syncthreads();                         // what the call before left has been read
+    if (t.size > 32) {
+        const int warps = t.size / 32, first = t.mine * warps;
+        t.sync();                                // what the call before left has been read
         if (threadIdx.x % 32 == 0) fold[threadIdx.x / 32] = s;
-        __syncthreads();
-        s = make_float2(0.0f, 0.0f);
-        for (int i = 0; i < warps; ++i) {
-            s.x += fold[i].x;
-            s.y += fold[i].y;
+        t.sync();
+        s = threadIdx.x % 32 < warps ? fold[first + threadIdx.x % 32] : make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            s.x += __shfl_xor_sync(kAll, s.x, o);
+            s.y += __shfl_xor_sync(kAll, s.y, o);
         }
     }
     return s;
 }
+__device__ __forceinline__ float team_sum(float s, const Team &t, float2 *fold) {
+    for (int o = (t.size < 32 ? t.size : 32) / 2; o; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
+    if (t.size > 32) {
+        const int warps = t.size / 32, first = t.mine * warps;
+        t.sync();
+        if (threadIdx.x % 32 == 0) fold[threadIdx.x / 32].x = s;
+        t.sync();
+        s = threadIdx.x % 32 < warps ? fold[first + threadIdx.x % 32].x : 0.0f;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
+    }
+    return s;
+}
 // Largest of the bits of values without a sign: their order is that of the values, NaN above infinity.
-__device__ __forceinline__ unsigned team_max(unsigned m, int team, unsigned *fold) {
-    for (int o = (team < 32 ? team : 32) / 2; o; o >>= 1) m = max(m, __shfl_xor_sync(kAll, m, o));
-    if (team > 32) {
-        const int warps = team / 32;
-        __syncthreads();
+__device__ __forceinline__ unsigned team_max(unsigned m, const Team &t, unsigned *fold) {
+    for (int o = (t.size < 32 ? t.size : 32) / 2; o; o >>= 1) m = max(m, __shfl_xor_sync(kAll, m, o));
+    if (t.size > 32) {
+        const int warps = t.size / 32, first = t.mine * warps;
+        t.sync();
         if (threadIdx.x % 32 == 0) fold[threadIdx.x / 32] = m;
-        __syncthreads();
-        m = 0;
-        for (int i = 0; i < warps; ++i) m = max(m, fold[i]);
+        t.sync();
+        m = threadIdx.x % 32 < warps ? fold[first + threadIdx.x % 32] : 0;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) m = max(m, __shfl_xor_sync(kAll, m, o));
     }
     return m;
 }
@@ -68,230 +98,416 @@ __device__ __forceinline__ float scale_of(unsigned largest) {
     return m != m ? m : fmaxf(m / kLargestE4m3, kLeastScale);
 }
 
-template <typename T, int V, int kMine, bool kBits8> __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid_constant__ NormParams P) {
-    wait_for_previous();
-    let_next_start();
-    constexpr int kVecs = kMine / V;
+// A thread's part of a row: kMine elements in vectors of V, dealt to the team in turn.  Vectors lie on the tensors' 16-byte
+// boundaries, so that rows of any width are read and written in whole vectors but for the two that hold a row's ends (kShift;
+// without, every row begins and ends on a boundary).
+// Elements are taken two at a time: bfloat16 is converted in pairs, and the sums and products are two to an instruction.
+template <typename T, int V, int kMine, bool kShift> struct Part {
+    static constexpr int kVecs = kMine / V, kPairs = kMine / 2;
     using Vec = Pack<T, V>;
-    __shared__ float2 fold[kNormThreads / 32];
-    __shared__ unsigned most[kBits8 ? 256 : 1];  // a row's or several rows' runs of 128 columns: threads * kMine / 128 of them at most
-    const int team = P.team, lane = static_cast<int>(threadIdx.x) % team, mine = static_cast<int>(threadIdx.x) / team, teams = static_cast<int>(blockDim.x) / team;
-    Vec w[kVecs];
-    if (P.w) {
+    Vec v[kVecs];
+    __device__ __forceinline__ static int column(const Team &t, int i) { return (i * t.size + t.lane) * V - (kShift ? t.shift : 0); }
+    __device__ __forceinline__ static bool inside(const Team &t, int i, int dim) { return column(t, i) < dim; }         // a part of it at least
+    __device__ __forceinline__ static bool whole(const Team &t, int i, int dim) { return !kShift || (column(t, i) >= 0 && column(t, i) + V <= dim); }
+    __device__ __forceinline__ void fill(float x) {
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const int at = (i * team + lane) * V;
-            if (at < P.dim) w[i] = *reinterpret_cast<const Vec *>(static_cast<const T *>(P.w) + at);
+        for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[i].v[j] = from_f32<T>(x);
+    }
+    // element by element where the row's ends are; columns past the row keep what they were filled with
+    __device__ __forceinline__ void load(const T *row, const Team &t, int dim, bool vectors) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+            if (inside(t, i, dim)) {
+                if (vectors && whole(t, i, dim)) {
+                    v[i] = *reinterpret_cast<const Vec *>(row + column(t, i));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (static_cast<unsigned>(column(t, i) + j) < static_cast<unsigned>(dim)) v[i].v[j] = row[column(t, i) + j];
+                }
+            }
+    }
+    __device__ __forceinline__ void store(T *row, const Team &t, int dim) const {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+            if (inside(t, i, dim)) {
+                if (whole(t, i, dim)) {
+                    *reinterpret_cast<Vec *>(row + column(t, i)) = v[i];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (static_cast<unsigned>(column(t, i) + j) < static_cast<unsigned>(dim)) row[column(t, i) + j] = v[i].v[j];
+                }
+            }
+    }
+    // zeros where a vector reaches past the row's ends
+    __device__ __forceinline__ void trim(const Team &t, int dim) {
+        if constexpr (kShift)
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+                if (!whole(t, i, dim))
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (static_cast<unsigned>(column(t, i) + j) >= static_cast<unsigned>(dim)) v[i].v[j] = from_f32<T>(0.0f);
+    }
+    __device__ __forceinline__ float2 operator[](int q) const {
+        if constexpr (V > 1 && sizeof(T) == 2) {
+            uint32_t w;
+            memcpy(&w, &v[2 * q / V].v[2 * q % V], 4);
+            return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        } else {
+            return make_float2(to_f32(v[2 * q / V].v[2 * q % V]), to_f32(v[(2 * q + 1) / V].v[(2 * q + 1) % V]));
         }
     }
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * teams; first < P.rows; first += static_cast<int64_t>(gridDim.x) * teams) {
-        const int64_t row = first + mine;
+    // Keeps pairs of bfloat16 as they are: what is converted before is converted again after, and holds no registers between.
+    __device__ __forceinline__ void keep() {
+        if constexpr (V > 1 && sizeof(T) == 2)
+#pragma unroll
+            for (int q = 0; q < kPairs; ++q) {
+                uint32_t w;
+                memcpy(&w, &v[2 * q / V].v[2 * q % V], 4);
+                asm volatile("" : "+r"(w));
+                memcpy(&v[2 * q / V].v[2 * q % V], &w, 4);
+            }
+    }
+    __device__ __forceinline__ void set(int q, float2 f) {
+        if constexpr (V > 1 && sizeof(T) == 2) {
+            const uint32_t w = tc::pack_bf16(f.x, f.y);
+            memcpy(&v[2 * q / V].v[2 * q % V], &w, 4);
+        } else {
+            v[2 * q / V].v[2 * q % V] = from_f32<T>(f.x);
+            v[(2 * q + 1) / V].v[(2 * q + 1) % V] = from_f32<T>(f.y);
+        }
+    }
+};
+template <typename T> __device__ __forceinline__ const T *row_at(const void *p, int64_t row, int64_t stride) { return static_cast<const T *>(p) + row * stride; }
+template <typename T> __device__ __forceinline__ T *row_at(void *p, int64_t row, int64_t stride) { return static_cast<T *>(p) + row * stride; }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// The rows on their way: for each of `depth` of them the thread's vectors of kTensors tensors, [row][tensor][vector][thread].
+// Single elements (tensors that do not share their boundaries) are read where they are needed instead.
+template <typename T, int V, int kMine, bool kShift, int kTensors> struct Ring {
+    using Row = Part<T, V, kMine, kShift>;
+    using Vec = typename Row::Vec;
+    static constexpr bool kCopies = V > 1;
+    Vec *const at;
+    const int depth;
+    int put = 0, got = 0;
+    __device__ __forceinline__ Ring(void *shared, int rows) : at(static_cast<Vec *>(shared) + threadIdx.x), depth(rows) {}
+    __device__ __forceinline__ Vec *place(int slot, int tensor, int i) const { return at + ((slot * kTensors + tensor) * Row::kVecs + i) * static_cast<int>(blockDim.x); }
+    // A vector with the row's begin has the end of the row before in it (the first row of a tensor begins on a boundary); of the
+    // one with its end only what is the row's is read.
+    __device__ __forceinline__ void copy(int tensor, const T *row, const Team &t, int dim, bool there) {
+        if constexpr (kCopies) {
+#pragma unroll
+            for (int i = 0; i < Row::kVecs; ++i) {
+                const int left = there ? (dim - Row::column(t, i)) * static_cast<int>(sizeof(T)) : 0, bytes = left < 0 ? 0 : left > 16 ? 16 : left;
+                const T *from = bytes ? row + Row::column(t, i) : none;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_addr(place(put, tensor, i))), "l"(from), "r"(bytes) : "memory");
+            }
+        }
+    }
+    const T *none;                               // any address that may be named; nothing is read there
+    __device__ __forceinline__ void sent() {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++put == depth) put = 0;
+    }
+    // the oldest row is there; `depth` rows have been sent
+    __device__ __forceinline__ void wait() const {
+        if (depth == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        else if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 2;" ::: "memory");
+    }
+    __device__ __forceinline__ void next() {
+        if (++got == depth) got = 0;
+    }
+    __device__ __forceinline__ void read(Row &r, int tensor) const {
+#pragma unroll
+        for (int i = 0; i < Row::kVecs; ++i) r.v[i] = *place(got, tensor, i);
+    }
+};
+
+template <typename T, int V, int kMine, bool kShift, bool kBits8>
+__global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid_constant__ NormParams P) {
+    wait_for_previous();
+    let_next_start();
+    using Row = Part<T, V, kMine, kShift>;
+    extern __shared__ __align__(16) uint8_t shared[];
+    __shared__ float2 fold[kNormThreads / 32];
+    __shared__ unsigned most[kBits8 ? 256 : 1];  // a row's or several rows' runs of 128 columns: threads * kMine / 128 of them at most
+    const Team t(P, V);
+    Ring<T, V, kMine, kShift, 2> ring(shared, P.depth);
+    ring.none = static_cast<const T *>(P.x);
+    Row w;
+    w.fill(1.0f);
+    if (P.w) w.load(static_cast<const T *>(P.w), t, P.dim, t.shift == 0);
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * t.all, mine = static_cast<int64_t>(blockIdx.x) * t.all + t.mine;
+    int64_t ahead = mine;
+    const auto send = [&]() {
+        ring.copy(0, row_at<T>(P.x, ahead, P.xs), t, P.dim, ahead < P.rows);
+        if (P.r) ring.copy(1, row_at<T>(P.r, ahead, P.rs), t, P.dim, ahead < P.rows);
+        ring.sent();
+        ahead += stride;
+    };
+    for (int i = 1; i < P.depth; ++i) send();
+    int64_t row = mine;
+    for (int64_t first = row - t.mine; first < P.rows; first += stride, row += stride) {
         const bool there = row < P.rows;
-        const T *x = static_cast<const T *>(P.x) + row * P.xs, *r = static_cast<const T *>(P.r) + row * P.rs;
-        Vec a[kVecs], b[kVecs];
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const int at = (i * team + lane) * V;
-            if (there && at < P.dim) {
-                a[i] = *reinterpret_cast<const Vec *>(x + at);
-                if (P.r) b[i] = *reinterpret_cast<const Vec *>(r + at);
+        send();
+        Row h, r;
+        r.fill(-0.0f);                           // x + -0 is x
+        if constexpr (Ring<T, V, kMine, kShift, 2>::kCopies) {
+            ring.wait();
+            ring.read(h, 0);
+            h.trim(t, P.dim);
+            if (P.r) {
+                ring.read(r, 1);
+                r.trim(t, P.dim);
+            }
+            ring.next();
+        } else {
+            h.fill(0.0f);
+            if (there) {
+                h.load(row_at<T>(P.x, row, P.xs), t, P.dim, true);
+                if (P.r) r.load(row_at<T>(P.r, row, P.rs), t, P.dim, true);
             }
         }
-        float2 sum = make_float2(0.0f, 0.0f);
+        float2 sum = both(0.0f);
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const int at = (i * team + lane) * V;
-            if (there && at < P.dim) {
-                if (P.r) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) a[i].v[j] = from_f32<T>(to_f32(a[i].v[j]) + to_f32(b[i].v[j]));
-                    *reinterpret_cast<Vec *>(static_cast<T *>(P.h) + row * P.hs + at) = a[i];
-                }
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float f = to_f32(a[i].v[j]);
-                    sum.x = fmaf(f, f, sum.x);
-                }
-            }
+        for (int q = 0; q < Row::kPairs; ++q) {
+            h.set(q, tc::add2(h[q], r[q]));
+            sum = tc::fma2(h[q], h[q], sum);
         }
-        const float by = rsqrtf(team_sum(sum, team, fold).x * P.over_dim + P.eps);
+        if (P.r && there) h.store(row_at<T>(P.h, row, P.hs), t, P.dim);
+        h.keep();
+        const float by = rsqrtf(team_sum(sum.x + sum.y, t, fold) * P.over_dim + P.eps);
+        h.keep();
+        w.keep();
         if constexpr (!kBits8) {
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                const int at = (i * team + lane) * V;
-                if (there && at < P.dim) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) a[i].v[j] = from_f32<T>(to_f32(a[i].v[j]) * by * (P.w ? to_f32(w[i].v[j]) : 1.0f));
-                    *reinterpret_cast<Vec *>(static_cast<T *>(P.y) + row * P.ys + at) = a[i];
-                }
-            }
+            for (int q = 0; q < Row::kPairs; ++q) h.set(q, tc::mul2(tc::mul2(h[q], both(by)), w[q]));
+            if (there) h.store(row_at<T>(P.y, row, P.ys), t, P.dim);
         } else {
-            float y[kVecs][V];
-            unsigned m[kVecs];
+            const auto y = [&](int q) { return tc::mul2(tc::mul2(h[q], both(by)), w[q]); };
+            uint32_t out[kMine / 4];             // a byte an element
+            // the largest of the row, or of each run of 128 columns: 16 lanes' vectors where rows begin on the boundaries
+            constexpr bool kLanes = V == 8 && !kShift;
+            const bool lanes = kLanes && t.size >= 32;
+            if (P.block == 0 || lanes) {
+                unsigned m[Row::kVecs], all = 0;
+                float over[Row::kVecs];          // one over the scale
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                const int at = (i * team + lane) * V;
-                m[i] = 0;
-                if (there && at < P.dim) {
+                for (int i = 0; i < Row::kVecs; ++i) {
+                    float x = 0.0f;                                  // NaN where one is
+                    if constexpr (V == 1) {
+                        const float2 f = y(i / 2);
+                        x = fabsf(i % 2 ? f.y : f.x);
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        y[i][j] = to_f32(a[i].v[j]) * by * (P.w ? to_f32(w[i].v[j]) : 1.0f);
-                        m[i] = max(m[i], __float_as_uint(y[i][j]) & 0x7fffffffu);
+                        for (int q = i * V / 2; q < (i + 1) * V / 2; ++q) {
+                            const float2 f = y(q);
+                            x = tc::max3(x, fabsf(f.x), fabsf(f.y));
+                        }
+                    }
+                    m[i] = __float_as_uint(x);
+                }
+                if (P.block == 0) {
+#pragma unroll
+                    for (int i = 0; i < Row::kVecs; ++i) all = max(all, m[i]);
+                    all = team_max(all, t, reinterpret_cast<unsigned *>(fold));
+                    const float s = scale_of(all);
+                    if (there && t.lane == 0) P.scale[row] = s;
+#pragma unroll
+                    for (int i = 0; i < Row::kVecs; ++i) over[i] = 1.0f / s;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < Row::kVecs; ++i) {
+#pragma unroll
+                        for (int o = 8; o; o >>= 1) m[i] = max(m[i], __shfl_xor_sync(kAll, m[i], o));
+                        const float s = scale_of(m[i]);
+                        over[i] = 1.0f / s;
+                        if (there && threadIdx.x % 16 == 0 && Row::inside(t, i, P.dim)) P.scale[row * P.groups + Row::column(t, i) / kScaleBlock] = s;
                     }
                 }
-            }
-            unsigned all = 0;
-            if (P.block == 0) {
 #pragma unroll
-                for (int i = 0; i < kVecs; ++i) all = max(all, m[i]);
-                all = team_max(all, team, reinterpret_cast<unsigned *>(fold));
-                if (there && lane == 0) P.scale[row] = scale_of(all);
+                for (int q = 0; q < Row::kPairs; ++q) {
+                    const float2 f = y(q);
+                    const uint32_t e = __nv_cvt_float2_to_fp8x2(make_float2(f.x * over[2 * q / V], f.y * over[(2 * q + 1) / V]), __NV_SATFINITE, __NV_E4M3);
+                    out[q / 2] = q % 2 ? out[q / 2] | e << 16 : e;
+                }
             } else {
-                __syncthreads();                 // what the row before left has been read
-                for (int i = threadIdx.x; i < teams * P.groups; i += blockDim.x) most[i] = 0;
-                __syncthreads();
+                unsigned *const mine = most + t.mine * P.groups;
+                const auto run = [&](int i, int j) { return min(max(Row::column(t, i) + j, 0) / kScaleBlock, P.groups - 1); };
+                t.sync();                        // what the row before left has been read
+                for (int i = t.lane; i < P.groups; i += t.size) mine[i] = 0;
+                t.sync();
 #pragma unroll
-                for (int i = 0; i < kVecs; ++i) {
-                    const int at = (i * team + lane) * V;
-                    if (there && at < P.dim) atomicMax(&most[mine * P.groups + at / kScaleBlock], m[i]);
+                for (int q = 0; q < Row::kPairs; ++q) {              // past the row there are zeros
+                    const float2 f = y(q);
+                    atomicMax(&mine[run(2 * q / V, 2 * q % V)], __float_as_uint(f.x) & 0x7fffffffu);
+                    atomicMax(&mine[run((2 * q + 1) / V, (2 * q + 1) % V)], __float_as_uint(f.y) & 0x7fffffffu);
                 }
-                __syncthreads();
-                for (int i = lane; i < P.groups && there; i += team) P.scale[row * P.groups + i] = scale_of(most[mine * P.groups + i]);
+                t.sync();
+                for (int i = t.lane; i < P.groups && there; i += t.size) P.scale[row * P.groups + i] = scale_of(mine[i]);
+#pragma unroll
+                for (int q = 0; q < Row::kPairs; ++q) {
+                    const float2 f = y(q);
+                    const float a = scale_of(mine[run(2 * q / V, 2 * q % V)]), b = scale_of(mine[run((2 * q + 1) / V, (2 * q + 1) % V)]);
+                    const uint32_t e = __nv_cvt_float2_to_fp8x2(make_float2(f.x / a, f.y / b), __NV_SATFINITE, __NV_E4M3);
+                    out[q / 2] = q % 2 ? out[q / 2] | e << 16 : e;
+                }
             }
+            if (there) {
+                uint8_t *const to = row_at<uint8_t>(P.y, row, P.ys);
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                const int at = (i * team + lane) * V;
-                if (there && at < P.dim) {
-                    const float over = 1.0f / scale_of(P.block == 0 ? all : most[mine * P.groups + at / kScaleBlock]);
-                    Pack<__nv_fp8_storage_t, V> q;
+                for (int i = 0; i < Row::kVecs; ++i)
+                    if (Row::inside(t, i, P.dim)) {
+                        if (V > 1 && Row::whole(t, i, P.dim)) {
+                            if constexpr (V == 8) *reinterpret_cast<uint2 *>(to + Row::column(t, i)) = make_uint2(out[2 * i], out[2 * i + 1]);
+                            else if constexpr (V == 4) *reinterpret_cast<uint32_t *>(to + Row::column(t, i)) = out[i];
+                        } else {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) q.v[j] = __nv_cvt_float_to_fp8(y[i][j] * over, __NV_SATFINITE, __NV_E4M3);
-                    *reinterpret_cast<Pack<__nv_fp8_storage_t, V> *>(static_cast<__nv_fp8_storage_t *>(P.y) + row * P.ys + at) = q;
-                }
+                            for (int j = 0; j < V; ++j)
+                                if (static_cast<unsigned>(Row::column(t, i) + j) < static_cast<unsigned>(P.dim))
+                                    to[Row::column(t, i) + j] = static_cast<uint8_t>(out[(i * V + j) / 4] >> (i * V + j) % 4 * 8);
+                        }
+                    }
             }
         }
     }
 }
 
 // dx of every row, and over the block's rows the sums of dy n, each thread its own columns'.
-template <typename T, int V, int kMine> __global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const __grid_constant__ NormParams P) {
+template <typename T, int V, int kMine, bool kShift> __global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const __grid_constant__ NormParams P) {
     wait_for_previous();
     let_next_start();
-    constexpr int kVecs = kMine / V;
-    using Vec = Pack<T, V>;
+    using Row = Part<T, V, kMine, kShift>;
+    using Rows = Ring<T, V, kMine, kShift, 3>;           // what the norm was of, its output's gradient, the one past it
+    extern __shared__ __align__(16) uint8_t shared[];
     __shared__ float2 fold[kNormThreads / 32];
-    extern __shared__ float sums[];              // of a block of several teams: dw of each
-    const int team = P.team, lane = static_cast<int>(threadIdx.x) % team, mine = static_cast<int>(threadIdx.x) / team, teams = static_cast<int>(blockDim.x) / team;
-    Vec w[kVecs];
-    float dw[kVecs][V];
+    const Team t(P, V);
+    Rows ring(shared, P.depth);
+    ring.none = static_cast<const T *>(P.x);
+    Row w;
+    w.fill(1.0f);
+    if (P.w) w.load(static_cast<const T *>(P.w), t, P.dim, t.shift == 0);
+    float2 dw[Row::kPairs];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int at = (i * team + lane) * V;
-        if (P.w && at < P.dim) w[i] = *reinterpret_cast<const Vec *>(static_cast<const T *>(P.w) + at);
-#pragma unroll
-        for (int j = 0; j < V; ++j) dw[i][j] = 0.0f;
-    }
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * teams; first < P.rows; first += static_cast<int64_t>(gridDim.x) * teams) {
-        const int64_t row = first + mine;
+    for (int q = 0; q < Row::kPairs; ++q) dw[q] = both(0.0f);
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * t.all, mine = static_cast<int64_t>(blockIdx.x) * t.all + t.mine;
+    int64_t ahead = mine;
+    const auto send = [&]() {
+        ring.copy(0, row_at<T>(P.x, ahead, P.xs), t, P.dim, ahead < P.rows);
+        ring.copy(1, row_at<T>(P.dy, ahead, P.dys), t, P.dim, ahead < P.rows);
+        if (P.dt) ring.copy(2, row_at<T>(P.dt, ahead, P.dts), t, P.dim, ahead < P.rows);
+        ring.sent();
+        ahead += stride;
+    };
+    for (int i = 1; i < P.depth; ++i) send();
+    int64_t row = mine;
+    for (int64_t first = row - t.mine; first < P.rows; first += stride, row += stride) {
         const bool there = row < P.rows;
-        const T *h = static_cast<const T *>(P.x) + row * P.xs, *dy = static_cast<const T *>(P.dy) + row * P.dys, *dt = static_cast<const T *>(P.dt) + row * P.dts;
-        Vec a[kVecs], d[kVecs], t[kVecs];
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const int at = (i * team + lane) * V;
-            if (there && at < P.dim) {
-                a[i] = *reinterpret_cast<const Vec *>(h + at);
-                d[i] = *reinterpret_cast<const Vec *>(dy + at);
-                if (P.dt) t[i] = *reinterpret_cast<const Vec *>(dt + at);
+        send();
+        Row f, e, out;
+        if constexpr (Rows::kCopies) {
+            ring.wait();
+            ring.read(f, 0);
+            ring.read(e, 1);
+            f.trim(t, P.dim);
+            e.trim(t, P.dim);
+        } else {
+            f.fill(0.0f);
+            e.fill(0.0f);
+            if (there) {
+                f.load(row_at<T>(P.x, row, P.xs), t, P.dim, true);
+                e.load(row_at<T>(P.dy, row, P.dys), t, P.dim, true);
             }
         }
-        float2 sum = make_float2(0.0f, 0.0f);    // of h^2 and of dy w h
+        float2 squares = both(0.0f), dots = both(0.0f);              // of h^2 and of dy w h
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const int at = (i * team + lane) * V;
-            if (there && at < P.dim) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float f = to_f32(a[i].v[j]), g = to_f32(d[i].v[j]) * (P.w ? to_f32(w[i].v[j]) : 1.0f);
-                    sum.x = fmaf(f, f, sum.x);
-                    sum.y = fmaf(f, g, sum.y);
-                }
-            }
+        for (int q = 0; q < Row::kPairs; ++q) {
+            squares = tc::fma2(f[q], f[q], squares);
+            dots = tc::fma2(f[q], tc::mul2(e[q], w[q]), dots);
         }
-        sum = team_sum(sum, team, fold);
-        const float by = rsqrtf(sum.x * P.over_dim + P.eps), pull = sum.y * P.over_dim * by * by;
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const int at = (i * team + lane) * V;
-            if (there && at < P.dim) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float f = to_f32(a[i].v[j]), e = to_f32(d[i].v[j]);
-                    const float g = e * (P.w ? to_f32(w[i].v[j]) : 1.0f);
-                    dw[i][j] = fmaf(e, f * by, dw[i][j]);
-                    float out = by * (g - f * pull);
-                    if (P.dt) out += to_f32(t[i].v[j]);
-                    a[i].v[j] = from_f32<T>(out);
-                }
-                *reinterpret_cast<Vec *>(static_cast<T *>(P.dx) + row * P.dxs + at) = a[i];
-            }
+        f.keep();
+        e.keep();
+        w.keep();
+        const float2 sum = team_sum(make_float2(squares.x + squares.y, dots.x + dots.y), t, fold);
+        const float by = rsqrtf(sum.x * P.over_dim + P.eps), pull = -sum.y * P.over_dim * by * by;
+        out.fill(0.0f);
+        if (P.dt) {
+            if constexpr (Rows::kCopies) ring.read(out, 2);
+            else if (there) out.load(row_at<T>(P.dt, row, P.dts), t, P.dim, true);
         }
+        if (there) {
+#pragma unroll
+            for (int q = 0; q < Row::kPairs; ++q) {
+                dw[q] = tc::fma2(e[q], tc::mul2(f[q], both(by)), dw[q]);
+                out.set(q, tc::fma2(tc::fma2(f[q], both(pull), tc::mul2(e[q], w[q])), both(by), out[q]));
+            }
+            out.store(row_at<T>(P.dx, row, P.dxs), t, P.dim);
+        }
+        ring.next();
     }
     if (!P.wanted) return;
-    float *const part = P.part + static_cast<int64_t>(blockIdx.x) * P.dim;
-    if (teams == 1) {
+    float *const part = P.part + static_cast<int64_t>(blockIdx.x) * P.dim, *const sums = reinterpret_cast<float *>(shared);
+    float *const to = t.all == 1 ? part : sums + t.mine * P.dim;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");             // the ring's memory holds the teams' sums now
+    __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const int at = (i * team + lane) * V;
-            if (at < P.dim) *reinterpret_cast<Pack<float, V> *>(part + at) = *reinterpret_cast<Pack<float, V> *>(dw[i]);
-        }
-        return;
+    for (int i = 0; i < kMine; ++i) {
+        const int at = Row::column(t, i / V) + i % V;
+        if (static_cast<unsigned>(at) < static_cast<unsigned>(P.dim)) to[at] = i % 2 ? dw[i / 2].y : dw[i / 2].x;
     }
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int at = (i * team + lane) * V;
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (at < P.dim) sums[mine * P.dim + at + j] = dw[i][j];
-    }
+    if (t.all == 1) return;
     __syncthreads();
     for (int c = threadIdx.x; c < P.dim; c += blockDim.x) {
         float s = 0.0f;
-        for (int i = 0; i < teams; ++i) s += sums[i * P.dim + c];
+        for (int i = 0; i < t.all; ++i) s += sums[i * P.dim + c];
         part[c] = s;
     }
 }
 
-// The blocks' partial rows added in their order: 32 columns to a block, eight warps that each take an eighth of the rows.
-template <typename T> __global__ void __launch_bounds__(256) norm_weight_kernel(const float *part, int blocks, int dim, T *dw) {
+// The blocks' partial rows added in their order: 32 columns to a block, 32 warps that each take a part of the rows.
+template <typename T> __global__ void __launch_bounds__(1024) norm_weight_kernel(const float *part, int blocks, int dim, T *dw) {
     wait_for_previous();
     let_next_start();
-    __shared__ float fold[8][32];
+    __shared__ float fold[32][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = static_cast<int>(blockIdx.x) * 32 + lane;
-    const int per = (blocks + 7) / 8, from = warp * per, until = min(from + per, blocks);
+    const int per = (blocks + 31) / 32, from = warp * per, until = min(from + per, blocks);
     float s = 0.0f;
     if (c < dim)
 #pragma unroll 8
         for (int b = from; b < until; ++b) s += part[static_cast<int64_t>(b) * dim + c];
     fold[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && c < dim) {
-        s = 0.0f;
-        for (int i = 0; i < 8; ++i) s += fold[i][lane];
-        dw[c] = from_f32<T>(s);
-    }
+    s = fold[lane][warp];                        // warp w adds column w
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
+    const int column = static_cast<int>(blockIdx.x) * 32 + warp;
+    if (lane == 0 && column < dim) dw[column] = from_f32<T>(s);
 }
 
 namespace {
 
 using NormKernel = void (*)(const NormParams);
 
-template <typename T, int V, int kMine> NormKernel pick_norm(bool backward, bool bits8) {
-    if (backward) return norm_backward_kernel<T, V, kMine>;
-    return bits8 ? norm_forward_kernel<T, V, kMine, true> : norm_forward_kernel<T, V, kMine, false>;
+template <typename T, int V, int kMine, bool kShift> NormKernel pick_norm(bool backward, bool bits8) {
+    if (backward) return norm_backward_kernel<T, V, kMine, kShift>;
+    return bits8 ? norm_forward_kernel<T, V, kMine, kShift, true> : norm_forward_kernel<T, V, kMine, kShift, false>;
 }
-template <typename T, int V> NormKernel pick_norm(int dim, bool backward, bool bits8) {
-    return dim <= 8192 ? pick_norm<T, V, 16>(backward, bits8) : pick_norm<T, V, 32>(backward, bits8);
+template <typename T, int V> NormKernel pick_norm(int mine, bool shift, bool backward, bool bits8) {
+    if constexpr (V > 1) {
+        if constexpr (sizeof(T) == 4)
+            if (mine == 8) return shift ? pick_norm<T, V, 8, true>(backward, bits8) : pick_norm<T, V, 8, false>(backward, bits8);
+        return shift ? pick_norm<T, V, 16, true>(backward, bits8) : pick_norm<T, V, 16, false>(backward, bits8);
+    } else {
+        if constexpr (sizeof(T) == 4)
+            if (mine == 8) return pick_norm<T, V, 8, false>(backward, bits8);
+        return pick_norm<T, V, 16, false>(backward, bits8);
+    }
 }
 
 int check_norm(const loco_norm_t *c) {
@@ -302,54 +518,93 @@ int check_norm(const loco_norm_t *c) {
     return c->dim > kMaxDim ? LOCO_ERR_UNSUPPORTED : LOCO_OK;
 }
 
-// What the vector accesses of a call have to keep to: `vec` elements of every row and of the weight together.
-struct Widths {
+// Whether a call's rows can be taken in 16-byte vectors: every tensor begins on a boundary, and its rows keep the same distance
+// from one as those of the first.
+struct Vectors {
+    int64_t rows, stride = -1;
     int vec;
-    int64_t rows;
-    void narrow(int to) { vec = to < vec ? to : vec; }
-    void take(const void *at, int64_t stride, int size, int64_t dim) {
-        int v = vec;
-        while (v > 1 && (!aligned(at, static_cast<uintptr_t>(v * size)) || (rows > 1 && stride % v != 0) || dim % v != 0)) v /= 2;
-        narrow(v);
+    bool fit = true;
+    void take(const void *at, int64_t row_stride, int size) {
+        if (stride < 0) stride = row_stride;
+        fit = fit && aligned(at, static_cast<uintptr_t>(vec * size)) && (row_stride - stride) % vec == 0;
     }
 };
 
 // A tensor of rows: present where it has to be, aligned to its elements; an output's rows do not overlap.
-int take_rows(const loco_rows_t *t, int64_t rows, int dim, int size, bool written, Widths &W, int64_t &stride) {
+int take_rows(const loco_rows_t *t, int dim, int size, bool written, Vectors &V, int64_t &stride) {
     if (!t || !t->ptr) return LOCO_ERR_ARG;
-    stride = rows > 1 ? t->row_stride : 0;
-    if (stride < 0 || (written && rows > 1 && stride < dim)) return LOCO_ERR_ARG;
+    stride = V.rows > 1 ? t->row_stride : 0;
+    if (stride < 0 || (written && V.rows > 1 && stride < dim)) return LOCO_ERR_ARG;
     if (!aligned(t->ptr, static_cast<uintptr_t>(size))) return LOCO_ERR_ALIGN;
-    W.take(t->ptr, stride, size, dim);
+    V.take(t->ptr, stride, size);
     return LOCO_OK;
 }
 
-// Threads of a row, and blocks; 16 elements a thread, 32 above 8192.
-int launch_norm(NormParams &P, const loco_norm_t *c, bool backward, int vec, void *stream, int &blocks) {
+// Shared memory above the default limit, set once per device.
+bool allow(NormKernel fn, int which) {
+    static std::atomic<bool> set[64][48];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return false;
+    }
+    if (set[dev][which].load(std::memory_order_acquire)) return true;
+    if (cudaFuncSetAttribute(reinterpret_cast<const void *>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    set[dev][which].store(true, std::memory_order_release);
+    return true;
+}
+
+// Threads of a row, teams of a block, and blocks: as many as run at once, fewer teams where the rows would not fill the SMs.
+int launch_norm(NormParams &P, const loco_norm_t *c, bool backward, const Vectors &V, void *stream, int &blocks) {
     const int sms = sm_count();
     if (sms == 0) return LOCO_ERR_CUDA;
-    const int mine = c->dim <= 8192 ? 16 : 32, lanes = (c->dim + mine - 1) / mine;
+    // elements of a thread: 32 bytes of them, 64 where a row of fp32 needs more than a block
+    const int size = c->dtype == LOCO_BF16 ? 2 : 4;
+    int vec = V.fit ? V.vec : 1, columns = c->dim + (P.xs % vec ? vec - 1 : 0);      // a row and what lies before it up to a boundary
+    if (columns > 16 * kNormThreads) {
+        vec = 1;
+        columns = c->dim;
+    }
+    const int mine = size == 2 || columns > 8 * kNormThreads ? 16 : 8, lanes = (columns + mine - 1) / mine;
     int team = 4;
     while (team < 32 && team < lanes) team *= 2;
     if (lanes > 32) team = (lanes + 31) / 32 * 32;
-    const int threads = team > 32 ? team : kSmallBlock, teams = threads / team;
-    const int64_t all = (P.rows + teams - 1) / teams, most = backward ? (3 * sms < kPartials ? 3 * sms : kPartials) : static_cast<int64_t>(sms) * (2048 / threads);
+    int teams = kBlockThreads / team;
+    const int least = team < 32 ? 32 / team : 1;
+    const int64_t spread = P.rows / (2 * sms);
+    if (spread < teams) teams = static_cast<int>(spread) / least * least;
+    if (teams < least) teams = least;
+    const int threads = team * teams, tensors = backward ? 3 : 2;
+    // rows on their way: as many as the shared memory of the blocks that run at once holds, three at most
+    const int together = kNormThreads / threads, each = threads * mine * size * tensors;
+    int depth = kRingBytes / (together * each + 2048 * together);
+    depth = depth < 1 ? 1 : depth > 3 ? 3 : depth;
+    // Forward with a residual a block has 256 KB to move, and there are more than run at once: the SMs are not equally far from
+    // memory, and those that are done first take more of them.  16384 x 5120, bfloat16 with residual, 1, 2, 4, 8 times as many as run at once: 123, 111, 105,
+    // 103 us; without: 63, 63, 64, 68.  Backward every block costs a partial row: 47.5 us with one time, 56 with 1.5.
+    const int64_t all = (P.rows + teams - 1) / teams, once = static_cast<int64_t>(sms) * together;
+    const int64_t more = P.r ? P.rows * c->dim * size * 4 / (once * (256 << 10)) : 1;
+    int64_t most = backward || more < 1 ? once : once * more;
+    if (backward && most > kPartials) most = kPartials;
     blocks = static_cast<int>(all < most ? all : most);
+    if (all > most)                              // the rows of a team, blocks * teams apart, have one distance from the boundaries
+        while (static_cast<int64_t>(blocks) * teams % vec * (P.xs % vec) % vec != 0) --blocks;
     P.team = team;
+    P.depth = depth;
     P.dim = c->dim;
     P.block = c->block;
     P.groups = (c->dim + kScaleBlock - 1) / kScaleBlock;
     P.eps = c->eps;
     P.over_dim = 1.0f / static_cast<float>(c->dim);
-    NormKernel fn;
-    if (c->dtype == LOCO_BF16) {
-        fn = vec >= 8 ? pick_norm<__nv_bfloat16, 8>(c->dim, backward, c->bits8) : vec >= 2 ? pick_norm<__nv_bfloat16, 2>(c->dim, backward, c->bits8)
-                                                                                       : pick_norm<__nv_bfloat16, 1>(c->dim, backward, c->bits8);
-    } else {
-        fn = vec >= 4 ? pick_norm<float, 4>(c->dim, backward, c->bits8) : pick_norm<float, 1>(c->dim, backward, c->bits8);
-    }
-    const size_t shared = backward && teams > 1 && P.wanted ? static_cast<size_t>(teams) * c->dim * sizeof(float) : 0;
-    return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), static_cast<unsigned>(threads), shared, stream, P);
+    const bool shift = P.xs % vec != 0 || c->dim % vec != 0;
+    const NormKernel fn = size == 2 ? (vec > 1 ? pick_norm<__nv_bfloat16, 8>(mine, shift, backward, c->bits8) : pick_norm<__nv_bfloat16, 1>(mine, shift, backward, c->bits8))
+                                    : (vec > 1 ? pick_norm<float, 4>(mine, shift, backward, c->bits8) : pick_norm<float, 1>(mine, shift, backward, c->bits8));
+    const size_t ring = static_cast<size_t>(depth) * each;
+    if (!allow(fn, ((((size == 4) * 2 + (vec > 1)) * 2 + (mine * size > 32)) * 2 + shift) * 3 + (backward ? 2 : c->bits8 ? 1 : 0))) return LOCO_ERR_CUDA;
+    return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), static_cast<unsigned>(threads), ring, stream, P);
 }
 
 }  // namespace
@@ -369,14 +624,15 @@ int loco_norm_forward(const loco_norm_t *c, int64_t rows, const loco_rows_t *x, 
     const int size = c->dtype == LOCO_BF16 ? 2 : 4;
     NormParams P{};
     P.rows = rows;
-    Widths W{16 / size, rows};
-    if ((rc = take_rows(x, rows, c->dim, size, false, W, P.xs)) != LOCO_OK) return rc;
-    if (residual && (rc = take_rows(residual, rows, c->dim, size, false, W, P.rs)) != LOCO_OK) return rc;
-    if (total && (rc = take_rows(total, rows, c->dim, size, true, W, P.hs)) != LOCO_OK) return rc;
-    if ((rc = take_rows(y, rows, c->dim, c->bits8 ? 1 : size, true, W, P.ys)) != LOCO_OK) return rc;
+    Vectors V{rows};
+    V.vec = 16 / size;
+    if ((rc = take_rows(x, c->dim, size, false, V, P.xs)) != LOCO_OK) return rc;
+    if (residual && (rc = take_rows(residual, c->dim, size, false, V, P.rs)) != LOCO_OK) return rc;
+    if (total && (rc = take_rows(total, c->dim, size, true, V, P.hs)) != LOCO_OK) return rc;
+    if ((rc = take_rows(y, c->dim, c->bits8 ? 1 : size, true, V, P.ys)) != LOCO_OK) return rc;
     if (c->bits8 && !d_scale) return LOCO_ERR_ARG;
     if (!aligned(d_weight, static_cast<uintptr_t>(size)) || !aligned(d_scale, 4)) return LOCO_ERR_ALIGN;
-    if (d_weight) W.take(d_weight, 0, size, c->dim);
+    if (!aligned(d_weight, 16)) V.fit = false;
     P.x = x->ptr;
     P.r = residual ? residual->ptr : nullptr;
     P.h = total ? total->ptr : nullptr;
@@ -384,7 +640,7 @@ int loco_norm_forward(const loco_norm_t *c, int64_t rows, const loco_rows_t *x, 
     P.w = d_weight;
     P.scale = d_scale;
     int blocks;
-    return launch_norm(P, c, false, W.vec, stream, blocks);
+    return launch_norm(P, c, false, V, stream, blocks);
 }
 
 uint64_t loco_norm_backward_workspace_bytes(const loco_norm_t *c) {
@@ -409,24 +665,25 @@ int loco_norm_backward(const loco_norm_t *c, int64_t rows, const loco_rows_t *h,
     int blocks = 0;
     P.part = static_cast<float *>(d_work);
     if (rows > 0) {
-        Widths W{16 / size, rows};
-        if ((rc = take_rows(h, rows, c->dim, size, false, W, P.xs)) != LOCO_OK) return rc;
-        if ((rc = take_rows(dy, rows, c->dim, size, false, W, P.dys)) != LOCO_OK) return rc;
-        if (dtotal && (rc = take_rows(dtotal, rows, c->dim, size, false, W, P.dts)) != LOCO_OK) return rc;
-        if ((rc = take_rows(dx, rows, c->dim, size, true, W, P.dxs)) != LOCO_OK) return rc;
+        Vectors V{rows};
+        V.vec = 16 / size;
+        if ((rc = take_rows(h, c->dim, size, false, V, P.xs)) != LOCO_OK) return rc;
+        if ((rc = take_rows(dy, c->dim, size, false, V, P.dys)) != LOCO_OK) return rc;
+        if (dtotal && (rc = take_rows(dtotal, c->dim, size, false, V, P.dts)) != LOCO_OK) return rc;
+        if ((rc = take_rows(dx, c->dim, size, true, V, P.dxs)) != LOCO_OK) return rc;
         if (!aligned(d_weight, static_cast<uintptr_t>(size))) return LOCO_ERR_ALIGN;
-        if (d_weight) W.take(d_weight, 0, size, c->dim);
+        if (!aligned(d_weight, 16)) V.fit = false;
         P.x = h->ptr;
         P.dy = dy->ptr;
         P.dt = dtotal ? dtotal->ptr : nullptr;
         P.dx = dx->ptr;
         P.w = d_weight;
-        rc = launch_norm(P, c, true, W.vec, stream, blocks);
+        rc = launch_norm(P, c, true, V, stream, blocks);
         if (rc != LOCO_OK || !P.wanted) return rc;
     }
     const dim3 grid(static_cast<unsigned>((c->dim + 31) / 32));
-    if (c->dtype == LOCO_BF16) return launch_kernel(norm_weight_kernel<__nv_bfloat16>, grid, 256, 0, stream, P.part, blocks, c->dim, static_cast<__nv_bfloat16 *>(d_dweight));
-    return launch_kernel(norm_weight_kernel<float>, grid, 256, 0, stream, P.part, blocks, c->dim, static_cast<float *>(d_dweight));
+    if (c->dtype == LOCO_BF16) return launch_kernel(norm_weight_kernel<__nv_bfloat16>, grid, 1024, 0, stream, P.part, blocks, c->dim, static_cast<__nv_bfloat16 *>(d_dweight));
+    return launch_kernel(norm_weight_kernel<float>, grid, 1024, 0, stream, P.part, blocks, c->dim, static_cast<float *>(d_dweight));
 }
 
 }  // extern "C"
