@@ -6,8 +6,11 @@
 // The other passes move rows: a team of threads has a token, reads its row once and writes it to all of its places, or
 // reads them all and writes the sum.  One or two operations an element, so HBM bounds them.
 #include "layer_common.h"
+#include "layer_tc.cuh"
 
 namespace loco_layer {
+
+using namespace tc;
 
 constexpr int kMostExperts = 512;
 constexpr int kMostChoices = 16;
@@ -164,106 +167,178 @@ template <typename T, int V> __global__ void __launch_bounds__(kMoveThreads) exp
     }
 }
 
-template <typename T, int V> __global__ void __launch_bounds__(kMoveThreads) experts_combine_kernel(const __grid_constant__ MoveParams P) {
-    wait_for_previous();
-    let_next_start();
-    using Vec = Pack<T, V>;
-    const Seat s = seat(P.team);
-    if (s.token >= P.tokens) return;
-    const int32_t *place = P.place + s.token * P.top_k;
-    const float *weight = P.weight + s.token * P.top_k;
-    T *y = static_cast<T *>(P.out) + s.token * P.out_stride;
-    for (int c = s.lane * V; c < P.dim; c += P.team * V) {
-        float sum[V];
+// The choices j0 .. j0 + kRows - 1 of a token: their rows (-1: none) and weights.  Read again where they are needed again, from
+// L1: kept for all choices they cost the registers that keep enough threads at work (six choices: 46 us against 30).
+template <int kRows> __device__ __forceinline__ void choices_at(const MoveParams &P, int64_t token, int j0, int (&p)[kRows], float (&w)[kRows]) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-#pragma unroll 4
-        for (int j = 0; j < P.top_k; ++j) {
-            const int p = __ldg(place + j);
-            if (p >= 0 && p < P.row_count) {
-                const Vec v = *reinterpret_cast<const Vec *>(static_cast<const T *>(P.rows) + p * P.rows_stride + c);
-                const float w = P.weight ? __ldg(weight + j) : 1.0f;
-#pragma unroll
-                for (int i = 0; i < V; ++i) sum[i] = fmaf(w, to_f32(v.v[i]), sum[i]);
-            }
+    for (int j = 0; j < kRows; ++j) {
+        p[j] = -1;
+        w[j] = 0.0f;
+        if (j0 + j < P.top_k) {
+            const int at = __ldg(P.place + token * P.top_k + j0 + j);
+            p[j] = at < P.row_count ? at : -1;
+            w[j] = P.weight ? __ldg(P.weight + token * P.top_k + j0 + j) : 1.0f;
         }
-        Vec out;
-#pragma unroll
-        for (int i = 0; i < V; ++i) out.v[i] = from_f32<T>(sum[i]);
-        *reinterpret_cast<Vec *>(y + c) = out;
     }
 }
 
-// kMost: choices of a token at most.
-template <typename T, int V, int kMost> __global__ void __launch_bounds__(kMoveThreads) experts_backward_kernel(const __grid_constant__ MoveParams P) {
+// A thread asks for kRows * kPlaces vectors before it uses the first.  kEvery: kRows are all choices of a token; else four at a
+// time, at one place.
+template <typename T, int V, int kRows, int kPlaces, bool kEvery>
+__global__ void __launch_bounds__(kMoveThreads, 4) experts_combine_kernel(const __grid_constant__ MoveParams P) {
+    wait_for_previous();
+    let_next_start();
+    static_assert(kEvery || kPlaces == 1, "sums of one place are kept");
+    using Vec = Pack<T, V>;
+    constexpr int kPairs = (V + 1) / 2;
+    const Seat s = seat(P.team);
+    if (s.token >= P.tokens) return;
+    T *const y = static_cast<T *>(P.out) + s.token * P.out_stride;
+    const int step = P.team * V;
+    int p[kRows];
+    float w[kRows];
+    if (kEvery) choices_at<kRows>(P, s.token, 0, p, w);
+#pragma unroll 1
+    for (int c = s.lane * V; c < P.dim; c += kPlaces * step) {
+        float2 sum[kPairs];
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) sum[q] = make_float2(0.0f, 0.0f);
+#pragma unroll 1
+        for (int j0 = 0; j0 < (kEvery ? 1 : P.top_k); j0 += kRows) {
+            if (!kEvery) choices_at<kRows>(P, s.token, j0, p, w);
+            Vec v[kPlaces][kRows];
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                const T *const row = static_cast<const T *>(P.rows) + p[j] * P.rows_stride + c;
+#pragma unroll
+                for (int u = 0; u < kPlaces; ++u)
+                    if (p[j] >= 0 && c + u * step < P.dim) v[u][j] = *reinterpret_cast<const Vec *>(row + u * step);
+            }
+#pragma unroll
+            for (int u = 0; u < kPlaces; ++u) {
+#pragma unroll
+                for (int j = 0; j < kRows; ++j)
+                    if (p[j] >= 0)
+#pragma unroll
+                        for (int q = 0; q < kPairs; ++q) sum[q] = fma2(make_float2(w[j], w[j]), pair_of(v[u][j], q), sum[q]);
+                if (kEvery && c + u * step < P.dim) {
+                    Vec out;
+#pragma unroll
+                    for (int q = 0; q < kPairs; ++q) {
+                        set_pair(out, q, sum[q]);
+                        sum[q] = make_float2(0.0f, 0.0f);
+                    }
+                    *reinterpret_cast<Vec *>(y + c + u * step) = out;
+                }
+            }
+        }
+        if (!kEvery) {
+            Vec out;
+#pragma unroll
+            for (int q = 0; q < kPairs; ++q) set_pair(out, q, sum[q]);
+            *reinterpret_cast<Vec *>(y + c) = out;
+        }
+    }
+}
+
+// Sums of kN values over aligned groups of `width` lanes.  Lanes first share out the values (a step halves what each holds), so
+// that eight values over a warp take 7 + 2 exchanges instead of 40; value j ends in the lanes whose low bits are j.
+template <int kN> __device__ __forceinline__ float shared_sum(float (&x)[kN], int lane, int width) {
+    int o = 1;
+#pragma unroll
+    for (int n = kN / 2; n; n /= 2) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int j = 0; j < n; ++j) {                // values j and j + n: the lane's bit says which it keeps
+            const float give = upper ? x[2 * j] : x[2 * j + 1], keep = upper ? x[2 * j + 1] : x[2 * j];
+            x[j] = keep + __shfl_xor_sync(kAll, give, o);
+        }
+        o <<= 1;
+    }
+    float s = x[0];
+    for (; o < width; o <<= 1) s += __shfl_xor_sync(kAll, s, o);
+    return s;
+}
+
+// kRows choices at a time, at kPlaces places; dy is read again, from L1 or L2, for the next ones.
+template <typename T, int V, int kRows, int kPlaces>
+__global__ void __launch_bounds__(kMoveThreads, kRows > 4 ? 3 : 4) experts_backward_kernel(const __grid_constant__ MoveParams P) {
     wait_for_previous();
     let_next_start();
     using Vec = Pack<T, V>;
-    __shared__ float fold[kMoveThreads / 32][kMost];
+    __shared__ float fold[2][kMoveThreads / 32][kRows];
     const Seat s = seat(P.team);
     const bool there = s.token < P.tokens;
-    const T *dy = static_cast<const T *>(P.in) + s.token * P.in_stride;
-    float dot[kMost], w[kMost];
-    int p[kMost];
+    const int64_t token = there ? s.token : 0;
+    const T *const dy = static_cast<const T *>(P.in) + token * P.in_stride;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, width = P.team < 32 ? P.team : 32, step = P.team * V;
+    int side = 0;
+#pragma unroll 1
+    for (int j0 = 0; j0 < P.top_k; j0 += kRows) {
+        int p[kRows];
+        float w[kRows], dot[kRows];
+        choices_at<kRows>(P, token, j0, p, w);
 #pragma unroll
-    for (int j = 0; j < kMost; ++j) {
-        dot[j] = 0.0f;
-        w[j] = 0.0f;
-        p[j] = -1;
-        if (there && j < P.top_k) {
-            const int at = __ldg(P.place + s.token * P.top_k + j);
-            p[j] = at < P.row_count ? at : -1;
-            w[j] = __ldg(P.weight + s.token * P.top_k + j);
-        }
-    }
-    if (there)
-        for (int c = s.lane * V; c < P.dim; c += P.team * V) {
-            const Vec d = *reinterpret_cast<const Vec *>(dy + c);
+        for (int j = 0; j < kRows; ++j) dot[j] = 0.0f;
+#pragma unroll 1
+        for (int c = s.lane * V; c < P.dim && there; c += kPlaces * step) {
+            Vec d[kPlaces], r[kPlaces][kRows];
 #pragma unroll
-            for (int j = 0; j < kMost; ++j)
-                if (p[j] >= 0) {
-                    const Vec r = *reinterpret_cast<const Vec *>(static_cast<const T *>(P.rows) + p[j] * P.rows_stride + c);
-                    Vec out;
+            for (int u = 0; u < kPlaces; ++u)
+                if (c + u * step < P.dim) d[u] = *reinterpret_cast<const Vec *>(dy + c + u * step);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        dot[j] = fmaf(to_f32(d.v[i]), to_f32(r.v[i]), dot[j]);
-                        out.v[i] = from_f32<T>(w[j] * to_f32(d.v[i]));
+            for (int j = 0; j < kRows; ++j) {
+                const T *const row = static_cast<const T *>(P.rows) + p[j] * P.rows_stride + c;
+#pragma unroll
+                for (int u = 0; u < kPlaces; ++u)
+                    if (p[j] >= 0 && c + u * step < P.dim) r[u][j] = *reinterpret_cast<const Vec *>(row + u * step);
+            }
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                T *const row = static_cast<T *>(P.rows_out) + p[j] * P.rows_out_stride + c;
+#pragma unroll
+                for (int u = 0; u < kPlaces; ++u)
+                    if (p[j] >= 0 && c + u * step < P.dim) {
+                        Vec out;
+#pragma unroll
+                        for (int q = 0; q < (V + 1) / 2; ++q) {
+                            const float2 f = pair_of(d[u], q), g = pair_of(r[u][j], q);
+                            dot[j] = fmaf(f.x, g.x, fmaf(f.y, g.y, dot[j]));
+                            set_pair(out, q, mul2(make_float2(w[j], w[j]), f));
+                        }
+                        *reinterpret_cast<Vec *>(row + u * step) = out;
                     }
-                    *reinterpret_cast<Vec *>(static_cast<T *>(P.rows_out) + p[j] * P.rows_out_stride + c) = out;
-                }
+            }
         }
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-#pragma unroll
-    for (int j = 0; j < kMost; ++j)
-        for (int o = (P.team < 32 ? P.team : 32) / 2; o; o >>= 1) dot[j] += __shfl_xor_sync(kAll, dot[j], o);
-    float *const dw = P.dweight + s.token * P.top_k;
-    if (P.team <= 32) {
-        if (there && s.lane == 0)
-#pragma unroll
-            for (int j = 0; j < kMost; ++j)
-                if (j < P.top_k) dw[j] = dot[j];
-        return;
-    }
-    if (lane == 0)
-#pragma unroll
-        for (int j = 0; j < kMost; ++j) fold[warp][j] = dot[j];
-    __syncthreads();
-    if (there && s.lane < P.top_k) {
-        float sum = 0.0f;
-        for (int i = 0; i < P.team / 32; ++i) sum += fold[warp + i][s.lane];
-        dw[s.lane] = sum;
+        float sum = shared_sum<kRows>(dot, lane, width);
+        float *const dw = P.dweight + token * P.top_k + j0;
+        if (P.team <= 32) {
+            if (there && s.lane < kRows && j0 + s.lane < P.top_k) dw[s.lane] = sum;
+        } else {                                     // two sides: the next ones' sums go to the other
+            if (lane < kRows) fold[side][warp][lane] = sum;
+            __syncthreads();
+            if (there && s.lane < kRows && j0 + s.lane < P.top_k) {
+                sum = 0.0f;
+                for (int i = 0; i < P.team / 32; ++i) sum += fold[side][warp + i][s.lane];
+                dw[s.lane] = sum;
+            }
+            side ^= 1;
+        }
     }
 }
 
 namespace {
 
 using MoveKernel = void (*)(const MoveParams);
-template <typename T, int V> MoveKernel pick_backward(int k) {
-    return k <= 2 ? experts_backward_kernel<T, V, 2> : k <= 4 ? experts_backward_kernel<T, V, 4> : k <= 8 ? experts_backward_kernel<T, V, 8> : experts_backward_kernel<T, V, 16>;
-}
 enum Move { kDispatch, kCombine, kBackward };
-template <typename T, int V> MoveKernel pick_move(Move m, int k) {
-    return m == kDispatch ? experts_dispatch_kernel<T, V> : m == kCombine ? experts_combine_kernel<T, V> : pick_backward<T, V>(k);
+template <typename T, int V> MoveKernel pick_move(Move m, int k, int places) {
+    if (m == kDispatch) return experts_dispatch_kernel<T, V>;
+    // Combine, two choices, at one, two, four places: 16384 x 4096: 68, 71, 60 us; 700,000 x 64: 60, 53, 58; 30,000 x 1367 in single elements:
+    // 121, 86, 141.
+    if (m == kCombine)
+        return k <= 2 ? (places > 2 ? experts_combine_kernel<T, V, 2, 4, true> : experts_combine_kernel<T, V, 2, 2, true>)
+               : k <= 4 ? experts_combine_kernel<T, V, 4, 2, true> : experts_combine_kernel<T, V, 4, 1, false>;
+    return k <= 2 ? experts_backward_kernel<T, V, 2, 2> : k <= 4 ? experts_backward_kernel<T, V, 4, 1> : experts_backward_kernel<T, V, 8, 1>;
 }
 
 int check_experts(const loco_experts_t *c) {
@@ -291,17 +366,20 @@ int launch_move(Move m, MoveParams &P, const loco_experts_t *c, int vec, void *s
     P.row_count = c->rows;
     P.dim = c->dim;
     P.top_k = c->top_k;
-    MoveKernel fn;
-    int v;
-    if (c->dtype == LOCO_BF16) {
-        v = vec >= 8 ? 8 : vec >= 2 ? 2 : 1;
-        fn = v == 8 ? pick_move<__nv_bfloat16, 8>(m, c->top_k) : v == 2 ? pick_move<__nv_bfloat16, 2>(m, c->top_k) : pick_move<__nv_bfloat16, 1>(m, c->top_k);
-    } else {
-        v = vec >= 4 ? 4 : 1;
-        fn = v == 4 ? pick_move<float, 4>(m, c->top_k) : pick_move<float, 1>(m, c->top_k);
-    }
-    int team = 4;
-    while (team < kMoveThreads && team * v < c->dim) team *= 2;
+    const int v = c->dtype == LOCO_BF16 ? (vec >= 8 ? 8 : vec >= 2 ? 2 : 1) : vec >= 4 ? 4 : 1, k = c->top_k;
+    // places in a row that a thread takes at once
+    const int places = m == kCombine && k <= 2 ? (v > 1 && c->dim >= 128 * v ? 4 : 2) : (m == kCombine && k <= 4) || (m == kBackward && k <= 2) ? 2 : 1;
+    const MoveKernel fn = c->dtype == LOCO_BF16 ? (v == 8   ? pick_move<__nv_bfloat16, 8>(m, k, places)
+                                                   : v == 2 ? pick_move<__nv_bfloat16, 2>(m, k, places)
+                                                            : pick_move<__nv_bfloat16, 1>(m, k, places))
+                                                : (v == 4 ? pick_move<float, 4>(m, k, places) : pick_move<float, 1>(m, k, places));
+    const int least = m == kBackward && k > 4 ? 8 : 4;               // lanes that end with a choice's sum each
+    int team = least;
+    while (team < kMoveThreads && team * places * v < c->dim) team *= 2;
+    // With enough tokens a thread goes round twice (four times over single elements), so that the wait for the places and the sums over
+    // the team come to less: 5021 x 2040, six choices, backward once, twice, four times: 46.6, 42.4, 41.3 us, combine 29.1, 28.3, 31.4.
+    if (m == kBackward || (m == kCombine && (k > 2 || v == 1)))
+        for (int turns = 1; turns < (v == 1 ? 4 : 2) && team > 32 && c->tokens * (team / 2) >= sm_count() * 2048ll; turns *= 2) team /= 2;
     P.team = team;
     const int64_t blocks = (c->tokens + kMoveThreads / team - 1) / (kMoveThreads / team);
     return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), kMoveThreads, 0, stream, P);

@@ -1,8 +1,8 @@
 // Sum of squares over a list of gradients, and the list scaled down to a largest norm.
 //
 // The list travels in the kernel's parameters.  It is cut into chunks; every block takes a run of consecutive chunks, finds
-// the first by bisection and walks on from there.  HBM bounds both passes.  The second walks its run backwards, from what
-// the first has read last, which L2 still holds; a list that fits there is read from HBM once.
+// the first by bisection and walks on from there.  HBM bounds both passes.  The second walks the list backwards, from
+// what the first has read last, which L2 still holds; a list that fits there is read from HBM once.
 #include <type_traits>
 
 #include "layer_common.h"
@@ -13,7 +13,9 @@ constexpr int kListThreads = 512;
 constexpr int kMostSpans = 768;                  // of a launch: 21 KB of parameters
 constexpr int kFewSpans = 128;                   // 3.6 KB: a short list's launch costs less
 constexpr int kChunkBytes = 32768;
-constexpr int kMostRuns = 1024;                  // blocks whose sums the workspace holds
+constexpr int kAtOnce = kChunkBytes / 16 / kListThreads;             // vectors of a thread, asked for before it uses the first
+constexpr int kMostRuns = 4096;                  // blocks whose sums the workspace holds
+constexpr int kRunChunks = 8;
 constexpr uint64_t kTicketBytes = 256;
 constexpr unsigned kAll = 0xffffffffu;
 
@@ -33,91 +35,101 @@ template <int kMost> struct ListParams {
     float *norm;
 };
 
-// Elements of a span before the first 16-byte boundary of x.
-template <typename T> __device__ __forceinline__ uint32_t head_of(const void *x, uint64_t n) {
-    const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T), head = off ? 16 / sizeof(T) - off : 0;
-    return head < n ? head : static_cast<uint32_t>(n);
-}
+// A chunk of a span: `count` vectors of 16 bytes from `at` on.  The elements before the first 16-byte boundary of x belong to the
+// first chunk, those behind the last whole vector to the last.
+template <typename T> struct Piece {
+    static constexpr int kV = 16 / sizeof(T), kEach = kChunkBytes / 16;
+    using Vec = Pack<T, kV>;
+    uint64_t at;                                 // element
+    int count, head, tail;
+    uint64_t rest;                               // where the tail begins
+    __device__ __forceinline__ Piece(const void *x, uint64_t n, uint32_t chunk, uint32_t chunks) {
+        const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T);
+        const uint32_t before = min(static_cast<uint64_t>(off ? kV - off : 0), n);
+        const uint64_t vectors = (n - before) / kV, first = min(static_cast<uint64_t>(chunk) * kEach, vectors);
+        at = before + first * kV;
+        count = static_cast<int>(min(vectors - first, static_cast<uint64_t>(kEach)));
+        head = chunk == 0 ? before : 0;
+        rest = before + vectors * kV;
+        tail = chunk + 1 == chunks ? static_cast<int>(n - rest) : 0;
+    }
+};
 
-// Sum of squares of a few values, in 64 bits: formed in fp32 unless that leaves its range (values above 1e19 or below 1e-15;
+// Sum of squares of a vector in fp32; `wide` is raised where that leaves the type's range (values above 1e19 or below 1e-15;
 // zeros, of which an idle expert's gradient consists, are told apart).
-template <int V> __device__ __forceinline__ double squares_of(const float *f) {
+template <typename Vec, int kV> __device__ __forceinline__ float squares_of(const Vec &v, bool &wide) {
     float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < V; ++i) s = fmaf(f[i], f[i], s);
-    if (s > 1e-30f && s < 3e38f) return s;
     bool some = false;
 #pragma unroll
-    for (int i = 0; i < V; ++i) some = some || f[i] != 0.0f;
-    if (!some) return 0.0;
-    double d = 0.0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) d = fma(static_cast<double>(f[i]), static_cast<double>(f[i]), d);
-    return d;
+    for (int j = 0; j < kV; ++j) {
+        const float f = to_f32(v.v[j]);
+        s = fmaf(f, f, s);
+        some = some || f != 0.0f;
+    }
+    wide = wide || (some && !(s > 1e-30f && s < 3e38f));
+    return s;
 }
-
-// The chunk's part of a span: vectors of 16 bytes from `head` on; the first chunk has the head too, the last one the rest.
-struct Piece {
-    uint64_t from, until;                        // elements, multiples of the vector from `head`
-    bool head, tail;
-};
-template <typename T> __device__ __forceinline__ Piece piece_of(uint64_t n, uint32_t head, uint32_t chunk, uint32_t chunks) {
-    constexpr uint64_t kEach = kChunkBytes / sizeof(T), kV = 16 / sizeof(T);
-    const uint64_t body = (n - head) / kV * kV, from = min(chunk * kEach, body), until = chunk + 1 == chunks ? body : min(from + kEach, body);
-    return Piece{head + from, head + until, chunk == 0, chunk + 1 == chunks};
-}
+template <typename T> __device__ __forceinline__ double square(T x) { return static_cast<double>(to_f32(x)) * static_cast<double>(to_f32(x)); }
 
 template <typename T> __device__ __forceinline__ double square_piece(const T *x, uint64_t n, uint32_t chunk, uint32_t chunks) {
-    constexpr int kV = 16 / sizeof(T);
-    const uint32_t head = head_of<T>(x, n);
-    const Piece p = piece_of<T>(n, head, chunk, chunks);
-    double sum = 0.0;
-#pragma unroll 4
-    for (uint64_t i = p.from + threadIdx.x * kV; i < p.until; i += kListThreads * kV) {
-        const Pack<T, kV> v = *reinterpret_cast<const Pack<T, kV> *>(x + i);
-        float f[kV];
+    using P = Piece<T>;
+    const P p(x, n, chunk, chunks);
+    const typename P::Vec *const from = reinterpret_cast<const typename P::Vec *>(x + p.at);
+    const int tid = threadIdx.x;
+    typename P::Vec v[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < kV; ++j) f[j] = to_f32(v.v[j]);
-        sum += squares_of<kV>(f);
+    for (int u = 0; u < kAtOnce; ++u)
+        if (tid + u * kListThreads < p.count) v[u] = from[tid + u * kListThreads];
+    double sum = 0.0;
+    bool wide = false;
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+        if (tid + u * kListThreads < p.count) sum += static_cast<double>(squares_of<typename P::Vec, P::kV>(v[u], wide));
+    if (wide) {                                  // once more, in 64 bits
+        sum = 0.0;
+#pragma unroll 1
+        for (int i = tid; i < p.count; i += kListThreads)
+#pragma unroll 1
+            for (int j = 0; j < P::kV; ++j) sum += square(x[p.at + static_cast<uint64_t>(i) * P::kV + j]);
     }
-    if (p.head && threadIdx.x < head) {
-        const float f = to_f32(x[threadIdx.x]);
-        sum += squares_of<1>(&f);
-    }
-    if (p.tail && threadIdx.x < n - p.until) {
-        const float f = to_f32(x[p.until + threadIdx.x]);
-        sum += squares_of<1>(&f);
-    }
+    if (tid < p.head) sum += square(x[tid]);
+    if (tid < p.tail) sum += square(x[p.rest + tid]);
     return sum;
 }
 
 template <typename T> __device__ __forceinline__ void scale_piece(const T *x, T *y, uint64_t n, uint32_t chunk, uint32_t chunks, float by) {
-    constexpr int kV = 16 / sizeof(T);
-    const uint32_t head = head_of<T>(x, n);
-    const Piece p = piece_of<T>(n, head, chunk, chunks);
+    using P = Piece<T>;
+    const P p(x, n, chunk, chunks);
+    const int tid = threadIdx.x;
     if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15u) == 0) {
-#pragma unroll 4
-        for (uint64_t i = p.from + threadIdx.x * kV; i < p.until; i += kListThreads * kV) {
-            Pack<T, kV> v = *reinterpret_cast<const Pack<T, kV> *>(x + i);
+        const typename P::Vec *const from = reinterpret_cast<const typename P::Vec *>(x + p.at);
+        typename P::Vec *const to = reinterpret_cast<typename P::Vec *>(y + p.at);
+        typename P::Vec v[kAtOnce];
 #pragma unroll
-            for (int j = 0; j < kV; ++j) v.v[j] = from_f32<T>(to_f32(v.v[j]) * by);
-            *reinterpret_cast<Pack<T, kV> *>(y + i) = v;
-        }
+        for (int u = 0; u < kAtOnce; ++u)
+            if (tid + u * kListThreads < p.count) v[u] = from[tid + u * kListThreads];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (tid + u * kListThreads < p.count) {
+#pragma unroll
+                for (int j = 0; j < P::kV; ++j) v[u].v[j] = from_f32<T>(to_f32(v[u].v[j]) * by);
+                to[tid + u * kListThreads] = v[u];
+            }
     } else {                                     // the two do not meet 16-byte boundaries together
 #pragma unroll 4
-        for (uint64_t i = p.from + threadIdx.x; i < p.until; i += kListThreads) y[i] = from_f32<T>(to_f32(x[i]) * by);
+        for (int i = tid; i < p.count * P::kV; i += kListThreads) y[p.at + i] = from_f32<T>(to_f32(x[p.at + i]) * by);
     }
-    if (p.head && threadIdx.x < head) y[threadIdx.x] = from_f32<T>(to_f32(x[threadIdx.x]) * by);
-    if (p.tail && threadIdx.x < n - p.until) y[p.until + threadIdx.x] = from_f32<T>(to_f32(x[p.until + threadIdx.x]) * by);
+    if (tid < p.head) y[tid] = from_f32<T>(to_f32(x[tid]) * by);
+    if (tid < p.tail) y[p.rest + tid] = from_f32<T>(to_f32(x[p.rest + tid]) * by);
 }
 
-// The block's run of chunks, and the span that holds the first of them.
+// A block's run of chunks, and the span that holds the first of them.
 template <int kMost> struct Run {
     uint32_t at, until;
     int span;
-    __device__ __forceinline__ explicit Run(const ListParams<kMost> &P) {
-        at = static_cast<uint32_t>(static_cast<uint64_t>(P.chunks) * blockIdx.x / gridDim.x);
-        until = static_cast<uint32_t>(static_cast<uint64_t>(P.chunks) * (blockIdx.x + 1) / gridDim.x);
+    __device__ __forceinline__ Run(const ListParams<kMost> &P, uint32_t which) {
+        at = static_cast<uint32_t>(static_cast<uint64_t>(P.chunks) * which / gridDim.x);
+        until = static_cast<uint32_t>(static_cast<uint64_t>(P.chunks) * (which + 1) / gridDim.x);
     }
     __device__ __forceinline__ void find(const ListParams<kMost> &P, uint32_t chunk) {   // the last span that starts at or before it
         int lo = 0, hi = P.count - 1;
@@ -131,12 +143,12 @@ template <int kMost> struct Run {
 };
 
 // Adds the blocks' sums, in their order, when all are there; fp64 of the block's own sum in every thread of the first warp.
-template <int kMost> __global__ void __launch_bounds__(kListThreads) gradient_squares_kernel(const __grid_constant__ ListParams<kMost> P) {
+template <int kMost> __global__ void __launch_bounds__(kListThreads, 2) gradient_squares_kernel(const __grid_constant__ ListParams<kMost> P) {
     wait_for_previous();
     let_next_start();
     __shared__ double fold[kListThreads / 32];
     __shared__ bool last;
-    Run<kMost> r(P);
+    Run<kMost> r(P, blockIdx.x);
     double sum = 0.0;
     if (r.at < r.until) r.find(P, r.at);
     for (; r.at < r.until; ++r.at) {
@@ -153,7 +165,7 @@ template <int kMost> __global__ void __launch_bounds__(kListThreads) gradient_sq
     if (warp == 0) {
         sum = lane < kListThreads / 32 ? fold[lane] : 0.0;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+        for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
     }
     if (threadIdx.x == 0) {
         P.part[blockIdx.x] = sum;
@@ -161,12 +173,18 @@ template <int kMost> __global__ void __launch_bounds__(kListThreads) gradient_sq
         last = atomicAdd(P.ticket, 1u) == gridDim.x - 1;
     }
     __syncthreads();
-    if (!last || warp != 0) return;
+    if (!last) return;
     __threadfence();
     sum = 0.0;
-    for (unsigned i = lane; i < gridDim.x; i += 32) sum += __ldcg(P.part + i);
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += kListThreads) sum += __ldcg(P.part + i);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+    if (lane == 0) fold[warp] = sum;
+    __syncthreads();
+    if (warp != 0) return;
+    sum = lane < kListThreads / 32 ? fold[lane] : 0.0;
+#pragma unroll
+    for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
     if (lane == 0) {
         if (!P.begin) sum += *P.running;
         if (P.end) *P.squares = sum;
@@ -175,13 +193,13 @@ template <int kMost> __global__ void __launch_bounds__(kListThreads) gradient_sq
     }
 }
 
-template <int kMost> __global__ void __launch_bounds__(kListThreads) gradient_clip_kernel(const __grid_constant__ ListParams<kMost> P) {
+template <int kMost> __global__ void __launch_bounds__(kListThreads, 2) gradient_clip_kernel(const __grid_constant__ ListParams<kMost> P) {
     wait_for_previous();
     let_next_start();
     const double norm = sqrt(*P.in);
     if (P.begin && blockIdx.x == 0 && threadIdx.x == 0 && P.norm) *P.norm = static_cast<float>(norm);
     const float by = norm <= P.max_norm ? 1.0f : static_cast<float>(P.max_norm / norm);
-    Run<kMost> r(P);
+    Run<kMost> r(P, gridDim.x - 1 - blockIdx.x);
     if (r.at >= r.until) return;
     r.find(P, r.until - 1);
     for (uint32_t c = r.until; c-- > r.at;) {
@@ -237,8 +255,9 @@ template <int kMost, bool kClip> int launch_list(const loco_span_t *s, int32_t c
     int32_t at = 0;
     do {
         at = fill_list(P, s, count, at);
-        const int64_t most = sms * 4 < kMostRuns ? sms * 4 : kMostRuns;
-        const unsigned blocks = P.chunks < 1 ? 1 : P.chunks > most ? static_cast<unsigned>(most) : P.chunks;
+        // runs of kRunChunks: more blocks than run at once, of which the SMs that are nearer to memory take more
+        const int64_t few = sms * 3, runs = P.chunks <= few ? P.chunks : P.chunks / kRunChunks < few ? few : P.chunks / kRunChunks;
+        const unsigned blocks = runs < 1 ? 1 : runs > kMostRuns ? kMostRuns : static_cast<unsigned>(runs);
         const int rc = launch_kernel(kClip ? gradient_clip_kernel<kMost> : gradient_squares_kernel<kMost>, dim3(blocks), kListThreads, 0, stream, P);
         if (rc != LOCO_OK) return rc;
     } while (at < count);

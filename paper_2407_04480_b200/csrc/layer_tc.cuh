@@ -5,6 +5,10 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <cstring>
+
+#include "layer_common.h"
+
 namespace loco_layer {
 namespace tc {
 
@@ -192,6 +196,30 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
+}
+// Elements 2q and 2q + 1 of a vector in fp32 (a vector of one: the element and 0), and back, rounded.  bfloat16 in pairs: a shift
+// and a mask one way, one conversion the other.
+template <typename T, int V> __device__ __forceinline__ float2 pair_of(const Pack<T, V> &p, int q) {
+    if constexpr (V == 1) {
+        return make_float2(to_f32(p.v[0]), 0.0f);
+    } else if constexpr (sizeof(T) == 2) {
+        uint32_t w;
+        memcpy(&w, &p.v[2 * q], 4);
+        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    } else {
+        return make_float2(to_f32(p.v[2 * q]), to_f32(p.v[2 * q + 1]));
+    }
+}
+template <typename T, int V> __device__ __forceinline__ void set_pair(Pack<T, V> &p, int q, float2 f) {
+    if constexpr (V == 1) {
+        p.v[0] = from_f32<T>(f.x);
+    } else if constexpr (sizeof(T) == 2) {
+        const uint32_t w = pack_bf16(f.x, f.y);
+        memcpy(&p.v[2 * q], &w, 4);
+    } else {
+        p.v[2 * q] = from_f32<T>(f.x);
+        p.v[2 * q + 1] = from_f32<T>(f.y);
+    }
 }
 // Largest of three or two, NaN if one is.
 __device__ __forceinline__ float max3(float a, float b, float c) {
