@@ -22,23 +22,30 @@ int sm_count();
 // here calls wait_for_previous() before it touches global memory, which restores the stream's order, and then
 // let_next_start().  A call in a row of short ones takes 2 to 4 us less that way.
 template <typename... Params, typename... Args>
-int launch_kernel(void (*fn)(Params...), dim3 grid, unsigned threads, size_t shared, void *stream, const Args &...args) {
+int launch_clusters(void (*fn)(Params...), dim3 grid, unsigned threads, size_t shared, void *stream, unsigned cluster, const Args &...args) {
     cudaLaunchConfig_t how{};
     how.gridDim = grid;
     how.blockDim = dim3(threads);
     how.dynamicSmemBytes = shared;
     how.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute early{};
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    how.attrs = &early;
-    how.numAttrs = 1;
+    cudaLaunchAttribute attrs[2]{};
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = cluster;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    how.attrs = attrs;
+    how.numAttrs = cluster > 1 ? 2 : 1;
     if (cudaLaunchKernelEx(&how, fn, args...) != cudaSuccess) {
         cudaGetLastError();
         return LOCO_ERR_CUDA;
     }
     g_launches.fetch_add(1);
     return LOCO_OK;
+}
+template <typename... Params, typename... Args>
+int launch_kernel(void (*fn)(Params...), dim3 grid, unsigned threads, size_t shared, void *stream, const Args &...args) {
+    return launch_clusters(fn, grid, threads, shared, stream, 1, args...);
 }
 
 // Returns when the launch before is complete and its results are visible.

@@ -35,7 +35,7 @@ struct ProductParams {
 
 constexpr int kMostStages = 8;
 struct ProductShared {
-    uint64_t full[kMostStages], empty[kMostStages], ready[2], written[2], drain;
+    uint64_t full[kMostStages], empty[kMostStages], clean[kMostStages], ready[2], written[2], drain;
     uint32_t tmem, failed;
     int32_t begin[kMostExperts], count[kMostExperts], first[kMostExperts + 1];      // rows of an expert, its tiles before
 };
@@ -59,28 +59,109 @@ __device__ __forceinline__ void load_box3(uint32_t to, const CUtensorMap *map, i
 struct Tile {
     int expert, row, col, rows, steps;           // first row within the expert (product) or the matrix (weights), columns; rows of the expert, steps of the contraction
 };
-template <bool kWeights, int kCols> struct Walk {
+template <bool kWeights, int kRows, int kCols> struct Walk {
     int expert = 0;
     __device__ __forceinline__ Tile at(const ProductShared &S, const ProductParams &P, int tile) {
         const int across = (P.wide + kCols - 1) / kCols;
         if constexpr (kWeights) {
-            const int down = (P.high + kTileRows - 1) / kTileRows, each = down * across;
+            const int down = (P.high + kRows - 1) / kRows, each = down * across;
             expert = tile / each;
             const int r = tile - expert * each, n = S.count[expert];
-            return Tile{expert, r % down * kTileRows, r / down * kCols, n, (n + kStep - 1) / kStep};
+            return Tile{expert, r % down * kRows, r / down * kCols, n, (n + kStep - 1) / kStep};
         } else {
             while (tile >= S.first[expert + 1] * across) ++expert;
             const int down = S.first[expert + 1] - S.first[expert], r = tile - S.first[expert] * across;
             // bands of eight tiles of rows, column by column, so that the blocks at work share rows and columns in L2
             const int band = r / (8 * across), high = min(8, down - band * 8), q = r - band * 8 * across;
-            return Tile{expert, (band * 8 + q % high) * kTileRows, q / high * kCols, S.count[expert], (P.deep + kStep - 1) / kStep};
+            return Tile{expert, (band * 8 + q % high) * kRows, q / high * kCols, S.count[expert], (P.deep + kStep - 1) / kStep};
         }
     }
 };
 
+// Zeros in the rows from `left` on up to the next step of 16 in each of kBlocks blocks of 64 columns, by one warp.
+template <int kBlocks> __device__ __forceinline__ void clean_rows(uint8_t *stage, int left, int lane) {
+    const int end = (left + 15) / 16 * 16;
+    for (int x = 0; x < kBlocks; ++x)
+        for (int i = left * 8 + lane; i < end * 8; i += 32) reinterpret_cast<uint4 *>(stage + x * (kStep * 128))[i] = make_uint4(0, 0, 0, 0);
+    fence_async_shared();
+    __syncwarp();
+}
+
+// Rows of every expert, and the tiles of kRows rows before it, to shared memory; by the whole block.
+template <int kRows> __device__ __forceinline__ void find_rows(ProductShared &S, const ProductParams &P) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    for (int e = threadIdx.x; e < P.experts; e += kProductThreads) {       // offsets are clamped to the tensor, whatever they hold
+        const int64_t lo = min(max(static_cast<int64_t>(P.offsets[e]), static_cast<int64_t>(0)), P.rows);
+        const int64_t hi = min(max(static_cast<int64_t>(P.offsets[e + 1]), lo), P.rows);
+        S.begin[e] = static_cast<int>(lo);
+        S.count[e] = static_cast<int>(hi - lo);
+    }
+    __syncthreads();
+    if (warp == 0) {                             // tiles of rows before each expert
+        int before = 0;
+        for (int e0 = 0; e0 < P.experts; e0 += 32) {
+            const int e = e0 + lane;
+            int n = e < P.experts ? (S.count[e] + kRows - 1) / kRows : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, n, o);
+                n += lane >= o ? y : 0;
+            }
+            if (e < P.experts) S.first[e + 1] = before + n;
+            before += __shfl_sync(0xffffffffu, n, 31);
+        }
+        if (lane == 0) S.first[0] = 0;
+    }
+}
+
 __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
     const uint64_t begin = now_ns();
     while (!bar_test(bar, parity) && now_ns() - begin < kWaitLimitNs / 20) {}
+}
+
+// A writing warp's 32 rows of a tile's accumulator, `below` rows into the tile, through shared memory to whole rows of the output;
+// `done` is called by one lane when the accumulator has been read.  Zeros for a tile without a contraction.
+template <bool kWeights, int kCols, typename Done>
+__device__ __forceinline__ void write_tile(const ProductShared &S, const ProductParams &P, const Tile &t, int below, uint32_t accumulator, uint8_t *staging,
+                                           const Done &done) {
+    const int lane = threadIdx.x % 32, part = threadIdx.x / 32 % 4, first = t.row + below + part * 32;
+    uint8_t *const stage = staging + part * kStageOut;
+    const int live = min((kWeights ? P.high : t.rows) - first, 32);                     // rows that are written
+    __nv_bfloat16 *const out = P.out + (kWeights ? t.expert * P.out_expert : S.begin[t.expert] * P.out_row) + first * P.out_row;
+    const int cols = min(kCols, P.wide - t.col);
+    for (int c = 0; c < kCols; c += 64) {
+        if (t.steps > 0) {
+            uint32_t r[2][32];
+            const uint32_t at = accumulator + c + (static_cast<uint32_t>(part * 32) << 16);
+            load_columns(at, r[0]);
+            load_columns(at + 32, r[1]);
+            wait_loads();
+            pin(r[0]);
+            pin(r[1]);
+            if (c + 64 >= kCols) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) done();
+            }
+#pragma unroll
+            for (int i = 0; i < 64; i += 8) {
+                uint4 w;
+                const uint32_t *f = &r[i / 32][i % 32];
+                w.x = pack_bf16(__uint_as_float(f[0]), __uint_as_float(f[1]));
+                w.y = pack_bf16(__uint_as_float(f[2]), __uint_as_float(f[3]));
+                w.z = pack_bf16(__uint_as_float(f[4]), __uint_as_float(f[5]));
+                w.w = pack_bf16(__uint_as_float(f[6]), __uint_as_float(f[7]));
+                *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i / 8 ^ lane % 8) << 4)) = w;
+            }
+            __syncwarp();
+        }
+        const int piece = lane % 8, col = c + piece * 8;
+        if (col < cols)
+            for (int row = lane / 8; row < live; row += 4)
+                *reinterpret_cast<uint4 *>(out + row * P.out_row + t.col + col) =
+                    t.steps > 0 ? *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ row % 8) << 4)) : make_uint4(0, 0, 0, 0);
+        __syncwarp();
+    }
 }
 
 // kDown: B's rows are the contraction (matrices [in, out], and weights), else its columns.
@@ -111,28 +192,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if (warp == kIssueWarp) tmem_alloc<kTmem>(smem_addr(&S.tmem));
     wait_for_previous();
     let_next_start();
-    for (int e = threadIdx.x; e < P.experts; e += kProductThreads) {       // offsets are clamped to the tensor, whatever they hold
-        const int64_t lo = min(max(static_cast<int64_t>(P.offsets[e]), static_cast<int64_t>(0)), P.rows);
-        const int64_t hi = min(max(static_cast<int64_t>(P.offsets[e + 1]), lo), P.rows);
-        S.begin[e] = static_cast<int>(lo);
-        S.count[e] = static_cast<int>(hi - lo);
-    }
-    __syncthreads();
-    if (warp == 0) {                             // tiles of rows before each expert
-        int before = 0;
-        for (int e0 = 0; e0 < P.experts; e0 += 32) {
-            const int e = e0 + lane;
-            int n = e < P.experts ? (S.count[e] + kTileRows - 1) / kTileRows : 0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, n, o);
-                n += lane >= o ? y : 0;
-            }
-            if (e < P.experts) S.first[e + 1] = before + n;
-            before += __shfl_sync(0xffffffffu, n, 31);
-        }
-        if (lane == 0) S.first[0] = 0;
-    }
+    find_rows<kTileRows>(S, P);
     fence_before();
     __syncthreads();
     fence_after();
@@ -141,7 +201,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     const int tiles = kWeights ? P.experts * ((P.high + kTileRows - 1) / kTileRows) * across : S.first[P.experts] * across;
     const int stride = static_cast<int>(gridDim.x);
     const uint32_t base = smem_addr(ring);
-    Walk<kWeights, kCols> walk;
+    Walk<kWeights, kTileRows, kCols> walk;
 
     if (warp == kLoadWarp) {
         if (lane == 0) {
@@ -194,22 +254,17 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             for (int k = 0; k < t.steps; ++k) {
                 bar_wait(smem_addr(&S.full[slot]), phase, failed);
                 __syncwarp();
-                const int left = t.rows - k * kStep;
-                if (kWeights && left < kStep) {  // rows past the expert's last
-                    uint4 *const at = reinterpret_cast<uint4 *>(ring + slot * kBytes);
-                    for (int x = 0; x < (kTileRows + kCols) / 64; ++x)
-                        for (int i = left * 8 + lane; i < kStep * 8; i += 32) at[x * (kStep * 8) + i] = make_uint4(0, 0, 0, 0);
-                    fence_async_shared();
-                    __syncwarp();
-                }
+                const int left = kWeights ? t.rows - k * kStep : kStep;
+                if (left < kStep) clean_rows<(kTileRows + kCols) / 64>(ring + slot * kBytes, left, lane);
                 fence_after();
                 const uint32_t a = base + slot * kBytes, b = a + kTileRows * 128;
                 const uint32_t da = kWeights ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
                 const uint32_t db = kWeights || kDown ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
 #pragma unroll
                 for (int x = 0; x < kStep; x += 16)
-                    mma_ss(lead, tmem + buffer * kCols, da + (kWeights ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights || kDown ? x * 128 >> 4 : x * 2 >> 4), word,
-                           k > 0 || x > 0);
+                    if (!kWeights || x < left)   // whole steps past the expert's last row are left out
+                        mma_ss(lead, tmem + buffer * kCols, da + (kWeights ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights || kDown ? x * 128 >> 4 : x * 2 >> 4), word,
+                               k > 0 || x > 0);
                 commit(lead, smem_addr(&S.empty[slot]));
                 if (++slot == kStages) {
                     slot = 0;
@@ -224,53 +279,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         bar_wait(smem_addr(&S.drain), 0, failed);
         if (*failed) settle(smem_addr(&S.drain), 0);
     } else if (warp >= kWriteWarps) {
-        const int part = warp % 4;
-        uint8_t *const stage = staging + part * kStageOut;
         int buffer = 0, turn = 0;
         for (int tile = blockIdx.x; tile < tiles; tile += stride) {
             const Tile t = walk.at(S, P, tile);
-            const int limit = kWeights ? P.high : t.rows;
-            const int live = min(limit - t.row - part * 32, 32);         // rows of this warp that are written
-            __nv_bfloat16 *const out = P.out + (kWeights ? t.expert * P.out_expert : S.begin[t.expert] * P.out_row) + (t.row + part * 32ll) * P.out_row;
             if (t.steps > 0) {
                 bar_wait(smem_addr(&S.ready[buffer]), turn, failed);
                 __syncwarp();
                 fence_after();
             }
-            const int cols = min(kCols, P.wide - t.col);
-            for (int c = 0; c < kCols; c += 64) {
-                if (t.steps > 0) {
-                    uint32_t r[2][32];
-                    const uint32_t at = tmem + buffer * kCols + c + (static_cast<uint32_t>(part * 32) << 16);
-                    load_columns(at, r[0]);
-                    load_columns(at + 32, r[1]);
-                    wait_loads();
-                    pin(r[0]);
-                    pin(r[1]);
-                    if (c + 64 >= kCols) {
-                        fence_before();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(smem_addr(&S.written[buffer]));
-                    }
-#pragma unroll
-                    for (int i = 0; i < 64; i += 8) {
-                        uint4 w;
-                        const uint32_t *f = &r[i / 32][i % 32];
-                        w.x = pack_bf16(__uint_as_float(f[0]), __uint_as_float(f[1]));
-                        w.y = pack_bf16(__uint_as_float(f[2]), __uint_as_float(f[3]));
-                        w.z = pack_bf16(__uint_as_float(f[4]), __uint_as_float(f[5]));
-                        w.w = pack_bf16(__uint_as_float(f[6]), __uint_as_float(f[7]));
-                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i / 8 ^ lane % 8) << 4)) = w;
-                    }
-                    __syncwarp();
-                }
-                const int piece = lane % 8, col = c + piece * 8;
-                if (col < cols)
-                    for (int row = lane / 8; row < live; row += 4)
-                        *reinterpret_cast<uint4 *>(out + row * P.out_row + t.col + col) =
-                            t.steps > 0 ? *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ row % 8) << 4)) : make_uint4(0, 0, 0, 0);
-                __syncwarp();
-            }
+            write_tile<kWeights, kCols>(S, P, t, 0, tmem + buffer * kCols, staging, [&] { bar_arrive(smem_addr(&S.written[buffer])); });
             if (t.steps > 0) {
                 buffer ^= 1;
                 if (buffer == 0) turn ^= 1;
@@ -282,6 +299,220 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     __syncthreads();
     fence_after();
     if (warp == kIssueWarp) tmem_free<kTmem>(tmem);
+    if (threadIdx.x == 0 && S.failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
+}
+
+// ---- two SMs to a tile -----------------------------------------------------------------------
+
+// Tiles of 256 x 256 by a cluster of two blocks: each holds 128 rows of A and 128 columns of B, and 128 rows of the accumulator;
+// the products, issued by the first, read both.  Against one SM's 128 x 256 each byte of B is copied to and read from shared
+// memory half as often.
+constexpr int kPairRows = 256, kPairCols = 256, kPairStage = 2 * kTileRows * 128;
+constexpr int kPairStages = (227 * 1024 - 1024 - kWriteWarps * kStageOut - static_cast<int>(sizeof(ProductShared))) / kPairStage;
+constexpr int kPairBytes = 1024 + kPairStages * kPairStage + kWriteWarps * kStageOut + static_cast<int>(sizeof(ProductShared));
+static_assert(kPairStages <= kMostStages && kPairBytes <= 227 * 1024, "shared memory of a block");
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// The same place in the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void bar_arrive_in(uint32_t bar) {        // in any block of the cluster
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// What a block of the cluster has arrived with is visible after this; the wait before has passed or given up.
+__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+// A box to this block's shared memory; completes on a barrier of either block.
+__device__ __forceinline__ void load_box3_pair(uint32_t to, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+template <int kColumns> __device__ __forceinline__ void tmem_alloc_pair(uint32_t to) {       // one warp of each block
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "n"(kColumns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+template <int kColumns> __device__ __forceinline__ void tmem_free_pair(uint32_t at) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "n"(kColumns) : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t word, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p, q;\n .reg .b64 a, b;\n mov.b64 a, {%1, %6};\n mov.b64 b, {%2, %6};\n setp.ne.u32 p, %4, 0;\n setp.ne.u32 q, %5, 0;\n"
+                 " @q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "r"(b), "r"(word), "r"(accumulate), "r"(lead), "r"(kDescHigh) : "memory");
+}
+// Arrives on the barrier of both blocks when every product issued is complete.
+__device__ __forceinline__ void commit_pair(uint32_t lead, uint32_t bar) {
+    asm volatile("{\n .reg .pred q;\n .reg .b16 m;\n setp.ne.u32 q, %1, 0;\n mov.b16 m, 3;\n"
+                 " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n}\n"
+                 ::"r"(bar), "r"(lead) : "memory");
+}
+
+template <bool kWeights, bool kDown>
+__global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
+    extern __shared__ uint8_t raw[];
+    uint8_t *const ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint8_t *const staging = ring + kPairStages * kPairStage;
+    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * kStageOut);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = cluster_rank();
+    volatile uint32_t *const failed = &S.failed;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPairStages; ++i) {
+            bar_init(smem_addr(&S.full[i]), 1);                      // the first block's: both blocks' copies, but for one with rows past
+            bar_init(smem_addr(&S.empty[i]), 1);                     // an expert's end in it; the second's: such a copy of its own
+            bar_init(smem_addr(&S.clean[i]), 1);                     // the first block's: those rows are zero in the second
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_addr(&S.ready[i]), 1);
+            bar_init(smem_addr(&S.written[i]), 2 * kWriteWarps);     // the first block's: both blocks' warps
+        }
+        bar_init(smem_addr(&S.drain), 1);
+        S.failed = 0;
+        fence_bar_init();
+        fence_async_shared();
+    }
+    if (warp == kIssueWarp) tmem_alloc_pair<512>(smem_addr(&S.tmem));
+    wait_for_previous();
+    let_next_start();
+    find_rows<kPairRows>(S, P);
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+    const uint32_t tmem = S.tmem;
+    const int across = (P.wide + kPairCols - 1) / kPairCols;
+    const int tiles = kWeights ? P.experts * ((P.high + kPairRows - 1) / kPairRows) * across : S.first[P.experts] * across;
+    const int begin = static_cast<int>(blockIdx.x) / 2, stride = static_cast<int>(gridDim.x) / 2;
+    const uint32_t base = smem_addr(ring);
+    Walk<kWeights, kPairRows, kPairCols> walk;
+
+    if (warp == kLoadWarp) {
+        if (lane == 0) {
+            int slot = 0, phase = 0, issued = 0;
+            for (int tile = begin; tile < tiles && !*failed; tile += stride) {
+                const Tile t = walk.at(S, P, tile);
+                const int first = S.begin[t.expert], row = t.row + rank * kTileRows, col = t.col + rank * kTileRows;
+                for (int k = 0; k < t.steps; ++k) {
+                    bar_wait(smem_addr(&S.empty[slot]), phase ^ 1, failed);
+                    if (*failed) break;
+                    const bool ragged = kWeights && t.rows - k * kStep < kStep;
+                    const uint32_t a = base + slot * kPairStage, b = a + kTileRows * 128;
+                    const uint32_t bar = in_block(smem_addr(&S.full[slot]), ragged ? rank : 0);
+                    if (rank == 0 || ragged) bar_expect(smem_addr(&S.full[slot]), ragged ? kPairStage : 2 * kPairStage);
+                    if constexpr (kWeights) {
+#pragma unroll
+                        for (int x = 0; x < kTileRows; x += 64) {
+                            load_box3_pair(a + x * 128, &M.a, row + x, first + k * kStep, 0, bar);
+                            load_box3_pair(b + x * 128, &M.b, col + x, first + k * kStep, 0, bar);
+                        }
+                    } else {
+                        load_box3_pair(a, &M.a, k * kStep, first + row, 0, bar);
+                        if constexpr (kDown) {
+#pragma unroll
+                            for (int x = 0; x < kTileRows; x += 64) load_box3_pair(b + x * 128, &M.b, col + x, k * kStep, t.expert, bar);
+                        } else {
+                            load_box3_pair(b, &M.b, k * kStep, col, t.expert, bar);
+                        }
+                    }
+                    ++issued;
+                    if (++slot == kPairStages) {
+                        slot = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            for (int i = 0; i < kPairStages && i < issued; ++i) {    // the first block's products say so in this one's memory
+                slot = slot ? slot - 1 : kPairStages - 1;
+                if (slot == kPairStages - 1) phase ^= 1;
+                bar_wait(smem_addr(&S.empty[slot]), phase, failed);
+            }
+            if (*failed && issued > 0) {         // copies in flight end before the blocks' shared memory goes away: nothing tells when, so
+                const uint64_t from = now_ns();  // they get far more time than a copy takes
+                while (now_ns() - from < 1000000ull) {}
+            }
+        }
+    } else if (warp == kIssueWarp) {
+        const uint32_t lead = elect_lane();
+        constexpr uint32_t word = (product(kPairCols, kDown || kWeights) & 0x00ffffffu) | (16u << 24) | (kWeights ? 1u << 15 : 0u);      // 256 rows
+        int slot = 0, phase = 0, buffer = 0, turn = 0;
+        uint32_t ends = 0;                       // by slot: the phase of its next tile with rows past an end (rank 0: of `clean`, rank 1: of `full`)
+        for (int tile = begin; tile < tiles; tile += stride) {
+            const Tile t = walk.at(S, P, tile);
+            if (t.steps == 0) continue;
+            if (rank == 0) {
+                bar_wait(smem_addr(&S.written[buffer]), turn ^ 1, failed);
+                fence_after();
+            }
+            for (int k = 0; k < t.steps; ++k) {
+                const int left = kWeights ? t.rows - k * kStep : kStep;
+                if (rank == 0) {
+                    bar_wait(smem_addr(&S.full[slot]), phase, failed);
+                    __syncwarp();
+                    if (left < kStep) {
+                        clean_rows<2 * kTileRows / 64>(ring + slot * kPairStage, left, lane);
+                        bar_wait(smem_addr(&S.clean[slot]), ends >> slot & 1, failed);
+                        fence_cluster();
+                    }
+                    fence_after();
+                    const uint32_t a = base + slot * kPairStage, b = a + kTileRows * 128;
+                    const uint32_t da = kWeights ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
+                    const uint32_t db = kWeights || kDown ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
+#pragma unroll
+                    for (int x = 0; x < kStep; x += 16)
+                        if (!kWeights || x < left)
+                            mma_pair(lead, tmem + buffer * kPairCols, da + (kWeights ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights || kDown ? x * 128 >> 4 : x * 2 >> 4),
+                                     word, k > 0 || x > 0);
+                    commit_pair(lead, smem_addr(&S.empty[slot]));
+                } else if (left < kStep) {
+                    bar_wait(smem_addr(&S.full[slot]), ends >> slot & 1, failed);
+                    __syncwarp();
+                    clean_rows<2 * kTileRows / 64>(ring + slot * kPairStage, left, lane);
+                    if (lane == 0) bar_arrive_in(in_block(smem_addr(&S.clean[slot]), 0));
+                }
+                if (left < kStep) ends ^= 1u << slot;
+                if (++slot == kPairStages) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+            }
+            if (rank == 0) commit_pair(lead, smem_addr(&S.ready[buffer]));
+            buffer ^= 1;
+            if (buffer == 0) turn ^= 1;
+        }
+        if (rank == 0) commit_pair(lead, smem_addr(&S.drain));
+        bar_wait(smem_addr(&S.drain), 0, failed);
+        if (*failed) settle(smem_addr(&S.drain), 0);
+    } else if (warp >= kWriteWarps) {
+        int buffer = 0, turn = 0;
+        for (int tile = begin; tile < tiles; tile += stride) {
+            const Tile t = walk.at(S, P, tile);
+            if (t.steps > 0) {
+                bar_wait(smem_addr(&S.ready[buffer]), turn, failed);
+                __syncwarp();
+                fence_after();
+            }
+            write_tile<kWeights, kPairCols>(S, P, t, rank * kTileRows, tmem + buffer * kPairCols, staging,
+                                            [&] { bar_arrive_in(in_block(smem_addr(&S.written[buffer]), 0)); });
+            if (t.steps > 0) {
+                buffer ^= 1;
+                if (buffer == 0) turn ^= 1;
+            }
+        }
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    cluster_sync();                              // neither block leaves while the other's products read it or its arrivals are under way
+    fence_after();
+    if (warp == kIssueWarp) tmem_free_pair<512>(tmem);
     if (threadIdx.x == 0 && S.failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
 }
 
@@ -356,6 +587,15 @@ template <bool kWeights, bool kDown, int kCols> int launch_product(const Product
     return launch_kernel(fn, dim3(static_cast<unsigned>(tiles < sms ? tiles : sms)), kProductThreads, product_bytes<kCols>(), stream, P, M);
 }
 
+template <bool kWeights, bool kDown> int launch_pair(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
+    const int pairs = sm_count() / 2;
+    if (pairs == 0) return LOCO_ERR_CUDA;
+    if (tiles > 0x7fffffff - pairs) return LOCO_ERR_UNSUPPORTED;
+    constexpr ProductKernel fn = product_pair_kernel<kWeights, kDown>;
+    if (!allow(fn, which, kPairBytes)) return LOCO_ERR_CUDA;
+    return launch_clusters(fn, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), kProductThreads, kPairBytes, stream, 2, P, M);
+}
+
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
@@ -381,10 +621,16 @@ int loco_experts_product(const loco_product_t *c, const loco_rows_t *x, const lo
     ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(y->ptr), 0, c->rows > 1 ? y->row_stride : 0, c->rows, c->experts, c->d_in, 0, c->d_out};
     ProductMaps M;
     constexpr int kCols = 256;
+    const bool pair = c->rows >= 192ll * c->experts;
     if (!make_map(M.a, x->ptr, c->d_in, c->rows, 1, x->row_stride, 0, kTileRows) ||
-        !make_map(M.b, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? kCols : kStep)) return LOCO_ERR_CUDA;
+        !make_map(M.b, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? (pair ? kTileRows : kCols) : kStep)) return LOCO_ERR_CUDA;
     // every expert may end in a tile of its own
-    const int64_t tiles = (c->rows / kTileRows + (c->rows < c->experts ? c->rows : c->experts)) * over(c->d_out, kCols);
+    const int64_t ends = c->rows < c->experts ? c->rows : c->experts;
+    if (pair) {
+        const int64_t tiles = (c->rows / kPairRows + ends) * over(c->d_out, kPairCols);
+        return turned ? launch_pair<false, false>(P, M, tiles, 3, stream) : launch_pair<false, true>(P, M, tiles, 4, stream);
+    }
+    const int64_t tiles = (c->rows / kTileRows + ends) * over(c->d_out, kCols);
     return turned ? launch_product<false, false, kCols>(P, M, tiles, 0, stream) : launch_product<false, true, kCols>(P, M, tiles, 1, stream);
 }
 
@@ -402,6 +648,7 @@ int loco_experts_product_weights(const loco_product_t *c, const loco_rows_t *a, 
     const bool none = c->rows == 0;
     if (!make_map(M.a, none ? dw->ptr : a->ptr, c->d_in, none ? 1 : c->rows, 1, none ? 0 : a->row_stride, 0, kStep) ||
         !make_map(M.b, none ? dw->ptr : b->ptr, c->d_out, none ? 1 : c->rows, 1, none ? 0 : b->row_stride, 0, kStep)) return LOCO_ERR_CUDA;
+    if (c->d_in >= kPairRows) return launch_pair<true, true>(P, M, c->experts * over(c->d_in, kPairRows) * over(c->d_out, kPairCols), 5, stream);
     return launch_product<true, true, kCols>(P, M, c->experts * over(c->d_in, kTileRows) * over(c->d_out, kCols), 2, stream);
 }
 
