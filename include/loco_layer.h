@@ -265,7 +265,7 @@ typedef struct {
 /*
  * y_t = x_t W_e, transposed: x_t W_e^T, for the rows t of every expert e; x [rows, d_in], y [rows, d_out]; bfloat16, fp32
  * sums.  The gradient of x is the same call on dy with `transposed` the other way round (d_in and d_out change places).
- * d_offsets: int32 [experts + 1], ascending; they are read on the device and clamped to the rows.  Rows outside every expert
+ * d_offsets: int32 [experts + 1], ascending; they are read on the device, as the largest so far and within the rows.  Rows outside every expert
  * are neither read as numbers nor written.  A NaN or infinity in a row or matrix reaches that row's or expert's outputs only.
  * One launch.  Errors: ARG, ALIGN (a pointer not 16-byte aligned or a stride not a multiple of 8 elements), UNSUPPORTED, CUDA.
  */

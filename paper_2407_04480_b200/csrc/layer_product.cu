@@ -10,6 +10,8 @@
 //             in both, so that whatever lies there (NaN included) adds nothing.
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "layer_maps.h"
 #include "layer_tc.cuh"
 
@@ -21,11 +23,11 @@ constexpr int kMostExperts = 512;
 constexpr int kTileRows = 128;                   // of the accumulator
 constexpr int kStep = 64;                        // of the contraction: a swizzled row of 128 bytes
 constexpr int kProductThreads = 256;
-constexpr int kLoadWarp = 0, kIssueWarp = 1, kWriteWarps = 4;      // the last four write; lanes of TMEM go by the warp's number modulo 4
+constexpr int kLoadWarp = 0, kIssueWarp = 1, kFirstWriter = 4, kWriteWarps = 4;        // lanes of TMEM go by the warp's number modulo 4
 
 __device__ unsigned g_product_status;            // LOCO_LAYER_FLAG_*
 
-struct ProductMaps { CUtensorMap a, b; };
+struct ProductMaps { CUtensorMap a, b, out; };
 struct ProductParams {
     const int32_t *offsets;
     __nv_bfloat16 *out;
@@ -33,27 +35,44 @@ struct ProductParams {
     int32_t experts, deep, high, wide;           // contraction (product), rows of an output matrix (weights), columns of the output
 };
 
-constexpr int kMostStages = 8;
+constexpr int kMostStages = 12;
 struct ProductShared {
     uint64_t full[kMostStages], empty[kMostStages], clean[kMostStages], ready[2], written[2], drain;
     uint32_t tmem, failed;
     int32_t begin[kMostExperts], count[kMostExperts], first[kMostExperts + 1];      // rows of an expert, its tiles before
 };
 constexpr int kStageOut = 32 * 128;              // bytes a writing warp puts 32 rows of 64 columns in
-template <int kCols> __host__ __device__ constexpr int stage_bytes() { return (kTileRows + kCols) * 128; }
-template <int kCols> __host__ __device__ constexpr int stages() {
-    constexpr int n = (227 * 1024 - 1024 - kWriteWarps * kStageOut - static_cast<int>(sizeof(ProductShared))) / stage_bytes<kCols>();
+// Such places of a writing warp: over few rows the matrices' gradient is all writing, and one place is filled while another's is
+// copied out; elsewhere the tiles' contraction covers it, and the memory is better as a stage.
+template <bool kWeights> __host__ __device__ constexpr int places() { return kWeights ? 2 : 1; }
+// Shared memory besides the stages, and up to 1 KB to a boundary.
+template <bool kWeights> __host__ __device__ constexpr int besides() {
+    return 1024 + kWriteWarps * places<kWeights>() * kStageOut + static_cast<int>(sizeof(ProductShared));
+}
+// kRows of A are copied, of the 128 that the product reads: what it reads past them (B, other stages) is in accumulator rows
+// that are not written.
+template <int kRows, int kCols> __host__ __device__ constexpr int stage_bytes() { return (kRows + kCols) * 128; }
+template <bool kWeights, int kRows, int kCols> __host__ __device__ constexpr int stages() {
+    constexpr int n = (227 * 1024 - besides<kWeights>()) / stage_bytes<kRows, kCols>();
     return n < kMostStages ? n : kMostStages;
 }
-template <int kCols> constexpr int product_bytes() {
-    return 1024 + stages<kCols>() * stage_bytes<kCols>() + kWriteWarps * kStageOut + static_cast<int>(sizeof(ProductShared));
+template <bool kWeights, int kRows, int kCols> constexpr int product_bytes() {
+    return besides<kWeights>() + stages<kWeights, kRows, kCols>() * stage_bytes<kRows, kCols>();
 }
-static_assert(product_bytes<256>() <= 227 * 1024 && product_bytes<64>() <= 227 * 1024, "shared memory of a block");
 
 __device__ __forceinline__ void load_box3(uint32_t to, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+
+// 32 rows of 64 columns from a writing warp's part of shared memory; nothing is written past the tensor.
+__device__ __forceinline__ void store_box3(const CUtensorMap *map, uint32_t from, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];\n cp.async.bulk.commit_group;"
+                 ::"l"(map), "r"(from), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// All but the last kLeft such copies have read what they copy.
+template <int kLeft> __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // Where the tiles are.  `walk` goes on to the tile's expert; tiles only grow.
 struct Tile {
@@ -87,31 +106,40 @@ template <int kBlocks> __device__ __forceinline__ void clean_rows(uint8_t *stage
     __syncwarp();
 }
 
-// Rows of every expert, and the tiles of kRows rows before it, to shared memory; by the whole block.
+// Rows of every expert, and the tiles of kRows rows before it, to shared memory.  Offsets are read as the largest so far, within the
+// tensor, whatever they hold: experts' rows never overlap.
 template <int kRows> __device__ __forceinline__ void find_rows(ProductShared &S, const ProductParams &P) {
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    for (int e = threadIdx.x; e < P.experts; e += kProductThreads) {       // offsets are clamped to the tensor, whatever they hold
-        const int64_t lo = min(max(static_cast<int64_t>(P.offsets[e]), static_cast<int64_t>(0)), P.rows);
-        const int64_t hi = min(max(static_cast<int64_t>(P.offsets[e + 1]), lo), P.rows);
-        S.begin[e] = static_cast<int>(lo);
-        S.count[e] = static_cast<int>(hi - lo);
-    }
-    __syncthreads();
-    if (warp == 0) {                             // tiles of rows before each expert
-        int before = 0;
-        for (int e0 = 0; e0 < P.experts; e0 += 32) {
-            const int e = e0 + lane;
-            int n = e < P.experts ? (S.count[e] + kRows - 1) / kRows : 0;
+    const int lane = threadIdx.x % 32;
+    if (threadIdx.x >= 32) return;
+    const auto offset = [&](int e) {
+        const int64_t o = P.offsets[e < P.experts ? e : P.experts];
+        return static_cast<int>(o < 0 ? 0 : o > P.rows ? P.rows : o);
+    };
+    int most = 0, before = 0;                    // of the offsets and of the tiles of the experts before
+    for (int e0 = 0; e0 < P.experts; e0 += 32) {
+        const int e = e0 + lane;
+        int lo = max(offset(e), most);
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, n, o);
-                n += lane >= o ? y : 0;
-            }
-            if (e < P.experts) S.first[e + 1] = before + n;
-            before += __shfl_sync(0xffffffffu, n, 31);
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, lo, o);
+            lo = lane >= o ? max(lo, y) : lo;
         }
-        if (lane == 0) S.first[0] = 0;
+        const int hi = max(offset(e + 1), lo);
+        int n = e < P.experts ? (hi - lo + kRows - 1) / kRows : 0;
+        if (e < P.experts) {
+            S.begin[e] = lo;
+            S.count[e] = hi - lo;
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, n, o);
+            n += lane >= o ? y : 0;
+        }
+        if (e < P.experts) S.first[e + 1] = before + n;
+        before += __shfl_sync(0xffffffffu, n, 31);
+        most = __shfl_sync(0xffffffffu, hi, 31);
     }
+    if (lane == 0) S.first[0] = 0;
 }
 
 __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
@@ -119,60 +147,71 @@ __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
     while (!bar_test(bar, parity) && now_ns() - begin < kWaitLimitNs / 20) {}
 }
 
-// A writing warp's 32 rows of a tile's accumulator, `below` rows into the tile, through shared memory to whole rows of the output;
-// `done` is called by one lane when the accumulator has been read.  Zeros for a tile without a contraction.
-template <bool kWeights, int kCols, typename Done>
-__device__ __forceinline__ void write_tile(const ProductShared &S, const ProductParams &P, const Tile &t, int below, uint32_t accumulator, uint8_t *staging,
-                                           const Done &done) {
-    const int lane = threadIdx.x % 32, part = threadIdx.x / 32 % 4, first = t.row + below + part * 32;
-    uint8_t *const stage = staging + part * kStageOut;
-    const int live = min((kWeights ? P.high : t.rows) - first, 32);                     // rows that are written
-    __nv_bfloat16 *const out = P.out + (kWeights ? t.expert * P.out_expert : S.begin[t.expert] * P.out_row) + first * P.out_row;
-    const int cols = min(kCols, P.wide - t.col);
-    for (int c = 0; c < kCols; c += 64) {
-        if (t.steps > 0) {
-            uint32_t r[2][32];
-            const uint32_t at = accumulator + c + (static_cast<uint32_t>(part * 32) << 16);
-            load_columns(at, r[0]);
-            load_columns(at + 32, r[1]);
-            wait_loads();
-            pin(r[0]);
-            pin(r[1]);
-            if (c + 64 >= kCols) {
-                fence_before();
-                __syncwarp();
-                if (lane == 0) done();
-            }
+// A writing warp's 32 rows of a tile's accumulator, `below` rows into the tile: through shared memory and out with copies of 64
+// columns, or row by row where the expert ends among them.  `done` is called by one lane when
+// the accumulator has been read.  Zeros for a tile without a contraction.
+template <bool kWeights, int kRows, int kCols, typename Done>
+__device__ __forceinline__ void write_tile(const ProductShared &S, const ProductParams &P, const CUtensorMap *map, const Tile &t, int below, uint32_t accumulator,
+                                           uint8_t *staging, const Done &done) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32 - kFirstWriter, part = warp % 4, first = t.row + below + part * 32;
+    const int live = min(min((kWeights ? P.high : t.rows), t.row + kRows) - first, 32), until = min(kCols, P.wide - t.col);
+    if (live > 0)
+        for (int c = 0; c < until; c += 64) {
+            uint8_t *const stage = staging + (warp * places<kWeights>() + c / 64 % places<kWeights>()) * kStageOut;
+            uint4 w[8];
+            if (t.steps > 0) {
+                uint32_t r[2][32];
+                const uint32_t at = accumulator + c + (static_cast<uint32_t>(part * 32) << 16);
+                load_columns(at, r[0]);
+                load_columns(at + 32, r[1]);
+                wait_loads();
+                pin(r[0]);
+                pin(r[1]);
 #pragma unroll
-            for (int i = 0; i < 64; i += 8) {
-                uint4 w;
-                const uint32_t *f = &r[i / 32][i % 32];
-                w.x = pack_bf16(__uint_as_float(f[0]), __uint_as_float(f[1]));
-                w.y = pack_bf16(__uint_as_float(f[2]), __uint_as_float(f[3]));
-                w.z = pack_bf16(__uint_as_float(f[4]), __uint_as_float(f[5]));
-                w.w = pack_bf16(__uint_as_float(f[6]), __uint_as_float(f[7]));
-                *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i / 8 ^ lane % 8) << 4)) = w;
+                for (int i = 0; i < 64; i += 8) {
+                    const uint32_t *f = &r[i / 32][i % 32];
+                    w[i / 8].x = pack_bf16(__uint_as_float(f[0]), __uint_as_float(f[1]));
+                    w[i / 8].y = pack_bf16(__uint_as_float(f[2]), __uint_as_float(f[3]));
+                    w[i / 8].z = pack_bf16(__uint_as_float(f[4]), __uint_as_float(f[5]));
+                    w[i / 8].w = pack_bf16(__uint_as_float(f[6]), __uint_as_float(f[7]));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = make_uint4(0, 0, 0, 0);
             }
+            if (lane == 0) stores_read<places<kWeights>() - 1>();    // the place is free
             __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ lane % 8) << 4)) = w[i];
+            if (kWeights || live == 32) {
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) store_box3(map, smem_addr(stage), t.col + c, (kWeights ? 0 : S.begin[t.expert]) + first, kWeights ? t.expert : 0);
+            } else {
+                __syncwarp();
+                __nv_bfloat16 *const out = P.out + (static_cast<int64_t>(S.begin[t.expert]) + first) * P.out_row + t.col + c;
+                const int piece = lane % 8;
+                if (t.col + c + piece * 8 < P.wide)
+                    for (int row = lane / 8; row < live; row += 4)
+                        *reinterpret_cast<uint4 *>(out + row * P.out_row + piece * 8) = *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ row % 8) << 4));
+            }
         }
-        const int piece = lane % 8, col = c + piece * 8;
-        if (col < cols)
-            for (int row = lane / 8; row < live; row += 4)
-                *reinterpret_cast<uint4 *>(out + row * P.out_row + t.col + col) =
-                    t.steps > 0 ? *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ row % 8) << 4)) : make_uint4(0, 0, 0, 0);
+    if (t.steps > 0) {
+        fence_before();
         __syncwarp();
+        if (lane == 0) done();
     }
 }
 
 // kDown: B's rows are the contraction (matrices [in, out], and weights), else its columns.
-template <bool kWeights, bool kDown, int kCols>
+template <bool kWeights, bool kDown, int kRows, int kCols>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
-    constexpr int kStages = stages<kCols>(), kBytes = stage_bytes<kCols>();
-    constexpr uint32_t kTmem = 2 * kCols < 32 ? 32 : 2 * kCols;
+    constexpr int kStages = stages<kWeights, kRows, kCols>(), kBytes = stage_bytes<kRows, kCols>();
+    constexpr uint32_t kTmem = 2 * kCols;
     extern __shared__ uint8_t raw[];
     uint8_t *const ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint8_t *const staging = ring + kStages * kBytes;
-    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * kStageOut);
+    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * places<kWeights>() * kStageOut);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     volatile uint32_t *const failed = &S.failed;
     if (threadIdx.x == 0) {
@@ -192,16 +231,16 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if (warp == kIssueWarp) tmem_alloc<kTmem>(smem_addr(&S.tmem));
     wait_for_previous();
     let_next_start();
-    find_rows<kTileRows>(S, P);
+    find_rows<kRows>(S, P);
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = S.tmem;
     const int across = (P.wide + kCols - 1) / kCols;
-    const int tiles = kWeights ? P.experts * ((P.high + kTileRows - 1) / kTileRows) * across : S.first[P.experts] * across;
+    const int tiles = kWeights ? P.experts * ((P.high + kRows - 1) / kRows) * across : S.first[P.experts] * across;
     const int stride = static_cast<int>(gridDim.x);
     const uint32_t base = smem_addr(ring);
-    Walk<kWeights, kTileRows, kCols> walk;
+    Walk<kWeights, kRows, kCols> walk;
 
     if (warp == kLoadWarp) {
         if (lane == 0) {
@@ -212,11 +251,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 for (int k = 0; k < t.steps; ++k) {
                     bar_wait(smem_addr(&S.empty[slot]), phase ^ 1, failed);
                     if (*failed) break;
-                    const uint32_t a = base + slot * kBytes, b = a + kTileRows * 128, bar = smem_addr(&S.full[slot]);
+                    const uint32_t a = base + slot * kBytes, b = a + kRows * 128, bar = smem_addr(&S.full[slot]);
                     bar_expect(bar, kBytes);
                     if constexpr (kWeights) {
 #pragma unroll
-                        for (int x = 0; x < kTileRows; x += 64) load_box3(a + x * 128, &M.a, t.row + x, begin + k * kStep, 0, bar);
+                        for (int x = 0; x < kRows; x += 64) load_box3(a + x * 128, &M.a, t.row + x, begin + k * kStep, 0, bar);
 #pragma unroll
                         for (int x = 0; x < kCols; x += 64) load_box3(b + x * 128, &M.b, t.col + x, begin + k * kStep, 0, bar);
                     } else {
@@ -234,6 +273,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         phase ^= 1;
                     }
                 }
+            }
+            for (int i = 0, s = slot, p = phase; i < kStages && i < issued; ++i) {
+                s = s ? s - 1 : kStages - 1;
+                if (s == kStages - 1) p ^= 1;
+                bar_wait(smem_addr(&S.empty[s]), p, failed);
             }
             if (*failed)                         // copies in flight end before the block's shared memory goes away
                 for (int i = 0; i < kStages && i < issued; ++i) {
@@ -255,9 +299,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 bar_wait(smem_addr(&S.full[slot]), phase, failed);
                 __syncwarp();
                 const int left = kWeights ? t.rows - k * kStep : kStep;
-                if (left < kStep) clean_rows<(kTileRows + kCols) / 64>(ring + slot * kBytes, left, lane);
+                if (left < kStep) clean_rows<(kRows + kCols) / 64>(ring + slot * kBytes, left, lane);
                 fence_after();
-                const uint32_t a = base + slot * kBytes, b = a + kTileRows * 128;
+                const uint32_t a = base + slot * kBytes, b = a + kRows * 128;
                 const uint32_t da = kWeights ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
                 const uint32_t db = kWeights || kDown ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
 #pragma unroll
@@ -278,7 +322,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         commit(lead, smem_addr(&S.drain));
         bar_wait(smem_addr(&S.drain), 0, failed);
         if (*failed) settle(smem_addr(&S.drain), 0);
-    } else if (warp >= kWriteWarps) {
+    } else if (warp >= kFirstWriter) {
         int buffer = 0, turn = 0;
         for (int tile = blockIdx.x; tile < tiles; tile += stride) {
             const Tile t = walk.at(S, P, tile);
@@ -287,12 +331,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 __syncwarp();
                 fence_after();
             }
-            write_tile<kWeights, kCols>(S, P, t, 0, tmem + buffer * kCols, staging, [&] { bar_arrive(smem_addr(&S.written[buffer])); });
+            write_tile<kWeights, kRows, kCols>(S, P, &M.out, t, 0, tmem + buffer * kCols, staging, [&] { bar_arrive(smem_addr(&S.written[buffer])); });
             if (t.steps > 0) {
                 buffer ^= 1;
                 if (buffer == 0) turn ^= 1;
             }
         }
+        if (lane == 0) stores_done();
     }
     __syncwarp();
     fence_before();
@@ -308,9 +353,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 // the products, issued by the first, read both.  Against one SM's 128 x 256 each byte of B is copied to and read from shared
 // memory half as often.
 constexpr int kPairRows = 256, kPairCols = 256, kPairStage = 2 * kTileRows * 128;
-constexpr int kPairStages = (227 * 1024 - 1024 - kWriteWarps * kStageOut - static_cast<int>(sizeof(ProductShared))) / kPairStage;
-constexpr int kPairBytes = 1024 + kPairStages * kPairStage + kWriteWarps * kStageOut + static_cast<int>(sizeof(ProductShared));
-static_assert(kPairStages <= kMostStages && kPairBytes <= 227 * 1024, "shared memory of a block");
+template <bool kWeights> __host__ __device__ constexpr int pair_stages() { return (227 * 1024 - besides<kWeights>()) / kPairStage; }
+template <bool kWeights> constexpr int pair_bytes() { return besides<kWeights>() + pair_stages<kWeights>() * kPairStage; }
+static_assert(pair_stages<false>() == 6 && pair_stages<true>() == 5, "shared memory of a block");
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -357,10 +402,11 @@ __device__ __forceinline__ void commit_pair(uint32_t lead, uint32_t bar) {
 
 template <bool kWeights, bool kDown>
 __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
+    constexpr int kPairStages = pair_stages<kWeights>();
     extern __shared__ uint8_t raw[];
     uint8_t *const ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint8_t *const staging = ring + kPairStages * kPairStage;
-    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * kStageOut);
+    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * places<kWeights>() * kStageOut);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
     volatile uint32_t *const failed = &S.failed;
@@ -490,7 +536,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
         if (rank == 0) commit_pair(lead, smem_addr(&S.drain));
         bar_wait(smem_addr(&S.drain), 0, failed);
         if (*failed) settle(smem_addr(&S.drain), 0);
-    } else if (warp >= kWriteWarps) {
+    } else if (warp >= kFirstWriter) {
         int buffer = 0, turn = 0;
         for (int tile = begin; tile < tiles; tile += stride) {
             const Tile t = walk.at(S, P, tile);
@@ -499,13 +545,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
                 __syncwarp();
                 fence_after();
             }
-            write_tile<kWeights, kPairCols>(S, P, t, rank * kTileRows, tmem + buffer * kPairCols, staging,
+            write_tile<kWeights, kPairRows, kPairCols>(S, P, &M.out, t, rank * kTileRows, tmem + buffer * kPairCols, staging,
                                             [&] { bar_arrive_in(in_block(smem_addr(&S.written[buffer]), 0)); });
             if (t.steps > 0) {
                 buffer ^= 1;
                 if (buffer == 0) turn ^= 1;
             }
         }
+        if (lane == 0) stores_done();
     }
     __syncwarp();
     fence_before();
@@ -522,7 +569,7 @@ using ProductKernel = void (*)(const ProductParams, const ProductMaps);
 
 // Shared-memory limit of a kernel, set once per device.
 bool allow(ProductKernel fn, int which, int bytes) {
-    static std::atomic<bool> set[64][8];
+    static std::atomic<bool> set[64][20];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
         cudaGetLastError();
@@ -578,13 +625,14 @@ int check_matrices(const loco_matrices_t *t, int64_t experts, int64_t rows, int6
     return LOCO_OK;
 }
 
-template <bool kWeights, bool kDown, int kCols> int launch_product(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
+template <bool kWeights, bool kDown, int kRows, int kCols> int launch_product(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
+    static_assert(product_bytes<kWeights, kRows, kCols>() <= 227 * 1024 && stages<kWeights, kRows, kCols>() >= 4, "shared memory of a block");
     const int sms = sm_count();
     if (sms == 0) return LOCO_ERR_CUDA;
     if (tiles > 0x7fffffff - sms) return LOCO_ERR_UNSUPPORTED;
-    constexpr ProductKernel fn = product_kernel<kWeights, kDown, kCols>;
-    if (!allow(fn, which, product_bytes<kCols>())) return LOCO_ERR_CUDA;
-    return launch_kernel(fn, dim3(static_cast<unsigned>(tiles < sms ? tiles : sms)), kProductThreads, product_bytes<kCols>(), stream, P, M);
+    constexpr ProductKernel fn = product_kernel<kWeights, kDown, kRows, kCols>;
+    if (!allow(fn, which, product_bytes<kWeights, kRows, kCols>())) return LOCO_ERR_CUDA;
+    return launch_kernel(fn, dim3(static_cast<unsigned>(tiles < sms ? tiles : sms)), kProductThreads, product_bytes<kWeights, kRows, kCols>(), stream, P, M);
 }
 
 template <bool kWeights, bool kDown> int launch_pair(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
@@ -592,8 +640,8 @@ template <bool kWeights, bool kDown> int launch_pair(const ProductParams &P, con
     if (pairs == 0) return LOCO_ERR_CUDA;
     if (tiles > 0x7fffffff - pairs) return LOCO_ERR_UNSUPPORTED;
     constexpr ProductKernel fn = product_pair_kernel<kWeights, kDown>;
-    if (!allow(fn, which, kPairBytes)) return LOCO_ERR_CUDA;
-    return launch_clusters(fn, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), kProductThreads, kPairBytes, stream, 2, P, M);
+    if (!allow(fn, which, pair_bytes<kWeights>())) return LOCO_ERR_CUDA;
+    return launch_clusters(fn, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), kProductThreads, pair_bytes<kWeights>(), stream, 2, P, M);
 }
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -620,18 +668,29 @@ int loco_experts_product(const loco_product_t *c, const loco_rows_t *x, const lo
         (rc = check_matrices(w, c->experts, rows, columns, false)) != LOCO_OK) return rc;
     ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(y->ptr), 0, c->rows > 1 ? y->row_stride : 0, c->rows, c->experts, c->d_in, 0, c->d_out};
     ProductMaps M;
-    constexpr int kCols = 256;
-    const bool pair = c->rows >= 192ll * c->experts;
-    if (!make_map(M.a, x->ptr, c->d_in, c->rows, 1, x->row_stride, 0, kTileRows) ||
-        !make_map(M.b, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? (pair ? kTileRows : kCols) : kStep)) return LOCO_ERR_CUDA;
-    // every expert may end in a tile of its own
-    const int64_t ends = c->rows < c->experts ? c->rows : c->experts;
-    if (pair) {
-        const int64_t tiles = (c->rows / kPairRows + ends) * over(c->d_out, kPairCols);
-        return turned ? launch_pair<false, false>(P, M, tiles, 3, stream) : launch_pair<false, true>(P, M, tiles, 4, stream);
-    }
-    const int64_t tiles = (c->rows / kTileRows + ends) * over(c->d_out, kCols);
-    return turned ? launch_product<false, false, kCols>(P, M, tiles, 0, stream) : launch_product<false, true, kCols>(P, M, tiles, 1, stream);
+    const int sms = sm_count();
+    if (sms == 0) return LOCO_ERR_CUDA;
+    // Tiles by the rows an expert has on average: pairs of SMs where they fill 256 rows, else 32, 64 or 128 rows.  128 columns: eight
+    // rows of five experts at work, 4096 x 28672, in tiles of 64, 128, 256 columns: 201, 146, 148 us (HBM 143); 14336 x 4096: 167, 71, 83
+    // (HBM 72).  256 where that takes the SMs no more rounds.
+    const int64_t each = c->rows / c->experts, ends = c->rows < c->experts ? c->rows : c->experts;           // every expert may end in a tile of its own
+    const bool pair = each >= 192;
+    const int high = pair ? kTileRows : each < 24 ? 32 : each < 56 ? 64 : 128;
+    const auto count = [&](int w) { return (c->rows / high + ends) * over(c->d_out, w); };
+    const int wide = high == 64 && over(count(256), sms) * 2 <= over(count(128), sms) ? 256 : 128;
+    const int64_t tiles = pair ? (c->rows / kPairRows + ends) * over(c->d_out, kPairCols) : count(wide);
+    if (!make_map(M.a, x->ptr, c->d_in, c->rows, 1, x->row_stride, 0, high) ||
+        !make_map(M.b, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? (pair ? kTileRows : wide) : kStep) ||
+        !make_map(M.out, y->ptr, c->d_out, c->rows, 1, y->row_stride, 0, 32)) return LOCO_ERR_CUDA;
+    const auto go = [&](auto down) {
+        constexpr bool kDown = decltype(down)::value;
+        constexpr int kFirst = kDown ? 8 : 0;
+        if (pair) return launch_pair<false, kDown>(P, M, tiles, kFirst, stream);
+        if (high == 32) return launch_product<false, kDown, 32, 128>(P, M, tiles, kFirst + 1, stream);
+        if (high == 64) return wide == 128 ? launch_product<false, kDown, 64, 128>(P, M, tiles, kFirst + 2, stream) : launch_product<false, kDown, 64, 256>(P, M, tiles, kFirst + 3, stream);
+        return launch_product<false, kDown, 128, 128>(P, M, tiles, kFirst + 4, stream);
+    };
+    return turned ? go(std::false_type{}) : go(std::true_type{});
 }
 
 int loco_experts_product_weights(const loco_product_t *c, const loco_rows_t *a, const loco_rows_t *b, const int32_t *d_offsets, const loco_matrices_t *dw,
@@ -643,13 +702,13 @@ int loco_experts_product_weights(const loco_product_t *c, const loco_rows_t *a, 
     ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(dw->ptr), c->experts > 1 ? dw->expert_stride : 0, c->d_in > 1 ? dw->row_stride : 0, c->rows, c->experts,
                     0, c->d_in, c->d_out};
     ProductMaps M;
-    constexpr int kCols = 256;
     // without rows nothing is read: the maps need a valid address all the same
-    const bool none = c->rows == 0;
+    const bool none = c->rows == 0, pair = c->d_in > kTileRows;
     if (!make_map(M.a, none ? dw->ptr : a->ptr, c->d_in, none ? 1 : c->rows, 1, none ? 0 : a->row_stride, 0, kStep) ||
-        !make_map(M.b, none ? dw->ptr : b->ptr, c->d_out, none ? 1 : c->rows, 1, none ? 0 : b->row_stride, 0, kStep)) return LOCO_ERR_CUDA;
-    if (c->d_in >= kPairRows) return launch_pair<true, true>(P, M, c->experts * over(c->d_in, kPairRows) * over(c->d_out, kPairCols), 5, stream);
-    return launch_product<true, true, kCols>(P, M, c->experts * over(c->d_in, kTileRows) * over(c->d_out, kCols), 2, stream);
+        !make_map(M.b, none ? dw->ptr : b->ptr, c->d_out, none ? 1 : c->rows, 1, none ? 0 : b->row_stride, 0, kStep) ||
+        !make_map(M.out, dw->ptr, c->d_out, c->d_in, c->experts, dw->row_stride, dw->expert_stride, 32)) return LOCO_ERR_CUDA;
+    if (pair) return launch_pair<true, true>(P, M, c->experts * over(c->d_in, kPairRows) * over(c->d_out, kPairCols), 16, stream);
+    return launch_product<true, true, kTileRows, 128>(P, M, c->experts * over(c->d_in, kTileRows) * over(c->d_out, 128), 17, stream);
 }
 
 }  // extern "C"

@@ -86,12 +86,13 @@ def combine_gradient(dy, rows, place, weight):
 
 
 def spans(offsets, rows):
-    """(first, end) of every expert as the offsets are read: clamped to the rows."""
-    out, o = [], [int(x) for x in offsets.cpu()]
-    for a, b in zip(o[:-1], o[1:]):
-        lo = min(max(a, 0), rows)
-        out.append((lo, min(max(b, lo), rows)))
-    return out
+    """(first, end) of every expert as the offsets are read: the largest so far, within the rows."""
+    out, most = [], 0
+    for o in (int(x) for x in offsets.cpu()):
+        out.append(most)
+        most = max(most, min(max(o, 0), rows))
+        out[-1] = most
+    return list(zip(out[:-1], out[1:]))
 
 
 def product(x, w, offsets, transposed):

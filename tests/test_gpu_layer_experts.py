@@ -282,7 +282,8 @@ def offsets_of(loads, start=0):
 
 
 PRODUCTS = [([1], 8, 8), ([0], 64, 64), ([3, 0, 1], 64, 256), ([130], 72, 264), ([128, 256, 64], 128, 512), ([0, 5, 0, 700, 63, 0], 200, 328), ([2, 1, 1, 0, 2, 2, 0, 0], 512, 1032),
-            ([64] * 20, 64, 128), ([33, 129, 1, 65, 127], 1000, 776), ([1] * 100, 136, 72), ([0, 0, 0], 64, 64), ([300, 2500], 264, 512)]
+            ([64] * 20, 64, 128), ([33, 129, 1, 65, 127], 1000, 776), ([1] * 100, 136, 72), ([0, 0, 0], 64, 64), ([300, 2500], 264, 512), ([40] * 5, 328, 40000), ([40] * 5, 64, 2000), ([9, 60, 12], 200, 20000), ([1], 4096, 20000),
+            ([100, 0, 31, 200, 257], 520, 1000), ([1000], 128, 256), ([1000], 120, 512), ([513, 255], 1000, 264), ([15, 17, 16, 1, 31, 33, 49, 47], 264, 264)]
 
 
 @pytest.mark.parametrize("loads,d_in,d_out", PRODUCTS)
@@ -339,17 +340,16 @@ def test_product_of_rows_that_are_not_finite_stays_with_them():
     assert torch.equal(dw[[0, 2]], dv[[0, 2]]) and not torch.isfinite(dw[1, 7]).any() and torch.isfinite(dw[1, 1:7]).all()
 
 
-@pytest.mark.parametrize("offsets", [[0, 10, 5, 40], [-4, 10, 20, 30], [0, 20, 100, 200], [50, 60, 70, 80], [40, 40, 40, 40], [0, 0, 0, 0]])
+@pytest.mark.parametrize("offsets", [[0, 10, 5, 40], [40, 0, 40, 0], [7, 30, 2, 1 << 30], [-4, 10, 20, 30], [0, 20, 100, 200], [50, 60, 70, 80], [40, 40, 40, 40], [0, 0, 0, 0]])
 def test_product_clamps_offsets(offsets):
     g = gen(7)
     o = torch.tensor(offsets, dtype=torch.int32, device=DEV)
     x, w, b = normal(g, 40, 64), normal(g, 3, 64, 72), normal(g, 40, 72)
     y, dw = torch.full((40, 72), 7.0, dtype=BF, device=DEV), torch.empty(3, 64, 72, dtype=BF, device=DEV)
-    if all(p <= q for p, q in zip(offsets[:-1], offsets[1:])):            # else two experts write the same rows
-        layer.loco_experts_product(x, w, o, y)
-        want, terms, live = ref.product(x, w, o, False)
-        within(y[live], want[live], terms[live], 128, BF)
-        assert (y[~live] == 7.0).all()
+    layer.loco_experts_product(x, w, o, y)
+    want, terms, live = ref.product(x, w, o, False)
+    within(y[live], want[live], terms[live], 128, BF)
+    assert (y[~live] == 7.0).all()
     layer.loco_experts_product_weights(x, b, o, dw)
     want, terms = ref.product_weights(x, b, o)
     within(dw, want, terms, 82, BF)
