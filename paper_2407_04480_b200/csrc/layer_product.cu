@@ -22,12 +22,12 @@ using namespace tc;
 constexpr int kMostExperts = 512;
 constexpr int kTileRows = 128;                   // of the accumulator
 constexpr int kStep = 64;                        // of the contraction: a swizzled row of 128 bytes
-constexpr int kProductThreads = 256;
-constexpr int kLoadWarp = 0, kIssueWarp = 1, kFirstWriter = 4, kWriteWarps = 4;        // lanes of TMEM go by the warp's number modulo 4
+constexpr int kProductThreads = 384;
+constexpr int kLoadWarp = 0, kIssueWarp = 1, kCleanWarp = 2, kFirstWriter = 4, kWriteWarps = 8;        // lanes of TMEM go by the warp's number modulo 4
 
 __device__ unsigned g_product_status;            // LOCO_LAYER_FLAG_*
 
-struct ProductMaps { CUtensorMap a, b, out; };
+struct ProductMaps { CUtensorMap a, b; };
 struct ProductParams {
     const int32_t *offsets;
     __nv_bfloat16 *out;
@@ -41,38 +41,22 @@ struct ProductShared {
     uint32_t tmem, failed;
     int32_t begin[kMostExperts], count[kMostExperts], first[kMostExperts + 1];      // rows of an expert, its tiles before
 };
-constexpr int kStageOut = 32 * 128;              // bytes a writing warp puts 32 rows of 64 columns in
-// Such places of a writing warp: over few rows the matrices' gradient is all writing, and one place is filled while another's is
-// copied out; elsewhere the tiles' contraction covers it, and the memory is better as a stage.
-template <bool kWeights> __host__ __device__ constexpr int places() { return kWeights ? 2 : 1; }
-// Shared memory besides the stages, and up to 1 KB to a boundary.
-template <bool kWeights> __host__ __device__ constexpr int besides() {
-    return 1024 + kWriteWarps * places<kWeights>() * kStageOut + static_cast<int>(sizeof(ProductShared));
-}
+constexpr int kPiece = 32;                       // columns that a writing warp puts to shared memory at a time
+constexpr int kPieceBytes = 32 * kPiece * 2;     // of its 32 rows
+constexpr int kBesides = 1024 + kWriteWarps * kPieceBytes + static_cast<int>(sizeof(ProductShared));     // of shared memory besides the stages
 // kRows of A are copied, of the 128 that the product reads: what it reads past them (B, other stages) is in accumulator rows
 // that are not written.
 template <int kRows, int kCols> __host__ __device__ constexpr int stage_bytes() { return (kRows + kCols) * 128; }
-template <bool kWeights, int kRows, int kCols> __host__ __device__ constexpr int stages() {
-    constexpr int n = (227 * 1024 - besides<kWeights>()) / stage_bytes<kRows, kCols>();
+template <int kRows, int kCols> __host__ __device__ constexpr int stages() {
+    constexpr int n = (227 * 1024 - kBesides) / stage_bytes<kRows, kCols>();
     return n < kMostStages ? n : kMostStages;
 }
-template <bool kWeights, int kRows, int kCols> constexpr int product_bytes() {
-    return besides<kWeights>() + stages<kWeights, kRows, kCols>() * stage_bytes<kRows, kCols>();
-}
+template <int kRows, int kCols> constexpr int product_bytes() { return kBesides + stages<kRows, kCols>() * stage_bytes<kRows, kCols>(); }
 
 __device__ __forceinline__ void load_box3(uint32_t to, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-
-// 32 rows of 64 columns from a writing warp's part of shared memory; nothing is written past the tensor.
-__device__ __forceinline__ void store_box3(const CUtensorMap *map, uint32_t from, int x, int y, int z) {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];\n cp.async.bulk.commit_group;"
-                 ::"l"(map), "r"(from), "r"(x), "r"(y), "r"(z) : "memory");
-}
-// All but the last kLeft such copies have read what they copy.
-template <int kLeft> __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
-__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // Where the tiles are.  `walk` goes on to the tile's expert; tiles only grow.
 struct Tile {
@@ -147,71 +131,66 @@ __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
     while (!bar_test(bar, parity) && now_ns() - begin < kWaitLimitNs / 20) {}
 }
 
-// A writing warp's 32 rows of a tile's accumulator, `below` rows into the tile: through shared memory and out with copies of 64
-// columns, or row by row where the expert ends among them.  `done` is called by one lane when
-// the accumulator has been read.  Zeros for a tile without a contraction.
+// A writing warp's part of a tile's accumulator: 32 rows of half the columns, `below` rows into the tile, through shared memory so
+// that a store covers 64 bytes of a row.  (With copies of 64 columns by the copy engine instead of stores the gradient of 64
+// matrices of 2048 x 1032 over 47 rows each took 102 us, 50634 rows of 256 through 3328 columns 171.)  `done` is called by one lane
+// when the accumulator has been read.  Zeros for a tile without a contraction.
 template <bool kWeights, int kRows, int kCols, typename Done>
-__device__ __forceinline__ void write_tile(const ProductShared &S, const ProductParams &P, const CUtensorMap *map, const Tile &t, int below, uint32_t accumulator,
-                                           uint8_t *staging, const Done &done) {
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32 - kFirstWriter, part = warp % 4, first = t.row + below + part * 32;
-    const int live = min(min((kWeights ? P.high : t.rows), t.row + kRows) - first, 32), until = min(kCols, P.wide - t.col);
-    if (live > 0)
-        for (int c = 0; c < until; c += 64) {
-            uint8_t *const stage = staging + (warp * places<kWeights>() + c / 64 % places<kWeights>()) * kStageOut;
-            uint4 w[8];
-            if (t.steps > 0) {
-                uint32_t r[2][32];
-                const uint32_t at = accumulator + c + (static_cast<uint32_t>(part * 32) << 16);
-                load_columns(at, r[0]);
-                load_columns(at + 32, r[1]);
-                wait_loads();
-                pin(r[0]);
-                pin(r[1]);
-#pragma unroll
-                for (int i = 0; i < 64; i += 8) {
-                    const uint32_t *f = &r[i / 32][i % 32];
-                    w[i / 8].x = pack_bf16(__uint_as_float(f[0]), __uint_as_float(f[1]));
-                    w[i / 8].y = pack_bf16(__uint_as_float(f[2]), __uint_as_float(f[3]));
-                    w[i / 8].z = pack_bf16(__uint_as_float(f[4]), __uint_as_float(f[5]));
-                    w[i / 8].w = pack_bf16(__uint_as_float(f[6]), __uint_as_float(f[7]));
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = make_uint4(0, 0, 0, 0);
-            }
-            if (lane == 0) stores_read<places<kWeights>() - 1>();    // the place is free
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ lane % 8) << 4)) = w[i];
-            if (kWeights || live == 32) {
-                fence_async_shared();
-                __syncwarp();
-                if (lane == 0) store_box3(map, smem_addr(stage), t.col + c, (kWeights ? 0 : S.begin[t.expert]) + first, kWeights ? t.expert : 0);
-            } else {
-                __syncwarp();
-                __nv_bfloat16 *const out = P.out + (static_cast<int64_t>(S.begin[t.expert]) + first) * P.out_row + t.col + c;
-                const int piece = lane % 8;
-                if (t.col + c + piece * 8 < P.wide)
-                    for (int row = lane / 8; row < live; row += 4)
-                        *reinterpret_cast<uint4 *>(out + row * P.out_row + piece * 8) = *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ row % 8) << 4));
-            }
-        }
-    if (t.steps > 0) {
+__device__ __forceinline__ void write_tile(const ProductShared &S, const ProductParams &P, const Tile &t, int below, uint32_t accumulator, uint8_t *staging,
+                                           const Done &done) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32 - kFirstWriter, part = warp % 4, half = warp / 4 * (kCols / 2), first = t.row + below + part * 32;
+    uint8_t *const stage = staging + warp * kPieceBytes;
+    const int live = min(min((kWeights ? P.high : t.rows), t.row + kRows) - first, 32), cols = P.wide - t.col - half;       // that are written
+    __nv_bfloat16 *const out = P.out + (kWeights ? t.expert * P.out_expert : S.begin[t.expert] * P.out_row) + first * P.out_row + t.col + half;
+    const int piece = lane % 4, end = live > 0 ? min(kCols / 2, cols) : 0;
+    const auto read = [&] {                      // ahead of the last stores, which the arrival need not wait for
         fence_before();
         __syncwarp();
         if (lane == 0) done();
+    };
+    if (t.steps > 0 && end <= 0) read();
+#pragma unroll 1
+    for (int c = 0; c < end; c += kPiece) {
+        uint32_t r[32];
+        if (t.steps > 0) {
+            load_columns(accumulator + half + c + (static_cast<uint32_t>(part * 32) << 16), r);
+            wait_loads();
+            pin(r);
+            if (c + kPiece >= end) read();
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kPiece; i += 8) {
+            uint4 w;
+            w.x = pack_bf16(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+            w.y = pack_bf16(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+            w.z = pack_bf16(__uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
+            w.w = pack_bf16(__uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
+            *reinterpret_cast<uint4 *>(stage + lane * 64 + ((i / 8 ^ lane / 2 % 4) << 4)) = w;
+        }
+        __syncwarp();
+        if (c + piece * 8 < cols)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = lane / 4 + i * 8;
+                if (row < live)
+                    *reinterpret_cast<uint4 *>(out + row * P.out_row + c + piece * 8) = *reinterpret_cast<const uint4 *>(stage + row * 64 + ((piece ^ row / 2 % 4) << 4));
+            }
+        __syncwarp();
     }
 }
 
 // kDown: B's rows are the contraction (matrices [in, out], and weights), else its columns.
 template <bool kWeights, bool kDown, int kRows, int kCols>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
-    constexpr int kStages = stages<kWeights, kRows, kCols>(), kBytes = stage_bytes<kRows, kCols>();
+    constexpr int kStages = stages<kRows, kCols>(), kBytes = stage_bytes<kRows, kCols>();
     constexpr uint32_t kTmem = 2 * kCols;
     extern __shared__ uint8_t raw[];
-    uint8_t *const ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint8_t *const ring = raw + (1024 - smem_addr(raw) % 1024) % 1024;      // not by an integer, past which nobody knows that it is shared memory
     uint8_t *const staging = ring + kStages * kBytes;
-    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * places<kWeights>() * kStageOut);
+    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * kPieceBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     volatile uint32_t *const failed = &S.failed;
     if (threadIdx.x == 0) {
@@ -331,13 +310,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 __syncwarp();
                 fence_after();
             }
-            write_tile<kWeights, kRows, kCols>(S, P, &M.out, t, 0, tmem + buffer * kCols, staging, [&] { bar_arrive(smem_addr(&S.written[buffer])); });
+            write_tile<kWeights, kRows, kCols>(S, P, t, 0, tmem + buffer * kCols, staging, [&] { bar_arrive(smem_addr(&S.written[buffer])); });
             if (t.steps > 0) {
                 buffer ^= 1;
                 if (buffer == 0) turn ^= 1;
             }
         }
-        if (lane == 0) stores_done();
     }
     __syncwarp();
     fence_before();
@@ -353,9 +331,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 // the products, issued by the first, read both.  Against one SM's 128 x 256 each byte of B is copied to and read from shared
 // memory half as often.
 constexpr int kPairRows = 256, kPairCols = 256, kPairStage = 2 * kTileRows * 128;
-template <bool kWeights> __host__ __device__ constexpr int pair_stages() { return (227 * 1024 - besides<kWeights>()) / kPairStage; }
-template <bool kWeights> constexpr int pair_bytes() { return besides<kWeights>() + pair_stages<kWeights>() * kPairStage; }
-static_assert(pair_stages<false>() == 6 && pair_stages<true>() == 5, "shared memory of a block");
+constexpr int kPairStages = (227 * 1024 - kBesides) / kPairStage;
+constexpr int kPairBytes = kBesides + kPairStages * kPairStage;
+static_assert(kPairStages == 6, "shared memory of a block");
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -371,11 +349,22 @@ __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void bar_arrive_in(uint32_t bar) {        // in any block of the cluster
+// In any block of the cluster, with what this thread wrote before...
+__device__ __forceinline__ void bar_arrive_in(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// What a block of the cluster has arrived with is visible after this; the wait before has passed or given up.
-__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+// ... or without: a release to the cluster waits for the thread's stores to global memory (2600 tiles of 256 steps: 120 us with it).
+__device__ __forceinline__ void bar_arrive_in_relaxed(uint32_t bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// Once more, for what another block of the cluster did before it arrived.
+__device__ __forceinline__ bool bar_test_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
 // A box to this block's shared memory; completes on a barrier of either block.
 __device__ __forceinline__ void load_box3_pair(uint32_t to, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -402,11 +391,10 @@ __device__ __forceinline__ void commit_pair(uint32_t lead, uint32_t bar) {
 
 template <bool kWeights, bool kDown>
 __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
-    constexpr int kPairStages = pair_stages<kWeights>();
     extern __shared__ uint8_t raw[];
-    uint8_t *const ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint8_t *const ring = raw + (1024 - smem_addr(raw) % 1024) % 1024;      // not by an integer, past which nobody knows that it is shared memory
     uint8_t *const staging = ring + kPairStages * kPairStage;
-    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * places<kWeights>() * kStageOut);
+    ProductShared &S = *reinterpret_cast<ProductShared *>(staging + kWriteWarps * kPieceBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
     volatile uint32_t *const failed = &S.failed;
@@ -414,7 +402,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
         for (int i = 0; i < kPairStages; ++i) {
             bar_init(smem_addr(&S.full[i]), 1);                      // the first block's: both blocks' copies, but for one with rows past
             bar_init(smem_addr(&S.empty[i]), 1);                     // an expert's end in it; the second's: such a copy of its own
-            bar_init(smem_addr(&S.clean[i]), 1);                     // the first block's: those rows are zero in the second
+            bar_init(smem_addr(&S.clean[i]), 2);                     // the first block's: those rows are zero in both
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_addr(&S.ready[i]), 1);
@@ -489,53 +477,65 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
         const uint32_t lead = elect_lane();
         constexpr uint32_t word = (product(kPairCols, kDown || kWeights) & 0x00ffffffu) | (16u << 24) | (kWeights ? 1u << 15 : 0u);      // 256 rows
         int slot = 0, phase = 0, buffer = 0, turn = 0;
-        uint32_t ends = 0;                       // by slot: the phase of its next tile with rows past an end (rank 0: of `clean`, rank 1: of `full`)
-        for (int tile = begin; tile < tiles; tile += stride) {
+        uint32_t ends = 0;                       // by slot: the phase of `clean`
+        for (int tile = begin; tile < tiles && rank == 0; tile += stride) {
             const Tile t = walk.at(S, P, tile);
             if (t.steps == 0) continue;
-            if (rank == 0) {
-                bar_wait(smem_addr(&S.written[buffer]), turn ^ 1, failed);
-                fence_after();
-            }
+            bar_wait(smem_addr(&S.written[buffer]), turn ^ 1, failed);
             for (int k = 0; k < t.steps; ++k) {
                 const int left = kWeights ? t.rows - k * kStep : kStep;
-                if (rank == 0) {
-                    bar_wait(smem_addr(&S.full[slot]), phase, failed);
-                    __syncwarp();
-                    if (left < kStep) {
-                        clean_rows<2 * kTileRows / 64>(ring + slot * kPairStage, left, lane);
-                        bar_wait(smem_addr(&S.clean[slot]), ends >> slot & 1, failed);
-                        fence_cluster();
-                    }
-                    fence_after();
-                    const uint32_t a = base + slot * kPairStage, b = a + kTileRows * 128;
-                    const uint32_t da = kWeights ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
-                    const uint32_t db = kWeights || kDown ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
-#pragma unroll
-                    for (int x = 0; x < kStep; x += 16)
-                        if (!kWeights || x < left)
-                            mma_pair(lead, tmem + buffer * kPairCols, da + (kWeights ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights || kDown ? x * 128 >> 4 : x * 2 >> 4),
-                                     word, k > 0 || x > 0);
-                    commit_pair(lead, smem_addr(&S.empty[slot]));
-                } else if (left < kStep) {
-                    bar_wait(smem_addr(&S.full[slot]), ends >> slot & 1, failed);
-                    __syncwarp();
-                    clean_rows<2 * kTileRows / 64>(ring + slot * kPairStage, left, lane);
-                    if (lane == 0) bar_arrive_in(in_block(smem_addr(&S.clean[slot]), 0));
+                bar_wait(smem_addr(&S.full[slot]), phase, failed);
+                if (left < kStep) {
+                    bar_wait(smem_addr(&S.clean[slot]), ends >> slot & 1, failed);
+                    bar_test_cluster(smem_addr(&S.clean[slot]), ends >> slot & 1);     // what the other block did before it arrived is seen
+                    ends ^= 1u << slot;
                 }
-                if (left < kStep) ends ^= 1u << slot;
+                __syncwarp();
+                fence_after();
+                const uint32_t a = base + slot * kPairStage, b = a + kTileRows * 128;
+                const uint32_t da = kWeights ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
+                const uint32_t db = kWeights || kDown ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
+#pragma unroll
+                for (int x = 0; x < kStep; x += 16)
+                    if (!kWeights || x < left)
+                        mma_pair(lead, tmem + buffer * kPairCols, da + (kWeights ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights || kDown ? x * 128 >> 4 : x * 2 >> 4),
+                                 word, k > 0 || x > 0);
+                commit_pair(lead, smem_addr(&S.empty[slot]));
                 if (++slot == kPairStages) {
                     slot = 0;
                     phase ^= 1;
                 }
             }
-            if (rank == 0) commit_pair(lead, smem_addr(&S.ready[buffer]));
+            commit_pair(lead, smem_addr(&S.ready[buffer]));
             buffer ^= 1;
             if (buffer == 0) turn ^= 1;
         }
         if (rank == 0) commit_pair(lead, smem_addr(&S.drain));
         bar_wait(smem_addr(&S.drain), 0, failed);
         if (*failed) settle(smem_addr(&S.drain), 0);
+    } else if (warp == kCleanWarp && kWeights) {
+        // Zeros in the rows past an expert's last, in this block's part of the step that holds them.  The first block's copies are waited
+        // for one after the other (a phase told by its parity has to be the current one or the last); the second's `full` has
+        // such steps' phases alone.
+        int slot = 0, phase = 0;
+        uint32_t ends = 0;                       // by slot: the phase of the second block's `full`
+        for (int tile = begin; tile < tiles; tile += stride) {
+            const Tile t = walk.at(S, P, tile);
+            for (int k = 0; k < t.steps; ++k) {
+                const int left = t.rows - k * kStep;
+                if (rank == 0 || left < kStep) bar_wait(smem_addr(&S.full[slot]), rank == 0 ? phase : ends >> slot & 1, failed);
+                if (left < kStep) {
+                    ends ^= 1u << slot;
+                    __syncwarp();
+                    clean_rows<2 * kTileRows / 64>(ring + slot * kPairStage, left, lane);
+                    if (lane == 0) bar_arrive_in(in_block(smem_addr(&S.clean[slot]), 0));
+                }
+                if (++slot == kPairStages) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+            }
+        }
     } else if (warp >= kFirstWriter) {
         int buffer = 0, turn = 0;
         for (int tile = begin; tile < tiles; tile += stride) {
@@ -545,14 +545,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
                 __syncwarp();
                 fence_after();
             }
-            write_tile<kWeights, kPairRows, kPairCols>(S, P, &M.out, t, rank * kTileRows, tmem + buffer * kPairCols, staging,
-                                            [&] { bar_arrive_in(in_block(smem_addr(&S.written[buffer]), 0)); });
+            write_tile<kWeights, kPairRows, kPairCols>(S, P, t, rank * kTileRows, tmem + buffer * kPairCols, staging,
+                                            [&] { bar_arrive_in_relaxed(in_block(smem_addr(&S.written[buffer]), 0)); });
             if (t.steps > 0) {
                 buffer ^= 1;
                 if (buffer == 0) turn ^= 1;
             }
         }
-        if (lane == 0) stores_done();
     }
     __syncwarp();
     fence_before();
@@ -626,13 +625,13 @@ int check_matrices(const loco_matrices_t *t, int64_t experts, int64_t rows, int6
 }
 
 template <bool kWeights, bool kDown, int kRows, int kCols> int launch_product(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
-    static_assert(product_bytes<kWeights, kRows, kCols>() <= 227 * 1024 && stages<kWeights, kRows, kCols>() >= 4, "shared memory of a block");
+    static_assert(product_bytes<kRows, kCols>() <= 227 * 1024 && stages<kRows, kCols>() >= 4, "shared memory of a block");
     const int sms = sm_count();
     if (sms == 0) return LOCO_ERR_CUDA;
     if (tiles > 0x7fffffff - sms) return LOCO_ERR_UNSUPPORTED;
     constexpr ProductKernel fn = product_kernel<kWeights, kDown, kRows, kCols>;
-    if (!allow(fn, which, product_bytes<kWeights, kRows, kCols>())) return LOCO_ERR_CUDA;
-    return launch_kernel(fn, dim3(static_cast<unsigned>(tiles < sms ? tiles : sms)), kProductThreads, product_bytes<kWeights, kRows, kCols>(), stream, P, M);
+    if (!allow(fn, which, product_bytes<kRows, kCols>())) return LOCO_ERR_CUDA;
+    return launch_kernel(fn, dim3(static_cast<unsigned>(tiles < sms ? tiles : sms)), kProductThreads, product_bytes<kRows, kCols>(), stream, P, M);
 }
 
 template <bool kWeights, bool kDown> int launch_pair(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
@@ -640,8 +639,8 @@ template <bool kWeights, bool kDown> int launch_pair(const ProductParams &P, con
     if (pairs == 0) return LOCO_ERR_CUDA;
     if (tiles > 0x7fffffff - pairs) return LOCO_ERR_UNSUPPORTED;
     constexpr ProductKernel fn = product_pair_kernel<kWeights, kDown>;
-    if (!allow(fn, which, pair_bytes<kWeights>())) return LOCO_ERR_CUDA;
-    return launch_clusters(fn, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), kProductThreads, pair_bytes<kWeights>(), stream, 2, P, M);
+    if (!allow(fn, which, kPairBytes)) return LOCO_ERR_CUDA;
+    return launch_clusters(fn, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), kProductThreads, kPairBytes, stream, 2, P, M);
 }
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -674,14 +673,13 @@ int loco_experts_product(const loco_product_t *c, const loco_rows_t *x, const lo
     // rows of five experts at work, 4096 x 28672, in tiles of 64, 128, 256 columns: 201, 146, 148 us (HBM 143); 14336 x 4096: 167, 71, 83
     // (HBM 72).  256 where that takes the SMs no more rounds.
     const int64_t each = c->rows / c->experts, ends = c->rows < c->experts ? c->rows : c->experts;           // every expert may end in a tile of its own
-    const bool pair = each >= 192;
+    const bool pair = each >= 160;
     const int high = pair ? kTileRows : each < 24 ? 32 : each < 56 ? 64 : 128;
     const auto count = [&](int w) { return (c->rows / high + ends) * over(c->d_out, w); };
     const int wide = high == 64 && over(count(256), sms) * 2 <= over(count(128), sms) ? 256 : 128;
     const int64_t tiles = pair ? (c->rows / kPairRows + ends) * over(c->d_out, kPairCols) : count(wide);
     if (!make_map(M.a, x->ptr, c->d_in, c->rows, 1, x->row_stride, 0, high) ||
-        !make_map(M.b, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? (pair ? kTileRows : wide) : kStep) ||
-        !make_map(M.out, y->ptr, c->d_out, c->rows, 1, y->row_stride, 0, 32)) return LOCO_ERR_CUDA;
+        !make_map(M.b, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? (pair ? kTileRows : wide) : kStep)) return LOCO_ERR_CUDA;
     const auto go = [&](auto down) {
         constexpr bool kDown = decltype(down)::value;
         constexpr int kFirst = kDown ? 8 : 0;
@@ -705,8 +703,7 @@ int loco_experts_product_weights(const loco_product_t *c, const loco_rows_t *a, 
     // without rows nothing is read: the maps need a valid address all the same
     const bool none = c->rows == 0, pair = c->d_in > kTileRows;
     if (!make_map(M.a, none ? dw->ptr : a->ptr, c->d_in, none ? 1 : c->rows, 1, none ? 0 : a->row_stride, 0, kStep) ||
-        !make_map(M.b, none ? dw->ptr : b->ptr, c->d_out, none ? 1 : c->rows, 1, none ? 0 : b->row_stride, 0, kStep) ||
-        !make_map(M.out, dw->ptr, c->d_out, c->d_in, c->experts, dw->row_stride, dw->expert_stride, 32)) return LOCO_ERR_CUDA;
+        !make_map(M.b, none ? dw->ptr : b->ptr, c->d_out, none ? 1 : c->rows, 1, none ? 0 : b->row_stride, 0, kStep)) return LOCO_ERR_CUDA;
     if (pair) return launch_pair<true, true>(P, M, c->experts * over(c->d_in, kPairRows) * over(c->d_out, kPairCols), 16, stream);
     return launch_product<true, true, kTileRows, 128>(P, M, c->experts * over(c->d_in, kTileRows) * over(c->d_out, 128), 17, stream);
 }
