@@ -1,11 +1,13 @@
 // The products of every expert's rows with its matrix, and the gradient of the matrices, on the tensor cores.
 //
-// One block to an SM takes tiles of 128 x kCols outputs, one after the other, expert by expert; where an expert's rows begin is
-// known on the device only.  One warp copies 64 of the contraction at a time to a ring in shared memory (TMA, 128-byte
-// swizzle), one issues the products, four write the accumulator out while the next tile's products run into the other half of
-// TMEM.
-//   product   A is 128 rows of x, B is of the expert's matrix, either way round.  Rows of a tile past the expert's last belong to
-//             the next expert (or are the copy's zero fill): what they give is in accumulator rows that are not written.
+// One block to an SM, or two that work together, take tiles of outputs one after the other, expert by expert; where an expert's
+// rows begin is known on the device only.  One warp copies 64 of the contraction at a time to a ring in shared memory (TMA,
+// 128-byte swizzle), one issues the products, eight write the accumulator out while the next tile's products run into the other
+// half of TMEM.
+//   product   A, the 128 lanes of the accumulator, are columns of the expert's matrix, either way round, and B, its columns, are rows
+//             of x: as many as the expert has left, rounded up to 16 (two blocks: 32), so that no product is spent on an
+//             expert's ragged end.  Rows past it belong to the next expert (or are the copy's zero fill): what they give is in
+//             accumulator columns that are not written.
 //   weights   A and B are rows of a and b, contracted along the rows.  Rows past the expert's last are zeroed in shared memory
 //             in both, so that whatever lies there (NaN included) adds nothing.
 #include <cuda.h>
@@ -33,25 +35,26 @@ struct ProductParams {
     __nv_bfloat16 *out;
     int64_t out_expert, out_row, rows;
     int32_t experts, deep, high, wide;           // contraction (product), rows of an output matrix (weights), columns of the output
+    int32_t last;                                // experts' last tiles of rows, where they are not full, come after all full ones
 };
 
 constexpr int kMostStages = 12;
 struct ProductShared {
     uint64_t full[kMostStages], empty[kMostStages], clean[kMostStages], ready[2], written[2], drain;
     uint32_t tmem, failed;
-    int32_t begin[kMostExperts], count[kMostExperts], first[kMostExperts + 1];      // rows of an expert, its tiles before
+    int32_t begin[kMostExperts], count[kMostExperts];                // rows of an expert
+    int32_t first[kMostExperts + 1], ends[kMostExperts + 1];         // tiles of rows, and tiles that come last, before it
 };
 constexpr int kPiece = 32;                       // columns that a writing warp puts to shared memory at a time
 constexpr int kPieceBytes = 32 * kPiece * 2;     // of its 32 rows
 constexpr int kBesides = 1024 + kWriteWarps * kPieceBytes + static_cast<int>(sizeof(ProductShared));     // of shared memory besides the stages
-// kRows of A are copied, of the 128 that the product reads: what it reads past them (B, other stages) is in accumulator rows
-// that are not written.
-template <int kRows, int kCols> __host__ __device__ constexpr int stage_bytes() { return (kRows + kCols) * 128; }
-template <int kRows, int kCols> __host__ __device__ constexpr int stages() {
-    constexpr int n = (227 * 1024 - kBesides) / stage_bytes<kRows, kCols>();
+// 128 of A and kN of B to a stage of one block.
+template <int kN> __host__ __device__ constexpr int stage_bytes() { return (kTileRows + kN) * 128; }
+template <int kN> __host__ __device__ constexpr int stages() {
+    constexpr int n = (227 * 1024 - kBesides) / stage_bytes<kN>();
     return n < kMostStages ? n : kMostStages;
 }
-template <int kRows, int kCols> constexpr int product_bytes() { return kBesides + stages<kRows, kCols>() * stage_bytes<kRows, kCols>(); }
+template <int kN> constexpr int product_bytes() { return kBesides + stages<kN>() * stage_bytes<kN>(); }
 
 __device__ __forceinline__ void load_box3(uint32_t to, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -64,19 +67,32 @@ struct Tile {
 };
 template <bool kWeights, int kRows, int kCols> struct Walk {
     int expert = 0;
+    bool ends = false;
+    __device__ __forceinline__ static int across(const ProductParams &P) { return (P.wide + kCols - 1) / kCols; }
+    __device__ __forceinline__ static int tiles(const ProductShared &S, const ProductParams &P) {
+        return (kWeights ? P.experts * ((P.high + kRows - 1) / kRows) : S.first[P.experts] + S.ends[P.experts]) * across(P);
+    }
     __device__ __forceinline__ Tile at(const ProductShared &S, const ProductParams &P, int tile) {
-        const int across = (P.wide + kCols - 1) / kCols;
+        const int wide = across(P);
         if constexpr (kWeights) {
-            const int down = (P.high + kRows - 1) / kRows, each = down * across;
+            const int down = (P.high + kRows - 1) / kRows, each = down * wide;
             expert = tile / each;
             const int r = tile - expert * each, n = S.count[expert];
             return Tile{expert, r % down * kRows, r / down * kCols, n, (n + kStep - 1) / kStep};
         } else {
-            while (tile >= S.first[expert + 1] * across) ++expert;
-            const int down = S.first[expert + 1] - S.first[expert], r = tile - S.first[expert] * across;
-            // bands of eight tiles of rows, column by column, so that the blocks at work share rows and columns in L2
-            const int band = r / (8 * across), high = min(8, down - band * 8), q = r - band * 8 * across;
-            return Tile{expert, (band * 8 + q % high) * kRows, q / high * kCols, S.count[expert], (P.deep + kStep - 1) / kStep};
+            const int steps = (P.deep + kStep - 1) / kStep, full = S.first[P.experts] * wide;
+            if (tile < full) {
+                while (tile >= S.first[expert + 1] * wide) ++expert;
+                const int down = S.first[expert + 1] - S.first[expert], r = tile - S.first[expert] * wide;
+                // bands of eight tiles of rows, column by column, so that the blocks at work share rows and columns in L2
+                const int band = r / (8 * wide), high = min(8, down - band * 8), q = r - band * 8 * wide;
+                return Tile{expert, (band * 8 + q % high) * kRows, q / high * kCols, S.count[expert], steps};
+            }
+            if (!ends) expert = 0;
+            ends = true;
+            const int r = tile - full, end = r / wide;
+            while (end >= S.ends[expert + 1]) ++expert;
+            return Tile{expert, S.count[expert] / kRows * kRows, (r - end * wide) * kCols, S.count[expert], steps};
         }
     }
 };
@@ -99,7 +115,7 @@ template <int kRows> __device__ __forceinline__ void find_rows(ProductShared &S,
         const int64_t o = P.offsets[e < P.experts ? e : P.experts];
         return static_cast<int>(o < 0 ? 0 : o > P.rows ? P.rows : o);
     };
-    int most = 0, before = 0;                    // of the offsets and of the tiles of the experts before
+    int most = 0, before = 0, ended = 0;         // of the offsets, the tiles and the last tiles of the experts before
     for (int e0 = 0; e0 < P.experts; e0 += 32) {
         const int e = e0 + lane;
         int lo = max(offset(e), most);
@@ -108,22 +124,27 @@ template <int kRows> __device__ __forceinline__ void find_rows(ProductShared &S,
             const int y = __shfl_up_sync(0xffffffffu, lo, o);
             lo = lane >= o ? max(lo, y) : lo;
         }
-        const int hi = max(offset(e + 1), lo);
-        int n = e < P.experts ? (hi - lo + kRows - 1) / kRows : 0;
+        const int hi = max(offset(e + 1), lo), rows = e < P.experts ? hi - lo : 0;
+        int n = P.last ? rows / kRows : (rows + kRows - 1) / kRows;
+        const unsigned ends = __ballot_sync(0xffffffffu, P.last && rows % kRows != 0);
         if (e < P.experts) {
             S.begin[e] = lo;
-            S.count[e] = hi - lo;
+            S.count[e] = rows;
         }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, n, o);
             n += lane >= o ? y : 0;
         }
-        if (e < P.experts) S.first[e + 1] = before + n;
+        if (e < P.experts) {
+            S.first[e + 1] = before + n;
+            S.ends[e + 1] = ended + __popc(ends & (0xffffffffu >> (31 - lane)));
+        }
         before += __shfl_sync(0xffffffffu, n, 31);
+        ended += __popc(ends);
         most = __shfl_sync(0xffffffffu, hi, 31);
     }
-    if (lane == 0) S.first[0] = 0;
+    if (lane == 0) S.first[0] = S.ends[0] = 0;
 }
 
 __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
@@ -131,17 +152,17 @@ __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
     while (!bar_test(bar, parity) && now_ns() - begin < kWaitLimitNs / 20) {}
 }
 
-// A writing warp's part of a tile's accumulator: 32 rows of half the columns, `below` rows into the tile, through shared memory so
+// A writing warp's part of the accumulator of a tile of dw: 32 rows of half the columns, `below` rows into the tile, through shared memory so
 // that a store covers 64 bytes of a row.  (With copies of 64 columns by the copy engine instead of stores the gradient of 64
 // matrices of 2048 x 1032 over 47 rows each took 102 us, 50634 rows of 256 through 3328 columns 171.)  `done` is called by one lane
 // when the accumulator has been read.  Zeros for a tile without a contraction.
-template <bool kWeights, int kRows, int kCols, typename Done>
+template <int kRows, int kCols, typename Done>
 __device__ __forceinline__ void write_tile(const ProductShared &S, const ProductParams &P, const Tile &t, int below, uint32_t accumulator, uint8_t *staging,
                                            const Done &done) {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32 - kFirstWriter, part = warp % 4, half = warp / 4 * (kCols / 2), first = t.row + below + part * 32;
     uint8_t *const stage = staging + warp * kPieceBytes;
-    const int live = min(min((kWeights ? P.high : t.rows), t.row + kRows) - first, 32), cols = P.wide - t.col - half;       // that are written
-    __nv_bfloat16 *const out = P.out + (kWeights ? t.expert * P.out_expert : S.begin[t.expert] * P.out_row) + first * P.out_row + t.col + half;
+    const int live = min(min(P.high, t.row + kRows) - first, 32), cols = P.wide - t.col - half;       // that are written
+    __nv_bfloat16 *const out = P.out + t.expert * P.out_expert + first * P.out_row + t.col + half;
     const int piece = lane % 4, end = live > 0 ? min(kCols / 2, cols) : 0;
     const auto read = [&] {                      // ahead of the last stores, which the arrival need not wait for
         fence_before();
@@ -182,11 +203,55 @@ __device__ __forceinline__ void write_tile(const ProductShared &S, const Product
     }
 }
 
-// kDown: B's rows are the contraction (matrices [in, out], and weights), else its columns.
-template <bool kWeights, bool kDown, int kRows, int kCols>
+// The same of a product's tile: the warp's 32 lanes are columns of the output from `col` on, the accumulator's columns its rows.
+// The two halves of the writing warps take 32 rows in turn.
+template <int kN, typename Done>
+__device__ __forceinline__ void write_rows(const ProductShared &S, const ProductParams &P, const Tile &t, int col, uint32_t accumulator, uint8_t *staging,
+                                           const Done &done) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32 - kFirstWriter, part = warp % 4, first = warp / 4 * 32;
+    uint8_t *const stage = staging + warp * kPieceBytes;
+    col += part * 32;
+    const int piece = lane % 4, end = col < P.wide ? min(t.rows - t.row, kN) : 0;
+    __nv_bfloat16 *const out = P.out + (S.begin[t.expert] + static_cast<int64_t>(t.row)) * P.out_row + col + piece * 8;
+    const auto read = [&] {
+        fence_before();
+        __syncwarp();
+        if (lane == 0) done();
+    };
+    if (first >= end) read();
+#pragma unroll 1
+    for (int j = first; j < end; j += 64) {
+        uint32_t r[32];
+        load_columns(accumulator + j + (static_cast<uint32_t>(part * 32) << 16), r);
+        wait_loads();
+        pin(r);
+        if (j + 64 >= end) read();
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            const uint32_t w = pack_bf16(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+            *reinterpret_cast<uint16_t *>(stage + i * 64 + lane * 2) = static_cast<uint16_t>(w);
+            *reinterpret_cast<uint16_t *>(stage + i * 64 + 64 + lane * 2) = static_cast<uint16_t>(w >> 16);
+        }
+        __syncwarp();
+        if (col + piece * 8 < P.wide)
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+                const int row = lane / 4 + i;
+                if (j + row < end) *reinterpret_cast<uint4 *>(out + (j + row) * P.out_row) = *reinterpret_cast<const uint4 *>(stage + row * 64 + piece * 16);
+            }
+        __syncwarp();
+    }
+}
+
+// An instruction word's part for n columns of the accumulator.
+__device__ __forceinline__ uint32_t columns_word(int n) { return static_cast<uint32_t>(n >> 3) << 17; }
+
+// kDown: the matrices are [in, out], their rows are the contraction (and in weights a's and b's); else [out, in].
+template <bool kWeights, bool kDown, int kN>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
-    constexpr int kStages = stages<kRows, kCols>(), kBytes = stage_bytes<kRows, kCols>();
-    constexpr uint32_t kTmem = 2 * kCols;
+    constexpr int kStages = stages<kN>(), kBytes = stage_bytes<kN>();
+    constexpr int kRows = kWeights ? kTileRows : kN, kCols = kWeights ? kN : kTileRows;          // of the output's tile
+    constexpr uint32_t kTmem = 2 * kN;
     extern __shared__ uint8_t raw[];
     uint8_t *const ring = raw + (1024 - smem_addr(raw) % 1024) % 1024;      // not by an integer, past which nobody knows that it is shared memory
     uint8_t *const staging = ring + kStages * kBytes;
@@ -215,11 +280,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     __syncthreads();
     fence_after();
     const uint32_t tmem = S.tmem;
-    const int across = (P.wide + kCols - 1) / kCols;
-    const int tiles = kWeights ? P.experts * ((P.high + kRows - 1) / kRows) * across : S.first[P.experts] * across;
     const int stride = static_cast<int>(gridDim.x);
     const uint32_t base = smem_addr(ring);
     Walk<kWeights, kRows, kCols> walk;
+    const int tiles = walk.tiles(S, P);
 
     if (warp == kLoadWarp) {
         if (lane == 0) {
@@ -230,21 +294,21 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 for (int k = 0; k < t.steps; ++k) {
                     bar_wait(smem_addr(&S.empty[slot]), phase ^ 1, failed);
                     if (*failed) break;
-                    const uint32_t a = base + slot * kBytes, b = a + kRows * 128, bar = smem_addr(&S.full[slot]);
+                    const uint32_t a = base + slot * kBytes, b = a + kTileRows * 128, bar = smem_addr(&S.full[slot]);
                     bar_expect(bar, kBytes);
                     if constexpr (kWeights) {
 #pragma unroll
-                        for (int x = 0; x < kRows; x += 64) load_box3(a + x * 128, &M.a, t.row + x, begin + k * kStep, 0, bar);
+                        for (int x = 0; x < kTileRows; x += 64) load_box3(a + x * 128, &M.a, t.row + x, begin + k * kStep, 0, bar);
 #pragma unroll
-                        for (int x = 0; x < kCols; x += 64) load_box3(b + x * 128, &M.b, t.col + x, begin + k * kStep, 0, bar);
+                        for (int x = 0; x < kN; x += 64) load_box3(b + x * 128, &M.b, t.col + x, begin + k * kStep, 0, bar);
                     } else {
-                        load_box3(a, &M.a, k * kStep, begin + t.row, 0, bar);
                         if constexpr (kDown) {
 #pragma unroll
-                            for (int x = 0; x < kCols; x += 64) load_box3(b + x * 128, &M.b, t.col + x, k * kStep, t.expert, bar);
+                            for (int x = 0; x < kTileRows; x += 64) load_box3(a + x * 128, &M.a, t.col + x, k * kStep, t.expert, bar);
                         } else {
-                            load_box3(b, &M.b, k * kStep, t.col, t.expert, bar);
+                            load_box3(a, &M.a, k * kStep, t.col, t.expert, bar);
                         }
+                        load_box3(b, &M.b, k * kStep, begin + t.row, 0, bar);
                     }
                     ++issued;
                     if (++slot == kStages) {
@@ -267,27 +331,27 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
     } else if (warp == kIssueWarp) {
         const uint32_t lead = elect_lane();
-        constexpr uint32_t word = product(kCols, kDown || kWeights) | (kWeights ? 1u << 15 : 0u);
+        constexpr uint32_t plain = product(0, kWeights) | (kDown ? 1u << 15 : 0u);
         int slot = 0, phase = 0, buffer = 0, turn = 0;
         for (int tile = blockIdx.x; tile < tiles; tile += stride) {
             const Tile t = walk.at(S, P, tile);
             if (t.steps == 0) continue;
+            const uint32_t word = plain | columns_word(kWeights ? kN : min(kN, (t.rows - t.row + 15) / 16 * 16));
             bar_wait(smem_addr(&S.written[buffer]), turn ^ 1, failed);
             fence_after();
             for (int k = 0; k < t.steps; ++k) {
                 bar_wait(smem_addr(&S.full[slot]), phase, failed);
                 __syncwarp();
                 const int left = kWeights ? t.rows - k * kStep : kStep;
-                if (left < kStep) clean_rows<(kRows + kCols) / 64>(ring + slot * kBytes, left, lane);
+                if (left < kStep) clean_rows<(kTileRows + kN) / 64>(ring + slot * kBytes, left, lane);
                 fence_after();
-                const uint32_t a = base + slot * kBytes, b = a + kRows * 128;
-                const uint32_t da = kWeights ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
-                const uint32_t db = kWeights || kDown ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
+                const uint32_t a = base + slot * kBytes, b = a + kTileRows * 128;
+                const uint32_t da = kDown ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
+                const uint32_t db = kWeights ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
 #pragma unroll
                 for (int x = 0; x < kStep; x += 16)
                     if (!kWeights || x < left)   // whole steps past the expert's last row are left out
-                        mma_ss(lead, tmem + buffer * kCols, da + (kWeights ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights || kDown ? x * 128 >> 4 : x * 2 >> 4), word,
-                               k > 0 || x > 0);
+                        mma_ss(lead, tmem + buffer * kN, da + (kDown ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights ? x * 128 >> 4 : x * 2 >> 4), word, k > 0 || x > 0);
                 commit(lead, smem_addr(&S.empty[slot]));
                 if (++slot == kStages) {
                     slot = 0;
@@ -310,7 +374,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 __syncwarp();
                 fence_after();
             }
-            write_tile<kWeights, kRows, kCols>(S, P, t, 0, tmem + buffer * kCols, staging, [&] { bar_arrive(smem_addr(&S.written[buffer])); });
+            const auto done = [&] { bar_arrive(smem_addr(&S.written[buffer])); };
+            if constexpr (kWeights) write_tile<kTileRows, kN>(S, P, t, 0, tmem + buffer * kN, staging, done);
+            else write_rows<kN>(S, P, t, t.col, tmem + buffer * kN, staging, done);
             if (t.steps > 0) {
                 buffer ^= 1;
                 if (buffer == 0) turn ^= 1;
@@ -327,9 +393,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 
 // ---- two SMs to a tile -----------------------------------------------------------------------
 
-// Tiles of 256 x 256 by a cluster of two blocks: each holds 128 rows of A and 128 columns of B, and 128 rows of the accumulator;
-// the products, issued by the first, read both.  Against one SM's 128 x 256 each byte of B is copied to and read from shared
-// memory half as often.
+// Tiles of 256 x 256 by a cluster of two blocks: each holds 128 of A and 128 of B, and 128 lanes of the accumulator; the products,
+// issued by the first, read both.  Against one SM's 128 x 256 each byte of B is copied to and read from shared memory half as
+// often.
 constexpr int kPairRows = 256, kPairCols = 256, kPairStage = 2 * kTileRows * 128;
 constexpr int kPairStages = (227 * 1024 - kBesides) / kPairStage;
 constexpr int kPairBytes = kBesides + kPairStages * kPairStage;
@@ -389,6 +455,9 @@ __device__ __forceinline__ void commit_pair(uint32_t lead, uint32_t bar) {
                  ::"r"(bar), "r"(lead) : "memory");
 }
 
+// Columns of a product's accumulator: the rows that the expert has left, half of them each block's.
+__device__ __forceinline__ int pair_columns(const Tile &t) { return min(kPairRows, (t.rows - t.row + 31) / 32 * 32); }
+
 template <bool kWeights, bool kDown>
 __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
     extern __shared__ uint8_t raw[];
@@ -422,18 +491,17 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
     cluster_sync();
     fence_after();
     const uint32_t tmem = S.tmem;
-    const int across = (P.wide + kPairCols - 1) / kPairCols;
-    const int tiles = kWeights ? P.experts * ((P.high + kPairRows - 1) / kPairRows) * across : S.first[P.experts] * across;
     const int begin = static_cast<int>(blockIdx.x) / 2, stride = static_cast<int>(gridDim.x) / 2;
     const uint32_t base = smem_addr(ring);
     Walk<kWeights, kPairRows, kPairCols> walk;
+    const int tiles = walk.tiles(S, P);
 
     if (warp == kLoadWarp) {
         if (lane == 0) {
             int slot = 0, phase = 0, issued = 0;
             for (int tile = begin; tile < tiles && !*failed; tile += stride) {
                 const Tile t = walk.at(S, P, tile);
-                const int first = S.begin[t.expert], row = t.row + rank * kTileRows, col = t.col + rank * kTileRows;
+                const int first = S.begin[t.expert], row = t.row + rank * (kWeights ? kTileRows : pair_columns(t) / 2), col = t.col + rank * kTileRows;
                 for (int k = 0; k < t.steps; ++k) {
                     bar_wait(smem_addr(&S.empty[slot]), phase ^ 1, failed);
                     if (*failed) break;
@@ -448,13 +516,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
                             load_box3_pair(b + x * 128, &M.b, col + x, first + k * kStep, 0, bar);
                         }
                     } else {
-                        load_box3_pair(a, &M.a, k * kStep, first + row, 0, bar);
                         if constexpr (kDown) {
 #pragma unroll
-                            for (int x = 0; x < kTileRows; x += 64) load_box3_pair(b + x * 128, &M.b, col + x, k * kStep, t.expert, bar);
+                            for (int x = 0; x < kTileRows; x += 64) load_box3_pair(a + x * 128, &M.a, col + x, k * kStep, t.expert, bar);
                         } else {
-                            load_box3_pair(b, &M.b, k * kStep, col, t.expert, bar);
+                            load_box3_pair(a, &M.a, k * kStep, col, t.expert, bar);
                         }
+                        load_box3_pair(b, &M.b, k * kStep, first + row, 0, bar);
                     }
                     ++issued;
                     if (++slot == kPairStages) {
@@ -468,6 +536,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
                 if (slot == kPairStages - 1) phase ^= 1;
                 bar_wait(smem_addr(&S.empty[slot]), phase, failed);
             }
+            if (rank == 1 && !*failed) bar_wait(smem_addr(&S.drain), 0, failed);      // the last arrival from there
             if (*failed && issued > 0) {         // copies in flight end before the blocks' shared memory goes away: nothing tells when, so
                 const uint64_t from = now_ns();  // they get far more time than a copy takes
                 while (now_ns() - from < 1000000ull) {}
@@ -475,12 +544,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
         }
     } else if (warp == kIssueWarp) {
         const uint32_t lead = elect_lane();
-        constexpr uint32_t word = (product(kPairCols, kDown || kWeights) & 0x00ffffffu) | (16u << 24) | (kWeights ? 1u << 15 : 0u);      // 256 rows
+        constexpr uint32_t plain = (product(0, kWeights) & 0x00ffffffu) | (16u << 24) | (kDown ? 1u << 15 : 0u);       // 256 lanes
         int slot = 0, phase = 0, buffer = 0, turn = 0;
         uint32_t ends = 0;                       // by slot: the phase of `clean`
         for (int tile = begin; tile < tiles && rank == 0; tile += stride) {
             const Tile t = walk.at(S, P, tile);
             if (t.steps == 0) continue;
+            const uint32_t word = plain | columns_word(kWeights ? kPairCols : pair_columns(t));
             bar_wait(smem_addr(&S.written[buffer]), turn ^ 1, failed);
             for (int k = 0; k < t.steps; ++k) {
                 const int left = kWeights ? t.rows - k * kStep : kStep;
@@ -493,13 +563,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
                 __syncwarp();
                 fence_after();
                 const uint32_t a = base + slot * kPairStage, b = a + kTileRows * 128;
-                const uint32_t da = kWeights ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
-                const uint32_t db = kWeights || kDown ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
+                const uint32_t da = kDown ? desc_along_rows(a, kStep * 128) : desc_along_columns(a);
+                const uint32_t db = kWeights ? desc_along_rows(b, kStep * 128) : desc_along_columns(b);
 #pragma unroll
                 for (int x = 0; x < kStep; x += 16)
                     if (!kWeights || x < left)
-                        mma_pair(lead, tmem + buffer * kPairCols, da + (kWeights ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights || kDown ? x * 128 >> 4 : x * 2 >> 4),
-                                 word, k > 0 || x > 0);
+                        mma_pair(lead, tmem + buffer * kPairCols, da + (kDown ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights ? x * 128 >> 4 : x * 2 >> 4), word, k > 0 || x > 0);
                 commit_pair(lead, smem_addr(&S.empty[slot]));
                 if (++slot == kPairStages) {
                     slot = 0;
@@ -510,9 +579,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
             buffer ^= 1;
             if (buffer == 0) turn ^= 1;
         }
-        if (rank == 0) commit_pair(lead, smem_addr(&S.drain));
-        bar_wait(smem_addr(&S.drain), 0, failed);
-        if (*failed) settle(smem_addr(&S.drain), 0);
+        if (rank == 0) {
+            commit_pair(lead, smem_addr(&S.drain));
+            bar_wait(smem_addr(&S.drain), 0, failed);
+            if (*failed) settle(smem_addr(&S.drain), 0);
+        }
     } else if (warp == kCleanWarp && kWeights) {
         // Zeros in the rows past an expert's last, in this block's part of the step that holds them.  The first block's copies are waited
         // for one after the other (a phase told by its parity has to be the current one or the last); the second's `full` has
@@ -545,8 +616,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
                 __syncwarp();
                 fence_after();
             }
-            write_tile<kWeights, kPairRows, kPairCols>(S, P, t, rank * kTileRows, tmem + buffer * kPairCols, staging,
-                                            [&] { bar_arrive_in_relaxed(in_block(smem_addr(&S.written[buffer]), 0)); });
+            const auto done = [&] { bar_arrive_in_relaxed(in_block(smem_addr(&S.written[buffer]), 0)); };
+            if constexpr (kWeights) write_tile<kPairRows, kPairCols>(S, P, t, rank * kTileRows, tmem + buffer * kPairCols, staging, done);
+            else write_rows<kPairRows>(S, P, t, t.col + rank * kTileRows, tmem + buffer * kPairCols, staging, done);
             if (t.steps > 0) {
                 buffer ^= 1;
                 if (buffer == 0) turn ^= 1;
@@ -568,7 +640,7 @@ using ProductKernel = void (*)(const ProductParams, const ProductMaps);
 
 // Shared-memory limit of a kernel, set once per device.
 bool allow(ProductKernel fn, int which, int bytes) {
-    static std::atomic<bool> set[64][20];
+    static std::atomic<bool> set[64][10];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
         cudaGetLastError();
@@ -624,14 +696,14 @@ int check_matrices(const loco_matrices_t *t, int64_t experts, int64_t rows, int6
     return LOCO_OK;
 }
 
-template <bool kWeights, bool kDown, int kRows, int kCols> int launch_product(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
-    static_assert(product_bytes<kRows, kCols>() <= 227 * 1024 && stages<kRows, kCols>() >= 4, "shared memory of a block");
+template <bool kWeights, bool kDown, int kN> int launch_product(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
+    static_assert(product_bytes<kN>() <= 227 * 1024 && stages<kN>() >= 4, "shared memory of a block");
     const int sms = sm_count();
     if (sms == 0) return LOCO_ERR_CUDA;
     if (tiles > 0x7fffffff - sms) return LOCO_ERR_UNSUPPORTED;
-    constexpr ProductKernel fn = product_kernel<kWeights, kDown, kRows, kCols>;
-    if (!allow(fn, which, product_bytes<kRows, kCols>())) return LOCO_ERR_CUDA;
-    return launch_kernel(fn, dim3(static_cast<unsigned>(tiles < sms ? tiles : sms)), kProductThreads, product_bytes<kRows, kCols>(), stream, P, M);
+    constexpr ProductKernel fn = product_kernel<kWeights, kDown, kN>;
+    if (!allow(fn, which, product_bytes<kN>())) return LOCO_ERR_CUDA;
+    return launch_kernel(fn, dim3(static_cast<unsigned>(tiles < sms ? tiles : sms)), kProductThreads, product_bytes<kN>(), stream, P, M);
 }
 
 template <bool kWeights, bool kDown> int launch_pair(const ProductParams &P, const ProductMaps &M, int64_t tiles, int which, void *stream) {
@@ -665,28 +737,25 @@ int loco_experts_product(const loco_product_t *c, const loco_rows_t *x, const lo
     const int64_t rows = turned ? c->d_out : c->d_in, columns = turned ? c->d_in : c->d_out;
     if ((rc = check_rows(x, c->rows, c->d_in, false)) != LOCO_OK || (rc = check_rows(y, c->rows, c->d_out, true)) != LOCO_OK ||
         (rc = check_matrices(w, c->experts, rows, columns, false)) != LOCO_OK) return rc;
-    ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(y->ptr), 0, c->rows > 1 ? y->row_stride : 0, c->rows, c->experts, c->d_in, 0, c->d_out};
+    ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(y->ptr), 0, c->rows > 1 ? y->row_stride : 0, c->rows, c->experts, c->d_in, 0, c->d_out, 0};
     ProductMaps M;
-    const int sms = sm_count();
-    if (sms == 0) return LOCO_ERR_CUDA;
-    // Tiles by the rows an expert has on average: pairs of SMs where they fill 256 rows, else 32, 64 or 128 rows.  128 columns: eight
-    // rows of five experts at work, 4096 x 28672, in tiles of 64, 128, 256 columns: 201, 146, 148 us (HBM 143); 14336 x 4096: 167, 71, 83
-    // (HBM 72).  256 where that takes the SMs no more rounds.
+    // Tiles by the rows an expert has on average: 32 and 64 for few, which leave the more of shared memory to the matrices on their
+    // way (12 and 8 stages), else 256 by pairs of SMs.  64 a pair's against 128 of one SM: 64 rows an expert, 4096 x 14336: 139, 147 us; pairs
+    // against 64 for 47 rows an expert, 1032 x 2048: 62, 57 us.
     const int64_t each = c->rows / c->experts, ends = c->rows < c->experts ? c->rows : c->experts;           // every expert may end in a tile of its own
-    const bool pair = each >= 160;
-    const int high = pair ? kTileRows : each < 24 ? 32 : each < 56 ? 64 : 128;
-    const auto count = [&](int w) { return (c->rows / high + ends) * over(c->d_out, w); };
-    const int wide = high == 64 && over(count(256), sms) * 2 <= over(count(128), sms) ? 256 : 128;
-    const int64_t tiles = pair ? (c->rows / kPairRows + ends) * over(c->d_out, kPairCols) : count(wide);
-    if (!make_map(M.a, x->ptr, c->d_in, c->rows, 1, x->row_stride, 0, high) ||
-        !make_map(M.b, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? (pair ? kTileRows : wide) : kStep)) return LOCO_ERR_CUDA;
+    const bool pair = each >= 56;
+    // Where products bound the call, the tiles with less to do fill the last rounds (16384 rows of 14336 through 4096 columns, eight experts:
+    // 1720 us expert by expert, 1635 so); where the matrices' reading does, an expert's tiles stay together (3001 rows, 64 experts: 57, 69).
+    P.last = each >= 512;
+    const int high = pair ? kTileRows : each < 24 ? 32 : 64;
+    const int64_t tiles = pair ? (c->rows / kPairRows + ends) * over(c->d_out, kPairCols) : (c->rows / high + ends) * over(c->d_out, kTileRows);
+    if (!make_map(M.a, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? kTileRows : kStep) ||
+        !make_map(M.b, x->ptr, c->d_in, c->rows, 1, x->row_stride, 0, high)) return LOCO_ERR_CUDA;
     const auto go = [&](auto down) {
         constexpr bool kDown = decltype(down)::value;
-        constexpr int kFirst = kDown ? 8 : 0;
+        constexpr int kFirst = kDown ? 4 : 0;
         if (pair) return launch_pair<false, kDown>(P, M, tiles, kFirst, stream);
-        if (high == 32) return launch_product<false, kDown, 32, 128>(P, M, tiles, kFirst + 1, stream);
-        if (high == 64) return wide == 128 ? launch_product<false, kDown, 64, 128>(P, M, tiles, kFirst + 2, stream) : launch_product<false, kDown, 64, 256>(P, M, tiles, kFirst + 3, stream);
-        return launch_product<false, kDown, 128, 128>(P, M, tiles, kFirst + 4, stream);
+        return high == 32 ? launch_product<false, kDown, 32>(P, M, tiles, kFirst + 1, stream) : launch_product<false, kDown, 64>(P, M, tiles, kFirst + 2, stream);
     };
     return turned ? go(std::false_type{}) : go(std::true_type{});
 }
@@ -698,14 +767,14 @@ int loco_experts_product_weights(const loco_product_t *c, const loco_rows_t *a, 
     if ((rc = check_matrices(dw, c->experts, c->d_in, c->d_out, true)) != LOCO_OK) return rc;
     if (c->rows > 0 && ((rc = check_rows(a, c->rows, c->d_in, false)) != LOCO_OK || (rc = check_rows(b, c->rows, c->d_out, false)) != LOCO_OK)) return rc;
     ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(dw->ptr), c->experts > 1 ? dw->expert_stride : 0, c->d_in > 1 ? dw->row_stride : 0, c->rows, c->experts,
-                    0, c->d_in, c->d_out};
+                    0, c->d_in, c->d_out, 0};
     ProductMaps M;
     // without rows nothing is read: the maps need a valid address all the same
     const bool none = c->rows == 0, pair = c->d_in > kTileRows;
     if (!make_map(M.a, none ? dw->ptr : a->ptr, c->d_in, none ? 1 : c->rows, 1, none ? 0 : a->row_stride, 0, kStep) ||
         !make_map(M.b, none ? dw->ptr : b->ptr, c->d_out, none ? 1 : c->rows, 1, none ? 0 : b->row_stride, 0, kStep)) return LOCO_ERR_CUDA;
-    if (pair) return launch_pair<true, true>(P, M, c->experts * over(c->d_in, kPairRows) * over(c->d_out, kPairCols), 16, stream);
-    return launch_product<true, true, kTileRows, 128>(P, M, c->experts * over(c->d_in, kTileRows) * over(c->d_out, 128), 17, stream);
+    if (pair) return launch_pair<true, true>(P, M, c->experts * over(c->d_in, kPairRows) * over(c->d_out, kPairCols), 8, stream);
+    return launch_product<true, true, 128>(P, M, c->experts * over(c->d_in, kTileRows) * over(c->d_out, 128), 9, stream);
 }
 
 }  // extern "C"
