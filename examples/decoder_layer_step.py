@@ -1,10 +1,11 @@
 """Training steps of one Mixtral-shaped decoder layer with compressed gradients, on one GPU.
 
-    python examples/decoder_layer_step.py [--steps 8] [--workers 2] [--full]
+    python examples/decoder_layer_step.py [--steps 8] [--workers 2] [--clip 1.0] [--full]
 
-Every worker runs the layer on its own batch: rotary positions, causal attention with shared key heads, a top-2 router with
-balance and z loss (paper_2407_04480_b200.layer), projections and experts as torch products.  Its gradient, flattened in
-bfloat16 like a bucket of a trainer, goes through the send pass; the receive pass averages the workers' packed buffers and
+Every worker runs the layer on its own batch: norms with the residual's addition, rotary positions, causal attention with shared
+key heads, a top-2 router with balance and z loss, the tokens sorted by expert, the experts' products and the sum back
+(paper_2407_04480_b200.layer), projections as torch products.  Its gradient, flattened in bfloat16 like a bucket of a trainer and
+scaled down to a largest norm where one is given, goes through the send pass; the receive pass averages the workers' packed buffers and
 applies the Adam-family step to the fp32 weights (paper_2407_04480_b200.loco).  The workers are simulated one after the other.
 The data is random: a fixed target function of the input that the layer learns.
 """
@@ -14,7 +15,7 @@ import argparse
 import os
 import sys
 from dataclasses import dataclass
-from typing import Dict, List
+from typing import Dict, List, Optional
 
 import torch
 
@@ -45,7 +46,16 @@ MIXTRAL = Shape(4096, 32, 8, 128, 14336, 8, 2)
 
 
 def norm(x: torch.Tensor) -> torch.Tensor:
+    """layer.norm's plain form."""
     return (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-5)).to(x.dtype)
+
+
+def sorted_experts(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, index: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
+    """experts() without a look at the counts on the host: the tokens sorted by expert, one product for all of them."""
+    offsets, place = layer.experts_sort(index, shape.experts)
+    w1, w2 = (torch.stack([w["%s.%d" % (n, e)] for e in range(shape.experts)]) for n in ("w1", "w2"))
+    a, b = layer.experts_product(layer.dispatch(x, place, offsets), w1, offsets).chunk(2, -1)
+    return layer.combine(layer.experts_product(torch.nn.functional.silu(a) * b, w2, offsets), place, offsets, weight)
 
 
 def experts(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, index: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
@@ -62,18 +72,18 @@ def experts(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, index: to
 def forward(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, table: torch.Tensor, router: layer.Router, work: torch.Tensor):
     """(output, tokens per expert, balance and z loss) of x [batch, seq, d_model]."""
     b, s, _ = x.shape
-    qkv = (norm(x) @ w["qkv"]).unflatten(-1, (-1, shape.head_dim))
+    qkv = (layer.norm(x) @ w["qkv"]).unflatten(-1, (-1, shape.head_dim))
     q, k, v = qkv.split((shape.heads, shape.heads_kv, shape.heads_kv), 2)
     q, k = layer.rotary(q, k, table)
     o = layer.attention(q, k, v, causal=True)
-    x = x + o.flatten(2) @ w["out"]
-    h = norm(x).flatten(0, 1)
+    h, x = layer.norm(o.flatten(2) @ w["out"], residual=x)
+    h = h.flatten(0, 1)
     index, weight, counts, _, losses = layer.router(h @ w["router"], router, work=work)
-    return x + experts(shape, w, h, index, weight).view_as(x), counts, losses
+    return x + sorted_experts(shape, w, h, index, weight).view_as(x), counts, losses
 
 
 def run(shape: Shape = Shape(), steps: int = 8, workers: int = 2, batch: int = 2, seq: int = 320, seed: int = 0,
-        lr: float = 2e-3, report=print) -> List[float]:
+        lr: float = 2e-3, report=print, max_norm: Optional[float] = None) -> List[float]:
     """Training loss of every step."""
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
@@ -104,7 +114,10 @@ def run(shape: Shape = Shape(), steps: int = 8, workers: int = 2, batch: int = 2
             target = x + torch.tanh(x.cumsum(1) / (torch.arange(seq, device="cuda") + 1.0).sqrt()[:, None].to(x.dtype) @ turn)
             loss = (y.float() - target.float()).square().mean() + losses.sum()
             grad, = torch.autograd.grad(loss, flat)
-            loco.loco_compensate_quantize_pack(states[rank], grad.contiguous(), comms[rank], k + 1)
+            grad = grad.contiguous()
+            if max_norm is not None:
+                layer.clip_gradients([grad], max_norm)
+            loco.loco_compensate_quantize_pack(states[rank], grad, comms[rank], k + 1)
             total += float(loss.detach()) / workers
             idle += int((counts[:shape.experts] == 0).sum())          # experts whose gradient segments are all zero
         loco.loco_unpack_dequant_reduce_adam(cfg, comms, n, *moments, theta, lr=lr, beta1=0.1, beta2=0.01, delta=1e-12)
@@ -120,5 +133,6 @@ if __name__ == "__main__":
     ap.add_argument("--steps", type=int, default=8)
     ap.add_argument("--workers", type=int, default=2)
     ap.add_argument("--full", action="store_true", help="Mixtral-8x7B's layer: 4096 wide, 32 / 8 heads, experts of 14336")
+    ap.add_argument("--clip", type=float, default=None, help="largest norm of a worker's gradient")
     a = ap.parse_args()
-    run(MIXTRAL if a.full else Shape(), steps=a.steps, workers=a.workers)
+    run(MIXTRAL if a.full else Shape(), steps=a.steps, workers=a.workers, max_norm=a.clip)

@@ -327,6 +327,14 @@ __global__ void __launch_bounds__(kMoveThreads, kRows > 4 ? 3 : 4) experts_backw
     }
 }
 
+// Rows from the last offset on: nothing to write, as a rule.
+template <typename T> __global__ void __launch_bounds__(kMoveThreads) experts_clear_kernel(T *rows, int64_t stride, int64_t count, int dim, const int32_t *last) {
+    wait_for_previous();
+    let_next_start();
+    for (int64_t r = max(*last, 0) + static_cast<int64_t>(blockIdx.x); r < count; r += gridDim.x)
+        for (int c = threadIdx.x; c < dim; c += kMoveThreads) rows[r * stride + c] = from_f32<T>(0.0f);
+}
+
 namespace {
 
 using MoveKernel = void (*)(const MoveParams);
@@ -426,6 +434,24 @@ int loco_experts_sort(int32_t experts, int64_t tokens, int32_t top_k, const int3
         if (rc != LOCO_OK) return rc;
     }
     return launch_kernel(experts_place_kernel, grid, kSortThreads, static_cast<size_t>(kSortWarps) * experts * sizeof(int), stream, P);
+}
+
+int loco_experts_clear(int32_t dtype, int32_t dim, int64_t rows_count, const loco_rows_t *rows, int32_t experts, const int32_t *d_offsets, void *stream) {
+    const loco_experts_t c{dtype, dim, 1, 0, rows_count};
+    int rc = check_experts(&c);
+    if (rc != LOCO_OK) return rc;
+    if (experts < 1 || experts > kMostExperts || !d_offsets) return LOCO_ERR_ARG;
+    int vec = 1;
+    int64_t stride;
+    if ((rc = take_rows(&c, rows, rows_count, true, vec, stride)) != LOCO_OK) return rc;
+    if (!aligned(d_offsets, 4)) return LOCO_ERR_ALIGN;
+    if (rows_count == 0) return LOCO_OK;
+    const int sms = sm_count();
+    if (sms == 0) return LOCO_ERR_CUDA;
+    const dim3 grid(static_cast<unsigned>(rows_count < sms * 4 ? rows_count : sms * 4));
+    if (dtype == LOCO_BF16)
+        return launch_kernel(experts_clear_kernel<__nv_bfloat16>, grid, kMoveThreads, 0, stream, static_cast<__nv_bfloat16 *>(rows->ptr), stride, rows_count, dim, d_offsets + experts);
+    return launch_kernel(experts_clear_kernel<float>, grid, kMoveThreads, 0, stream, static_cast<float *>(rows->ptr), stride, rows_count, dim, d_offsets + experts);
 }
 
 int loco_experts_dispatch(const loco_experts_t *c, const loco_rows_t *x, const int32_t *d_place, const loco_rows_t *rows, void *stream) {

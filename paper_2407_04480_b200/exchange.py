@@ -28,7 +28,7 @@ from typing import List, Optional
 import torch
 import torch.distributed as dist
 
-from . import loco
+from . import layer, loco
 
 TRANSPORTS = ("collective", "peer_store")
 
@@ -61,6 +61,23 @@ def scatter_table(peer_area_ptrs: List[int], cfg: "loco.Config", n: int, my_rank
 def shard_elems(cfg: "loco.Config", n: int, rank: int) -> int:
     """Elements of the averaged gradient that rank owns after the exchange."""
     return loco.loco_partition_elems(cfg, n, rank)
+
+
+def clip_shards(shards: List[torch.Tensor], max_norm: float, group: Optional[dist.ProcessGroup] = None,
+                work: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scale the averaged gradient, of which every rank holds the shards that BucketExchange.step left it, down to a global norm of
+    max_norm, in place; returns the norm it had (fp32 [1], the same on every rank).
+
+    One double is added up over the ranks between the two passes over the shards; nothing synchronises the host.  work: a
+    workspace to keep between calls (layer.loco_gradient_squares_workspace_bytes() bytes, zeroed once); None allocates one."""
+    device = shards[0].device
+    if work is None:
+        work = torch.zeros(layer.loco_gradient_squares_workspace_bytes(), dtype=torch.uint8, device=device)
+    squares, norm = torch.empty(1, dtype=torch.float64, device=device), torch.empty(1, dtype=torch.float32, device=device)
+    layer.loco_gradient_squares(shards, squares, work)
+    dist.all_reduce(squares, group=group)
+    layer.loco_gradient_clip(shards, shards, squares, norm, max_norm)
+    return norm
 
 
 class Transport:

@@ -29,7 +29,7 @@ SCALINGS = {"plain": ROTARY_PLAIN, "linear": ROTARY_LINEAR, "parts": ROTARY_PART
 EXPORTS = ("loco_rotary_table", "loco_rotary_apply", "loco_attention_forward", "loco_attention_backward",
            "loco_attention_backward_workspace_bytes", "loco_router_workspace_bytes", "loco_router_forward",
            "loco_router_backward", "loco_norm_forward", "loco_norm_backward", "loco_norm_backward_workspace_bytes",
-           "loco_experts_sort", "loco_experts_sort_workspace_bytes", "loco_experts_dispatch", "loco_experts_combine",
+           "loco_experts_sort", "loco_experts_sort_workspace_bytes", "loco_experts_clear", "loco_experts_dispatch", "loco_experts_combine",
            "loco_experts_combine_backward", "loco_experts_product", "loco_experts_product_weights", "loco_gradient_squares",
            "loco_gradient_squares_workspace_bytes", "loco_gradient_clip", "loco_layer_status", "loco_layer_launch_count")
 FLAG_TIMEOUT = 1
@@ -72,6 +72,7 @@ def lib() -> C.CDLL:
         L.loco_norm_backward_workspace_bytes.argtypes = [st]
         L.loco_experts_sort.argtypes = [i32, i64, i32, vp, vp, vp, vp, u64, vp]
         L.loco_experts_sort_workspace_bytes.argtypes = [i32]
+        L.loco_experts_clear.argtypes = [i32, i32, i64, st, i32, vp, vp]
         L.loco_experts_dispatch.argtypes = [st, st, vp, st, vp]
         L.loco_experts_combine.argtypes = [st, st, vp, vp, st, vp]
         L.loco_experts_combine_backward.argtypes = [st, st, st, vp, vp, st, vp, vp]
@@ -274,6 +275,11 @@ def loco_experts_combine_backward(dy, rows, place, weight, drows, dweight, strea
     _check(_binding().experts_combine_backward(dy, rows, place, weight, drows, dweight, _raw(stream)), "loco_experts_combine_backward")
 
 
+def loco_experts_clear(rows, offsets, stream=None) -> None:
+    """Zeros in rows [rows, dim] from offsets[experts] on, which the other calls leave as they are."""
+    _check(_binding().experts_clear(rows, offsets, _raw(stream)), "loco_experts_clear")
+
+
 def loco_experts_product(x, w, offsets, y, transposed: bool = False, stream=None) -> None:
     """y[t] = x[t] @ w[e] for the rows t of every expert e, offsets[e] to offsets[e + 1]; bfloat16.
 
@@ -420,3 +426,165 @@ def router(logits, cfg: Router, mask=None, work: Optional[torch.Tensor] = None):
     if work is None:
         work = torch.zeros(loco_router_workspace_bytes(cfg), dtype=torch.uint8, device=logits.device)
     return _Router.apply(logits, cfg, mask, work)
+
+
+def _flat(t: torch.Tensor) -> torch.Tensor:
+    """[rows, dim] of any leading dimensions, the rows contiguous; a copy where strides say so."""
+    t = t.reshape(-1, t.shape[-1])
+    return t if t.stride(1) == 1 or t.shape[1] == 1 else t.contiguous()
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps):
+        flat, y = _flat(x), torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        loco_norm_forward(flat, _flat(y), weight=weight, residual=None if residual is None else _flat(residual),
+                          total=None if total is None else _flat(total), eps=eps)
+        ctx.save_for_backward(x if total is None else total, weight)
+        ctx.eps, ctx.had_residual = eps, residual is not None
+        ctx.set_materialize_grads(False)
+        return y, total
+
+    @staticmethod
+    def backward(ctx, dy, dtotal):
+        def compute(h, weight, dy, dtotal):
+            if dy is None:
+                return dtotal, None if weight is None else torch.zeros_like(weight)
+            dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+            dweight = None if weight is None or not ctx.needs_input_grad[2] else torch.empty_like(weight, memory_format=torch.contiguous_format)
+            work = None if dweight is None else torch.empty(loco_norm_backward_workspace_bytes(h.shape[-1], h.dtype), dtype=torch.uint8, device=h.device)
+            loco_norm_backward(_flat(h), _flat(dy), _flat(dx), work, weight=weight, dweight=dweight, dtotal=None if dtotal is None else _flat(dtotal),
+                               eps=ctx.eps)
+            return dx, dweight
+        if dy is None and dtotal is None:
+            return None, None, None, None
+        dx, dweight = _gradient("norm", compute, *ctx.saved_tensors, dy, dtotal)
+        return dx, dx if ctx.had_residual else None, dweight, None
+
+
+def norm(x, weight=None, residual=None, eps: float = 1e-5):
+    """Root-mean-square norm of x [..., dim], times weight [dim]; with a residual (norm of x + residual, x + residual as it is kept).
+
+    Differentiable once."""
+    y, total = _Norm.apply(x, residual, weight, eps)
+    return y if residual is None else (y, total)
+
+
+def experts_sort(index, experts: int, work: Optional[torch.Tensor] = None):
+    """(offsets, place) of the router's choices index [tokens, top_k], as loco_experts_sort.
+
+    work: a workspace to keep between calls (loco_experts_sort_workspace_bytes() bytes); None allocates one."""
+    offsets = torch.empty(experts + 1, dtype=torch.int32, device=index.device)
+    place = torch.empty(index.shape, dtype=torch.int32, device=index.device)
+    if work is None:
+        work = torch.empty(loco_experts_sort_workspace_bytes(experts), dtype=torch.uint8, device=index.device)
+    loco_experts_sort(index, offsets, place, work)
+    return offsets, place
+
+
+def _cleared(rows, offsets):
+    loco_experts_clear(rows, offsets)
+    return rows
+
+
+class _Dispatch(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, place, offsets):
+        rows = torch.empty(place.numel(), x.shape[1], dtype=x.dtype, device=x.device)
+        loco_experts_dispatch(_flat(x), place, rows)
+        ctx.save_for_backward(place)
+        return _cleared(rows, offsets)
+
+    @staticmethod
+    def backward(ctx, drows):
+        def compute(place, drows):
+            dx = torch.empty(place.shape[0], drows.shape[1], dtype=drows.dtype, device=drows.device)
+            loco_experts_combine(_flat(drows), place, dx)
+            return dx
+        return _gradient("dispatch", compute, *ctx.saved_tensors, drows), None, None
+
+
+def dispatch(x, place, offsets):
+    """The tokens x [tokens, dim] in the order of experts_sort's (offsets, place): [tokens * top_k, dim], zeros in rows that no
+    choice has.  Differentiable once."""
+    return _Dispatch.apply(x, place, offsets)
+
+
+class _Combine(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, rows, place, offsets, weight):
+        y = torch.empty(place.shape[0], rows.shape[1], dtype=rows.dtype, device=rows.device)
+        loco_experts_combine(_flat(rows), place, y, weight=weight)
+        # without weights the gradient depends on nothing of the rows but their shape
+        ctx.save_for_backward(None if weight is None else rows, place, offsets, weight)
+        ctx.rows = rows.shape[0]
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        def compute(rows, place, offsets, weight, dy):
+            drows = torch.empty(ctx.rows, dy.shape[1], dtype=dy.dtype, device=dy.device)
+            if weight is None:
+                loco_experts_dispatch(_flat(dy), place, drows)
+                return _cleared(drows, offsets), None
+            dweight = torch.empty(place.shape, dtype=torch.float32, device=dy.device)
+            loco_experts_combine_backward(_flat(dy), _flat(rows), place, weight, drows, dweight)
+            return _cleared(drows, offsets), dweight
+        drows, dweight = _gradient("combine", compute, *ctx.saved_tensors, dy)
+        return drows, None, None, dweight
+
+
+def combine(rows, place, offsets, weight=None):
+    """The experts' rows summed back to their tokens, with the choices' weights (fp32 [tokens, top_k]; None: ones).
+
+    Differentiable once."""
+    return _Combine.apply(rows, place, offsets, weight)
+
+
+class _Product(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, offsets, transposed):
+        y = torch.empty(x.shape[0], w.shape[1 if transposed else 2], dtype=x.dtype, device=x.device)
+        loco_experts_product(x, w, offsets, y, transposed=transposed)
+        ctx.save_for_backward(x, w, offsets)
+        ctx.transposed = transposed
+        return _cleared(y, offsets)
+
+    @staticmethod
+    def backward(ctx, dy):
+        def compute(x, w, offsets, dy):
+            dy = dy.contiguous()
+            if dy.data_ptr() % 16:                   # a contiguous view, off the boundaries that the kernels need
+                dy = dy.clone()
+            dx = dw = None
+            if ctx.needs_input_grad[0]:
+                dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+                loco_experts_product(dy, w, offsets, dx, transposed=not ctx.transposed)
+                _cleared(dx, offsets)
+            if ctx.needs_input_grad[1]:
+                dw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
+                loco_experts_product_weights(*((dy, x) if ctx.transposed else (x, dy)), offsets, dw)
+            return dx, dw
+        dx, dw = _gradient("experts_product", compute, *ctx.saved_tensors, dy)
+        return dx, dw, None, None
+
+
+def experts_product(x, w, offsets, transposed: bool = False):
+    """x[t] @ w[e] for the rows t of every expert e, as loco_experts_product; zeros in rows behind the last expert's.
+
+    Differentiable once."""
+    return _Product.apply(x, w, offsets, transposed)
+
+
+def clip_gradients(gradients, max_norm: float, work: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scale a list of contiguous gradients down, in place, to a global norm of max_norm; returns the norm they had (fp32 [1]).
+
+    work: a workspace to keep between calls (loco_gradient_squares_workspace_bytes() bytes, zeroed once); None allocates one."""
+    device = gradients[0].device
+    if work is None:
+        work = torch.zeros(loco_gradient_squares_workspace_bytes(), dtype=torch.uint8, device=device)
+    squares, norm = torch.empty(1, dtype=torch.float64, device=device), torch.empty(1, dtype=torch.float32, device=device)
+    loco_gradient_squares(gradients, squares, work)
+    loco_gradient_clip(gradients, gradients, squares, norm, max_norm)
+    return norm
