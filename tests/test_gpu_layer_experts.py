@@ -598,3 +598,146 @@ def test_refusals(call):
     with pytest.raises((ValueError, loco.LocoError)):
         call()
     assert layer.loco_layer_launch_count() == before
+
+
+# ---- differentiable forms --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_norm_form(dtype):
+    """Leading dimensions, an operand cut out of a wider one, a broadcast gradient, one that never comes."""
+    g = gen(21)
+    wide = normal(g, 3, 5, 144, dtype=dtype)
+    x, r, w = wide[..., 8:136].requires_grad_(), normal(g, 3, 5, 128, dtype=dtype).requires_grad_(), normal(g, 128, dtype=dtype).requires_grad_()
+    y, total = layer.norm(x, w, residual=r)
+    assert torch.equal(total, (x.detach().double() + r.detach().double()).to(dtype))
+    want, _ = ref.norm(total.detach().flatten(0, 1), w.detach(), 1e-5)
+    within(y.detach().flatten(0, 1), want, want.abs(), NORM_ADDITIONS, dtype)
+    dy, dt = normal(g, 3, 1, 128, dtype=dtype).expand(3, 5, 128), normal(g, 3, 5, 128, dtype=dtype)
+    for gy, gt in ((dy, dt), (dy, None), (None, dt)):
+        outs, grads = zip(*[(o, d) for o, d in ((y, gy), (total, gt)) if d is not None])
+        dx, dr, dw = torch.autograd.grad(outs, (x, r, w), grads, retain_graph=True)
+        flat = lambda t: None if t is None else t.flatten(0, 1)
+        want, terms, gw, gterms = ref.norm_gradient(flat(total.detach()), flat(dy if gy is not None else torch.zeros_like(dt)), w.detach(), flat(gt), 1e-5)
+        within(dx.flatten(0, 1), want, terms, 3 * NORM_ADDITIONS, dtype)
+        within(dw, gw, gterms, 15 + NORM_ADDITIONS, dtype)
+        assert torch.equal(dx, dr)
+
+
+def expert_block(x, index, weight, w1, w2):
+    offsets, place = layer.experts_sort(index, w1.shape[0])
+    a, b = layer.experts_product(layer.dispatch(x, place, offsets), w1, offsets).chunk(2, -1)
+    return layer.combine(layer.experts_product(torch.nn.functional.silu(a) * b, w2, offsets, transposed=True), place, offsets, weight)
+
+
+def block_inputs(seed, t=217, d=136, f=88, e=8, k=2):
+    g = gen(seed)
+    index = choices(g, t, k, e, "holes")
+    return [normal(g, t, d), index, torch.rand(t, k, generator=g, device=DEV), normal(g, e, d, 2 * f, sigma=d ** -0.5), normal(g, e, d, f, sigma=f ** -0.5)]
+
+
+def test_expert_forms_against_64_bits():
+    """Two products, a gate and the weighted sum in a row, and back: a dozen roundings to 16 bits, each 2^-8 of its value, on the way
+    to every gradient; the norm of the difference stays within 12 * 2^-8."""
+    x, index, weight, w1, w2 = block_inputs(31)
+    x, weight, w1, w2 = (t.requires_grad_() for t in (x, weight, w1, w2))
+    y = expert_block(x, index, weight, w1, w2)
+    dy = normal(gen(32), *y.shape)
+    got = torch.autograd.grad(y, (x, weight, w1, w2), dy)
+    X, W, A, B = (t.detach().double().requires_grad_() for t in (x, weight, w1, w2))
+    Y = torch.zeros(x.shape, dtype=torch.float64, device=DEV)
+    for e in range(8):
+        token, slot = torch.where(index == e)
+        a, b = (X[token] @ A[e]).chunk(2, -1)
+        Y = Y.index_add(0, token, (torch.nn.functional.silu(a) * b) @ B[e].T * W[token, slot, None])
+    want = torch.autograd.grad(Y, (X, W, A, B), dy.double())
+    for a, b in zip((y.detach(), *got), (Y.detach(), *want)):
+        assert float((a.double() - b).norm()) <= 12 * 2.0 ** -8 * float(b.norm())
+    none = (index < 0) | (index >= 8)
+    assert not got[1][none].any() and not got[0][none.all(1)].any()
+
+
+def test_forms_leave_nothing_undefined_behind_the_last_expert():
+    """Memory that the allocator hands out holds NaN; what goes on with all rows, a bias' gradient for one, must not see it."""
+    x, index, weight, w1, w2 = block_inputs(33)
+    junk = [torch.full((1 << 22,), math.nan, device=DEV, dtype=BF) for _ in range(4)]
+    del junk
+    offsets, place = layer.experts_sort(index, 8)
+    used = int(offsets[-1])
+    assert used < index.numel()
+    bias = torch.zeros(w1.shape[2], device=DEV, dtype=BF, requires_grad=True)
+    x.requires_grad_()
+    rows = layer.dispatch(x, place, offsets)
+    mid = layer.experts_product(rows, w1, offsets) + bias
+    assert not rows[used:].any() and torch.isfinite(mid).all()
+    y = layer.combine(layer.experts_product(mid.chunk(2, -1)[0].contiguous(), w2, offsets, transposed=True), place, offsets, weight)
+    dx, db = torch.autograd.grad(y, (x, bias), torch.ones_like(y))
+    assert torch.isfinite(dx).all() and torch.isfinite(db).all()
+
+
+def test_forms_are_captured_into_a_graph():
+    given = block_inputs(35)
+    x, index, weight, w1, w2 = given
+    leaves = [t.requires_grad_() for t in (x, weight, w1, w2)]
+    scale = normal(gen(36), x.shape[1]).requires_grad_()
+
+    def step():
+        h, total = layer.norm(x, scale, residual=x.detach())
+        grads = list(torch.autograd.grad((total + expert_block(h, index, weight, w1, w2)).float().square().mean(), [*leaves, scale]))
+        norm = layer.clip_gradients(grads, 0.5, work=work)
+        return [*grads, norm]
+    work = torch.zeros(layer.loco_gradient_squares_workspace_bytes(), dtype=torch.uint8, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for seed in (37, 38):
+        with torch.no_grad():
+            for t, n in zip(given, block_inputs(seed)):
+                t.copy_(n)
+        graph.replay()
+        assert all(torch.equal(a, b) and bool(a.any()) for a, b in zip(got, step()))
+
+
+def test_clip_gradients_in_place():
+    g = gen(41)
+    grads = [normal(g, 7, 11), normal(g, 1001, dtype=F32), normal(g, 3)]
+    kept = [t.clone() for t in grads]
+    n = math.sqrt(ref.squares(kept))
+    norm = layer.clip_gradients(grads, 2 * n)
+    assert abs(float(norm) - n) <= 6 * STEP * n and all(torch.equal(a, b) for a, b in zip(grads, kept))
+    layer.clip_gradients(grads, 0.25 * n)
+    for a, b in zip(grads, kept):
+        within(a, b.double() / 4, b.double().abs() / 4, 8, a.dtype)
+
+
+def test_clear_zeroes_what_lies_behind_the_last_row():
+    for dtype in (BF, F32):
+        for last, dim in ((0, 5), (3, 130), (7, 64), (9, 64), (-5, 7)):
+            rows = torch.full((7, dim + 3), 7.0, dtype=dtype, device=DEV)
+            layer.loco_experts_clear(rows[:, 1:1 + dim], torch.tensor([0, 0, last], dtype=torch.int32, device=DEV))
+            kept = min(max(last, 0), 7)
+            assert (rows[:kept] == 7.0).all() and not rows[kept:, 1:1 + dim].any() and (rows[:, 0] == 7.0).all() and (rows[:, 1 + dim:] == 7.0).all()
+
+
+def test_calls_from_a_thread_that_has_not_touched_the_device():
+    import threading
+    x, index, weight, w1, w2 = block_inputs(43)
+    want = expert_block(x, index, weight, w1, w2)
+    torch.cuda.synchronize()
+    got, failed = [], []
+
+    def run():
+        try:
+            got.append(expert_block(x, index, weight, w1, w2))
+            torch.cuda.synchronize()
+        except Exception as e:
+            failed.append(e)
+    t = threading.Thread(target=run)
+    t.start()
+    t.join()
+    assert not failed, failed
+    assert torch.equal(got[0], want)
