@@ -1,11 +1,13 @@
 // Sum of squares over a list of gradients, and the list scaled down to a largest norm.
 //
 // The list travels in the kernel's parameters.  It is cut into chunks; every block takes a run of consecutive chunks, finds
-// the first by bisection and walks on from there.  HBM bounds both passes.  The second walks the list backwards, from
+// the first by bisection and walks on from there.  HBM bounds both passes; the next chunks are on their way to shared memory
+// (cp.async, every thread its own vectors, so that no barrier is needed) while one is worked on.  The second walks the list backwards, from
 // what the first has read last, which L2 still holds; a list that fits there is read from HBM once.
 #include <type_traits>
 
 #include "layer_common.h"
+#include "layer_tc.cuh"
 
 namespace loco_layer {
 
@@ -13,9 +15,13 @@ constexpr int kListThreads = 512;
 constexpr int kMostSpans = 768;                  // of a launch: 21 KB of parameters
 constexpr int kFewSpans = 128;                   // 3.6 KB: a short list's launch costs less
 constexpr int kChunkBytes = 32768;
-constexpr int kAtOnce = kChunkBytes / 16 / kListThreads;             // vectors of a thread, asked for before it uses the first
+constexpr int kAtOnce = kChunkBytes / 16 / kListThreads;             // vectors of a thread
+constexpr int kAhead = 3;                        // chunks on their way, the one at work among them
+constexpr size_t kListShared = static_cast<size_t>(kAhead) * kChunkBytes;
 constexpr int kMostRuns = 4096;                  // blocks whose sums the workspace holds
-constexpr int kRunChunks = 8;
+// Chunks of a run: more blocks than run at once, of which the SMs that are nearer to memory take more, against what a block costs to
+// start.  842 million bfloat16 elements, runs of 8, 16, 32: squares 308, 307, 290 us, scaling 537, 544, 567.
+template <bool kClip> constexpr int kRunChunks = kClip ? 8 : 32;
 constexpr uint64_t kTicketBytes = 256;
 constexpr unsigned kAll = 0xffffffffu;
 
@@ -55,14 +61,41 @@ template <typename T> struct Piece {
     }
 };
 
+// Chunks on their way: [chunk][vector][thread] of shared memory.  What lies past a chunk's vectors reads as zeros.
+struct Ahead {
+    uint4 *const at;
+    int put = 0, got = 0;
+    __device__ __forceinline__ explicit Ahead(void *shared) : at(static_cast<uint4 *>(shared) + threadIdx.x) {}
+    __device__ __forceinline__ void send(const uint4 *from, int count) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = static_cast<int>(threadIdx.x) + u * kListThreads;
+            const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(at + (put * kAtOnce + u) * kListThreads));
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from + (i < count ? i : 0)), "r"(i < count ? 16 : 0) : "memory");
+        }
+        if (++put == kAhead) put = 0;
+    }
+    // Of the chunks sent (none, too, counts as one) the oldest is there.
+    __device__ __forceinline__ void wait() const { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory"); }
+    __device__ __forceinline__ static void sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    __device__ __forceinline__ uint4 operator[](int u) const { return at[(got * kAtOnce + u) * kListThreads]; }
+    __device__ __forceinline__ void next() {
+        if (++got == kAhead) got = 0;
+    }
+};
+
+template <typename T> __device__ __forceinline__ float element(const uint4 &v, int j) {
+    const uint32_t w = sizeof(T) == 2 ? (&v.x)[j / 2] : (&v.x)[j];
+    return sizeof(T) == 2 ? __uint_as_float(j % 2 ? w & 0xffff0000u : w << 16) : __uint_as_float(w);
+}
 // Sum of squares of a vector in fp32; `wide` is raised where that leaves the type's range (values above 1e19 or below 1e-15;
 // zeros, of which an idle expert's gradient consists, are told apart).
-template <typename Vec, int kV> __device__ __forceinline__ float squares_of(const Vec &v, bool &wide) {
+template <typename T> __device__ __forceinline__ float squares_of(const uint4 &v, bool &wide) {
     float s = 0.0f;
     bool some = false;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) {
-        const float f = to_f32(v.v[j]);
+    for (int j = 0; j < static_cast<int>(16 / sizeof(T)); ++j) {
+        const float f = element<T>(v, j);
         s = fmaf(f, f, s);
         some = some || f != 0.0f;
     }
@@ -71,76 +104,77 @@ template <typename Vec, int kV> __device__ __forceinline__ float squares_of(cons
 }
 template <typename T> __device__ __forceinline__ double square(T x) { return static_cast<double>(to_f32(x)) * static_cast<double>(to_f32(x)); }
 
-template <typename T> __device__ __forceinline__ double square_piece(const T *x, uint64_t n, uint32_t chunk, uint32_t chunks) {
-    using P = Piece<T>;
-    const P p(x, n, chunk, chunks);
-    const typename P::Vec *const from = reinterpret_cast<const typename P::Vec *>(x + p.at);
+template <typename T> __device__ __forceinline__ double square_piece(const T *x, const Piece<T> &p, const Ahead &ahead) {
     const int tid = threadIdx.x;
-    typename P::Vec v[kAtOnce];
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-        if (tid + u * kListThreads < p.count) v[u] = from[tid + u * kListThreads];
     double sum = 0.0;
     bool wide = false;
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-        if (tid + u * kListThreads < p.count) sum += static_cast<double>(squares_of<typename P::Vec, P::kV>(v[u], wide));
+    for (int u = 0; u < kAtOnce; ++u) sum += static_cast<double>(squares_of<T>(ahead[u], wide));
     if (wide) {                                  // once more, in 64 bits
         sum = 0.0;
 #pragma unroll 1
         for (int i = tid; i < p.count; i += kListThreads)
 #pragma unroll 1
-            for (int j = 0; j < P::kV; ++j) sum += square(x[p.at + static_cast<uint64_t>(i) * P::kV + j]);
+            for (int j = 0; j < Piece<T>::kV; ++j) sum += square(x[p.at + static_cast<uint64_t>(i) * Piece<T>::kV + j]);
     }
     if (tid < p.head) sum += square(x[tid]);
     if (tid < p.tail) sum += square(x[p.rest + tid]);
     return sum;
 }
 
-template <typename T> __device__ __forceinline__ void scale_piece(const T *x, T *y, uint64_t n, uint32_t chunk, uint32_t chunks, float by) {
-    using P = Piece<T>;
-    const P p(x, n, chunk, chunks);
+template <typename T> __device__ __forceinline__ void scale_piece(const T *x, T *y, const Piece<T> &p, const Ahead &ahead, float by) {
     const int tid = threadIdx.x;
     if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15u) == 0) {
-        const typename P::Vec *const from = reinterpret_cast<const typename P::Vec *>(x + p.at);
-        typename P::Vec *const to = reinterpret_cast<typename P::Vec *>(y + p.at);
-        typename P::Vec v[kAtOnce];
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
-            if (tid + u * kListThreads < p.count) v[u] = from[tid + u * kListThreads];
+        uint4 *const to = reinterpret_cast<uint4 *>(y + p.at);
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u)
             if (tid + u * kListThreads < p.count) {
+                uint4 v = ahead[u];
 #pragma unroll
-                for (int j = 0; j < P::kV; ++j) v[u].v[j] = from_f32<T>(to_f32(v[u].v[j]) * by);
-                to[tid + u * kListThreads] = v[u];
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t &w = (&v.x)[k];
+                    w = sizeof(T) == 2 ? tc::pack_bf16(__uint_as_float(w << 16) * by, __uint_as_float(w & 0xffff0000u) * by)
+                                       : __float_as_uint(__uint_as_float(w) * by);
+                }
+                to[tid + u * kListThreads] = v;
             }
     } else {                                     // the two do not meet 16-byte boundaries together
 #pragma unroll 4
-        for (int i = tid; i < p.count * P::kV; i += kListThreads) y[p.at + i] = from_f32<T>(to_f32(x[p.at + i]) * by);
+        for (int i = tid; i < p.count * Piece<T>::kV; i += kListThreads) y[p.at + i] = from_f32<T>(to_f32(x[p.at + i]) * by);
     }
     if (tid < p.head) y[tid] = from_f32<T>(to_f32(x[tid]) * by);
     if (tid < p.tail) y[p.rest + tid] = from_f32<T>(to_f32(x[p.rest + tid]) * by);
 }
 
-// A block's run of chunks, and the span that holds the first of them.
+// The block's run of chunks, and a place in it: a chunk and the span that holds it.
 template <int kMost> struct Run {
-    uint32_t at, until;
-    int span;
+    uint32_t first, until;
     __device__ __forceinline__ Run(const ListParams<kMost> &P, uint32_t which) {
-        at = static_cast<uint32_t>(static_cast<uint64_t>(P.chunks) * which / gridDim.x);
+        first = static_cast<uint32_t>(static_cast<uint64_t>(P.chunks) * which / gridDim.x);
         until = static_cast<uint32_t>(static_cast<uint64_t>(P.chunks) * (which + 1) / gridDim.x);
     }
-    __device__ __forceinline__ void find(const ListParams<kMost> &P, uint32_t chunk) {   // the last span that starts at or before it
-        int lo = 0, hi = P.count - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (P.first[mid] <= chunk) lo = mid;
-            else hi = mid - 1;
-        }
-        span = lo;
-    }
 };
+template <int kMost> __device__ __forceinline__ int span_of(const ListParams<kMost> &P, uint32_t chunk) {      // the last span that starts at or before it
+    int lo = 0, hi = P.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (P.first[mid] <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+template <typename T, int kMost> __device__ __forceinline__ Piece<T> piece_at(const ListParams<kMost> &P, int span, uint32_t chunk) {
+    return Piece<T>(P.x[span], P.n[span], chunk - P.first[span], P.first[span + 1] - P.first[span]);
+}
+template <int kMost> __device__ __forceinline__ void send_chunk(const ListParams<kMost> &P, int span, uint32_t chunk, Ahead &ahead) {
+    if (P.type[span] == LOCO_BF16) {
+        const Piece<__nv_bfloat16> p = piece_at<__nv_bfloat16>(P, span, chunk);
+        ahead.send(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(P.x[span]) + p.at), p.count);
+    } else {
+        const Piece<float> p = piece_at<float>(P, span, chunk);
+        ahead.send(reinterpret_cast<const uint4 *>(static_cast<const float *>(P.x[span]) + p.at), p.count);
+    }
+}
 
 // Adds the blocks' sums, in their order, when all are there; fp64 of the block's own sum in every thread of the first warp.
 template <int kMost> __global__ void __launch_bounds__(kListThreads, 2) gradient_squares_kernel(const __grid_constant__ ListParams<kMost> P) {
@@ -148,14 +182,27 @@ template <int kMost> __global__ void __launch_bounds__(kListThreads, 2) gradient
     let_next_start();
     __shared__ double fold[kListThreads / 32];
     __shared__ bool last;
-    Run<kMost> r(P, blockIdx.x);
+    extern __shared__ __align__(16) uint8_t shared[];
+    const Run<kMost> run(P, blockIdx.x);
+    Ahead ahead(shared);
     double sum = 0.0;
-    if (r.at < r.until) r.find(P, r.at);
-    for (; r.at < r.until; ++r.at) {
-        while (r.at >= P.first[r.span + 1]) ++r.span;
-        const uint32_t chunk = r.at - P.first[r.span], chunks = P.first[r.span + 1] - P.first[r.span];
-        if (P.type[r.span] == LOCO_BF16) sum += square_piece(static_cast<const __nv_bfloat16 *>(P.x[r.span]), P.n[r.span], chunk, chunks);
-        else sum += square_piece(static_cast<const float *>(P.x[r.span]), P.n[r.span], chunk, chunks);
+    int span = run.first < run.until ? span_of(P, run.first) : 0, next_span = span;
+    uint32_t next = run.first;
+    const auto send = [&] {
+        if (next < run.until) {
+            while (next >= P.first[next_span + 1]) ++next_span;
+            send_chunk(P, next_span, next++, ahead);
+        }
+        ahead.sent();
+    };
+    for (int i = 1; i < kAhead; ++i) send();
+    for (uint32_t c = run.first; c < run.until; ++c) {
+        while (c >= P.first[span + 1]) ++span;
+        send();
+        ahead.wait();
+        if (P.type[span] == LOCO_BF16) sum += square_piece(static_cast<const __nv_bfloat16 *>(P.x[span]), piece_at<__nv_bfloat16>(P, span, c), ahead);
+        else sum += square_piece(static_cast<const float *>(P.x[span]), piece_at<float>(P, span, c), ahead);
+        ahead.next();
     }
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
 #pragma unroll
@@ -199,16 +246,31 @@ template <int kMost> __global__ void __launch_bounds__(kListThreads, 2) gradient
     const double norm = sqrt(*P.in);
     if (P.begin && blockIdx.x == 0 && threadIdx.x == 0 && P.norm) *P.norm = static_cast<float>(norm);
     const float by = norm <= P.max_norm ? 1.0f : static_cast<float>(P.max_norm / norm);
-    Run<kMost> r(P, gridDim.x - 1 - blockIdx.x);
-    if (r.at >= r.until) return;
-    r.find(P, r.until - 1);
-    for (uint32_t c = r.until; c-- > r.at;) {
-        while (c < P.first[r.span]) --r.span;
-        if (by == 1.0f && P.x[r.span] == P.y[r.span]) continue;
-        const uint32_t chunk = c - P.first[r.span], chunks = P.first[r.span + 1] - P.first[r.span];
-        if (P.type[r.span] == LOCO_BF16)
-            scale_piece(static_cast<const __nv_bfloat16 *>(P.x[r.span]), static_cast<__nv_bfloat16 *>(P.y[r.span]), P.n[r.span], chunk, chunks, by);
-        else scale_piece(static_cast<const float *>(P.x[r.span]), static_cast<float *>(P.y[r.span]), P.n[r.span], chunk, chunks, by);
+    extern __shared__ __align__(16) uint8_t shared[];
+    const Run<kMost> run(P, gridDim.x - 1 - blockIdx.x);
+    if (run.first >= run.until) return;
+    Ahead ahead(shared);
+    int span = span_of(P, run.until - 1), next_span = span;
+    uint32_t next = run.until;
+    const auto kept = [&](int span) { return by == 1.0f && P.x[span] == P.y[span]; };
+    const auto send = [&] {
+        if (next > run.first) {
+            --next;
+            while (next < P.first[next_span]) --next_span;
+            if (!kept(next_span)) send_chunk(P, next_span, next, ahead);
+        }
+        ahead.sent();
+    };
+    for (int i = 1; i < kAhead; ++i) send();
+    for (uint32_t c = run.until; c-- > run.first;) {
+        while (c < P.first[span]) --span;
+        send();
+        if (kept(span)) continue;
+        ahead.wait();
+        if (P.type[span] == LOCO_BF16)
+            scale_piece(static_cast<const __nv_bfloat16 *>(P.x[span]), static_cast<__nv_bfloat16 *>(P.y[span]), piece_at<__nv_bfloat16>(P, span, c), ahead, by);
+        else scale_piece(static_cast<const float *>(P.x[span]), static_cast<float *>(P.y[span]), piece_at<float>(P, span, c), ahead, by);
+        ahead.next();
     }
 }
 
@@ -248,17 +310,34 @@ template <int kMost> int32_t fill_list(ListParams<kMost> &P, const loco_span_t *
     return at;
 }
 
+// Shared memory above the default limit, set once per device and kernel.
+template <int kMost, bool kClip> bool allow() {
+    static std::atomic<bool> set[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return false;
+    }
+    if (set[dev].load(std::memory_order_acquire)) return true;
+    const auto fn = kClip ? gradient_clip_kernel<kMost> : gradient_squares_kernel<kMost>;
+    if (cudaFuncSetAttribute(reinterpret_cast<const void *>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kListShared)) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    set[dev].store(true, std::memory_order_release);
+    return true;
+}
+
 // One launch for as many spans as fit, in order.
 template <int kMost, bool kClip> int launch_list(const loco_span_t *s, int32_t count, ListParams<kMost> &P, void *stream) {
     const int sms = sm_count();
-    if (sms == 0) return LOCO_ERR_CUDA;
+    if (sms == 0 || !allow<kMost, kClip>()) return LOCO_ERR_CUDA;
     int32_t at = 0;
     do {
         at = fill_list(P, s, count, at);
-        // runs of kRunChunks: more blocks than run at once, of which the SMs that are nearer to memory take more
-        const int64_t few = sms * 3, runs = P.chunks <= few ? P.chunks : P.chunks / kRunChunks < few ? few : P.chunks / kRunChunks;
+        const int64_t few = sms * 2, runs = P.chunks <= few ? P.chunks : P.chunks / kRunChunks<kClip> < few ? few : P.chunks / kRunChunks<kClip>;
         const unsigned blocks = runs < 1 ? 1 : runs > kMostRuns ? kMostRuns : static_cast<unsigned>(runs);
-        const int rc = launch_kernel(kClip ? gradient_clip_kernel<kMost> : gradient_squares_kernel<kMost>, dim3(blocks), kListThreads, 0, stream, P);
+        const int rc = launch_kernel(kClip ? gradient_clip_kernel<kMost> : gradient_squares_kernel<kMost>, dim3(blocks), kListThreads, kListShared, stream, P);
         if (rc != LOCO_OK) return rc;
     } while (at < count);
     return LOCO_OK;
