@@ -84,33 +84,38 @@ struct Ahead {
     }
 };
 
-template <typename T> __device__ __forceinline__ float element(const uint4 &v, int j) {
-    const uint32_t w = sizeof(T) == 2 ? (&v.x)[j / 2] : (&v.x)[j];
-    return sizeof(T) == 2 ? __uint_as_float(j % 2 ? w & 0xffff0000u : w << 16) : __uint_as_float(w);
-}
-// Sum of squares of a vector in fp32; `wide` is raised where that leaves the type's range (values above 1e19 or below 1e-15;
-// zeros, of which an idle expert's gradient consists, are told apart).
-template <typename T> __device__ __forceinline__ float squares_of(const uint4 &v, bool &wide) {
-    float s = 0.0f;
-    bool some = false;
+// Sum of squares of a vector in fp32, and whether there is anything in it but zeros.
+template <typename T> __device__ __forceinline__ float squares_of(const uint4 &v, bool &some) {
+    some = some || ((v.x | v.y | v.z | v.w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) != 0;
+    float2 s = make_float2(0.0f, 0.0f);
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int j = 0; j < static_cast<int>(16 / sizeof(T)); ++j) {
-        const float f = element<T>(v, j);
-        s = fmaf(f, f, s);
-        some = some || f != 0.0f;
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t w = (&v.x)[k];
+            const float2 f = make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+            s = tc::fma2(f, f, s);
+        }
+    } else {
+        const float2 f = make_float2(__uint_as_float(v.x), __uint_as_float(v.y)), g = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
+        s = tc::fma2(g, g, tc::mul2(f, f));
     }
-    wide = wide || (some && !(s > 1e-30f && s < 3e38f));
-    return s;
+    return s.x + s.y;
 }
 template <typename T> __device__ __forceinline__ double square(T x) { return static_cast<double>(to_f32(x)) * static_cast<double>(to_f32(x)); }
 
 template <typename T> __device__ __forceinline__ double square_piece(const T *x, const Piece<T> &p, const Ahead &ahead) {
     const int tid = threadIdx.x;
-    double sum = 0.0;
-    bool wide = false;
+    // A thread's 32 (fp32: 16) squares are added in fp32, seven roundings in a row at most, and only then in 64 bits: a conversion and an
+    // addition a vector kept the issue slots 78% busy.  Where the sum leaves fp32's range (values above 1e19 or below 1e-15) all
+    // of it is done in 64 bits; zeros, of which an idle expert's gradient consists, are told apart.
+    bool some = false;
+    float group[kAtOnce];
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) sum += static_cast<double>(squares_of<T>(ahead[u], wide));
-    if (wide) {                                  // once more, in 64 bits
+    for (int u = 0; u < kAtOnce; ++u) group[u] = squares_of<T>(ahead[u], some);
+    static_assert(kAtOnce == 4, "a tree of four");
+    const float all = (group[0] + group[1]) + (group[2] + group[3]);
+    double sum = static_cast<double>(all);
+    if (some && !(all > 1e-30f && all < 3e38f)) {
         sum = 0.0;
 #pragma unroll 1
         for (int i = tid; i < p.count; i += kListThreads)
