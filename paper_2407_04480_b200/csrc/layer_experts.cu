@@ -30,6 +30,7 @@ struct SortParams {
 
 // Counts of each warp's own run of choices, in shared memory.
 __device__ __forceinline__ void count_run(const SortParams &P, int *mine, int64_t from, int64_t until, int lane) {
+#pragma unroll 8
     for (int64_t i = from + lane; i < until; i += 32) {
         const int e = P.index[i];
         if (static_cast<unsigned>(e) < static_cast<unsigned>(P.experts)) atomicAdd(&mine[e], 1);
@@ -80,6 +81,7 @@ __global__ void __launch_bounds__(kSortThreads) experts_place_kernel(const SortP
     let_next_start();
     extern __shared__ int next[];                // [warp][expert]: counts, then the warp's next row of the expert
     __shared__ int fold[kSortWarps];
+    __shared__ int2 counted[kSortThreads];
     static_assert(kMostExperts <= kSortThreads, "one expert a thread");
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, E = P.experts, blocks = static_cast<int>(gridDim.x);
     for (int i = threadIdx.x; i < kSortWarps * E; i += kSortThreads) next[i] = 0;
@@ -90,17 +92,27 @@ __global__ void __launch_bounds__(kSortThreads) experts_place_kernel(const SortP
     __syncthreads();
     const int e = threadIdx.x;
     int all = 0, before = 0;                     // of the expert: choices of all blocks, of the blocks before this one
-    if (e < E) {
-        if (blocks == 1) {
+    if (blocks == 1) {
+        if (e < E)
             for (int w = 0; w < kSortWarps; ++w) all += next[w * E + e];
-        } else {
+    } else {                                     // the blocks' counts are dealt to as many threads for each expert as there are
+        const int parts = kSortThreads / E, part = e / E, mine = e % E;
+        if (part < parts) {
 #pragma unroll 8
-            for (int b = 0; b < blocks; ++b) {
-                const int n = __ldcg(P.counts + static_cast<int64_t>(b) * E + e);
+            for (int b = part; b < blocks; b += parts) {
+                const int n = __ldcg(P.counts + static_cast<int64_t>(b) * E + mine);
                 all += n;
                 before += b < static_cast<int>(blockIdx.x) ? n : 0;
             }
         }
+        counted[e] = make_int2(all, before);
+        __syncthreads();
+        all = before = 0;
+        if (e < E)
+            for (int p = 0; p < parts; ++p) {
+                all += counted[p * E + e].x;
+                before += counted[p * E + e].y;
+            }
     }
     int total;
     const int first = before_in_block(all, fold, total);
@@ -118,16 +130,22 @@ __global__ void __launch_bounds__(kSortThreads) experts_place_kernel(const SortP
     }
     __syncthreads();
     int *const mine = next + warp * E;
-    for (int64_t i = from; i < until; i += 32) {
-        const int64_t at = i + lane;
-        const int chosen = at < until ? P.index[at] : -1;
-        const bool some = static_cast<unsigned>(chosen) < static_cast<unsigned>(E);
-        const unsigned same = __match_any_sync(kAll, some ? chosen : -1);
-        const int row = some ? mine[chosen] : 0;
-        __syncwarp();
-        if (some && lane == __ffs(same) - 1) mine[chosen] = row + __popc(same);
-        __syncwarp();
-        if (at < until) P.place[at] = some ? row + __popc(same & ((1u << lane) - 1)) : -1;
+    constexpr int kAtOnce = 8;                   // of the warp's loads: one by one they are what a long run waits for
+    for (int64_t i = from; i < until; i += 32 * kAtOnce) {
+        int chosen[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) chosen[u] = i + u * 32 + lane < until ? P.index[i + u * 32 + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t at = i + u * 32 + lane;
+            const bool some = static_cast<unsigned>(chosen[u]) < static_cast<unsigned>(E);
+            const unsigned same = __match_any_sync(kAll, some ? chosen[u] : -1);
+            const int row = some ? mine[chosen[u]] : 0;
+            __syncwarp();
+            if (some && lane == __ffs(same) - 1) mine[chosen[u]] = row + __popc(same);
+            __syncwarp();
+            if (at < until) P.place[at] = some ? row + __popc(same & ((1u << lane) - 1)) : -1;
+        }
     }
 }
 
