@@ -345,6 +345,199 @@ __global__ void __launch_bounds__(kMoveThreads, kRows > 4 ? 3 : 4) experts_backw
     }
 }
 
+// ---- rows that do not share their 16-byte boundaries -----------------------------------------
+
+// Rows of an odd width lie each at a distance of its own from the boundaries.  What is written is then cut into the aligned vectors of
+// its own row, but for the ends; what is read comes as the two aligned vectors that hold its 16 bytes, slid together.  Every
+// tensor begins on a boundary.  In single elements 30,000 tokens of 1367, two choices, bfloat16, are laid out in 123 us.
+template <typename T> struct Slide {
+    static constexpr int kV = 16 / sizeof(T);
+    const T *row;
+    int64_t left;                                // elements from `row` to the end of the tensor
+    struct Two {
+        uint4 lo, hi;
+    };
+    __device__ __forceinline__ unsigned off(int c) const { return static_cast<unsigned>(reinterpret_cast<uintptr_t>(row + c)) & 15u; }
+    // The vectors that hold elements c .. c + kV - 1 of the row, all of them the row's.
+    __device__ __forceinline__ Two ask(int c) const {
+        const unsigned o = off(c);
+        const uint4 *const from = reinterpret_cast<const uint4 *>(reinterpret_cast<const uint8_t *>(row + c) - o);
+        Two t{from[0], make_uint4(0, 0, 0, 0)};
+        const int have = o / sizeof(T);          // elements in the second one
+        if (have && c + 2 * kV - have <= left) {
+            t.hi = from[1];
+        } else if (have) {                       // past the tensor's end there may be nothing: what is the row's, one by one
+#pragma unroll
+            for (int j = 0; j < kV; ++j)
+                if (j < have) {
+                    const T *const at = row + c + kV - have + j;
+                    const uint32_t bits = sizeof(T) == 2 ? *reinterpret_cast<const uint16_t *>(at) : *reinterpret_cast<const uint32_t *>(at);
+                    (&t.hi.x)[j * sizeof(T) / 4] |= bits << (j * sizeof(T) % 4 * 8);
+                }
+        }
+        return t;
+    }
+    __device__ __forceinline__ Pack<T, kV> join(const Two &t, int c) const {
+        const unsigned o = off(c);
+        uint32_t w[8] = {t.lo.x, t.lo.y, t.lo.z, t.lo.w, t.hi.x, t.hi.y, t.hi.z, t.hi.w};
+#pragma unroll
+        for (int k = 0; k < 6; ++k) w[k] = o & 8u ? w[k + 2] : w[k];
+#pragma unroll
+        for (int k = 0; k < 5; ++k) w[k] = o & 4u ? w[k + 1] : w[k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], o & 2u ? 16 : 0);
+        Pack<T, kV> v;
+        memcpy(&v, w, 16);
+        return v;
+    }
+};
+template <typename T> __device__ __forceinline__ Slide<T> slide(const void *base, int64_t row, int64_t stride, int64_t rows, int dim) {
+    return Slide<T>{static_cast<const T *>(base) + row * stride, (rows - 1 - row) * stride + dim};
+}
+// A row that is written: its vectors begin this many elements ahead of it.
+template <typename T> __device__ __forceinline__ int shift_of(const T *row) { return static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T)); }
+// The 16 bytes within the row that hold what vector c has of it: the vector itself, or at the row's ends the first or the last ones.
+template <int kV> __device__ __forceinline__ int within_row(int c, int dim) { return min(max(c, 0), dim - kV); }
+// Vector c of a row, of which `v` holds the elements from `at` on; element by element at the row's ends.
+template <typename T, int kV> __device__ __forceinline__ void put(T *row, int c, int at, int dim, const Pack<T, kV> &v) {
+    if (c == at) {
+        *reinterpret_cast<Pack<T, kV> *>(row + c) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kV; ++i)
+            if (at + i >= c && at + i < c + kV) row[at + i] = v.v[i];
+    }
+}
+
+// Both of a thread's vectors are asked for before the first is written: loads are not moved over stores.
+template <typename T> __global__ void __launch_bounds__(kMoveThreads) experts_dispatch_slide_kernel(const __grid_constant__ MoveParams P) {
+    wait_for_previous();
+    let_next_start();
+    constexpr int kV = 16 / sizeof(T);
+    const Seat s = seat(P.team);
+    if (s.token >= P.tokens) return;
+    const Slide<T> x = slide<T>(P.in, s.token, P.in_stride, P.tokens, P.dim);
+    const int step = P.team * kV;
+    for (int j = 0; j < P.top_k; ++j) {
+        const int p = __ldg(P.place + s.token * P.top_k + j);
+        if (p < 0 || p >= P.row_count) continue;
+        T *const row = static_cast<T *>(P.rows_out) + p * P.rows_out_stride;
+        for (int c0 = s.lane * kV - shift_of(row); c0 < P.dim; c0 += 2 * step) {
+            typename Slide<T>::Two t[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (c0 + u * step < P.dim) t[u] = x.ask(within_row<kV>(c0 + u * step, P.dim));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int c = c0 + u * step, at = within_row<kV>(c, P.dim);
+                if (c < P.dim) put<T, kV>(row, c, at, P.dim, x.join(t[u], at));
+            }
+        }
+    }
+}
+
+// kRows choices at a time, all asked for before the first is used.
+template <typename T, int kRows> __global__ void __launch_bounds__(kMoveThreads, 4) experts_combine_slide_kernel(const __grid_constant__ MoveParams P) {
+    wait_for_previous();
+    let_next_start();
+    constexpr int kV = 16 / sizeof(T);
+    const Seat s = seat(P.team);
+    if (s.token >= P.tokens) return;
+    T *const y = static_cast<T *>(P.out) + s.token * P.out_stride;
+#pragma unroll 1
+    for (int c = s.lane * kV - shift_of(y); c < P.dim; c += P.team * kV) {
+        const int at = within_row<kV>(c, P.dim);
+        float2 sum[kV / 2];
+#pragma unroll
+        for (int q = 0; q < kV / 2; ++q) sum[q] = make_float2(0.0f, 0.0f);
+#pragma unroll 1
+        for (int j0 = 0; j0 < P.top_k; j0 += kRows) {
+            int p[kRows];
+            float w[kRows];
+            choices_at<kRows>(P, s.token, j0, p, w);
+            typename Slide<T>::Two t[kRows];
+#pragma unroll
+            for (int j = 0; j < kRows; ++j)
+                if (p[j] >= 0) t[j] = slide<T>(P.rows, p[j], P.rows_stride, P.row_count, P.dim).ask(at);
+#pragma unroll
+            for (int j = 0; j < kRows; ++j)
+                if (p[j] >= 0) {
+                    const Pack<T, kV> v = slide<T>(P.rows, p[j], P.rows_stride, P.row_count, P.dim).join(t[j], at);
+#pragma unroll
+                    for (int q = 0; q < kV / 2; ++q) sum[q] = fma2(make_float2(w[j], w[j]), pair_of(v, q), sum[q]);
+                }
+        }
+        Pack<T, kV> out;
+#pragma unroll
+        for (int q = 0; q < kV / 2; ++q) set_pair(out, q, sum[q]);
+        put<T, kV>(y, c, at, P.dim, out);
+    }
+}
+
+// One choice after the other, each in its own row's vectors, two at a time.
+template <typename T> __global__ void __launch_bounds__(kMoveThreads, 4) experts_backward_slide_kernel(const __grid_constant__ MoveParams P) {
+    wait_for_previous();
+    let_next_start();
+    constexpr int kV = 16 / sizeof(T);
+    __shared__ float fold[2][kMoveThreads / 32];
+    const Seat s = seat(P.team);
+    const bool there = s.token < P.tokens;
+    const int64_t token = there ? s.token : 0;
+    const Slide<T> dy = slide<T>(P.in, token, P.in_stride, P.tokens, P.dim);
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, width = P.team < 32 ? P.team : 32, step = P.team * kV;
+#pragma unroll 1
+    for (int j = 0; j < P.top_k; ++j) {
+        const int place = there ? __ldg(P.place + token * P.top_k + j) : -1, p = place < P.row_count ? place : -1;
+        float dot = 0.0f;
+        if (p >= 0) {
+            const float w = __ldg(P.weight + token * P.top_k + j);
+            const Slide<T> r = slide<T>(P.rows, p, P.rows_stride, P.row_count, P.dim);
+            T *const row = static_cast<T *>(P.rows_out) + p * P.rows_out_stride;
+#pragma unroll 1
+            for (int c0 = s.lane * kV - shift_of(row); c0 < P.dim; c0 += 2 * step) {
+                typename Slide<T>::Two a[2], b[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (c0 + u * step < P.dim) {
+                        const int at = within_row<kV>(c0 + u * step, P.dim);
+                        a[u] = dy.ask(at);
+                        b[u] = r.ask(at);
+                    }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int c = c0 + u * step, at = within_row<kV>(c, P.dim);
+                    if (c < P.dim) {
+                        const Pack<T, kV> d = dy.join(a[u], at), f = r.join(b[u], at);
+                        Pack<T, kV> out;
+                        const int from = max(c, 0) - at, until = min(c + kV, P.dim) - at;      // what of it is this vector's
+#pragma unroll
+                        for (int q = 0; q < kV / 2; ++q) {
+                            const float2 x = pair_of(d, q), y = pair_of(f, q);
+                            dot = 2 * q >= from && 2 * q < until ? fmaf(x.x, y.x, dot) : dot;
+                            dot = 2 * q + 1 >= from && 2 * q + 1 < until ? fmaf(x.y, y.y, dot) : dot;
+                            set_pair(out, q, mul2(make_float2(w, w), x));
+                        }
+                        put<T, kV>(row, c, at, P.dim, out);
+                    }
+                }
+            }
+        }
+        for (int o = width / 2; o; o >>= 1) dot += __shfl_xor_sync(kAll, dot, o);
+        float *const dw = P.dweight + token * P.top_k + j;
+        if (P.team <= 32) {
+            if (there && s.lane == 0) *dw = dot;
+        } else {                                     // two sides: the next choice's sums go to the other
+            if (lane == 0) fold[j & 1][warp] = dot;
+            __syncthreads();
+            if (there && s.lane == 0) {
+                dot = 0.0f;
+                for (int i = 0; i < P.team / 32; ++i) dot += fold[j & 1][warp + i];
+                *dw = dot;
+            }
+        }
+    }
+}
+
 // Rows from the last offset on: nothing to write, as a rule.
 template <typename T> __global__ void __launch_bounds__(kMoveThreads) experts_clear_kernel(T *rows, int64_t stride, int64_t count, int dim, const int32_t *last) {
     wait_for_previous();
@@ -367,6 +560,10 @@ template <typename T, int V> MoveKernel pick_move(Move m, int k, int places) {
     return k <= 2 ? experts_backward_kernel<T, V, 2, 2> : k <= 4 ? experts_backward_kernel<T, V, 4, 1> : experts_backward_kernel<T, V, 8, 1>;
 }
 
+template <typename T> MoveKernel pick_slide(Move m) {
+    return m == kDispatch ? experts_dispatch_slide_kernel<T> : m == kCombine ? experts_combine_slide_kernel<T, 4> : experts_backward_slide_kernel<T>;
+}
+
 int check_experts(const loco_experts_t *c) {
     if (!c) return LOCO_ERR_ARG;
     if (c->dtype != LOCO_F32 && c->dtype != LOCO_BF16) return LOCO_ERR_ARG;
@@ -375,36 +572,48 @@ int check_experts(const loco_experts_t *c) {
     return LOCO_OK;
 }
 
-// A tensor of rows: present, aligned to its elements; an output's rows do not overlap.  Narrows `vec` to what its rows allow.
-int take_rows(const loco_experts_t *c, const loco_rows_t *t, int64_t rows, bool written, int &vec, int64_t &stride) {
+// What the accesses of a call can be: all rows on 16-byte boundaries, or on those of four, or every tensor on the former at least.
+struct Vectors {
+    bool rows = true, words = true, tensors = true;
+};
+// A tensor of rows: present, aligned to its elements; an output's rows do not overlap.
+int take_rows(const loco_experts_t *c, const loco_rows_t *t, int64_t rows, bool written, Vectors &V, int64_t &stride) {
     if (!t) return LOCO_ERR_ARG;
     stride = rows > 1 ? t->row_stride : 0;
     if (rows == 0) return LOCO_OK;
     const int size = c->dtype == LOCO_BF16 ? 2 : 4;
     if (!t->ptr || stride < 0 || (written && rows > 1 && stride < c->dim)) return LOCO_ERR_ARG;
     if (!aligned(t->ptr, static_cast<uintptr_t>(size))) return LOCO_ERR_ALIGN;
-    while (vec > 1 && (!aligned(t->ptr, static_cast<uintptr_t>(vec * size)) || stride % vec != 0 || c->dim % vec != 0)) vec /= 2;
+    V.tensors = V.tensors && aligned(t->ptr, 16);
+    V.rows = V.rows && V.tensors && stride * size % 16 == 0 && c->dim * size % 16 == 0;
+    V.words = V.words && aligned(t->ptr, 4) && stride * size % 4 == 0 && c->dim * size % 4 == 0;
     return LOCO_OK;
 }
 
-int launch_move(Move m, MoveParams &P, const loco_experts_t *c, int vec, void *stream) {
+int launch_move(Move m, MoveParams &P, const loco_experts_t *c, const Vectors &V, void *stream) {
     P.tokens = c->tokens;
     P.row_count = c->rows;
     P.dim = c->dim;
     P.top_k = c->top_k;
-    const int v = c->dtype == LOCO_BF16 ? (vec >= 8 ? 8 : vec >= 2 ? 2 : 1) : vec >= 4 ? 4 : 1, k = c->top_k;
+    // Off the boundaries rows are slid together, but for a sum of up to four: in words or elements, sliding, bfloat16, 30,000 x 1367, two
+    // choices: laid out 123, 64 us, summed 69, 89; 20,000 x 1004, four: 52, 44 and 53, 57; 9000 x 1367, six, backward 166, 132, summed 162, 54.
+    const bool bf16 = c->dtype == LOCO_BF16;
+    const int k = c->top_k;
+    const bool slides = V.tensors && !V.rows && c->dim >= (bf16 ? 8 : 4) && (m != kCombine || k > 4);
+    const int v = slides || V.rows ? (bf16 ? 8 : 4) : bf16 && V.words ? 2 : 1;
     // places in a row that a thread takes at once
-    const int places = m == kCombine && k <= 2 ? (v > 1 && c->dim >= 128 * v ? 4 : 2) : (m == kCombine && k <= 4) || (m == kBackward && k <= 2) ? 2 : 1;
-    const MoveKernel fn = c->dtype == LOCO_BF16 ? (v == 8   ? pick_move<__nv_bfloat16, 8>(m, k, places)
-                                                   : v == 2 ? pick_move<__nv_bfloat16, 2>(m, k, places)
-                                                            : pick_move<__nv_bfloat16, 1>(m, k, places))
-                                                : (v == 4 ? pick_move<float, 4>(m, k, places) : pick_move<float, 1>(m, k, places));
+    const int places = slides ? (m == kCombine ? 1 : 2) : m == kCombine && k <= 2 ? (v > 1 && c->dim >= 128 * v ? 4 : 2) : (m == kCombine && k <= 4) || (m == kBackward && k <= 2) ? 2 : 1;
+    const MoveKernel fn = slides ? (bf16 ? pick_slide<__nv_bfloat16>(m) : pick_slide<float>(m))
+                          : bf16 ? (v == 8   ? pick_move<__nv_bfloat16, 8>(m, k, places)
+                                    : v == 2 ? pick_move<__nv_bfloat16, 2>(m, k, places)
+                                             : pick_move<__nv_bfloat16, 1>(m, k, places))
+                                 : (v == 4 ? pick_move<float, 4>(m, k, places) : pick_move<float, 1>(m, k, places));
     const int least = m == kBackward && k > 4 ? 8 : 4;               // lanes that end with a choice's sum each
     int team = least;
     while (team < kMoveThreads && team * places * v < c->dim) team *= 2;
     // With enough tokens a thread goes round twice (four times over single elements), so that the wait for the places and the sums over
     // the team come to less: 5021 x 2040, six choices, backward once, twice, four times: 46.6, 42.4, 41.3 us, combine 29.1, 28.3, 31.4.
-    if (m == kBackward || (m == kCombine && (k > 2 || v == 1)))
+    if (!slides && (m == kBackward || (m == kCombine && (k > 2 || v == 1))))
         for (int turns = 1; turns < (v == 1 ? 4 : 2) && team > 32 && c->tokens * (team / 2) >= sm_count() * 2048ll; turns *= 2) team /= 2;
     P.team = team;
     const int64_t blocks = (c->tokens + kMoveThreads / team - 1) / (kMoveThreads / team);
@@ -459,9 +668,9 @@ int loco_experts_clear(int32_t dtype, int32_t dim, int64_t rows_count, const loc
     int rc = check_experts(&c);
     if (rc != LOCO_OK) return rc;
     if (experts < 1 || experts > kMostExperts || !d_offsets) return LOCO_ERR_ARG;
-    int vec = 1;
+    Vectors V;
     int64_t stride;
-    if ((rc = take_rows(&c, rows, rows_count, true, vec, stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(&c, rows, rows_count, true, V, stride)) != LOCO_OK) return rc;
     if (!aligned(d_offsets, 4)) return LOCO_ERR_ALIGN;
     if (rows_count == 0) return LOCO_OK;
     const int sms = sm_count();
@@ -476,14 +685,14 @@ int loco_experts_dispatch(const loco_experts_t *c, const loco_rows_t *x, const i
     int rc = start(c, d_place, nullptr);
     if (rc != LOCO_OK || c->tokens == 0) return rc;
     MoveParams P{};
-    int vec = c->dtype == LOCO_BF16 ? 8 : 4;
-    if ((rc = take_rows(c, x, c->tokens, false, vec, P.in_stride)) != LOCO_OK) return rc;
-    if ((rc = take_rows(c, rows, c->rows, true, vec, P.rows_out_stride)) != LOCO_OK) return rc;
+    Vectors V;
+    if ((rc = take_rows(c, x, c->tokens, false, V, P.in_stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(c, rows, c->rows, true, V, P.rows_out_stride)) != LOCO_OK) return rc;
     if (c->rows == 0) return LOCO_OK;
     P.in = x->ptr;
     P.rows_out = rows->ptr;
     P.place = d_place;
-    return launch_move(kDispatch, P, c, vec, stream);
+    return launch_move(kDispatch, P, c, V, stream);
 }
 
 int loco_experts_combine(const loco_experts_t *c, const loco_rows_t *rows, const int32_t *d_place, const float *d_weight,
@@ -491,14 +700,14 @@ int loco_experts_combine(const loco_experts_t *c, const loco_rows_t *rows, const
     int rc = start(c, d_place, d_weight);
     if (rc != LOCO_OK || c->tokens == 0) return rc;
     MoveParams P{};
-    int vec = c->dtype == LOCO_BF16 ? 8 : 4;
-    if ((rc = take_rows(c, rows, c->rows, false, vec, P.rows_stride)) != LOCO_OK) return rc;
-    if ((rc = take_rows(c, y, c->tokens, true, vec, P.out_stride)) != LOCO_OK) return rc;
+    Vectors V;
+    if ((rc = take_rows(c, rows, c->rows, false, V, P.rows_stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(c, y, c->tokens, true, V, P.out_stride)) != LOCO_OK) return rc;
     P.rows = rows->ptr;
     P.out = y->ptr;
     P.place = d_place;
     P.weight = d_weight;
-    return launch_move(kCombine, P, c, vec, stream);
+    return launch_move(kCombine, P, c, V, stream);
 }
 
 int loco_experts_combine_backward(const loco_experts_t *c, const loco_rows_t *dy, const loco_rows_t *rows, const int32_t *d_place,
@@ -508,17 +717,17 @@ int loco_experts_combine_backward(const loco_experts_t *c, const loco_rows_t *dy
     if (!d_weight || !d_dweight) return LOCO_ERR_ARG;
     if (!aligned(d_dweight, 4)) return LOCO_ERR_ALIGN;
     MoveParams P{};
-    int vec = c->dtype == LOCO_BF16 ? 8 : 4;
-    if ((rc = take_rows(c, dy, c->tokens, false, vec, P.in_stride)) != LOCO_OK) return rc;
-    if ((rc = take_rows(c, rows, c->rows, false, vec, P.rows_stride)) != LOCO_OK) return rc;
-    if ((rc = take_rows(c, drows, c->rows, true, vec, P.rows_out_stride)) != LOCO_OK) return rc;
+    Vectors V;
+    if ((rc = take_rows(c, dy, c->tokens, false, V, P.in_stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(c, rows, c->rows, false, V, P.rows_stride)) != LOCO_OK) return rc;
+    if ((rc = take_rows(c, drows, c->rows, true, V, P.rows_out_stride)) != LOCO_OK) return rc;
     P.in = dy->ptr;
     P.rows = rows->ptr;
     P.rows_out = drows->ptr;
     P.place = d_place;
     P.weight = d_weight;
     P.dweight = d_dweight;
-    return launch_move(kBackward, P, c, vec, stream);
+    return launch_move(kBackward, P, c, V, stream);
 }
 
 }  // extern "C"
