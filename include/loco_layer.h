@@ -174,6 +174,7 @@ int loco_router_backward(const loco_router_t *cfg, int64_t tokens, const void *d
  *   h = x + residual, rounded to the type of x (no residual: h = x)
  *   r = 1 / sqrt(mean_i h_i^2 + eps)         y_i = h_i r w_i   (no weight: w = 1)
  *   8 bits: per row, or per run of `block` columns of a row,  scale = max(max_i |y_i| / 448, 2^-126),  y_i / scale as e4m3
+ *   (y_i not rounded before; the weight times h_i has to stay within fp32)
  *   backward, from h:  g = dy w,  n = h r:   dx = r (g - n mean(g n)) + dtotal,   dw = sum over rows of dy n
  * dx is the gradient of x and of the residual alike; dtotal is the one that reaches h past the norm.  Through the 8-bit
  * output it is passed as if nothing had been rounded.  The norm is that of h as it is kept, so that y of a kept h has the

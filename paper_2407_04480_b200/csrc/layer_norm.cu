@@ -93,10 +93,34 @@ __device__ __forceinline__ unsigned team_max(unsigned m, const Team &t, unsigned
     }
     return m;
 }
-__device__ __forceinline__ float scale_of(unsigned largest) {
-    const float m = __uint_as_float(largest);
-    return m != m ? m : fmaxf(m / kLargestE4m3, kLeastScale);
-}
+// An 8-bit scale from the largest |h w| of its columns and the row's r: max |y| / 448.  y / scale is then (h w) (448 / max |h w|), r
+// leaves it, and h w of bfloat16 is exact in fp32: with 448 / max in two fp32 (`over`, `rest`) the value is rounded once before it
+// is rounded to 8 bits, and falls on the wrong side of a step where the exact one is within 2^-24 of it.
+struct Scale {
+    float scale, over, rest;
+    bool least;                                  // the scale is its least value: y first, over it then
+    __device__ __forceinline__ Scale(unsigned largest, float r) {
+        const float m = __uint_as_float(largest), s = m * r / kLargestE4m3;
+        least = !(s > kLeastScale);
+        if (!least) {
+            scale = s;
+            over = kLargestE4m3 / m;
+            rest = fmaf(-over, m, kLargestE4m3) / m;
+        } else {                                 // nothing there, or NaN
+            scale = s != s ? s : kLeastScale;
+            over = r;
+            rest = 0.0f;
+        }
+    }
+    // y / scale; fp32: what h w was rounded by is taken along
+    template <typename T> __device__ __forceinline__ float2 apply(float2 h, float2 w) const {
+        const float2 p = tc::mul2(h, w), o = make_float2(over, over);
+        float2 low = tc::mul2(p, make_float2(rest, rest));
+        if constexpr (sizeof(T) == 4) low = tc::fma2(tc::fma2(h, w, make_float2(-p.x, -p.y)), o, low);
+        const float2 f = tc::fma2(p, o, low);
+        return least ? tc::mul2(f, make_float2(1.0f / kLeastScale, 1.0f / kLeastScale)) : f;
+    }
+};
 
 // A thread's part of a row: kMine elements in vectors of V, dealt to the team in turn.  Vectors lie on the tensors' 16-byte
 // boundaries, so that rows of any width are read and written in whole vectors but for the two that hold a row's ends (kShift;
@@ -236,6 +260,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid
     using Row = Part<T, V, kMine, kShift>;
     extern __shared__ __align__(16) uint8_t shared[];
     __shared__ float2 fold[kNormThreads / 32];
+    __shared__ unsigned tops[kBits8 ? kNormThreads / 32 : 1];        // not `fold`, which another team may be at
     __shared__ unsigned most[kBits8 ? 256 : 1];  // a row's or several rows' runs of 128 columns: threads * kMine / 128 of them at most
     const Team t(P, V);
     Ring<T, V, kMine, kShift, 2> ring(shared, P.depth);
@@ -290,14 +315,17 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid
             for (int q = 0; q < Row::kPairs; ++q) h.set(q, tc::mul2(tc::mul2(h[q], both(by)), w[q]));
             if (there) h.store(row_at<T>(P.y, row, P.ys), t, P.dim);
         } else {
-            const auto y = [&](int q) { return tc::mul2(tc::mul2(h[q], both(by)), w[q]); };
+            const auto y = [&](int q) { return tc::mul2(h[q], w[q]); };          // but for r
             uint32_t out[kMine / 4];             // a byte an element
+            const auto pack = [&](int q, float2 f) {
+                const uint32_t e = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+                out[q / 2] = q % 2 ? out[q / 2] | e << 16 : e;
+            };
             // the largest of the row, or of each run of 128 columns: 16 lanes' vectors where rows begin on the boundaries
             constexpr bool kLanes = V == 8 && !kShift;
             const bool lanes = kLanes && t.size >= 32;
             if (P.block == 0 || lanes) {
                 unsigned m[Row::kVecs], all = 0;
-                float over[Row::kVecs];          // one over the scale
 #pragma unroll
                 for (int i = 0; i < Row::kVecs; ++i) {
                     float x = 0.0f;                                  // NaN where one is
@@ -316,26 +344,20 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid
                 if (P.block == 0) {
 #pragma unroll
                     for (int i = 0; i < Row::kVecs; ++i) all = max(all, m[i]);
-                    all = team_max(all, t, reinterpret_cast<unsigned *>(fold));
-                    const float s = scale_of(all);
-                    if (there && t.lane == 0) P.scale[row] = s;
+                    const Scale s(team_max(all, t, tops), by);
+                    if (there && t.lane == 0) P.scale[row] = s.scale;
 #pragma unroll
-                    for (int i = 0; i < Row::kVecs; ++i) over[i] = 1.0f / s;
-                } else {
+                    for (int q = 0; q < Row::kPairs; ++q) pack(q, s.apply<T>(h[q], w[q]));
+                } else if constexpr (kLanes) {
 #pragma unroll
                     for (int i = 0; i < Row::kVecs; ++i) {
 #pragma unroll
                         for (int o = 8; o; o >>= 1) m[i] = max(m[i], __shfl_xor_sync(kAll, m[i], o));
-                        const float s = scale_of(m[i]);
-                        over[i] = 1.0f / s;
-                        if (there && threadIdx.x % 16 == 0 && Row::inside(t, i, P.dim)) P.scale[row * P.groups + Row::column(t, i) / kScaleBlock] = s;
-                    }
-                }
+                        const Scale s(m[i], by);
+                        if (there && threadIdx.x % 16 == 0 && Row::inside(t, i, P.dim)) P.scale[row * P.groups + Row::column(t, i) / kScaleBlock] = s.scale;
 #pragma unroll
-                for (int q = 0; q < Row::kPairs; ++q) {
-                    const float2 f = y(q);
-                    const uint32_t e = __nv_cvt_float2_to_fp8x2(make_float2(f.x * over[2 * q / V], f.y * over[(2 * q + 1) / V]), __NV_SATFINITE, __NV_E4M3);
-                    out[q / 2] = q % 2 ? out[q / 2] | e << 16 : e;
+                        for (int q = i * V / 2; q < (i + 1) * V / 2; ++q) pack(q, s.apply<T>(h[q], w[q]));
+                    }
                 }
             } else {
                 unsigned *const mine = most + t.mine * P.groups;
@@ -350,13 +372,11 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid
                     atomicMax(&mine[run((2 * q + 1) / V, (2 * q + 1) % V)], __float_as_uint(f.y) & 0x7fffffffu);
                 }
                 t.sync();
-                for (int i = t.lane; i < P.groups && there; i += t.size) P.scale[row * P.groups + i] = scale_of(mine[i]);
+                for (int i = t.lane; i < P.groups && there; i += t.size) P.scale[row * P.groups + i] = Scale(mine[i], by).scale;
 #pragma unroll
                 for (int q = 0; q < Row::kPairs; ++q) {
-                    const float2 f = y(q);
-                    const float a = scale_of(mine[run(2 * q / V, 2 * q % V)]), b = scale_of(mine[run((2 * q + 1) / V, (2 * q + 1) % V)]);
-                    const uint32_t e = __nv_cvt_float2_to_fp8x2(make_float2(f.x / a, f.y / b), __NV_SATFINITE, __NV_E4M3);
-                    out[q / 2] = q % 2 ? out[q / 2] | e << 16 : e;
+                    const Scale a(mine[run(2 * q / V, 2 * q % V)], by), b(mine[run((2 * q + 1) / V, (2 * q + 1) % V)], by);
+                    pack(q, make_float2(a.apply<T>(h[q], w[q]).x, b.apply<T>(h[q], w[q]).y));
                 }
             }
             if (there) {

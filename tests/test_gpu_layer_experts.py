@@ -40,7 +40,9 @@ def within(got, want, terms, additions, dtype):
 # a chain of 32 elements a thread, five steps of a warp, sixteen warps: 53 additions in a row; then a root, products
 NORM_ADDITIONS = 64
 NORM_SHAPES = [(1, 1), (1, 8), (3, 7), (5, 64), (70, 76), (9, 512), (33, 513), (4, 1367), (130, 1032), (2, 4096), (3, 5120), (2, 8192), (3, 8200),
-               (2, 16384), (2, 16383), (0, 64), (700, 128)]
+               (2, 16384), (2, 16383), (0, 64), (700, 128),
+               (3000, 513), (2500, 1367), (1300, 2040), (700, 4096), (9000, 72),      # several teams of threads to a block,
+               (60000, 40), (20011, 129), (5000, 1024)]                               # and several rows one after the other to a team
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -83,6 +85,21 @@ def test_norm_in_8_bits(rows, dim, dtype, block):
     room = q.abs() * (2.0 ** -4 + (2 * NORM_ADDITIONS + 4) * STEP) + 2.0 ** -10
     assert bool(((y.double() - q).abs() <= room).all())
     assert float(y.float().abs().max()) <= 448.0
+
+
+@pytest.mark.parametrize("block", [0, 128])
+@pytest.mark.parametrize("size", [1e-37, 1e-30, 1e-3, 1e18])
+def test_norm_in_8_bits_of_small_and_large_weights(block, size):
+    """Below 448 * 2^-126 the scale is its least value; nothing overflows on the way.  Values that fp32 holds as subnormals are off
+    by 2^-150, which over 2^-126 is less than the 8 bits' least half step."""
+    g = gen(12)
+    x, w = normal(g, 5, 300, dtype=F32), normal(g, 300, dtype=F32, sigma=size)
+    y, scale = torch.empty(5, 300, dtype=E4M3, device=DEV), torch.empty(5, -(-300 // block) if block else 1, device=DEV)
+    layer.loco_norm_forward(x, y, weight=w, scale=scale, block=block)
+    s, q = ref.e4m3(ref.norm(x, w, 1e-5)[0], block)
+    assert float(((scale.double() - s).abs() / s).max()) <= (NORM_ADDITIONS + 2) * STEP
+    room = q.abs() * (2.0 ** -4 + (2 * NORM_ADDITIONS + 4) * STEP) + 2.0 ** -10
+    assert bool(((y.double() - q).abs() <= room).all())
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -160,6 +177,53 @@ def test_norm_strides_alignment_and_places(dtype, dim):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,dim", [(3000, 200), (2500, 700), (1000, 2100)])
+def test_norm_of_many_rows_that_share_no_boundaries(rows, dim, dtype):
+    """In single elements: a base off the boundaries, widths of their own."""
+    g = gen(dim)
+    x, r, dy = (normal(g, rows, dim + k, dtype=dtype)[:, k:] for k in (1, 3, 5))
+    w = normal(g, dim + 1, dtype=dtype)[1:]
+    y, h = torch.empty(rows, dim, dtype=dtype, device=DEV), torch.empty(rows, dim, dtype=dtype, device=DEV)
+    layer.loco_norm_forward(x, y, weight=w, residual=r, total=h)
+    assert torch.equal(h, (x.double() + r.double()).to(dtype))
+    want, _ = ref.norm(h, w, 1e-5)
+    within(y, want, want.abs(), NORM_ADDITIONS, dtype)
+    for block in (0, 128):
+        q, scale = torch.empty(rows, dim, dtype=E4M3, device=DEV), torch.empty(rows, -(-dim // block) if block else 1, device=DEV)
+        layer.loco_norm_forward(h[:, :], q, weight=w, scale=scale, block=block)
+        s, exact = ref.e4m3(want, block)
+        assert float(((scale.double() - s).abs() / s).max()) <= (NORM_ADDITIONS + 2) * STEP
+        assert bool(((q.double() - exact).abs() <= exact.abs() * (2.0 ** -4 + (2 * NORM_ADDITIONS + 4) * STEP) + 2.0 ** -10).all())
+    dx, dw = torch.empty_like(y), torch.empty_like(w)
+    layer.loco_norm_backward(h, dy, dx, torch.empty(layer.loco_norm_backward_workspace_bytes(dim, dtype), dtype=torch.uint8, device=DEV), weight=w, dweight=dw, dtotal=r)
+    want, terms, gw, gterms = ref.norm_gradient(h, dy, w, r, 1e-5)
+    within(dx, want, terms, 3 * NORM_ADDITIONS, dtype)
+    within(dw, gw, gterms, rows + NORM_ADDITIONS, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("k,dim", [(2, 200), (6, 130), (3, 1001)])
+def test_moves_of_rows_that_share_no_boundaries(k, dim, dtype):
+    g = gen(dim)
+    t, e = 3000, 8
+    _, place = sorted_by(choices(g, t, k, e, "holes"), e)
+    x, back, weight = normal(g, t, dim + 1, dtype=dtype)[:, 1:], normal(g, t * k, dim + 3, dtype=dtype)[:, 3:], torch.rand(t, k, generator=g, device=DEV)
+    rows = torch.full((t * k, dim + 1), 7.0, dtype=dtype, device=DEV)[:, 1:]
+    layer.loco_experts_dispatch(x, place, rows)
+    some = place >= 0
+    assert torch.equal(rows[place[some].long()], x[torch.arange(t, device=DEV)[:, None].expand(-1, k)[some]])
+    y = torch.empty(t, dim + 1, dtype=dtype, device=DEV)[:, 1:]
+    layer.loco_experts_combine(back, place, y, weight=weight)
+    want, terms = ref.combine(back, place, weight)
+    within(y, want, terms, k + 1, dtype)
+    dweight = torch.empty(t, k, device=DEV)
+    layer.loco_experts_combine_backward(x, back, place, weight, rows, dweight)
+    want, live, dw, terms = ref.combine_gradient(x, back, place, weight)
+    within(rows[live], want[live], want[live].abs(), 1, dtype)
+    within(dweight, dw, terms, dim // 4 + 16, F32)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_norm_of_values_that_are_not_finite(dtype):
     """They reach their own row only; in 8 bits the scale says so."""
     g = gen(9)
@@ -205,7 +269,8 @@ def test_sort(tokens, k, experts, how):
     assert torch.equal(offsets.cpu(), first) and torch.equal(place.cpu(), want)
 
 
-MOVES = [(1, 1, 1, 8), (9, 2, 8, 4096), (70, 2, 4, 76), (33, 6, 160, 2040), (51, 16, 64, 100), (40, 3, 8, 7), (300, 4, 8, 64), (5, 8, 16, 5121), (2, 2, 4, 1)]
+MOVES = [(1, 1, 1, 8), (9, 2, 8, 4096), (70, 2, 4, 76), (33, 6, 160, 2040), (51, 16, 64, 100), (40, 3, 8, 7), (300, 4, 8, 64), (5, 8, 16, 5121), (2, 2, 4, 1),
+         (5000, 6, 16, 520), (3000, 2, 8, 1032), (20000, 3, 8, 72), (5000, 2, 8, 515), (4000, 5, 16, 1001), (2500, 16, 64, 264), (6000, 1, 4, 2056), (700, 4, 8, 1004)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -283,7 +348,8 @@ def offsets_of(loads, start=0):
 
 PRODUCTS = [([1], 8, 8), ([0], 64, 64), ([3, 0, 1], 64, 256), ([130], 72, 264), ([128, 256, 64], 128, 512), ([0, 5, 0, 700, 63, 0], 200, 328), ([2, 1, 1, 0, 2, 2, 0, 0], 512, 1032),
             ([64] * 20, 64, 128), ([33, 129, 1, 65, 127], 1000, 776), ([1] * 100, 136, 72), ([0, 0, 0], 64, 64), ([300, 2500], 264, 512), ([40] * 5, 328, 40000), ([40] * 5, 64, 2000), ([9, 60, 12], 200, 20000), ([1], 4096, 20000),
-            ([100, 0, 31, 200, 257], 520, 1000), ([1000], 128, 256), ([1000], 120, 512), ([513, 255], 1000, 264), ([15, 17, 16, 1, 31, 33, 49, 47], 264, 264)]
+            ([100, 0, 31, 200, 257], 520, 1000), ([1000], 128, 256), ([1000], 120, 512), ([513, 255], 1000, 264), ([15, 17, 16, 1, 31, 33, 49, 47], 264, 264),
+            ([(i * 97) % 900 + 300 for i in range(40)], 72, 264), ([i % 3 for i in range(512)], 64, 72), ([i % 150 for i in range(70)], 264, 136), ([600, 0, 513, 1024], 136, 520)]
 
 
 @pytest.mark.parametrize("loads,d_in,d_out", PRODUCTS)
