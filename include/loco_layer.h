@@ -208,7 +208,7 @@ uint64_t loco_norm_backward_workspace_bytes(const loco_norm_t *cfg);
 /*
  *   h        what the norm was taken of               dtotal    NULL: none
  *   d_dweight  NULL: not wanted (d_work may be NULL then); else [dim], the type of x.  d_work: 16-byte aligned, contents
- *              irrelevant before and after.
+ *              irrelevant before and after; calls that may run at the same time need workspaces of their own.
  * dx may be dy or dtotal itself, with its stride.  No atomics on values: the same inputs give the same bits.  One launch, two
  * with d_dweight.  Errors: ARG, ALIGN, SIZE, CUDA.
  */
@@ -236,7 +236,7 @@ int loco_experts_sort(int32_t experts, int64_t tokens, int32_t top_k, const int3
 
 typedef struct {
     int32_t dtype;           /* loco_dtype_t of the tokens and rows                       */
-    int32_t dim;             /* >= 1                                                      */
+    int32_t dim;             /* 1 .. 2^30                                                 */
     int32_t top_k;           /* 1 .. 16                                                   */
     int64_t tokens;          /* tokens * top_k < 2^31                                     */
     int64_t rows;            /* rows of the sorted tensors: places are below, < 2^31      */
@@ -263,7 +263,7 @@ typedef struct {
 typedef struct {
     int32_t experts;         /* 1 .. 512                                                                          */
     int64_t rows;            /* of x and y, < 2^31; expert e has rows offsets[e] .. offsets[e + 1] - 1            */
-    int32_t d_in, d_out;     /* multiples of 8                                                                    */
+    int32_t d_in, d_out;     /* multiples of 8, to 2^30                                                           */
     int32_t transposed;      /* product: the matrices are [experts, d_out, d_in]; else [experts, d_in, d_out]     */
 } loco_product_t;
 
@@ -303,7 +303,7 @@ uint64_t loco_gradient_squares_workspace_bytes(void);
  * One launch for every 768 spans.  Errors: ARG, ALIGN, SIZE, CUDA. */
 int loco_gradient_squares(const loco_span_t *spans, int32_t count, double *d_squares, void *d_work, uint64_t d_work_bytes, void *stream);
 
-/* d_norm: one fp32, or NULL.  max_norm >= 0.  Where c is 1 nothing is written to a y that is x.  One launch for every 768
+/* d_norm: one fp32, or NULL.  max_norm >= 0.  No output may overlap another, or another's gradient.  Where c is 1 nothing is written to a y that is x.  One launch for every 768
  * spans.  Errors: ARG, ALIGN, CUDA. */
 int loco_gradient_clip(const loco_span_t *spans, int32_t count, const double *d_squares, double max_norm, float *d_norm, void *stream);
 

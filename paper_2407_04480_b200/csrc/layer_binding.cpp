@@ -8,9 +8,11 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "../../include/loco_layer.h"
@@ -454,6 +456,15 @@ List list_of(PyObject *xs, PyObject *ys, PyObject *beside) {
             s.y = y.data_ptr();
         }
         l.spans.push_back(s);
+    }
+    if (ys) {                                    // a gradient that is there twice would be scaled twice, by whichever blocks come first
+        std::vector<std::pair<uintptr_t, uintptr_t>> places;
+        places.reserve(l.spans.size());
+        for (const loco_span_t &s : l.spans)
+            if (s.n > 0) places.emplace_back(reinterpret_cast<uintptr_t>(s.y), reinterpret_cast<uintptr_t>(s.y) + s.n * (s.dtype == LOCO_BF16 ? 2 : 4));
+        std::sort(places.begin(), places.end());
+        for (size_t i = 1; i < places.size(); ++i)
+            if (places[i].first < places[i - 1].second) refuse("the outputs overlap");
     }
     return l;
 }

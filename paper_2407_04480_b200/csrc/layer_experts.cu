@@ -19,6 +19,7 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortBlocks = 148;                 // most blocks, each leaves its counts to the others
 constexpr int kSortEach = 2048;                  // choices a block is worth starting for
 constexpr int kMoveThreads = 256;
+constexpr int kMostDim = 1 << 30;               // of a row: places in it are counted in 32 bits, some of them past its end
 constexpr unsigned kAll = 0xffffffffu;
 
 struct SortParams {
@@ -569,7 +570,7 @@ int check_experts(const loco_experts_t *c) {
     if (c->dtype != LOCO_F32 && c->dtype != LOCO_BF16) return LOCO_ERR_ARG;
     if (c->dim < 1 || c->top_k < 1 || c->top_k > kMostChoices) return LOCO_ERR_ARG;
     if (c->tokens < 0 || c->tokens > 0x7fffffff / c->top_k || c->rows < 0 || c->rows > 0x7fffffff) return LOCO_ERR_ARG;
-    return LOCO_OK;
+    return c->dim > kMostDim ? LOCO_ERR_UNSUPPORTED : LOCO_OK;
 }
 
 // What the accesses of a call can be: all rows on 16-byte boundaries, or on those of four, or every tensor on the former at least.

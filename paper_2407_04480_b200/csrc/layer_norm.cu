@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid
             if (there) h.store(row_at<T>(P.y, row, P.ys), t, P.dim);
         } else {
             const auto y = [&](int q) { return tc::mul2(h[q], w[q]); };          // but for r
-            uint32_t out[kMine / 4];             // a byte an element
+            uint32_t out[kMine / 4] = {};        // a byte an element
             const auto pack = [&](int q, float2 f) {
                 const uint32_t e = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
                 out[q / 2] = q % 2 ? out[q / 2] | e << 16 : e;

@@ -22,6 +22,7 @@ namespace loco_layer {
 using namespace tc;
 
 constexpr int kMostExperts = 512;
+constexpr int kMostColumns = 1 << 30;            // coordinates are 32 bits, some of them past the end
 constexpr int kTileRows = 128;                   // of the accumulator
 constexpr int kStep = 64;                        // of the contraction: a swizzled row of 128 bytes
 constexpr int kProductThreads = 384;
@@ -667,7 +668,7 @@ bool make_map(CUtensorMap &map, void *at, int64_t columns, int64_t rows, int64_t
 int check_product(const loco_product_t *c, const int32_t *offsets) {
     if (!c) return LOCO_ERR_ARG;
     if (c->experts < 1 || c->experts > kMostExperts || c->rows < 0 || c->rows > 0x7fffffff || c->d_in < 1 || c->d_out < 1) return LOCO_ERR_ARG;
-    if (c->d_in % 8 || c->d_out % 8) return LOCO_ERR_UNSUPPORTED;
+    if (c->d_in % 8 || c->d_out % 8 || c->d_in > kMostColumns || c->d_out > kMostColumns) return LOCO_ERR_UNSUPPORTED;
     if (!offsets) return LOCO_ERR_ARG;
     return aligned(offsets, 4) ? LOCO_OK : LOCO_ERR_ALIGN;
 }
@@ -740,7 +741,7 @@ int loco_experts_product(const loco_product_t *c, const loco_rows_t *x, const lo
     ProductParams P{d_offsets, static_cast<__nv_bfloat16 *>(y->ptr), 0, c->rows > 1 ? y->row_stride : 0, c->rows, c->experts, c->d_in, 0, c->d_out, 0};
     ProductMaps M;
     // Tiles by the rows an expert has on average: 32 and 64 for few, which leave the more of shared memory to the matrices on their
-    // way (12 and 8 stages), else 256 by pairs of SMs.  64 a pair's against 128 of one SM: 64 rows an expert, 4096 x 14336: 139, 147 us; pairs
+    // way (10 and 8 stages), else 256 by pairs of SMs.  64 a pair's against 128 of one SM: 64 rows an expert, 4096 x 14336: 139, 147 us; pairs
     // against 64 for 47 rows an expert, 1032 x 2048: 62, 57 us.
     const int64_t each = c->rows / c->experts, ends = c->rows < c->experts ? c->rows : c->experts;           // every expert may end in a tile of its own
     const bool pair = each >= 56;

@@ -68,8 +68,10 @@ def clip_shards(shards: List[torch.Tensor], max_norm: float, group: Optional[dis
     """Scale the averaged gradient, of which every rank holds the shards that BucketExchange.step left it, down to a global norm of
     max_norm, in place; returns the norm it had (fp32 [1], the same on every rank).
 
-    One double is added up over the ranks between the two passes over the shards; nothing synchronises the host.  work: a
+    Every rank has one shard at least, which may be empty.  One double is added up over the ranks between the two passes over the shards; nothing synchronises the host.  work: a
     workspace to keep between calls (layer.loco_gradient_squares_workspace_bytes() bytes, zeroed once); None allocates one."""
+    if not shards:
+        raise ValueError("clip_shards: no shards")
     device = shards[0].device
     if work is None:
         work = torch.zeros(layer.loco_gradient_squares_workspace_bytes(), dtype=torch.uint8, device=device)

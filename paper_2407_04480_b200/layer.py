@@ -580,7 +580,10 @@ def experts_product(x, w, offsets, transposed: bool = False):
 def clip_gradients(gradients, max_norm: float, work: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scale a list of contiguous gradients down, in place, to a global norm of max_norm; returns the norm they had (fp32 [1]).
 
-    work: a workspace to keep between calls (loco_gradient_squares_workspace_bytes() bytes, zeroed once); None allocates one."""
+    No gradient may be there twice, or overlap another.  work: a workspace to keep between calls
+    (loco_gradient_squares_workspace_bytes() bytes, zeroed once); None allocates one."""
+    if not gradients:
+        raise ValueError("clip_gradients: no gradients")
     device = gradients[0].device
     if work is None:
         work = torch.zeros(loco_gradient_squares_workspace_bytes(), dtype=torch.uint8, device=device)

@@ -658,6 +658,9 @@ def test_the_stream_argument_is_the_one_that_is_used():
     lambda: layer.loco_gradient_clip([torch.ones(4, device=DEV)], [], torch.zeros(1, device=DEV, dtype=torch.float64), None, 1.0),
     lambda: layer.loco_gradient_clip([torch.ones(4, device=DEV)], [torch.ones(4, device=DEV)], torch.zeros(1, device=DEV, dtype=torch.float64), None, -1.0),
     lambda: layer.loco_gradient_clip([torch.ones(4, device=DEV)], [torch.ones(4, device=DEV)], torch.zeros(1, device=DEV, dtype=torch.float64), None, math.nan),
+    lambda: layer.loco_gradient_clip([torch.ones(4, device=DEV)] * 2, [torch.ones(4, device=DEV)] * 2, torch.zeros(1, device=DEV, dtype=torch.float64), None, 1.0),
+    lambda: layer.loco_gradient_clip(list(torch.ones(12, device=DEV).unfold(0, 8, 4)), list(torch.ones(12, device=DEV).unfold(0, 8, 4)),
+                                     torch.zeros(1, device=DEV, dtype=torch.float64), None, 1.0),
 ])
 def test_refusals(call):
     before = layer.loco_layer_launch_count()
@@ -778,6 +781,69 @@ def test_clip_gradients_in_place():
     layer.clip_gradients(grads, 0.25 * n)
     for a, b in zip(grads, kept):
         within(a, b.double() / 4, b.double().abs() / 4, 8, a.dtype)
+
+
+def test_a_gradient_that_is_there_twice_is_refused_and_left_alone():
+    x, work = torch.full((64,), 2.0, device=DEV), torch.zeros(layer.loco_gradient_squares_workspace_bytes(), dtype=torch.uint8, device=DEV)
+    with pytest.raises(ValueError):
+        layer.clip_gradients([x, torch.ones(3, device=DEV), x], 1.0, work=work)
+    with pytest.raises(ValueError):
+        layer.clip_gradients([x[:40], x[39:]], 1.0, work=work)
+    assert (x == 2.0).all()
+    layer.clip_gradients([x[40:], torch.ones(0, device=DEV), x[:40], x[:0]], 4.0, work=work)
+    within(x, torch.full_like(x, 0.5), torch.full_like(x, 0.5), 4, F32)
+
+
+def far(rows, dim, dtype=BF):
+    """[rows, dim] whose last row lies past 2^32 elements, in a tensor of rows of 2^28."""
+    space = torch.empty((rows - 1) * (1 << 28) + dim, dtype=dtype, device=DEV)
+    return space.as_strided((rows, dim), (1 << 28, 1))
+
+
+def test_rows_past_32_bits():
+    g = gen(47)
+    t, d = 18, 72
+    x, y = far(t, d), far(t, d)
+    x.copy_(normal(g, t, d))
+    near = x.contiguous()
+    layer.loco_norm_forward(x, y)
+    want, dx, h = torch.empty_like(near), torch.empty_like(near), near.clone()
+    layer.loco_norm_forward(near, want)
+    assert torch.equal(y, want)
+    layer.loco_norm_backward(x, x, y)
+    layer.loco_norm_backward(near, near, dx)
+    assert torch.equal(y, dx)
+    place = torch.randperm(t, generator=g, device=DEV).int()[:, None]
+    layer.loco_experts_dispatch(x, place, y)
+    assert torch.equal(y[place[:, 0].long()], near)
+    back = far(t, d)
+    layer.loco_experts_combine(y, place, back)
+    assert torch.equal(back, near)
+    weight, dweight = torch.rand(t, 1, generator=g, device=DEV), torch.empty(t, 1, device=DEV)
+    layer.loco_experts_combine_backward(x, y, place, weight, back, dweight)
+    want, _, dw, terms = ref.combine_gradient(near, y.contiguous(), place, weight)
+    within(back, want, want.abs(), 1, BF)
+    within(dweight, dw, terms, d, F32)
+    w, offsets = normal(g, 2, d, d), offsets_of([11, 7])
+    layer.loco_experts_product(x, w, offsets, y)
+    want, terms, _ = ref.product(near, w, offsets, False)
+    within(y, want, terms, d, BF)
+    layer.loco_experts_product_weights(x, y, offsets, w)
+    want, terms = ref.product_weights(near, y.contiguous(), offsets)
+    within(w, want, terms, 32, BF)
+    layer.loco_experts_clear(y, offsets_of([16, 0]))
+    assert y[:16].any(1).all() and not y[16:].any()
+    assert torch.equal(h, near)
+
+
+def test_a_gradient_past_32_bits():
+    x = torch.zeros((1 << 32) + 11, dtype=BF, device=DEV)
+    x[::1 << 24] = 3.0
+    x[-1] = 4.0
+    n = math.sqrt(257 * 9.0 + 16.0)
+    norm = layer.clip_gradients([x], n / 2)
+    assert abs(float(norm) - n) <= 2 * STEP * n
+    assert float(x[-1]) == 2.0 and (x[::1 << 24] == 1.5).all() and int(x.count_nonzero()) == 258
 
 
 def test_clear_zeroes_what_lies_behind_the_last_row():

@@ -113,6 +113,7 @@ def test_moves_refuse_bad_arguments():
     for name, call in calls.items():
         for bad in (dict(dtype=3), dict(dim=0), dict(k=0), dict(k=17), dict(tokens=-1), dict(tokens=1 << 30), dict(n=-1), dict(n=1 << 31)):
             assert call(cfg(**bad)) == loco.ERR_ARG, (name, bad)
+        assert call(cfg(dim=(1 << 30) + 8), a=rows(stride=1 << 31), b=rows(stride=1 << 31)) == loco.ERR_UNSUPPORTED
         assert call(None) == loco.ERR_ARG and call(cfg(), p=None) == loco.ERR_ARG and call(cfg(), a=None) == loco.ERR_ARG and call(cfg(), b=rows(ptr=0)) == loco.ERR_ARG
         assert call(cfg(), p=PTR + 2) == loco.ERR_ALIGN and call(cfg(), a=rows(ptr=PTR + 1)) == loco.ERR_ALIGN and call(cfg(), b=rows(ptr=PTR + 1)) == loco.ERR_ALIGN
         assert call(cfg(tokens=0), a=rows(ptr=0), p=None) == loco.OK
@@ -138,6 +139,7 @@ def test_product_refuses_bad_arguments():
     for call in (plain, weights):
         for bad in (dict(experts=0), dict(experts=513), dict(n=-1), dict(n=1 << 31), dict(d_in=0), dict(d_out=-8)):
             assert call(cfg(**bad)) == loco.ERR_ARG, bad
+        assert call(cfg(d_in=(1 << 30) + 8)) == loco.ERR_UNSUPPORTED and call(cfg(d_out=(1 << 30) + 8)) == loco.ERR_UNSUPPORTED
         assert call(cfg(d_in=60)) == loco.ERR_UNSUPPORTED and call(cfg(d_out=4)) == loco.ERR_UNSUPPORTED
         assert call(None) == loco.ERR_ARG and call(cfg(), o=None) == loco.ERR_ARG and call(cfg(), a=None) == loco.ERR_ARG and call(cfg(), w=None) == loco.ERR_ARG
         for bad in (dict(a=rows(ptr=PTR + 8)), dict(a=rows(stride=68)), dict(y=rows(ptr=PTR + 2)), dict(w=matrices(ptr=PTR + 8)), dict(w=matrices(r=68)),
@@ -163,6 +165,13 @@ def test_gradient_refuses_bad_lists():
     assert squares(w=None) == loco.ERR_ARG and squares(w=PTR + 8) == loco.ERR_ALIGN and squares(n=need - 1) == loco.ERR_SIZE
     assert clip(s=span(y=0)) == loco.ERR_ARG and clip(s=span(y=PTR + 1)) == loco.ERR_ALIGN and clip(norm=PTR + 2) == loco.ERR_ALIGN
     assert clip(m=-1.0) == loco.ERR_ARG and clip(m=math.nan) == loco.ERR_ARG
+
+
+def test_an_empty_list_of_gradients_is_refused():
+    with pytest.raises(ValueError):
+        layer.clip_gradients([], 1.0)
+    with pytest.raises(ValueError):
+        exchange.clip_shards([], 1.0)
 
 
 # ---- differentiable forms over stand-ins -----------------------------------------------------
