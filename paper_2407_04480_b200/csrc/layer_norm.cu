@@ -97,19 +97,19 @@ __device__ __forceinline__ unsigned team_max(unsigned m, const Team &t, unsigned
 // leaves it, and h w of bfloat16 is exact in fp32: with 448 / max in two fp32 (`over`, `rest`) the value is rounded once before it
 // is rounded to 8 bits, and falls on the wrong side of a step where the exact one is within 2^-24 of it.
 struct Scale {
-    float scale, over, rest;
-    bool least;                                  // the scale is its least value: y first, over it then
+    float scale, over, rest, then;               // then: 1, or, where the scale is its least value, over it
     __device__ __forceinline__ Scale(unsigned largest, float r) {
         const float m = __uint_as_float(largest), s = m * r / kLargestE4m3;
-        least = !(s > kLeastScale);
-        if (!least) {
+        if (s > kLeastScale) {
             scale = s;
             over = kLargestE4m3 / m;
             rest = fmaf(-over, m, kLargestE4m3) / m;
+            then = 1.0f;
         } else {                                 // nothing there, or NaN
             scale = s != s ? s : kLeastScale;
             over = r;
             rest = 0.0f;
+            then = 1.0f / kLeastScale;
         }
     }
     // y / scale; fp32: what h w was rounded by is taken along
@@ -117,8 +117,7 @@ struct Scale {
         const float2 p = tc::mul2(h, w), o = make_float2(over, over);
         float2 low = tc::mul2(p, make_float2(rest, rest));
         if constexpr (sizeof(T) == 4) low = tc::fma2(tc::fma2(h, w, make_float2(-p.x, -p.y)), o, low);
-        const float2 f = tc::fma2(p, o, low);
-        return least ? tc::mul2(f, make_float2(1.0f / kLeastScale, 1.0f / kLeastScale)) : f;
+        return tc::mul2(tc::fma2(p, o, low), make_float2(then, then));
     }
 };
 
