@@ -46,7 +46,8 @@ struct Team {
     }
 };
 
-// Sums over the team, the same in every lane of it.  `fold` has a place for every warp of the block.
+// Sums over the team, the same in every lane of it.  `fold` has a place for every warp of the block, twice: a row's sums go to the
+// one side, the next row's to the other, so that one barrier a row will do.
 __device__ __forceinline__ float2 team_sum(float2 s, const Team &t, float2 *fold) {
     for (int o = (t.size < 32 ? t.size : 32) / 2; o; o >>= 1) {
         s.x += __shfl_xor_sync(kAll, s.x, o);
@@ -54,7 +55,6 @@ __device__ __forceinline__ float2 team_sum(float2 s, const Team &t, float2 *fold
     }
     if (t.size > 32) {
         const int warps = t.size / 32, first = t.mine * warps;
-        t.sync();                                // what the call before left has been read
         if (threadIdx.x % 32 == 0) fold[threadIdx.x / 32] = s;
         t.sync();
         s = threadIdx.x % 32 < warps ? fold[first + threadIdx.x % 32] : make_float2(0.0f, 0.0f);
@@ -70,7 +70,6 @@ __device__ __forceinline__ float team_sum(float s, const Team &t, float2 *fold) 
     for (int o = (t.size < 32 ? t.size : 32) / 2; o; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
     if (t.size > 32) {
         const int warps = t.size / 32, first = t.mine * warps;
-        t.sync();
         if (threadIdx.x % 32 == 0) fold[threadIdx.x / 32].x = s;
         t.sync();
         s = threadIdx.x % 32 < warps ? fold[first + threadIdx.x % 32].x : 0.0f;
@@ -79,12 +78,12 @@ __device__ __forceinline__ float team_sum(float s, const Team &t, float2 *fold) 
     }
     return s;
 }
-// Largest of the bits of values without a sign: their order is that of the values, NaN above infinity.
+// Largest of the bits of values without a sign: their order is that of the values, NaN above infinity.  Between two calls there
+// is a barrier of the team, that of the row's sum.
 __device__ __forceinline__ unsigned team_max(unsigned m, const Team &t, unsigned *fold) {
     for (int o = (t.size < 32 ? t.size : 32) / 2; o; o >>= 1) m = max(m, __shfl_xor_sync(kAll, m, o));
     if (t.size > 32) {
         const int warps = t.size / 32, first = t.mine * warps;
-        t.sync();
         if (threadIdx.x % 32 == 0) fold[threadIdx.x / 32] = m;
         t.sync();
         m = threadIdx.x % 32 < warps ? fold[first + threadIdx.x % 32] : 0;
@@ -258,7 +257,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid
     let_next_start();
     using Row = Part<T, V, kMine, kShift>;
     extern __shared__ __align__(16) uint8_t shared[];
-    __shared__ float2 fold[kNormThreads / 32];
+    __shared__ float2 fold[2][kNormThreads / 32];
     __shared__ unsigned tops[kBits8 ? kNormThreads / 32 : 1];        // not `fold`, which another team may be at
     __shared__ unsigned most[kBits8 ? 256 : 1];  // a row's or several rows' runs of 128 columns: threads * kMine / 128 of them at most
     const Team t(P, V);
@@ -277,36 +276,38 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid
     };
     for (int i = 1; i < P.depth; ++i) send();
     int64_t row = mine;
-    for (int64_t first = row - t.mine; first < P.rows; first += stride, row += stride) {
+    int side = 0;
+    for (int64_t first = row - t.mine; first < P.rows; first += stride, row += stride, side ^= 1) {
         const bool there = row < P.rows;
         send();
-        Row h, r;
-        r.fill(-0.0f);                           // x + -0 is x
+        Row h;
         if constexpr (Ring<T, V, kMine, kShift, 2>::kCopies) {
             ring.wait();
             ring.read(h, 0);
             h.trim(t, P.dim);
-            if (P.r) {
-                ring.read(r, 1);
-                r.trim(t, P.dim);
-            }
-            ring.next();
         } else {
             h.fill(0.0f);
-            if (there) {
-                h.load(row_at<T>(P.x, row, P.xs), t, P.dim, true);
-                if (P.r) r.load(row_at<T>(P.r, row, P.rs), t, P.dim, true);
-            }
+            if (there) h.load(row_at<T>(P.x, row, P.xs), t, P.dim, true);
         }
+        if (P.r) {
+            Row r;
+            if constexpr (Ring<T, V, kMine, kShift, 2>::kCopies) {
+                ring.read(r, 1);
+                r.trim(t, P.dim);
+            } else {
+                r.fill(0.0f);
+                if (there) r.load(row_at<T>(P.r, row, P.rs), t, P.dim, true);
+            }
+#pragma unroll
+            for (int q = 0; q < Row::kPairs; ++q) h.set(q, tc::add2(h[q], r[q]));
+            if (there) h.store(row_at<T>(P.h, row, P.hs), t, P.dim);
+        }
+        ring.next();
         float2 sum = both(0.0f);
 #pragma unroll
-        for (int q = 0; q < Row::kPairs; ++q) {
-            h.set(q, tc::add2(h[q], r[q]));
-            sum = tc::fma2(h[q], h[q], sum);
-        }
-        if (P.r && there) h.store(row_at<T>(P.h, row, P.hs), t, P.dim);
+        for (int q = 0; q < Row::kPairs; ++q) sum = tc::fma2(h[q], h[q], sum);
         h.keep();
-        const float by = rsqrtf(team_sum(sum.x + sum.y, t, fold) * P.over_dim + P.eps);
+        const float by = rsqrtf(team_sum(sum.x + sum.y, t, fold[side]) * P.over_dim + P.eps);
         h.keep();
         w.keep();
         if constexpr (!kBits8) {
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const __grid
             } else {
                 unsigned *const mine = most + t.mine * P.groups;
                 const auto run = [&](int i, int j) { return min(max(Row::column(t, i) + j, 0) / kScaleBlock, P.groups - 1); };
-                t.sync();                        // what the row before left has been read
+                if (t.size <= 32) __syncwarp();  // what the row before left has been read; larger teams know from the sum's barrier
                 for (int i = t.lane; i < P.groups; i += t.size) mine[i] = 0;
                 t.sync();
 #pragma unroll
@@ -405,7 +406,7 @@ template <typename T, int V, int kMine, bool kShift> __global__ void __launch_bo
     using Row = Part<T, V, kMine, kShift>;
     using Rows = Ring<T, V, kMine, kShift, 3>;           // what the norm was of, its output's gradient, the one past it
     extern __shared__ __align__(16) uint8_t shared[];
-    __shared__ float2 fold[kNormThreads / 32];
+    __shared__ float2 fold[2][kNormThreads / 32];
     const Team t(P, V);
     Rows ring(shared, P.depth);
     ring.none = static_cast<const T *>(P.x);
@@ -426,6 +427,7 @@ template <typename T, int V, int kMine, bool kShift> __global__ void __launch_bo
     };
     for (int i = 1; i < P.depth; ++i) send();
     int64_t row = mine;
+    int side = 0;
     for (int64_t first = row - t.mine; first < P.rows; first += stride, row += stride) {
         const bool there = row < P.rows;
         send();
@@ -453,7 +455,10 @@ template <typename T, int V, int kMine, bool kShift> __global__ void __launch_bo
         f.keep();
         e.keep();
         w.keep();
-        const float2 sum = team_sum(make_float2(squares.x + squares.y, dots.x + dots.y), t, fold);
+        // fp32 has no register to spare for the side, and takes a barrier more: 20000 x 4096, 198 us against 203; bfloat16, 4000 x 16384: 112, 109.
+        if constexpr (sizeof(T) == 4) t.sync();
+        const float2 sum = team_sum(make_float2(squares.x + squares.y, dots.x + dots.y), t, fold[side]);
+        if constexpr (sizeof(T) == 2) side ^= 1;
         const float by = rsqrtf(sum.x * P.over_dim + P.eps), pull = -sum.y * P.over_dim * by * by;
         out.fill(0.0f);
         if (P.dt) {
