@@ -554,11 +554,13 @@ enum Move { kDispatch, kCombine, kBackward };
 template <typename T, int V> MoveKernel pick_move(Move m, int k, int places) {
     if (m == kDispatch) return experts_dispatch_kernel<T, V>;
     // Combine, two choices, at one, two, four places: 16384 x 4096: 68, 71, 60 us; 700,000 x 64: 60, 53, 58; 30,000 x 1367 in single elements:
-    // 121, 86, 141.
+    // 121, 86, 141.  At two, four: 70,001 x 768 68, 54; 300,001 x 150 in words 121, 130; fp32 in words 20,000 x 1367 69, 57.
+    // A single choice, four places, against the kernels for two choices: 40 million elements in rows of 1024, fp32, combine 52, 50 us, backward
+    // 82, 72; bfloat16 30, 28 and 43, 39; in words 67, 46 and 86, 67.
     if (m == kCombine)
-        return k <= 2 ? (places > 2 ? experts_combine_kernel<T, V, 2, 4, true> : experts_combine_kernel<T, V, 2, 2, true>)
+        return k == 1 ? experts_combine_kernel<T, V, 1, 4, true> : k <= 2 ? (places > 2 ? experts_combine_kernel<T, V, 2, 4, true> : experts_combine_kernel<T, V, 2, 2, true>)
                : k <= 4 ? experts_combine_kernel<T, V, 4, 2, true> : experts_combine_kernel<T, V, 4, 1, false>;
-    return k <= 2 ? experts_backward_kernel<T, V, 2, 2> : k <= 4 ? experts_backward_kernel<T, V, 4, 1> : experts_backward_kernel<T, V, 8, 1>;
+    return k == 1 ? experts_backward_kernel<T, V, 1, 4> : k <= 2 ? experts_backward_kernel<T, V, 2, 2> : k <= 4 ? experts_backward_kernel<T, V, 4, 1> : experts_backward_kernel<T, V, 8, 1>;
 }
 
 template <typename T> MoveKernel pick_slide(Move m) {
@@ -596,14 +598,18 @@ int launch_move(Move m, MoveParams &P, const loco_experts_t *c, const Vectors &V
     P.row_count = c->rows;
     P.dim = c->dim;
     P.top_k = c->top_k;
-    // Off the boundaries rows are slid together, but for a sum of up to four: in words or elements, sliding, bfloat16, 30,000 x 1367, two
-    // choices: laid out 123, 64 us, summed 69, 89; 20,000 x 1004, four: 52, 44 and 53, 57; 9000 x 1367, six, backward 166, 132, summed 162, 54.
+    // Off the boundaries rows are slid together where single elements would be moved one by one, or rows are short: 30,000 x 1367, bfloat16, two
+    // choices, in elements or sliding: laid out 123, 64 us, backward 171, 167; 9000 x 1367, six, 166, 132; 399,644 x 101, fp32, one, 189, 159.
+    // Long rows of words are faster word by word, but laid out: 40 million elements in rows of 1002, two choices, bfloat16, in words or sliding: backward
+    // 64, 67 us, in rows of 2502 53, 84, fp32 100, 111; 20,000 x 1004, four, laid out 52, 44.  Sums slide from five choices on: 20,000 x
+    // 1004, four, 53, 57; 30,000 x 1367, two, 69, 89; 9000 x 1367, six, 162, 54.
     const bool bf16 = c->dtype == LOCO_BF16;
     const int k = c->top_k;
-    const bool slides = V.tensors && !V.rows && c->dim >= (bf16 ? 8 : 4) && (m != kCombine || k > 4);
+    const bool slides = V.tensors && !V.rows && c->dim >= (bf16 ? 8 : 4) && (m == kDispatch || (m == kCombine ? k > 4 : (bf16 && !V.words) || c->dim < 128));
     const int v = slides || V.rows ? (bf16 ? 8 : 4) : bf16 && V.words ? 2 : 1;
     // places in a row that a thread takes at once
-    const int places = slides ? (m == kCombine ? 1 : 2) : m == kCombine && k <= 2 ? (v > 1 && c->dim >= 128 * v ? 4 : 2) : (m == kCombine && k <= 4) || (m == kBackward && k <= 2) ? 2 : 1;
+    const bool four = k == 1 || (m == kCombine && k == 2 && (bf16 ? v > 1 : true) && c->dim >= (bf16 && v == 2 ? 128 : 64) * v);
+    const int places = slides ? (m == kCombine ? 1 : 2) : m == kDispatch ? 1 : four ? 4 : k <= (m == kCombine ? 4 : 2) ? 2 : 1;
     const MoveKernel fn = slides ? (bf16 ? pick_slide<__nv_bfloat16>(m) : pick_slide<float>(m))
                           : bf16 ? (v == 8   ? pick_move<__nv_bfloat16, 8>(m, k, places)
                                     : v == 2 ? pick_move<__nv_bfloat16, 2>(m, k, places)

@@ -202,7 +202,7 @@ def test_norm_of_many_rows_that_share_no_boundaries(rows, dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("k,dim", [(2, 200), (6, 130), (3, 1001)])
+@pytest.mark.parametrize("k,dim", [(2, 200), (6, 130), (3, 1001), (1, 129), (1, 1001), (1, 70), (2, 150), (4, 203), (5, 2502), (1, 5120), (2, 1367)])
 def test_moves_of_rows_that_share_no_boundaries(k, dim, dtype):
     g = gen(dim)
     t, e = 3000, 8
@@ -270,7 +270,8 @@ def test_sort(tokens, k, experts, how):
 
 
 MOVES = [(1, 1, 1, 8), (9, 2, 8, 4096), (70, 2, 4, 76), (33, 6, 160, 2040), (51, 16, 64, 100), (40, 3, 8, 7), (300, 4, 8, 64), (5, 8, 16, 5121), (2, 2, 4, 1),
-         (5000, 6, 16, 520), (3000, 2, 8, 1032), (20000, 3, 8, 72), (5000, 2, 8, 515), (4000, 5, 16, 1001), (2500, 16, 64, 264), (6000, 1, 4, 2056), (700, 4, 8, 1004)]
+         (5000, 6, 16, 520), (3000, 2, 8, 1032), (20000, 3, 8, 72), (5000, 2, 8, 515), (4000, 5, 16, 1001), (2500, 16, 64, 264), (6000, 1, 4, 2056), (700, 4, 8, 1004),
+         (9000, 1, 8, 64), (5000, 1, 8, 101), (3000, 1, 64, 502), (4000, 1, 8, 768), (4000, 2, 8, 520), (4000, 2, 8, 502), (2000, 2, 8, 1367), (2000, 6, 8, 502)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
