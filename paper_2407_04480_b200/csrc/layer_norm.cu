@@ -9,7 +9,7 @@
 //
 // bfloat16 with residual, 16384 x 5120: 105 us, 6.4 TB/s; 300,000 x 128: 50 us, 6.1 TB/s; 50,003 x 1367, whose rows begin anywhere,
 // 109 us, 5.0 TB/s; 16384 x 4096 to 8 bits 97 us, 4.9 TB/s: there the instructions bound it, some thirty for two elements.  Backward 8192 x 4096:
-// 45 us, 6.0 TB/s, and 7 for the sum of the blocks' parts of dw; 20,000 x 4096 in fp32 193 us, 6.8 TB/s.
+// 45 us, 6.0 TB/s, and 6 for the sum of the blocks' parts of dw; 20,000 x 4096 in fp32 193 us, 6.8 TB/s.
 #include <cuda_fp8.h>
 
 #include <cstring>
@@ -498,8 +498,10 @@ template <typename T, int V, int kMine, bool kShift> __global__ void __launch_bo
     }
 }
 
-// The blocks' partial rows added in their order: 32 columns to a block, 16 warps that each take a part of the rows.
-constexpr int kWeightWarps = 16;
+// The blocks' partial rows added in their order: 32 columns to a block, 16 warps that each take a part of the rows, five of them asked
+// for at once and none left over (by a loop unrolled ten times with a rest both gradients of 300,000 x 128 took 60.4 us, so 57.8; by 32 warps 57.4, but
+// 64 x 4096 9.6 against 7.2).
+constexpr int kWeightWarps = 16, kWeightRows = 5;
 template <typename T> __global__ void __launch_bounds__(kWeightWarps * 32) norm_weight_kernel(const float *part, int blocks, int dim, T *dw) {
     wait_for_previous();
     let_next_start();
@@ -508,8 +510,13 @@ template <typename T> __global__ void __launch_bounds__(kWeightWarps * 32) norm_
     const int per = (blocks + kWeightWarps - 1) / kWeightWarps, from = warp * per, until = min(from + per, blocks);
     float s = 0.0f;
     if (c < dim)
-#pragma unroll 10
-        for (int b = from; b < until; ++b) s += part[static_cast<int64_t>(b) * dim + c];
+        for (int b = from; b < until; b += kWeightRows) {
+            float x[kWeightRows];
+#pragma unroll
+            for (int u = 0; u < kWeightRows; ++u) x[u] = b + u < until ? part[static_cast<int64_t>(b + u) * dim + c] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < kWeightRows; ++u) s += x[u];
+        }
     fold[warp][lane] = s;
     __syncthreads();
     s = fold[lane % kWeightWarps][warp * 2 + lane / kWeightWarps];   // warp w adds columns 2w and 2w + 1
