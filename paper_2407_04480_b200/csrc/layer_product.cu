@@ -3,7 +3,7 @@
 // One block to an SM, or two that work together, take tiles of outputs one after the other, expert by expert; where an expert's
 // rows begin is known on the device only.  One warp copies 64 of the contraction at a time to a ring in shared memory (TMA,
 // 128-byte swizzle), one issues the products, eight write the accumulator out while the next tile's products run into the other
-// half of TMEM.
+// half of TMEM.  Where there are few tiles, up to eight blocks share the contraction of each.
 //   product   A, the 128 lanes of the accumulator, are columns of the expert's matrix, either way round, and B, its columns, are rows
 //             of x: as many as the expert has left, rounded up to 16 (two blocks: 32), so that no product is spent on an
 //             expert's ragged end.  Rows past it belong to the next expert (or are the copy's zero fill): what they give is in
@@ -40,6 +40,7 @@ struct ProductParams {
 };
 
 constexpr int kMostStages = 12;
+constexpr int kMostParts = 8;                    // SMs to the contraction of a tile
 struct ProductShared {
     uint64_t full[kMostStages], empty[kMostStages], clean[kMostStages], ready[2], written[2], drain;
     uint32_t tmem, failed;
@@ -637,13 +638,159 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
     if (threadIdx.x == 0 && S.failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
 }
 
+// ---- several SMs to the contraction of a tile -------------------------------------------------
+
+__device__ __forceinline__ uint32_t cluster_blocks() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ float4 load_in_block(uint32_t at) {
+    float4 f;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(at) : "memory");
+    return f;
+}
+
+// Few tiles with a long contraction: the blocks of a cluster take a part of it each for one tile of kN rows by 128 columns, leave
+// their sums in shared memory, and each adds up, in the blocks' order, and writes a part of the tile.
+template <bool kDown, int kN>
+__global__ void __launch_bounds__(kProductThreads, 1) product_split_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ ProductMaps M) {
+    constexpr int kStages = stages<kN>(), kBytes = stage_bytes<kN>();
+    static_assert(kN * kTileRows * 4 <= kStages * kBytes, "the sums are left where the copies were");
+    extern __shared__ uint8_t raw[];
+    uint8_t *const ring = raw + (1024 - smem_addr(raw) % 1024) % 1024;
+    ProductShared &S = *reinterpret_cast<ProductShared *>(ring + kStages * kBytes + kWriteWarps * kPieceBytes);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = static_cast<int>(cluster_rank()), parts = static_cast<int>(cluster_blocks());
+    volatile uint32_t *const failed = &S.failed;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            bar_init(smem_addr(&S.full[i]), 1);
+            bar_init(smem_addr(&S.empty[i]), 1);
+        }
+        bar_init(smem_addr(&S.ready[0]), 1);
+        S.failed = 0;
+        fence_bar_init();
+        fence_async_shared();
+    }
+    if (warp == kIssueWarp) tmem_alloc<kN>(smem_addr(&S.tmem));
+    wait_for_previous();
+    let_next_start();
+    find_rows<kN>(S, P);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = S.tmem, base = smem_addr(ring);
+    Walk<false, kN, kTileRows> walk;
+    const int tile = static_cast<int>(blockIdx.x) / parts;
+    const bool some = tile < walk.tiles(S, P);   // the same for all blocks of the cluster
+    Tile t{};
+    if (some) t = walk.at(S, P, tile);
+    const int from = static_cast<int>(static_cast<int64_t>(t.steps) * rank / parts), until = static_cast<int>(static_cast<int64_t>(t.steps) * (rank + 1) / parts);
+    const int rows = min(t.rows - t.row, kN);
+
+    if (some && warp == kLoadWarp) {
+        if (lane == 0) {
+            int slot = 0, phase = 0, issued = 0;
+            for (int k = from; k < until; ++k) {
+                bar_wait(smem_addr(&S.empty[slot]), phase ^ 1, failed);
+                if (*failed) break;
+                const uint32_t a = base + slot * kBytes, b = a + kTileRows * 128, bar = smem_addr(&S.full[slot]);
+                bar_expect(bar, kBytes);
+                if constexpr (kDown) {
+#pragma unroll
+                    for (int x = 0; x < kTileRows; x += 64) load_box3(a + x * 128, &M.a, t.col + x, k * kStep, t.expert, bar);
+                } else {
+                    load_box3(a, &M.a, k * kStep, t.col, t.expert, bar);
+                }
+                load_box3(b, &M.b, k * kStep, S.begin[t.expert] + t.row, 0, bar);
+                ++issued;
+                if (++slot == kStages) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+            }
+            for (int i = 0, s = slot, p = phase; i < kStages && i < issued; ++i) {
+                s = s ? s - 1 : kStages - 1;
+                if (s == kStages - 1) p ^= 1;
+                bar_wait(smem_addr(&S.empty[s]), p, failed);
+            }
+            if (*failed)                         // copies in flight end before the block's shared memory goes away
+                for (int i = 0; i < kStages && i < issued; ++i) {
+                    slot = slot ? slot - 1 : kStages - 1;
+                    if (slot == kStages - 1) phase ^= 1;
+                    settle(smem_addr(&S.full[slot]), phase);
+                }
+        }
+    } else if (some && warp == kIssueWarp) {
+        const uint32_t lead = elect_lane();
+        const uint32_t word = product(0, false) | (kDown ? 1u << 15 : 0u) | columns_word((rows + 15) / 16 * 16);
+        int slot = 0, phase = 0;
+        for (int k = from; k < until; ++k) {
+            bar_wait(smem_addr(&S.full[slot]), phase, failed);
+            __syncwarp();
+            fence_after();
+            // within the block's own shared memory: above these bits an address says which block of the cluster is meant
+            const uint32_t a = (base & 0x3ffffu) + slot * kBytes, b = a + kTileRows * 128;
+            const uint32_t da = kDown ? desc_along_rows(a, kStep * 128) : desc_along_columns(a), db = desc_along_columns(b);
+#pragma unroll
+            for (int x = 0; x < kStep; x += 16) mma_ss(lead, tmem, da + (kDown ? x * 128 >> 4 : x * 2 >> 4), db + (x * 2 >> 4), word, k > from || x > 0);
+            commit(lead, smem_addr(&S.empty[slot]));
+            if (++slot == kStages) {
+                slot = 0;
+                phase ^= 1;
+            }
+        }
+        commit(lead, smem_addr(&S.ready[0]));
+        bar_wait(smem_addr(&S.ready[0]), 0, failed);
+        if (*failed) settle(smem_addr(&S.ready[0]), 0);
+    } else if (some && warp >= kFirstWriter) {
+        const int part = warp % 4, first = (warp - kFirstWriter) / 4 * 32;
+        if (first < kN) {
+            bar_wait(smem_addr(&S.ready[0]), 0, failed);
+            __syncwarp();
+            fence_after();
+            uint32_t r[32];
+            load_columns(tmem + first + (static_cast<uint32_t>(part * 32) << 16), r);
+            wait_loads();
+            pin(r);
+            float *const sums = reinterpret_cast<float *>(ring) + part * 32 + lane;              // [row][column]: every product that read the ring is done
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sums[(first + i) * kTileRows] = __uint_as_float(r[i]);
+        }
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    cluster_sync();                              // all blocks' sums are there
+    fence_after();
+    if (warp == kIssueWarp) tmem_free<kN>(tmem);
+    if (some) {
+        __nv_bfloat16 *const out = P.out + (S.begin[t.expert] + static_cast<int64_t>(t.row)) * P.out_row + t.col;
+        for (int u = rank * kProductThreads + static_cast<int>(threadIdx.x); u < rows * (kTileRows / 8); u += parts * kProductThreads) {
+            const int row = u / (kTileRows / 8), c = u % (kTileRows / 8) * 8;
+            if (t.col + c >= P.wide) continue;
+            float4 lo = make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi = lo;
+            for (int b = 0; b < parts; ++b) {
+                const uint32_t at = in_block(base + (row * kTileRows + c) * 4, b);
+                const float4 x = load_in_block(at), y = load_in_block(at + 16);
+                lo = make_float4(lo.x + x.x, lo.y + x.y, lo.z + x.z, lo.w + x.w);
+                hi = make_float4(hi.x + y.x, hi.y + y.y, hi.z + y.z, hi.w + y.w);
+            }
+            *reinterpret_cast<uint4 *>(out + row * P.out_row + c) = make_uint4(pack_bf16(lo.x, lo.y), pack_bf16(lo.z, lo.w), pack_bf16(hi.x, hi.y), pack_bf16(hi.z, hi.w));
+        }
+    }
+    __syncwarp();
+    cluster_sync();                              // no block leaves while another reads its sums
+    if (threadIdx.x == 0 && S.failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
+}
+
 namespace {
 
 using ProductKernel = void (*)(const ProductParams, const ProductMaps);
 
 // Shared-memory limit of a kernel, set once per device.
 bool allow(ProductKernel fn, int which, int bytes) {
-    static std::atomic<bool> set[64][10];
+    static std::atomic<bool> set[64][14];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
         cudaGetLastError();
@@ -718,6 +865,12 @@ template <bool kWeights, bool kDown> int launch_pair(const ProductParams &P, con
     return launch_clusters(fn, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), kProductThreads, kPairBytes, stream, 2, P, M);
 }
 
+template <bool kDown, int kN> int launch_split(const ProductParams &P, const ProductMaps &M, int64_t tiles, int parts, int which, void *stream) {
+    constexpr ProductKernel fn = product_split_kernel<kDown, kN>;
+    if (!allow(fn, which, product_bytes<kN>())) return LOCO_ERR_CUDA;
+    return launch_clusters(fn, dim3(static_cast<unsigned>(tiles * parts)), kProductThreads, product_bytes<kN>(), stream, parts, P, M);
+}
+
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
@@ -751,13 +904,22 @@ int loco_experts_product(const loco_product_t *c, const loco_rows_t *x, const lo
     // Where products bound the call, the tiles with less to do fill the last rounds (16384 rows of 14336 through 4096 columns, eight experts:
     // 1720 us expert by expert, 1635 so); where the matrices' reading does, an expert's tiles stay together (3001 rows, 64 experts: 57, 69).
     P.last = each >= 512;
-    const int high = pair ? kTileRows : many ? 256 : each < 24 ? 32 : 64;
+    // Where tiles of up to 64 rows would leave half of the SMs without one, up to eight SMs share each tile's contraction, twelve steps each at
+    // least: one token's two experts of 14,336 x 4096 58.6, 39.0 us; 23 rows of 12,568 through 160 columns 48.0, 13.4; 300 rows of 8192 through 120
+    // 50.2, 13.9; with eight steps each 100 rows of 1024 through 1024 take 9.5 instead of 8.4.
+    const int few = each < 24 ? 32 : 64, sms = sm_count();
+    const int64_t small = (c->rows / few + ends) * over(c->d_out, kTileRows), steps = over(c->d_in, kStep);
+    int parts = 1;
+    while (parts < kMostParts && small * parts * 2 <= sms && steps / (parts * 2) >= 12) parts *= 2;
+    const int high = parts > 1 ? few : pair ? kTileRows : many ? 256 : few;
     const int64_t tiles = pair ? (c->rows / kPairRows + ends) * over(c->d_out, kPairCols) : (c->rows / high + ends) * over(c->d_out, kTileRows);
     if (!make_map(M.a, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? kTileRows : kStep) ||
         !make_map(M.b, x->ptr, c->d_in, c->rows, 1, x->row_stride, 0, high)) return LOCO_ERR_CUDA;
     const auto go = [&](auto down) {
         constexpr bool kDown = decltype(down)::value;
         constexpr int kFirst = kDown ? 4 : 0;
+        if (parts > 1)
+            return high == 32 ? launch_split<kDown, 32>(P, M, small, parts, kDown ? 12 : 10, stream) : launch_split<kDown, 64>(P, M, small, parts, kDown ? 13 : 11, stream);
         if (pair) return launch_pair<false, kDown>(P, M, tiles, kFirst, stream);
         if (many) return launch_product<false, kDown, 256>(P, M, tiles, kFirst + 3, stream);
         return high == 32 ? launch_product<false, kDown, 32>(P, M, tiles, kFirst + 1, stream) : launch_product<false, kDown, 64>(P, M, tiles, kFirst + 2, stream);

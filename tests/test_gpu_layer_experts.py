@@ -351,7 +351,8 @@ PRODUCTS = [([1], 8, 8), ([0], 64, 64), ([3, 0, 1], 64, 256), ([130], 72, 264), 
             ([64] * 20, 64, 128), ([33, 129, 1, 65, 127], 1000, 776), ([1] * 100, 136, 72), ([0, 0, 0], 64, 64), ([300, 2500], 264, 512), ([40] * 5, 328, 40000), ([40] * 5, 64, 2000), ([9, 60, 12], 200, 20000), ([1], 4096, 20000),
             ([100, 0, 31, 200, 257], 520, 1000), ([1000], 128, 256), ([1000], 120, 512), ([513, 255], 1000, 264), ([15, 17, 16, 1, 31, 33, 49, 47], 264, 264),
             ([(i * 97) % 900 + 300 for i in range(40)], 72, 264), ([i % 3 for i in range(512)], 64, 72), ([i % 150 for i in range(70)], 264, 136), ([600, 0, 513, 1024], 136, 520),
-            ([600, 0, 513, 1024, 300], 264, 96), ([256, 255, 257, 64, 1], 136, 128), ([70, 80, 90], 72, 8), ([600, 31, 513], 96, 264), ([1100], 200, 40)]
+            ([600, 0, 513, 1024, 300], 264, 96), ([256, 255, 257, 64, 1], 136, 128), ([70, 80, 90], 72, 8), ([600, 31, 513], 96, 264), ([1100], 200, 40),
+            ([0, 1, 0, 1], 14336, 264), ([5, 17, 1], 12568, 160), ([150, 0, 150], 8192, 120), ([31, 33], 1544, 1000), ([64, 128, 1], 3080, 72), ([700], 4096, 128)]
 
 
 @pytest.mark.parametrize("loads,d_in,d_out", PRODUCTS)
