@@ -865,6 +865,41 @@ template <bool kWeights, bool kDown> int launch_pair(const ProductParams &P, con
     return launch_clusters(fn, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), kProductThreads, kPairBytes, stream, 2, P, M);
 }
 
+// Clusters of `parts` blocks that run at once, asked for once per device: fewer than the SMs there are would make, since a cluster's lie together.
+template <bool kDown, int kN> int clusters_at_once(int parts, int which) {
+    static std::atomic<int> known[64][kMostParts + 1];               // one more than the answer
+    constexpr ProductKernel fn = product_split_kernel<kDown, kN>;
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return 0;
+    }
+    if ((n = known[dev][parts].load(std::memory_order_relaxed)) > 0) return n - 1;
+    if (!allow(fn, which, product_bytes<kN>())) return 0;
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3(static_cast<unsigned>(parts));
+    how.blockDim = dim3(kProductThreads);
+    how.dynamicSmemBytes = product_bytes<kN>();
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = static_cast<unsigned>(parts);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    how.attrs = &attr;
+    how.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, fn, &how) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+    }
+    known[dev][parts].store(n + 1, std::memory_order_relaxed);
+    return n;
+}
+// Blocks to a tile's contraction: as many as leave every tile its cluster at once and a block twelve steps.
+template <bool kDown, int kN> int parts_of(int64_t tiles, int64_t steps, int which) {
+    for (int parts = kMostParts; parts > 1; --parts)
+        if (steps / parts >= 12 && tiles * parts <= sm_count() && tiles <= clusters_at_once<kDown, kN>(parts, which)) return parts;
+    return 1;
+}
+
 template <bool kDown, int kN> int launch_split(const ProductParams &P, const ProductMaps &M, int64_t tiles, int parts, int which, void *stream) {
     constexpr ProductKernel fn = product_split_kernel<kDown, kN>;
     if (!allow(fn, which, product_bytes<kN>())) return LOCO_ERR_CUDA;
@@ -904,13 +939,14 @@ int loco_experts_product(const loco_product_t *c, const loco_rows_t *x, const lo
     // Where products bound the call, the tiles with less to do fill the last rounds (16384 rows of 14336 through 4096 columns, eight experts:
     // 1720 us expert by expert, 1635 so); where the matrices' reading does, an expert's tiles stay together (3001 rows, 64 experts: 57, 69).
     P.last = each >= 512;
-    // Where tiles of up to 64 rows would leave half of the SMs without one, up to eight SMs share each tile's contraction, twelve steps each at
+    // Where tiles of up to 64 rows leave half of the SMs without one, two to eight SMs share each tile's contraction, twelve steps each at
     // least: one token's two experts of 14,336 x 4096 58.6, 39.0 us; 23 rows of 12,568 through 160 columns 48.0, 13.4; 300 rows of 8192 through 120
-    // 50.2, 13.9; with eight steps each 100 rows of 1024 through 1024 take 9.5 instead of 8.4.
-    const int few = each < 24 ? 32 : 64, sms = sm_count();
+    // 50.2, 13.9; with eight steps each 100 rows of 1024 through 1024 take 9.5 instead of 8.4.  Clusters that have to wait for others are worse
+    // than smaller ones: of eight SMs fifteen run at once, and one row of 14,336 through 1920 columns takes 14.4 us, but through 2048 27.3.
+    const int few = each < 24 ? 32 : 64;
     const int64_t small = (c->rows / few + ends) * over(c->d_out, kTileRows), steps = over(c->d_in, kStep);
-    int parts = 1;
-    while (parts < kMostParts && small * parts * 2 <= sms && steps / (parts * 2) >= 12) parts *= 2;
+    const int parts = turned ? (few == 32 ? parts_of<false, 32>(small, steps, 10) : parts_of<false, 64>(small, steps, 11))
+                             : (few == 32 ? parts_of<true, 32>(small, steps, 12) : parts_of<true, 64>(small, steps, 13));
     const int high = parts > 1 ? few : pair ? kTileRows : many ? 256 : few;
     const int64_t tiles = pair ? (c->rows / kPairRows + ends) * over(c->d_out, kPairCols) : (c->rows / high + ends) * over(c->d_out, kTileRows);
     if (!make_map(M.a, w->ptr, columns, rows, c->experts, w->row_stride, w->expert_stride, turned ? kTileRows : kStep) ||
