@@ -42,7 +42,7 @@ struct ProductParams {
 constexpr int kMostStages = 12;
 constexpr int kMostParts = 8;                    // SMs to the contraction of a tile
 struct ProductShared {
-    uint64_t full[kMostStages], empty[kMostStages], clean[kMostStages], ready[2], written[2], drain;
+    uint64_t full[kMostStages], edge[kMostStages], empty[kMostStages], clean[kMostStages], ready[2], written[2], drain;
     uint32_t tmem, failed;
     int32_t begin[kMostExperts], count[kMostExperts];                // rows of an expert
     int32_t first[kMostExperts + 1], ends[kMostExperts + 1];         // tiles of rows, and tiles that come last, before it
@@ -473,8 +473,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
     volatile uint32_t *const failed = &S.failed;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kPairStages; ++i) {
-            bar_init(smem_addr(&S.full[i]), 1);                      // the first block's: both blocks' copies, but for one with rows past
-            bar_init(smem_addr(&S.empty[i]), 1);                     // an expert's end in it; the second's: such a copy of its own
+            bar_init(smem_addr(&S.full[i]), 1);                      // the first block's: both blocks' copies, but for those with rows past
+            bar_init(smem_addr(&S.edge[i]), 1);                      // an expert's end in them, which each block has on its own `edge`
+            bar_init(smem_addr(&S.empty[i]), 1);
             bar_init(smem_addr(&S.clean[i]), 2);                     // the first block's: those rows are zero in both
         }
         for (int i = 0; i < 2; ++i) {
@@ -511,8 +512,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
                     if (*failed) break;
                     const bool ragged = kWeights && t.rows - k * kStep < kStep;
                     const uint32_t a = base + slot * kPairStage, b = a + kTileRows * 128;
-                    const uint32_t bar = in_block(smem_addr(&S.full[slot]), ragged ? rank : 0);
-                    if (rank == 0 || ragged) bar_expect(smem_addr(&S.full[slot]), ragged ? kPairStage : 2 * kPairStage);
+                    const uint32_t own = smem_addr(ragged ? &S.edge[slot] : &S.full[slot]), bar = in_block(own, ragged ? rank : 0);
+                    if (rank == 0 || ragged) bar_expect(own, ragged ? kPairStage : 2 * kPairStage);
                     if constexpr (kWeights) {
 #pragma unroll
                         for (int x = 0; x < kTileRows; x += 64) {
@@ -549,8 +550,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
     } else if (warp == kIssueWarp) {
         const uint32_t lead = elect_lane();
         constexpr uint32_t plain = (product(0, kWeights) & 0x00ffffffu) | (16u << 24) | (kDown ? 1u << 15 : 0u);       // 256 lanes
-        int slot = 0, phase = 0, buffer = 0, turn = 0;
-        uint32_t ends = 0;                       // by slot: the phase of `clean`
+        int slot = 0, buffer = 0, turn = 0;
+        uint32_t fulls = 0, ends = 0;            // by slot: the phases of `full`, and of `edge` and `clean`
         for (int tile = begin; tile < tiles && rank == 0; tile += stride) {
             const Tile t = walk.at(S, P, tile);
             if (t.steps == 0) continue;
@@ -558,11 +559,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
             bar_wait(smem_addr(&S.written[buffer]), turn ^ 1, failed);
             for (int k = 0; k < t.steps; ++k) {
                 const int left = kWeights ? t.rows - k * kStep : kStep;
-                bar_wait(smem_addr(&S.full[slot]), phase, failed);
                 if (left < kStep) {
+                    bar_wait(smem_addr(&S.edge[slot]), ends >> slot & 1, failed);
                     bar_wait(smem_addr(&S.clean[slot]), ends >> slot & 1, failed);
                     bar_test_cluster(smem_addr(&S.clean[slot]), ends >> slot & 1);     // what the other block did before it arrived is seen
                     ends ^= 1u << slot;
+                } else {
+                    bar_wait(smem_addr(&S.full[slot]), fulls >> slot & 1, failed);
+                    fulls ^= 1u << slot;
                 }
                 __syncwarp();
                 fence_after();
@@ -574,10 +578,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
                     if (!kWeights || x < left)
                         mma_pair(lead, tmem + buffer * kPairCols, da + (kDown ? x * 128 >> 4 : x * 2 >> 4), db + (kWeights ? x * 128 >> 4 : x * 2 >> 4), word, k > 0 || x > 0);
                 commit_pair(lead, smem_addr(&S.empty[slot]));
-                if (++slot == kPairStages) {
-                    slot = 0;
-                    phase ^= 1;
-                }
+                if (++slot == kPairStages) slot = 0;
             }
             commit_pair(lead, smem_addr(&S.ready[buffer]));
             buffer ^= 1;
@@ -589,27 +590,24 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
             if (*failed) settle(smem_addr(&S.drain), 0);
         }
     } else if (warp == kCleanWarp && kWeights) {
-        // Zeros in the rows past an expert's last, in this block's part of the step that holds them.  The first block's copies are waited
-        // for one after the other (a phase told by its parity has to be the current one or the last); the second's `full` has
-        // such steps' phases alone.
-        int slot = 0, phase = 0;
-        uint32_t ends = 0;                       // by slot: the phase of the second block's `full`
+        // Zeros in the rows past an expert's last, in this block's part of the step that holds them.  A phase told by its parity has to be
+        // the current one or the last: `edge` has such steps' phases alone, and their slots are filled again only after their products,
+        // which wait for this warp's arrival.
+        int slot = 0;
+        uint32_t ends = 0;                       // by slot: the phase of `edge`
         for (int tile = begin; tile < tiles; tile += stride) {
             const Tile t = walk.at(S, P, tile);
-            for (int k = 0; k < t.steps; ++k) {
-                const int left = t.rows - k * kStep;
-                if (rank == 0 || left < kStep) bar_wait(smem_addr(&S.full[slot]), rank == 0 ? phase : ends >> slot & 1, failed);
-                if (left < kStep) {
-                    ends ^= 1u << slot;
-                    __syncwarp();
-                    clean_rows<2 * kTileRows / 64>(ring + slot * kPairStage, left, lane);
-                    if (lane == 0) bar_arrive_in(in_block(smem_addr(&S.clean[slot]), 0));
-                }
-                if (++slot == kPairStages) {
-                    slot = 0;
-                    phase ^= 1;
-                }
+            if (t.steps == 0) continue;
+            slot = (slot + t.steps - 1) % kPairStages;               // of the tile's last step
+            const int left = t.rows - (t.steps - 1) * kStep;
+            if (left < kStep) {
+                bar_wait(smem_addr(&S.edge[slot]), ends >> slot & 1, failed);
+                ends ^= 1u << slot;
+                __syncwarp();
+                clean_rows<2 * kTileRows / 64>(ring + slot * kPairStage, left, lane);
+                if (lane == 0) bar_arrive_in(in_block(smem_addr(&S.clean[slot]), 0));
             }
+            slot = (slot + 1) % kPairStages;
         }
     } else if (warp >= kFirstWriter) {
         int buffer = 0, turn = 0;
