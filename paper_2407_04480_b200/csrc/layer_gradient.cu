@@ -49,15 +49,20 @@ template <typename T> struct Piece {
     uint64_t at;                                 // element
     int count, head, tail;
     uint64_t rest;                               // where the tail begins
-    __device__ __forceinline__ Piece(const void *x, uint64_t n, uint32_t chunk, uint32_t chunks) {
+    __host__ __device__ __forceinline__ Piece(const void *x, uint64_t n, uint32_t chunk, uint32_t chunks) {
         const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T);
-        const uint32_t before = min(static_cast<uint64_t>(off ? kV - off : 0), n);
-        const uint64_t vectors = (n - before) / kV, first = min(static_cast<uint64_t>(chunk) * kEach, vectors);
+        const uint64_t to_boundary = off ? kV - off : 0, before = to_boundary < n ? to_boundary : n;
+        const uint64_t vectors = (n - before) / kV, skipped = static_cast<uint64_t>(chunk) * kEach, first = skipped < vectors ? skipped : vectors;
         at = before + first * kV;
-        count = static_cast<int>(min(vectors - first, static_cast<uint64_t>(kEach)));
-        head = chunk == 0 ? before : 0;
+        count = static_cast<int>(vectors - first < kEach ? vectors - first : kEach);
+        head = chunk == 0 ? static_cast<int>(before) : 0;
         rest = before + vectors * kV;
         tail = chunk + 1 == chunks ? static_cast<int>(n - rest) : 0;
+    }
+    // What the copy of vector i names.  Past the vectors nothing is read, but an address has to be a boundary all the same: the one
+    // at or before the span, which need not have a vector at all.
+    __host__ __device__ __forceinline__ const uint4 *vector(const void *x, int i) const {
+        return reinterpret_cast<const uint4 *>(i < count ? reinterpret_cast<uintptr_t>(static_cast<const T *>(x) + at) + i * 16ull : reinterpret_cast<uintptr_t>(x) & ~uintptr_t{15});
     }
 };
 
@@ -66,12 +71,12 @@ struct Ahead {
     uint4 *const at;
     int put = 0, got = 0;
     __device__ __forceinline__ explicit Ahead(void *shared) : at(static_cast<uint4 *>(shared) + threadIdx.x) {}
-    __device__ __forceinline__ void send(const uint4 *from, int count) {
+    template <typename T> __device__ __forceinline__ void send(const void *x, const Piece<T> &p) {
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const int i = static_cast<int>(threadIdx.x) + u * kListThreads;
             const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(at + (put * kAtOnce + u) * kListThreads));
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from + (i < count ? i : 0)), "r"(i < count ? 16 : 0) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p.vector(x, i)), "r"(i < p.count ? 16 : 0) : "memory");
         }
         if (++put == kAhead) put = 0;
     }
@@ -172,13 +177,8 @@ template <typename T, int kMost> __device__ __forceinline__ Piece<T> piece_at(co
     return Piece<T>(P.x[span], P.n[span], chunk - P.first[span], P.first[span + 1] - P.first[span]);
 }
 template <int kMost> __device__ __forceinline__ void send_chunk(const ListParams<kMost> &P, int span, uint32_t chunk, Ahead &ahead) {
-    if (P.type[span] == LOCO_BF16) {
-        const Piece<__nv_bfloat16> p = piece_at<__nv_bfloat16>(P, span, chunk);
-        ahead.send(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(P.x[span]) + p.at), p.count);
-    } else {
-        const Piece<float> p = piece_at<float>(P, span, chunk);
-        ahead.send(reinterpret_cast<const uint4 *>(static_cast<const float *>(P.x[span]) + p.at), p.count);
-    }
+    if (P.type[span] == LOCO_BF16) ahead.send(P.x[span], piece_at<__nv_bfloat16>(P, span, chunk));
+    else ahead.send(P.x[span], piece_at<float>(P, span, chunk));
 }
 
 // Adds the blocks' sums, in their order, when all are there; fp64 of the block's own sum in every thread of the first warp.
