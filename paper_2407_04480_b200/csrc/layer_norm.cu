@@ -100,14 +100,16 @@ __device__ __forceinline__ unsigned team_max(unsigned m, const Team &t, unsigned
 // leaves it, and h w of bfloat16 is exact in fp32: with 448 / max in two fp32 (`over`, `rest`) the value is rounded once before it
 // is rounded to 8 bits, and falls on the wrong side of a step where the exact one is within 2^-24 of it.
 struct Scale {
-    float scale, over, rest, then;               // then: 1, or, where the scale is its least value, over it
+    float scale, over, rest, then;               // then: 1, what `over` is off by, or, where the scale is its least value, over it
     __device__ __forceinline__ Scale(unsigned largest, float r) {
         const float m = __uint_as_float(largest), s = m * r / kLargestE4m3;
         if (s > kLeastScale) {
+            // below 1.3e-36 the quotient leaves fp32's range, though a large r keeps the scale above its least value: there both are 2^64 off
+            const float up = m < 0x1p-64f ? 0x1p64f : 1.0f, n = m * up;
             scale = s;
-            over = kLargestE4m3 / m;
-            rest = fmaf(-over, m, kLargestE4m3) / m;
-            then = 1.0f;
+            over = kLargestE4m3 / n;
+            rest = fmaf(-over, n, kLargestE4m3) / n;
+            then = up;
         } else {                                 // nothing there, or NaN
             scale = s != s ? s : kLeastScale;
             over = r;
