@@ -539,12 +539,19 @@ template <typename T> __global__ void __launch_bounds__(kMoveThreads, 4) experts
     }
 }
 
-// Rows from the last offset on: nothing to write, as a rule.
-template <typename T> __global__ void __launch_bounds__(kMoveThreads) experts_clear_kernel(T *rows, int64_t stride, int64_t count, int dim, const int32_t *last) {
+// Rows of no expert: ahead of the first offset, and from the largest on, which is how the products read them.  Nothing to write, as a rule.
+template <typename T>
+__global__ void __launch_bounds__(kMoveThreads) experts_clear_kernel(T *rows, int64_t stride, int64_t count, int dim, const int32_t *offsets, int experts) {
     wait_for_previous();
     let_next_start();
-    for (int64_t r = max(*last, 0) + static_cast<int64_t>(blockIdx.x); r < count; r += gridDim.x)
-        for (int c = threadIdx.x; c < dim; c += kMoveThreads) rows[r * stride + c] = from_f32<T>(0.0f);
+    int end = 0;
+    for (int e = threadIdx.x % 32; e <= experts; e += 32) end = max(end, offsets[e]);
+    end = __reduce_max_sync(kAll, end);
+    const int64_t ahead = min(static_cast<int64_t>(max(offsets[0], 0)), count), none = ahead + max(count - end, static_cast<int64_t>(0));
+    for (int64_t i = blockIdx.x; i < none; i += gridDim.x) {
+        T *const row = rows + (i < ahead ? i : i - ahead + end) * stride;
+        for (int c = threadIdx.x; c < dim; c += kMoveThreads) row[c] = from_f32<T>(0.0f);
+    }
 }
 
 namespace {
@@ -684,8 +691,8 @@ int loco_experts_clear(int32_t dtype, int32_t dim, int64_t rows_count, const loc
     if (sms == 0) return LOCO_ERR_CUDA;
     const dim3 grid(static_cast<unsigned>(rows_count < sms * 4 ? rows_count : sms * 4));
     if (dtype == LOCO_BF16)
-        return launch_kernel(experts_clear_kernel<__nv_bfloat16>, grid, kMoveThreads, 0, stream, static_cast<__nv_bfloat16 *>(rows->ptr), stride, rows_count, dim, d_offsets + experts);
-    return launch_kernel(experts_clear_kernel<float>, grid, kMoveThreads, 0, stream, static_cast<float *>(rows->ptr), stride, rows_count, dim, d_offsets + experts);
+        return launch_kernel(experts_clear_kernel<__nv_bfloat16>, grid, kMoveThreads, 0, stream, static_cast<__nv_bfloat16 *>(rows->ptr), stride, rows_count, dim, d_offsets, experts);
+    return launch_kernel(experts_clear_kernel<float>, grid, kMoveThreads, 0, stream, static_cast<float *>(rows->ptr), stride, rows_count, dim, d_offsets, experts);
 }
 
 int loco_experts_dispatch(const loco_experts_t *c, const loco_rows_t *x, const int32_t *d_place, const loco_rows_t *rows, void *stream) {

@@ -276,7 +276,8 @@ def loco_experts_combine_backward(dy, rows, place, weight, drows, dweight, strea
 
 
 def loco_experts_clear(rows, offsets, stream=None) -> None:
-    """Zeros in rows [rows, dim] from offsets[experts] on, which the other calls leave as they are."""
+    """Zeros in the rows of [rows, dim] that no expert has: ahead of offsets[0], and from the largest offset on.  The other calls leave
+    them as they are."""
     _check(_binding().experts_clear(rows, offsets, _raw(stream)), "loco_experts_clear")
 
 
@@ -571,7 +572,7 @@ class _Product(torch.autograd.Function):
 
 
 def experts_product(x, w, offsets, transposed: bool = False):
-    """x[t] @ w[e] for the rows t of every expert e, as loco_experts_product; zeros in rows behind the last expert's.
+    """x[t] @ w[e] for the rows t of every expert e, as loco_experts_product; zeros in rows that no expert has.
 
     Differentiable once."""
     return _Product.apply(x, w, offsets, transposed)

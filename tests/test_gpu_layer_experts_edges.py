@@ -7,7 +7,7 @@ import torch
 
 from paper_2407_04480_b200 import layer, loco
 from tests import experts_reference as ref
-from tests.test_gpu_layer_experts import BF, DEV, E4M3, F32, NORM_ADDITIONS, STEP, gen, normal
+from tests.test_gpu_layer_experts import BF, DEV, E4M3, F32, NORM_ADDITIONS, STEP, gen, normal, within
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,43 @@ def test_norm_in_8_bits_of_tiny_values_that_a_small_row_lifts(dim, block, dtype,
     assert float(((scale.double() - s).abs() / s).max()) <= (NORM_ADDITIONS + 3) * STEP
     room = q.abs() * (2.0 ** -4 + (2 * NORM_ADDITIONS + 5) * STEP) + 2.0 ** -10
     assert bool(((y.double() - q).abs() <= room).all())
+
+
+OFFSETS = [[0, 10, 5, 40], [40, 0, 40, 0], [7, 30, 2, 1 << 30], [-4, 10, 20, 30], [0, 20, 100, 200], [50, 60, 70, 80], [40, 40, 40, 40], [0, 0, 0, 0], [3, 9, 9, 25],
+           [39, 39, 39, 39], [0, 30, 10, 20]]
+
+
+@pytest.mark.parametrize("offsets", OFFSETS, ids=str)
+def test_rows_of_no_expert_are_zeros_in_the_differentiable_product(offsets):
+    """Offsets that do not begin with 0, or do not ascend, are read as the largest so far: the rows that this leaves to no expert are zeros
+    in the outputs and in the gradient, and those of an expert are its products."""
+    g = gen(51)
+    junk = [torch.full((1 << 22,), math.nan, device=DEV, dtype=BF) for _ in range(4)]
+    del junk
+    o = torch.tensor(offsets, dtype=torch.int32, device=DEV)
+    x, w, dy = normal(g, 40, 64).requires_grad_(), normal(g, 3, 64, 72), normal(g, 40, 72)
+    y = layer.experts_product(x, w, o)
+    dx, = torch.autograd.grad(y, x, dy)
+    for got, (want, terms, live), n in ((y.detach(), ref.product(x.detach(), w, o, False), 64), (dx, ref.product(dy, w, o, True), 72)):
+        within(got[live], want[live], terms[live], 2 * n, BF)
+        assert not got[~live].any() and torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("offsets", OFFSETS, ids=str)
+def test_clear_zeroes_the_rows_of_no_expert_and_no_others(offsets, dtype):
+    space = torch.full((40, 75), 7.0, dtype=dtype, device=DEV)
+    rows = space[:, 1:74]
+    o = torch.tensor(offsets, dtype=torch.int32, device=DEV)
+    layer.loco_experts_clear(rows, o)
+    live = torch.zeros(40, dtype=torch.bool)
+    for a, b in ref.spans(o, 40):
+        live[a:b] = True
+    assert (rows[live] == 7.0).all() and not rows[~live].any() and (space[:, 0] == 7.0).all() and (space[:, 74] == 7.0).all()
+
+
+def test_clear_with_as_many_experts_as_there_can_be():
+    offsets = torch.arange(2, 515, dtype=torch.int32, device=DEV)     # 512 rows from the second on
+    rows = torch.full((600, 8), 7.0, device=DEV)
+    layer.loco_experts_clear(rows, offsets)
+    assert not rows[:2].any() and (rows[2:514] == 7.0).all() and not rows[514:].any()
