@@ -457,14 +457,23 @@ List list_of(PyObject *xs, PyObject *ys, PyObject *beside) {
         }
         l.spans.push_back(s);
     }
-    if (ys) {                                    // a gradient that is there twice would be scaled twice, by whichever blocks come first
+    if (ys) {
+        // An output that lies in another, or in another's gradient, would be written and read by whichever blocks come first; so would one
+        // that covers a part of its own gradient, or all of it at another place.
         std::vector<std::pair<uintptr_t, uintptr_t>> places;
         places.reserve(l.spans.size());
+        const auto end = [](const void *at, const loco_span_t &s) { return reinterpret_cast<uintptr_t>(at) + s.n * (s.dtype == LOCO_BF16 ? 2 : 4); };
         for (const loco_span_t &s : l.spans)
-            if (s.n > 0) places.emplace_back(reinterpret_cast<uintptr_t>(s.y), reinterpret_cast<uintptr_t>(s.y) + s.n * (s.dtype == LOCO_BF16 ? 2 : 4));
+            if (s.n > 0) places.emplace_back(reinterpret_cast<uintptr_t>(s.y), end(s.y, s));
         std::sort(places.begin(), places.end());
         for (size_t i = 1; i < places.size(); ++i)
             if (places[i].first < places[i - 1].second) refuse("the outputs overlap");
+        for (const loco_span_t &s : l.spans) {
+            if (s.n == 0 || s.y == s.x) continue;    // scaled in place: what overlaps the gradient overlaps its output
+            const uintptr_t from = reinterpret_cast<uintptr_t>(s.x);
+            const auto first = std::upper_bound(places.begin(), places.end(), from, [](uintptr_t x, const auto &p) { return x < p.second; });     // that ends behind its begin
+            if (first != places.end() && first->first < end(s.x, s)) refuse("an output overlaps a gradient that is not its own");
+        }
     }
     return l;
 }

@@ -70,3 +70,28 @@ def test_clear_with_as_many_experts_as_there_can_be():
     rows = torch.full((600, 8), 7.0, device=DEV)
     layer.loco_experts_clear(rows, offsets)
     assert not rows[:2].any() and (rows[2:514] == 7.0).all() and not rows[514:].any()
+
+
+def _lists():
+    x = torch.full((64,), 2.0, device=DEV)
+    a, b = torch.ones(40, device=DEV), torch.ones(40, device=DEV)
+    return {"swapped": ([a, b], [b, a]), "one in the other": ([x[:20], x[20:40]], [torch.empty(20, device=DEV), x[:20]]),
+            "half of its own": ([x[:40]], [x[20:60]]), "ahead of its own": ([x[20:60]], [x[:40]]), "the last element": ([a, x[:25]], [x[24:], b[:25]]),
+            "inside a larger one": ([x, a[:3]], [torch.empty(64, device=DEV), x[30:33]])}
+
+
+@pytest.mark.parametrize("name", ["swapped", "one in the other", "half of its own", "ahead of its own", "the last element", "inside a larger one"])
+def test_an_output_in_another_gradient_is_refused(name):
+    gradients, outputs = _lists()[name]
+    squares = torch.full((1,), 1e6, dtype=torch.float64, device=DEV)
+    kept, before = [t.clone() for t in gradients], layer.loco_layer_launch_count()
+    with pytest.raises(ValueError, match="overlap"):
+        layer.loco_gradient_clip(gradients, outputs, squares, None, 1.0)
+    assert layer.loco_layer_launch_count() == before and all(torch.equal(a, b) for a, b in zip(gradients, kept))
+
+
+def test_outputs_beside_gradients_are_taken():
+    x = torch.full((64,), 2.0, device=DEV)
+    squares = torch.full((1,), 16.0, dtype=torch.float64, device=DEV)
+    layer.loco_gradient_clip([x[:16], x[16:32], x[5:5]], [x[32:48], x[16:32], x[40:40]], squares, None, 1.0)
+    assert x.tolist() == [2.0] * 16 + [0.5] * 32 + [2.0] * 16
