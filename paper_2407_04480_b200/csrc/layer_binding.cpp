@@ -494,9 +494,16 @@ int gradient_clip(PyObject *const *a) {
         PyErr_Clear();
         refuse("max_norm must be a number");
     }
-    return loco_gradient_clip(l.spans.data(), small(static_cast<int64_t>(l.spans.size()), "list"),
-                              static_cast<const double *>(flat(a[2], {1}, ScalarType::Double, l.device, "squares")), most,
-                              static_cast<float *>(flat(a[3], {1}, ScalarType::Float, l.device, "norm")), stream_of(a[5], l.device));
+    const int rc = loco_gradient_clip(l.spans.data(), small(static_cast<int64_t>(l.spans.size()), "list"),
+                                      static_cast<const double *>(flat(a[2], {1}, ScalarType::Double, l.device, "squares")), most,
+                                      static_cast<float *>(flat(a[3], {1}, ScalarType::Float, l.device, "norm")), stream_of(a[5], l.device));
+    // A graph that kept one of them has to notice, as it does after torch's own operations in place.
+    if (rc == LOCO_OK)
+        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(a[1]); ++i) {
+            const at::Tensor &y = THPVariable_Unpack(PySequence_Fast_GET_ITEM(a[1], i));
+            if (!y.is_inference()) y.unsafeGetTensorImpl()->bump_version();
+        }
+    return rc;
 }
 
 template <int (*kCall)(PyObject *const *), int kArgs> PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {

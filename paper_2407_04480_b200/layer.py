@@ -310,7 +310,8 @@ def loco_gradient_squares(gradients, squares, work, stream=None) -> None:
 def loco_gradient_clip(gradients, outputs, squares, norm, max_norm: float, stream=None) -> None:
     """outputs = gradients times max_norm / sqrt(squares) where that is below one; norm (fp32 [1], or None) = sqrt(squares).
 
-    An output may be its gradient itself; where nothing is to be scaled nothing is written to it then."""
+    An output may be its gradient itself; where nothing is to be scaled nothing is written to it then.  Autograd takes the outputs as
+    changed, as after an operation of torch's in place."""
     _check(_binding().gradient_clip(gradients, outputs, squares, norm, max_norm, _raw(stream)), "loco_gradient_clip")
 
 

@@ -95,3 +95,22 @@ def test_outputs_beside_gradients_are_taken():
     squares = torch.full((1,), 16.0, dtype=torch.float64, device=DEV)
     layer.loco_gradient_clip([x[:16], x[16:32], x[5:5]], [x[32:48], x[16:32], x[40:40]], squares, None, 1.0)
     assert x.tolist() == [2.0] * 16 + [0.5] * 32 + [2.0] * 16
+
+
+def test_a_graph_notices_that_a_gradient_it_kept_has_been_clipped():
+    x = torch.full((9,), 3.0, device=DEV, requires_grad=True)
+    grad, = torch.autograd.grad((x ** 3).sum(), x, create_graph=True)
+    kept = grad * grad                               # its backward pass needs the gradient as it was
+    grad = grad.detach()
+    version = grad._version
+    norm = layer.clip_gradients([grad], 1.0)
+    assert grad._version > version and float(norm) == pytest.approx(81.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        kept.sum().backward()
+
+
+def test_gradients_without_a_version_are_clipped_all_the_same():
+    with torch.inference_mode():
+        grad = torch.full((4,), 2.0, device=DEV)
+        layer.clip_gradients([grad], 1.0)
+    assert grad.tolist() == [0.5] * 4
