@@ -29,6 +29,10 @@ constexpr int kProductThreads = 384;
 constexpr int kLoadWarp = 0, kIssueWarp = 1, kCleanWarp = 2, kFirstWriter = 4, kWriteWarps = 8;        // lanes of TMEM go by the warp's number modulo 4
 
 __device__ unsigned g_product_status;            // LOCO_LAYER_FLAG_*
+// At a block's end: whether one of its waits has run out.
+__device__ __forceinline__ void report(uint32_t failed) {
+    if (threadIdx.x == 0 && failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
+}
 
 struct ProductMaps { CUtensorMap a, b; };
 struct ProductParams {
@@ -392,7 +396,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     __syncthreads();
     fence_after();
     if (warp == kIssueWarp) tmem_free<kTmem>(tmem);
-    if (threadIdx.x == 0 && S.failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
+    report(S.failed);
 }
 
 // ---- two SMs to a tile -----------------------------------------------------------------------
@@ -633,7 +637,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_pair_kernel(const 
     cluster_sync();                              // neither block leaves while the other's products read it or its arrivals are under way
     fence_after();
     if (warp == kIssueWarp) tmem_free_pair<512>(tmem);
-    if (threadIdx.x == 0 && S.failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
+    report(S.failed);
 }
 
 // ---- several SMs to the contraction of a tile -------------------------------------------------
@@ -779,7 +783,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_split_kernel(const
     }
     __syncwarp();
     cluster_sync();                              // no block leaves while another reads its sums
-    if (threadIdx.x == 0 && S.failed) atomicOr(&g_product_status, LOCO_LAYER_FLAG_TIMEOUT);
+    report(S.failed);
 }
 
 namespace {

@@ -1,11 +1,15 @@
 """Norm, sorted experts, their products and the clipped gradient where their ranges end: tiny values, offsets of every kind, lists that
 overlap.  Tolerances count roundings, as in test_gpu_layer_experts.py."""
+import ctypes
 import math
+import os
+import subprocess
 
 import pytest
 import torch
 
-from paper_2407_04480_b200 import layer, loco
+from paper_2407_04480_b200 import build as loco_build
+from paper_2407_04480_b200 import layer
 from tests import experts_reference as ref
 from tests.test_gpu_layer_experts import BF, DEV, E4M3, F32, NORM_ADDITIONS, STEP, gen, normal, within
 
@@ -114,3 +118,22 @@ def test_gradients_without_a_version_are_clipped_all_the_same():
         grad = torch.full((4,), 2.0, device=DEV)
         layer.clip_gradients([grad], 1.0)
     assert grad.tolist() == [0.5] * 4
+
+
+def test_a_wait_of_the_product_kernels_that_runs_out_raises_the_flag(tmp_path):
+    """Built into a library of its own, with the attention kernels', so that the flags of the one in use stay as they are."""
+    here, lib = os.path.dirname(os.path.abspath(__file__)), str(tmp_path / "wait.so")
+    subprocess.check_call([loco_build.nvcc_path(), *loco_build.NVCC_FLAGS, "-shared", "-cudart", "static", "-o", lib,
+                           os.path.join(here, "product_wait.cu"), os.path.join(here, "attention_wait.cu")])
+    L = ctypes.CDLL(lib)
+    L.run_product_wait.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p]
+    L.loco_layer_status.argtypes = [ctypes.POINTER(ctypes.c_uint32), ctypes.c_void_p]
+    ns, flags, stream = torch.zeros(3, dtype=torch.int64, device=DEV), ctypes.c_uint32(7), torch.cuda.current_stream().cuda_stream
+    assert L.loco_layer_status(ctypes.byref(flags), stream) == 0 and flags.value == 0
+    assert L.run_product_wait(ns.data_ptr(), 100, stream) == 0
+    torch.cuda.synchronize()
+    out, after, word = ns.tolist()
+    assert 20_000_000 <= out < 1_000_000_000 and word == 1
+    assert after < 2_000_000_000, "a hundred waits after it take less together than the limit of one"
+    assert L.loco_layer_status(ctypes.byref(flags), stream) == 0 and flags.value == layer.FLAG_TIMEOUT
+    assert layer.loco_layer_status() == 0
