@@ -180,23 +180,24 @@ template <typename T, int V> __global__ void __launch_bounds__(kMoveThreads) exp
     for (int c = s.lane * V; c < P.dim; c += P.team * V) {
         const Vec v = *reinterpret_cast<const Vec *>(x + c);
         for (int j = 0; j < P.top_k; ++j) {
-            const int p = __ldg(place + j);
+            const int p = place[j];
             if (p >= 0 && p < P.row_count) *reinterpret_cast<Vec *>(static_cast<T *>(P.rows_out) + p * P.rows_out_stride + c) = v;
         }
     }
 }
 
 // The choices j0 .. j0 + kRows - 1 of a token: their rows (-1: none) and weights.  Read again where they are needed again, from
-// L1: kept for all choices they cost the registers that keep enough threads at work (six choices: 46 us against 30).
+// L1: kept for all choices they cost the registers that keep enough threads at work (six choices: 46 us against 30).  By ordinary loads: the launch
+// before, which may have written them, need not have ended when this one starts, so that they are not constant over its lifetime.
 template <int kRows> __device__ __forceinline__ void choices_at(const MoveParams &P, int64_t token, int j0, int (&p)[kRows], float (&w)[kRows]) {
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
         p[j] = -1;
         w[j] = 0.0f;
         if (j0 + j < P.top_k) {
-            const int at = __ldg(P.place + token * P.top_k + j0 + j);
+            const int at = P.place[token * P.top_k + j0 + j];
             p[j] = at < P.row_count ? at : -1;
-            w[j] = P.weight ? __ldg(P.weight + token * P.top_k + j0 + j) : 1.0f;
+            w[j] = P.weight ? P.weight[token * P.top_k + j0 + j] : 1.0f;
         }
     }
 }
@@ -420,7 +421,7 @@ template <typename T> __global__ void __launch_bounds__(kMoveThreads) experts_di
     const Slide<T> x = slide<T>(P.in, s.token, P.in_stride, P.tokens, P.dim);
     const int step = P.team * kV;
     for (int j = 0; j < P.top_k; ++j) {
-        const int p = __ldg(P.place + s.token * P.top_k + j);
+        const int p = P.place[s.token * P.top_k + j];
         if (p < 0 || p >= P.row_count) continue;
         T *const row = static_cast<T *>(P.rows_out) + p * P.rows_out_stride;
         for (int c0 = s.lane * kV - shift_of(row); c0 < P.dim; c0 += 2 * step) {
@@ -455,11 +456,18 @@ template <typename T, int kRows> __global__ void __launch_bounds__(kMoveThreads,
         for (int j0 = 0; j0 < P.top_k; j0 += kRows) {
             int p[kRows];
             float w[kRows];
-            choices_at<kRows>(P, s.token, j0, p, w);
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                p[j] = j0 + j < P.top_k ? P.place[s.token * P.top_k + j0 + j] : -1;
+                if (p[j] >= P.row_count) p[j] = -1;
+            }
             typename Slide<T>::Two t[kRows];
 #pragma unroll
             for (int j = 0; j < kRows; ++j)
                 if (p[j] >= 0) t[j] = slide<T>(P.rows, p[j], P.rows_stride, P.row_count, P.dim).ask(at);
+#pragma unroll
+            for (int j = 0; j < kRows; ++j)                              // behind what takes longer: 9000 x 1367, six choices, 55 us against 70
+                w[j] = j0 + j >= P.top_k ? 0.0f : P.weight ? P.weight[s.token * P.top_k + j0 + j] : 1.0f;
 #pragma unroll
             for (int j = 0; j < kRows; ++j)
                 if (p[j] >= 0) {
@@ -488,10 +496,10 @@ template <typename T> __global__ void __launch_bounds__(kMoveThreads, 4) experts
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, width = P.team < 32 ? P.team : 32, step = P.team * kV;
 #pragma unroll 1
     for (int j = 0; j < P.top_k; ++j) {
-        const int place = there ? __ldg(P.place + token * P.top_k + j) : -1, p = place < P.row_count ? place : -1;
+        const int place = there ? P.place[token * P.top_k + j] : -1, p = place < P.row_count ? place : -1;
         float dot = 0.0f;
         if (p >= 0) {
-            const float w = __ldg(P.weight + token * P.top_k + j);
+            const float w = P.weight[token * P.top_k + j];
             const Slide<T> r = slide<T>(P.rows, p, P.rows_stride, P.row_count, P.dim);
             T *const row = static_cast<T *>(P.rows_out) + p * P.rows_out_stride;
 #pragma unroll 1

@@ -47,16 +47,17 @@ struct RotaryParams {
 
 constexpr int kRotaryThreads = 256;
 
+// By ordinary loads: the launch before, which may have written the table, need not have ended when this one starts.
 template <int N> __device__ __forceinline__ void load_floats(const float *p, float *out) {
     if constexpr (N % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            const float4 f = __ldg(reinterpret_cast<const float4 *>(p) + i);
+            const float4 f = reinterpret_cast<const float4 *>(p)[i];
             out[4 * i] = f.x; out[4 * i + 1] = f.y; out[4 * i + 2] = f.z; out[4 * i + 3] = f.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) out[i] = __ldg(p + i);
+        for (int i = 0; i < N; ++i) out[i] = p[i];
     }
 }
 

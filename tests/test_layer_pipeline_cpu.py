@@ -144,3 +144,11 @@ def test_the_cleaning_warp_waits_only_where_the_products_wait_for_it():
     ragged = issue[issue.index("if (left < kStep) {"):]
     ragged = ragged[:ragged.index("} else {")]
     assert "S.edge[slot]" in ragged and "S.clean[slot]" in ragged and "S.full[slot]" not in ragged
+
+
+def test_no_kernel_takes_memory_for_constant_that_the_launch_before_may_write():
+    """A load through the path for constants promises that nothing writes the place while the kernel lives; kernels here start under
+    the launch before theirs."""
+    for name in os.listdir(CSRC):
+        if name.startswith("layer_") and name.endswith((".cu", ".cuh", ".h")):
+            assert not re.search(r"__ldg\(|ld\.global(\.\w+)*\.nc|__restrict__", open(os.path.join(CSRC, name)).read()), name
