@@ -469,6 +469,8 @@ def norm(x, weight=None, residual=None, eps: float = 1e-5):
     """Root-mean-square norm of x [..., dim], times weight [dim]; with a residual (norm of x + residual, x + residual as it is kept).
 
     Differentiable once."""
+    if residual is not None and residual.shape != x.shape and residual.numel() == x.numel() and residual.shape[-1] == x.shape[-1]:
+        residual = residual.reshape(x.shape)         # other leading dimensions, which its gradient has to have again
     y, total = _Norm.apply(x, residual, weight, eps)
     return y if residual is None else (y, total)
 
@@ -508,9 +510,9 @@ class _Dispatch(torch.autograd.Function):
 
 
 def dispatch(x, place, offsets):
-    """The tokens x [tokens, dim] in the order of experts_sort's (offsets, place): [tokens * top_k, dim], zeros in rows that no
-    choice has.  Differentiable once."""
-    return _Dispatch.apply(x, place, offsets)
+    """The tokens x [tokens, dim] (or [..., dim]) in the order of experts_sort's (offsets, place): [tokens * top_k, dim], zeros in rows
+    that no choice has.  Differentiable once."""
+    return _Dispatch.apply(x.flatten(0, -2) if x.dim() > 2 else x, place, offsets)
 
 
 class _Combine(torch.autograd.Function):
@@ -541,7 +543,7 @@ def combine(rows, place, offsets, weight=None):
     """The experts' rows summed back to their tokens, with the choices' weights (fp32 [tokens, top_k]; None: ones).
 
     Differentiable once."""
-    return _Combine.apply(rows, place, offsets, weight)
+    return _Combine.apply(rows.flatten(0, -2) if rows.dim() > 2 else rows, place, offsets, weight)
 
 
 class _Product(torch.autograd.Function):
