@@ -51,9 +51,10 @@ def norm(x: torch.Tensor) -> torch.Tensor:
 
 
 def sorted_experts(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, index: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
-    """experts() without a look at the counts on the host: the tokens sorted by expert, one product for all of them."""
+    """experts() without a look at the counts on the host: the tokens sorted by expert, one product for all of them.  The matrices are
+    w["w1"] and w["w2"], [experts, in, out] at any distance, or are put together of each expert's own."""
     offsets, place = layer.experts_sort(index, shape.experts)
-    w1, w2 = (torch.stack([w["%s.%d" % (n, e)] for e in range(shape.experts)]) for n in ("w1", "w2"))
+    w1, w2 = (w[n] if n in w else torch.stack([w["%s.%d" % (n, e)] for e in range(shape.experts)]) for n in ("w1", "w2"))
     a, b = layer.experts_product(layer.dispatch(x, place, offsets), w1, offsets).chunk(2, -1)
     return layer.combine(layer.experts_product(torch.nn.functional.silu(a) * b, w2, offsets), place, offsets, weight)
 
@@ -67,6 +68,18 @@ def experts(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, index: to
             out = (torch.nn.functional.silu(a) * b) @ w["w2.%d" % e]
             y = y.index_add(0, token, out * weight[token, place, None].to(out.dtype))
     return y
+
+
+def views(shape: Shape, flat: torch.Tensor) -> Dict[str, torch.Tensor]:
+    """The parameters where they lie in the flat weights, the experts' matrices together.  Split, not sliced: the gradient of a split is
+    put together once, that of every slice is as large as all weights."""
+    sizes = shape.parameters()
+    dense = [n for n in sizes if "." not in n]               # they come first
+    parts = flat.split([sizes[n][0] * sizes[n][1] for n in dense] + [sum(a * b for n, (a, b) in sizes.items() if "." in n)])
+    w = {n: t.view(sizes[n]) for n, t in zip(dense, parts)}
+    (a1, b1), (a2, b2) = sizes["w1.0"], sizes["w2.0"]
+    w1, w2 = parts[-1].view(shape.experts, a1 * b1 + a2 * b2).split((a1 * b1, a2 * b2), 1)
+    return {**w, "w1": w1.unflatten(1, (a1, b1)), "w2": w2.unflatten(1, (a2, b2))}
 
 
 def forward(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, table: torch.Tensor, router: layer.Router, work: torch.Tensor):
@@ -105,12 +118,8 @@ def run(shape: Shape = Shape(), steps: int = 8, workers: int = 2, batch: int = 2
         total, idle = 0.0, 0
         for rank in range(workers):
             flat = theta.to(torch.bfloat16).requires_grad_()          # the weights every worker computes with
-            parts, at = {}, 0
-            for name, (a, b) in sizes.items():
-                parts[name] = flat[at:at + a * b].view(a, b)
-                at += a * b
             x = inputs[rank]
-            y, counts, losses = forward(shape, parts, x, table, router, work)
+            y, counts, losses = forward(shape, views(shape, flat), x, table, router, work)
             target = x + torch.tanh(x.cumsum(1) / (torch.arange(seq, device="cuda") + 1.0).sqrt()[:, None].to(x.dtype) @ turn)
             loss = (y.float() - target.float()).square().mean() + losses.sum()
             grad, = torch.autograd.grad(loss, flat)
