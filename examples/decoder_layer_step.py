@@ -50,6 +50,11 @@ def norm(x: torch.Tensor) -> torch.Tensor:
     return (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-5)).to(x.dtype)
 
 
+def products_take(shape: Shape) -> bool:
+    """Whether the experts' widths and number are those that layer.experts_product takes; others go expert by expert."""
+    return shape.d_model % 8 == 0 and shape.d_ffn % 8 == 0 and shape.experts <= 512
+
+
 def sorted_experts(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, index: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
     """experts() without a look at the counts on the host: the tokens sorted by expert, one product for all of them.  The matrices are
     w["w1"] and w["w2"], [experts, in, out] at any distance, or are put together of each expert's own."""
@@ -79,7 +84,10 @@ def views(shape: Shape, flat: torch.Tensor) -> Dict[str, torch.Tensor]:
     w = {n: t.view(sizes[n]) for n, t in zip(dense, parts)}
     (a1, b1), (a2, b2) = sizes["w1.0"], sizes["w2.0"]
     w1, w2 = parts[-1].view(shape.experts, a1 * b1 + a2 * b2).split((a1 * b1, a2 * b2), 1)
-    return {**w, "w1": w1.unflatten(1, (a1, b1)), "w2": w2.unflatten(1, (a2, b2))}
+    w1, w2 = w1.unflatten(1, (a1, b1)), w2.unflatten(1, (a2, b2))
+    if products_take(shape):
+        return {**w, "w1": w1, "w2": w2}
+    return {**w, **{"%s.%d" % (n, e): m[e] for n, m in (("w1", w1), ("w2", w2)) for e in range(shape.experts)}}
 
 
 def forward(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, table: torch.Tensor, router: layer.Router, work: torch.Tensor):
@@ -92,7 +100,8 @@ def forward(shape: Shape, w: Dict[str, torch.Tensor], x: torch.Tensor, table: to
     h, x = layer.norm(o.flatten(2) @ w["out"], residual=x)
     h = h.flatten(0, 1)
     index, weight, counts, _, losses = layer.router(h @ w["router"], router, work=work)
-    return x + sorted_experts(shape, w, h, index, weight).view_as(x), counts, losses
+    mixture = sorted_experts if products_take(shape) else experts
+    return x + mixture(shape, w, h, index, weight).view_as(x), counts, losses
 
 
 def run(shape: Shape = Shape(), steps: int = 8, workers: int = 2, batch: int = 2, seq: int = 320, seed: int = 0,
