@@ -11,7 +11,7 @@ import torch
 from paper_2407_04480_b200 import build as loco_build
 from paper_2407_04480_b200 import layer
 from tests import experts_reference as ref
-from tests.test_gpu_layer_experts import BF, DEV, E4M3, F32, NORM_ADDITIONS, STEP, gen, normal, within
+from tests.test_gpu_layer_experts import BF, DEV, E4M3, F32, NORM_ADDITIONS, STEP, gen, normal, offsets_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -136,4 +136,59 @@ def test_a_wait_of_the_product_kernels_that_runs_out_raises_the_flag(tmp_path):
     assert 20_000_000 <= out < 1_000_000_000 and word == 1
     assert after < 2_000_000_000, "a hundred waits after it take less together than the limit of one"
     assert L.loco_layer_status(ctypes.byref(flags), stream) == 0 and flags.value == layer.FLAG_TIMEOUT
+    assert layer.loco_layer_status() == 0
+
+
+SKEWED = [([1200 if e == 20 else 4 + e % 3 for e in range(64)], 264, 520), ([0] * 100 + [1500] + [1] * 27, 520, 136), ([3000 if e == 0 else 0 for e in range(160)], 200, 72),
+          ([2, 700, 1, 1], 1032, 264), ([5000] + [20] * 7, 264, 1000)]
+
+
+@pytest.mark.parametrize("loads,d_in,d_out", SKEWED, ids=lambda v: "most %d" % max(v) if isinstance(v, list) else str(v))
+@pytest.mark.parametrize("transposed", [False, True])
+def test_products_of_one_expert_with_most_of_the_rows(loads, d_in, d_out, transposed):
+    """The tiles' height goes by the average load, which says little here."""
+    g = gen(sum(loads))
+    n, e = sum(loads), len(loads)
+    offsets = offsets_of(loads)
+    x, b = normal(g, n, d_in), normal(g, n, d_out)
+    w = normal(g, e, d_out, d_in) if transposed else normal(g, e, d_in, d_out)
+    y, dw = torch.full((n, d_out), 7.0, dtype=BF, device=DEV), torch.full((e, d_in, d_out), 7.0, dtype=BF, device=DEV)
+    layer.loco_experts_product(x, w, offsets, y, transposed=transposed)
+    want, terms, _ = ref.product(x, w, offsets, transposed)
+    within(y, want, terms, 2 * d_in, BF)
+    layer.loco_experts_product_weights(x, b, offsets, dw)
+    want, terms = ref.product_weights(x, b, offsets)
+    within(dw, want, terms, 2 * max(loads) + 2, BF)
+    assert layer.loco_layer_status() == 0
+
+
+@pytest.mark.parametrize("loads,d_in,d_out", [([3, 0, 5], 4096, 1024), ([1] * 8, 1024, 2048), ([33, 129, 1, 65, 127], 1000, 776), ([700, 61, 1000, 0, 130], 520, 1000), ([64] * 30, 264, 264),
+                                              ([127] * 40, 264, 520)])
+def test_products_repeat_bit_for_bit_beside_other_work(loads, d_in, d_out):
+    """The same inputs again, with another stream at the memory and calls close behind one another: every copy and product that an output
+    depends on is waited for, or some repeat would differ."""
+    g = gen(3)
+    n, e = sum(loads), len(loads)
+    offsets = offsets_of(loads)
+    x, dy, w = normal(g, n, d_in), normal(g, n, d_out), normal(g, e, d_in, d_out)
+    y, dx, dw = normal(g, n, d_out), torch.empty_like(x), torch.empty_like(w)
+
+    def run():
+        layer.loco_experts_product(x, w, offsets, y)
+        layer.loco_experts_product(dy, w, offsets, dx, transposed=True)
+        layer.loco_experts_product_weights(x, dy, offsets, dw)
+    run()
+    want = [t.clone() for t in (y, dx, dw)]
+    junk, side = torch.zeros(1 << 26, dtype=torch.uint8, device=DEV), torch.cuda.Stream()
+    for i in range(30):
+        for t in (y, dx, dw):
+            t.fill_(float(i))
+        if i % 3:
+            with torch.cuda.stream(side):
+                for _ in range(8):
+                    junk.add_(1)
+        for _ in range(1 + i % 3):
+            run()
+        assert all(torch.equal(a, b) for a, b in zip((y, dx, dw), want)), i
+    side.synchronize()
     assert layer.loco_layer_status() == 0
