@@ -222,7 +222,8 @@ int loco_norm_backward(const loco_norm_t *cfg, int64_t rows, const loco_rows_t *
  *   combine     y[t] = sum_j weight[t, j] rows[place[t, j]]     (no weight: 1; no choice: nothing)
  * Dispatch's gradient is combine without weights, combine's without weights is dispatch.  With weights:
  *   drows[place[t, j]] = weight[t, j] dy[t]      dweight[t, j] = dy[t] . rows[place[t, j]]   (0 where there is no choice)
- * Rows that no choice has are not written; a place outside the rows is none.  Sums in fp32, in the order of the slots.
+ * Rows that no choice has are not written; a place outside the rows is none.  Sums in fp32, in the order of the slots; dweight's in fp32 too,
+ * at most max(64, dim / 64) products one after the other, then some ten sums of those.  No output may overlap an input.
  */
 
 /* Device workspace of loco_experts_sort for any number of tokens (0 for a bad number of experts). */
@@ -273,7 +274,8 @@ typedef struct {
  * sums.  The gradient of x is the same call on dy with `transposed` the other way round (d_in and d_out change places).
  * d_offsets: int32 [experts + 1], ascending; they are read on the device, as the largest so far and within the rows.  Rows outside every expert
  * are neither read as numbers nor written.  A NaN or infinity in a row or matrix reaches that row's or expert's outputs only.
- * One launch.  Errors: ARG, ALIGN (a pointer not 16-byte aligned or a stride not a multiple of 8 elements), UNSUPPORTED, CUDA.
+ * y may not overlap x or the matrices.  One launch.  Errors: ARG, ALIGN (a pointer not 16-byte aligned or a stride not a multiple of 8
+ * elements), UNSUPPORTED, CUDA.
  */
 int loco_experts_product(const loco_product_t *cfg, const loco_rows_t *x, const loco_matrices_t *w, const int32_t *d_offsets,
                          const loco_rows_t *y, void *stream);
@@ -285,9 +287,11 @@ int loco_experts_product_weights(const loco_product_t *cfg, const loco_rows_t *a
                                  const loco_matrices_t *dw, void *stream);
 
 /* ---- gradient ------------------------------------------------------------------------------
- * Of a list of gradients g:   squares = sum over all elements of g^2 (64 bits),   norm = sqrt(squares),
+ * Of a list of gradients g:   squares = sum over all elements of g^2,   norm = sqrt(squares),
  *   out = c g  with  c = max_norm / norm where norm > max_norm, else 1   (a norm that is infinite: c = 0; NaN: c = NaN)
- * Between the two calls the squares of the ranks that hold the other shards can be added.
+ * Between the two calls the squares of the ranks that hold the other shards can be added.  Groups of 32 squares (fp32 gradients: 16) are added
+ * in fp32, six roundings in a row at most, and the groups in 64 bits: squares is off by at most 6 * 2^-24 of itself.  A group that leaves
+ * fp32's range is squared and added in 64 bits.
  */
 typedef struct {
     const void *x;           /* n elements, any alignment to their own size                                       */
@@ -304,8 +308,8 @@ uint64_t loco_gradient_squares_workspace_bytes(void);
  * One launch for every 768 spans.  Errors: ARG, ALIGN, SIZE, CUDA. */
 int loco_gradient_squares(const loco_span_t *spans, int32_t count, double *d_squares, void *d_work, uint64_t d_work_bytes, void *stream);
 
-/* d_norm: one fp32, or NULL.  max_norm >= 0.  No output may overlap another, or another's gradient.  Where c is 1 nothing is written to a y that is x.  One launch for every 768
- * spans.  Errors: ARG, ALIGN, CUDA. */
+/* d_norm: one fp32, or NULL.  max_norm >= 0.  No output may overlap another, another's gradient, or its own unless it is that.  Where c is 1
+ * nothing is written to a y that is x.  One launch for every 768 spans.  Errors: ARG, ALIGN, CUDA. */
 int loco_gradient_clip(const loco_span_t *spans, int32_t count, const double *d_squares, double max_norm, float *d_norm, void *stream);
 
 /*

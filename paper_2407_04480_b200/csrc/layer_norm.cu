@@ -8,7 +8,7 @@
 // backward kernel spilled what it waited for: 8192 rows of 4096, bfloat16, 99 us.
 //
 // bfloat16 with residual, 16384 x 5120: 105 us, 6.4 TB/s; 300,000 x 128: 50 us, 6.1 TB/s; 50,003 x 1367, whose rows begin anywhere,
-// 109 us, 5.0 TB/s; 16384 x 4096 to 8 bits 97 us, 4.9 TB/s: there the instructions bound it, some thirty for two elements.  Backward 8192 x 4096:
+// 109 us, 5.0 TB/s; 16384 x 4096 to 8 bits 96 us, 4.9 TB/s: there the instructions bound it, some thirty for two elements.  Backward 8192 x 4096:
 // 45 us, 6.0 TB/s, and 6 for the sum of the blocks' parts of dw; 20,000 x 4096 in fp32 193 us, 6.8 TB/s.
 #include <cuda_fp8.h>
 

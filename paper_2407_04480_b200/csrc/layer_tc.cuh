@@ -1,5 +1,5 @@
-// Thin wrappers over the sm_100a instructions of the attention kernels: mbarriers, tensor copies, tensor-core products
-// with their accumulators in tensor memory.  Every wait is bounded.
+// Thin wrappers over the sm_100a instructions of the attention and product kernels: mbarriers, tensor copies, tensor-core products
+// with their accumulators in tensor memory, and small arithmetic that the other kernels use too.  Every wait is bounded.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>

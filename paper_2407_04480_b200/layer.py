@@ -2,9 +2,9 @@
 
 The functions named loco_* have the name of the C entry point they call and only marshal arguments (in the native module
 _layer_binding, csrc/layer_binding.cpp): every tensor, outputs included, is the caller's, nothing is allocated and nothing
-synchronises.  `rotary`, `attention` and `router` wrap them as torch.autograd functions that allocate their results.  All
-arithmetic runs in the CUDA kernels of libloco_layer_b200.so; there is no CPU fallback: if the library cannot be loaded, the
-first call raises.
+synchronises.  `rotary`, `attention`, `router`, `norm`, `dispatch`, `combine` and `experts_product` wrap them as torch.autograd
+functions that allocate their results, `experts_sort` and `clip_gradients` as plain ones.  All arithmetic runs in the CUDA kernels of
+libloco_layer_b200.so; there is no CPU fallback: if the library cannot be loaded, the first call raises.
 """
 from __future__ import annotations
 
@@ -119,7 +119,7 @@ def loco_layer_launch_count() -> int:
 def loco_layer_status(stream=None) -> int:
     """Flags raised on the current device since the library was loaded; synchronises the stream.
 
-    FLAG_TIMEOUT: a wait in an attention kernel ran out and that call's outputs are meaningless.  Nothing else reads the
+    FLAG_TIMEOUT: a wait in an attention or product kernel ran out and that call's outputs are meaningless.  Nothing else reads the
     flag: a program asks where it synchronises anyway, once a step or a checkpoint."""
     flags = C.c_uint32(0)
     _check(lib().loco_layer_status(C.byref(flags), (torch.cuda.current_stream() if stream is None else stream).cuda_stream),
@@ -301,7 +301,7 @@ def loco_gradient_squares_workspace_bytes() -> int:
 
 
 def loco_gradient_squares(gradients, squares, work, stream=None) -> None:
-    """squares (fp64 [1]) = the sum of squares over a list of contiguous gradients (bfloat16 or fp32, of any shapes).
+    """squares (fp64 [1]) = the sum of squares over a list of contiguous gradients (bfloat16 or fp32, of any shapes), within 6 * 2^-24.
 
     work: a CUDA tensor of loco_gradient_squares_workspace_bytes() bytes, zero before its first use."""
     _check(_binding().gradient_squares(gradients, squares, work, _raw(stream)), "loco_gradient_squares")

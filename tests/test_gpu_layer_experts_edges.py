@@ -192,3 +192,16 @@ def test_products_repeat_bit_for_bit_beside_other_work(loads, d_in, d_out):
         assert all(torch.equal(a, b) for a, b in zip((y, dx, dw), want)), i
     side.synchronize()
     assert layer.loco_layer_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [1, 32, 1000, 65_537, 4_000_001])
+def test_squares_are_within_six_roundings(n, dtype):
+    """bfloat16: a product of two is exact in fp32; three sums of a vector's pairs, one of the two halves, two of four vectors: six in a row.
+    fp32: a product, a fused sum, the halves, four vectors: five.  All terms are positive, so that the bounds of the roundings add up to
+    that of the sum; what comes in 64 bits after them is below 2^-40."""
+    x = normal(gen(n), n, dtype=dtype, sigma=1e-3)
+    squares, work = torch.empty(1, dtype=torch.float64, device=DEV), torch.zeros(layer.loco_gradient_squares_workspace_bytes(), dtype=torch.uint8, device=DEV)
+    layer.loco_gradient_squares([x], squares, work)
+    total = ref.squares([x])
+    assert abs(float(squares) - total) <= (6 if dtype == BF else 5) * 1.00001 * STEP * total
