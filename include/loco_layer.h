@@ -251,10 +251,13 @@ int loco_experts_combine(const loco_experts_t *cfg, const loco_rows_t *rows, con
 int loco_experts_combine_backward(const loco_experts_t *cfg, const loco_rows_t *dy, const loco_rows_t *rows, const int32_t *d_place,
                                   const float *d_weight, const loco_rows_t *drows, float *d_dweight, void *stream);
 
-/* Zeros in the rows of [rows, dim] that no expert has (d_offsets: int32 [experts + 1], read as loco_experts_product does: those ahead of
- * offsets[0] and those from the largest offset on), which the calls here leave as they were: for what goes on with all rows.  One
- * launch.  Errors: ARG, ALIGN, CUDA. */
+/* Zeros in rows [rows, dim] from offsets[experts] on (d_offsets: int32 [experts + 1]), which the calls here leave as they were: for
+ * what goes on with all rows.  One launch.  Errors: ARG, ALIGN, CUDA. */
 int loco_experts_clear(int32_t dtype, int32_t dim, int64_t rows_count, const loco_rows_t *rows, int32_t experts, const int32_t *d_offsets, void *stream);
+
+/* The same for all rows that no expert has, the offsets being read as loco_experts_product reads them: those ahead of offsets[0] too, and
+ * those from the largest offset on. */
+int loco_experts_clear_others(int32_t dtype, int32_t dim, int64_t rows_count, const loco_rows_t *rows, int32_t experts, const int32_t *d_offsets, void *stream);
 
 /* The experts' matrices, [experts, first, second]: element (e, i, j) at ptr + e*expert_stride + i*row_stride + j. */
 typedef struct {

@@ -389,14 +389,15 @@ int experts_combine_backward(PyObject *const *a) {
 }
 
 // rows, offsets, stream
-int experts_clear(PyObject *const *a) {
+template <int (*kCall)(int32_t, int32_t, int64_t, const loco_rows_t *, int32_t, const int32_t *, void *)> int clear(PyObject *const *a) {
     const at::Tensor &rows = rows_of(a[0], "rows");
     const int device = device_of(rows);
     const int64_t e = need(a[1], "offsets").numel() - 1;
     const loco_rows_t r = matrix(rows, rows.size(0), rows.size(1), rows.scalar_type(), device, "rows");
-    return loco_experts_clear(dtype_of(rows), small(rows.size(1), "dim"), rows.size(0), &r, small(e, "experts"),
-                              static_cast<const int32_t *>(flat(a[1], {e + 1}, ScalarType::Int, device, "offsets")), stream_of(a[2], device));
+    return kCall(dtype_of(rows), small(rows.size(1), "dim"), rows.size(0), &r, small(e, "experts"),
+                 static_cast<const int32_t *>(flat(a[1], {e + 1}, ScalarType::Int, device, "offsets")), stream_of(a[2], device));
 }
+constexpr auto experts_clear = clear<loco_experts_clear>, experts_clear_others = clear<loco_experts_clear_others>;
 
 // [experts, rows, columns] bfloat16, the columns contiguous.
 loco_matrices_t matrices(const at::Tensor &t, at::IntArrayRef shape, int device, const char *what) {
@@ -524,7 +525,7 @@ template <int (*kCall)(PyObject *const *), int kArgs> PyObject *entry(PyObject *
 #define LOCO_ENTRY(name, args) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(entry<name, args>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LOCO_ENTRY(rotary_apply, 9), LOCO_ENTRY(attention_forward, 14), LOCO_ENTRY(attention_backward, 19),
                          LOCO_ENTRY(router_forward, 14), LOCO_ENTRY(router_backward, 13), LOCO_ENTRY(norm_forward, 9), LOCO_ENTRY(norm_backward, 9),
-                         LOCO_ENTRY(experts_sort, 5), LOCO_ENTRY(experts_clear, 3), LOCO_ENTRY(experts_dispatch, 4), LOCO_ENTRY(experts_combine, 5), LOCO_ENTRY(experts_combine_backward, 7),
+                         LOCO_ENTRY(experts_sort, 5), LOCO_ENTRY(experts_clear, 3), LOCO_ENTRY(experts_clear_others, 3), LOCO_ENTRY(experts_dispatch, 4), LOCO_ENTRY(experts_combine, 5), LOCO_ENTRY(experts_combine_backward, 7),
                          LOCO_ENTRY(experts_product, 6), LOCO_ENTRY(experts_product_weights, 5), LOCO_ENTRY(gradient_squares, 4), LOCO_ENTRY(gradient_clip, 6), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layer_binding", LOCO_BUILT_FOR, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

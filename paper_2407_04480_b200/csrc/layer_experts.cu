@@ -547,15 +547,20 @@ template <typename T> __global__ void __launch_bounds__(kMoveThreads, 4) experts
     }
 }
 
-// Rows of no expert: ahead of the first offset, and from the largest on, which is how the products read them.  Nothing to write, as a rule.
-template <typename T>
+// Rows from the last offset on, or (kOthers) all that no expert has as the products read the offsets: ahead of the first, and from the
+// largest on.  Nothing to write, as a rule.
+template <typename T, bool kOthers>
 __global__ void __launch_bounds__(kMoveThreads) experts_clear_kernel(T *rows, int64_t stride, int64_t count, int dim, const int32_t *offsets, int experts) {
     wait_for_previous();
     let_next_start();
-    int end = 0;
-    for (int e = threadIdx.x % 32; e <= experts; e += 32) end = max(end, offsets[e]);
-    end = __reduce_max_sync(kAll, end);
-    const int64_t ahead = min(static_cast<int64_t>(max(offsets[0], 0)), count), none = ahead + max(count - end, static_cast<int64_t>(0));
+    int64_t ahead = 0;
+    int end = kOthers ? 0 : max(offsets[experts], 0);
+    if constexpr (kOthers) {
+        for (int e = threadIdx.x % 32; e <= experts; e += 32) end = max(end, offsets[e]);
+        end = __reduce_max_sync(kAll, end);
+        ahead = min(static_cast<int64_t>(max(offsets[0], 0)), count);
+    }
+    const int64_t none = ahead + max(count - end, static_cast<int64_t>(0));
     for (int64_t i = blockIdx.x; i < none; i += gridDim.x) {
         T *const row = rows + (i < ahead ? i : i - ahead + end) * stride;
         for (int c = threadIdx.x; c < dim; c += kMoveThreads) row[c] = from_f32<T>(0.0f);
@@ -642,6 +647,24 @@ int launch_move(Move m, MoveParams &P, const loco_experts_t *c, const Vectors &V
     return launch_kernel(fn, dim3(static_cast<unsigned>(blocks)), kMoveThreads, 0, stream, P);
 }
 
+template <bool kOthers> int clear(int32_t dtype, int32_t dim, int64_t rows_count, const loco_rows_t *rows, int32_t experts, const int32_t *d_offsets, void *stream) {
+    const loco_experts_t c{dtype, dim, 1, 0, rows_count};
+    int rc = check_experts(&c);
+    if (rc != LOCO_OK) return rc;
+    if (experts < 1 || experts > kMostExperts || !d_offsets) return LOCO_ERR_ARG;
+    Vectors V;
+    int64_t stride;
+    if ((rc = take_rows(&c, rows, rows_count, true, V, stride)) != LOCO_OK) return rc;
+    if (!aligned(d_offsets, 4)) return LOCO_ERR_ALIGN;
+    if (rows_count == 0) return LOCO_OK;
+    const int sms = sm_count();
+    if (sms == 0) return LOCO_ERR_CUDA;
+    const dim3 grid(static_cast<unsigned>(rows_count < sms * 4 ? rows_count : sms * 4));
+    if (dtype == LOCO_BF16)
+        return launch_kernel(experts_clear_kernel<__nv_bfloat16, kOthers>, grid, kMoveThreads, 0, stream, static_cast<__nv_bfloat16 *>(rows->ptr), stride, rows_count, dim, d_offsets, experts);
+    return launch_kernel(experts_clear_kernel<float, kOthers>, grid, kMoveThreads, 0, stream, static_cast<float *>(rows->ptr), stride, rows_count, dim, d_offsets, experts);
+}
+
 int start(const loco_experts_t *c, const int32_t *place, const float *weight) {
     const int rc = check_experts(c);
     if (rc != LOCO_OK || c->tokens == 0) return rc;
@@ -686,21 +709,11 @@ int loco_experts_sort(int32_t experts, int64_t tokens, int32_t top_k, const int3
 }
 
 int loco_experts_clear(int32_t dtype, int32_t dim, int64_t rows_count, const loco_rows_t *rows, int32_t experts, const int32_t *d_offsets, void *stream) {
-    const loco_experts_t c{dtype, dim, 1, 0, rows_count};
-    int rc = check_experts(&c);
-    if (rc != LOCO_OK) return rc;
-    if (experts < 1 || experts > kMostExperts || !d_offsets) return LOCO_ERR_ARG;
-    Vectors V;
-    int64_t stride;
-    if ((rc = take_rows(&c, rows, rows_count, true, V, stride)) != LOCO_OK) return rc;
-    if (!aligned(d_offsets, 4)) return LOCO_ERR_ALIGN;
-    if (rows_count == 0) return LOCO_OK;
-    const int sms = sm_count();
-    if (sms == 0) return LOCO_ERR_CUDA;
-    const dim3 grid(static_cast<unsigned>(rows_count < sms * 4 ? rows_count : sms * 4));
-    if (dtype == LOCO_BF16)
-        return launch_kernel(experts_clear_kernel<__nv_bfloat16>, grid, kMoveThreads, 0, stream, static_cast<__nv_bfloat16 *>(rows->ptr), stride, rows_count, dim, d_offsets, experts);
-    return launch_kernel(experts_clear_kernel<float>, grid, kMoveThreads, 0, stream, static_cast<float *>(rows->ptr), stride, rows_count, dim, d_offsets, experts);
+    return clear<false>(dtype, dim, rows_count, rows, experts, d_offsets, stream);
+}
+
+int loco_experts_clear_others(int32_t dtype, int32_t dim, int64_t rows_count, const loco_rows_t *rows, int32_t experts, const int32_t *d_offsets, void *stream) {
+    return clear<true>(dtype, dim, rows_count, rows, experts, d_offsets, stream);
 }
 
 int loco_experts_dispatch(const loco_experts_t *c, const loco_rows_t *x, const int32_t *d_place, const loco_rows_t *rows, void *stream) {

@@ -29,7 +29,7 @@ SCALINGS = {"plain": ROTARY_PLAIN, "linear": ROTARY_LINEAR, "parts": ROTARY_PART
 EXPORTS = ("loco_rotary_table", "loco_rotary_apply", "loco_attention_forward", "loco_attention_backward",
            "loco_attention_backward_workspace_bytes", "loco_router_workspace_bytes", "loco_router_forward",
            "loco_router_backward", "loco_norm_forward", "loco_norm_backward", "loco_norm_backward_workspace_bytes",
-           "loco_experts_sort", "loco_experts_sort_workspace_bytes", "loco_experts_clear", "loco_experts_dispatch", "loco_experts_combine",
+           "loco_experts_sort", "loco_experts_sort_workspace_bytes", "loco_experts_clear", "loco_experts_clear_others", "loco_experts_dispatch", "loco_experts_combine",
            "loco_experts_combine_backward", "loco_experts_product", "loco_experts_product_weights", "loco_gradient_squares",
            "loco_gradient_squares_workspace_bytes", "loco_gradient_clip", "loco_layer_status", "loco_layer_launch_count")
 FLAG_TIMEOUT = 1
@@ -72,7 +72,7 @@ def lib() -> C.CDLL:
         L.loco_norm_backward_workspace_bytes.argtypes = [st]
         L.loco_experts_sort.argtypes = [i32, i64, i32, vp, vp, vp, vp, u64, vp]
         L.loco_experts_sort_workspace_bytes.argtypes = [i32]
-        L.loco_experts_clear.argtypes = [i32, i32, i64, st, i32, vp, vp]
+        L.loco_experts_clear.argtypes = L.loco_experts_clear_others.argtypes = [i32, i32, i64, st, i32, vp, vp]
         L.loco_experts_dispatch.argtypes = [st, st, vp, st, vp]
         L.loco_experts_combine.argtypes = [st, st, vp, vp, st, vp]
         L.loco_experts_combine_backward.argtypes = [st, st, st, vp, vp, st, vp, vp]
@@ -276,9 +276,14 @@ def loco_experts_combine_backward(dy, rows, place, weight, drows, dweight, strea
 
 
 def loco_experts_clear(rows, offsets, stream=None) -> None:
-    """Zeros in the rows of [rows, dim] that no expert has: ahead of offsets[0], and from the largest offset on.  The other calls leave
-    them as they are."""
+    """Zeros in rows [rows, dim] from offsets[experts] on, which the other calls leave as they are."""
     _check(_binding().experts_clear(rows, offsets, _raw(stream)), "loco_experts_clear")
+
+
+def loco_experts_clear_others(rows, offsets, stream=None) -> None:
+    """Zeros in all rows of [rows, dim] that no expert has as loco_experts_product reads the offsets: ahead of offsets[0] too, and from
+    the largest offset on."""
+    _check(_binding().experts_clear_others(rows, offsets, _raw(stream)), "loco_experts_clear_others")
 
 
 def loco_experts_product(x, w, offsets, y, transposed: bool = False, stream=None) -> None:
@@ -487,8 +492,9 @@ def experts_sort(index, experts: int, work: Optional[torch.Tensor] = None):
     return offsets, place
 
 
-def _cleared(rows, offsets):
-    loco_experts_clear(rows, offsets)
+def _cleared(rows, offsets, others: bool = False):
+    """`others`: where the offsets may be a caller's own.  Rows on the host are those of a stand-in for the kernels, whose offsets begin with 0."""
+    (loco_experts_clear_others if others and rows.is_cuda else loco_experts_clear)(rows, offsets)
     return rows
 
 
@@ -553,7 +559,7 @@ class _Product(torch.autograd.Function):
         loco_experts_product(x, w, offsets, y, transposed=transposed)
         ctx.save_for_backward(x, w, offsets)
         ctx.transposed = transposed
-        return _cleared(y, offsets)
+        return _cleared(y, offsets, others=True)
 
     @staticmethod
     def backward(ctx, dy):
@@ -565,7 +571,7 @@ class _Product(torch.autograd.Function):
             if ctx.needs_input_grad[0]:
                 dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
                 loco_experts_product(dy, w, offsets, dx, transposed=not ctx.transposed)
-                _cleared(dx, offsets)
+                _cleared(dx, offsets, others=True)
             if ctx.needs_input_grad[1]:
                 dw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
                 loco_experts_product_weights(*((dy, x) if ctx.transposed else (x, dy)), offsets, dw)

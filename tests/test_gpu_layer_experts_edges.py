@@ -58,21 +58,23 @@ def test_rows_of_no_expert_are_zeros_in_the_differentiable_product(offsets):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("offsets", OFFSETS, ids=str)
-def test_clear_zeroes_the_rows_of_no_expert_and_no_others(offsets, dtype):
-    space = torch.full((40, 75), 7.0, dtype=dtype, device=DEV)
-    rows = space[:, 1:74]
+def test_clear_others_zeroes_the_rows_of_no_expert_and_clear_those_from_the_last_offset_on(offsets, dtype):
+    """The latter leaves alone what lies ahead: the rows of the experts before, where the offsets are a part of longer ones."""
     o = torch.tensor(offsets, dtype=torch.int32, device=DEV)
-    layer.loco_experts_clear(rows, o)
-    live = torch.zeros(40, dtype=torch.bool)
+    others, behind = torch.ones(40, dtype=torch.bool), torch.arange(40) >= max(offsets[-1], 0)
     for a, b in ref.spans(o, 40):
-        live[a:b] = True
-    assert (rows[live] == 7.0).all() and not rows[~live].any() and (space[:, 0] == 7.0).all() and (space[:, 74] == 7.0).all()
+        others[a:b] = False
+    for call, zeros in ((layer.loco_experts_clear_others, others), (layer.loco_experts_clear, behind)):
+        space = torch.full((40, 75), 7.0, dtype=dtype, device=DEV)
+        rows = space[:, 1:74]
+        call(rows, o)
+        assert (rows[~zeros] == 7.0).all() and not rows[zeros].any() and (space[:, 0] == 7.0).all() and (space[:, 74] == 7.0).all()
 
 
-def test_clear_with_as_many_experts_as_there_can_be():
+def test_clear_others_with_as_many_experts_as_there_can_be():
     offsets = torch.arange(2, 515, dtype=torch.int32, device=DEV)     # 512 rows from the second on
     rows = torch.full((600, 8), 7.0, device=DEV)
-    layer.loco_experts_clear(rows, offsets)
+    layer.loco_experts_clear_others(rows, offsets)
     assert not rows[:2].any() and (rows[2:514] == 7.0).all() and not rows[514:].any()
 
 

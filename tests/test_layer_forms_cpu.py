@@ -31,3 +31,14 @@ def test_tokens_with_leading_dimensions_are_laid_out_and_have_their_gradient(ker
     assert dx.shape == x.shape and torch.equal(dx.reshape(4, -1), torch.stack([dy[2], dy[0], torch.zeros_like(dy[0]), dy[1]]))
     back = layer.combine(rows.detach().view(shape).requires_grad_(), place, offsets)
     assert torch.equal(back.detach()[[0, 1, 3]], flat[[0, 1, 3]]) and not back[2].any()
+
+
+def test_clearing_the_rows_of_no_expert_refuses_what_clearing_those_behind_the_last_does():
+    from paper_2407_04480_b200 import loco
+    from tests.test_layer_experts_cpu import PTR, rows
+    layer.lib()
+    for call in (layer.lib().loco_experts_clear, layer.lib().loco_experts_clear_others):
+        clear = lambda dtype=loco.BF16, d=64, n=4, r=rows(), e=8, o=PTR: call(dtype, d, n, r, e, o, None)
+        for bad in (dict(dtype=2), dict(d=0), dict(n=-1), dict(r=None), dict(r=rows(stride=0)), dict(e=0), dict(e=513), dict(o=None)):
+            assert clear(**bad) == loco.ERR_ARG, bad
+        assert clear(o=PTR + 2) == loco.ERR_ALIGN and clear(r=rows(ptr=PTR + 1)) == loco.ERR_ALIGN and clear(n=0, r=rows(ptr=0)) == loco.OK
