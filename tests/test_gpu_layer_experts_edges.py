@@ -207,3 +207,31 @@ def test_squares_are_within_six_roundings(n, dtype):
     layer.loco_gradient_squares([x], squares, work)
     total = ref.squares([x])
     assert abs(float(squares) - total) <= (6 if dtype == BF else 5) * 1.00001 * STEP * total
+
+
+def test_products_whose_contraction_is_shared_run_two_at_once_and_captured():
+    """Few tiles: clusters of blocks share each, and leave their sums to one another.  On two streams at once, from a first call inside a
+    capture, and replayed on other inputs."""
+    given = [(normal(gen(s), 8, 4096), normal(gen(s + 1), 3, 4096, 1024)) for s in (61, 63)]
+    offsets = offsets_of([3, 0, 5])
+    outs = [[torch.empty(8, 1024, dtype=BF, device=DEV) for _ in range(20)] for _ in range(2)]
+    graph, held = torch.cuda.CUDAGraph(), torch.empty(8, 1024, dtype=BF, device=DEV)
+    x, w = (t.clone() for t in given[0])
+    with torch.cuda.graph(graph):
+        layer.loco_experts_product(x, w, offsets, held)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s, (a, b), out in zip(streams, given, outs):
+            with torch.cuda.stream(s):
+                layer.loco_experts_product(a, b, offsets, out[i])
+    torch.cuda.synchronize()
+    for (a, b), out in zip(given, outs):
+        want, terms, _ = ref.product(a, b, offsets, False)
+        within(out[0], want, terms, 2 * 4096, BF)
+        assert all(torch.equal(out[0], o) for o in out)
+        x.copy_(a), w.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, out[0])
+    assert layer.loco_layer_status() == 0
