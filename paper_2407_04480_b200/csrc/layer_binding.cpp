@@ -489,12 +489,12 @@ int gradient_squares(PyObject *const *a) {
 
 // gradients, outputs, squares, norm, max_norm, stream
 int gradient_clip(PyObject *const *a) {
-    const List l = list_of(a[0], a[1], a[2]);
-    const double most = PyFloat_AsDouble(a[4]);
+    const double most = PyFloat_AsDouble(a[4]);      // ahead of the lists, which its conversion could change
     if (most == -1.0 && PyErr_Occurred()) {
         PyErr_Clear();
         refuse("max_norm must be a number");
     }
+    const List l = list_of(a[0], a[1], a[2]);
     const int rc = loco_gradient_clip(l.spans.data(), small(static_cast<int64_t>(l.spans.size()), "list"),
                                       static_cast<const double *>(flat(a[2], {1}, ScalarType::Double, l.device, "squares")), most,
                                       static_cast<float *>(flat(a[3], {1}, ScalarType::Float, l.device, "norm")), stream_of(a[5], l.device));

@@ -235,3 +235,18 @@ def test_products_whose_contraction_is_shared_run_two_at_once_and_captured():
         torch.cuda.synchronize()
         assert torch.equal(held, out[0])
     assert layer.loco_layer_status() == 0
+
+
+def test_a_largest_norm_whose_conversion_changes_the_list():
+    """The list is read after it: a number may be any object that converts to one."""
+    gradients = [torch.full((4,), 2.0, device=DEV), torch.full((4,), 2.0, device=DEV)]
+    outputs = [torch.empty(4, device=DEV), torch.empty(4, device=DEV)]
+
+    class Limit:
+        def __float__(self):
+            gradients[1] = outputs[1] = None
+            return 1.0
+    before = layer.loco_layer_launch_count()
+    with pytest.raises(ValueError, match="missing"):
+        layer.loco_gradient_clip(gradients, outputs, torch.full((1,), 16.0, dtype=torch.float64, device=DEV), None, Limit())
+    assert layer.loco_layer_launch_count() == before
